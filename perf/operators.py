@@ -151,10 +151,11 @@ def prepare(case, seed):
     if case["kind"] == "matvec":
         n, k, b, group = case["n"], case["k"], case["b"], case["group"]
         # Normalised weights are spread normally over +-1: the codes of a codebook fitted to them crowd in the middle.
-        codes = (torch.randn(n, k + k % 2, generator=gen, device="cuda") * 2.6 + 8.0).clamp_(0, 15).to(torch.uint8)
-        if k % 2:
-            codes[:, k] = 0
-        codes = codes[:, 0::2] | (codes[:, 1::2] << 4)
+        wide = -(-k // 128) * 128
+        idx = (torch.randn(n, wide, generator=gen, device="cuda") * 2.6 + 8.0).clamp_(0, 15).to(torch.uint8)
+        idx[:, k:] = 0
+        # Blocks of 128 columns, sixteen words of eight codes each, the words of a block stored as a transposed 4 x 4 square.
+        codes = (idx[:, 0::2] | (idx[:, 1::2] << 4)).view(n, wide // 128, 4, 4, 4).transpose(2, 3).reshape(n, wide // 2)
         levels = torch.linspace(-1, 1, 16, device="cuda") ** 3 * 0.6 + torch.linspace(-0.4, 0.4, 16, device="cuda")
         scales = (torch.rand(n, -(-k // group), generator=gen, device="cuda") + 0.5) / math.sqrt(k)
         x = torch.randn(b, k, generator=gen, device="cuda")
@@ -204,7 +205,8 @@ def _unpack(codes, k):
 def _plain_matvec(s):
     case = s["case"]
     k, group = case["k"], case["group"]
-    w = s["levels"].float()[_unpack(s["codes"], k)]
+    codes = s["codes"].view(case["n"], -1, 4, 4, 4).transpose(2, 3).flatten(1)
+    w = s["levels"].float()[_unpack(codes, k)]
     w = w * s["scales"].float().repeat_interleave(group, dim=1)[:, :k]
     return (s["x"].float() @ w.T).to(s["x"].dtype)
 
@@ -291,11 +293,12 @@ def _exact_matvec(s, case):
     """Column by column of the batch, the scales folded into the activations of each group."""
     n, k, b, group = case["n"], case["k"], case["b"], case["group"]
     y = torch.zeros(b, n, dtype=torch.float64, device="cuda")
+    col = torch.arange(k, device="cuda")
+    word = col % 128 // 8
+    byte = col // 128 * 64 + (word % 4 * 4 + word // 4) * 4 + col % 8 // 2
     for at in range(0, n, 4096):
-        c = s["codes"][at:at + 4096]
-        w = torch.empty(c.shape[0], 2 * c.shape[1], dtype=torch.float64, device="cuda")
-        w[:, 0::2] = s["levels"].double()[(c % 16).int()]
-        w[:, 1::2] = s["levels"].double()[(c // 16).int()]
+        c = s["codes"][at:at + 4096][:, byte].int() // torch.where(col % 2 == 1, 16, 1).int() % 16
+        w = s["levels"].double()[c]
         for i in range(-(-k // group)):
             part = slice(i * group, min(k, (i + 1) * group))
             y[:, at:at + 4096] += s["x"][:, part].double() @ w[:, part].T * s["scales"][at:at + 4096, i].double()
