@@ -384,6 +384,122 @@ size_t ecasq_workspace_size_prep(int64_t d);
 int ecasq_prepare(const float *x, int64_t d, void *ws, size_t ws_bytes, float *v, int64_t *w, int64_t *N,
                   double *S, double *S2, int64_t *p_out, ecasq_stream_t stream);
 
+/* ---------------------------------------------------------------- 4-bit codes
+ * What reads and writes codes of at most 16 levels: products with a coded weight
+ * matrix, attention over a paged key-value cache whose rows may be coded, and the
+ * encode of new cache rows.  These calls neither synchronise nor use host memory
+ * after they return, so a graph can capture them; device-side findings go to a
+ * sticky status word of the caller's (`status`, one int32, may be NULL): bits of
+ * ECASQ_BAD_* are or-ed into it and never cleared.
+ * Element types: */
+#define ECASQ_F32 0  /* fp32 */
+#define ECASQ_F16 1  /* IEEE binary16 */
+#define ECASQ_BF16 2 /* bfloat16 */
+/* bits of a status word */
+#define ECASQ_BAD_PAGE 1   /* a page number outside [0, pages) (its keys are left out) or a slot beyond the cache (its row is dropped) */
+#define ECASQ_BAD_LENGTH 2 /* a sequence longer than max_len (cut to it) */
+#define ECASQ_BAD_COUNT 4  /* a codebook's m outside [1, s] (clamped) */
+#define ECASQ_BAD_VALUE 8  /* a cache row with NaN or Inf (NaN takes code 0, Inf an end of the codebook) */
+
+/* Indices of ecasq_quantize (one byte each, < 16; only the low four bits are read)
+ * as the packed rows that ecasq_matvec reads.  Row r of `codes` has
+ * 64 * ceil(k / 128) bytes: 64 bytes for each block of 128 columns, which hold
+ * sixteen 32-bit little-endian words of eight codes, word w the columns 8w .. 8w+7
+ * of the block with the lowest column in the lowest four bits; word w is stored as
+ * word 4 (w mod 4) + w div 4 of the block.  Columns beyond k are zero.
+ *   idx   device [n rows of idx_row bytes], codes device [n rows of code_row bytes]
+ * ECASQ_EINVAL for n or k < 1, rows shorter than their contents, code_row not a
+ * multiple of 16 or codes not 16-byte aligned. */
+int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_t *codes, int64_t code_row,
+               ecasq_stream_t stream);
+
+/* y = x W^T for W [n, k] of 4-bit codes with one codebook and group scales:
+ *   y[i, r] = sum_c x[i, c] scales[r, c div group] levels[code[r, c]].
+ * Products and sums are fp32; y is rounded once, to x's type.
+ *   x       device [b rows of x_row elements], of `type`; b >= 0 (weights are read once
+ *           for each eight rows of x)
+ *   codes   device, rows of code_row bytes as ecasq_pack writes them, 16-byte aligned
+ *   levels  device [m], m <= 16, of `type`, finite; a code >= m stands for 0.  A codebook that
+ *           a solve found for 16-bit values holds such values (Q is a subset of X),
+ *           so the type loses nothing
+ *   scales  device [n rows of scale_row elements], ceil(k / group) a row, of
+ *           scale_type: `type` or ECASQ_F32
+ *   group   a multiple of 32; one >= k means one scale a row
+ *   y       device [b rows of y_row elements], of `type`, output
+ * ECASQ_EINVAL for n or k < 1, b < 0, m outside [1, 16], a bad type, group or
+ * alignment. */
+int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
+                 const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
+                 int64_t k, int32_t group, void *y, int64_t y_row, ecasq_stream_t stream);
+
+/* One side (the keys or the values) of a paged cache.  Slot t of a sequence is slot
+ * t mod page_size of its page t div page_size; a page has a row of d values for each
+ * head in each slot.  Plain rows (levels_n = 0) hold values of `type`.  Coded rows
+ * hold d / 2 bytes, entry 2i in the low four bits of byte i, and a codebook of
+ * levels_n = 8 or 16 levels of `type` (F16 or BF16) a row; entry e stands for
+ * levels[code e], codes are below levels_n.
+ * Strides are in elements of `type`, of the rows of codes in bytes; a row's own
+ * entries are contiguous.  Every row and codebook starts at a multiple of 16 bytes.
+ * d: plain F32 a multiple of 4, plain F16 and BF16 of 8, coded of 32; 256 at most. */
+typedef struct ecasq_cache {
+    void *rows;
+    void *levels;                              /* NULL for plain rows */
+    int64_t row_page, row_slot, row_head;
+    int64_t level_page, level_slot, level_head;
+    int64_t pages;
+    int32_t page_size;
+    int32_t heads;
+    int32_t d;
+    int32_t type;
+    int32_t levels_n;
+    int32_t reserved;
+} ecasq_cache_t;
+
+/* Encodes the rows x [n, heads, d] of n new slots into a coded cache, each with its
+ * own codebook, by the unbiased rounding of ecasq_quantize (Sec. 2).
+ * Row (i, h): its levels are r_j = Q[j] rounded to the cache's type for j < m and
+ * r_j = r_{m-1} beyond.  Entry e with a = max{r_j <= x, j < m} (r_0 if there is none)
+ * keeps a's code if it equals a or a is the last; otherwise it takes the next one iff
+ * fl32(fl32(k 2^-24) fl32(b - a)) < fl32(x - a), k = top 24 bits of SplitMix64(seed +
+ * (c+1) 0x9E3779B97F4A7C15), c = (i heads + h) d + e: ecasq_quantize's rule and counter
+ * over the flat x, so a codebook that the rounding leaves as it is gives its indices.
+ * An entry outside the codebook's range takes the nearer end.
+ *   x      device, of x_type (F32, or the cache's type), strides in elements, entries
+ *          contiguous
+ *   Q      device fp32 [n * heads, s], s <= levels_n: rows as ecasq_solve_batched
+ *          writes them for x seen as n * heads rows of d
+ *   m      device int32 [n * heads] or NULL (all s)
+ *   slots  device int64 [n]: page * page_size + slot; negative: the row is not
+ *          written.  Slots of one call are distinct.
+ * ECASQ_EINVAL for a plain cache, s outside [1, levels_n], n < 0 or a bad type. */
+int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, int64_t x_head, const float *Q,
+                      int32_t s, const int32_t *m, const int64_t *slots, const ecasq_cache_t *cache, uint64_t seed,
+                      int32_t *status, ecasq_stream_t stream);
+
+/* Attention of one new token a sequence over a paged cache.  For sequence i and
+ * query head h, which reads key head h div (heads / k->heads):
+ *   s_t = scale q . K_t,  out = sum_t softmax(s)_t V_t,  lse = log sum_t exp(s_t)
+ * over the keys t in [starts[i], lengths[i]); a sequence without keys gives out = 0 and
+ * lse = -inf, and so does one whose weights are all zero.  Scores, weights and sums are fp32;
+ * out is rounded once, to q's type.  Nothing outside that range is read, whatever it holds.
+ *   q        device [b, heads, d] of the cache's type, strides in elements, entries
+ *            contiguous; out likewise
+ *   k, v     host structs of one type, kind, d, heads, pages and page_size
+ *   table    device int32 [b rows of table_row entries]: page numbers, at least
+ *            ceil(max_len / page_size) a row
+ *   lengths  device int32 [b]; starts device int32 [b] or NULL (0)
+ *   max_len  host bound of the lengths; sizes the launch and the workspace
+ *   lse      device fp32 [b, heads] or NULL
+ * Workspace: ecasq_workspace_size_attend with the same sizes (0 bytes may be returned: ws
+ * may then be NULL).  Splits and sums do not depend on other sequences' lengths, and equal calls give equal bits.
+ * ECASQ_EINVAL for b or max_len < 0, heads not a multiple of k->heads, a cache
+ * outside the limits of ecasq_cache_t, or caches that differ. */
+size_t ecasq_workspace_size_attend(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len);
+int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_t heads, const ecasq_cache_t *k,
+                 const ecasq_cache_t *v, const int32_t *table, int64_t table_row, const int32_t *lengths,
+                 const int32_t *starts, int64_t max_len, float scale, void *out, int64_t out_row, int64_t out_head,
+                 float *lse, void *ws, size_t ws_bytes, int32_t *status, ecasq_stream_t stream);
+
 /* Kernels this library has launched in the calling process so far (all
  * threads, all entry points): a monotone counter for launch accounting. */
 int64_t ecasq_kernel_launches(void);

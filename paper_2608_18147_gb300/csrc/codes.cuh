@@ -1,0 +1,35 @@
+// codes.cuh -- element types and checks shared by the operators on 4-bit codes.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace ecasq {
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+static inline bool type_ok(int32_t t) { return t == ECASQ_F32 || t == ECASQ_F16 || t == ECASQ_BF16; }
+static inline int64_t type_size(int32_t t) { return t == ECASQ_F32 ? 4 : 2; }
+static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// The limits that ecasq_cache_t states; bytes of a row's entries and of its codebook.
+static inline bool cache_ok(const ecasq_cache_t *c) {
+    if (!c || !c->rows || !type_ok(c->type) || c->pages < 1 || c->page_size < 1 || c->heads < 1 || c->d < 1 || c->d > 256)
+        return false;
+    if (c->pages > INT64_MAX / c->page_size) return false;
+    const int64_t e = c->levels_n ? 1 : type_size(c->type);
+    if (!aligned16(c->rows) || c->row_page * e % 16 || c->row_slot * e % 16 || c->row_head * e % 16) return false;
+    if (!c->levels_n) return c->d * e % 16 == 0;
+    if ((c->levels_n != 8 && c->levels_n != 16) || c->type == ECASQ_F32 || c->d % 32 || !c->levels) return false;
+    return aligned16(c->levels) && c->level_page % 8 == 0 && c->level_slot % 8 == 0 && c->level_head % 8 == 0;
+}
+
+}  // namespace ecasq

@@ -17,6 +17,8 @@ import numpy as np
 from . import build as _build
 
 OK, EINVAL, ENONFINITE, EINFEASIBLE, EWORKSPACE, ECUDA, ETIMEOUT, ERANGE = 0, -1, -2, -3, -4, -5, -6, -7
+F32, F16, BF16 = 0, 1, 2  # element types of the operators on 4-bit codes
+BAD_PAGE, BAD_LENGTH, BAD_COUNT, BAD_VALUE = 1, 2, 4, 8  # bits of their status word
 EXACT_S, NO_REFINE_GUARD, DP_REFERENCE, TIME_KERNELS, EXACT_TABLES, RESIDENT_COSTS, STREAMED_COSTS = 1, 2, 4, 8, 16, 32, 64
 ONE_PART_PUBLISH = 128  # accepted, without effect
 UNSEEDED_SEARCH = 256  # fast DP search: no seeded tile skipping (same results)
@@ -61,6 +63,13 @@ class Timeshare(C.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class Cache(C.Structure):
+    _fields_ = [("rows", C.c_void_p), ("levels", C.c_void_p), ("row_page", C.c_int64), ("row_slot", C.c_int64),
+                ("row_head", C.c_int64), ("level_page", C.c_int64), ("level_slot", C.c_int64),
+                ("level_head", C.c_int64), ("pages", C.c_int64), ("page_size", C.c_int32), ("heads", C.c_int32),
+                ("d", C.c_int32), ("type", C.c_int32), ("levels_n", C.c_int32), ("reserved", C.c_int32)]
+
+
 class EcasqError(RuntimeError):
     def __init__(self, code, where):
         self.code = code
@@ -86,6 +95,7 @@ def lib():
         pi64 = C.POINTER(C.c_int64)
         PP = C.POINTER(Params)
         PR = C.POINTER(Result)
+        PC = C.POINTER(Cache)
         sig = {
             "ecasq_version": (C.c_int, []),
             "ecasq_strerror": (C.c_char_p, [C.c_int]),
@@ -110,6 +120,12 @@ def lib():
             "ecasq_quantize_noalloc": (C.c_int, [vp, i64, vp, i32, u64, vp, vp, pd, vp]),
             "ecasq_solve_batched": (C.c_int, [vp, i64, i64, PP, vp, sz, vp, vp, PR, vp]),
             "ecasq_prepare": (C.c_int, [vp, i64, vp, sz, vp, vp, vp, vp, vp, pi64, vp]),
+            "ecasq_pack": (C.c_int, [vp, i64, i64, i64, vp, i64, vp]),
+            "ecasq_matvec": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, vp, i64, vp]),
+            "ecasq_cache_write": (C.c_int, [vp, i32, i64, i64, i64, vp, i32, vp, vp, PC, u64, vp, vp]),
+            "ecasq_workspace_size_attend": (sz, [i64, i32, i32, i32, i64]),
+            "ecasq_attend": (C.c_int, [vp, i64, i64, i64, i32, PC, PC, vp, i64, vp, vp, i64, C.c_float, vp, i64, i64,
+                                       vp, vp, sz, vp, vp]),
             "ecasq_kernel_launches": (i64, []),
         }
         for name, (res, args) in sig.items():
@@ -130,7 +146,8 @@ def exported_symbols():
                  "ecasq_dp_pass",
                  "ecasq_dp_tables", "ecasq_workspace_size_linear", "ecasq_dp_linear", "ecasq_refine", "ecasq_evaluate", "ecasq_quantize", "ecasq_quantize_noalloc",
                  "ecasq_solve_batched",
-                 "ecasq_prepare", "ecasq_kernel_launches"):
+                 "ecasq_prepare", "ecasq_pack", "ecasq_matvec", "ecasq_cache_write", "ecasq_workspace_size_attend",
+                 "ecasq_attend", "ecasq_kernel_launches"):
         if hasattr(L, name):
             names.append(name)
     return names
@@ -536,6 +553,205 @@ def ecasq_prepare(x, ws=None):
     return dict(p=p, v=v[:p], w=w[:p], N=N[:p + 1], S_hi=S[:p + 1], S_lo=S[p + 1:2 * p + 2],
                 S2_hi=S2[:p + 1], S2_lo=S2[p + 1:2 * p + 2])
 
+
+# ------------------------------------------------------ operators on 4-bit codes
+
+_TYPES = {}
+
+
+def _types():
+    if not _TYPES:
+        torch = _torch()
+        _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    return _TYPES
+
+
+def _refuse(where, what):
+    raise EcasqError(EINVAL, "%s: %s" % (where, what))
+
+
+def _device_of(where, *tensors):
+    """The one CUDA device that the given tensors (None allowed) are on; it has to be the current one, whose
+    stream the call uses."""
+    torch = _torch()
+    at = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == at):
+            _refuse(where, "tensors must be on the current CUDA device")
+
+
+def _stream_of(device_index):
+    return _torch()._C._cuda_getCurrentRawStream(device_index)
+
+
+def _status_ptr(where, status):
+    if status is None:
+        return None
+    torch = _torch()
+    if status.dtype != torch.int32 or status.numel() < 1:
+        _refuse(where, "status must be an int32 tensor")
+    return status.data_ptr()
+
+
+def ecasq_pack(idx):
+    """Indices [n, k] (uint8, < 16) of a weight matrix as the packed rows that ecasq_matvec reads: uint8
+    [n, 64 ceil(k / 128)]."""
+    torch = _torch()
+    where = "ecasq_pack"
+    _device_of(where, idx)
+    if idx.dtype != torch.uint8 or idx.dim() != 2 or (idx.shape[1] > 1 and idx.stride(1) != 1):
+        _refuse(where, "idx must be uint8 [n, k] with contiguous rows")
+    n, k = idx.shape
+    codes = torch.empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=idx.device)
+    rc = lib().ecasq_pack(idx.data_ptr(), idx.stride(0) if n > 1 else k, n, k, codes.data_ptr(), codes.shape[1],
+                          _stream_of(idx.device.index))
+    _check(rc, where)
+    return codes
+
+
+def ecasq_matvec(x, codes, levels, scales, group, out=None):
+    """y = x W^T for the 4-bit matrix W[r, c] = scales[r, c // group] * levels[code[r, c]].
+
+    x [b, k] or [k] (float32, float16 or bfloat16), codes [n, 64 ceil(k / 128)] as ecasq_pack gives them,
+    levels [m <= 16] of x's type, scales [n, ceil(k / group)] of x's type or float32, group a multiple of 32.
+    Returns y [b, n] or [n] of x's type (`out` if given)."""
+    torch = _torch()
+    where = "ecasq_matvec"
+    _device_of(where, x, codes, levels, scales, out)
+    T = _types().get(x.dtype)
+    x2 = x if x.dim() == 2 else x.unsqueeze(0)
+    if T is None or x2.dim() != 2 or (x2.shape[1] > 1 and x2.stride(1) != 1):
+        _refuse(where, "x must be [b, k] or [k] of float32, float16 or bfloat16 with contiguous rows")
+    b, k = x2.shape
+    group = int(group)
+    if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.stride(1) != 1 or codes.shape[1] < 64 * -(-k // 128):
+        _refuse(where, "codes must be uint8 [n, 64 ceil(k / 128)] with contiguous rows")
+    n = codes.shape[0]
+    if levels.dtype != x.dtype or levels.dim() != 1 or not levels.is_contiguous() or not 1 <= levels.numel() <= 16:
+        _refuse(where, "levels must be 1 to 16 values of x's type")
+    if group < 32 or group % 32:
+        _refuse(where, "group must be a multiple of 32")
+    groups = -(-k // group)
+    if (scales.dtype not in (x.dtype, torch.float32) or scales.dim() != 2 or scales.shape[0] != n
+            or scales.shape[1] < groups or (groups > 1 and scales.stride(1) != 1)):
+        _refuse(where, "scales must be [n, ceil(k / group)] of x's type or float32 with contiguous rows")
+    if out is None:
+        y = torch.empty((b, n), dtype=x.dtype, device=x.device)
+    else:
+        y = out if out.dim() == 2 else out.unsqueeze(0)
+        if out.dtype != x.dtype or out.dim() != x.dim() or y.shape != (b, n) or (n > 1 and y.stride(1) != 1):
+            _refuse(where, "out must be [b, n] (or [n]) of x's type with contiguous rows")
+    rc = lib().ecasq_matvec(x2.data_ptr(), x2.stride(0), T, b, codes.data_ptr(), codes.stride(0) if n > 1 else codes.shape[1],
+                            levels.data_ptr(), levels.numel(), scales.data_ptr(),
+                            scales.stride(0) if n > 1 else scales.shape[1], _types()[scales.dtype], n, k, group,
+                            y.data_ptr(), y.stride(0), _stream_of(x.device.index))
+    _check(rc, where)
+    return out if out is not None else y if x.dim() == 2 else y[0]
+
+
+def _cache(where, rows, levels):
+    """The C view of one side of a paged cache: rows [pages, page_size, heads, d] (coded: [..., d / 2] uint8 with levels
+    [pages, page_size, heads, 8 or 16]); any strides, a row's entries contiguous."""
+    torch = _torch()
+    if rows.dim() != 4 or rows.stride(3) != 1:
+        _refuse(where, "cache rows must be [pages, page_size, heads, d] with contiguous entries")
+    pages, page_size, heads, d = rows.shape
+    rs = rows.stride()
+    if levels is None:
+        T = _types().get(rows.dtype)
+        if T is None:
+            _refuse(where, "plain cache rows must be float32, float16 or bfloat16")
+        return Cache(rows.data_ptr(), None, rs[0], rs[1], rs[2], 0, 0, 0, pages, page_size, heads, d, T, 0, 0)
+    if (rows.dtype != torch.uint8 or levels.dim() != 4 or levels.shape[:3] != rows.shape[:3] or levels.stride(3) != 1
+            or levels.dtype not in (torch.float16, torch.bfloat16) or levels.shape[3] not in (8, 16)):
+        _refuse(where, "a coded cache is uint8 [pages, page_size, heads, d / 2] with levels [pages, page_size, heads, "
+                       "8 or 16] of float16 or bfloat16")
+    ls = levels.stride()
+    return Cache(rows.data_ptr(), levels.data_ptr(), rs[0], rs[1], rs[2], ls[0], ls[1], ls[2], pages, page_size, heads,
+                 2 * d, _types()[levels.dtype], levels.shape[3], 0)
+
+
+def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
+    """Encodes new rows x [n, heads, d] into a coded cache, each with its own codebook, by the rounding of ecasq_quantize.
+
+    Q float32 [n * heads, s] or [n, heads, s] and m int32 [n * heads] (or None) as ecasq_solve_batched gives them,
+    slots int64 [n] (page * page_size + slot, negative: not written), codes uint8 [pages, page_size, heads, d / 2],
+    levels [pages, page_size, heads, 8 or 16] of float16 or bfloat16; x float32 or of levels' type.  status: int32
+    tensor that BAD_* bits are or-ed into.  Returns (codes, levels), written in place."""
+    torch = _torch()
+    where = "ecasq_cache_write"
+    _device_of(where, x, Q, m, slots, codes, levels, status)
+    c = _cache(where, codes, levels)
+    n = slots.numel()
+    if (x.dtype not in (torch.float32, levels.dtype) or x.dim() != 3 or x.shape != (n, c.heads, c.d)
+            or x.stride(2) != 1):
+        _refuse(where, "x must be [n, heads, d] of float32 or the cache's type with contiguous entries")
+    rows = n * c.heads
+    s = Q.shape[-1]
+    if Q.dtype != torch.float32 or not Q.is_contiguous() or Q.numel() != rows * s or not 1 <= s <= c.levels_n:
+        _refuse(where, "Q must be contiguous float32 [n * heads, s], s at most the cache's levels")
+    if m is not None and (m.dtype != torch.int32 or not m.is_contiguous() or m.numel() != rows):
+        _refuse(where, "m must be contiguous int32 [n * heads]")
+    if slots.dtype != torch.int64 or not slots.is_contiguous():
+        _refuse(where, "slots must be contiguous int64 [n]")
+    rc = lib().ecasq_cache_write(x.data_ptr(), _types()[x.dtype], n, x.stride(0), x.stride(1), Q.data_ptr(), s,
+                                 None if m is None else m.data_ptr(), slots.data_ptr(), C.byref(c),
+                                 int(seed) & 0xFFFFFFFFFFFFFFFF, _status_ptr(where, status),
+                                 _stream_of(x.device.index))
+    _check(rc, where)
+    return codes, levels
+
+
+def workspace_attend(b, heads, kv_heads, d, max_len):
+    """A device workspace for ecasq_attend with these sizes (it may be empty)."""
+    torch = _torch()
+    n = int(lib().ecasq_workspace_size_attend(int(b), int(heads), int(kv_heads), int(d), int(max_len)))
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None, v_levels=None, max_len=None, out=None,
+                 ws=None, status=None):
+    """Attention of one new token a sequence over a paged cache of plain or coded rows: (out, lse).
+
+    q [b, heads, d]; k, v [pages, page_size, kv_heads, d] of q's type, or uint8 [..., d / 2] with k_levels, v_levels
+    [..., 8 or 16] of q's type; table int32 [b, pages of a sequence]; lengths int32 [b], starts int32 [b] or None: the
+    keys [starts, lengths) are seen.  scale: 1 / sqrt(d) if None.  max_len: host bound of the lengths (None: what the table
+    holds).  status: int32 tensor that BAD_* bits are or-ed into.  out [b, heads, d] of q's type, lse float32 [b, heads]
+    (natural logarithm; -inf where no key is seen, with out = 0)."""
+    torch = _torch()
+    where = "ecasq_attend"
+    _device_of(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws, status)
+    if (k_levels is None) != (v_levels is None):
+        _refuse(where, "k and v must both be plain or both be coded")
+    ck, cv = _cache(where, k, k_levels), _cache(where, v, v_levels)
+    if q.dim() != 3 or q.stride(2) != 1 or _types().get(q.dtype) != ck.type or q.shape[2] != ck.d:
+        _refuse(where, "q must be [b, heads, d] of the cache's type and row length with contiguous entries")
+    b, heads, d = q.shape
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != b or (table.shape[1] > 1 and table.stride(1) != 1):
+        _refuse(where, "table must be int32 [b, pages of a sequence] with contiguous rows")
+    if lengths.dtype != torch.int32 or lengths.shape != (b,) or not lengths.is_contiguous():
+        _refuse(where, "lengths must be contiguous int32 [b]")
+    if starts is not None and (starts.dtype != torch.int32 or starts.shape != (b,) or not starts.is_contiguous()):
+        _refuse(where, "starts must be contiguous int32 [b]")
+    most = table.shape[1] * ck.page_size
+    max_len = most if max_len is None else int(max_len)
+    if max_len > most:
+        _refuse(where, "the table has too few pages for max_len")
+    if out is None:
+        out = torch.empty((b, heads, d), dtype=q.dtype, device=q.device)
+    elif out.dtype != q.dtype or out.shape != q.shape or out.stride(2) != 1:
+        _refuse(where, "out must be like q")
+    lse = torch.empty((b, heads), dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = workspace_attend(b, heads, ck.heads, d, max_len)
+    rc = lib().ecasq_attend(q.data_ptr(), q.stride(0), q.stride(1), b, heads, C.byref(ck), C.byref(cv), table.data_ptr(),
+                            table.stride(0) if b > 1 else table.shape[1], lengths.data_ptr(),
+                            None if starts is None else starts.data_ptr(), max_len,
+                            d ** -0.5 if scale is None else float(scale), out.data_ptr(), out.stride(0), out.stride(1),
+                            lse.data_ptr(), ws.data_ptr(), ws.numel(), _status_ptr(where, status),
+                            _stream_of(q.device.index))
+    _check(rc, where)
+    return out, lse
 
 def ecasq_kernel_launches() -> int:
     """Kernels the library has launched in this process so far."""
