@@ -492,8 +492,9 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
  *   lse      device fp32 [b, heads] or NULL
  * Workspace: ecasq_workspace_size_attend with the same sizes (0 bytes may be returned: ws
  * may then be NULL).  Splits and sums do not depend on other sequences' lengths, and equal calls give equal bits.
- * ECASQ_EINVAL for b or max_len < 0, heads not a multiple of k->heads, a cache
- * outside the limits of ecasq_cache_t, or caches that differ. */
+ * ECASQ_EINVAL for b outside [0, 65535], max_len outside [0, 2^30], heads not a multiple
+ * of k->heads or above 65535, a cache outside the limits of ecasq_cache_t, or caches that
+ * differ. */
 size_t ecasq_workspace_size_attend(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len);
 int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_t heads, const ecasq_cache_t *k,
                  const ecasq_cache_t *v, const int32_t *table, int64_t table_row, const int32_t *lengths,

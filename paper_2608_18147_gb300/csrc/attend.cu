@@ -1,84 +1,61 @@
-// attend.cu -- attention of one new token a sequence over a paged cache (ecasq_attend).
+// attend.cu -- ecasq_attend: checks, splits and the join of the splits' results.
 #include <algorithm>
 
-#include "codes.cuh"
+#include "attend.cuh"
 
 namespace ecasq {
 
-struct AttendArgs {
-    const void *q;
-    void *out;
-    const int32_t *table, *lengths, *starts;
-    float *lse;
-    int32_t *status;
-    ecasq_cache_t k, v;
-    int64_t q_row, q_head, out_row, out_head, table_row, max_len;
-    float scale;
-    int heads;
-};
+// Splits.  A block has a fixed cost of its own (its first loads' latency, the join), so a split should be long; and the
+// blocks should fill the card evenly.  kSlots blocks run at once; up to kLong keys for each of them there is
+// one round of blocks, beyond that as many rounds as keep a split at most about that long.
+constexpr int kSlots = 2 * 152, kLong = 1024, kStep = 64;
 
-template <typename T>
-__device__ __forceinline__ float entry(const ecasq_cache_t &c, int64_t page, int64_t slot, int64_t head, int e) {
-    if (!c.levels_n) return to_f32(static_cast<const T *>(c.rows)[page * c.row_page + slot * c.row_slot + head * c.row_head + e]);
-    const uint8_t byte = static_cast<const uint8_t *>(c.rows)[page * c.row_page + slot * c.row_slot + head * c.row_head + e / 2];
-    const T *levels = static_cast<const T *>(c.levels) + page * c.level_page + slot * c.level_slot + head * c.level_head;
-    return to_f32(levels[(e & 1 ? byte >> 4 : byte & 15) & (c.levels_n - 1)]);
+struct Splits {
+    int32_t chunk, count;
+};
+static Splits make_splits(int64_t b, int64_t blocks, int64_t max_len) {
+    const int64_t per = cdiv(b * blocks * max_len, kSlots);
+    const int64_t want = std::max<int64_t>(1, cdiv(per, cdiv(std::max<int64_t>(per, 1), kLong)));
+    // Splits count from the tile of the first key, so one more tile than max_len may be needed.
+    const int64_t span = max_len + kTile - 1;
+    const int64_t count = std::min<int64_t>(std::max<int64_t>(1, cdiv(span, cdiv(want, kStep) * kStep)), 65535);
+    const int64_t chunk = cdiv(cdiv(span, count), kStep) * kStep;
+    return {(int32_t)chunk, (int32_t)cdiv(span, chunk)};
 }
 
-// One block a sequence and query head, 128 keys at a time: a thread a key for the scores, a
-// thread two entries for the sums.
+// A block a sequence and query head: the splits' maxima and sums, then their entries.
 template <typename T>
-__global__ void __launch_bounds__(128) k_attend(AttendArgs a) {
-    __shared__ float q[256], p[128], red[4];
-    __shared__ int64_t pages[128];
+__global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendArgs a) {
+    __shared__ float red[8];
     const int64_t seq = blockIdx.y;
-    const int h = blockIdx.x, d = a.k.d, kh = h / (a.heads / a.k.heads), tid = threadIdx.x;
-    for (int e = tid; e < d; e += 128) q[e] = to_f32(static_cast<const T *>(a.q)[seq * a.q_row + h * a.q_head + e]);
-    int64_t end = a.lengths[seq], first = a.starts ? max(0, a.starts[seq]) : 0;
-    int bad = 0;
-    if (end > a.max_len) { end = a.max_len; bad = ECASQ_BAD_LENGTH; }
-    float top = -CUDART_INF_F, total = 0.f, acc[2] = {0.f, 0.f};
-    for (int64_t t0 = first; t0 < end; t0 += 128) {
-        const int64_t t = t0 + tid;
-        float s = -CUDART_INF_F;
-        __syncthreads();
-        pages[tid] = -1;
-        if (t < end) {
-            const int64_t page = a.table[seq * a.table_row + t / a.k.page_size];
-            if (page < 0 || page >= a.k.pages) bad |= ECASQ_BAD_PAGE;
-            else {
-                pages[tid] = page;
-                s = 0.f;
-                for (int e = 0; e < d; e++) s = fmaf(q[e], entry<T>(a.k, page, t % a.k.page_size, kh, e), s);
-                s *= a.scale;
-            }
-        }
-        float mx = s;
-        for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        if ((tid & 31) == 0) red[tid >> 5] = mx;
-        __syncthreads();
-        mx = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), top);
-        const float base = mx == -CUDART_INF_F ? 0.f : mx, shrink = expf(top - base);
-        p[tid] = expf(s - base);
-        __syncthreads();
-        total *= shrink;
-        acc[0] *= shrink;
-        acc[1] *= shrink;
-        top = mx;
-        for (int j = 0; j < 128 && t0 + j < end; j++) {
-            if (pages[j] < 0) continue;
-            total += p[j];
-            for (int u = 0; u < 2; u++)
-                if (tid + 128 * u < d)
-                    acc[u] = fmaf(p[j], entry<T>(a.v, pages[j], (t0 + j) % a.k.page_size, kh, tid + 128 * u), acc[u]);
-        }
+    const int h = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int n = max(splits_of(a, seq_span(a, seq)), 1);
+    const PartAt at(a.d);
+    const float *part = at.at(a.part, seq, a.heads, h, a.splits, 0);
+    float m = -CUDART_INF_F;
+    for (int i = threadIdx.x; i < n; i += 128) m = fmaxf(m, part[i * at.stride + a.d]);
+    for (int x = 16; x; x /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    if (lane == 0) red[wid] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float base = m == -CUDART_INF_F ? 0.f : m;
+    float l = 0.f;
+    for (int i = threadIdx.x; i < n; i += 128) l += part[i * at.stride + a.d + 1] * exp2_fast(part[i * at.stride + a.d] - base);
+    for (int x = 16; x; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (lane == 0) red[4 + wid] = l;
+    __syncthreads();
+    l = (red[4] + red[5]) + (red[6] + red[7]);
+    for (int e = threadIdx.x; e < a.d; e += 128) {
+        float x = 0.f;
+        for (int i = 0; i < n; i++) x = fmaf(part[i * at.stride + e], exp2_fast(part[i * at.stride + a.d] - base), x);
+        static_cast<T *>(a.out)[seq * a.out_row + h * a.out_head + e] = from_f32<T>(l == 0.f ? 0.f : x / l);
     }
-    for (int u = 0; u < 2; u++)
-        if (tid + 128 * u < d)
-            static_cast<T *>(a.out)[seq * a.out_row + h * a.out_head + tid + 128 * u] =
-                from_f32<T>(total == 0.f ? 0.f : acc[u] / total);
-    if (tid == 0 && a.lse) a.lse[seq * a.heads + h] = total == 0.f ? -CUDART_INF_F : top + logf(total);
-    if (bad && a.status) atomicOr(a.status, bad);
+    if (threadIdx.x == 0 && a.lse) a.lse[seq * a.heads + h] = l == 0.f ? -CUDART_INF_F : m * kLn2 + logf(l);
+}
+
+static bool sizes_ok(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {
+    return b >= 0 && b <= 65535 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0 && heads <= 65535 && d >= 1 && d <= 256 && max_len >= 0 &&
+           max_len <= (int64_t)1 << 30;
 }
 
 }  // namespace ecasq
@@ -88,7 +65,9 @@ using namespace ecasq;
 extern "C" {
 
 size_t ecasq_workspace_size_attend(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {
-    return 0;
+    if (!sizes_ok(b, heads, kv_heads, d, max_len)) return 0;
+    const Splits s = make_splits(b, (int64_t)kv_heads * cdiv(heads / kv_heads, kHeads), max_len);
+    return s.count > 1 ? (size_t)(b * heads * s.count * PartAt(d).stride) * 4 : 0;
 }
 
 int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_t heads, const ecasq_cache_t *k,
@@ -96,19 +75,80 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
                  const int32_t *starts, int64_t max_len, float scale, void *out, int64_t out_row, int64_t out_head,
                  float *lse, void *ws, size_t ws_bytes, int32_t *status, ecasq_stream_t stream) {
     if (!cache_ok(k) || !cache_ok(v) || k->type != v->type || k->levels_n != v->levels_n || k->d != v->d ||
-        k->heads != v->heads || k->pages != v->pages || k->page_size != v->page_size || b < 0 || b > 65535 || heads < 1 ||
-        heads % k->heads || max_len < 0 || max_len >= (int64_t)1 << 31)
+        k->heads != v->heads || k->pages != v->pages || k->page_size != v->page_size ||
+        !sizes_ok(b, heads, k->heads, k->d, max_len))
         return ECASQ_EINVAL;
     if (b == 0) return ECASQ_OK;
     if (!q || !out || !lengths || (max_len && (!table || table_row < cdiv(max_len, k->page_size)))) return ECASQ_EINVAL;
-    const AttendArgs a{q, out, table, lengths, starts, lse, status, *k, *v, q_row, q_head, out_row, out_head,
-                       table_row, max_len, scale, heads};
+    AttendArgs a{};
+    a.q = q;
+    a.out = out;
+    a.table = table;
+    a.lengths = lengths;
+    a.starts = starts;
+    a.lse = lse;
+    a.status = status;
+    const int64_t e = k->levels_n ? 1 : type_size(k->type);
+    a.k = static_cast<const char *>(k->rows);
+    a.v = static_cast<const char *>(v->rows);
+    a.kt = static_cast<const char *>(k->levels);
+    a.vt = static_cast<const char *>(v->levels);
+    a.k_page = k->row_page * e;
+    a.k_slot = k->row_slot * e;
+    a.k_head = k->row_head * e;
+    a.v_page = v->row_page * e;
+    a.v_slot = v->row_slot * e;
+    a.v_head = v->row_head * e;
+    a.kt_page = k->level_page * 2;
+    a.kt_slot = k->level_slot * 2;
+    a.kt_head = k->level_head * 2;
+    a.vt_page = v->level_page * 2;
+    a.vt_slot = v->level_slot * 2;
+    a.vt_head = v->level_head * 2;
+    a.q_row = q_row;
+    a.q_head = q_head;
+    a.out_row = out_row;
+    a.out_head = out_head;
+    a.table_row = table_row;
+    a.pages = k->pages;
+    a.scale2 = scale * kLog2e;
+    a.heads = heads;
+    a.group = heads / k->heads;
+    a.htiles = (int32_t)cdiv(a.group, kHeads);
+    a.d = k->d;
+    a.page_size = k->page_size;
+    a.max_len = (int32_t)max_len;
+    const Splits s = make_splits(b, (int64_t)k->heads * a.htiles, max_len);
+    a.chunk = s.chunk;
+    a.splits = s.count;
+    // t div page_size for t < 2^31: with 2^(c-1) < page_size <= 2^c the quotient is floor(t ceil(2^(31+c) / page_size) / 2^(31+c)),
+    // as the rounding up adds less than t 2^c / (page_size 2^(31+c)) < 1 / page_size (Granlund and Montgomery 1994).
+    int c = 0;
+    while (((int64_t)1 << c) < k->page_size) c++;
+    if (((int64_t)1 << c) == k->page_size) {
+        a.div_shift = (uint32_t)c;
+    } else {
+        a.div_mul = (uint32_t)((((uint64_t)1 << (31 + c)) + k->page_size - 1) / k->page_size);
+        a.div_shift = (uint32_t)(c - 1);
+    }
+    if (a.splits > 1) {
+        if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || ws_bytes < (size_t)(b * heads * a.splits * PartAt(a.d).stride) * 4)
+            return ECASQ_EWORKSPACE;
+        a.part = static_cast<float *>(ws);
+    }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const bool bf16 = k->type == ECASQ_BF16;
+    int rc;
+    if (k->type == ECASQ_F32) rc = launch_attend_f32(a, b, st);
+    else if (!k->levels_n) rc = launch_attend_16(a, bf16, b, st);
+    else if (k->levels_n == 8) rc = launch_attend_coded8(a, bf16, b, st);
+    else rc = launch_attend_coded16(a, bf16, b, st);
+    if (rc || a.splits == 1) return rc;
     const dim3 grid((unsigned)heads, (unsigned)b);
     note_launch();
-    if (k->type == ECASQ_F32) k_attend<float><<<grid, 128, 0, st>>>(a);
-    else if (k->type == ECASQ_F16) k_attend<__half><<<grid, 128, 0, st>>>(a);
-    else k_attend<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
+    if (k->type == ECASQ_F32) k_attend_join<float><<<grid, 128, 0, st>>>(a);
+    else if (bf16) k_attend_join<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
+    else k_attend_join<__half><<<grid, 128, 0, st>>>(a);
     ECASQ_LAUNCH_CHECK();
     return ECASQ_OK;
 }

@@ -1,0 +1,639 @@
+// attend.cuh -- attention of one new token a sequence over a paged cache (ecasq_attend).
+//
+// For query head h and the keys t of its sequence: s_t = scale q . K_t, out = sum softmax(s)_t V_t.
+// One pass over the cache with a running maximum m and sum l: a tile of 16 keys with scores s
+// moves m to m' = max(m, max s), O and l shrink by 2^(m - m') and gain sum 2^(s - m') V and
+// sum 2^(s - m') (s scaled to base 2).  A key row is read once for up to eight query heads.
+//
+// What bounds it: the cache's bytes.  So each warp works alone on tiles of 16 keys through a ring of its own in
+// shared memory that cp.async fills a few tiles ahead, without a barrier in the loop.  The sequence is cut into
+// splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory
+// and k_attend_join joins the splits.
+//
+// 16-bit rows: S^T = K Q^T and O^T = V^T P^T on mma.m16n8k16 with the eight heads as n, fp32 sums.  (One
+// token a sequence is a matrix-vector product for each key head; with eight columns there is nothing for the
+// larger tensor tiles to reuse.)  Both products may take their reduction index in any order, so that a lane reads
+// 16 consecutive bytes of a row where the fragments want scattered pairs:
+//   lane (g, t) = (lane / 4, lane mod 4) holds rows g and g + 8 of K, 16-byte chunks t, t + 4, ...,
+//   and of V the chunks g, g + 8, ... of the keys 2t, 2t + 1, 2t + 8, 2t + 9, paired by byte permutes.
+// Weights enter the second product as a high and a low 16-bit part (their sum keeps 16 bits or more): one part alone would
+// add an error as large as the rounding of the result.
+// Coded rows: a lane holds its row's codebook as planes of low and of high bytes; a byte permute with four
+// codes as its selector looks four entries up in eight levels at once, so that a pair of entries costs two lookups
+// and two permutes and no shared-memory access.
+// fp32 rows: fp32 products on the FMA pipe in the same frame.
+#pragma once
+
+#include <type_traits>
+
+#include "codes.cuh"
+
+namespace ecasq {
+
+constexpr int kTile = 16;        // keys of a tile
+constexpr int kHeads = 8;        // query heads of a block
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttendArgs {
+    const void *q;
+    void *out;
+    const int32_t *table, *lengths, *starts;
+    float *lse, *part;           // part: splits' results, see PartAt
+    int32_t *status;
+    const char *k, *v, *kt, *vt; // rows and codebooks
+    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;          // strides in bytes
+    int64_t kt_page, kt_slot, kt_head, vt_page, vt_slot, vt_head;
+    int64_t q_row, q_head, out_row, out_head, table_row, pages;
+    float scale2;                // scale log2(e)
+    int32_t heads, group, htiles, d, page_size, max_len, chunk, splits;  // group: query heads a key head
+    uint32_t div_mul, div_shift; // t div page_size = umulhi(t, div_mul) >> div_shift, or t >> div_shift if div_mul is 0
+};
+
+// A split's result for one query head: d sums, then its maximum (base 2) and its sum of weights.
+struct PartAt {
+    int64_t stride;
+    __host__ __device__ explicit PartAt(int d) : stride(d + 4) {}
+    __device__ float *at(float *part, int64_t seq, int heads, int head, int splits, int split) const {
+        return part + ((seq * heads + head) * splits + split) * stride;
+    }
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes to shared memory, or 16 zero bytes (src is not read then).
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool read) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0));
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N)); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s) {
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(s));
+    return d;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma16<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16<__nv_bfloat16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two values as a pair of T, the first in the low half.
+template <typename T> __device__ __forceinline__ uint32_t pack2(float x, float y) {
+    const T lo = from_f32<T>(x), hi = from_f32<T>(y);
+    return (uint32_t)reinterpret_cast<const uint16_t &>(lo) | (uint32_t)reinterpret_cast<const uint16_t &>(hi) << 16;
+}
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v) {
+    const uint16_t lo = (uint16_t)v, hi = (uint16_t)(v >> 16);
+    return make_float2(to_f32(reinterpret_cast<const T &>(lo)), to_f32(reinterpret_cast<const T &>(hi)));
+}
+
+// A row's codebook as byte planes.
+template <int LV> struct Book {
+    uint32_t lo[LV / 4], hi[LV / 4];
+    __device__ __forceinline__ void load(const char *p) {
+#pragma unroll
+        for (int i = 0; i < LV / 8; i++) {
+            const uint4 r = reinterpret_cast<const uint4 *>(p)[i];
+            lo[2 * i] = prmt(r.x, r.y, 0x6420);
+            hi[2 * i] = prmt(r.x, r.y, 0x7531);
+            lo[2 * i + 1] = prmt(r.z, r.w, 0x6420);
+            hi[2 * i + 1] = prmt(r.z, r.w, 0x7531);
+        }
+    }
+    // Entries 4H .. 4H+3 of the word w of eight codes: their low and their high bytes.
+    template <int H> __device__ __forceinline__ void look(uint32_t w, uint32_t &l, uint32_t &h) const {
+        if (LV == 8) {
+            const uint32_t s = H ? w >> 16 : w;
+            l = prmt(lo[0], lo[1], s);
+            h = prmt(hi[0], hi[1], s);
+        } else {
+            // The lower and the upper eight levels by the codes' low three bits, then a choice by the fourth: a byte
+            // permute spreads the sign bits of w << 4 and of w, which are the codes' fourth bits.
+            const uint32_t s = (H ? w >> 16 : w) & 0x7777u, m = prmt(w << 4, w, H ? 0xFBEA : 0xD9C8);
+            const uint32_t l0 = prmt(lo[0], lo[1], s), l1 = prmt(lo[2 % (LV / 4)], lo[3 % (LV / 4)], s);
+            const uint32_t h0 = prmt(hi[0], hi[1], s), h1 = prmt(hi[2 % (LV / 4)], hi[3 % (LV / 4)], s);
+            l = (l0 & ~m) | (l1 & m);
+            h = (h0 & ~m) | (h1 & m);
+        }
+    }
+};
+
+// A tile in shared memory: 16 rows of K, 16 of V, then their codebooks.  T and LV: the rows' type and
+// levels (0: plain); NV: the row length is at most 64 NV.
+template <typename T, int LV, int NV> struct Shape {
+    static constexpr bool kF32 = sizeof(T) == 4;
+    static constexpr int kRow = LV ? 32 * NV : 64 * NV * (int)sizeof(T);   // bytes of a row's room
+    static constexpr int kChunks = kRow / 16;
+    static constexpr int kBook = 2 * LV;                                   // bytes of a codebook
+    static constexpr int kBytes = 2 * kTile * (kRow + kBook);
+    static constexpr int kWarps = kBytes > 16384 ? 2 : 4;
+    static constexpr int kStages = kBytes > 4096 ? 3 : 4;
+    static constexpr int kRing = kStages * kBytes;                         // of a warp
+    static constexpr int kJoin = kHeads * 64 * NV * 4;                     // a warp's sums at the end, in its ring
+    static constexpr int kExtra = (kF32 ? kHeads * 64 * NV * 4 + kWarps * kTile * kHeads * 4 : 0) + kWarps * (2 * kHeads * 4) + kWarps * kStages * 4;
+    static constexpr int kSmem = kWarps * kRing + kExtra;
+    static_assert(kJoin <= kRing, "");
+    static_assert(kSmem <= 227 * 1024, "");
+    static constexpr int kPieces = kTile * kChunks / 32;                   // 16-byte pieces of K (and of V) for a lane
+    // Where chunk c of key position r lies: swizzled so that the reads described above do not meet in a bank.
+    __device__ static __forceinline__ int k_at(int r, int c) {
+        if (LV && NV < 4) return r * kRow + 16 * c;
+        return r * kRow + 16 * (c ^ ((r & 1) << 2));
+    }
+    // Row 2t + e + 8f of V is stored as row t + 4 (e + 2f).
+    __device__ static __forceinline__ int v_row(int r) { return ((r >> 1) & 3) + 4 * ((r & 1) + 2 * (r >> 3)); }
+    __device__ static __forceinline__ int v_at(int stored, int c) {
+        if (kF32) return stored * kRow + 16 * c;
+        if (LV) {
+            if (NV == 1) return stored * kRow + 16 * c;
+            if (NV == 2) return stored * kRow + 16 * (c ^ (stored & 2));
+        }
+        return stored * kRow + 16 * (c ^ ((stored & 3) << 1));
+    }
+};
+
+__device__ __forceinline__ int page_of(const AttendArgs &a, int t) {
+    return a.div_mul ? (int)(__umulhi((uint32_t)t, a.div_mul) >> a.div_shift) : t >> a.div_shift;
+}
+
+// The keys [first, end) that a block sees of its sequence.
+struct Span {
+    int first, end;
+    bool too_long;
+};
+__device__ __forceinline__ Span seq_span(const AttendArgs &a, int64_t seq) {
+    Span s;
+    s.end = a.lengths[seq];
+    s.first = a.starts ? max(a.starts[seq], 0) : 0;
+    s.too_long = s.end > a.max_len;
+    if (s.too_long) s.end = a.max_len;
+    return s;
+}
+// Splits are counted from the tile of the first key.
+__device__ __forceinline__ int splits_of(const AttendArgs &a, const Span &s) {
+    const int lead = s.first & ~(kTile - 1);
+    return s.end > s.first ? (s.end - lead + a.chunk - 1) / a.chunk : 0;
+}
+
+template <typename T, int LV, int NV>
+__global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const __grid_constant__ AttendArgs a) {
+    using S = Shape<T, LV, NV>;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int64_t seq = blockIdx.z;
+    const int split = blockIdx.y, kh = blockIdx.x / a.htiles, h0 = kh * a.group + (blockIdx.x % a.htiles) * kHeads;
+    const int nh = min(kHeads, a.group - (int)(blockIdx.x % a.htiles) * kHeads);
+    const Span span = seq_span(a, seq);
+    if (span.too_long && threadIdx.x == 0 && split == 0 && a.status) atomicOr(a.status, ECASQ_BAD_LENGTH);
+    const int active = splits_of(a, span);
+    if (split >= max(active, 1)) return;
+    const int lead = span.first & ~(kTile - 1);
+    const int begin = lead + split * a.chunk, end = min(span.end, begin + a.chunk);  // keys of this split (from `first` on)
+
+    char *ring = smem + wid * S::kRing;
+    float *qs = reinterpret_cast<float *>(smem + S::kWarps * S::kRing);  // fp32: q, then each warp's weights
+    float *ps = qs + kHeads * 64 * NV + wid * kTile * kHeads;
+    float *wmax = qs + (S::kF32 ? kHeads * 64 * NV + S::kWarps * kTile * kHeads : 0), *wsum = wmax + S::kWarps * kHeads;
+    uint32_t *seen = reinterpret_cast<uint32_t *>(wsum + S::kWarps * kHeads) + wid * S::kStages;  // keys of a stage that count
+
+    // Chunks beyond the row's end are read but never filled.
+    const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
+    if (row_chunks < S::kChunks)
+        for (int i = lane; i < S::kRing / 16; i += 32) reinterpret_cast<uint4 *>(ring)[i] = make_uint4(0, 0, 0, 0);
+    const T *qp = static_cast<const T *>(a.q) + seq * a.q_row + h0 * a.q_head;
+    if (S::kF32) {
+        for (int i = threadIdx.x; i < kHeads * 64 * NV; i += 32 * S::kWarps) {
+            const int h = i / (64 * NV), e = i % (64 * NV);
+            qs[i] = h < nh && e < a.d ? to_f32(qp[h * a.q_head + e]) : 0.f;
+        }
+    }
+    __syncthreads();
+
+    // ---- copies
+    const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
+    const char *ktb = LV ? a.kt + kh * a.kt_head : nullptr, *vtb = LV ? a.vt + kh * a.vt_head : nullptr;
+    const int32_t *table = a.table + seq * a.table_row;
+    const bool whole = a.page_size % kTile == 0;  // a tile lies in one page
+    bool bad_page = false;
+    // Page and slot of the lane's key (key `lane` mod 16 of the tile) of the tile that is fetched next.
+    int page = 0, slot = 0;
+    auto find = [&](int t0) {
+        const int key = t0 + (lane & 15);
+        if (key < span.first || key >= end) { page = -2; slot = 0; return; }  // beyond: not an error
+        const int p = page_of(a, key);
+        slot = key - p * a.page_size;
+        page = table[p];
+    };
+    auto fetch = [&](int t0, int stage) {
+        char *dst = ring + stage * S::kBytes;
+        const bool ok = page >= 0 && page < a.pages;
+        if (page != -2 && !ok) bad_page = true;
+        const uint32_t mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+        if (lane == 0) seen[stage] = mask;
+        int64_t kp = 0, vp = 0;
+        if (whole) {  // one page: the first counted key's
+            const int from = mask ? __ffs(mask) - 1 : 0;
+            const int64_t p = mask ? __shfl_sync(0xffffffffu, page, from) : 0;
+            const int s = __shfl_sync(0xffffffffu, slot, from) - from;
+            kp = p * a.k_page + s * a.k_slot;
+            vp = p * a.v_page + s * a.v_slot;
+        }
+#pragma unroll
+        for (int i = 0; i < S::kPieces; i++) {
+            const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
+            const bool read = mask >> r & 1;
+            int64_t ko, vo;
+            if (whole) {
+                ko = kp + r * a.k_slot;
+                vo = vp + r * a.v_slot;
+            } else {
+                const int64_t p = __shfl_sync(0xffffffffu, page, r), s = __shfl_sync(0xffffffffu, slot, r);
+                ko = p * a.k_page + s * a.k_slot;
+                vo = p * a.v_page + s * a.v_slot;
+            }
+            if (c < row_chunks) {
+                copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + ko + 16 * c : kb, read);
+                copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), c)), read ? vb + vo + 16 * c : vb, read);
+            }
+        }
+        if (LV) {  // codebooks: the lanes 0 .. 15 the keys', 16 .. 31 the values'
+            const int r = lane & 15;
+            const bool read = mask >> r & 1, isv = lane >= 16;
+            const int64_t p = read ? page : 0, s = read ? slot : 0;  // lanes 16 .. 31 hold the same keys
+            const char *src = isv ? vtb + p * a.vt_page + s * a.vt_slot : ktb + p * a.kt_page + s * a.kt_slot;
+            char *to = dst + 2 * kTile * S::kRow + (isv ? kTile * S::kBook + S::v_row(r) * S::kBook : r * S::kBook);
+#pragma unroll
+            for (int i = 0; i < LV / 8; i++) copy16(smem_addr(to + 16 * i), src + 16 * i, read);
+        }
+    };
+
+    // ---- state: maximum and sum of the heads 2t, 2t + 1 (the sums of this lane's keys alone), and O
+    float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
+    constexpr int kOut = S::kF32 ? (NV == 4 ? 2 : 1) * kHeads * 4 : 16 * NV;
+    float o[kOut];
+#pragma unroll
+    for (int i = 0; i < kOut; i++) o[i] = 0.f;
+    // 16-bit: q as the second operand of S^T, in the order of the lane's chunks of K
+    constexpr int kSteps = S::kF32 ? 1 : 4 * NV;
+    uint32_t qf[2 * kSteps];
+    if (!S::kF32) {
+        constexpr int kRun = LV ? (NV == 1 ? 16 : 32) : 8;  // consecutive entries of a lane's chunk
+#pragma unroll
+        for (int i = 0; i < 2 * kSteps; i++) {
+            const int run = 2 * i / kRun, e = kRun * (t + 4 * run) + 2 * i % kRun;
+            const bool in = g < nh && e < a.d;
+            qf[i] = in ? pack2<T>(to_f32(qp[g * a.q_head + e]), to_f32(qp[g * a.q_head + e + 1])) : 0u;
+        }
+    }
+
+    const int step = kTile * S::kWarps;
+    int next = begin + kTile * wid, fill = 0;
+    find(next);
+#pragma unroll
+    for (int i = 0; i < S::kStages - 1; i++) {
+        if (next < end) {
+            fetch(next, fill);
+            find(next + step);
+        }
+        copies_commit();
+        next += step;
+        fill++;
+    }
+    int use = 0;
+    for (int t0 = begin + kTile * wid; t0 < end; t0 += step) {
+        if (next < end) {
+            fetch(next, fill);
+            find(next + step);
+        }
+        copies_commit();
+        next += step;
+        fill = fill + 1 == S::kStages ? 0 : fill + 1;
+        copies_wait<S::kStages - 1>();
+        __syncwarp();
+        const char *kt = ring + use * S::kBytes, *vt = kt + kTile * S::kRow, *bk = vt + kTile * S::kRow, *bv = bk + kTile * S::kBook;
+        const uint32_t mask = seen[use];
+
+        // ---- scores: c[0], c[1] of key g, c[2], c[3] of key g + 8, heads 2t and 2t + 1
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (S::kF32) {
+            float v[2][kHeads];
+#pragma unroll
+            for (int h = 0; h < kHeads; h++) v[0][h] = v[1][h] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4 * NV; i++) {
+                if (16 * i >= a.d) break;
+                const float4 x = *reinterpret_cast<const float4 *>(kt + S::k_at(g, t + 4 * i));
+                const float4 y = *reinterpret_cast<const float4 *>(kt + S::k_at(g + 8, t + 4 * i));
+#pragma unroll
+                for (int h = 0; h < kHeads; h++) {
+                    if (h >= nh) break;
+                    const float4 q4 = *reinterpret_cast<const float4 *>(qs + h * 64 * NV + 4 * (t + 4 * i));
+                    v[0][h] = fmaf(x.w, q4.w, fmaf(x.z, q4.z, fmaf(x.y, q4.y, fmaf(x.x, q4.x, v[0][h]))));
+                    v[1][h] = fmaf(y.w, q4.w, fmaf(y.z, q4.z, fmaf(y.y, q4.y, fmaf(y.x, q4.x, v[1][h]))));
+                }
+            }
+            // sums over t; lane t keeps the heads 2t, 2t + 1
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                float w[4];
+#pragma unroll
+                for (int h = 0; h < 4; h++) {
+                    const float keep = t & 2 ? v[u][h + 4] : v[u][h], give = t & 2 ? v[u][h] : v[u][h + 4];
+                    w[h] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float keep = t & 1 ? w[h + 2] : w[h], give = t & 1 ? w[h] : w[h + 2];
+                    c[2 * u + h] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+                }
+            }
+        } else {
+            float c2[4] = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (LV == 0) {
+#pragma unroll
+                for (int i = 0; i < 2 * NV; i++) {
+                    if (32 * i >= a.d) break;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(kt + S::k_at(g, t + 4 * i));
+                    const uint4 y = *reinterpret_cast<const uint4 *>(kt + S::k_at(g + 8, t + 4 * i));
+                    mma16<T>(c, x.x, y.x, x.y, y.y, qf[4 * i], qf[4 * i + 1]);
+                    mma16<T>(c2, x.z, y.z, x.w, y.w, qf[4 * i + 2], qf[4 * i + 3]);
+                }
+            } else {
+                Book<LV> b0, b1;
+                b0.load(bk + g * S::kBook);
+                b1.load(bk + (g + 8) * S::kBook);
+#pragma unroll
+                for (int i = 0; i < (NV == 4 ? 2 : 1); i++) {
+                    constexpr int kWords = NV == 1 ? 2 : 4;
+                    alignas(16) uint32_t x[kWords], y[kWords];
+                    if constexpr (NV == 1) {
+                        *reinterpret_cast<uint2 *>(x) = *reinterpret_cast<const uint2 *>(kt + g * S::kRow + 8 * t);
+                        *reinterpret_cast<uint2 *>(y) = *reinterpret_cast<const uint2 *>(kt + (g + 8) * S::kRow + 8 * t);
+                    } else {
+                        *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(kt + S::k_at(g, t + 4 * i));
+                        *reinterpret_cast<uint4 *>(y) = *reinterpret_cast<const uint4 *>(kt + S::k_at(g + 8, t + 4 * i));
+                    }
+#pragma unroll
+                    for (int w = 0; w < kWords; w++) {
+                        const uint32_t *q4 = qf + 4 * (kWords * i + w);
+                        uint32_t xl, xh, yl, yh;
+                        b0.template look<0>(x[w], xl, xh);
+                        b1.template look<0>(y[w], yl, yh);
+                        mma16<T>(c, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[0], q4[1]);
+                        b0.template look<1>(x[w], xl, xh);
+                        b1.template look<1>(y[w], yl, yh);
+                        mma16<T>(c2, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[2], q4[3]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) c[i] += c2[i];
+        }
+
+        // ---- running maximum, weights, sums
+#pragma unroll
+        for (int i = 0; i < 4; i++) c[i] *= a.scale2;
+        if (mask != 0xffffu) {  // rows that are not seen hold zeros; their scores do not count
+            if (!(mask >> g & 1)) c[0] = c[1] = -CUDART_INF_F;
+            if (!(mask >> (g + 8) & 1)) c[2] = c[3] = -CUDART_INF_F;
+        }
+        float n0 = fmaxf(c[0], c[2]), n1 = fmaxf(c[1], c[3]);
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) {
+            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, x));
+            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, x));
+        }
+        n0 = fmaxf(n0, m0);
+        n1 = fmaxf(n1, m1);
+        // with no weight yet (maximum -inf) the exponents are taken from 0
+        const float base0 = n0 == -CUDART_INF_F ? 0.f : n0, base1 = n1 == -CUDART_INF_F ? 0.f : n1;
+        if (__any_sync(0xffffffffu, n0 != m0 || n1 != m1)) {
+            const float s0 = exp2_fast(m0 - base0), s1 = exp2_fast(m1 - base1);
+            l0 *= s0;
+            l1 *= s1;
+            if constexpr (S::kF32) {
+#pragma unroll
+                for (int h = 0; h < kHeads; h++) {  // this lane holds some entries of all heads
+                    const float sh = __shfl_sync(0xffffffffu, h & 1 ? s1 : s0, h >> 1);
+#pragma unroll
+                    for (int i = 0; i < kOut / kHeads; i++) o[h * (kOut / kHeads) + i] *= sh;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kOut; i += 2) {
+                    o[i] *= s0;
+                    o[i + 1] *= s1;
+                }
+            }
+            m0 = n0;
+            m1 = n1;
+        }
+        c[0] = exp2_fast(c[0] - base0);
+        c[1] = exp2_fast(c[1] - base1);
+        c[2] = exp2_fast(c[2] - base0);
+        c[3] = exp2_fast(c[3] - base1);
+        l0 += c[0] + c[2];
+        l1 += c[1] + c[3];
+
+        // ---- values
+        if constexpr (S::kF32) {
+            *reinterpret_cast<float2 *>(ps + g * kHeads + 2 * t) = make_float2(c[0], c[1]);
+            *reinterpret_cast<float2 *>(ps + (g + 8) * kHeads + 2 * t) = make_float2(c[2], c[3]);
+            __syncwarp();
+            constexpr int kLanes = NV == 1 ? 16 : 32, kRows = 32 / kLanes, kCols = NV == 4 ? 2 : 1;
+#pragma unroll 4
+            for (int r = lane / kLanes; r < kTile; r += kRows) {
+                const float4 p0 = *reinterpret_cast<const float4 *>(ps + r * kHeads), p1 = *reinterpret_cast<const float4 *>(ps + r * kHeads + 4);
+                const float p[kHeads] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+#pragma unroll
+                for (int i = 0; i < kCols; i++) {
+                    const float4 x = *reinterpret_cast<const float4 *>(vt + S::v_at(S::v_row(r), lane % kLanes + 32 * i));
+#pragma unroll
+                    for (int h = 0; h < kHeads; h++) {
+                        if (h >= nh) break;
+                        float *oh = o + (h * kCols + i) * 4;
+                        oh[0] = fmaf(p[h], x.x, oh[0]);
+                        oh[1] = fmaf(p[h], x.y, oh[1]);
+                        oh[2] = fmaf(p[h], x.z, oh[2]);
+                        oh[3] = fmaf(p[h], x.w, oh[3]);
+                    }
+                }
+            }
+        } else {
+            // P^T as second operand: keys 2t, 2t + 1 (and + 8) of head g, in two parts
+            uint32_t b[4];
+            {
+                const uint32_t h01 = pack2<T>(c[0], c[1]), h23 = pack2<T>(c[2], c[3]);
+                const float2 f01 = unpack2<T>(h01), f23 = unpack2<T>(h23);
+                b[0] = transpose8x8(h01);
+                b[1] = transpose8x8(h23);
+                b[2] = transpose8x8(pack2<T>(c[0] - f01.x, c[1] - f01.y));
+                b[3] = transpose8x8(pack2<T>(c[2] - f23.x, c[3] - f23.y));
+            }
+            // o[4 j ..]: two entries of the row (of head 2t, 2t + 1 each)
+            auto put = [&](int j, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+                float(&acc)[4] = *reinterpret_cast<float(*)[4]>(o + 4 * j);
+                mma16<T>(acc, a0, a1, a2, a3, b[0], b[1]);
+                mma16<T>(acc, a0, a1, a2, a3, b[2], b[3]);
+            };
+            if constexpr (LV == 0) {
+#pragma unroll
+                for (int i = 0; i < NV; i++) {
+                    if (64 * i >= a.d) break;
+                    alignas(16) uint32_t x[4][4];
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+                        *reinterpret_cast<uint4 *>(x[r]) = *reinterpret_cast<const uint4 *>(vt + S::v_at(t + 4 * r, g + 8 * i));
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        put(4 * i + j, prmt(x[0][j], x[1][j], 0x5410), prmt(x[0][j], x[1][j], 0x7632), prmt(x[2][j], x[3][j], 0x5410),
+                            prmt(x[2][j], x[3][j], 0x7632));
+                }
+            } else {
+                Book<LV> bb[4];
+                alignas(16) uint32_t x[4][NV];
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    bb[r].load(bv + (t + 4 * r) * S::kBook);
+                    if constexpr (NV == 1) x[r][0] = *reinterpret_cast<const uint32_t *>(vt + S::v_at(t + 4 * r, 0) + 4 * g);
+                    else if constexpr (NV == 2)
+                        *reinterpret_cast<uint2 *>(x[r]) = *reinterpret_cast<const uint2 *>(vt + S::v_at(t + 4 * r, g >> 1) + 8 * (g & 1));
+                    else *reinterpret_cast<uint4 *>(x[r]) = *reinterpret_cast<const uint4 *>(vt + S::v_at(t + 4 * r, g));
+                }
+                auto half = [&](int w, auto hh) {
+                    constexpr int H = decltype(hh)::value;
+                    uint32_t p[4][2];  // entries 0, 1 and 2, 3 of each key
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        uint32_t lo, hi;
+                        bb[r].template look<H>(x[r][w], lo, hi);
+                        p[r][0] = prmt(lo, hi, 0x5140);
+                        p[r][1] = prmt(lo, hi, 0x7362);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; u++)
+                        put(4 * w + 2 * H + u, prmt(p[0][u], p[1][u], 0x5410), prmt(p[0][u], p[1][u], 0x7632),
+                            prmt(p[2][u], p[3][u], 0x5410), prmt(p[2][u], p[3][u], 0x7632));
+                };
+#pragma unroll
+                for (int w = 0; w < NV; w++) {
+                    half(w, std::integral_constant<int, 0>());
+                    half(w, std::integral_constant<int, 1>());
+                }
+            }
+        }
+        use = use + 1 == S::kStages ? 0 : use + 1;
+        __syncwarp();
+    }
+    copies_wait<0>();
+    if (bad_page && a.status) atomicOr(a.status, ECASQ_BAD_PAGE);
+
+    // ---- the block's warps: maxima and sums, then each warp's O shrunk to the common maximum
+#pragma unroll
+    for (int x = 4; x < 32; x *= 2) {
+        l0 += __shfl_xor_sync(0xffffffffu, l0, x);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, x);
+    }
+    if (g == 0) {
+        wmax[wid * kHeads + 2 * t] = m0;
+        wmax[wid * kHeads + 2 * t + 1] = m1;
+        wsum[wid * kHeads + 2 * t] = l0;
+        wsum[wid * kHeads + 2 * t + 1] = l1;
+    }
+    __syncthreads();
+    auto top = [&](int h) {
+        float m = wmax[h];
+        for (int w = 1; w < S::kWarps; w++) m = fmaxf(m, wmax[w * kHeads + h]);
+        return m;
+    };
+    auto shrink = [&](int w, int h, float m) { return m == -CUDART_INF_F ? 0.f : exp2_fast(wmax[w * kHeads + h] - m); };
+    constexpr int kWide = 64 * NV;
+    float *mine = reinterpret_cast<float *>(ring);
+    if constexpr (S::kF32) {
+        constexpr int kLanes = NV == 1 ? 16 : 32, kCols = NV == 4 ? 2 : 1;
+#pragma unroll
+        for (int h = 0; h < kHeads; h++) {
+            const float sh = shrink(wid, h, top(h));
+#pragma unroll
+            for (int i = 0; i < kCols; i++) {
+                float *oh = o + (h * kCols + i) * 4;
+                float4 x = make_float4(oh[0] * sh, oh[1] * sh, oh[2] * sh, oh[3] * sh);
+                if (kLanes == 16) {
+                    x.x += __shfl_xor_sync(0xffffffffu, x.x, 16);
+                    x.y += __shfl_xor_sync(0xffffffffu, x.y, 16);
+                    x.z += __shfl_xor_sync(0xffffffffu, x.z, 16);
+                    x.w += __shfl_xor_sync(0xffffffffu, x.w, 16);
+                }
+                if (lane < kLanes) *reinterpret_cast<float4 *>(mine + h * kWide + 4 * (lane + 32 * i)) = x;
+            }
+        }
+    } else {
+        const float s0 = shrink(wid, 2 * t, top(2 * t)), s1 = shrink(wid, 2 * t + 1, top(2 * t + 1));
+#pragma unroll
+        for (int j = 0; j < 4 * NV; j++) {
+            // plain: entries 8 (g + 8 i) + 2 j', coded: 8 NV g + 2 j
+            const int e = LV ? 8 * NV * g + 2 * j : 8 * (g + 8 * (j >> 2)) + 2 * (j & 3);
+            *reinterpret_cast<float2 *>(mine + 2 * t * kWide + e) = make_float2(o[4 * j] * s0, o[4 * j + 2] * s0);
+            *reinterpret_cast<float2 *>(mine + (2 * t + 1) * kWide + e) = make_float2(o[4 * j + 1] * s1, o[4 * j + 3] * s1);
+        }
+    }
+    __syncthreads();
+    const PartAt at(a.d);
+    for (int h = 0; h < nh; h++) {
+        const float m = top(h);
+        float l = 0.f;
+        for (int w = 0; w < S::kWarps; w++) l += wsum[w * kHeads + h] * shrink(w, h, m);
+        float *part = a.splits > 1 ? at.at(a.part, seq, a.heads, h0 + h, a.splits, split) : nullptr;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        for (int e = threadIdx.x; e < a.d; e += 32 * S::kWarps) {
+            float x = 0.f;
+#pragma unroll
+            for (int w = 0; w < S::kWarps; w++) x += reinterpret_cast<const float *>(smem + w * S::kRing)[h * kWide + e];
+            if (part) part[e] = x;
+            else static_cast<T *>(a.out)[seq * a.out_row + (h0 + h) * a.out_head + e] = from_f32<T>(l == 0.f ? 0.f : x * inv);
+        }
+        if (threadIdx.x == 0) {
+            if (part) {
+                part[a.d] = m;
+                part[a.d + 1] = l;
+            } else if (a.lse) a.lse[seq * a.heads + h0 + h] = l == 0.f ? -CUDART_INF_F : m * kLn2 + logf(l);
+        }
+    }
+}
+
+template <typename T, int LV, int NV>
+static int launch_attend(const AttendArgs &a, int64_t b, cudaStream_t st) {
+    using S = Shape<T, LV, NV>;
+    ECASQ_CUDA_TRY(cudaFuncSetAttribute(k_attend<T, LV, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+    const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
+    note_launch();
+    k_attend<T, LV, NV><<<grid, 32 * S::kWarps, S::kSmem, st>>>(a);
+    ECASQ_LAUNCH_CHECK();
+    return ECASQ_OK;
+}
+template <typename T, int LV>
+static int launch_attend_rows(const AttendArgs &a, int64_t b, cudaStream_t st) {
+    if (a.d <= 64) return launch_attend<T, LV, 1>(a, b, st);
+    if (a.d <= 128) return launch_attend<T, LV, 2>(a, b, st);
+    return launch_attend<T, LV, 4>(a, b, st);
+}
+
+// One translation unit each.
+int launch_attend_f32(const AttendArgs &a, int64_t b, cudaStream_t st);
+int launch_attend_16(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
+int launch_attend_coded8(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
+int launch_attend_coded16(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
+
+}  // namespace ecasq

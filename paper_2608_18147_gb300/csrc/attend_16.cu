@@ -1,0 +1,8 @@
+// attend_16.cu -- ecasq_attend's kernels for plain 16-bit rows.
+#include "attend.cuh"
+
+namespace ecasq {
+int launch_attend_16(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st) {
+    return bf16 ? launch_attend_rows<__nv_bfloat16, 0>(a, b, st) : launch_attend_rows<__half, 0>(a, b, st);
+}
+}  // namespace ecasq

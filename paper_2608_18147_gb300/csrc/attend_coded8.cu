@@ -1,0 +1,8 @@
+// attend_coded8.cu -- ecasq_attend's kernels for rows coded with eight levels.
+#include "attend.cuh"
+
+namespace ecasq {
+int launch_attend_coded8(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st) {
+    return bf16 ? launch_attend_rows<__nv_bfloat16, 8>(a, b, st) : launch_attend_rows<__half, 8>(a, b, st);
+}
+}  // namespace ecasq
