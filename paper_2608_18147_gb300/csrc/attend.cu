@@ -121,16 +121,9 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     const Splits s = make_splits(b, (int64_t)k->heads * a.htiles, max_len);
     a.chunk = s.chunk;
     a.splits = s.count;
-    // t div page_size for t < 2^31: with 2^(c-1) < page_size <= 2^c the quotient is floor(t ceil(2^(31+c) / page_size) / 2^(31+c)),
-    // as the rounding up adds less than t 2^c / (page_size 2^(31+c)) < 1 / page_size (Granlund and Montgomery 1994).
-    int c = 0;
-    while (((int64_t)1 << c) < k->page_size) c++;
-    if (((int64_t)1 << c) == k->page_size) {
-        a.div_shift = (uint32_t)c;
-    } else {
-        a.div_mul = (uint32_t)((((uint64_t)1 << (31 + c)) + k->page_size - 1) / k->page_size);
-        a.div_shift = (uint32_t)(c - 1);
-    }
+    const FastDiv div(k->page_size);
+    a.div_mul = div.mul;
+    a.div_shift = div.shift;
     if (a.splits > 1) {
         if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || ws_bytes < (size_t)(b * heads * a.splits * PartAt(a.d).stride) * 4)
             return ECASQ_EWORKSPACE;

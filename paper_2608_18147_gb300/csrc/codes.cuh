@@ -20,6 +20,23 @@ static inline bool type_ok(int32_t t) { return t == ECASQ_F32 || t == ECASQ_F16 
 static inline int64_t type_size(int32_t t) { return t == ECASQ_F32 ? 4 : 2; }
 static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// t div n for 0 <= t < 2^31: umulhi(t, mul) >> shift, or t >> shift if mul is 0.  With 2^(c-1) < n < 2^c the
+// quotient is floor(t ceil(2^(31+c) / n) / 2^(31+c)): the rounding up adds less than t / 2^(31+c) < 2^-c < 1 / n (Granlund
+// and Montgomery 1994).
+struct FastDiv {
+    uint32_t mul = 0, shift = 0;
+    explicit FastDiv(int32_t n) {
+        int c = 0;
+        while (((int64_t)1 << c) < n) c++;
+        if (((int64_t)1 << c) == n) {
+            shift = (uint32_t)c;
+        } else {
+            mul = (uint32_t)((((uint64_t)1 << (31 + c)) + n - 1) / n);
+            shift = (uint32_t)(c - 1);
+        }
+    }
+};
+
 // The limits that ecasq_cache_t states; bytes of a row's entries and of its codebook.
 static inline bool cache_ok(const ecasq_cache_t *c) {
     if (!c || !c->rows || !type_ok(c->type) || c->pages < 1 || c->page_size < 1 || c->heads < 1 || c->d < 1 || c->d > 256)

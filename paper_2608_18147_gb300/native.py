@@ -570,18 +570,24 @@ def _refuse(where, what):
     raise EcasqError(EINVAL, "%s: %s" % (where, what))
 
 
-def _device_of(where, *tensors):
-    """The one CUDA device that the given tensors (None allowed) are on; it has to be the current one, whose
+def _device_of(where, first, *others):
+    """The index of the CUDA device that the given tensors (None allowed after the first) are on: the current one, whose
     stream the call uses."""
     torch = _torch()
-    at = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.device.index == at):
-            _refuse(where, "tensors must be on the current CUDA device")
+    try:
+        at = first.get_device()
+        for t in others:
+            if t is not None and t.get_device() != at:
+                at = -1
+    except (AttributeError, RuntimeError):
+        at = -1
+    if at < 0 or at != torch.cuda.current_device():
+        _refuse(where, "tensors must be on the current CUDA device")
+    return at
 
 
-def _stream_of(device_index):
-    return _torch()._C._cuda_getCurrentRawStream(device_index)
+def _stream_of(index):
+    return _torch()._C._cuda_getCurrentRawStream(index)
 
 
 def _status_ptr(where, status):
@@ -598,13 +604,13 @@ def ecasq_pack(idx):
     [n, 64 ceil(k / 128)]."""
     torch = _torch()
     where = "ecasq_pack"
-    _device_of(where, idx)
+    at = _device_of(where, idx)
     if idx.dtype != torch.uint8 or idx.dim() != 2 or (idx.shape[1] > 1 and idx.stride(1) != 1):
         _refuse(where, "idx must be uint8 [n, k] with contiguous rows")
     n, k = idx.shape
     codes = torch.empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=idx.device)
     rc = lib().ecasq_pack(idx.data_ptr(), idx.stride(0) if n > 1 else k, n, k, codes.data_ptr(), codes.shape[1],
-                          _stream_of(idx.device.index))
+                          _stream_of(at))
     _check(rc, where)
     return codes
 
@@ -617,7 +623,7 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None):
     Returns y [b, n] or [n] of x's type (`out` if given)."""
     torch = _torch()
     where = "ecasq_matvec"
-    _device_of(where, x, codes, levels, scales, out)
+    at = _device_of(where, x, codes, levels, scales, out)
     T = _types().get(x.dtype)
     x2 = x if x.dim() == 2 else x.unsqueeze(0)
     if T is None or x2.dim() != 2 or (x2.shape[1] > 1 and x2.stride(1) != 1):
@@ -644,7 +650,7 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None):
     rc = lib().ecasq_matvec(x2.data_ptr(), x2.stride(0), T, b, codes.data_ptr(), codes.stride(0) if n > 1 else codes.shape[1],
                             levels.data_ptr(), levels.numel(), scales.data_ptr(),
                             scales.stride(0) if n > 1 else scales.shape[1], _types()[scales.dtype], n, k, group,
-                            y.data_ptr(), y.stride(0), _stream_of(x.device.index))
+                            y.data_ptr(), y.stride(0), _stream_of(at))
     _check(rc, where)
     return out if out is not None else y if x.dim() == 2 else y[0]
 
@@ -680,7 +686,7 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
     tensor that BAD_* bits are or-ed into.  Returns (codes, levels), written in place."""
     torch = _torch()
     where = "ecasq_cache_write"
-    _device_of(where, x, Q, m, slots, codes, levels, status)
+    at = _device_of(where, x, Q, m, slots, codes, levels, status)
     c = _cache(where, codes, levels)
     n = slots.numel()
     if (x.dtype not in (torch.float32, levels.dtype) or x.dim() != 3 or x.shape != (n, c.heads, c.d)
@@ -697,7 +703,7 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
     rc = lib().ecasq_cache_write(x.data_ptr(), _types()[x.dtype], n, x.stride(0), x.stride(1), Q.data_ptr(), s,
                                  None if m is None else m.data_ptr(), slots.data_ptr(), C.byref(c),
                                  int(seed) & 0xFFFFFFFFFFFFFFFF, _status_ptr(where, status),
-                                 _stream_of(x.device.index))
+                                 _stream_of(at))
     _check(rc, where)
     return codes, levels
 
@@ -720,7 +726,7 @@ def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None
     (natural logarithm; -inf where no key is seen, with out = 0)."""
     torch = _torch()
     where = "ecasq_attend"
-    _device_of(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws, status)
+    at = _device_of(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws, status)
     if (k_levels is None) != (v_levels is None):
         _refuse(where, "k and v must both be plain or both be coded")
     ck, cv = _cache(where, k, k_levels), _cache(where, v, v_levels)
@@ -749,7 +755,7 @@ def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None
                             None if starts is None else starts.data_ptr(), max_len,
                             d ** -0.5 if scale is None else float(scale), out.data_ptr(), out.stride(0), out.stride(1),
                             lse.data_ptr(), ws.data_ptr(), ws.numel(), _status_ptr(where, status),
-                            _stream_of(q.device.index))
+                            _stream_of(at))
     _check(rc, where)
     return out, lse
 

@@ -50,6 +50,7 @@ CASES = [
     (1, 1, 1, 32), (1, 7, 2, 32), (3, 31, 1, 32), (8, 32, 1, 32), (9, 33, 8, 32), (16, 127, 3, 64), (17, 128, 2, 128),
     (31, 129, 4, 96), (40, 257, 5, 32), (65, 640, 8, 160), (130, 1000, 1, 96), (300, 2050, 3, 64), (1216, 384, 8, 128),
     (2500, 520, 2, 256), (24, 9000, 8, 64), (7, 20001, 1, 1 << 20),
+    (37, 25000, 8, 96), (700, 11400, 8, 128),
 ]
 
 
