@@ -8,7 +8,7 @@ namespace ecasq {
 // Splits.  A block has a fixed cost of its own (its first loads' latency, the join), so a split should be long; and the
 // blocks should fill the card evenly.  kSlots blocks run at once; up to kLong keys for each of them there is
 // one round of blocks, beyond that as many rounds as keep a split at most about that long.
-constexpr int kSlots = 2 * 152, kLong = 1024, kStep = 64;
+constexpr int kSlots = 3 * 152, kLong = 1024, kStep = 64;
 
 struct Splits {
     int32_t chunk, count;
@@ -23,34 +23,86 @@ static Splits make_splits(int64_t b, int64_t blocks, int64_t max_len) {
     return {(int32_t)chunk, (int32_t)cdiv(span, chunk)};
 }
 
-// A block a sequence and query head: the splits' maxima and sums, then their entries.
+// A block a sequence and query head: the splits' maxima and sums give each split's share, then 16 to 64 lanes a split add
+// the entries, four a lane, several splits at a time.
+constexpr int kJoinThreads = 256, kShares = 1024;
 template <typename T>
-__global__ void __launch_bounds__(128) k_attend_join(const __grid_constant__ AttendArgs a) {
-    __shared__ float red[8];
+__global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_constant__ AttendArgs a, int lanes) {
+    __shared__ float red[2 * kJoinThreads / 32], share[kShares];
+    __shared__ __align__(16) float4 sums[kJoinThreads];
     const int64_t seq = blockIdx.y;
-    const int h = blockIdx.x, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int h = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int n = max(splits_of(a, seq_span(a, seq)), 1);
     const PartAt at(a.d);
     const float *part = at.at(a.part, seq, a.heads, h, a.splits, 0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     float m = -CUDART_INF_F;
-    for (int i = threadIdx.x; i < n; i += 128) m = fmaxf(m, part[i * at.stride + a.d]);
+    for (int i = tid; i < n; i += kJoinThreads) m = fmaxf(m, part[i * at.stride + a.d]);
     for (int x = 16; x; x /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
     if (lane == 0) red[wid] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    m = red[0];
+    for (int w = 1; w < kJoinThreads / 32; w++) m = fmaxf(m, red[w]);
     const float base = m == -CUDART_INF_F ? 0.f : m;
     float l = 0.f;
-    for (int i = threadIdx.x; i < n; i += 128) l += part[i * at.stride + a.d + 1] * exp2_fast(part[i * at.stride + a.d] - base);
-    for (int x = 16; x; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
-    if (lane == 0) red[4 + wid] = l;
-    __syncthreads();
-    l = (red[4] + red[5]) + (red[6] + red[7]);
-    for (int e = threadIdx.x; e < a.d; e += 128) {
-        float x = 0.f;
-        for (int i = 0; i < n; i++) x = fmaf(part[i * at.stride + e], exp2_fast(part[i * at.stride + a.d] - base), x);
-        static_cast<T *>(a.out)[seq * a.out_row + h * a.out_head + e] = from_f32<T>(l == 0.f ? 0.f : x / l);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int e = 4 * (tid % lanes), from = tid / lanes, apart = kJoinThreads / lanes;
+    for (int i0 = 0; i0 < n; i0 += kShares) {
+        const int some = min(kShares, n - i0);
+        const float *p = part + i0 * at.stride;
+        for (int i = tid; i < some; i += kJoinThreads) {
+            const float2 ml = *reinterpret_cast<const float2 *>(p + i * at.stride + a.d);
+            share[i] = exp2_fast(ml.x - base);
+            l += ml.y * share[i];
+        }
+        __syncthreads();
+        if (e < a.d) {
+#pragma unroll 4
+            for (int i = from; i < some; i += apart) {
+                const float4 x = *reinterpret_cast<const float4 *>(p + i * at.stride + e);
+                const float s = share[i];
+                v.x = fmaf(x.x, s, v.x);
+                v.y = fmaf(x.y, s, v.y);
+                v.z = fmaf(x.z, s, v.z);
+                v.w = fmaf(x.w, s, v.w);
+            }
+        }
+        __syncthreads();
     }
-    if (threadIdx.x == 0 && a.lse) a.lse[seq * a.heads + h] = l == 0.f ? -CUDART_INF_F : m * kLn2 + logf(l);
+    for (int x = 16; x; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (lane == 0) red[kJoinThreads / 32 + wid] = l;
+    sums[tid] = v;
+    __syncthreads();
+    l = 0.f;
+    for (int w = 0; w < kJoinThreads / 32; w++) l += red[kJoinThreads / 32 + w];
+    if (tid < lanes && e < a.d) {
+        for (int i = 1; i < apart; i++) {
+            const float4 x = sums[i * lanes + tid];
+            v.x += x.x;
+            v.y += x.y;
+            v.z += x.z;
+            v.w += x.w;
+        }
+        store_out<T>(a, seq, h, e, v, l);
+    }
+    if (tid == 0 && a.lse) a.lse[seq * a.heads + h] = log_sum(m, l);
+}
+
+template <typename T>
+static int launch_join(const AttendArgs &a, int64_t b, cudaStream_t st) {
+    // May start while the splits' kernel ends: it waits for the results itself.
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)a.heads, (unsigned)b);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    note_launch();
+    ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_attend_join<T>, a, a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64));
+    return ECASQ_OK;
 }
 
 static bool sizes_ok(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {
@@ -137,13 +189,8 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     else if (k->levels_n == 8) rc = launch_attend_coded8(a, bf16, b, st);
     else rc = launch_attend_coded16(a, bf16, b, st);
     if (rc || a.splits == 1) return rc;
-    const dim3 grid((unsigned)heads, (unsigned)b);
-    note_launch();
-    if (k->type == ECASQ_F32) k_attend_join<float><<<grid, 128, 0, st>>>(a);
-    else if (bf16) k_attend_join<__nv_bfloat16><<<grid, 128, 0, st>>>(a);
-    else k_attend_join<__half><<<grid, 128, 0, st>>>(a);
-    ECASQ_LAUNCH_CHECK();
-    return ECASQ_OK;
+    if (k->type == ECASQ_F32) return launch_join<float>(a, b, st);
+    return bf16 ? launch_join<__nv_bfloat16>(a, b, st) : launch_join<__half>(a, b, st);
 }
 
 }  // extern "C"

@@ -10,12 +10,17 @@
 // splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory
 // and k_attend_join joins the splits.
 //
-// 16-bit rows: S^T = K Q^T and O^T = V^T P^T on mma.m16n8k16 with the eight heads as n, fp32 sums.  (One
+// 16-bit rows: S^T = K Q^T and O^T = V^T P^T on mma.m16n8k16 with the query heads as n, fp32 sums.  (One
 // token a sequence is a matrix-vector product for each key head; with eight columns there is nothing for the
 // larger tensor tiles to reuse.)  Both products may take their reduction index in any order, so that a lane reads
 // 16 consecutive bytes of a row where the fragments want scattered pairs:
 //   lane (g, t) = (lane / 4, lane mod 4) holds rows g and g + 8 of K, 16-byte chunks t, t + 4, ...,
-//   and of V the chunks g, g + 8, ... of the keys 2t, 2t + 1, 2t + 8, 2t + 9, paired by byte permutes.
+//   and of V the chunks g, g + 8, ... of the keys 2t, 2t + 1, 2t + 8, 2t + 9.
+// The reduction of the second product runs over keys, but a register of V holds two neighbouring entries of one key.
+// With up to four heads (HT = 4) a pair of reduction indices is such a pair of entries instead, and a head has two
+// columns, which hold its weights on the even and on the odd index: sum_t V_t[e] P_t and sum_t V_t[e + 1] P_t come
+// out side by side, in as many products as before.  With up to eight (HT = 8) the columns are taken, and two keys'
+// registers are first permuted into pairs of keys.
 // Weights enter the second product as a high and a low 16-bit part (their sum keeps 16 bits or more): one part alone would
 // add an error as large as the rounding of the result.
 // Coded rows: a lane holds its row's codebook as planes of low and of high bytes; a byte permute with four
@@ -31,7 +36,7 @@
 namespace ecasq {
 
 constexpr int kTile = 16;        // keys of a tile
-constexpr int kHeads = 8;        // query heads of a block
+constexpr int kHeads = 8;        // query heads of a block at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendArgs {
@@ -138,8 +143,8 @@ template <typename T, int LV, int NV> struct Shape {
     static constexpr int kChunks = kRow / 16;
     static constexpr int kBook = 2 * LV;                                   // bytes of a codebook
     static constexpr int kBytes = 2 * kTile * (kRow + kBook);
-    static constexpr int kWarps = kBytes > 16384 ? 2 : 4;
-    static constexpr int kStages = kBytes > 4096 ? 3 : 4;
+    static constexpr int kWarps = kBytes > 16384 ? 3 : kBytes > 8192 ? 2 : 4;
+    static constexpr int kStages = kBytes > 4096 + 1024 ? 2 : kBytes > 2560 ? 3 : 4;
     static constexpr int kRing = kStages * kBytes;                         // of a warp
     static constexpr int kJoin = kHeads * 64 * NV * 4;                     // a warp's sums at the end, in its ring
     static constexpr int kExtra = (kF32 ? kHeads * 64 * NV * 4 + kWarps * kTile * kHeads * 4 : 0) + kWarps * (2 * kHeads * 4) + kWarps * kStages * 4;
@@ -187,14 +192,26 @@ __device__ __forceinline__ int splits_of(const AttendArgs &a, const Span &s) {
     return s.end > s.first ? (s.end - lead + a.chunk - 1) / a.chunk : 0;
 }
 
-template <typename T, int LV, int NV>
+__device__ __forceinline__ float log_sum(float top, float sum) { return sum == 0.f ? -CUDART_INF_F : top * kLn2 + logf(sum); }
+// Four entries of a head's result: sums over keys by the sum of the weights (none: 0).
+template <typename T>
+__device__ __forceinline__ void store_out(const AttendArgs &a, int64_t seq, int head, int e, float4 v, float sum) {
+    T *out = static_cast<T *>(a.out) + seq * a.out_row + head * a.out_head + e;
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) out[i] = from_f32<T>(sum == 0.f ? 0.f : x[i] / sum);
+}
+
+// HT: query heads of a block, 4 or 8.
+template <typename T, int LV, int NV, int HT>
 __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const __grid_constant__ AttendArgs a) {
     using S = Shape<T, LV, NV>;
+    constexpr int HL = HT / 4;  // heads of a lane's scores: HT = 8: 2t, 2t + 1; HT = 4: t
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int64_t seq = blockIdx.z;
-    const int split = blockIdx.y, kh = blockIdx.x / a.htiles, h0 = kh * a.group + (blockIdx.x % a.htiles) * kHeads;
-    const int nh = min(kHeads, a.group - (int)(blockIdx.x % a.htiles) * kHeads);
+    const int split = blockIdx.y, kh = blockIdx.x / a.htiles, h0 = kh * a.group + (blockIdx.x % a.htiles) * HT;
+    const int nh = min(HT, a.group - (int)(blockIdx.x % a.htiles) * HT);
     const Span span = seq_span(a, seq);
     if (span.too_long && threadIdx.x == 0 && split == 0 && a.status) atomicOr(a.status, ECASQ_BAD_LENGTH);
     const int active = splits_of(a, span);
@@ -208,114 +225,132 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     float *wmax = qs + (S::kF32 ? kHeads * 64 * NV + S::kWarps * kTile * kHeads : 0), *wsum = wmax + S::kWarps * kHeads;
     uint32_t *seen = reinterpret_cast<uint32_t *>(wsum + S::kWarps * kHeads) + wid * S::kStages;  // keys of a stage that count
 
-    // Chunks beyond the row's end are read but never filled.
+    // ---- copies.  The lane's key of a tile is number lane mod 16; find() looks its page up, a tile ahead of fetch().
+    const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
+    const char *tb = LV ? (lane < 16 ? a.kt + kh * a.kt_head : a.vt + kh * a.vt_head) : nullptr;  // lanes 16 .. 31 fetch V's codebooks
+    const int64_t t_page = lane < 16 ? a.kt_page : a.vt_page, t_slot = lane < 16 ? a.kt_slot : a.vt_slot;
+    const int32_t *table = a.table + seq * a.table_row;
+    const bool whole = a.page_size % kTile == 0;  // a tile lies in one page
     const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
-    if (row_chunks < S::kChunks)
+    bool bad_page = false;
+    struct Found {
+        int page, slot;  // page -2: beyond the split, no error
+    };
+    auto find = [&](int t0) {
+        const int key = t0 + (lane & 15);
+        Found f{-2, 0};
+        if (key >= span.first && key < end) {
+            const int p = page_of(a, key);
+            f.slot = key - p * a.page_size;
+            f.page = table[p];
+        }
+        return f;
+    };
+    auto fetch = [&](Found f, int stage) {
+        char *dst = ring + stage * S::kBytes;
+        const bool ok = f.page >= 0 && f.page < a.pages;
+        bad_page |= f.page != -2 && !ok;
+        const uint32_t mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+        if (lane == 0) seen[stage] = mask;
+        if (whole && mask == 0xffffu) {  // sixteen neighbouring slots
+            const int slot0 = f.slot - (lane & 15);
+            const int r0 = lane / S::kChunks, c = lane % (S::kChunks < 32 ? S::kChunks : 32);
+            const char *kp = kb + f.page * a.k_page + (slot0 + r0) * a.k_slot + 16 * c;
+            const char *vp = vb + f.page * a.v_page + (slot0 + r0) * a.v_slot + 16 * c;
+#pragma unroll
+            for (int i = 0; i < S::kPieces; i++) {
+                // piece lane + 32 i: chunks come round in a row first
+                constexpr int kSame = S::kChunks > 32 ? S::kChunks / 32 : 1, kRows = S::kChunks > 32 ? 1 : 32 / S::kChunks;
+                const int r = r0 + i / kSame * kRows, cc = c + i % kSame * 32;
+                if (cc < row_chunks) {
+                    copy16(smem_addr(dst + S::k_at(r, cc)), kp + i % kSame * 512, true);
+                    copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), cc)), vp + i % kSame * 512, true);
+                }
+                if (i % kSame == kSame - 1) {
+                    kp += kRows * a.k_slot;
+                    vp += kRows * a.v_slot;
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < S::kPieces; i++) {
+                const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
+                const int64_t p = __shfl_sync(0xffffffffu, f.page, r), s = __shfl_sync(0xffffffffu, f.slot, r);
+                const bool read = mask >> r & 1;
+                if (c < row_chunks) {
+                    copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + p * a.k_page + s * a.k_slot + 16 * c : kb, read);
+                    copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), c)), read ? vb + p * a.v_page + s * a.v_slot + 16 * c : vb, read);
+                }
+            }
+        }
+        if (LV) {
+            const char *src = ok ? tb + f.page * t_page + f.slot * t_slot : tb;
+            char *to = dst + 2 * kTile * S::kRow + (lane < 16 ? lane : kTile + S::v_row(lane & 15)) * S::kBook;
+#pragma unroll
+            for (int i = 0; i < LV / 8; i++) copy16(smem_addr(to + 16 * i), src + 16 * i, ok);
+        }
+    };
+
+    // The first tiles are on their way before anything else: all their pages at once, then the rows.
+    const int step = kTile * S::kWarps;
+    const int mine = begin + kTile * wid;
+    // Chunks beyond the row's end are read but never filled.
+    if (row_chunks < S::kChunks) {
         for (int i = lane; i < S::kRing / 16; i += 32) reinterpret_cast<uint4 *>(ring)[i] = make_uint4(0, 0, 0, 0);
+        __syncwarp();
+    }
+    Found found[S::kStages];
+#pragma unroll
+    for (int i = 0; i < S::kStages; i++) found[i] = find(mine + i * step);
+#pragma unroll
+    for (int i = 0; i < S::kStages - 1; i++) {
+        if (mine + i * step < end) fetch(found[i], i);
+        copies_commit();
+    }
+    Found next_found = found[S::kStages - 1];
+    int next = mine + (S::kStages - 1) * step, fill = S::kStages - 1;
+
     const T *qp = static_cast<const T *>(a.q) + seq * a.q_row + h0 * a.q_head;
     if (S::kF32) {
         for (int i = threadIdx.x; i < kHeads * 64 * NV; i += 32 * S::kWarps) {
             const int h = i / (64 * NV), e = i % (64 * NV);
             qs[i] = h < nh && e < a.d ? to_f32(qp[h * a.q_head + e]) : 0.f;
         }
+        __syncthreads();
     }
-    __syncthreads();
-
-    // ---- copies
-    const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
-    const char *ktb = LV ? a.kt + kh * a.kt_head : nullptr, *vtb = LV ? a.vt + kh * a.vt_head : nullptr;
-    const int32_t *table = a.table + seq * a.table_row;
-    const bool whole = a.page_size % kTile == 0;  // a tile lies in one page
-    bool bad_page = false;
-    // Page and slot of the lane's key (key `lane` mod 16 of the tile) of the tile that is fetched next.
-    int page = 0, slot = 0;
-    auto find = [&](int t0) {
-        const int key = t0 + (lane & 15);
-        if (key < span.first || key >= end) { page = -2; slot = 0; return; }  // beyond: not an error
-        const int p = page_of(a, key);
-        slot = key - p * a.page_size;
-        page = table[p];
-    };
-    auto fetch = [&](int t0, int stage) {
-        char *dst = ring + stage * S::kBytes;
-        const bool ok = page >= 0 && page < a.pages;
-        if (page != -2 && !ok) bad_page = true;
-        const uint32_t mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
-        if (lane == 0) seen[stage] = mask;
-        int64_t kp = 0, vp = 0;
-        if (whole) {  // one page: the first counted key's
-            const int from = mask ? __ffs(mask) - 1 : 0;
-            const int64_t p = mask ? __shfl_sync(0xffffffffu, page, from) : 0;
-            const int s = __shfl_sync(0xffffffffu, slot, from) - from;
-            kp = p * a.k_page + s * a.k_slot;
-            vp = p * a.v_page + s * a.v_slot;
-        }
-#pragma unroll
-        for (int i = 0; i < S::kPieces; i++) {
-            const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
-            const bool read = mask >> r & 1;
-            int64_t ko, vo;
-            if (whole) {
-                ko = kp + r * a.k_slot;
-                vo = vp + r * a.v_slot;
-            } else {
-                const int64_t p = __shfl_sync(0xffffffffu, page, r), s = __shfl_sync(0xffffffffu, slot, r);
-                ko = p * a.k_page + s * a.k_slot;
-                vo = p * a.v_page + s * a.v_slot;
-            }
-            if (c < row_chunks) {
-                copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + ko + 16 * c : kb, read);
-                copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), c)), read ? vb + vo + 16 * c : vb, read);
-            }
-        }
-        if (LV) {  // codebooks: the lanes 0 .. 15 the keys', 16 .. 31 the values'
-            const int r = lane & 15;
-            const bool read = mask >> r & 1, isv = lane >= 16;
-            const int64_t p = read ? page : 0, s = read ? slot : 0;  // lanes 16 .. 31 hold the same keys
-            const char *src = isv ? vtb + p * a.vt_page + s * a.vt_slot : ktb + p * a.kt_page + s * a.kt_slot;
-            char *to = dst + 2 * kTile * S::kRow + (isv ? kTile * S::kBook + S::v_row(r) * S::kBook : r * S::kBook);
-#pragma unroll
-            for (int i = 0; i < LV / 8; i++) copy16(smem_addr(to + 16 * i), src + 16 * i, read);
-        }
-    };
-
-    // ---- state: maximum and sum of the heads 2t, 2t + 1 (the sums of this lane's keys alone), and O
-    float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, l0 = 0.f, l1 = 0.f;
-    constexpr int kOut = S::kF32 ? (NV == 4 ? 2 : 1) * kHeads * 4 : 16 * NV;
-    float o[kOut];
-#pragma unroll
-    for (int i = 0; i < kOut; i++) o[i] = 0.f;
     // 16-bit: q as the second operand of S^T, in the order of the lane's chunks of K
     constexpr int kSteps = S::kF32 ? 1 : 4 * NV;
     uint32_t qf[2 * kSteps];
     if (!S::kF32) {
         constexpr int kRun = LV ? (NV == 1 ? 16 : 32) : 8;  // consecutive entries of a lane's chunk
+        const int h = g * HT / 8;
 #pragma unroll
         for (int i = 0; i < 2 * kSteps; i++) {
             const int run = 2 * i / kRun, e = kRun * (t + 4 * run) + 2 * i % kRun;
-            const bool in = g < nh && e < a.d;
-            qf[i] = in ? pack2<T>(to_f32(qp[g * a.q_head + e]), to_f32(qp[g * a.q_head + e + 1])) : 0u;
+            const bool in = h < nh && e < a.d;
+            qf[i] = in ? pack2<T>(to_f32(qp[h * a.q_head + e]), to_f32(qp[h * a.q_head + e + 1])) : 0u;
         }
     }
 
-    const int step = kTile * S::kWarps;
-    int next = begin + kTile * wid, fill = 0;
-    find(next);
+    // ---- state: maximum and sum of the lane's heads (the sums of this lane's keys alone), and O
+    float m[HL], l[HL];
 #pragma unroll
-    for (int i = 0; i < S::kStages - 1; i++) {
-        if (next < end) {
-            fetch(next, fill);
-            find(next + step);
-        }
-        copies_commit();
-        next += step;
-        fill++;
+    for (int h = 0; h < HL; h++) {
+        m[h] = -CUDART_INF_F;
+        l[h] = 0.f;
     }
+    constexpr int kOut = S::kF32 ? (NV == 4 ? 2 : 1) * kHeads * 4 : 2 * HT * NV;
+    float o[kOut];
+#pragma unroll
+    for (int i = 0; i < kOut; i++) o[i] = 0.f;
+    // HT = 4: selectors that put one of a register's two weights on the even or on the odd index
+    const uint32_t sel0 = g & 1 ? 0x1044 : 0x4410, sel1 = g & 1 ? 0x3244 : 0x4432;
+
     int use = 0;
-    for (int t0 = begin + kTile * wid; t0 < end; t0 += step) {
+    for (int t0 = mine; t0 < end; t0 += step) {
         if (next < end) {
-            fetch(next, fill);
-            find(next + step);
+            fetch(next_found, fill);
+            next_found = find(next + step);
         }
         copies_commit();
         next += step;
@@ -325,8 +360,8 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         const char *kt = ring + use * S::kBytes, *vt = kt + kTile * S::kRow, *bk = vt + kTile * S::kRow, *bv = bk + kTile * S::kBook;
         const uint32_t mask = seen[use];
 
-        // ---- scores: c[0], c[1] of key g, c[2], c[3] of key g + 8, heads 2t and 2t + 1
-        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        // ---- scores: c[0][.] of key g, c[1][.] of key g + 8
+        float c[2][HL];
         if constexpr (S::kF32) {
             float v[2][kHeads];
 #pragma unroll
@@ -356,18 +391,18 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const float keep = t & 1 ? w[h + 2] : w[h], give = t & 1 ? w[h] : w[h + 2];
-                    c[2 * u + h] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+                    c[u][h % HL] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
                 }
             }
         } else {
-            float c2[4] = {0.f, 0.f, 0.f, 0.f};
+            float c1[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};
             if constexpr (LV == 0) {
 #pragma unroll
                 for (int i = 0; i < 2 * NV; i++) {
                     if (32 * i >= a.d) break;
                     const uint4 x = *reinterpret_cast<const uint4 *>(kt + S::k_at(g, t + 4 * i));
                     const uint4 y = *reinterpret_cast<const uint4 *>(kt + S::k_at(g + 8, t + 4 * i));
-                    mma16<T>(c, x.x, y.x, x.y, y.y, qf[4 * i], qf[4 * i + 1]);
+                    mma16<T>(c1, x.x, y.x, x.y, y.y, qf[4 * i], qf[4 * i + 1]);
                     mma16<T>(c2, x.z, y.z, x.w, y.w, qf[4 * i + 2], qf[4 * i + 3]);
                 }
             } else {
@@ -391,7 +426,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                         uint32_t xl, xh, yl, yh;
                         b0.template look<0>(x[w], xl, xh);
                         b1.template look<0>(y[w], yl, yh);
-                        mma16<T>(c, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[0], q4[1]);
+                        mma16<T>(c1, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[0], q4[1]);
                         b0.template look<1>(x[w], xl, xh);
                         b1.template look<1>(y[w], yl, yh);
                         mma16<T>(c2, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[2], q4[3]);
@@ -399,58 +434,67 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; i++) c[i] += c2[i];
+            for (int h = 0; h < HL; h++) {
+                c[0][h] = c1[h] + c2[h];
+                c[1][h] = c1[2 + h] + c2[2 + h];
+            }
         }
 
         // ---- running maximum, weights, sums
 #pragma unroll
-        for (int i = 0; i < 4; i++) c[i] *= a.scale2;
+        for (int h = 0; h < HL; h++) {
+            c[0][h] *= a.scale2;
+            c[1][h] *= a.scale2;
+        }
         if (mask != 0xffffu) {  // rows that are not seen hold zeros; their scores do not count
-            if (!(mask >> g & 1)) c[0] = c[1] = -CUDART_INF_F;
-            if (!(mask >> (g + 8) & 1)) c[2] = c[3] = -CUDART_INF_F;
-        }
-        float n0 = fmaxf(c[0], c[2]), n1 = fmaxf(c[1], c[3]);
 #pragma unroll
-        for (int x = 4; x < 32; x *= 2) {
-            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, x));
-            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, x));
+            for (int h = 0; h < HL; h++) {
+                if (!(mask >> g & 1)) c[0][h] = -CUDART_INF_F;
+                if (!(mask >> (g + 8) & 1)) c[1][h] = -CUDART_INF_F;
+            }
         }
-        n0 = fmaxf(n0, m0);
-        n1 = fmaxf(n1, m1);
-        // with no weight yet (maximum -inf) the exponents are taken from 0
-        const float base0 = n0 == -CUDART_INF_F ? 0.f : n0, base1 = n1 == -CUDART_INF_F ? 0.f : n1;
-        if (__any_sync(0xffffffffu, n0 != m0 || n1 != m1)) {
-            const float s0 = exp2_fast(m0 - base0), s1 = exp2_fast(m1 - base1);
-            l0 *= s0;
-            l1 *= s1;
+        float top[HL], base[HL];
+        bool moved = false;
+#pragma unroll
+        for (int h = 0; h < HL; h++) {
+            top[h] = fmaxf(c[0][h], c[1][h]);
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], x));
+            top[h] = fmaxf(top[h], m[h]);
+            base[h] = top[h] == -CUDART_INF_F ? 0.f : top[h];  // with no weight yet the exponents are taken from 0
+            moved |= top[h] != m[h];
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+            float s[HL];
+#pragma unroll
+            for (int h = 0; h < HL; h++) {
+                s[h] = exp2_fast(m[h] - base[h]);
+                l[h] *= s[h];
+                m[h] = top[h];
+            }
             if constexpr (S::kF32) {
 #pragma unroll
                 for (int h = 0; h < kHeads; h++) {  // this lane holds some entries of all heads
-                    const float sh = __shfl_sync(0xffffffffu, h & 1 ? s1 : s0, h >> 1);
+                    const float sh = __shfl_sync(0xffffffffu, s[h % HL], h / HL);
 #pragma unroll
                     for (int i = 0; i < kOut / kHeads; i++) o[h * (kOut / kHeads) + i] *= sh;
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < kOut; i += 2) {
-                    o[i] *= s0;
-                    o[i + 1] *= s1;
-                }
+                for (int i = 0; i < kOut; i++) o[i] *= s[i % HL];
             }
-            m0 = n0;
-            m1 = n1;
         }
-        c[0] = exp2_fast(c[0] - base0);
-        c[1] = exp2_fast(c[1] - base1);
-        c[2] = exp2_fast(c[2] - base0);
-        c[3] = exp2_fast(c[3] - base1);
-        l0 += c[0] + c[2];
-        l1 += c[1] + c[3];
+#pragma unroll
+        for (int h = 0; h < HL; h++) {
+            c[0][h] = exp2_fast(c[0][h] - base[h]);
+            c[1][h] = exp2_fast(c[1][h] - base[h]);
+            l[h] += c[0][h] + c[1][h];
+        }
 
         // ---- values
         if constexpr (S::kF32) {
-            *reinterpret_cast<float2 *>(ps + g * kHeads + 2 * t) = make_float2(c[0], c[1]);
-            *reinterpret_cast<float2 *>(ps + (g + 8) * kHeads + 2 * t) = make_float2(c[2], c[3]);
+            *reinterpret_cast<float2 *>(ps + g * kHeads + 2 * t) = make_float2(c[0][0], c[0][HL - 1]);
+            *reinterpret_cast<float2 *>(ps + (g + 8) * kHeads + 2 * t) = make_float2(c[1][0], c[1][HL - 1]);
             __syncwarp();
             constexpr int kLanes = NV == 1 ? 16 : 32, kRows = 32 / kLanes, kCols = NV == 4 ? 2 : 1;
 #pragma unroll 4
@@ -472,34 +516,52 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                 }
             }
         } else {
-            // P^T as second operand: keys 2t, 2t + 1 (and + 8) of head g, in two parts
-            uint32_t b[4];
-            {
-                const uint32_t h01 = pack2<T>(c[0], c[1]), h23 = pack2<T>(c[2], c[3]);
-                const float2 f01 = unpack2<T>(h01), f23 = unpack2<T>(h23);
-                b[0] = transpose8x8(h01);
-                b[1] = transpose8x8(h23);
-                b[2] = transpose8x8(pack2<T>(c[0] - f01.x, c[1] - f01.y));
-                b[3] = transpose8x8(pack2<T>(c[2] - f23.x, c[3] - f23.y));
+            // The weights as second operand, high parts and low parts.  After the transposition the lane holds those
+            // of the keys 2t, 2t + 1 and of 2t + 8, 2t + 9, of head g or (HT = 4) g / 2.
+            uint32_t hi[HT == 4 ? 4 : 2], lo[HT == 4 ? 4 : 2];
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const uint32_t h = pack2<T>(c[u][0], c[u][HL - 1]);
+                const float2 f = unpack2<T>(h);
+                const uint32_t th = transpose8x8(h), tl = transpose8x8(pack2<T>(c[u][0] - f.x, c[u][HL - 1] - f.y));
+                if constexpr (HT == 4) {
+                    hi[2 * u] = prmt(th, 0, sel0);
+                    hi[2 * u + 1] = prmt(th, 0, sel1);
+                    lo[2 * u] = prmt(tl, 0, sel0);
+                    lo[2 * u + 1] = prmt(tl, 0, sel1);
+                } else {
+                    hi[u] = th;
+                    lo[u] = tl;
+                }
             }
-            // o[4 j ..]: two entries of the row (of head 2t, 2t + 1 each)
-            auto put = [&](int j, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
-                float(&acc)[4] = *reinterpret_cast<float(*)[4]>(o + 4 * j);
-                mma16<T>(acc, a0, a1, a2, a3, b[0], b[1]);
-                mma16<T>(acc, a0, a1, a2, a3, b[2], b[3]);
+            // x[r]: four neighbouring entries (two registers) of the lane's key r; they go to o[HT j ..].
+            auto put = [&](int j, const uint32_t (&x)[4][2]) {
+                if constexpr (HT == 4) {
+                    float(&acc)[4] = *reinterpret_cast<float(*)[4]>(o + 4 * j);
+                    mma16<T>(acc, x[0][0], x[0][1], x[1][0], x[1][1], hi[0], hi[1]);
+                    mma16<T>(acc, x[2][0], x[2][1], x[3][0], x[3][1], hi[2], hi[3]);
+                    mma16<T>(acc, x[0][0], x[0][1], x[1][0], x[1][1], lo[0], lo[1]);
+                    mma16<T>(acc, x[2][0], x[2][1], x[3][0], x[3][1], lo[2], lo[3]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 2; u++) {
+                        float(&acc)[4] = *reinterpret_cast<float(*)[4]>(o + 8 * j + 4 * u);
+                        const uint32_t a0 = prmt(x[0][u], x[1][u], 0x5410), a1 = prmt(x[0][u], x[1][u], 0x7632);
+                        const uint32_t a2 = prmt(x[2][u], x[3][u], 0x5410), a3 = prmt(x[2][u], x[3][u], 0x7632);
+                        mma16<T>(acc, a0, a1, a2, a3, hi[0], hi[1]);
+                        mma16<T>(acc, a0, a1, a2, a3, lo[0], lo[1]);
+                    }
+                }
             };
             if constexpr (LV == 0) {
 #pragma unroll
                 for (int i = 0; i < NV; i++) {
                     if (64 * i >= a.d) break;
-                    alignas(16) uint32_t x[4][4];
+                    uint4 x[4];
 #pragma unroll
-                    for (int r = 0; r < 4; r++)
-                        *reinterpret_cast<uint4 *>(x[r]) = *reinterpret_cast<const uint4 *>(vt + S::v_at(t + 4 * r, g + 8 * i));
-#pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        put(4 * i + j, prmt(x[0][j], x[1][j], 0x5410), prmt(x[0][j], x[1][j], 0x7632), prmt(x[2][j], x[3][j], 0x5410),
-                            prmt(x[2][j], x[3][j], 0x7632));
+                    for (int r = 0; r < 4; r++) x[r] = *reinterpret_cast<const uint4 *>(vt + S::v_at(t + 4 * r, g + 8 * i));
+                    put(2 * i, {{x[0].x, x[0].y}, {x[1].x, x[1].y}, {x[2].x, x[2].y}, {x[3].x, x[3].y}});
+                    put(2 * i + 1, {{x[0].z, x[0].w}, {x[1].z, x[1].w}, {x[2].z, x[2].w}, {x[3].z, x[3].w}});
                 }
             } else {
                 Book<LV> bb[4];
@@ -514,18 +576,15 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                 }
                 auto half = [&](int w, auto hh) {
                     constexpr int H = decltype(hh)::value;
-                    uint32_t p[4][2];  // entries 0, 1 and 2, 3 of each key
+                    uint32_t p[4][2];
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        uint32_t lo, hi;
-                        bb[r].template look<H>(x[r][w], lo, hi);
-                        p[r][0] = prmt(lo, hi, 0x5140);
-                        p[r][1] = prmt(lo, hi, 0x7362);
+                        uint32_t bl, bh;
+                        bb[r].template look<H>(x[r][w], bl, bh);
+                        p[r][0] = prmt(bl, bh, 0x5140);
+                        p[r][1] = prmt(bl, bh, 0x7362);
                     }
-#pragma unroll
-                    for (int u = 0; u < 2; u++)
-                        put(4 * w + 2 * H + u, prmt(p[0][u], p[1][u], 0x5410), prmt(p[0][u], p[1][u], 0x7632),
-                            prmt(p[2][u], p[3][u], 0x5410), prmt(p[2][u], p[3][u], 0x7632));
+                    put(2 * w + H, p);
                 };
 #pragma unroll
                 for (int w = 0; w < NV; w++) {
@@ -539,33 +598,32 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     }
     copies_wait<0>();
     if (bad_page && a.status) atomicOr(a.status, ECASQ_BAD_PAGE);
+    if (a.splits > 1) asm volatile("griddepcontrol.launch_dependents;");
 
     // ---- the block's warps: maxima and sums, then each warp's O shrunk to the common maximum
 #pragma unroll
-    for (int x = 4; x < 32; x *= 2) {
-        l0 += __shfl_xor_sync(0xffffffffu, l0, x);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, x);
-    }
-    if (g == 0) {
-        wmax[wid * kHeads + 2 * t] = m0;
-        wmax[wid * kHeads + 2 * t + 1] = m1;
-        wsum[wid * kHeads + 2 * t] = l0;
-        wsum[wid * kHeads + 2 * t + 1] = l1;
+    for (int h = 0; h < HL; h++) {
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
+        if (g == 0) {
+            wmax[wid * kHeads + HL * t + h] = m[h];
+            wsum[wid * kHeads + HL * t + h] = l[h];
+        }
     }
     __syncthreads();
-    auto top = [&](int h) {
-        float m = wmax[h];
-        for (int w = 1; w < S::kWarps; w++) m = fmaxf(m, wmax[w * kHeads + h]);
-        return m;
+    auto top_of = [&](int h) {
+        float x = wmax[h];
+        for (int w = 1; w < S::kWarps; w++) x = fmaxf(x, wmax[w * kHeads + h]);
+        return x;
     };
-    auto shrink = [&](int w, int h, float m) { return m == -CUDART_INF_F ? 0.f : exp2_fast(wmax[w * kHeads + h] - m); };
+    auto shrink = [&](int w, int h, float x) { return x == -CUDART_INF_F ? 0.f : exp2_fast(wmax[w * kHeads + h] - x); };
     constexpr int kWide = 64 * NV;
-    float *mine = reinterpret_cast<float *>(ring);
+    float *own = reinterpret_cast<float *>(ring);
     if constexpr (S::kF32) {
         constexpr int kLanes = NV == 1 ? 16 : 32, kCols = NV == 4 ? 2 : 1;
 #pragma unroll
         for (int h = 0; h < kHeads; h++) {
-            const float sh = shrink(wid, h, top(h));
+            const float sh = shrink(wid, h, top_of(h));
 #pragma unroll
             for (int i = 0; i < kCols; i++) {
                 float *oh = o + (h * kCols + i) * 4;
@@ -576,58 +634,75 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                     x.z += __shfl_xor_sync(0xffffffffu, x.z, 16);
                     x.w += __shfl_xor_sync(0xffffffffu, x.w, 16);
                 }
-                if (lane < kLanes) *reinterpret_cast<float4 *>(mine + h * kWide + 4 * (lane + 32 * i)) = x;
+                if (lane < kLanes) *reinterpret_cast<float4 *>(own + h * kWide + 4 * (lane + 32 * i)) = x;
             }
         }
     } else {
-        const float s0 = shrink(wid, 2 * t, top(2 * t)), s1 = shrink(wid, 2 * t + 1, top(2 * t + 1));
+        float s[HL];
 #pragma unroll
-        for (int j = 0; j < 4 * NV; j++) {
-            // plain: entries 8 (g + 8 i) + 2 j', coded: 8 NV g + 2 j
-            const int e = LV ? 8 * NV * g + 2 * j : 8 * (g + 8 * (j >> 2)) + 2 * (j & 3);
-            *reinterpret_cast<float2 *>(mine + 2 * t * kWide + e) = make_float2(o[4 * j] * s0, o[4 * j + 2] * s0);
-            *reinterpret_cast<float2 *>(mine + (2 * t + 1) * kWide + e) = make_float2(o[4 * j + 1] * s1, o[4 * j + 3] * s1);
+        for (int h = 0; h < HL; h++) s[h] = shrink(wid, HL * t + h, top_of(HL * t + h));
+#pragma unroll
+        for (int j = 0; j < 2 * NV; j++) {
+            // four entries of the lane's heads: plain 8 (g + 8 i) + 4 (j mod 2), i = j div 2; coded 8 NV g + 4 j
+            const int e = LV ? 8 * NV * g + 4 * j : 8 * (g + 8 * (j >> 1)) + 4 * (j & 1);
+            const float *x = o + HT * j;
+            if constexpr (HT == 4) {
+                *reinterpret_cast<float4 *>(own + t * kWide + e) = make_float4(x[0] * s[0], x[1] * s[0], x[2] * s[0], x[3] * s[0]);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+                    *reinterpret_cast<float4 *>(own + (2 * t + h) * kWide + e) =
+                        make_float4(x[h] * s[h % HL], x[2 + h] * s[h % HL], x[4 + h] * s[h % HL], x[6 + h] * s[h % HL]);
+            }
         }
     }
     __syncthreads();
     const PartAt at(a.d);
-    for (int h = 0; h < nh; h++) {
-        const float m = top(h);
-        float l = 0.f;
-        for (int w = 0; w < S::kWarps; w++) l += wsum[w * kHeads + h] * shrink(w, h, m);
-        float *part = a.splits > 1 ? at.at(a.part, seq, a.heads, h0 + h, a.splits, split) : nullptr;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        for (int e = threadIdx.x; e < a.d; e += 32 * S::kWarps) {
-            float x = 0.f;
+    const int quads = a.d / 4;  // four entries a thread
+    for (int i = threadIdx.x; i < nh * quads; i += 32 * S::kWarps) {
+        const int h = i / quads, e = 4 * (i % quads);
+        const float x = top_of(h);
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < S::kWarps; w++) x += reinterpret_cast<const float *>(smem + w * S::kRing)[h * kWide + e];
-            if (part) part[e] = x;
-            else static_cast<T *>(a.out)[seq * a.out_row + (h0 + h) * a.out_head + e] = from_f32<T>(l == 0.f ? 0.f : x * inv);
+        for (int w = 0; w < S::kWarps; w++) {
+            sum += wsum[w * kHeads + h] * shrink(w, h, x);
+            const float4 y = *reinterpret_cast<const float4 *>(smem + w * S::kRing + 4 * (h * kWide + e));
+            v.x += y.x;
+            v.y += y.y;
+            v.z += y.z;
+            v.w += y.w;
         }
-        if (threadIdx.x == 0) {
-            if (part) {
-                part[a.d] = m;
-                part[a.d + 1] = l;
-            } else if (a.lse) a.lse[seq * a.heads + h0 + h] = l == 0.f ? -CUDART_INF_F : m * kLn2 + logf(l);
+        if (a.splits > 1) {
+            float *part = at.at(a.part, seq, a.heads, h0 + h, a.splits, split);
+            *reinterpret_cast<float4 *>(part + e) = v;
+            if (e == 0) *reinterpret_cast<float2 *>(part + a.d) = make_float2(x, sum);
+        } else {
+            store_out<T>(a, seq, h0 + h, e, v, sum);
+            if (e == 0 && a.lse) a.lse[seq * a.heads + h0 + h] = log_sum(x, sum);
         }
     }
 }
 
-template <typename T, int LV, int NV>
+template <typename T, int LV, int NV, int HT>
 static int launch_attend(const AttendArgs &a, int64_t b, cudaStream_t st) {
     using S = Shape<T, LV, NV>;
-    ECASQ_CUDA_TRY(cudaFuncSetAttribute(k_attend<T, LV, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+    ECASQ_CUDA_TRY(cudaFuncSetAttribute(k_attend<T, LV, NV, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
     const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
     note_launch();
-    k_attend<T, LV, NV><<<grid, 32 * S::kWarps, S::kSmem, st>>>(a);
+    k_attend<T, LV, NV, HT><<<grid, 32 * S::kWarps, S::kSmem, st>>>(a);
     ECASQ_LAUNCH_CHECK();
     return ECASQ_OK;
 }
-template <typename T, int LV>
+template <typename T, int LV, int HT>
 static int launch_attend_rows(const AttendArgs &a, int64_t b, cudaStream_t st) {
-    if (a.d <= 64) return launch_attend<T, LV, 1>(a, b, st);
-    if (a.d <= 128) return launch_attend<T, LV, 2>(a, b, st);
-    return launch_attend<T, LV, 4>(a, b, st);
+    if (a.d <= 64) return launch_attend<T, LV, 1, HT>(a, b, st);
+    if (a.d <= 128) return launch_attend<T, LV, 2, HT>(a, b, st);
+    return launch_attend<T, LV, 4, HT>(a, b, st);
+}
+template <typename T, int LV>
+static int launch_attend_heads(const AttendArgs &a, int64_t b, cudaStream_t st) {
+    return a.group <= 4 ? launch_attend_rows<T, LV, 4>(a, b, st) : launch_attend_rows<T, LV, 8>(a, b, st);
 }
 
 // One translation unit each.

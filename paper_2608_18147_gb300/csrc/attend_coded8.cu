@@ -3,6 +3,6 @@
 
 namespace ecasq {
 int launch_attend_coded8(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st) {
-    return bf16 ? launch_attend_rows<__nv_bfloat16, 8>(a, b, st) : launch_attend_rows<__half, 8>(a, b, st);
+    return bf16 ? launch_attend_heads<__nv_bfloat16, 8>(a, b, st) : launch_attend_heads<__half, 8>(a, b, st);
 }
 }  // namespace ecasq
