@@ -6,21 +6,32 @@
 namespace ecasq {
 
 // Splits.  A block has a fixed cost of its own (its first loads' latency, the join), so a split should be long; and the
-// blocks should fill the card evenly.  kSlots blocks run at once; up to kLong keys for each of them there is
+// blocks should fill the card evenly.  `slots` blocks run at once; up to kLong keys for each of them there is
 // one round of blocks, beyond that as many rounds as keep a split at most about that long.
-constexpr int kSlots = 3 * 152, kLong = 1024, kStep = 64;
+constexpr int kSms = 152, kMostResident = 8, kLong = 1024, kStep = 64;
 
 struct Splits {
     int32_t chunk, count;
 };
-static Splits make_splits(int64_t b, int64_t blocks, int64_t max_len) {
-    const int64_t per = cdiv(b * blocks * max_len, kSlots);
-    const int64_t want = std::max<int64_t>(1, cdiv(per, cdiv(std::max<int64_t>(per, 1), kLong)));
+static Splits make_splits(int64_t b, int64_t blocks, int64_t max_len, int64_t slots) {
+    const int64_t per = std::max<int64_t>(1, cdiv(b * blocks * max_len, slots));
+    const int64_t want = cdiv(per, cdiv(per, kLong));
     // Splits count from the tile of the first key, so one more tile than max_len may be needed.
     const int64_t span = max_len + kTile - 1;
     const int64_t count = std::min<int64_t>(std::max<int64_t>(1, cdiv(span, cdiv(want, kStep) * kStep)), 65535);
     const int64_t chunk = cdiv(cdiv(span, count), kStep) * kStep;
     return {(int32_t)chunk, (int32_t)cdiv(span, chunk)};
+}
+static size_t part_bytes(int64_t b, int64_t heads, int32_t d, int64_t splits) { return (size_t)(b * heads * splits * PartAt(d).stride) * 4; }
+
+int split_attend(AttendArgs &a, int64_t b, int resident) {
+    const Splits s = make_splits(b, (int64_t)(a.heads / a.group) * a.htiles, a.max_len, kSms * std::min(resident, kMostResident));
+    a.chunk = s.chunk;
+    a.splits = s.count;
+    if (a.splits == 1) return ECASQ_OK;
+    if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, a.d, a.splits)) return ECASQ_EWORKSPACE;
+    a.part = static_cast<float *>(a.ws);
+    return ECASQ_OK;
 }
 
 // A block a sequence and query head: the splits' maxima and sums give each split's share, then 16 to 64 lanes a split add
@@ -118,8 +129,11 @@ extern "C" {
 
 size_t ecasq_workspace_size_attend(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {
     if (!sizes_ok(b, heads, kv_heads, d, max_len)) return 0;
-    const Splits s = make_splits(b, (int64_t)kv_heads * cdiv(heads / kv_heads, kHeads), max_len);
-    return s.count > 1 ? (size_t)(b * heads * s.count * PartAt(d).stride) * 4 : 0;
+    // The most splits over what an SM may hold of the kernels.
+    const int64_t blocks = (int64_t)kv_heads * cdiv(heads / kv_heads, kHeads);
+    int64_t most = 1;
+    for (int r = 1; r <= kMostResident; r++) most = std::max<int64_t>(most, make_splits(b, blocks, max_len, kSms * r).count);
+    return most > 1 ? part_bytes(b, heads, d, most) : 0;
 }
 
 int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_t heads, const ecasq_cache_t *k,
@@ -170,17 +184,11 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     a.d = k->d;
     a.page_size = k->page_size;
     a.max_len = (int32_t)max_len;
-    const Splits s = make_splits(b, (int64_t)k->heads * a.htiles, max_len);
-    a.chunk = s.chunk;
-    a.splits = s.count;
+    a.ws = ws;
+    a.ws_bytes = ws_bytes;
     const FastDiv div(k->page_size);
     a.div_mul = div.mul;
     a.div_shift = div.shift;
-    if (a.splits > 1) {
-        if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || ws_bytes < (size_t)(b * heads * a.splits * PartAt(a.d).stride) * 4)
-            return ECASQ_EWORKSPACE;
-        a.part = static_cast<float *>(ws);
-    }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool bf16 = k->type == ECASQ_BF16;
     int rc;

@@ -29,6 +29,7 @@
 // fp32 rows: fp32 products on the FMA pipe in the same frame.
 #pragma once
 
+#include <atomic>
 #include <type_traits>
 
 #include "codes.cuh"
@@ -44,6 +45,8 @@ struct AttendArgs {
     void *out;
     const int32_t *table, *lengths, *starts;
     float *lse, *part;           // part: splits' results, see PartAt
+    void *ws;
+    size_t ws_bytes;
     int32_t *status;
     const char *k, *v, *kt, *vt; // rows and codebooks
     int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;          // strides in bytes
@@ -62,6 +65,9 @@ struct PartAt {
         return part + ((seq * heads + head) * splits + split) * stride;
     }
 };
+
+// Sets a.chunk, a.splits and, where there are several, a.part from the workspace; `resident`: blocks that an SM holds.
+int split_attend(AttendArgs &a, int64_t b, int resident);
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // 16 bytes to shared memory, or 16 zero bytes (src is not read then).
@@ -272,14 +278,16 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                 }
             }
         } else {
-#pragma unroll 1
+            // lanes 0 .. 15 hold where the rows of K begin, 16 .. 31 those of V
+            const int64_t row = !ok ? 0 : lane < 16 ? f.page * a.k_page + f.slot * a.k_slot : f.page * a.v_page + f.slot * a.v_slot;
+#pragma unroll
             for (int i = 0; i < S::kPieces; i++) {
                 const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
-                const int64_t p = __shfl_sync(0xffffffffu, f.page, r), s = __shfl_sync(0xffffffffu, f.slot, r);
-                const bool read = mask >> r & 1;
+                const int64_t ko = __shfl_sync(0xffffffffu, row, r), vo = __shfl_sync(0xffffffffu, row, 16 + r);
                 if (c < row_chunks) {
-                    copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + p * a.k_page + s * a.k_slot + 16 * c : kb, read);
-                    copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), c)), read ? vb + p * a.v_page + s * a.v_slot + 16 * c : vb, read);
+                    const bool read = mask >> r & 1;
+                    copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + ko + 16 * c : kb, read);
+                    copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), c)), read ? vb + vo + 16 * c : vb, read);
                 }
             }
         }
@@ -684,10 +692,31 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     }
 }
 
+// Blocks of a kernel that an SM holds; 0 if the query fails.
 template <typename T, int LV, int NV, int HT>
-static int launch_attend(const AttendArgs &a, int64_t b, cudaStream_t st) {
+static int prepare_attend() {
     using S = Shape<T, LV, NV>;
-    ECASQ_CUDA_TRY(cudaFuncSetAttribute(k_attend<T, LV, NV, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+    int n = 0;
+    if (cudaFuncSetAttribute(k_attend<T, LV, NV, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attend<T, LV, NV, HT>, 32 * S::kWarps, S::kSmem) != cudaSuccess) return 0;
+    return n;
+}
+constexpr int kDevices = 16;
+// Splits the sequences (split_attend) and launches.
+template <typename T, int LV, int NV, int HT>
+static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
+    using S = Shape<T, LV, NV>;
+    static std::atomic<int> known[kDevices];  // by device, once each
+    int device = 0;
+    ECASQ_CUDA_TRY(cudaGetDevice(&device));
+    int resident = device < kDevices ? known[device].load(std::memory_order_acquire) : 0;
+    if (resident < 1) {
+        resident = prepare_attend<T, LV, NV, HT>();
+        if (resident < 1) return ECASQ_ECUDA;
+        if (device < kDevices) known[device].store(resident, std::memory_order_release);
+    }
+    const int rc = split_attend(a, b, resident);
+    if (rc) return rc;
     const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
     note_launch();
     k_attend<T, LV, NV, HT><<<grid, 32 * S::kWarps, S::kSmem, st>>>(a);
@@ -695,20 +724,20 @@ static int launch_attend(const AttendArgs &a, int64_t b, cudaStream_t st) {
     return ECASQ_OK;
 }
 template <typename T, int LV, int HT>
-static int launch_attend_rows(const AttendArgs &a, int64_t b, cudaStream_t st) {
+static int launch_attend_rows(AttendArgs &a, int64_t b, cudaStream_t st) {
     if (a.d <= 64) return launch_attend<T, LV, 1, HT>(a, b, st);
     if (a.d <= 128) return launch_attend<T, LV, 2, HT>(a, b, st);
     return launch_attend<T, LV, 4, HT>(a, b, st);
 }
 template <typename T, int LV>
-static int launch_attend_heads(const AttendArgs &a, int64_t b, cudaStream_t st) {
+static int launch_attend_heads(AttendArgs &a, int64_t b, cudaStream_t st) {
     return a.group <= 4 ? launch_attend_rows<T, LV, 4>(a, b, st) : launch_attend_rows<T, LV, 8>(a, b, st);
 }
 
 // One translation unit each.
-int launch_attend_f32(const AttendArgs &a, int64_t b, cudaStream_t st);
-int launch_attend_16(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
-int launch_attend_coded8(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
-int launch_attend_coded16(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
+int launch_attend_f32(AttendArgs &a, int64_t b, cudaStream_t st);
+int launch_attend_16(AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
+int launch_attend_coded8(AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
+int launch_attend_coded16(AttendArgs &a, bool bf16, int64_t b, cudaStream_t st);
 
 }  // namespace ecasq

@@ -2,7 +2,7 @@
 #include "attend.cuh"
 
 namespace ecasq {
-int launch_attend_coded16(const AttendArgs &a, bool bf16, int64_t b, cudaStream_t st) {
+int launch_attend_coded16(AttendArgs &a, bool bf16, int64_t b, cudaStream_t st) {
     return bf16 ? launch_attend_heads<__nv_bfloat16, 16>(a, b, st) : launch_attend_heads<__half, 16>(a, b, st);
 }
 }  // namespace ecasq

@@ -2,5 +2,5 @@
 #include "attend.cuh"
 
 namespace ecasq {
-int launch_attend_f32(const AttendArgs &a, int64_t b, cudaStream_t st) { return launch_attend_rows<float, 0, 8>(a, b, st); }
+int launch_attend_f32(AttendArgs &a, int64_t b, cudaStream_t st) { return launch_attend_rows<float, 0, 8>(a, b, st); }
 }  // namespace ecasq
