@@ -400,6 +400,7 @@ int ecasq_prepare(const float *x, int64_t d, void *ws, size_t ws_bytes, float *v
 #define ECASQ_BAD_LENGTH 2 /* a sequence longer than max_len (cut to it) */
 #define ECASQ_BAD_COUNT 4  /* a codebook's m outside [1, s] (clamped) */
 #define ECASQ_BAD_VALUE 8  /* a cache row with NaN or Inf (NaN takes code 0, Inf an end of the codebook) */
+#define ECASQ_BAD_WAIT 16  /* a bounded wait for a copy into shared memory ran out (the outputs concerned are NaN) */
 
 /* Indices of ecasq_quantize (one byte each, < 16; only the low four bits are read)
  * as the packed rows that ecasq_matvec reads.  Row r of `codes` has
@@ -430,7 +431,7 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
  * alignment. */
 int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
                  const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
-                 int64_t k, int32_t group, void *y, int64_t y_row, ecasq_stream_t stream);
+                 int64_t k, int32_t group, void *y, int64_t y_row, int32_t *status, ecasq_stream_t stream);
 
 /* One side (the keys or the values) of a paged cache.  Slot t of a sequence is slot
  * t mod page_size of its page t div page_size; a page has a row of d values for each

@@ -7,7 +7,7 @@ ecasq_dp_pass, ecasq_refine, ecasq_quantize, ecasq_solve_batched, ...).
 There is no CPU fallback: without libecasq.so and a GPU every call raises.
 """
 from . import workloads
-from .native import (BAD_COUNT, BAD_LENGTH, BAD_PAGE, BAD_VALUE, DP_REFERENCE, EXACT_S, EXACT_TABLES, NO_REFINE_GUARD, ONE_PART_PUBLISH, RESIDENT_COSTS,
+from .native import (BAD_COUNT, BAD_LENGTH, BAD_PAGE, BAD_VALUE, BAD_WAIT, DP_REFERENCE, EXACT_S, EXACT_TABLES, NO_REFINE_GUARD, ONE_PART_PUBLISH, RESIDENT_COSTS,
                      STREAMED_COSTS, TEST_SELF_SEED, TEST_SHORT_PARTS, TEST_STALL, UNSEEDED_SEARCH,
                      TIME_KERNELS,
                      EcasqError,
@@ -23,5 +23,5 @@ __all__ = ["workloads", "ecasq_solve", "ecasq_solve_grid", "ecasq_solve_timeshar
            "ecasq_workspace_size_flags", "ecasq_kernel_launches", "workspace", "uniform_grid", "lib", "EcasqError",
            "EXACT_S", "EXACT_TABLES", "RESIDENT_COSTS", "NO_REFINE_GUARD", "DP_REFERENCE", "TIME_KERNELS", "TEST_STALL", "STREAMED_COSTS", "ONE_PART_PUBLISH",
            "ecasq_pack", "ecasq_matvec", "ecasq_cache_write", "ecasq_attend", "workspace_attend",
-           "BAD_PAGE", "BAD_LENGTH", "BAD_COUNT", "BAD_VALUE",
+           "BAD_PAGE", "BAD_LENGTH", "BAD_COUNT", "BAD_VALUE", "BAD_WAIT",
            "UNSEEDED_SEARCH", "TEST_SELF_SEED", "TEST_SHORT_PARTS"]

@@ -1,5 +1,7 @@
 // matvec.cu -- products with a matrix of 4-bit codes (ecasq_pack, ecasq_matvec).
 #include <algorithm>
+#include <cstring>
+#include <type_traits>
 
 #include "codes.cuh"
 
@@ -28,47 +30,78 @@ struct MatvecArgs {
     const void *x, *levels, *scales;
     const uint8_t *codes;
     void *y;
+    int32_t *status;
     int64_t x_row, code_row, scale_row, y_row, n, k;
     int32_t b, m, groups;
-    int32_t warps_k;              // warps that share a row tile along k, a power of two
-    int32_t chunk;                // columns of x in shared memory at a time, a multiple of 128
-    int32_t x_pitch;              // elements from one row of x to the next there
+    int32_t warps_k;              // warps that share a row tile along k, a power of two; the others take other tiles
+    int32_t chunk;                // columns that one pass over the rows covers, a multiple of 128
+    int32_t stages;               // stages of the codes' ring
     uint32_t div_mul, div_shift;  // words of 32 columns to scale groups: w div (group / 32), as umulhi(w, div_mul) >> div_shift
                                   // or w >> div_shift if div_mul is 0
 };
 
-// One block takes a run of rows, sixteen at a time, and up to eight rows of x; its warps share a tile's 128-column
-// blocks and, where there are few of those, its tiles.
+// One block takes a run of rows and up to eight rows of x.  Its 16 warps share the 128-column blocks of a tile of
+// sixteen rows and, where there are few of those, take several tiles at once; a stage of the ring holds those tiles' rows,
+// brought in by one bulk copy a row a few stages ahead, and one barrier a stage joins the sums and frees it.
 //
-// What bounds it: the codes' bytes in the end, and on the way there shared memory: a byte of codes is two weights, and
-// one lookup in a table of all 256 pairs of levels gives both.  The table is held once a lane (entry e of
-// lane l at word 32 e + l), so that no two lanes meet in a bank; 32 lookups, 4 to 16 reads of x and the
-// codes' own 8 transactions for each KB of codes stand against the 44 clocks that memory needs for it.
+// What bounds it: the codes' bytes in the end, and on the way there shared memory and the issue slots: a byte of codes is
+// two weights, and one lookup in a table of all 256 pairs of levels gives both.  The table is held once a lane
+// (entry e of lane l at word 32 e + l), so that no two lanes meet in a bank; 32 lookups, 8 transactions for the
+// codes themselves and up to 8 for the scales stand, for each KB of codes, against the 44 clocks that memory needs for it.
 //
 // 16-bit types: a pair of weights is an operand register of mma.m16n8k16 as it stands, with the rows of x as its
 // eight columns and fp32 sums.  The order of the columns within a product is free, and the packed layout is
-// made for it: a lane (g, t) = (lane / 4, lane mod 4) loads 16 bytes of row g, words t, t + 4, t + 8 and t + 12 of the
+// made for it: a lane (g, t) = (lane / 4, lane mod 4) reads 16 bytes of row g, words t, t + 4, t + 8 and t + 12 of the
 // block, so that one step of all lanes covers 32 neighbouring columns, which lie in one scale group; the scale is
-// applied to the fp32 sums of its group.  (With one to eight columns there is no reuse that a larger tensor
-// tile could draw on.)
-// fp32: the same lookups in a table of fp32 pairs, held once for each two lanes, and FMAs.
-constexpr int kWarps = 16, kThreads = 32 * kWarps, kDepth = 4;  // kDepth: 1 KB loads that a warp has in flight
-constexpr int kRowsMost = 512;                                 // rows of a block
-constexpr int kTableBytes = 256 * 128, kSumBytes = 2 * kWarps * 16 * 8 * 4, kRowSumBytes = kRowsMost * 8 * 4;
+// applied to the fp32 sums of its group.  A warp keeps to its R blocks for all rows, with their x in registers.
+// (With one to eight columns there is no reuse that a larger tensor tile could draw on.)
+// fp32: the same lookups in a table of fp32 pairs, held once for each two lanes, x in shared memory, and FMAs.
+constexpr int kWarps = 16, kThreads = 32 * kWarps;
+constexpr int kRowsMost = 512;  // rows of a block
+constexpr int kMostStages = 4;
+constexpr int kTableBytes = 256 * 128, kSumBytes = 2 * kWarps * 16 * 8 * 4, kRowSumBytes = kRowsMost * 8 * 4, kBarBytes = 64;
+constexpr int kRowPad = 64;     // a row's room in a stage is its bytes and this: two rows' reads do not meet in a bank
+constexpr int kSpins = 1 << 18; // of a wait, each of a microsecond or so
 
-__device__ __forceinline__ uint4 load_codes(const uint8_t *p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < kSpins; i++) {
+        uint32_t done;
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
+                     : "=r"(done) : "r"(bar), "r"(parity), "r"(1000) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+// d = c + A B
+template <typename T> __device__ __forceinline__ void mma_pairs(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma_pairs<__half>(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+template <> __device__ __forceinline__ void mma_pairs<__nv_bfloat16>(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+// Entry `byte j of w` of the table of pairs; l: the address of the lane's copy of entry 0.  The address is left to the integer
+// multiply-add, as the permutes already fill their own pipe.
+template <int J> __device__ __forceinline__ uint32_t entry_at(uint32_t w, uint32_t l) {
+    uint32_t byte, at;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(byte) : "r"(w), "n"(0x4440 | J));
+    asm("mad.lo.u32 %0, %1, 128, %2;" : "=r"(at) : "r"(byte), "r"(l));
+    return at;
+}
+template <int J> __device__ __forceinline__ uint32_t pair16(uint32_t w, uint32_t l) {
+    uint32_t v;
+    asm("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(entry_at<J>(w, l)));
     return v;
 }
-template <typename T> __device__ __forceinline__ void mma_pairs(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
-template <> __device__ __forceinline__ void mma_pairs<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-template <> __device__ __forceinline__ void mma_pairs<__nv_bfloat16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+template <int J> __device__ __forceinline__ float2 pair32(uint32_t w, uint32_t l) {
+    float2 v;
+    asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(entry_at<J>(w, l)));
+    return v;
 }
 
 // A warp's part of a row tile: 16 rows, and of the eight columns the two of its lane.
@@ -82,14 +115,12 @@ template <typename T> struct Sums {
         c[2] = fmaf(sb, o.c[2], c[2]);
         c[3] = fmaf(sb, o.c[3], c[3]);
     }
-    // Adds eight columns: codes wa of row g and wb of row g + 8, x at xs (row g of x; only read if g < nb).
-    __device__ __forceinline__ void word(uint32_t wa, uint32_t wb, const char *table, const T *xs, int, int lane, int nb) {
-        uint4 xv = make_uint4(0, 0, 0, 0);
-        if ((lane >> 2) < nb) xv = *reinterpret_cast<const uint4 *>(xs);
-        const uint32_t l4 = 4 * lane;
-        auto look = [&](uint32_t byte7) { return *reinterpret_cast<const uint32_t *>(table + ((byte7 & 0x7f80u) | l4)); };
-        mma_pairs<T>(c, look(wa << 7), look(wb << 7), look(wa >> 1), look(wb >> 1), xv.x, xv.y);
-        mma_pairs<T>(c, look(wa >> 9), look(wb >> 9), look(wa >> 17), look(wb >> 17), xv.z, xv.w);
+    // Eight more columns (FIRST: the first): codes wa of row g and wb of row g + 8, xv those of row g of x.
+    template <bool FIRST> __device__ __forceinline__ void word(uint32_t wa, uint32_t wb, uint32_t l, const uint32_t (&xv)[4]) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        if (FIRST) mma_pairs<T>(c, zero, pair16<0>(wa, l), pair16<0>(wb, l), pair16<1>(wa, l), pair16<1>(wb, l), xv[0], xv[1]);
+        else mma_pairs<T>(c, c, pair16<0>(wa, l), pair16<0>(wb, l), pair16<1>(wa, l), pair16<1>(wb, l), xv[0], xv[1]);
+        mma_pairs<T>(c, c, pair16<2>(wa, l), pair16<2>(wb, l), pair16<3>(wa, l), pair16<3>(wb, l), xv[2], xv[3]);
     }
     __device__ __forceinline__ void finish(int) {}
 };
@@ -107,18 +138,10 @@ template <> struct Sums<float> {
             p[1][i] = fmaf(sb, o.p[1][i], p[1][i]);
         }
     }
-    __device__ __forceinline__ void word(uint32_t wa, uint32_t wb, const char *table, const float *xs, int pitch, int lane, int nb) {
-        const uint32_t l8 = 8 * (lane & 15);
-        float2 va[4], vb[4];
-        auto look = [&](uint32_t byte7) { return *reinterpret_cast<const float2 *>(table + ((byte7 & 0x7f80u) | l8)); };
-        va[0] = look(wa << 7);
-        va[1] = look(wa >> 1);
-        va[2] = look(wa >> 9);
-        va[3] = look(wa >> 17);
-        vb[0] = look(wb << 7);
-        vb[1] = look(wb >> 1);
-        vb[2] = look(wb >> 9);
-        vb[3] = look(wb >> 17);
+    template <bool FIRST> __device__ __forceinline__ void word(uint32_t wa, uint32_t wb, uint32_t l, const float *xs, int pitch, int nb) {
+        if (FIRST) clear();
+        const float2 va[4] = {pair32<0>(wa, l), pair32<1>(wa, l), pair32<2>(wa, l), pair32<3>(wa, l)};
+        const float2 vb[4] = {pair32<0>(wb, l), pair32<1>(wb, l), pair32<2>(wb, l), pair32<3>(wb, l)};
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             if (i >= nb) break;
@@ -149,178 +172,253 @@ template <> struct Sums<float> {
     }
 };
 
-// WIDE: a scale group holds whole 128-column blocks.
-template <typename T, typename S, bool WIDE>
+// WIDE: a scale group holds whole 128-column blocks.  R: blocks of a warp in a chunk at most (16-bit types).
+template <typename T, typename S, bool WIDE, int R>
 __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ MatvecArgs a) {
     extern __shared__ __align__(128) char smem[];
     constexpr bool kF32 = sizeof(T) == 4;
     char *table = smem;
+    const uint32_t entry0 = smem_at(table) + (kF32 ? 8 * (threadIdx.x & 15) : 4 * (threadIdx.x & 31));
     float *sums = reinterpret_cast<float *>(smem + kTableBytes);
-    float *row_sums = sums + kSumBytes / 4;  // [kRowsMost][8], only with several chunks
-    T *xs = reinterpret_cast<T *>(smem + kTableBytes + kSumBytes + (a.chunk < a.k ? kRowSumBytes : 0));
+    const uint32_t bars = smem_at(smem + kTableBytes + kSumBytes);
+    char *rest = smem + kTableBytes + kSumBytes + kBarBytes;
+    float *row_sums = reinterpret_cast<float *>(rest);  // [kRowsMost][8], only with several chunks
+    if (a.chunk < a.k) rest += kRowSumBytes;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int wk = wid & (a.warps_k - 1), wr = wid / a.warps_k, tiles_apart = kWarps / a.warps_k;
+    const int wk = wid & (a.warps_k - 1), wr = wid / a.warps_k, tiles = kWarps / a.warps_k, rows_at_once = 16 * tiles;
     const int i0 = 8 * blockIdx.y, nb = min(8, a.b - i0);
+    T *xs = reinterpret_cast<T *>(rest);  // fp32: x, a.chunk columns a row
+    if (kF32) rest += nb * a.chunk * 4;
+    const char *ring = rest;
+    const int pitch = a.chunk / 2 + kRowPad, stage_bytes = rows_at_once * pitch;
     // Runs of whole eights of rows, as even as they can be.
     const int64_t units = (a.n + 7) / 8;
-    const int64_t r0 = units * blockIdx.x / gridDim.x * 8, r1 = min(a.n, units * (blockIdx.x + 1) / gridDim.x * 8);
-    const int tiles = (int)((r1 - r0 + 15) / 16);
-    const S *scales = static_cast<const S *>(a.scales);
+    const int64_t r0 = units * blockIdx.x / gridDim.x * 8;
+    const int rows = (int)(min(a.n, units * (blockIdx.x + 1) / gridDim.x * 8) - r0), rounds = (rows + rows_at_once - 1) / rows_at_once;
+    const uint8_t *codes = a.codes + r0 * a.code_row;
+    const S *scales = static_cast<const S *>(a.scales) + r0 * a.scale_row;
 
-    struct Load {
-        uint4 a, b;
-        float sa, sb;
-    } ring[kDepth];
+    if (tid == 0)
+        for (int s = 0; s < a.stages; s++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * s) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+
+    uint32_t parity = 0;  // of the stages' next waits, a bit each
+    bool lost = false;    // a wait ran out
+    int turn = 0;
     for (int64_t k0 = 0; k0 < a.k; k0 += a.chunk) {
         const int cols = (int)min((int64_t)a.chunk, a.k - k0), blocks = (cols + 127) / 128;
-        const bool some = wk < blocks;  // a last chunk may have fewer blocks than warps_k
-        // Two walks over (tile, block), one ahead for the loads.
-        int ahead_tile = wr, ahead_block = wk;
-        auto load = [&](Load &l) {
-            if (ahead_tile < tiles) {
-                const int64_t ra = r0 + 16 * ahead_tile + g, rb = ra + 8;
-                const int64_t at = (k0 + 128 * ahead_block) / 2 + 16 * t;
-                uint32_t w = (uint32_t)(k0 / 32) + 4 * ahead_block + (WIDE ? 0 : t);
-                w = a.div_mul ? __umulhi(w, a.div_mul) >> a.div_shift : w >> a.div_shift;
-                w = min(w, (uint32_t)a.groups - 1);
-                l.a = l.b = make_uint4(0, 0, 0, 0);
-                l.sa = l.sb = 0.f;
-                if (some && ra < r1) {
-                    l.a = load_codes(a.codes + ra * a.code_row + at);
-                    l.sa = to_f32(scales[ra * a.scale_row + w]);
-                }
-                if (some && rb < r1) {
-                    l.b = load_codes(a.codes + rb * a.code_row + at);
-                    l.sb = to_f32(scales[rb * a.scale_row + w]);
-                }
-                ahead_block += a.warps_k;
-                if (ahead_block >= blocks) {
-                    ahead_block = wk;
-                    ahead_tile += tiles_apart;
-                }
-            }
+        const int own = wk < blocks ? (blocks - wk + a.warps_k - 1) / a.warps_k : 0;  // this warp's blocks
+        if (k0) __syncthreads();
+        auto fetch = [&](int round, int s) {
+            const int first = round * rows_at_once, count = min(rows_at_once, rows - first);
+            if (tid == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bars + 8 * s), "r"(count * blocks * 64) : "memory");
+            if (tid < count)
+                asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                 smem_at(ring + s * stage_bytes + tid * pitch)),
+                             "l"(codes + (first + tid) * a.code_row + k0 / 2), "r"(blocks * 64), "r"(bars + 8 * s)
+                             : "memory");
         };
-#pragma unroll
-        for (int s = 0; s < kDepth; s++) load(ring[s]);
+        for (int s = 0; s < a.stages && s < rounds; s++) fetch(s, s);
 
-        // The codebook's pairs and the chunk of x, zero beyond k.
-        if (k0 == 0) {
-            const T *levels = static_cast<const T *>(a.levels);
-            constexpr int kCopies = kF32 ? 16 : 32;
-            for (int i = tid; i < 256 * kCopies; i += kThreads) {
-                const int e = i / kCopies, lo = e & 15, hi = e >> 4;
-                const T zero = from_f32<T>(0.f);
-                reinterpret_cast<T *>(table)[2 * i] = lo < a.m ? levels[lo] : zero;
-                reinterpret_cast<T *>(table)[2 * i + 1] = hi < a.m ? levels[hi] : zero;
-            }
-        } else {
-            __syncthreads();
-        }
-        const T *x = static_cast<const T *>(a.x) + i0 * a.x_row + k0;
-        constexpr int kVec = 16 / sizeof(T);
-        const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (nb == 1 || a.x_row % kVec == 0);
-        for (int i = 0; i < nb; i++)
-            for (int c = kVec * tid; c < 128 * blocks; c += kVec * kThreads) {
-                alignas(16) T v[kVec];
-                T *to = xs + i * a.x_pitch + c;
-                if (vec && c + kVec <= cols) {
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(x + i * a.x_row + c));
-                    continue;
-                }
+        // Scales of a round's tile, fetched a round ahead: of rows g and g + 8, for the lane's words t of each block (WIDE: for
+        // the block).  Rows beyond the run repeat its last one; their sums are not stored.
+        constexpr int kHeld = kF32 ? 1 : R;
+        S sa[kHeld], sb[kHeld];
+        auto scale_at = [&](int r) {
+            uint32_t w = (uint32_t)(k0 / 32) + 4 * (wk + r * a.warps_k) + (WIDE ? 0 : t);
+            w = a.div_mul ? __umulhi(w, a.div_mul) >> a.div_shift : w >> a.div_shift;
+            return min(w, (uint32_t)a.groups - 1);
+        };
+        uint32_t at[kHeld];
 #pragma unroll
-                for (int j = 0; j < kVec; j++) v[j] = c + j < cols ? x[i * a.x_row + c + j] : from_f32<T>(0.f);
-                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);
+        for (int r = 0; r < kHeld; r++) at[r] = scale_at(r);
+        auto rows_of = [&](int round, const S *&qa, const S *&qb) {
+            const int row = round * rows_at_once + 16 * wr + g;
+            qa = scales + min(row, rows - 1) * a.scale_row;
+            qb = scales + min(row + 8, rows - 1) * a.scale_row;
+        };
+        auto fetch_scales = [&](int round) {
+            const S *qa, *qb;
+            rows_of(round, qa, qb);
+#pragma unroll
+            for (int r = 0; r < kHeld; r++)
+                if (r < own) {
+                    sa[r] = qa[at[r]];
+                    sb[r] = qb[at[r]];
+                }
+        };
+        if (!kF32) fetch_scales(0);
+
+        // The codebook's pairs: warp w the sixteen with the second level w, a lane a copy.
+        if (k0 == 0) {
+            const T mine = (lane & 15) < a.m ? static_cast<const T *>(a.levels)[lane & 15] : from_f32<T>(0.f);
+            uint32_t bits = 0;
+            memcpy(&bits, &mine, sizeof(T));
+            const uint32_t high = __shfl_sync(0xffffffffu, bits, wid);
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                const uint32_t low = __shfl_sync(0xffffffffu, bits, j);
+                const int e = 16 * wid + j;
+                if constexpr (kF32) {
+                    if (lane < 16) reinterpret_cast<uint2 *>(table)[16 * e + lane] = make_uint2(low, high);
+                } else {
+                    reinterpret_cast<uint32_t *>(table)[32 * e + lane] = low | high << 16;
+                }
             }
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        }
+        // x, zero beyond k.
+        const T *x = static_cast<const T *>(a.x) + i0 * a.x_row + k0;
+        uint32_t xr[kHeld][4][4];
+        if constexpr (kF32) {
+            for (int i = 0; i < nb; i++)
+                for (int c = tid; c < 128 * blocks; c += kThreads) xs[i * a.chunk + c] = c < cols ? x[i * a.x_row + c] : from_f32<T>(0.f);
+        } else {
+            const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (nb == 1 || a.x_row % 8 == 0);
+#pragma unroll
+            for (int r = 0; r < R; r++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int c = 128 * (wk + r * a.warps_k) + 32 * i + 8 * t;
+                    const T *from = x + g * a.x_row + c;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (g < nb && c < cols) {
+                        if (vec && c + 8 <= cols) {
+                            v = *reinterpret_cast<const uint4 *>(from);
+                        } else {
+                            alignas(16) T one[8];
+#pragma unroll
+                            for (int j = 0; j < 8; j++) one[j] = c + j < cols ? from[j] : from_f32<T>(0.f);
+                            v = *reinterpret_cast<const uint4 *>(one);
+                        }
+                    }
+                    xr[r][i][0] = v.x;
+                    xr[r][i][1] = v.y;
+                    xr[r][i][2] = v.z;
+                    xr[r][i][3] = v.w;
+                }
+        }
         __syncthreads();
 
-        int tile = wr, block = wk, turn = 0;
-        Sums<T> acc;
-        acc.clear();
-        const T *mine = xs + (kF32 ? 0 : g * a.x_pitch) + 8 * t;
-        while (tile < tiles) {
+        for (int round = 0, s = 0; round < rounds; round++) {
+            if (!wait_full(bars + 8 * s, parity >> s & 1)) lost = true;
+            parity ^= 1u << s;
+            const char *tile = ring + s * stage_bytes + (16 * wr + g) * pitch + 64 * wk + 16 * t;
+            Sums<T> acc;
+            acc.clear();
+            // One block: its codes, its scales, and word(first, i, codes a, codes b), which adds columns 32 i ...
+            auto block = [&](const char *p, float fa, float fb, auto &&word) {
+                const uint4 la = *reinterpret_cast<const uint4 *>(p), lb = *reinterpret_cast<const uint4 *>(p + 8 * pitch);
+                const uint32_t wa[4] = {la.x, la.y, la.z, la.w}, wb[4] = {lb.x, lb.y, lb.z, lb.w};
+                Sums<T> part;
 #pragma unroll
-            for (int s = 0; s < kDepth; s++) {
-                if (tile < tiles) {
-                    const Load &l = ring[s];
-                    const uint32_t wa[4] = {l.a.x, l.a.y, l.a.z, l.a.w}, wb[4] = {l.b.x, l.b.y, l.b.z, l.b.w};
-                    const T *xb = mine + 128 * block;
-                    Sums<T> part;
-                    if (some) {
-                        if (WIDE) part.clear();
+                for (int i = 0; i < 4; i++) {
+                    if (i == 0 || !WIDE) word(part, std::true_type(), i, wa[i], wb[i]);
+                    else word(part, std::false_type(), i, wa[i], wb[i]);
+                    if (!WIDE) acc.add(part, __shfl_sync(0xffffffffu, fa, (lane & ~3) | i), __shfl_sync(0xffffffffu, fb, (lane & ~3) | i));
+                }
+                if (WIDE) acc.add(part, fa, fb);
+            };
+            if constexpr (kF32) {
+                const S *qa, *qb;
+                rows_of(round, qa, qb);
+                for (int r = 0; r < own; r++) {
+                    const uint32_t w = scale_at(r);
+                    const T *xb = xs + 128 * (wk + r * a.warps_k) + 8 * t;
+                    block(tile + 64 * r * a.warps_k, to_f32(qa[w]), to_f32(qb[w]), [&](Sums<T> &part, auto first, int i, uint32_t wa, uint32_t wb) {
+                        part.template word<decltype(first)::value>(wa, wb, entry0, xb + 32 * i, a.chunk, nb);
+                    });
+                }
+            } else {
+                float fa[R], fb[R];
 #pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            if (!WIDE) part.clear();
-                            part.word(wa[i], wb[i], table, xb + 32 * i, a.x_pitch, lane, nb);
-                            if (!WIDE) acc.add(part, __shfl_sync(0xffffffffu, l.sa, (lane & ~3) | i), __shfl_sync(0xffffffffu, l.sb, (lane & ~3) | i));
-                        }
-                        if (WIDE) acc.add(part, l.sa, l.sb);
+                for (int r = 0; r < R; r++) {
+                    fa[r] = to_f32(sa[r]);
+                    fb[r] = to_f32(sb[r]);
+                }
+                if (round + 1 < rounds) fetch_scales(round + 1);
+#pragma unroll
+                for (int r = 0; r < R; r++)
+                    if (r < own)
+                        block(tile + 64 * r * a.warps_k, fa[r], fb[r], [&](Sums<T> &part, auto first, int i, uint32_t wa, uint32_t wb) {
+                            part.template word<decltype(first)::value>(wa, wb, entry0, xr[r][i]);
+                        });
+            }
+            acc.finish(t);
+            float *buf = sums + turn * kWarps * 128;
+            float *mine = buf + wid * 128 + 8 * g + 2 * t;
+            *reinterpret_cast<float2 *>(mine) = make_float2(acc.c[0], acc.c[1]);
+            *reinterpret_cast<float2 *>(mine + 64) = make_float2(acc.c[2], acc.c[3]);
+            __syncthreads();
+            if (round + a.stages < rounds) fetch(round + a.stages, s);
+            // The tiles' sums over their warps: 16 rows of 8 columns each.
+            for (int i = tid; i < 128 * tiles; i += kThreads) {
+                float v = 0.f;
+                const float *from = buf + (i >> 7) * a.warps_k * 128 + (i & 127);
+                for (int w = 0; w < a.warps_k; w++) v += from[w * 128];
+                const int row = round * rows_at_once + i / 8, col = i & 7;
+                if (row < rows && col < nb) {
+                    if (a.chunk < a.k) {
+                        if (k0) v += row_sums[row * 8 + col];
+                        row_sums[row * 8 + col] = v;
                     }
-                    load(ring[s]);
-                    block += a.warps_k;
-                    if (block >= blocks) {  // the tile's sums over its warps
-                        acc.finish(t);
-                        float *buf = sums + (turn * kWarps + wr * a.warps_k) * 128;
-                        float *own = buf + wk * 128 + 8 * g + 2 * t;
-                        *reinterpret_cast<float2 *>(own) = make_float2(acc.c[0], acc.c[1]);
-                        *reinterpret_cast<float2 *>(own + 64) = make_float2(acc.c[2], acc.c[3]);
-                        if (a.warps_k > 1) asm volatile("bar.sync %0, %1;" ::"r"(wr + 1), "r"(32 * a.warps_k) : "memory");
-                        else __syncwarp();
-                        for (int i = 32 * wk + lane; i < 128; i += 32 * a.warps_k) {
-                            float v = 0.f;
-                            for (int w = 0; w < a.warps_k; w++) v += buf[w * 128 + i];
-                            const int64_t row = r0 + 16 * tile + i / 8;
-                            const int col = i & 7;
-                            if (row < r1 && col < nb) {
-                                if (a.chunk < a.k) {
-                                    float *keep = row_sums + (16 * tile + i / 8) * 8 + col;
-                                    if (k0) v += *keep;
-                                    *keep = v;
-                                }
-                                if (k0 + a.chunk >= a.k) static_cast<T *>(a.y)[(i0 + col) * a.y_row + row] = from_f32<T>(v);
-                            }
-                        }
-                        turn ^= 1;  // the next tile's sums go to the other half: one barrier a tile
-                        block = wk;
-                        tile += tiles_apart;
-                        acc.clear();
-                    }
+                    if (k0 + a.chunk >= a.k) static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(lost ? CUDART_NAN_F : v);
                 }
             }
+            turn ^= 1;  // the next round's sums go to the other half: one barrier a round
+            s = s + 1 == a.stages ? 0 : s + 1;
         }
     }
+    if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
 }
 
-// Shared memory for x: what is left beside the table and the sums.
-constexpr int64_t kXBytes = 227 * 1024 - kTableBytes - kSumBytes;
-
-template <typename T, typename S>
-static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
-    const int nb = std::min(a.b, 8);
-    // Rows of x lie 64 bytes off a multiple of 128 from one another, so that the reads of two rows do not meet in a bank.
-    const int64_t pad = 64 / (int64_t)sizeof(T), wide = cdiv(a.k, 128) * 128;
-    if (nb * (wide + pad) * (int64_t)sizeof(T) <= kXBytes) a.chunk = (int32_t)std::max(wide, a.k);
-    else a.chunk = (int32_t)(((kXBytes - kRowSumBytes) / (nb * (int64_t)sizeof(T)) - pad) / 128 * 128);
-    a.x_pitch = (int32_t)(std::min<int64_t>(a.chunk, wide) + pad);
-    const int smem = kTableBytes + kSumBytes + (a.chunk < a.k ? kRowSumBytes : 0) + nb * a.x_pitch * (int)sizeof(T);
-    // One block for each SM (152), more where a block would have over kRowsMost rows.
-    const int64_t units = cdiv(a.n, 8), blocks = std::max(std::min<int64_t>(units, 152), cdiv(units, kRowsMost / 8));
-    // The warps' split between columns and row tiles that leaves the fullest warp the least.
-    const int64_t kb = std::min<int64_t>(a.chunk, wide) / 128, tiles = cdiv(cdiv(units, blocks), 2);
-    int64_t best = INT64_MAX;
-    for (int w = 1; w <= kWarps && w <= kb; w *= 2) {
-        const int64_t cost = cdiv(kb, w) * cdiv(tiles, kWarps / w);
-        if (cost <= best) {
-            best = cost;
-            a.warps_k = w;
-        }
-    }
-    auto *kernel = group % 128 == 0 ? k_matvec<T, S, true> : k_matvec<T, S, false>;
+template <typename T, typename S, int R>
+static int launch_matvec_blocks(const MatvecArgs &a, bool wide, int smem, int64_t blocks, cudaStream_t st) {
+    auto *kernel = wide ? k_matvec<T, S, true, R> : k_matvec<T, S, false, R>;
     ECASQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     note_launch();
     kernel<<<dim3((unsigned)blocks, (unsigned)cdiv(a.b, 8)), kThreads, smem, st>>>(a);
     ECASQ_LAUNCH_CHECK();
     return ECASQ_OK;
+}
+
+template <typename T, typename S>
+static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
+    constexpr bool f32 = sizeof(T) == 4;
+    // One block for each SM (152), more where a block would have over kRowsMost rows.
+    const int64_t units = cdiv(a.n, 8), blocks = std::max(std::min<int64_t>(units, 152), cdiv(units, kRowsMost / 8));
+    const int64_t tiles = cdiv(cdiv(units, blocks), 2), kb = cdiv(a.k, 128);
+    const int64_t room = 227 * 1024 - kTableBytes - kSumBytes - kBarBytes - kRowSumBytes, nb = std::min(a.b, 8);
+    // The warps' split between columns and row tiles that leaves the fullest warp the least; of equal ones that with the
+    // fewest warps a tile, whose sums have to be joined.  A warp holds x for four blocks at most (fp32: any number).
+    int64_t best = INT64_MAX;
+    for (int w = kWarps; w >= 1; w /= 2) {
+        const int64_t cost = cdiv(kb, w) * cdiv(tiles, kWarps / w);
+        if (w < kWarps && (w > kb ? cost >= best : cost > best || (!f32 && cdiv(kb, w) > 4))) continue;
+        best = cost;
+        a.warps_k = w;
+    }
+    const int64_t at_once = 16 * (kWarps / a.warps_k), own = f32 ? 1 : std::min<int64_t>(cdiv(kb, a.warps_k), 4);  // blocks of a warp in a chunk
+    // A stage and, in fp32, x: bytes a column.  Two stages at least.
+    auto stage = [&](int64_t chunk) { return at_once * (chunk / 2 + kRowPad); };
+    if (f32) {
+        int64_t chunk = kb;
+        while (chunk > 1 && nb * chunk * 512 + 2 * stage(128 * chunk) > room) chunk--;
+        a.chunk = (int32_t)(128 * chunk);
+    } else {
+        a.chunk = (int32_t)(128 * std::min(kb, own * a.warps_k));
+    }
+    const int64_t x_bytes = f32 ? nb * a.chunk * 4 : 0;
+    a.stages = (int32_t)std::min<int64_t>(std::min<int64_t>(kMostStages, (room - x_bytes) / stage(a.chunk)), cdiv(tiles, kWarps / a.warps_k));
+    const int smem = (int)(227 * 1024 - room - (a.chunk < a.k ? 0 : kRowSumBytes) + x_bytes + a.stages * stage(a.chunk));
+    const bool wide = group % 128 == 0;
+    if (own == 1) return launch_matvec_blocks<T, S, 1>(a, wide, smem, blocks, st);
+    if constexpr (!f32) {
+        if (own == 2) return launch_matvec_blocks<T, S, 2>(a, wide, smem, blocks, st);
+        return launch_matvec_blocks<T, S, 4>(a, wide, smem, blocks, st);
+    }
+    return ECASQ_EINVAL;
 }
 
 }  // namespace ecasq
@@ -344,7 +442,7 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
 
 int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
                  const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
-                 int64_t k, int32_t group, void *y, int64_t y_row, ecasq_stream_t stream) {
+                 int64_t k, int32_t group, void *y, int64_t y_row, int32_t *status, ecasq_stream_t stream) {
     if (n < 1 || k < 1 || b < 0 || n >= (int64_t)1 << 31 || k >= (int64_t)1 << 31 || b > 8 * 65535 || m < 1 || m > 16 ||
         !type_ok(type) || (scale_type != type && scale_type != ECASQ_F32) || group < 32 || group % 32)
         return ECASQ_EINVAL;
@@ -358,6 +456,7 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
     a.scales = scales;
     a.codes = codes;
     a.y = y;
+    a.status = status;
     a.x_row = x_row;
     a.code_row = code_row;
     a.scale_row = scale_row;

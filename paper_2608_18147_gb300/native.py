@@ -18,7 +18,7 @@ from . import build as _build
 
 OK, EINVAL, ENONFINITE, EINFEASIBLE, EWORKSPACE, ECUDA, ETIMEOUT, ERANGE = 0, -1, -2, -3, -4, -5, -6, -7
 F32, F16, BF16 = 0, 1, 2  # element types of the operators on 4-bit codes
-BAD_PAGE, BAD_LENGTH, BAD_COUNT, BAD_VALUE = 1, 2, 4, 8  # bits of their status word
+BAD_PAGE, BAD_LENGTH, BAD_COUNT, BAD_VALUE, BAD_WAIT = 1, 2, 4, 8, 16  # bits of their status word
 EXACT_S, NO_REFINE_GUARD, DP_REFERENCE, TIME_KERNELS, EXACT_TABLES, RESIDENT_COSTS, STREAMED_COSTS = 1, 2, 4, 8, 16, 32, 64
 ONE_PART_PUBLISH = 128  # accepted, without effect
 UNSEEDED_SEARCH = 256  # fast DP search: no seeded tile skipping (same results)
@@ -121,7 +121,8 @@ def lib():
             "ecasq_solve_batched": (C.c_int, [vp, i64, i64, PP, vp, sz, vp, vp, PR, vp]),
             "ecasq_prepare": (C.c_int, [vp, i64, vp, sz, vp, vp, vp, vp, vp, pi64, vp]),
             "ecasq_pack": (C.c_int, [vp, i64, i64, i64, vp, i64, vp]),
-            "ecasq_matvec": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, vp, i64, vp]),
+            "ecasq_matvec": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, vp, i64, vp,
+                                       vp]),
             "ecasq_cache_write": (C.c_int, [vp, i32, i64, i64, i64, vp, i32, vp, vp, PC, u64, vp, vp]),
             "ecasq_workspace_size_attend": (sz, [i64, i32, i32, i32, i64]),
             "ecasq_attend": (C.c_int, [vp, i64, i64, i64, i32, PC, PC, vp, i64, vp, vp, i64, C.c_float, vp, i64, i64,
@@ -615,15 +616,15 @@ def ecasq_pack(idx):
     return codes
 
 
-def ecasq_matvec(x, codes, levels, scales, group, out=None):
+def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
     """y = x W^T for the 4-bit matrix W[r, c] = scales[r, c // group] * levels[code[r, c]].
 
     x [b, k] or [k] (float32, float16 or bfloat16), codes [n, 64 ceil(k / 128)] as ecasq_pack gives them,
     levels [m <= 16] of x's type, scales [n, ceil(k / group)] of x's type or float32, group a multiple of 32.
-    Returns y [b, n] or [n] of x's type (`out` if given)."""
+    status: int32 tensor that BAD_* bits are or-ed into.  Returns y [b, n] or [n] of x's type (`out` if given)."""
     torch = _torch()
     where = "ecasq_matvec"
-    at = _device_of(where, x, codes, levels, scales, out)
+    at = _device_of(where, x, codes, levels, scales, out, status)
     T = _types().get(x.dtype)
     x2 = x if x.dim() == 2 else x.unsqueeze(0)
     if T is None or x2.dim() != 2 or (x2.shape[1] > 1 and x2.stride(1) != 1):
@@ -650,7 +651,7 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None):
     rc = lib().ecasq_matvec(x2.data_ptr(), x2.stride(0), T, b, codes.data_ptr(), codes.stride(0) if n > 1 else codes.shape[1],
                             levels.data_ptr(), levels.numel(), scales.data_ptr(),
                             scales.stride(0) if n > 1 else scales.shape[1], _types()[scales.dtype], n, k, group,
-                            y.data_ptr(), y.stride(0), _stream_of(at))
+                            y.data_ptr(), y.stride(0), _status_ptr(where, status), _stream_of(at))
     _check(rc, where)
     return out if out is not None else y if x.dim() == 2 else y[0]
 

@@ -33,7 +33,7 @@ def test_matvec_and_pack_refusals():
     from paper_2608_18147_gb300 import native
     L = native.lib()
     good = dict(x=V, x_row=300, type=native.BF16, b=2, codes=V, code_row=192, levels=V, m=16, scales=V, scale_row=10,
-                scale_type=native.F32, n=5, k=300, group=32, y=V, y_row=5, stream=None)
+                scale_type=native.F32, n=5, k=300, group=32, y=V, y_row=5, status=None, stream=None)
     assert L.ecasq_matvec(*dict(good, b=0).values()) == native.OK
     for change in (dict(x=None), dict(type=3), dict(type=-1), dict(b=-1), dict(codes=None), dict(codes=V + 8), dict(code_row=191),
                    dict(code_row=128), dict(code_row=200), dict(levels=None), dict(m=0), dict(m=17), dict(scales=None),
