@@ -243,11 +243,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
             const S *qa, *qb;
             rows_of(round, qa, qb);
 #pragma unroll
-            for (int r = 0; r < kHeld; r++)
-                if (r < own) {
-                    sa[r] = qa[at[r]];
-                    sb[r] = qb[at[r]];
-                }
+            for (int r = 0; r < kHeld; r++) {
+                sa[r] = qa[at[r]];
+                sb[r] = qb[at[r]];
+            }
         };
         if (!kF32) fetch_scales(0);
 
@@ -338,9 +337,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
                     fb[r] = to_f32(sb[r]);
                 }
                 if (round + 1 < rounds) fetch_scales(round + 1);
+                // (All R blocks, without a branch between them: x is zero where there is none.)
 #pragma unroll
                 for (int r = 0; r < R; r++)
-                    if (r < own)
                         block(tile + 64 * r * a.warps_k, fa[r], fb[r], [&](Sums<T> &part, auto first, int i, uint32_t wa, uint32_t wb) {
                             part.template word<decltype(first)::value>(wa, wb, entry0, xr[r][i]);
                         });
@@ -407,7 +406,7 @@ static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
         while (chunk > 1 && nb * chunk * 512 + 2 * stage(128 * chunk) > room) chunk--;
         a.chunk = (int32_t)(128 * chunk);
     } else {
-        a.chunk = (int32_t)(128 * std::min(kb, own * a.warps_k));
+        a.chunk = (int32_t)(128 * own * a.warps_k);
     }
     const int64_t x_bytes = f32 ? nb * a.chunk * 4 : 0;
     a.stages = (int32_t)std::min<int64_t>(std::min<int64_t>(kMostStages, (room - x_bytes) / stage(a.chunk)), cdiv(tiles, kWarps / a.warps_k));
@@ -416,6 +415,7 @@ static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
     if (own == 1) return launch_matvec_blocks<T, S, 1>(a, wide, smem, blocks, st);
     if constexpr (!f32) {
         if (own == 2) return launch_matvec_blocks<T, S, 2>(a, wide, smem, blocks, st);
+        if (own == 3) return launch_matvec_blocks<T, S, 3>(a, wide, smem, blocks, st);
         return launch_matvec_blocks<T, S, 4>(a, wide, smem, blocks, st);
     }
     return ECASQ_EINVAL;
