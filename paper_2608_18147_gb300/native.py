@@ -28,6 +28,7 @@ TEST_SELF_SEED = 1 << 29  # test hook: a fixed-multiplier pass seeded with its o
 
 _lock = threading.Lock()
 _lib = None
+_torch_module = None
 
 
 class Params(C.Structure):
@@ -84,6 +85,8 @@ def lib_path() -> str:
 def lib():
     """Load libecasq.so (building it first if it is missing or stale)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -157,8 +160,11 @@ def exported_symbols():
 # ------------------------------------------------------------------ helpers
 
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _stream():
@@ -556,48 +562,50 @@ def ecasq_prepare(x, ws=None):
 
 
 # ------------------------------------------------------ operators on 4-bit codes
+#
+# These calls are short, so the binding is too: one condition over what the tensors are, and only where it fails a
+# second look that says what is wrong.
 
 _TYPES = {}
 
 
-def _types():
+def _ready():
+    """The library, with the element types known."""
+    L = lib()
     if not _TYPES:
         torch = _torch()
         _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
-    return _TYPES
+    return L
 
 
 def _refuse(where, what):
     raise EcasqError(EINVAL, "%s: %s" % (where, what))
 
 
-def _device_of(where, first, *others):
-    """The index of the CUDA device that the given tensors (None allowed after the first) are on: the current one, whose
-    stream the call uses."""
-    torch = _torch()
-    try:
-        at = first.get_device()
-        for t in others:
-            if t is not None and t.get_device() != at:
-                at = -1
-    except (AttributeError, RuntimeError):
-        at = -1
-    if at < 0 or at != torch.cuda.current_device():
-        _refuse(where, "tensors must be on the current CUDA device")
-    return at
-
-
-def _stream_of(index):
+def _raw_stream(index):
+    """The current stream of a device, as _stream() without the object around it."""
     return _torch()._C._cuda_getCurrentRawStream(index)
 
 
-def _status_ptr(where, status):
-    if status is None:
-        return None
+def _need(where, *wanted):
+    """Raises for the first of (condition, what it means) that does not hold; a condition is a function, as it may not
+    even be computable."""
+    for holds, what in wanted:
+        try:
+            ok = holds()
+        except (AttributeError, TypeError, IndexError, RuntimeError):
+            ok = False
+        if not ok:
+            _refuse(where, what)
+
+
+def _here(where, *tensors):
+    """The index of the CUDA device that all the given tensors (None allowed) are on: the current one, whose stream the call
+    uses."""
     torch = _torch()
-    if status.dtype != torch.int32 or status.numel() < 1:
-        _refuse(where, "status must be an int32 tensor")
-    return status.data_ptr()
+    devices = {t.get_device() if isinstance(t, torch.Tensor) else -1 for t in tensors if t is not None}
+    if len(devices) != 1 or -1 in devices or torch.cuda.current_device() not in devices:
+        _refuse(where, "tensors must be on the current CUDA device")
 
 
 def ecasq_pack(idx):
@@ -605,15 +613,36 @@ def ecasq_pack(idx):
     [n, 64 ceil(k / 128)]."""
     torch = _torch()
     where = "ecasq_pack"
-    at = _device_of(where, idx)
+    L = _ready()
+    _here(where, idx)
     if idx.dtype != torch.uint8 or idx.dim() != 2 or (idx.shape[1] > 1 and idx.stride(1) != 1):
         _refuse(where, "idx must be uint8 [n, k] with contiguous rows")
     n, k = idx.shape
     codes = torch.empty((n, 64 * -(-k // 128)), dtype=torch.uint8, device=idx.device)
-    rc = lib().ecasq_pack(idx.data_ptr(), idx.stride(0) if n > 1 else k, n, k, codes.data_ptr(), codes.shape[1],
-                          _stream_of(at))
+    rc = L.ecasq_pack(idx.data_ptr(), idx.stride(0) if n > 1 else k, n, k, codes.data_ptr(), codes.shape[1], _stream())
     _check(rc, where)
     return codes
+
+
+def _matvec_refused(torch, x, codes, levels, scales, group, out):
+    where = "ecasq_matvec"
+    _here(where, x, codes, levels, scales, out)
+    k = lambda: x.shape[-1]  # noqa: E731
+    _need(where,
+          (lambda: x.dtype in _TYPES and x.dim() in (1, 2) and (k() < 2 or x.stride(-1) == 1),
+           "x must be [b, k] or [k] of float32, float16 or bfloat16 with contiguous rows"),
+          (lambda: codes.dtype == torch.uint8 and codes.dim() == 2 and codes.stride(1) == 1 and codes.shape[1] >= 64 * -(-k() // 128),
+           "codes must be uint8 [n, 64 ceil(k / 128)] with contiguous rows"),
+          (lambda: levels.dtype == x.dtype and levels.dim() == 1 and levels.is_contiguous() and 1 <= levels.numel() <= 16,
+           "levels must be 1 to 16 values of x's type"),
+          (lambda: group >= 32 and group % 32 == 0, "group must be a multiple of 32"),
+          (lambda: scales.dtype in (x.dtype, torch.float32) and scales.dim() == 2 and scales.shape[0] == codes.shape[0]
+           and scales.shape[1] >= -(-k() // group) and (scales.shape[1] < 2 or scales.stride(1) == 1),
+           "scales must be [n, ceil(k / group)] of x's type or float32 with contiguous rows"),
+          (lambda: out is None or (out.dtype == x.dtype and out.shape == x.shape[:-1] + codes.shape[:1]
+                                   and (out.shape[-1] < 2 or out.stride(-1) == 1)),
+           "out must be [b, n] (or [n]) of x's type with contiguous rows"))
+    _refuse(where, "bad arguments")
 
 
 def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
@@ -622,60 +651,88 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
     x [b, k] or [k] (float32, float16 or bfloat16), codes [n, 64 ceil(k / 128)] as ecasq_pack gives them,
     levels [m <= 16] of x's type, scales [n, ceil(k / group)] of x's type or float32, group a multiple of 32.
     status: int32 tensor that BAD_* bits are or-ed into.  Returns y [b, n] or [n] of x's type (`out` if given)."""
+    L = _ready()
     torch = _torch()
-    where = "ecasq_matvec"
-    at = _device_of(where, x, codes, levels, scales, out, status)
-    T = _types().get(x.dtype)
-    x2 = x if x.dim() == 2 else x.unsqueeze(0)
-    if T is None or x2.dim() != 2 or (x2.shape[1] > 1 and x2.stride(1) != 1):
-        _refuse(where, "x must be [b, k] or [k] of float32, float16 or bfloat16 with contiguous rows")
-    b, k = x2.shape
-    group = int(group)
-    if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.stride(1) != 1 or codes.shape[1] < 64 * -(-k // 128):
-        _refuse(where, "codes must be uint8 [n, 64 ceil(k / 128)] with contiguous rows")
-    n = codes.shape[0]
-    if levels.dtype != x.dtype or levels.dim() != 1 or not levels.is_contiguous() or not 1 <= levels.numel() <= 16:
-        _refuse(where, "levels must be 1 to 16 values of x's type")
-    if group < 32 or group % 32:
-        _refuse(where, "group must be a multiple of 32")
-    groups = -(-k // group)
-    if (scales.dtype not in (x.dtype, torch.float32) or scales.dim() != 2 or scales.shape[0] != n
-            or scales.shape[1] < groups or (groups > 1 and scales.stride(1) != 1)):
-        _refuse(where, "scales must be [n, ceil(k / group)] of x's type or float32 with contiguous rows")
-    if out is None:
-        y = torch.empty((b, n), dtype=x.dtype, device=x.device)
+    try:
+        at, dtype, shape, strides = x.get_device(), x.dtype, x.shape, x.stride()
+        n, wide = codes.shape
+        code_row, one = codes.stride()
+        groups, (scale_row, by) = scales.shape, scales.stride()
+        (m,), T, S = levels.shape, _TYPES.get(dtype), _TYPES.get(scales.dtype)
+        k = shape[-1]
+        fine = (T is not None and (S == T or S == F32) and levels.dtype == dtype and codes.dtype == torch.uint8
+                and len(shape) <= 2 and (strides[-1] == 1 or k < 2) and one == 1 and wide >= 64 * -(-k // 128)
+                and group >= 32 and not group % 32 and 1 <= m <= 16 and (m == 1 or levels.stride(0) == 1)
+                and groups[0] == n and groups[1] >= -(-k // group) and (by == 1 or groups[1] < 2)
+                and at == codes.get_device() == levels.get_device() == scales.get_device() == torch.cuda.current_device())
+        if out is not None:
+            y = out
+            fine = (fine and y.get_device() == at and y.dtype == dtype and y.shape == shape[:-1] + codes.shape[:1]
+                    and (n < 2 or y.stride(-1) == 1))
+        elif fine:
+            y = torch.empty((shape[0], n) if len(shape) == 2 else (n,), dtype=dtype, device=x.device)
+    except (AttributeError, TypeError, ValueError, IndexError):
+        fine = False
+    if not fine:
+        _matvec_refused(torch, x, codes, levels, scales, group, out)
+    if len(shape) == 2:
+        b, x_row, y_row = shape[0], strides[0], y.stride(0)
     else:
-        y = out if out.dim() == 2 else out.unsqueeze(0)
-        if out.dtype != x.dtype or out.dim() != x.dim() or y.shape != (b, n) or (n > 1 and y.stride(1) != 1):
-            _refuse(where, "out must be [b, n] (or [n]) of x's type with contiguous rows")
-    rc = lib().ecasq_matvec(x2.data_ptr(), x2.stride(0), T, b, codes.data_ptr(), codes.stride(0) if n > 1 else codes.shape[1],
-                            levels.data_ptr(), levels.numel(), scales.data_ptr(),
-                            scales.stride(0) if n > 1 else scales.shape[1], _types()[scales.dtype], n, k, group,
-                            y.data_ptr(), y.stride(0), _status_ptr(where, status), _stream_of(at))
-    _check(rc, where)
-    return out if out is not None else y if x.dim() == 2 else y[0]
+        b, x_row, y_row = 1, k, n
+    rc = L.ecasq_matvec(x.data_ptr(), x_row, T, b, codes.data_ptr(), code_row if n > 1 else wide, levels.data_ptr(), m,
+                        scales.data_ptr(), scale_row if n > 1 else groups[1], S, n, k, group, y.data_ptr(), y_row,
+                        _status_ptr("ecasq_matvec", at, status), _raw_stream(at))
+    if rc:
+        _check(rc, "ecasq_matvec")
+    return y
 
 
-def _cache(where, rows, levels):
-    """The C view of one side of a paged cache: rows [pages, page_size, heads, d] (coded: [..., d / 2] uint8 with levels
-    [pages, page_size, heads, 8 or 16]); any strides, a row's entries contiguous."""
-    torch = _torch()
-    if rows.dim() != 4 or rows.stride(3) != 1:
-        _refuse(where, "cache rows must be [pages, page_size, heads, d] with contiguous entries")
-    pages, page_size, heads, d = rows.shape
-    rs = rows.stride()
+def _status_ptr(where, at, status):
+    if status is None:
+        return None
+    if status.dtype != _torch().int32 or status.numel() < 1 or status.get_device() != at:
+        _refuse(where, "status must be an int32 tensor on the device of the others")
+    return status.data_ptr()
+
+
+def _cache(rows, levels):
+    """(the C view of one side of a paged cache, its type, its rows' length), or None for the view if the tensors are not
+    one: rows [pages, page_size, heads, d] (coded: [..., d / 2] uint8 with levels [pages, page_size, heads, 8 or 16]); any strides, a
+    row's entries contiguous."""
+    pages, page_size, heads, d = shape = rows.shape
+    r0, r1, r2, r3 = rows.stride()
     if levels is None:
-        T = _types().get(rows.dtype)
-        if T is None:
-            _refuse(where, "plain cache rows must be float32, float16 or bfloat16")
-        return Cache(rows.data_ptr(), None, rs[0], rs[1], rs[2], 0, 0, 0, pages, page_size, heads, d, T, 0, 0)
-    if (rows.dtype != torch.uint8 or levels.dim() != 4 or levels.shape[:3] != rows.shape[:3] or levels.stride(3) != 1
-            or levels.dtype not in (torch.float16, torch.bfloat16) or levels.shape[3] not in (8, 16)):
-        _refuse(where, "a coded cache is uint8 [pages, page_size, heads, d / 2] with levels [pages, page_size, heads, "
-                       "8 or 16] of float16 or bfloat16")
-    ls = levels.stride()
-    return Cache(rows.data_ptr(), levels.data_ptr(), rs[0], rs[1], rs[2], ls[0], ls[1], ls[2], pages, page_size, heads,
-                 2 * d, _types()[levels.dtype], levels.shape[3], 0)
+        T = _TYPES.get(rows.dtype)
+        if T is None or r3 != 1:
+            return None, None, 0
+        return Cache(rows.data_ptr(), None, r0, r1, r2, 0, 0, 0, pages, page_size, heads, d, T, 0, 0), T, d
+    T, (l0, l1, l2, l3) = _TYPES.get(levels.dtype), levels.stride()
+    n = levels.shape[3]
+    if (not T or r3 != 1 or l3 != 1 or rows.dtype != _torch().uint8 or levels.shape[:3] != shape[:3] or (n != 8 and n != 16)
+            or levels.get_device() != rows.get_device()):
+        return None, None, 0
+    return Cache(rows.data_ptr(), levels.data_ptr(), r0, r1, r2, l0, l1, l2, pages, page_size, heads, 2 * d, T, n, 0), T, 2 * d
+
+
+_CACHE_IS = ("a cache is [pages, page_size, heads, d] of float32, float16 or bfloat16, or coded uint8 [..., d / 2] with levels "
+             "[pages, page_size, heads, 8 or 16] of float16 or bfloat16, with contiguous rows")
+
+
+def _write_refused(torch, x, Q, m, slots, codes, levels):
+    where = "ecasq_cache_write"
+    _here(where, x, Q, m, slots, codes, levels)
+    rows = lambda: slots.numel() * codes.shape[2]  # noqa: E731
+    _need(where,
+          (lambda: levels is not None and _cache(codes, levels)[0] is not None, _CACHE_IS),
+          (lambda: slots.dtype == torch.int64 and slots.is_contiguous(), "slots must be contiguous int64 [n]"),
+          (lambda: x.dtype in (torch.float32, levels.dtype) and x.stride(2) == 1
+           and x.shape == (slots.numel(), codes.shape[2], 2 * codes.shape[3]),
+           "x must be [n, heads, d] of float32 or the cache's type with contiguous entries"),
+          (lambda: Q.dtype == torch.float32 and Q.is_contiguous() and 1 <= Q.shape[-1] <= levels.shape[3]
+           and Q.numel() == rows() * Q.shape[-1], "Q must be contiguous float32 [n * heads, s], s at most the cache's levels"),
+          (lambda: m is None or (m.dtype == torch.int32 and m.is_contiguous() and m.numel() == rows()),
+           "m must be contiguous int32 [n * heads]"))
+    _refuse(where, "bad arguments")
 
 
 def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
@@ -685,27 +742,26 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
     slots int64 [n] (page * page_size + slot, negative: not written), codes uint8 [pages, page_size, heads, d / 2],
     levels [pages, page_size, heads, 8 or 16] of float16 or bfloat16; x float32 or of levels' type.  status: int32
     tensor that BAD_* bits are or-ed into.  Returns (codes, levels), written in place."""
+    L = _ready()
     torch = _torch()
-    where = "ecasq_cache_write"
-    at = _device_of(where, x, Q, m, slots, codes, levels, status)
-    c = _cache(where, codes, levels)
-    n = slots.numel()
-    if (x.dtype not in (torch.float32, levels.dtype) or x.dim() != 3 or x.shape != (n, c.heads, c.d)
-            or x.stride(2) != 1):
-        _refuse(where, "x must be [n, heads, d] of float32 or the cache's type with contiguous entries")
-    rows = n * c.heads
-    s = Q.shape[-1]
-    if Q.dtype != torch.float32 or not Q.is_contiguous() or Q.numel() != rows * s or not 1 <= s <= c.levels_n:
-        _refuse(where, "Q must be contiguous float32 [n * heads, s], s at most the cache's levels")
-    if m is not None and (m.dtype != torch.int32 or not m.is_contiguous() or m.numel() != rows):
-        _refuse(where, "m must be contiguous int32 [n * heads]")
-    if slots.dtype != torch.int64 or not slots.is_contiguous():
-        _refuse(where, "slots must be contiguous int64 [n]")
-    rc = lib().ecasq_cache_write(x.data_ptr(), _types()[x.dtype], n, x.stride(0), x.stride(1), Q.data_ptr(), s,
-                                 None if m is None else m.data_ptr(), slots.data_ptr(), C.byref(c),
-                                 int(seed) & 0xFFFFFFFFFFFFFFFF, _status_ptr(where, status),
-                                 _stream_of(at))
-    _check(rc, where)
+    try:
+        at, (n, heads, d), (x_row, x_head, one) = x.get_device(), x.shape, x.stride()
+        c, T, wide = _cache(codes, levels)
+        X, s, rows = _TYPES.get(x.dtype), Q.shape[-1], n * heads
+        fine = (c is not None and levels is not None and (X == F32 or X == T) and one == 1 and wide == d
+                and heads == codes.shape[2] and slots.dtype == torch.int64 and slots.numel() == n and slots.is_contiguous()
+                and Q.dtype == torch.float32 and Q.is_contiguous() and 1 <= s <= levels.shape[3] and Q.numel() == rows * s
+                and (m is None or (m.dtype == torch.int32 and m.numel() == rows and m.is_contiguous() and m.get_device() == at))
+                and at == Q.get_device() == slots.get_device() == codes.get_device() == torch.cuda.current_device())
+    except (AttributeError, TypeError, ValueError, IndexError):
+        fine = False
+    if not fine:
+        _write_refused(torch, x, Q, m, slots, codes, levels)
+    rc = L.ecasq_cache_write(x.data_ptr(), X, n, x_row, x_head, Q.data_ptr(), s, None if m is None else m.data_ptr(),
+                             slots.data_ptr(), C.byref(c), int(seed) & 0xFFFFFFFFFFFFFFFF,
+                             _status_ptr("ecasq_cache_write", at, status), _raw_stream(at))
+    if rc:
+        _check(rc, "ecasq_cache_write")
     return codes, levels
 
 
@@ -714,6 +770,26 @@ def workspace_attend(b, heads, kv_heads, d, max_len):
     torch = _torch()
     n = int(lib().ecasq_workspace_size_attend(int(b), int(heads), int(kv_heads), int(d), int(max_len)))
     return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def _attend_refused(torch, q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws):
+    where = "ecasq_attend"
+    _here(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws)
+    row = lambda t: t.dtype == torch.int32 and t.shape == q.shape[:1] and t.is_contiguous()  # noqa: E731
+    _need(where,
+          (lambda: (k_levels is None) == (v_levels is None), "k and v must both be plain or both be coded"),
+          (lambda: _cache(k, k_levels)[0] is not None and _cache(v, v_levels)[0] is not None, _CACHE_IS),
+          (lambda: q.dim() == 3 and q.stride(2) == 1 and _TYPES.get(q.dtype) == _cache(k, k_levels)[1]
+           and q.shape[2] == _cache(k, k_levels)[2],
+           "q must be [b, heads, d] of the cache's type and row length with contiguous entries"),
+          (lambda: table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == q.shape[0]
+           and (table.shape[1] < 2 or table.stride(1) == 1), "table must be int32 [b, pages of a sequence] with contiguous rows"),
+          (lambda: row(lengths), "lengths must be contiguous int32 [b]"),
+          (lambda: starts is None or row(starts), "starts must be contiguous int32 [b]"),
+          (lambda: max_len is None or max_len <= table.shape[1] * k.shape[1], "the table has too few pages for max_len"),
+          (lambda: out is None or (out.dtype == q.dtype and out.shape == q.shape and out.stride(2) == 1), "out must be like q"),
+          (lambda: ws is None or ws.dtype == torch.uint8, "ws must be uint8"))
+    _refuse(where, "bad arguments")
 
 
 def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None, v_levels=None, max_len=None, out=None,
@@ -725,40 +801,47 @@ def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None
     keys [starts, lengths) are seen.  scale: 1 / sqrt(d) if None.  max_len: host bound of the lengths (None: what the table
     holds).  status: int32 tensor that BAD_* bits are or-ed into.  out [b, heads, d] of q's type, lse float32 [b, heads]
     (natural logarithm; -inf where no key is seen, with out = 0)."""
+    L = _ready()
     torch = _torch()
-    where = "ecasq_attend"
-    at = _device_of(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws, status)
-    if (k_levels is None) != (v_levels is None):
-        _refuse(where, "k and v must both be plain or both be coded")
-    ck, cv = _cache(where, k, k_levels), _cache(where, v, v_levels)
-    if q.dim() != 3 or q.stride(2) != 1 or _types().get(q.dtype) != ck.type or q.shape[2] != ck.d:
-        _refuse(where, "q must be [b, heads, d] of the cache's type and row length with contiguous entries")
-    b, heads, d = q.shape
-    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != b or (table.shape[1] > 1 and table.stride(1) != 1):
-        _refuse(where, "table must be int32 [b, pages of a sequence] with contiguous rows")
-    if lengths.dtype != torch.int32 or lengths.shape != (b,) or not lengths.is_contiguous():
-        _refuse(where, "lengths must be contiguous int32 [b]")
-    if starts is not None and (starts.dtype != torch.int32 or starts.shape != (b,) or not starts.is_contiguous()):
-        _refuse(where, "starts must be contiguous int32 [b]")
-    most = table.shape[1] * ck.page_size
-    max_len = most if max_len is None else int(max_len)
-    if max_len > most:
-        _refuse(where, "the table has too few pages for max_len")
-    if out is None:
-        out = torch.empty((b, heads, d), dtype=q.dtype, device=q.device)
-    elif out.dtype != q.dtype or out.shape != q.shape or out.stride(2) != 1:
-        _refuse(where, "out must be like q")
+    try:
+        at, dtype, (b, heads, d), (q_row, q_head, one) = q.get_device(), q.dtype, q.shape, q.stride()
+        (ck, T, wide), (cv, Tv, wide_v) = _cache(k, k_levels), _cache(v, v_levels)
+        (seqs, columns), (table_row, by) = table.shape, table.stride()
+        i32 = torch.int32
+        fine = (ck is not None and cv is not None and (k_levels is None) == (v_levels is None) and one == 1
+                and T == Tv == _TYPES.get(dtype) and wide == wide_v == d and seqs == b and (by == 1 or columns < 2)
+                and table.dtype == i32 and lengths.dtype == i32 and lengths.shape == (b,) and lengths.is_contiguous()
+                and (starts is None or (starts.dtype == i32 and starts.shape == (b,) and starts.is_contiguous()
+                                        and starts.get_device() == at))
+                and at == k.get_device() == v.get_device() == table.get_device() == lengths.get_device()
+                == torch.cuda.current_device())
+        if fine:
+            most = columns * ck.page_size
+            if max_len is None:
+                max_len = most
+            if out is None:
+                out = torch.empty((b, heads, d), dtype=dtype, device=q.device)
+                out_row, out_head = heads * d, d
+            else:
+                out_row, out_head, one = out.stride()
+                fine = one == 1 and out.dtype == dtype and out.shape == q.shape and out.get_device() == at
+            if ws is None:
+                ws = workspace_attend(b, heads, ck.heads, d, max_len)
+            fine = fine and max_len <= most and ws.dtype == torch.uint8 and ws.get_device() == at
+    except (AttributeError, TypeError, ValueError, IndexError):
+        fine = False
+    if not fine:
+        _attend_refused(torch, q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws)
     lse = torch.empty((b, heads), dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = workspace_attend(b, heads, ck.heads, d, max_len)
-    rc = lib().ecasq_attend(q.data_ptr(), q.stride(0), q.stride(1), b, heads, C.byref(ck), C.byref(cv), table.data_ptr(),
-                            table.stride(0) if b > 1 else table.shape[1], lengths.data_ptr(),
-                            None if starts is None else starts.data_ptr(), max_len,
-                            d ** -0.5 if scale is None else float(scale), out.data_ptr(), out.stride(0), out.stride(1),
-                            lse.data_ptr(), ws.data_ptr(), ws.numel(), _status_ptr(where, status),
-                            _stream_of(at))
-    _check(rc, where)
+    rc = L.ecasq_attend(q.data_ptr(), q_row, q_head, b, heads, C.byref(ck), C.byref(cv), table.data_ptr(),
+                        table_row if b > 1 else columns, lengths.data_ptr(), None if starts is None else starts.data_ptr(),
+                        max_len, d ** -0.5 if scale is None else scale, out.data_ptr(), out_row, out_head, lse.data_ptr(),
+                        ws.data_ptr(), ws.numel(), _status_ptr("ecasq_attend", at, status),
+                        _raw_stream(at))
+    if rc:
+        _check(rc, "ecasq_attend")
     return out, lse
+
 
 def ecasq_kernel_launches() -> int:
     """Kernels the library has launched in this process so far."""
