@@ -664,7 +664,8 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
                 and len(shape) <= 2 and (strides[-1] == 1 or k < 2) and one == 1 and wide >= 64 * -(-k // 128)
                 and group >= 32 and not group % 32 and 1 <= m <= 16 and (m == 1 or levels.stride(0) == 1)
                 and groups[0] == n and groups[1] >= -(-k // group) and (by == 1 or groups[1] < 2)
-                and at == codes.get_device() == levels.get_device() == scales.get_device() == torch.cuda.current_device())
+                and at >= 0 and at == codes.get_device() == levels.get_device() == scales.get_device()
+                and at == torch.cuda.current_device())
         if out is not None:
             y = out
             fine = (fine and y.get_device() == at and y.dtype == dtype and y.shape == shape[:-1] + codes.shape[:1]
@@ -752,7 +753,8 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
                 and heads == codes.shape[2] and slots.dtype == torch.int64 and slots.numel() == n and slots.is_contiguous()
                 and Q.dtype == torch.float32 and Q.is_contiguous() and 1 <= s <= levels.shape[3] and Q.numel() == rows * s
                 and (m is None or (m.dtype == torch.int32 and m.numel() == rows and m.is_contiguous() and m.get_device() == at))
-                and at == Q.get_device() == slots.get_device() == codes.get_device() == torch.cuda.current_device())
+                and at >= 0 and at == Q.get_device() == slots.get_device() == codes.get_device()
+                and at == torch.cuda.current_device())
     except (AttributeError, TypeError, ValueError, IndexError):
         fine = False
     if not fine:
@@ -813,8 +815,8 @@ def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None
                 and table.dtype == i32 and lengths.dtype == i32 and lengths.shape == (b,) and lengths.is_contiguous()
                 and (starts is None or (starts.dtype == i32 and starts.shape == (b,) and starts.is_contiguous()
                                         and starts.get_device() == at))
-                and at == k.get_device() == v.get_device() == table.get_device() == lengths.get_device()
-                == torch.cuda.current_device())
+                and at >= 0 and at == k.get_device() == v.get_device() == table.get_device() == lengths.get_device()
+                and at == torch.cuda.current_device())
         if fine:
             most = columns * ck.page_size
             if max_len is None:
