@@ -23,39 +23,49 @@ template <typename X> __device__ __forceinline__ Four<X> load4(const X *p) {
     return x;
 }
 
-struct WriteArgs {
+// I: row numbers, slots and strides, 32 bits where all of them are below 2^31.
+template <typename I> struct WriteArgs {
     const void *x;
     const float *Q;
     const int32_t *m;
     const int64_t *slots;
-    ecasq_cache_t c;
-    int64_t x_row, x_head, rows;  // rows: n heads
+    uint8_t *codes;
+    void *levels;
+    int64_t end;                  // slots of the cache
     uint64_t seed;
-    int32_t s;
     int32_t *status;
-    FastDiv heads, page;
+    I x_row, x_head, row_page, row_slot, row_head, level_page, level_slot, level_head, rows;  // strides as in ecasq_cache_t; rows: n heads
+    int32_t s, d, heads, page_size;
+    FastDiv by_heads, by_page;
 };
+
+template <typename I> __device__ __forceinline__ I quotient(I v, const FastDiv &f, int32_t n) {
+    if (sizeof(I) == 8) return v / n;
+    return f.mul ? __umulhi((uint32_t)v, f.mul) >> f.shift : (uint32_t)v >> f.shift;
+}
+__device__ __forceinline__ uint64_t product(uint32_t a, uint32_t b) { return (uint64_t)a * b; }
+__device__ __forceinline__ int64_t product(int64_t a, int64_t b) { return a * b; }
+__device__ __forceinline__ float shared_float(uint32_t at) { return *static_cast<const float *>(__cvta_shared_to_generic(at)); }
 
 // LV levels a row.  W lanes take a row, four neighbouring entries at a time each: 16 for rows of up to 64 entries, else 32.
 // The row's levels and the gaps above them lie in shared memory, a word a bank, so lanes that look up different levels
-// do not meet.  I: row numbers and slots, 32 bits where they are below 2^31.
+// do not meet.
 //
 // What bounds it: instruction issue, as in the flat encode; the rule's draw alone is about 20 instructions an
 // entry.  So the draw is the 32-bit form of draw.cuh, the search takes log2 LV steps, and the gaps are formed once a row;
 // an entry equal to its level needs no test (its distance 0 is above no product), nor does one at or beyond the last level
-// (the gap there is infinite).  The next row is on its way while this one is encoded.
+// (the gap there is infinite).  The search's position is a shared-memory address that steps by predicated fp32 additions of
+// its bits, denormals whose sums are exact, on the pipe that has room.  The next row is on its way while this one is
+// encoded.
 constexpr int kWriteThreads = 256;
 template <typename X, typename T, int LV, int W, typename I>
-__global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_constant__ WriteArgs<I> a) {
     constexpr int kRows = kWriteThreads / W;  // of a block at a time
     __shared__ float books[kRows][32];        // levels, NaN beyond the last (no entry passes it), and gaps from word 16 on
     const int lane = threadIdx.x % W;
     float *book = books[threadIdx.x / W];
+    const uint32_t book_at = (uint32_t)__cvta_generic_to_shared(book);
     const unsigned group = W == 32 ? 0xffffffffu : 0xffffu << (threadIdx.x & 16);  // the row's lanes
-    auto quotient = [](I v, const FastDiv &f, int32_t n) -> I {
-        if (sizeof(I) == 8) return v / n;
-        return f.mul ? __umulhi((uint32_t)v, f.mul) >> f.shift : (uint32_t)v >> f.shift;
-    };
     struct Row {
         int64_t slot;
         I i, h;
@@ -63,84 +73,96 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
         float q;
         Four<X> x;
     };
+    auto row_of_x = [&](I i, I h) { return static_cast<const X *>(a.x) + product(i, a.x_row) + product(h, a.x_head); };
     auto fetch = [&](I row) {
         Row r;
-        r.i = quotient(row, a.heads, a.c.heads);
-        r.h = row - r.i * (I)a.c.heads;
+        r.i = quotient(row, a.by_heads, a.heads);
+        r.h = row - r.i * (I)a.heads;
         r.slot = a.slots[r.i];
         r.m = a.m ? a.m[row] : a.s;
-        r.q = lane < a.s ? a.Q[(int64_t)row * a.s + lane] : 0.f;
-        if (4 * lane < a.c.d) r.x = load4(static_cast<const X *>(a.x) + (int64_t)r.i * a.x_row + (int64_t)r.h * a.x_head + 4 * lane);
+        r.q = lane < a.s ? a.Q[product(row, (I)a.s) + lane] : 0.f;
+        if (4 * lane < a.d) r.x = load4(row_of_x(r.i, r.h) + 4 * lane);
         return r;
     };
     int bad = 0;
     const I stride = (I)gridDim.x * kRows;
     I row = (I)blockIdx.x * kRows + threadIdx.x / W;
     Row next;
-    if (row < (I)a.rows) next = fetch(row);
-    for (; row < (I)a.rows; row += stride) {
+    if (row < a.rows) next = fetch(row);
+    for (; row < a.rows; row += stride) {
         const Row r = next;
-        if ((I)a.rows - row > stride) next = fetch(row + stride);
+        if (a.rows - row > stride) next = fetch(row + stride);
         if (r.slot < 0) continue;
-        if (r.slot >= a.c.pages * a.c.page_size) {  // (before the division, which below 2^31 slots takes 32 bits)
+        if (r.slot >= a.end) {  // (before the division, which below 2^31 slots takes 32 bits)
             bad |= ECASQ_BAD_PAGE;
             continue;
         }
-        const I page = quotient((I)r.slot, a.page, a.c.page_size), at = (I)r.slot - page * (I)a.c.page_size;
+        const I page = quotient((I)r.slot, a.by_page, a.page_size), at = (I)r.slot - page * (I)a.page_size;
         const int m = min(max(r.m, 1), a.s);
         if (m != r.m) bad |= ECASQ_BAD_COUNT;
         __syncwarp(group);  // the row before is done with the book
         const T rounded = from_f32<T>(r.q);
         const float mine = to_f32(rounded), last = __shfl_sync(group, mine, m - 1, W), above = __shfl_down_sync(group, mine, 1, W);
         if (lane < LV) {
-            T *levels = static_cast<T *>(a.c.levels) + ((int64_t)page * a.c.level_page + (int64_t)at * a.c.level_slot + (int64_t)r.h * a.c.level_head);
+            T *levels = static_cast<T *>(a.levels) + product(page, a.level_page) + product(at, a.level_slot) + product(r.h, a.level_head);
             levels[lane] = lane < m ? rounded : from_f32<T>(last);
             book[lane] = lane < m ? mine : CUDART_NAN_F;
             book[16 + lane] = lane + 1 < m ? __fsub_rn(above, mine) : CUDART_INF_F;
         }
         __syncwarp(group);
-        uint8_t *codes = static_cast<uint8_t *>(a.c.rows) + ((int64_t)page * a.c.row_page + (int64_t)at * a.c.row_slot + (int64_t)r.h * a.c.row_head);
+        uint8_t *codes = a.codes + product(page, a.row_page) + product(at, a.row_slot) + product(r.h, a.row_head);
         Four<X> x = r.x;
-        uint64_t z = a.seed + ((uint64_t)row * (uint32_t)a.c.d + 4 * lane + 1) * kGamma;
-        for (int e = 4 * lane; e < a.c.d; e += 4 * W) {
+        uint64_t z = a.seed + ((uint64_t)row * (uint32_t)a.d + 4 * lane + 1) * kGamma;
+        for (int e = 4 * lane; e < a.d; e += 4 * W) {
             uint32_t zl = (uint32_t)z, zh = (uint32_t)(z >> 32), word = 0;
+            float largest = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const float v = to_f32(x.v[j]);
-                if (!isfinite(v)) bad |= ECASQ_BAD_VALUE;
-                int t = 0;
+                asm("max.NaN.f32 %0, %0, %1;" : "+f"(largest) : "f"(fabsf(v)));
+                float t = __uint_as_float(book_at);  // the address of the largest level passed
 #pragma unroll
                 for (int b = LV / 2; b; b >>= 1)
-                    if (book[t + b] <= v) t += b;
+                    if (shared_float(__float_as_uint(t) + 4 * b) <= v) t = __fadd_rn(t, __uint_as_float(4 * b));
                 const float k = __fmul_rn((float)(splitmix64_hi(zl, zh) >> 8), 0x1p-24f);
-                if (__fmul_rn(k, book[16 + t]) < __fsub_rn(v, book[t])) t++;
-                word |= t << (4 * j);
+                if (__fmul_rn(k, shared_float(__float_as_uint(t) + 64)) < __fsub_rn(v, shared_float(__float_as_uint(t))))
+                    t = __fadd_rn(t, __uint_as_float(4));
+                word += __float_as_uint(t) << (4 * j);
                 add_gamma(zl, zh);
             }
-            *reinterpret_cast<uint16_t *>(codes + e / 2) = (uint16_t)word;
-            if (e + 4 * W < a.c.d) x = load4(static_cast<const X *>(a.x) + (int64_t)r.i * a.x_row + (int64_t)r.h * a.x_head + e + 4 * W);
+            if (!(largest <= 3.402823466e38f)) bad |= ECASQ_BAD_VALUE;
+            *reinterpret_cast<uint16_t *>(codes + e / 2) = (uint16_t)((word - book_at * 0x1111u) >> 2);
+            if (e + 4 * W < a.d) x = load4(row_of_x(r.i, r.h) + e + 4 * W);
             z += 4 * W * kGamma;
         }
     }
     if (bad && a.status) atomicOr(a.status, bad);
 }
 
-template <typename X, typename T, int LV, int W>
-static void launch_write_lanes(const WriteArgs &a, cudaStream_t st) {
-    const unsigned blocks = (unsigned)std::min<int64_t>(cdiv(a.rows, kWriteThreads / W), 152 * 8);
-    const int64_t near = ((int64_t)1 << 31) - 1;
-    if (a.rows <= near && a.c.pages <= near / a.c.page_size) k_cache_write<X, T, LV, W, uint32_t><<<blocks, kWriteThreads, 0, st>>>(a);
-    else k_cache_write<X, T, LV, W, int64_t><<<blocks, kWriteThreads, 0, st>>>(a);
+template <typename X, typename T, typename I>
+static void launch_write(const WriteArgs<I> &a, int32_t levels, cudaStream_t st) {
+    const bool narrow = a.d <= 64;
+    const unsigned blocks = (unsigned)std::min<int64_t>(cdiv((int64_t)a.rows, kWriteThreads / (narrow ? 16 : 32)), 152 * 8);
+    auto *kernel = levels == 8 ? (narrow ? k_cache_write<X, T, 8, 16, I> : k_cache_write<X, T, 8, 32, I>)
+                               : (narrow ? k_cache_write<X, T, 16, 16, I> : k_cache_write<X, T, 16, 32, I>);
+    note_launch();
+    kernel<<<blocks, kWriteThreads, 0, st>>>(a);
 }
-template <typename X, typename T, int LV>
-static void launch_write(const WriteArgs &a, cudaStream_t st) {
-    if (a.c.d <= 64) launch_write_lanes<X, T, LV, 16>(a, st);
-    else launch_write_lanes<X, T, LV, 32>(a, st);
-}
-template <typename X, typename T>
-static void launch_write(const WriteArgs &a, cudaStream_t st) {
-    if (a.c.levels_n == 8) launch_write<X, T, 8>(a, st);
-    else launch_write<X, T, 16>(a, st);
+template <typename I>
+static int write_rows(const void *x, int32_t x_type, int64_t n, int64_t x_row, int64_t x_head, const float *Q, int32_t s, const int32_t *m,
+                      const int64_t *slots, const ecasq_cache_t &c, uint64_t seed, int32_t *status, cudaStream_t st) {
+    const WriteArgs<I> a{x, Q, m, slots, static_cast<uint8_t *>(c.rows), c.levels, c.pages * c.page_size, seed, status, (I)x_row, (I)x_head,
+                         (I)c.row_page, (I)c.row_slot, (I)c.row_head, (I)c.level_page, (I)c.level_slot, (I)c.level_head,
+                         (I)(n * c.heads), s, c.d, c.heads, c.page_size, FastDiv(c.heads), FastDiv(c.page_size)};
+    if (c.type == ECASQ_F16) {
+        if (x_type == ECASQ_F32) launch_write<float, __half>(a, c.levels_n, st);
+        else launch_write<__half, __half>(a, c.levels_n, st);
+    } else {
+        if (x_type == ECASQ_F32) launch_write<float, __nv_bfloat16>(a, c.levels_n, st);
+        else launch_write<__nv_bfloat16, __nv_bfloat16>(a, c.levels_n, st);
+    }
+    ECASQ_LAUNCH_CHECK();
+    return ECASQ_OK;
 }
 
 }  // namespace ecasq
@@ -157,18 +179,14 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
         return ECASQ_EINVAL;
     if (n == 0) return ECASQ_OK;
     if (!x || !Q || !slots) return ECASQ_EINVAL;
-    const WriteArgs a{x, Q, m, slots, *cache, x_row, x_head, n * cache->heads, seed, s, status, FastDiv(cache->heads), FastDiv(cache->page_size)};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    note_launch();
-    if (cache->type == ECASQ_F16) {
-        if (x_type == ECASQ_F32) launch_write<float, __half>(a, st);
-        else launch_write<__half, __half>(a, st);
-    } else {
-        if (x_type == ECASQ_F32) launch_write<float, __nv_bfloat16>(a, st);
-        else launch_write<__nv_bfloat16, __nv_bfloat16>(a, st);
-    }
-    ECASQ_LAUNCH_CHECK();
-    return ECASQ_OK;
+    const ecasq_cache_t &c = *cache;
+    bool near = true;
+    for (const int64_t v : {x_row, x_head, c.row_page, c.row_slot, c.row_head, c.level_page, c.level_slot, c.level_head, n * c.heads,
+                            c.pages * c.page_size})
+        near = near && v >= 0 && v < (int64_t)1 << 31;
+    return near ? write_rows<uint32_t>(x, x_type, n, x_row, x_head, Q, s, m, slots, c, seed, status, st)
+                : write_rows<int64_t>(x, x_type, n, x_row, x_head, Q, s, m, slots, c, seed, status, st);
 }
 
 }  // extern "C"

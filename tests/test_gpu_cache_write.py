@@ -194,6 +194,28 @@ def test_strided_rows():
     assert torch.equal(codes.cpu(), full[0]) and torch.equal(table.cpu(), full[1])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_slots_beyond_32_bits(d):
+    """Slot numbers of 2^31 and more (slots that share memory, as only two rows are written)."""
+    import paper_2608_18147_gb300 as E
+    x, Q, m = make(2, 1, d, 8, "bf16", "f32", seed=6)
+    room = torch.zeros(4, d // 2, dtype=torch.uint8, device="cuda")
+    books = torch.zeros(4, 8, dtype=torch.bfloat16, device="cuda")
+    codes = room.as_strided((4, 1 << 30, 1, d // 2), (d // 2, 0, d // 2, 1))
+    table = books.as_strided((4, 1 << 30, 1, 8), (8, 0, 8, 1))
+    slots = torch.tensor([(1 << 31) + 77, (3 << 30) + 5, ], device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    want, book = reference(x.view(2, d).numpy(), Q, m, 8, "bf16", 4)
+    E.ecasq_cache_write(x.cuda(), Q.cuda(), m.cuda(), slots, codes, table, 4, status=status)
+    assert status.item() == 0 and not room[:2].any() and not books[:2].any()
+    c = room[2:].cpu().numpy()
+    np.testing.assert_array_equal(np.stack((c & 15, c >> 4), axis=-1).reshape(2, d), want)
+    assert torch.equal(books[2:].cpu(), book)
+    E.ecasq_cache_write(x.cuda(), Q.cuda(), m.cuda(), slots + (1 << 31), codes, table, 5, status=status)
+    assert status.item() == E.BAD_PAGE
+    assert np.array_equal(room[2:].cpu().numpy(), c)
+
+
 def test_refusals():
     import paper_2608_18147_gb300 as E
     x, Q, m = make(4, 2, 64, 8, "f16", "f32")
