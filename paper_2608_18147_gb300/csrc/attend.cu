@@ -5,96 +5,147 @@
 
 namespace ecasq {
 
-// Splits.  A block has a fixed cost of its own (its first loads' latency, the join), so a split should be long; and the
-// blocks should fill the card evenly.  `slots` blocks run at once; up to kLong keys for each of them there is
-// one round of blocks, beyond that as many rounds as keep a split at most about that long.
-constexpr int kSms = 152, kMostResident = 8, kLong = 1024, kStep = 64;
+// Splits.  A block has a fixed cost of its own, about what kCost keys take it (its first loads' latency, the join), so a
+// split should be long; and the blocks should fill the card evenly: with `slots` of them at once, n splits a sequence take
+// ceil(b blocks n / slots) rounds of a split's keys and that cost.
+constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kStep = 64;
 
 struct Splits {
     int32_t chunk, count;
 };
-static Splits make_splits(int64_t b, int64_t blocks, int64_t max_len, int64_t slots) {
-    const int64_t per = std::max<int64_t>(1, cdiv(b * blocks * max_len, slots));
-    const int64_t want = cdiv(per, cdiv(per, kLong));
-    // Splits count from the tile of the first key, so one more tile than max_len may be needed.
-    const int64_t span = max_len + kTile - 1;
-    const int64_t count = std::min<int64_t>(std::max<int64_t>(1, cdiv(span, cdiv(want, kStep) * kStep)), 65535);
-    const int64_t chunk = cdiv(cdiv(span, count), kStep) * kStep;
-    return {(int32_t)chunk, (int32_t)cdiv(span, chunk)};
+static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots) {
+    const int64_t all = std::max<int64_t>(1, b * blocks);
+    Splits best{0, 0};
+    int64_t least = INT64_MAX;
+    for (int64_t rounds = 1; rounds <= kMostRounds; rounds++) {  // the most splits that this many rounds hold
+        const int64_t n = std::max<int64_t>(1, slots * rounds / all);
+        const int64_t chunk = std::max<int64_t>(1, cdiv(cdiv(span, n), kStep)) * kStep, count = std::max<int64_t>(1, cdiv(span, chunk));
+        const int64_t cost = cdiv(all * count, slots) * (chunk + kCost);
+        if (cost < least) {
+            least = cost;
+            best = {(int32_t)chunk, (int32_t)count};
+        }
+        if (chunk == kStep) break;
+    }
+    return best;
 }
-static size_t part_bytes(int64_t b, int64_t heads, int32_t d, int64_t splits) { return (size_t)(b * heads * splits * PartAt(d).stride) * 4; }
+// Bytes of the splits' results, for the most splits that make_splits may choose.  (Splits count from the tile of the first
+// key, so with a start one more tile may be needed.)
+static size_t part_bytes(int64_t b, int64_t heads, int64_t blocks, int32_t d, int64_t max_len) {
+    const int64_t all = std::max<int64_t>(1, b * blocks), most = std::max<int64_t>(1, (int64_t)kSms * kMostResident * kMostRounds / all);
+    const int64_t splits = std::min(most, cdiv(max_len + kTile - 1, kStep));
+    return splits > 1 ? (size_t)(b * heads * splits * PartAt(d).stride) * 4 : 0;
+}
 
 int split_attend(AttendArgs &a, int64_t b, int resident) {
-    const Splits s = make_splits(b, (int64_t)(a.heads / a.group) * a.htiles, a.max_len, kSms * std::min(resident, kMostResident));
+    const int64_t blocks = (int64_t)(a.heads / a.group) * a.htiles;
+    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? kTile - 1 : 0), kSms * std::min(resident, kMostResident));
     a.chunk = s.chunk;
     a.splits = s.count;
     if (a.splits == 1) return ECASQ_OK;
-    if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, a.d, a.splits)) return ECASQ_EWORKSPACE;
+    if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, blocks, a.d, a.max_len)) return ECASQ_EWORKSPACE;
     a.part = static_cast<float *>(a.ws);
     return ECASQ_OK;
 }
 
-// A block a sequence and query head: the splits' maxima and sums give each split's share, then 16 to 64 lanes a split add
-// the entries, four a lane, several splits at a time.
+// The splits' maxima and sums give each split's share, then 16 to 64 lanes a split add the entries, four a lane.  A head by
+// a warp (WARPS = 1, eight heads a block, nothing to wait for) where there are few splits, by a block where there are many.
+// A sequence of one split has its result already.
 constexpr int kJoinThreads = 256, kShares = 1024;
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_constant__ AttendArgs a, int lanes) {
-    __shared__ float red[2 * kJoinThreads / 32], share[kShares];
-    __shared__ __align__(16) float4 sums[kJoinThreads];
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_constant__ AttendArgs a) {
+    constexpr int kThreads = 32 * WARPS, kHeadsHere = kJoinThreads / kThreads;
+    __shared__ float red[2 * WARPS], share[WARPS == 1 ? 1 : kShares];
+    __shared__ __align__(16) float4 sums[WARPS == 1 ? 1 : kJoinThreads];
     const int64_t seq = blockIdx.y;
-    const int h = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const int n = max(splits_of(a, seq_span(a, seq)), 1);
+    const int h = blockIdx.x * kHeadsHere + threadIdx.x / kThreads, tid = threadIdx.x % kThreads, lane = tid & 31, wid = tid >> 5;
+    const int n = splits_of(a, seq_span(a, seq));
     const PartAt at(a.d);
     const float *part = at.at(a.part, seq, a.heads, h, a.splits, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (n <= 1 || h >= a.heads) return;
     float m = -CUDART_INF_F;
-    for (int i = tid; i < n; i += kJoinThreads) m = fmaxf(m, part[i * at.stride + a.d]);
+    for (int i = tid; i < n; i += kThreads) m = fmaxf(m, part[i * at.stride + a.d]);
     for (int x = 16; x; x /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    if (lane == 0) red[wid] = m;
-    __syncthreads();
-    m = red[0];
-    for (int w = 1; w < kJoinThreads / 32; w++) m = fmaxf(m, red[w]);
+    if (WARPS > 1) {
+        if (lane == 0) red[wid] = m;
+        __syncthreads();
+        m = red[0];
+        for (int w = 1; w < WARPS; w++) m = fmaxf(m, red[w]);
+    }
     const float base = m == -CUDART_INF_F ? 0.f : m;
     float l = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int e = 4 * (tid % lanes), from = tid / lanes, apart = kJoinThreads / lanes;
-    for (int i0 = 0; i0 < n; i0 += kShares) {
-        const int some = min(kShares, n - i0);
-        const float *p = part + i0 * at.stride;
-        for (int i = tid; i < some; i += kJoinThreads) {
-            const float2 ml = *reinterpret_cast<const float2 *>(p + i * at.stride + a.d);
-            share[i] = exp2_fast(ml.x - base);
-            l += ml.y * share[i];
-        }
-        __syncthreads();
-        if (e < a.d) {
+    if constexpr (WARPS == 1) {
+        const int quads = a.d / 4;
+        float4 v[2] = {};  // entries 4 lane .. and 128 + 4 lane ..
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            float mine = 0.f;
+            if (i0 + lane < n) {
+                const float2 ml = *reinterpret_cast<const float2 *>(part + (i0 + lane) * at.stride + a.d);
+                mine = exp2_fast(ml.x - base);
+                l += ml.y * mine;
+            }
+            const int some = min(32, n - i0);
 #pragma unroll 4
-            for (int i = from; i < some; i += apart) {
-                const float4 x = *reinterpret_cast<const float4 *>(p + i * at.stride + e);
-                const float s = share[i];
-                v.x = fmaf(x.x, s, v.x);
-                v.y = fmaf(x.y, s, v.y);
-                v.z = fmaf(x.z, s, v.z);
-                v.w = fmaf(x.w, s, v.w);
+            for (int i = 0; i < some; i++) {
+                const float s = __shfl_sync(0xffffffffu, mine, i);
+#pragma unroll
+                for (int c = 0; c < 2; c++)
+                    if (lane + 32 * c < quads) {
+                        const float4 x = *reinterpret_cast<const float4 *>(part + (i0 + i) * at.stride + 4 * (lane + 32 * c));
+                        v[c].x = fmaf(x.x, s, v[c].x);
+                        v[c].y = fmaf(x.y, s, v[c].y);
+                        v[c].z = fmaf(x.z, s, v[c].z);
+                        v[c].w = fmaf(x.w, s, v[c].w);
+                    }
             }
         }
-        __syncthreads();
-    }
-    for (int x = 16; x; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
-    if (lane == 0) red[kJoinThreads / 32 + wid] = l;
-    sums[tid] = v;
-    __syncthreads();
-    l = 0.f;
-    for (int w = 0; w < kJoinThreads / 32; w++) l += red[kJoinThreads / 32 + w];
-    if (tid < lanes && e < a.d) {
-        for (int i = 1; i < apart; i++) {
-            const float4 x = sums[i * lanes + tid];
-            v.x += x.x;
-            v.y += x.y;
-            v.z += x.z;
-            v.w += x.w;
+        for (int x = 16; x; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+#pragma unroll
+        for (int c = 0; c < 2; c++)
+            if (lane + 32 * c < quads) store_out<T>(a, seq, h, 4 * (lane + 32 * c), v[c], l);
+    } else {
+        const int lanes = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int e = 4 * (tid % lanes), from = tid / lanes, apart = kThreads / lanes;
+        for (int i0 = 0; i0 < n; i0 += kShares) {
+            const int some = min(kShares, n - i0);
+            const float *p = part + i0 * at.stride;
+            for (int i = tid; i < some; i += kThreads) {
+                const float2 ml = *reinterpret_cast<const float2 *>(p + i * at.stride + a.d);
+                share[i] = exp2_fast(ml.x - base);
+                l += ml.y * share[i];
+            }
+            __syncthreads();
+            if (e < a.d) {
+#pragma unroll 8
+                for (int i = from; i < some; i += apart) {
+                    const float4 x = *reinterpret_cast<const float4 *>(p + i * at.stride + e);
+                    const float s = share[i];
+                    v.x = fmaf(x.x, s, v.x);
+                    v.y = fmaf(x.y, s, v.y);
+                    v.z = fmaf(x.z, s, v.z);
+                    v.w = fmaf(x.w, s, v.w);
+                }
+            }
+            __syncthreads();
         }
-        store_out<T>(a, seq, h, e, v, l);
+        for (int x = 16; x; x /= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+        if (lane == 0) red[WARPS + wid] = l;
+        sums[tid] = v;
+        __syncthreads();
+        l = 0.f;
+        for (int w = 0; w < WARPS; w++) l += red[WARPS + w];
+        if (tid < lanes && e < a.d) {
+            for (int i = 1; i < apart; i++) {
+                const float4 x = sums[i * lanes + tid];
+                v.x += x.x;
+                v.y += x.y;
+                v.z += x.z;
+                v.w += x.w;
+            }
+            store_out<T>(a, seq, h, e, v, l);
+        }
     }
     if (tid == 0 && a.lse) a.lse[seq * a.heads + h] = log_sum(m, l);
 }
@@ -106,13 +157,15 @@ static int launch_join(const AttendArgs &a, int64_t b, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)a.heads, (unsigned)b);
+    const bool warps = a.splits <= 16;
+    cfg.gridDim = dim3((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b);
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     note_launch();
-    ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_attend_join<T>, a, a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64));
+    if (warps) ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_attend_join<T, 1>, a));
+    else ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_attend_join<T, kJoinThreads / 32>, a));
     return ECASQ_OK;
 }
 
@@ -129,11 +182,7 @@ extern "C" {
 
 size_t ecasq_workspace_size_attend(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {
     if (!sizes_ok(b, heads, kv_heads, d, max_len)) return 0;
-    // The most splits over what an SM may hold of the kernels.
-    const int64_t blocks = (int64_t)kv_heads * cdiv(heads / kv_heads, kHeads);
-    int64_t most = 1;
-    for (int r = 1; r <= kMostResident; r++) most = std::max<int64_t>(most, make_splits(b, blocks, max_len, kSms * r).count);
-    return most > 1 ? part_bytes(b, heads, d, most) : 0;
+    return part_bytes(b, heads, (int64_t)kv_heads * cdiv(heads / kv_heads, kHeads), d, max_len);
 }
 
 int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_t heads, const ecasq_cache_t *k,
@@ -159,9 +208,9 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     a.v = static_cast<const char *>(v->rows);
     a.kt = static_cast<const char *>(k->levels);
     a.vt = static_cast<const char *>(v->levels);
-    a.k_page = k->row_page * e;
-    a.k_slot = k->row_slot * e;
-    a.k_head = k->row_head * e;
+    a.k_page = (uint64_t)(k->row_page * e);
+    a.k_slot = (uint64_t)(k->row_slot * e);
+    a.k_head = (uint64_t)(k->row_head * e);
     a.v_page = v->row_page * e;
     a.v_slot = v->row_slot * e;
     a.v_head = v->row_head * e;

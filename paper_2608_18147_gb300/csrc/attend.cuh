@@ -49,8 +49,8 @@ struct AttendArgs {
     size_t ws_bytes;
     int32_t *status;
     const char *k, *v, *kt, *vt; // rows and codebooks
-    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;          // strides in bytes
-    int64_t kt_page, kt_slot, kt_head, vt_page, vt_slot, vt_head;
+    uint64_t k_page, k_slot, k_head, v_page, v_slot, v_head;         // strides in bytes (modulo 2^64)
+    uint64_t kt_page, kt_slot, kt_head, vt_page, vt_slot, vt_head;
     int64_t q_row, q_head, out_row, out_head, table_row, pages;
     float scale2;                // scale log2(e)
     int32_t heads, group, htiles, d, page_size, max_len, chunk, splits;  // group: query heads a key head
@@ -101,10 +101,18 @@ template <> __device__ __forceinline__ void mma16<__nv_bfloat16>(float (&c)[4], 
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // Two values as a pair of T, the first in the low half.
-template <typename T> __device__ __forceinline__ uint32_t pack2(float x, float y) {
-    const T lo = from_f32<T>(x), hi = from_f32<T>(y);
-    return (uint32_t)reinterpret_cast<const uint16_t &>(lo) | (uint32_t)reinterpret_cast<const uint16_t &>(hi) << 16;
+template <typename T> __device__ __forceinline__ uint32_t pack2(float x, float y);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float x, float y) {
+    uint32_t v;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(y), "f"(x));
+    return v;
 }
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float x, float y) {
+    uint32_t v;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(y), "f"(x));
+    return v;
+}
+template <> __device__ __forceinline__ uint32_t pack2<float>(float, float) { return 0; }  // (unused)
 template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v) {
     const uint16_t lo = (uint16_t)v, hi = (uint16_t)(v >> 16);
     return make_float2(to_f32(reinterpret_cast<const T &>(lo)), to_f32(reinterpret_cast<const T &>(hi)));
@@ -234,13 +242,14 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     // ---- copies.  The lane's key of a tile is number lane mod 16; find() looks its page up, a tile ahead of fetch().
     const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
     const char *tb = LV ? (lane < 16 ? a.kt + kh * a.kt_head : a.vt + kh * a.vt_head) : nullptr;  // lanes 16 .. 31 fetch V's codebooks
-    const int64_t t_page = lane < 16 ? a.kt_page : a.vt_page, t_slot = lane < 16 ? a.kt_slot : a.vt_slot;
+    const uint64_t t_page = lane < 16 ? a.kt_page : a.vt_page, t_slot = lane < 16 ? a.kt_slot : a.vt_slot;
     const int32_t *table = a.table + seq * a.table_row;
     const bool whole = a.page_size % kTile == 0;  // a tile lies in one page
     const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
     bool bad_page = false;
     struct Found {
         int page, slot;  // page -2: beyond the split, no error
+        __device__ uint64_t offset(uint64_t by_page, uint64_t by_slot) const { return (uint32_t)page * by_page + (uint32_t)slot * by_slot; }
     };
     auto find = [&](int t0) {
         const int key = t0 + (lane & 15);
@@ -259,10 +268,10 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         const uint32_t mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
         if (lane == 0) seen[stage] = mask;
         if (whole && mask == 0xffffu) {  // sixteen neighbouring slots
-            const int slot0 = f.slot - (lane & 15);
             const int r0 = lane / S::kChunks, c = lane % (S::kChunks < 32 ? S::kChunks : 32);
-            const char *kp = kb + f.page * a.k_page + (slot0 + r0) * a.k_slot + 16 * c;
-            const char *vp = vb + f.page * a.v_page + (slot0 + r0) * a.v_slot + 16 * c;
+            const Found first{f.page, f.slot - (lane & 15) + r0};
+            const char *kp = kb + first.offset(a.k_page, a.k_slot) + 16 * c;
+            const char *vp = vb + first.offset(a.v_page, a.v_slot) + 16 * c;
 #pragma unroll
             for (int i = 0; i < S::kPieces; i++) {
                 // piece lane + 32 i: chunks come round in a row first
@@ -279,11 +288,11 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
             }
         } else {
             // lanes 0 .. 15 hold where the rows of K begin, 16 .. 31 those of V
-            const int64_t row = !ok ? 0 : lane < 16 ? f.page * a.k_page + f.slot * a.k_slot : f.page * a.v_page + f.slot * a.v_slot;
+            const uint64_t row = !ok ? 0 : lane < 16 ? f.offset(a.k_page, a.k_slot) : f.offset(a.v_page, a.v_slot);
 #pragma unroll
             for (int i = 0; i < S::kPieces; i++) {
                 const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
-                const int64_t ko = __shfl_sync(0xffffffffu, row, r), vo = __shfl_sync(0xffffffffu, row, 16 + r);
+                const uint64_t ko = __shfl_sync(0xffffffffu, row, r), vo = __shfl_sync(0xffffffffu, row, 16 + r);
                 if (c < row_chunks) {
                     const bool read = mask >> r & 1;
                     copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + ko + 16 * c : kb, read);
@@ -292,7 +301,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
             }
         }
         if (LV) {
-            const char *src = ok ? tb + f.page * t_page + f.slot * t_slot : tb;
+            const char *src = ok ? tb + f.offset(t_page, t_slot) : tb;
             char *to = dst + 2 * kTile * S::kRow + (lane < 16 ? lane : kTile + S::v_row(lane & 15)) * S::kBook;
 #pragma unroll
             for (int i = 0; i < LV / 8; i++) copy16(smem_addr(to + 16 * i), src + 16 * i, ok);
@@ -681,7 +690,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
             v.z += y.z;
             v.w += y.w;
         }
-        if (a.splits > 1) {
+        if (active > 1) {
             float *part = at.at(a.part, seq, a.heads, h0 + h, a.splits, split);
             *reinterpret_cast<float4 *>(part + e) = v;
             if (e == 0) *reinterpret_cast<float2 *>(part + a.d) = make_float2(x, sum);
