@@ -8,24 +8,24 @@ namespace ecasq {
 // Splits.  A block has a fixed cost of its own, about what kCost keys take it (its first loads' latency, the join), so a
 // split should be long; and the blocks should fill the card evenly: with `slots` of them at once, n splits a sequence take
 // ceil(b blocks n / slots) rounds of a split's keys and that cost.
-constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kStep = 64;
+constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kLeastStep = 64;
 
 struct Splits {
     int32_t chunk, count;
 };
-static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots) {
+static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots, int64_t step) {
     const int64_t all = std::max<int64_t>(1, b * blocks);
     Splits best{0, 0};
     int64_t least = INT64_MAX;
     for (int64_t rounds = 1; rounds <= kMostRounds; rounds++) {  // the most splits that this many rounds hold
         const int64_t n = std::max<int64_t>(1, slots * rounds / all);
-        const int64_t chunk = std::max<int64_t>(1, cdiv(cdiv(span, n), kStep)) * kStep, count = std::max<int64_t>(1, cdiv(span, chunk));
+        const int64_t chunk = std::max<int64_t>(1, cdiv(cdiv(span, n), step)) * step, count = std::max<int64_t>(1, cdiv(span, chunk));
         const int64_t cost = cdiv(all * count, slots) * (chunk + kCost);
         if (cost < least) {
             least = cost;
             best = {(int32_t)chunk, (int32_t)count};
         }
-        if (chunk == kStep) break;
+        if (chunk == step) break;
     }
     return best;
 }
@@ -33,13 +33,13 @@ static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots
 // key, so with a start one more tile may be needed.)
 static size_t part_bytes(int64_t b, int64_t heads, int64_t blocks, int32_t d, int64_t max_len) {
     const int64_t all = std::max<int64_t>(1, b * blocks), most = std::max<int64_t>(1, (int64_t)kSms * kMostResident * kMostRounds / all);
-    const int64_t splits = std::min(most, cdiv(max_len + kTile - 1, kStep));
+    const int64_t splits = std::min(most, cdiv(max_len + kTile - 1, kLeastStep));
     return splits > 1 ? (size_t)(b * heads * splits * PartAt(d).stride) * 4 : 0;
 }
 
-int split_attend(AttendArgs &a, int64_t b, int resident) {
+int split_attend(AttendArgs &a, int64_t b, int resident, int step) {
     const int64_t blocks = (int64_t)(a.heads / a.group) * a.htiles;
-    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? kTile - 1 : 0), kSms * std::min(resident, kMostResident));
+    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? kTile - 1 : 0), kSms * std::min(resident, kMostResident), step);
     a.chunk = s.chunk;
     a.splits = s.count;
     if (a.splits == 1) return ECASQ_OK;
@@ -157,7 +157,7 @@ static int launch_join(const AttendArgs &a, int64_t b, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    const bool warps = a.splits <= 16;
+    const bool warps = a.splits <= 16 && a.heads * b >= 8 * kSms;  // (few heads: a warp each would leave the card idle)
     cfg.gridDim = dim3((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b);
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;

@@ -36,7 +36,7 @@
 
 namespace ecasq {
 
-constexpr int kTile = 16;        // keys of a tile
+constexpr int kTile = 16;        // keys of a matrix product; tiles are one or two of them
 constexpr int kHeads = 8;        // query heads of a block at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -66,8 +66,8 @@ struct PartAt {
     }
 };
 
-// Sets a.chunk, a.splits and, where there are several, a.part from the workspace; `resident`: blocks that an SM holds.
-int split_attend(AttendArgs &a, int64_t b, int resident);
+// Sets a.chunk, a.splits and, where there are several, a.part from the workspace; `resident`: blocks that an SM holds; splits are multiples of `step` keys.
+int split_attend(AttendArgs &a, int64_t b, int resident, int step);
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // 16 bytes to shared memory, or 16 zero bytes (src is not read then).
@@ -118,17 +118,40 @@ template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v) {
     return make_float2(to_f32(reinterpret_cast<const T &>(lo)), to_f32(reinterpret_cast<const T &>(hi)));
 }
 
-// A row's codebook as byte planes.
+// A row's codebook as byte planes: the levels' low bytes, then their high bytes.
 template <int LV> struct Book {
     uint32_t lo[LV / 4], hi[LV / 4];
+    // Where they lie as levels, puts them as planes.
+    __device__ static __forceinline__ void split(char *p) {
+        uint4 *q = reinterpret_cast<uint4 *>(p);
+        const uint4 a = q[0];
+        const uint32_t l0 = prmt(a.x, a.y, 0x6420), l1 = prmt(a.z, a.w, 0x6420), h0 = prmt(a.x, a.y, 0x7531), h1 = prmt(a.z, a.w, 0x7531);
+        if (LV == 8) {
+            q[0] = make_uint4(l0, l1, h0, h1);
+        } else {
+            const uint4 b = q[1];
+            q[0] = make_uint4(l0, l1, prmt(b.x, b.y, 0x6420), prmt(b.z, b.w, 0x6420));
+            q[1] = make_uint4(h0, h1, prmt(b.x, b.y, 0x7531), prmt(b.z, b.w, 0x7531));
+        }
+    }
     __device__ __forceinline__ void load(const char *p) {
-#pragma unroll
-        for (int i = 0; i < LV / 8; i++) {
-            const uint4 r = reinterpret_cast<const uint4 *>(p)[i];
-            lo[2 * i] = prmt(r.x, r.y, 0x6420);
-            hi[2 * i] = prmt(r.x, r.y, 0x7531);
-            lo[2 * i + 1] = prmt(r.z, r.w, 0x6420);
-            hi[2 * i + 1] = prmt(r.z, r.w, 0x7531);
+        const uint4 *q = reinterpret_cast<const uint4 *>(p);
+        const uint4 a = q[0];
+        if (LV == 8) {
+            lo[0] = a.x;
+            lo[1] = a.y;
+            hi[0] = a.z;
+            hi[1] = a.w;
+        } else {
+            const uint4 b = q[LV / 8 - 1];
+            lo[0] = a.x;
+            lo[1] = a.y;
+            lo[2 % (LV / 4)] = a.z;
+            lo[3 % (LV / 4)] = a.w;
+            hi[0] = b.x;
+            hi[1] = b.y;
+            hi[2 % (LV / 4)] = b.z;
+            hi[3 % (LV / 4)] = b.w;
         }
     }
     // Entries 4H .. 4H+3 of the word w of eight codes: their low and their high bytes.
@@ -149,23 +172,26 @@ template <int LV> struct Book {
     }
 };
 
-// A tile in shared memory: 16 rows of K, 16 of V, then their codebooks.  T and LV: the rows' type and
+// A tile in shared memory: rows of K, as many of V, then their codebooks.  Sixteen keys, of coded rows 32, whose
+// other costs (maxima, codebooks, addresses) are shared by more keys.  T and LV: the rows' type and
 // levels (0: plain); NV: the row length is at most 64 NV.
 template <typename T, int LV, int NV> struct Shape {
     static constexpr bool kF32 = sizeof(T) == 4;
     static constexpr int kRow = LV ? 32 * NV : 64 * NV * (int)sizeof(T);   // bytes of a row's room
     static constexpr int kChunks = kRow / 16;
     static constexpr int kBook = 2 * LV;                                   // bytes of a codebook
-    static constexpr int kBytes = 2 * kTile * (kRow + kBook);
+    static constexpr int kKeys = LV ? 32 : kTile, kHalves = kKeys / kTile;
+    static constexpr uint32_t kAll = kKeys == 32 ? 0xffffffffu : 0xffffu;
+    static constexpr int kBytes = 2 * kKeys * (kRow + kBook);
     static constexpr int kWarps = kBytes > 16384 ? 3 : kBytes > 8192 ? 2 : 4;
-    static constexpr int kStages = kBytes > 4096 + 1024 ? 2 : kBytes > 2560 ? 3 : 4;
+    static constexpr int kStages = kBytes > 5120 ? 2 : 3;
     static constexpr int kRing = kStages * kBytes;                         // of a warp
     static constexpr int kJoin = kHeads * 64 * NV * 4;                     // a warp's sums at the end, in its ring
     static constexpr int kExtra = (kF32 ? kHeads * 64 * NV * 4 + kWarps * kTile * kHeads * 4 : 0) + kWarps * (2 * kHeads * 4) + kWarps * kStages * 4;
     static constexpr int kSmem = kWarps * kRing + kExtra;
     static_assert(kJoin <= kRing, "");
     static_assert(kSmem <= 227 * 1024, "");
-    static constexpr int kPieces = kTile * kChunks / 32;                   // 16-byte pieces of K (and of V) for a lane
+    static constexpr int kPieces = kTile * kChunks / 32;                   // 16-byte pieces of K (and of V) for a lane and half
     // Where chunk c of key position r lies: swizzled so that the reads described above do not meet in a bank.
     __device__ static __forceinline__ int k_at(int r, int c) {
         if (LV && NV < 4) return r * kRow + 16 * c;
@@ -239,12 +265,11 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     float *wmax = qs + (S::kF32 ? kHeads * 64 * NV + S::kWarps * kTile * kHeads : 0), *wsum = wmax + S::kWarps * kHeads;
     uint32_t *seen = reinterpret_cast<uint32_t *>(wsum + S::kWarps * kHeads) + wid * S::kStages;  // keys of a stage that count
 
-    // ---- copies.  The lane's key of a tile is number lane mod 16; find() looks its page up, a tile ahead of fetch().
+    // ---- copies.  The lane's key of a tile is number lane mod kKeys; find() looks its page up, a tile ahead of fetch().
     const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
-    const char *tb = LV ? (lane < 16 ? a.kt + kh * a.kt_head : a.vt + kh * a.vt_head) : nullptr;  // lanes 16 .. 31 fetch V's codebooks
-    const uint64_t t_page = lane < 16 ? a.kt_page : a.vt_page, t_slot = lane < 16 ? a.kt_slot : a.vt_slot;
+    const char *ktb = LV ? a.kt + kh * a.kt_head : nullptr, *vtb = LV ? a.vt + kh * a.vt_head : nullptr;
     const int32_t *table = a.table + seq * a.table_row;
-    const bool whole = a.page_size % kTile == 0;  // a tile lies in one page
+    const bool whole = a.page_size % kTile == 0;  // sixteen keys lie in one page
     const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
     bool bad_page = false;
     struct Found {
@@ -252,7 +277,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         __device__ uint64_t offset(uint64_t by_page, uint64_t by_slot) const { return (uint32_t)page * by_page + (uint32_t)slot * by_slot; }
     };
     auto find = [&](int t0) {
-        const int key = t0 + (lane & 15);
+        const int key = t0 + (lane & (S::kKeys - 1));
         Found f{-2, 0};
         if (key >= span.first && key < end) {
             const int p = page_of(a, key);
@@ -265,52 +290,66 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         char *dst = ring + stage * S::kBytes;
         const bool ok = f.page >= 0 && f.page < a.pages;
         bad_page |= f.page != -2 && !ok;
-        const uint32_t mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+        const uint32_t mask = __ballot_sync(0xffffffffu, ok) & S::kAll;
         if (lane == 0) seen[stage] = mask;
-        if (whole && mask == 0xffffu) {  // sixteen neighbouring slots
-            const int r0 = lane / S::kChunks, c = lane % (S::kChunks < 32 ? S::kChunks : 32);
-            const Found first{f.page, f.slot - (lane & 15) + r0};
-            const char *kp = kb + first.offset(a.k_page, a.k_slot) + 16 * c;
-            const char *vp = vb + first.offset(a.v_page, a.v_slot) + 16 * c;
+        char *dv = dst + S::kKeys * S::kRow, *dk = dst;
 #pragma unroll
-            for (int i = 0; i < S::kPieces; i++) {
-                // piece lane + 32 i: chunks come round in a row first
-                constexpr int kSame = S::kChunks > 32 ? S::kChunks / 32 : 1, kRows = S::kChunks > 32 ? 1 : 32 / S::kChunks;
-                const int r = r0 + i / kSame * kRows, cc = c + i % kSame * 32;
-                if (cc < row_chunks) {
-                    copy16(smem_addr(dst + S::k_at(r, cc)), kp + i % kSame * 512, true);
-                    copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), cc)), vp + i % kSame * 512, true);
+        for (int half = 0; half < S::kHalves; half++) {
+            if (whole && (mask >> 16 * half & 0xffffu) == 0xffffu) {  // sixteen neighbouring slots
+                const int r0 = lane / S::kChunks, c = lane % (S::kChunks < 32 ? S::kChunks : 32);
+                Found first = f;
+                if (S::kHalves > 1) {
+                    first.page = __shfl_sync(0xffffffffu, f.page, kTile * half);
+                    first.slot = __shfl_sync(0xffffffffu, f.slot, kTile * half) + r0;
+                } else {
+                    first.slot += r0 - (lane & 15);
                 }
-                if (i % kSame == kSame - 1) {
-                    kp += kRows * a.k_slot;
-                    vp += kRows * a.v_slot;
+                const char *kp = kb + first.offset(a.k_page, a.k_slot) + 16 * c;
+                const char *vp = vb + first.offset(a.v_page, a.v_slot) + 16 * c;
+#pragma unroll
+                for (int i = 0; i < S::kPieces; i++) {
+                    // piece lane + 32 i: chunks come round in a row first
+                    constexpr int kSame = S::kChunks > 32 ? S::kChunks / 32 : 1, kRows = S::kChunks > 32 ? 1 : 32 / S::kChunks;
+                    const int r = r0 + i / kSame * kRows, cc = c + i % kSame * 32;
+                    if (cc < row_chunks) {
+                        copy16(smem_addr(dk + S::k_at(r, cc)), kp + i % kSame * 512, true);
+                        copy16(smem_addr(dv + S::v_at(S::v_row(r), cc)), vp + i % kSame * 512, true);
+                    }
+                    if (i % kSame == kSame - 1) {
+                        kp += kRows * a.k_slot;
+                        vp += kRows * a.v_slot;
+                    }
+                }
+            } else {
+                const uint64_t krow = ok ? f.offset(a.k_page, a.k_slot) : 0, vrow = ok ? f.offset(a.v_page, a.v_slot) : 0;
+#pragma unroll
+                for (int i = 0; i < S::kPieces; i++) {
+                    const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
+                    const uint64_t ko = __shfl_sync(0xffffffffu, krow, kTile * half + r), vo = __shfl_sync(0xffffffffu, vrow, kTile * half + r);
+                    if (c < row_chunks) {
+                        const bool read = mask >> (kTile * half + r) & 1;
+                        copy16(smem_addr(dk + S::k_at(r, c)), read ? kb + ko + 16 * c : kb, read);
+                        copy16(smem_addr(dv + S::v_at(S::v_row(r), c)), read ? vb + vo + 16 * c : vb, read);
+                    }
                 }
             }
-        } else {
-            // lanes 0 .. 15 hold where the rows of K begin, 16 .. 31 those of V
-            const uint64_t row = !ok ? 0 : lane < 16 ? f.offset(a.k_page, a.k_slot) : f.offset(a.v_page, a.v_slot);
-#pragma unroll
-            for (int i = 0; i < S::kPieces; i++) {
-                const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
-                const uint64_t ko = __shfl_sync(0xffffffffu, row, r), vo = __shfl_sync(0xffffffffu, row, 16 + r);
-                if (c < row_chunks) {
-                    const bool read = mask >> r & 1;
-                    copy16(smem_addr(dst + S::k_at(r, c)), read ? kb + ko + 16 * c : kb, read);
-                    copy16(smem_addr(dst + kTile * S::kRow + S::v_at(S::v_row(r), c)), read ? vb + vo + 16 * c : vb, read);
-                }
-            }
+            dk += kTile * S::kRow;
+            dv += kTile * S::kRow;
         }
-        if (LV) {
-            const char *src = ok ? tb + f.offset(t_page, t_slot) : tb;
-            char *to = dst + 2 * kTile * S::kRow + (lane < 16 ? lane : kTile + S::v_row(lane & 15)) * S::kBook;
+        if (LV) {  // a lane its key's codebooks
+            const char *ks = ok ? ktb + f.offset(a.kt_page, a.kt_slot) : ktb, *vs = ok ? vtb + f.offset(a.vt_page, a.vt_slot) : vtb;
+            char *to = dst + 2 * S::kKeys * S::kRow;
 #pragma unroll
-            for (int i = 0; i < LV / 8; i++) copy16(smem_addr(to + 16 * i), src + 16 * i, ok);
+            for (int i = 0; i < LV / 8; i++) {
+                copy16(smem_addr(to + lane * S::kBook + 16 * i), ks + 16 * i, ok);
+                copy16(smem_addr(to + (S::kKeys + (lane & 16) + S::v_row(lane & 15)) * S::kBook + 16 * i), vs + 16 * i, ok);
+            }
         }
     };
 
     // The first tiles are on their way before anything else: all their pages at once, then the rows.
-    const int step = kTile * S::kWarps;
-    const int mine = begin + kTile * wid;
+    const int step = S::kKeys * S::kWarps;
+    const int mine = begin + S::kKeys * wid;
     // Chunks beyond the row's end are read but never filled.
     if (row_chunks < S::kChunks) {
         for (int i = lane; i < S::kRing / 16; i += 32) reinterpret_cast<uint4 *>(ring)[i] = make_uint4(0, 0, 0, 0);
@@ -374,11 +413,16 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         fill = fill + 1 == S::kStages ? 0 : fill + 1;
         copies_wait<S::kStages - 1>();
         __syncwarp();
-        const char *kt = ring + use * S::kBytes, *vt = kt + kTile * S::kRow, *bk = vt + kTile * S::kRow, *bv = bk + kTile * S::kBook;
+        char *kt = ring + use * S::kBytes, *vt = kt + S::kKeys * S::kRow, *bk = vt + S::kKeys * S::kRow, *bv = bk + S::kKeys * S::kBook;
         const uint32_t mask = seen[use];
+        if (LV) {
+            Book<LV ? LV : 8>::split(bk + lane * S::kBook);
+            Book<LV ? LV : 8>::split(bv + lane * S::kBook);
+            __syncwarp();
+        }
 
-        // ---- scores: c[0][.] of key g, c[1][.] of key g + 8
-        float c[2][HL];
+        // ---- scores of each half: c[.][0] of key g, c[.][1] of key g + 8
+        float c[S::kHalves][2][HL];
         if constexpr (S::kF32) {
             float v[2][kHeads];
 #pragma unroll
@@ -408,73 +452,78 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const float keep = t & 1 ? w[h + 2] : w[h], give = t & 1 ? w[h] : w[h + 2];
-                    c[u][h % HL] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+                    c[0][u][h % HL] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
                 }
             }
         } else {
-            float c1[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (LV == 0) {
 #pragma unroll
-                for (int i = 0; i < 2 * NV; i++) {
-                    if (32 * i >= a.d) break;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(kt + S::k_at(g, t + 4 * i));
-                    const uint4 y = *reinterpret_cast<const uint4 *>(kt + S::k_at(g + 8, t + 4 * i));
-                    mma16<T>(c1, x.x, y.x, x.y, y.y, qf[4 * i], qf[4 * i + 1]);
-                    mma16<T>(c2, x.z, y.z, x.w, y.w, qf[4 * i + 2], qf[4 * i + 3]);
-                }
-            } else {
-                Book<LV> b0, b1;
-                b0.load(bk + g * S::kBook);
-                b1.load(bk + (g + 8) * S::kBook);
+            for (int half = 0; half < S::kHalves; half++) {
+                const char *kh16 = kt + half * kTile * S::kRow, *bh16 = bk + half * kTile * S::kBook;
+                float c1[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (LV == 0) {
 #pragma unroll
-                for (int i = 0; i < (NV == 4 ? 2 : 1); i++) {
-                    constexpr int kWords = NV == 1 ? 2 : 4;
-                    alignas(16) uint32_t x[kWords], y[kWords];
-                    if constexpr (NV == 1) {
-                        *reinterpret_cast<uint2 *>(x) = *reinterpret_cast<const uint2 *>(kt + g * S::kRow + 8 * t);
-                        *reinterpret_cast<uint2 *>(y) = *reinterpret_cast<const uint2 *>(kt + (g + 8) * S::kRow + 8 * t);
-                    } else {
-                        *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(kt + S::k_at(g, t + 4 * i));
-                        *reinterpret_cast<uint4 *>(y) = *reinterpret_cast<const uint4 *>(kt + S::k_at(g + 8, t + 4 * i));
+                    for (int i = 0; i < 2 * NV; i++) {
+                        if (32 * i >= a.d) break;
+                        const uint4 x = *reinterpret_cast<const uint4 *>(kh16 + S::k_at(g, t + 4 * i));
+                        const uint4 y = *reinterpret_cast<const uint4 *>(kh16 + S::k_at(g + 8, t + 4 * i));
+                        mma16<T>(c1, x.x, y.x, x.y, y.y, qf[4 * i], qf[4 * i + 1]);
+                        mma16<T>(c2, x.z, y.z, x.w, y.w, qf[4 * i + 2], qf[4 * i + 3]);
                     }
+                } else {
+                    Book<LV> b0, b1;
+                    b0.load(bh16 + g * S::kBook);
+                    b1.load(bh16 + (g + 8) * S::kBook);
 #pragma unroll
-                    for (int w = 0; w < kWords; w++) {
-                        const uint32_t *q4 = qf + 4 * (kWords * i + w);
-                        uint32_t xl, xh, yl, yh;
-                        b0.template look<0>(x[w], xl, xh);
-                        b1.template look<0>(y[w], yl, yh);
-                        mma16<T>(c1, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[0], q4[1]);
-                        b0.template look<1>(x[w], xl, xh);
-                        b1.template look<1>(y[w], yl, yh);
-                        mma16<T>(c2, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[2], q4[3]);
+                    for (int i = 0; i < (NV == 4 ? 2 : 1); i++) {
+                        constexpr int kWords = NV == 1 ? 2 : 4;
+                        alignas(16) uint32_t x[kWords], y[kWords];
+                        if constexpr (NV == 1) {
+                            *reinterpret_cast<uint2 *>(x) = *reinterpret_cast<const uint2 *>(kh16 + g * S::kRow + 8 * t);
+                            *reinterpret_cast<uint2 *>(y) = *reinterpret_cast<const uint2 *>(kh16 + (g + 8) * S::kRow + 8 * t);
+                        } else {
+                            *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(kh16 + S::k_at(g, t + 4 * i));
+                            *reinterpret_cast<uint4 *>(y) = *reinterpret_cast<const uint4 *>(kh16 + S::k_at(g + 8, t + 4 * i));
+                        }
+#pragma unroll
+                        for (int w = 0; w < kWords; w++) {
+                            const uint32_t *q4 = qf + 4 * (kWords * i + w);
+                            uint32_t xl, xh, yl, yh;
+                            b0.template look<0>(x[w], xl, xh);
+                            b1.template look<0>(y[w], yl, yh);
+                            mma16<T>(c1, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[0], q4[1]);
+                            b0.template look<1>(x[w], xl, xh);
+                            b1.template look<1>(y[w], yl, yh);
+                            mma16<T>(c2, prmt(xl, xh, 0x5140), prmt(yl, yh, 0x5140), prmt(xl, xh, 0x7362), prmt(yl, yh, 0x7362), q4[2], q4[3]);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int h = 0; h < HL; h++) {
-                c[0][h] = c1[h] + c2[h];
-                c[1][h] = c1[2 + h] + c2[2 + h];
+                for (int h = 0; h < HL; h++) {
+                    c[half][0][h] = c1[h] + c2[h];
+                    c[half][1][h] = c1[2 + h] + c2[2 + h];
+                }
             }
         }
 
         // ---- running maximum, weights, sums
+        if (mask != S::kAll) {  // rows that are not seen hold zeros; their scores do not count
 #pragma unroll
-        for (int h = 0; h < HL; h++) {
-            c[0][h] *= a.scale2;
-            c[1][h] *= a.scale2;
-        }
-        if (mask != 0xffffu) {  // rows that are not seen hold zeros; their scores do not count
+            for (int u = 0; u < 2 * S::kHalves; u++)
 #pragma unroll
-            for (int h = 0; h < HL; h++) {
-                if (!(mask >> g & 1)) c[0][h] = -CUDART_INF_F;
-                if (!(mask >> (g + 8) & 1)) c[1][h] = -CUDART_INF_F;
-            }
+                for (int h = 0; h < HL; h++)
+                    c[u >> 1][u & 1][h] = mask >> (8 * u + g) & 1 ? c[u >> 1][u & 1][h] * a.scale2 : -CUDART_INF_F;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2 * S::kHalves; u++)
+#pragma unroll
+                for (int h = 0; h < HL; h++) c[u >> 1][u & 1][h] *= a.scale2;
         }
         float top[HL], base[HL];
         bool moved = false;
 #pragma unroll
         for (int h = 0; h < HL; h++) {
-            top[h] = fmaxf(c[0][h], c[1][h]);
+            top[h] = fmaxf(c[0][0][h], c[0][1][h]);
+            if (S::kHalves > 1) top[h] = fmaxf(top[h], fmaxf(c[S::kHalves - 1][0][h], c[S::kHalves - 1][1][h]));
 #pragma unroll
             for (int x = 4; x < 32; x *= 2) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], x));
             top[h] = fmaxf(top[h], m[h]);
@@ -502,16 +551,18 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
             }
         }
 #pragma unroll
-        for (int h = 0; h < HL; h++) {
-            c[0][h] = exp2_fast(c[0][h] - base[h]);
-            c[1][h] = exp2_fast(c[1][h] - base[h]);
-            l[h] += c[0][h] + c[1][h];
-        }
+        for (int h = 0; h < HL; h++)
+#pragma unroll
+            for (int half = 0; half < S::kHalves; half++) {
+                c[half][0][h] = exp2_fast(c[half][0][h] - base[h]);
+                c[half][1][h] = exp2_fast(c[half][1][h] - base[h]);
+                l[h] += c[half][0][h] + c[half][1][h];
+            }
 
         // ---- values
         if constexpr (S::kF32) {
-            *reinterpret_cast<float2 *>(ps + g * kHeads + 2 * t) = make_float2(c[0][0], c[0][HL - 1]);
-            *reinterpret_cast<float2 *>(ps + (g + 8) * kHeads + 2 * t) = make_float2(c[1][0], c[1][HL - 1]);
+            *reinterpret_cast<float2 *>(ps + g * kHeads + 2 * t) = make_float2(c[0][0][0], c[0][0][HL - 1]);
+            *reinterpret_cast<float2 *>(ps + (g + 8) * kHeads + 2 * t) = make_float2(c[0][1][0], c[0][1][HL - 1]);
             __syncwarp();
             constexpr int kLanes = NV == 1 ? 16 : 32, kRows = 32 / kLanes, kCols = NV == 4 ? 2 : 1;
 #pragma unroll 4
@@ -533,14 +584,17 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                 }
             }
         } else {
+#pragma unroll
+          for (int part = 0; part < S::kHalves; part++) {
+            const char *v16 = vt + part * kTile * S::kRow, *b16 = bv + part * kTile * S::kBook;
             // The weights as second operand, high parts and low parts.  After the transposition the lane holds those
             // of the keys 2t, 2t + 1 and of 2t + 8, 2t + 9, of head g or (HT = 4) g / 2.
             uint32_t hi[HT == 4 ? 4 : 2], lo[HT == 4 ? 4 : 2];
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                const uint32_t h = pack2<T>(c[u][0], c[u][HL - 1]);
+                const uint32_t h = pack2<T>(c[part][u][0], c[part][u][HL - 1]);
                 const float2 f = unpack2<T>(h);
-                const uint32_t th = transpose8x8(h), tl = transpose8x8(pack2<T>(c[u][0] - f.x, c[u][HL - 1] - f.y));
+                const uint32_t th = transpose8x8(h), tl = transpose8x8(pack2<T>(c[part][u][0] - f.x, c[part][u][HL - 1] - f.y));
                 if constexpr (HT == 4) {
                     hi[2 * u] = prmt(th, 0, sel0);
                     hi[2 * u + 1] = prmt(th, 0, sel1);
@@ -576,7 +630,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                     if (64 * i >= a.d) break;
                     uint4 x[4];
 #pragma unroll
-                    for (int r = 0; r < 4; r++) x[r] = *reinterpret_cast<const uint4 *>(vt + S::v_at(t + 4 * r, g + 8 * i));
+                    for (int r = 0; r < 4; r++) x[r] = *reinterpret_cast<const uint4 *>(v16 + S::v_at(t + 4 * r, g + 8 * i));
                     put(2 * i, {{x[0].x, x[0].y}, {x[1].x, x[1].y}, {x[2].x, x[2].y}, {x[3].x, x[3].y}});
                     put(2 * i + 1, {{x[0].z, x[0].w}, {x[1].z, x[1].w}, {x[2].z, x[2].w}, {x[3].z, x[3].w}});
                 }
@@ -585,11 +639,11 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                 alignas(16) uint32_t x[4][NV];
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    bb[r].load(bv + (t + 4 * r) * S::kBook);
-                    if constexpr (NV == 1) x[r][0] = *reinterpret_cast<const uint32_t *>(vt + S::v_at(t + 4 * r, 0) + 4 * g);
+                    bb[r].load(b16 + (t + 4 * r) * S::kBook);
+                    if constexpr (NV == 1) x[r][0] = *reinterpret_cast<const uint32_t *>(v16 + S::v_at(t + 4 * r, 0) + 4 * g);
                     else if constexpr (NV == 2)
-                        *reinterpret_cast<uint2 *>(x[r]) = *reinterpret_cast<const uint2 *>(vt + S::v_at(t + 4 * r, g >> 1) + 8 * (g & 1));
-                    else *reinterpret_cast<uint4 *>(x[r]) = *reinterpret_cast<const uint4 *>(vt + S::v_at(t + 4 * r, g));
+                        *reinterpret_cast<uint2 *>(x[r]) = *reinterpret_cast<const uint2 *>(v16 + S::v_at(t + 4 * r, g >> 1) + 8 * (g & 1));
+                    else *reinterpret_cast<uint4 *>(x[r]) = *reinterpret_cast<const uint4 *>(v16 + S::v_at(t + 4 * r, g));
                 }
                 auto half = [&](int w, auto hh) {
                     constexpr int H = decltype(hh)::value;
@@ -609,6 +663,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                     half(w, std::integral_constant<int, 1>());
                 }
             }
+          }
         }
         use = use + 1 == S::kStages ? 0 : use + 1;
         __syncwarp();
@@ -724,7 +779,7 @@ static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
         if (resident < 1) return ECASQ_ECUDA;
         if (device < kDevices) known[device].store(resident, std::memory_order_release);
     }
-    const int rc = split_attend(a, b, resident);
+    const int rc = split_attend(a, b, resident, S::kKeys * 4);
     if (rc) return rc;
     const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
     note_launch();
