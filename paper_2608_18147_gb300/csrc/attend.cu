@@ -7,11 +7,12 @@ namespace ecasq {
 
 // Splits.  A block has a fixed cost of its own, about what kCost keys take it (its first loads' latency, the join), so a
 // split should be long; and the blocks should fill the card evenly: with `slots` of them at once, n splits a sequence take
-// ceil(b blocks n / slots) rounds of a split's keys and that cost.
+// ceil(b blocks n / slots) rounds of a split's keys and that cost.  With one round a shorter sequence takes shorter splits, so that
+// all blocks still work; with several the splits keep their length, and their number adapts.
 constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kLeastStep = 64;
 
 struct Splits {
-    int32_t chunk, count;
+    int32_t least, count;
 };
 static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots, int64_t step) {
     const int64_t all = std::max<int64_t>(1, b * blocks);
@@ -23,7 +24,7 @@ static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots
         const int64_t cost = cdiv(all * count, slots) * (chunk + kCost);
         if (cost < least) {
             least = cost;
-            best = {(int32_t)chunk, (int32_t)count};
+            best = {(int32_t)(all * count <= slots ? step : chunk), (int32_t)count};
         }
         if (chunk == step) break;
     }
@@ -37,10 +38,10 @@ static size_t part_bytes(int64_t b, int64_t heads, int64_t blocks, int32_t d, in
     return splits > 1 ? (size_t)(b * heads * splits * PartAt(d).stride) * 4 : 0;
 }
 
-int split_attend(AttendArgs &a, int64_t b, int resident, int step) {
+int split_attend(AttendArgs &a, int64_t b, int resident) {
     const int64_t blocks = (int64_t)(a.heads / a.group) * a.htiles;
-    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? kTile - 1 : 0), kSms * std::min(resident, kMostResident), step);
-    a.chunk = s.chunk;
+    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? kTile - 1 : 0), kSms * std::min(resident, kMostResident), a.step);
+    a.least = s.least;
     a.splits = s.count;
     if (a.splits == 1) return ECASQ_OK;
     if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, blocks, a.d, a.max_len)) return ECASQ_EWORKSPACE;
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_co
     __shared__ __align__(16) float4 sums[WARPS == 1 ? 1 : kJoinThreads];
     const int64_t seq = blockIdx.y;
     const int h = blockIdx.x * kHeadsHere + threadIdx.x / kThreads, tid = threadIdx.x % kThreads, lane = tid & 31, wid = tid >> 5;
-    const int n = splits_of(a, seq_span(a, seq));
+    const int n = cut_of(a, seq_span(a, seq)).count;
     const PartAt at(a.d);
     const float *part = at.at(a.part, seq, a.heads, h, a.splits, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -53,7 +53,7 @@ struct AttendArgs {
     uint64_t kt_page, kt_slot, kt_head, vt_page, vt_slot, vt_head;
     int64_t q_row, q_head, out_row, out_head, table_row, pages;
     float scale2;                // scale log2(e)
-    int32_t heads, group, htiles, d, page_size, max_len, chunk, splits;  // group: query heads a key head
+    int32_t heads, group, htiles, d, page_size, max_len, splits, step, least;  // group: query heads a key head; least: keys of a split
     uint32_t div_mul, div_shift; // t div page_size = umulhi(t, div_mul) >> div_shift, or t >> div_shift if div_mul is 0
 };
 
@@ -66,8 +66,8 @@ struct PartAt {
     }
 };
 
-// Sets a.chunk, a.splits and, where there are several, a.part from the workspace; `resident`: blocks that an SM holds; splits are multiples of `step` keys.
-int split_attend(AttendArgs &a, int64_t b, int resident, int step);
+// Sets a.splits, a.least and, where there are several, a.part from the workspace; `resident`: blocks that an SM holds; splits are multiples of a.step keys.
+int split_attend(AttendArgs &a, int64_t b, int resident);
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // 16 bytes to shared memory, or 16 zero bytes (src is not read then).
@@ -226,10 +226,18 @@ __device__ __forceinline__ Span seq_span(const AttendArgs &a, int64_t seq) {
     if (s.too_long) s.end = a.max_len;
     return s;
 }
-// Splits are counted from the tile of the first key.
-__device__ __forceinline__ int splits_of(const AttendArgs &a, const Span &s) {
-    const int lead = s.first & ~(kTile - 1);
-    return s.end > s.first ? (s.end - lead + a.chunk - 1) / a.chunk : 0;
+// A sequence's splits are counted from the tile of its first key.  They share its keys evenly, in multiples of a.step,
+// but none but the last has fewer than a.least.
+struct Cut {
+    int lead, chunk, count;
+};
+__device__ __forceinline__ Cut cut_of(const AttendArgs &a, const Span &s) {
+    Cut c{s.first & ~(kTile - 1), a.least, 0};
+    if (s.end <= s.first) return c;
+    const int keys = s.end - c.lead, even = (keys + a.splits - 1) / a.splits;
+    c.chunk = max(a.least, (even + a.step - 1) / a.step * a.step);
+    c.count = (keys + c.chunk - 1) / c.chunk;
+    return c;
 }
 
 __device__ __forceinline__ float log_sum(float top, float sum) { return sum == 0.f ? -CUDART_INF_F : top * kLn2 + logf(sum); }
@@ -254,10 +262,10 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     const int nh = min(HT, a.group - (int)(blockIdx.x % a.htiles) * HT);
     const Span span = seq_span(a, seq);
     if (span.too_long && threadIdx.x == 0 && split == 0 && a.status) atomicOr(a.status, ECASQ_BAD_LENGTH);
-    const int active = splits_of(a, span);
+    const Cut cut = cut_of(a, span);
+    const int active = cut.count;
     if (split >= max(active, 1)) return;
-    const int lead = span.first & ~(kTile - 1);
-    const int begin = lead + split * a.chunk, end = min(span.end, begin + a.chunk);  // keys of this split (from `first` on)
+    const int begin = cut.lead + split * cut.chunk, end = min(span.end, begin + cut.chunk);  // keys of this split (from `first` on)
 
     char *ring = smem + wid * S::kRing;
     float *qs = reinterpret_cast<float *>(smem + S::kWarps * S::kRing);  // fp32: q, then each warp's weights
@@ -779,7 +787,8 @@ static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
         if (resident < 1) return ECASQ_ECUDA;
         if (device < kDevices) known[device].store(resident, std::memory_order_release);
     }
-    const int rc = split_attend(a, b, resident, S::kKeys * 4);
+    a.step = S::kKeys * 4;
+    const int rc = split_attend(a, b, resident);
     if (rc) return rc;
     const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
     note_launch();
