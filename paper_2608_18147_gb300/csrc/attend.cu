@@ -49,8 +49,9 @@ int split_attend(AttendArgs &a, int64_t b, int resident) {
     return ECASQ_OK;
 }
 
-// The splits' maxima and sums give each split's share, then 16 to 64 lanes a split add the entries, four a lane.  A head by
-// a warp (WARPS = 1, eight heads a block, nothing to wait for) where there are few splits, by a block where there are many.
+// The splits' maxima and sums give each split's share, then the entries are added, four a lane.  A head by a warp (WARPS = 1,
+// eight heads a block, nothing to wait for) where there are few splits and many heads, else 64 entries of a head by a
+// block, 16 splits at a time.
 // A sequence of one split has its result already.
 constexpr int kJoinThreads = 256, kShares = 1024;
 template <typename T, int WARPS>
@@ -106,9 +107,9 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_co
         for (int c = 0; c < 2; c++)
             if (lane + 32 * c < quads) store_out<T>(a, seq, h, 4 * (lane + 32 * c), v[c], l);
     } else {
-        const int lanes = a.d <= 64 ? 16 : a.d <= 128 ? 32 : 64;
+        constexpr int lanes = 16;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int e = 4 * (tid % lanes), from = tid / lanes, apart = kThreads / lanes;
+        const int e = 64 * blockIdx.z + 4 * (tid % lanes), from = tid / lanes, apart = kThreads / lanes;
         for (int i0 = 0; i0 < n; i0 += kShares) {
             const int some = min(kShares, n - i0);
             const float *p = part + i0 * at.stride;
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_co
             store_out<T>(a, seq, h, e, v, l);
         }
     }
-    if (tid == 0 && a.lse) a.lse[seq * a.heads + h] = log_sum(m, l);
+    if (tid == 0 && blockIdx.z == 0 && a.lse) a.lse[seq * a.heads + h] = log_sum(m, l);
 }
 
 template <typename T>
@@ -159,7 +160,7 @@ static int launch_join(const AttendArgs &a, int64_t b, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
     const bool warps = a.splits <= 16 && a.heads * b >= 8 * kSms;  // (few heads: a warp each would leave the card idle)
-    cfg.gridDim = dim3((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b);
+    cfg.gridDim = dim3((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b, (unsigned)(warps ? 1 : cdiv(a.d, 64)));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;
     cfg.attrs = attr;

@@ -260,6 +260,35 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     const int64_t seq = blockIdx.z;
     const int split = blockIdx.y, kh = blockIdx.x / a.htiles, h0 = kh * a.group + (blockIdx.x % a.htiles) * HT;
     const int nh = min(HT, a.group - (int)(blockIdx.x % a.htiles) * HT);
+    // 16-bit: q as the second operand of S^T, in the order of the lane's chunks of K
+    const T *qp = static_cast<const T *>(a.q) + seq * a.q_row + h0 * a.q_head;
+    constexpr int kSteps = S::kF32 ? 2 : 4 * NV;
+    uint32_t qf[2 * kSteps];
+    if (!S::kF32) {
+        constexpr int kRun = LV ? (NV == 1 ? 16 : 32) : 8;  // consecutive entries of a lane's chunk
+        const int h = g * HT / 8;
+        const bool vec = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_row % 8 == 0 && a.q_head % 8 == 0;
+#pragma unroll
+        for (int i = 0; i < 2 * kSteps; i += 4) {  // eight entries (d is a multiple of eight)
+            const int run = 2 * i / kRun, e = kRun * (t + 4 * run) + 2 * i % kRun;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (h < nh && e < a.d) {
+                const T *from = qp + h * a.q_head + e;
+                if (vec) {
+                    v = *reinterpret_cast<const uint4 *>(from);
+                } else {
+                    v.x = pack2<T>(to_f32(from[0]), to_f32(from[1]));
+                    v.y = pack2<T>(to_f32(from[2]), to_f32(from[3]));
+                    v.z = pack2<T>(to_f32(from[4]), to_f32(from[5]));
+                    v.w = pack2<T>(to_f32(from[6]), to_f32(from[7]));
+                }
+            }
+            qf[i] = v.x;
+            qf[i + 1] = v.y;
+            qf[i + 2] = v.z;
+            qf[i + 3] = v.w;
+        }
+    }
     const Span span = seq_span(a, seq);
     if (span.too_long && threadIdx.x == 0 && split == 0 && a.status) atomicOr(a.status, ECASQ_BAD_LENGTH);
     const Cut cut = cut_of(a, span);
@@ -374,7 +403,6 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     Found next_found = found[S::kStages - 1];
     int next = mine + (S::kStages - 1) * step, fill = S::kStages - 1;
 
-    const T *qp = static_cast<const T *>(a.q) + seq * a.q_row + h0 * a.q_head;
     if (S::kF32) {
         for (int i = threadIdx.x; i < kHeads * 64 * NV; i += 32 * S::kWarps) {
             const int h = i / (64 * NV), e = i % (64 * NV);
@@ -382,20 +410,6 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         }
         __syncthreads();
     }
-    // 16-bit: q as the second operand of S^T, in the order of the lane's chunks of K
-    constexpr int kSteps = S::kF32 ? 1 : 4 * NV;
-    uint32_t qf[2 * kSteps];
-    if (!S::kF32) {
-        constexpr int kRun = LV ? (NV == 1 ? 16 : 32) : 8;  // consecutive entries of a lane's chunk
-        const int h = g * HT / 8;
-#pragma unroll
-        for (int i = 0; i < 2 * kSteps; i++) {
-            const int run = 2 * i / kRun, e = kRun * (t + 4 * run) + 2 * i % kRun;
-            const bool in = h < nh && e < a.d;
-            qf[i] = in ? pack2<T>(to_f32(qp[h * a.q_head + e]), to_f32(qp[h * a.q_head + e + 1])) : 0u;
-        }
-    }
-
     // ---- state: maximum and sum of the lane's heads (the sums of this lane's keys alone), and O
     float m[HL], l[HL];
 #pragma unroll
