@@ -2,7 +2,8 @@
 
 Each translation unit under csrc/ is compiled in parallel, then linked into
 paper_2608_18147_gb300/_build/libecasq.so with the CUDA runtime linked
-statically.
+statically.  csrc/binding.c becomes a Python extension beside it (the C
+compiler and Python's headers).
 """
 from __future__ import annotations
 
@@ -10,11 +11,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libecasq.so")
+BINDING_SRC = os.path.join(CSRC, "binding.c")
+BINDING = os.path.join(OUT, "_codes" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "--expt-relaxed-constexpr",
               "-Xcompiler", "-fPIC,-ffp-contract=off,-fno-fast-math", "-Xptxas", "-warn-spills"]
@@ -39,7 +43,24 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps if os.path.exists(p))
 
 
+def build_binding(force: bool = False) -> str:
+    """The Python extension of csrc/binding.c; its path."""
+    header = os.path.join(HERE, "..", "include", "ecasq.h")
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(map(os.path.getmtime, (BINDING_SRC, header))):
+        return BINDING
+    os.makedirs(OUT, exist_ok=True)
+    tmp = BINDING + ".%d.tmp" % os.getpid()
+    cmd = [os.environ.get("CC", "gcc"), "-std=c11", "-O2", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], BINDING_SRC,
+           "-o", tmp]
+    done = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    if done.returncode != 0:
+        raise RuntimeError("%s failed:\n%s" % (cmd[0], done.stdout.decode(errors="replace")))
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
+    build_binding(force)
     if not force and not _stale():
         return LIB
     os.makedirs(OUT, exist_ok=True)

@@ -563,28 +563,37 @@ def ecasq_prepare(x, ws=None):
 
 # ------------------------------------------------------ operators on 4-bit codes
 #
-# These calls are short, so the binding is too: one condition over what the tensors are, and only where it fails a
-# second look that says what is wrong.
+# These calls are short, so what is in front of them is C too (csrc/binding.c, built beside the library): it looks at the
+# tensors and calls the C entry point.  What it does not take comes back as None, and is looked at here once more to say why.
 
 _TYPES = {}
+_codes = None
 
 
 def _ready():
-    """The library, with the element types known."""
+    """The extension, set up with the library's entry points and torch."""
+    global _codes
     L = lib()
-    if not _TYPES:
-        torch = _torch()
-        _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
-    return L
+    with _lock:
+        if _codes is None:
+            import importlib.machinery
+            import importlib.util
+            torch = _torch()
+            _TYPES.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+            path = _build.build_binding()
+            loader = importlib.machinery.ExtensionFileLoader("_codes", path)
+            module = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_codes", path, loader=loader))
+            loader.exec_module(module)
+            address = lambda fn: C.cast(fn, C.c_void_p).value  # noqa: E731
+            module.setup(address(L.ecasq_matvec), address(L.ecasq_cache_write), address(L.ecasq_attend), torch.Tensor, torch.empty,
+                         torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, workspace_attend,
+                         (torch.float32, torch.float16, torch.bfloat16, torch.uint8, torch.int32, torch.int64))
+            _codes = module
+    return _codes
 
 
 def _refuse(where, what):
     raise EcasqError(EINVAL, "%s: %s" % (where, what))
-
-
-def _raw_stream(index):
-    """The current stream of a device, as _stream() without the object around it."""
-    return _torch()._C._cuda_getCurrentRawStream(index)
 
 
 def _need(where, *wanted):
@@ -613,7 +622,7 @@ def ecasq_pack(idx):
     [n, 64 ceil(k / 128)]."""
     torch = _torch()
     where = "ecasq_pack"
-    L = _ready()
+    L = lib()
     _here(where, idx)
     if idx.dtype != torch.uint8 or idx.dim() != 2 or (idx.shape[1] > 1 and idx.stride(1) != 1):
         _refuse(where, "idx must be uint8 [n, k] with contiguous rows")
@@ -624,7 +633,7 @@ def ecasq_pack(idx):
     return codes
 
 
-def _matvec_refused(torch, x, codes, levels, scales, group, out):
+def _matvec_refused(torch, x, codes, levels, scales, group, out, status):
     where = "ecasq_matvec"
     _here(where, x, codes, levels, scales, out)
     k = lambda: x.shape[-1]  # noqa: E731
@@ -641,7 +650,8 @@ def _matvec_refused(torch, x, codes, levels, scales, group, out):
            "scales must be [n, ceil(k / group)] of x's type or float32 with contiguous rows"),
           (lambda: out is None or (out.dtype == x.dtype and out.shape == x.shape[:-1] + codes.shape[:1]
                                    and (out.shape[-1] < 2 or out.stride(-1) == 1)),
-           "out must be [b, n] (or [n]) of x's type with contiguous rows"))
+           "out must be [b, n] (or [n]) of x's type with contiguous rows"),
+          (lambda: _is_status(status, x), "status must be an int32 tensor on the device of the others"))
     _refuse(where, "bad arguments")
 
 
@@ -651,80 +661,40 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
     x [b, k] or [k] (float32, float16 or bfloat16), codes [n, 64 ceil(k / 128)] as ecasq_pack gives them,
     levels [m <= 16] of x's type, scales [n, ceil(k / group)] of x's type or float32, group a multiple of 32.
     status: int32 tensor that BAD_* bits are or-ed into.  Returns y [b, n] or [n] of x's type (`out` if given)."""
-    L = _ready()
-    torch = _torch()
-    try:
-        at, dtype, shape, strides = x.get_device(), x.dtype, x.shape, x.stride()
-        n, wide = codes.shape
-        code_row, one = codes.stride()
-        groups, (scale_row, by) = scales.shape, scales.stride()
-        (m,), T, S = levels.shape, _TYPES.get(dtype), _TYPES.get(scales.dtype)
-        k = shape[-1]
-        fine = (T is not None and (S == T or S == F32) and levels.dtype == dtype and codes.dtype == torch.uint8
-                and len(shape) <= 2 and (strides[-1] == 1 or k < 2) and one == 1 and wide >= 64 * -(-k // 128)
-                and group >= 32 and not group % 32 and 1 <= m <= 16 and (m == 1 or levels.stride(0) == 1)
-                and groups[0] == n and groups[1] >= -(-k // group) and (by == 1 or groups[1] < 2)
-                and at >= 0 and at == codes.get_device() == levels.get_device() == scales.get_device()
-                and at == torch.cuda.current_device())
-        if out is not None:
-            y = out
-            fine = (fine and y.get_device() == at and y.dtype == dtype and y.shape == shape[:-1] + codes.shape[:1]
-                    and (n < 2 or y.stride(-1) == 1))
-        elif fine:
-            y = torch.empty((shape[0], n) if len(shape) == 2 else (n,), dtype=dtype, device=x.device)
-    except (AttributeError, TypeError, ValueError, IndexError):
-        fine = False
-    if not fine:
-        _matvec_refused(torch, x, codes, levels, scales, group, out)
-    if len(shape) == 2:
-        b, x_row, y_row = shape[0], strides[0], y.stride(0)
-    else:
-        b, x_row, y_row = 1, k, n
-    rc = L.ecasq_matvec(x.data_ptr(), x_row, T, b, codes.data_ptr(), code_row if n > 1 else wide, levels.data_ptr(), m,
-                        scales.data_ptr(), scale_row if n > 1 else groups[1], S, n, k, group, y.data_ptr(), y_row,
-                        _status_ptr("ecasq_matvec", at, status), _raw_stream(at))
-    if rc:
-        _check(rc, "ecasq_matvec")
+    y = (_codes or _ready()).matvec(x, codes, levels, scales, group, out, status)
+    if y is None:
+        _matvec_refused(_torch(), x, codes, levels, scales, group, out, status)
+    if y.__class__ is int:
+        _check(y, "ecasq_matvec")
     return y
 
 
-def _status_ptr(where, at, status):
-    if status is None:
-        return None
-    if status.dtype != _torch().int32 or status.numel() < 1 or status.get_device() != at:
-        _refuse(where, "status must be an int32 tensor on the device of the others")
-    return status.data_ptr()
+def _is_status(status, like):
+    return status is None or (status.dtype == _torch().int32 and status.numel() > 0 and status.get_device() == like.get_device())
 
 
-def _cache(rows, levels):
-    """(the C view of one side of a paged cache, its type, its rows' length), or None for the view if the tensors are not
-    one: rows [pages, page_size, heads, d] (coded: [..., d / 2] uint8 with levels [pages, page_size, heads, 8 or 16]); any strides, a
-    row's entries contiguous."""
-    pages, page_size, heads, d = shape = rows.shape
-    r0, r1, r2, r3 = rows.stride()
+def _cache_type(rows, levels):
+    """(type, row length) of one side of a paged cache; (None, 0) if it is not one."""
+    torch = _torch()
+    if rows.dim() != 4 or rows.stride(3) != 1:
+        return None, 0
     if levels is None:
-        T = _TYPES.get(rows.dtype)
-        if T is None or r3 != 1:
-            return None, None, 0
-        return Cache(rows.data_ptr(), None, r0, r1, r2, 0, 0, 0, pages, page_size, heads, d, T, 0, 0), T, d
-    T, (l0, l1, l2, l3) = _TYPES.get(levels.dtype), levels.stride()
-    n = levels.shape[3]
-    if (not T or r3 != 1 or l3 != 1 or rows.dtype != _torch().uint8 or levels.shape[:3] != shape[:3] or (n != 8 and n != 16)
-            or levels.get_device() != rows.get_device()):
-        return None, None, 0
-    return Cache(rows.data_ptr(), levels.data_ptr(), r0, r1, r2, l0, l1, l2, pages, page_size, heads, 2 * d, T, n, 0), T, 2 * d
+        return (rows.dtype, rows.shape[3]) if rows.dtype in _TYPES else (None, 0)
+    ok = (rows.dtype == torch.uint8 and levels.dim() == 4 and levels.stride(3) == 1 and levels.shape[:3] == rows.shape[:3]
+          and levels.shape[3] in (8, 16) and levels.dtype in (torch.float16, torch.bfloat16))
+    return (levels.dtype, 2 * rows.shape[3]) if ok else (None, 0)
 
 
 _CACHE_IS = ("a cache is [pages, page_size, heads, d] of float32, float16 or bfloat16, or coded uint8 [..., d / 2] with levels "
              "[pages, page_size, heads, 8 or 16] of float16 or bfloat16, with contiguous rows")
 
 
-def _write_refused(torch, x, Q, m, slots, codes, levels):
+def _write_refused(torch, x, Q, m, slots, codes, levels, status):
     where = "ecasq_cache_write"
     _here(where, x, Q, m, slots, codes, levels)
     rows = lambda: slots.numel() * codes.shape[2]  # noqa: E731
     _need(where,
-          (lambda: levels is not None and _cache(codes, levels)[0] is not None, _CACHE_IS),
+          (lambda: levels is not None and _cache_type(codes, levels)[0] is not None, _CACHE_IS),
           (lambda: slots.dtype == torch.int64 and slots.is_contiguous(), "slots must be contiguous int64 [n]"),
           (lambda: x.dtype in (torch.float32, levels.dtype) and x.stride(2) == 1
            and x.shape == (slots.numel(), codes.shape[2], 2 * codes.shape[3]),
@@ -732,7 +702,8 @@ def _write_refused(torch, x, Q, m, slots, codes, levels):
           (lambda: Q.dtype == torch.float32 and Q.is_contiguous() and 1 <= Q.shape[-1] <= levels.shape[3]
            and Q.numel() == rows() * Q.shape[-1], "Q must be contiguous float32 [n * heads, s], s at most the cache's levels"),
           (lambda: m is None or (m.dtype == torch.int32 and m.is_contiguous() and m.numel() == rows()),
-           "m must be contiguous int32 [n * heads]"))
+           "m must be contiguous int32 [n * heads]"),
+          (lambda: _is_status(status, x), "status must be an int32 tensor on the device of the others"))
     _refuse(where, "bad arguments")
 
 
@@ -743,25 +714,9 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
     slots int64 [n] (page * page_size + slot, negative: not written), codes uint8 [pages, page_size, heads, d / 2],
     levels [pages, page_size, heads, 8 or 16] of float16 or bfloat16; x float32 or of levels' type.  status: int32
     tensor that BAD_* bits are or-ed into.  Returns (codes, levels), written in place."""
-    L = _ready()
-    torch = _torch()
-    try:
-        at, (n, heads, d), (x_row, x_head, one) = x.get_device(), x.shape, x.stride()
-        c, T, wide = _cache(codes, levels)
-        X, s, rows = _TYPES.get(x.dtype), Q.shape[-1], n * heads
-        fine = (c is not None and levels is not None and (X == F32 or X == T) and one == 1 and wide == d
-                and heads == codes.shape[2] and slots.dtype == torch.int64 and slots.numel() == n and slots.is_contiguous()
-                and Q.dtype == torch.float32 and Q.is_contiguous() and 1 <= s <= levels.shape[3] and Q.numel() == rows * s
-                and (m is None or (m.dtype == torch.int32 and m.numel() == rows and m.is_contiguous() and m.get_device() == at))
-                and at >= 0 and at == Q.get_device() == slots.get_device() == codes.get_device()
-                and at == torch.cuda.current_device())
-    except (AttributeError, TypeError, ValueError, IndexError):
-        fine = False
-    if not fine:
-        _write_refused(torch, x, Q, m, slots, codes, levels)
-    rc = L.ecasq_cache_write(x.data_ptr(), X, n, x_row, x_head, Q.data_ptr(), s, None if m is None else m.data_ptr(),
-                             slots.data_ptr(), C.byref(c), int(seed) & 0xFFFFFFFFFFFFFFFF,
-                             _status_ptr("ecasq_cache_write", at, status), _raw_stream(at))
+    rc = (_codes or _ready()).cache_write(x, Q, m, slots, codes, levels, seed, status)
+    if rc is None:
+        _write_refused(_torch(), x, Q, m, slots, codes, levels, status)
     if rc:
         _check(rc, "ecasq_cache_write")
     return codes, levels
@@ -774,23 +729,24 @@ def workspace_attend(b, heads, kv_heads, d, max_len):
     return torch.empty(n, dtype=torch.uint8, device="cuda")
 
 
-def _attend_refused(torch, q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws):
+def _attend_refused(torch, q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws, status):
     where = "ecasq_attend"
     _here(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws)
     row = lambda t: t.dtype == torch.int32 and t.shape == q.shape[:1] and t.is_contiguous()  # noqa: E731
     _need(where,
           (lambda: (k_levels is None) == (v_levels is None), "k and v must both be plain or both be coded"),
-          (lambda: _cache(k, k_levels)[0] is not None and _cache(v, v_levels)[0] is not None, _CACHE_IS),
-          (lambda: q.dim() == 3 and q.stride(2) == 1 and _TYPES.get(q.dtype) == _cache(k, k_levels)[1]
-           and q.shape[2] == _cache(k, k_levels)[2],
+          (lambda: _cache_type(k, k_levels)[0] is not None and _cache_type(k, k_levels) == _cache_type(v, v_levels)
+           and (k_levels is None or k_levels.shape[3] == v_levels.shape[3]), _CACHE_IS + ", k and v alike"),
+          (lambda: q.dim() == 3 and q.stride(2) == 1 and (q.dtype, q.shape[2]) == _cache_type(k, k_levels),
            "q must be [b, heads, d] of the cache's type and row length with contiguous entries"),
           (lambda: table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == q.shape[0]
            and (table.shape[1] < 2 or table.stride(1) == 1), "table must be int32 [b, pages of a sequence] with contiguous rows"),
           (lambda: row(lengths), "lengths must be contiguous int32 [b]"),
           (lambda: starts is None or row(starts), "starts must be contiguous int32 [b]"),
-          (lambda: max_len is None or max_len <= table.shape[1] * k.shape[1], "the table has too few pages for max_len"),
+          (lambda: max_len is None or 0 <= max_len <= table.shape[1] * k.shape[1], "the table has too few pages for max_len"),
           (lambda: out is None or (out.dtype == q.dtype and out.shape == q.shape and out.stride(2) == 1), "out must be like q"),
-          (lambda: ws is None or ws.dtype == torch.uint8, "ws must be uint8"))
+          (lambda: ws is None or (ws.dtype == torch.uint8 and ws.is_contiguous()), "ws must be contiguous uint8"),
+          (lambda: _is_status(status, q), "status must be an int32 tensor on the device of the others"))
     _refuse(where, "bad arguments")
 
 
@@ -803,46 +759,12 @@ def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None
     keys [starts, lengths) are seen.  scale: 1 / sqrt(d) if None.  max_len: host bound of the lengths (None: what the table
     holds).  status: int32 tensor that BAD_* bits are or-ed into.  out [b, heads, d] of q's type, lse float32 [b, heads]
     (natural logarithm; -inf where no key is seen, with out = 0)."""
-    L = _ready()
-    torch = _torch()
-    try:
-        at, dtype, (b, heads, d), (q_row, q_head, one) = q.get_device(), q.dtype, q.shape, q.stride()
-        (ck, T, wide), (cv, Tv, wide_v) = _cache(k, k_levels), _cache(v, v_levels)
-        (seqs, columns), (table_row, by) = table.shape, table.stride()
-        i32 = torch.int32
-        fine = (ck is not None and cv is not None and (k_levels is None) == (v_levels is None) and one == 1
-                and T == Tv == _TYPES.get(dtype) and wide == wide_v == d and seqs == b and (by == 1 or columns < 2)
-                and table.dtype == i32 and lengths.dtype == i32 and lengths.shape == (b,) and lengths.is_contiguous()
-                and (starts is None or (starts.dtype == i32 and starts.shape == (b,) and starts.is_contiguous()
-                                        and starts.get_device() == at))
-                and at >= 0 and at == k.get_device() == v.get_device() == table.get_device() == lengths.get_device()
-                and at == torch.cuda.current_device())
-        if fine:
-            most = columns * ck.page_size
-            if max_len is None:
-                max_len = most
-            if out is None:
-                out = torch.empty((b, heads, d), dtype=dtype, device=q.device)
-                out_row, out_head = heads * d, d
-            else:
-                out_row, out_head, one = out.stride()
-                fine = one == 1 and out.dtype == dtype and out.shape == q.shape and out.get_device() == at
-            if ws is None:
-                ws = workspace_attend(b, heads, ck.heads, d, max_len)
-            fine = fine and max_len <= most and ws.dtype == torch.uint8 and ws.get_device() == at
-    except (AttributeError, TypeError, ValueError, IndexError):
-        fine = False
-    if not fine:
-        _attend_refused(torch, q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws)
-    lse = torch.empty((b, heads), dtype=torch.float32, device=q.device)
-    rc = L.ecasq_attend(q.data_ptr(), q_row, q_head, b, heads, C.byref(ck), C.byref(cv), table.data_ptr(),
-                        table_row if b > 1 else columns, lengths.data_ptr(), None if starts is None else starts.data_ptr(),
-                        max_len, d ** -0.5 if scale is None else scale, out.data_ptr(), out_row, out_head, lse.data_ptr(),
-                        ws.data_ptr(), ws.numel(), _status_ptr("ecasq_attend", at, status),
-                        _raw_stream(at))
-    if rc:
-        _check(rc, "ecasq_attend")
-    return out, lse
+    both = (_codes or _ready()).attend(q, k, v, table, lengths, scale, starts, k_levels, v_levels, max_len, out, ws, status)
+    if both is None:
+        _attend_refused(_torch(), q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws, status)
+    if both.__class__ is int:
+        _check(both, "ecasq_attend")
+    return both
 
 
 def ecasq_kernel_launches() -> int:
