@@ -29,7 +29,6 @@
 // fp32 rows: fp32 products on the FMA pipe in the same frame.
 #pragma once
 
-#include <atomic>
 #include <type_traits>
 
 #include "codes.cuh"
@@ -787,7 +786,6 @@ static int prepare_attend() {
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attend<T, LV, NV, HT>, 32 * S::kWarps, S::kSmem) != cudaSuccess) return 0;
     return n;
 }
-constexpr int kDevices = 16;
 // Splits the sequences (split_attend) and launches.
 template <typename T, int LV, int NV, int HT>
 static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {

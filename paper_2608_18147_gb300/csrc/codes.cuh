@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace ecasq {
@@ -36,6 +38,17 @@ struct FastDiv {
         }
     }
 };
+
+// Lets a kernel have `bytes` of dynamic shared memory, once for each device: done[device] says so.
+constexpr int kDevices = 16;
+template <typename K> static inline int allow_smem(K *kernel, int bytes, std::atomic<int> *done) {
+    int device = 0;
+    ECASQ_CUDA_TRY(cudaGetDevice(&device));
+    if (device < kDevices && done[device].load(std::memory_order_acquire)) return ECASQ_OK;
+    ECASQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (device < kDevices) done[device].store(1, std::memory_order_release);
+    return ECASQ_OK;
+}
 
 // The limits that ecasq_cache_t states; bytes of a row's entries and of its codebook.
 static inline bool cache_ok(const ecasq_cache_t *c) {

@@ -223,49 +223,63 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
     if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
 }
 
-template <typename T, typename S, int R>
-static int launch_matvec_blocks(const MatvecArgs &a, bool wide, cudaStream_t st) {
-    auto *kernel = wide ? k_matvec<T, S, true, R> : k_matvec<T, S, false, R>;
-    ECASQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes));
+template <typename T, typename S, bool WIDE, int R>
+static int launch_matvec_blocks(const MatvecArgs &a, cudaStream_t st) {
+    static std::atomic<int> allowed[kDevices];
+    const int rc = allow_smem(k_matvec<T, S, WIDE, R>, kSmemBytes, allowed);
+    if (rc) return rc;
     note_launch();
-    kernel<<<dim3((unsigned)row_blocks(a.n), (unsigned)cdiv(a.b, 8)), kThreads, kSmemBytes, st>>>(a);
+    k_matvec<T, S, WIDE, R><<<dim3((unsigned)row_blocks(a.n), (unsigned)cdiv(a.b, 8)), kThreads, kSmemBytes, st>>>(a);
     ECASQ_LAUNCH_CHECK();
     return ECASQ_OK;
 }
 
 template <typename T, typename S>
 static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
-    const int64_t tiles = cdiv(cdiv(cdiv(a.n, 8), row_blocks(a.n)), 2), kb = cdiv(a.k, 128);
+    // (32-bit arithmetic: this runs in every call.)
+    const auto over = [](int v, int by) { return (v + by - 1) / by; };
+    const int tiles = (int)cdiv(cdiv(cdiv(a.n, 8), row_blocks(a.n)), 2), kb = (int)cdiv(a.k, 128);
     // The warps' split between columns and row tiles, with one to four blocks a warp, that takes the least time: passes over
     // the rows, rounds in each, and the blocks of a round, which costs about half a block of its own; and more where the
     // next round's codes have no stage to come into.
-    int64_t best = INT64_MAX, own = 1;
-    for (int w = kWarps; w >= 1; w /= 2)
+    int64_t best = INT64_MAX;
+    int own = 0;
+    for (int w = kWarps; w >= 1; w /= 2) {
+        const int rounds = over(tiles, kWarps / w), at_once = 16 * (kWarps / w);
         for (int r = 4; r >= 1; r--) {
-            const int64_t passes = cdiv(kb, w * r), rounds = cdiv(tiles, kWarps / w), at_once = 16 * (kWarps / w), chunk = 128 * r * w;
+            const int passes = over(kb, w * r), chunk = 128 * r * w;
+            int64_t cost = (int64_t)passes * rounds * (2 * r + 1);
+            if (cost >= best) continue;
             // A row's room in a stage: its bytes, and what makes it an odd multiple of 64, so that two rows' reads do not meet in
             // a bank; its scales' room: the pieces of 16 bytes that may hold them, and an odd multiple of 16.
-            const int64_t pitch = chunk / 2 + (r * w % 2 ? 0 : 64), piece = at_once / 2 * pitch;
-            const int64_t groups = std::min<int64_t>(a.groups, chunk / group + 2), scale_pitch = (groups * (int64_t)sizeof(S) + 30) / 32 * 32 + 16;
-            const int64_t left = kBelowRoom - (passes > 1 ? kRowSumBytes : 0) - 2 * at_once * scale_pitch;
-            const int64_t stages = left < 0 ? 0 : std::min<int64_t>({(left / piece + kAboveRoom / piece) / 2, rounds, kMostStages});
-            const int64_t cost = passes * rounds * (2 * r + 1) * (stages < 2 && rounds > 1 ? 2 : 1);
+            const int pitch = chunk / 2 + (r * w % 2 ? 0 : 64), piece = at_once / 2 * pitch;
+            const int groups = std::min(a.groups, chunk / group + 2), scale_pitch = (groups * (int)sizeof(S) + 30) / 32 * 32 + 16;
+            const int left = kBelowRoom - (passes > 1 ? kRowSumBytes : 0) - 2 * at_once * scale_pitch;
+            if (left < 0) continue;
+            const int below = left / piece, stages = std::min({(below + kAboveRoom / piece) / 2, rounds, kMostStages});
+            if (stages < 2 && rounds > 1) cost *= 2;
             if (stages < 1 || cost >= best) continue;
             best = cost;
             own = r;
             a.warps_k = w;
-            a.chunk = (int32_t)chunk;
-            a.pitch = (int32_t)pitch;
-            a.scale_pitch = (int32_t)scale_pitch;
-            a.stages = (int32_t)stages;
-            a.pieces_below = (int32_t)(left / piece);
+            a.chunk = chunk;
+            a.pitch = pitch;
+            a.scale_pitch = scale_pitch;
+            a.stages = stages;
+            a.pieces_below = below;
         }
+    }
     if (best == INT64_MAX) return ECASQ_EINVAL;  // (no size leads here: one block a warp always fits)
-    const bool wide = group % 128 == 0;
-    if (own == 1) return launch_matvec_blocks<T, S, 1>(a, wide, st);
-    if (own == 2) return launch_matvec_blocks<T, S, 2>(a, wide, st);
-    if (own == 3) return launch_matvec_blocks<T, S, 3>(a, wide, st);
-    return launch_matvec_blocks<T, S, 4>(a, wide, st);
+    switch (2 * own + (group % 128 == 0)) {
+        case 2: return launch_matvec_blocks<T, S, false, 1>(a, st);
+        case 3: return launch_matvec_blocks<T, S, true, 1>(a, st);
+        case 4: return launch_matvec_blocks<T, S, false, 2>(a, st);
+        case 5: return launch_matvec_blocks<T, S, true, 2>(a, st);
+        case 6: return launch_matvec_blocks<T, S, false, 3>(a, st);
+        case 7: return launch_matvec_blocks<T, S, true, 3>(a, st);
+        case 8: return launch_matvec_blocks<T, S, false, 4>(a, st);
+        default: return launch_matvec_blocks<T, S, true, 4>(a, st);
+    }
 }
 
 }  // namespace ecasq

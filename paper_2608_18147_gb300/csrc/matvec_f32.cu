@@ -199,8 +199,11 @@ int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st) {
     const int64_t x_bytes = nb * chunk * 512;
     a.stages = (int32_t)std::min<int64_t>(std::min<int64_t>(kMostStages, (room - x_bytes) / stage(chunk)), cdiv(tiles, kWarps / a.warps_k));
     const int smem = (int)(227 * 1024 - room - (a.chunk < a.k ? 0 : kRowSumBytes) + x_bytes + a.stages * stage(chunk));
-    auto *kernel = group % 128 == 0 ? k_matvec_f32<true> : k_matvec_f32<false>;
-    ECASQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static std::atomic<int> allowed[2][kDevices];
+    const bool wide = group % 128 == 0;
+    auto *kernel = wide ? k_matvec_f32<true> : k_matvec_f32<false>;
+    const int rc = allow_smem(kernel, 227 * 1024, allowed[wide]);
+    if (rc) return rc;
     note_launch();
     kernel<<<dim3((unsigned)blocks, (unsigned)cdiv(a.b, 8)), kThreads, smem, st>>>(a);
     ECASQ_LAUNCH_CHECK();
