@@ -7,18 +7,20 @@
 
 namespace ecasq {
 
-// Four neighbouring entries as they lie in memory; one load where their address allows it.
-template <typename X> struct Four {
-    X v[4];
+// E neighbouring entries as they lie in memory; loads of 8 or 16 bytes where their address allows it.
+template <typename X, int E> struct Entries {
+    X v[E];
 };
-template <typename X> __device__ __forceinline__ Four<X> load4(const X *p) {
-    using Vec = std::conditional_t<sizeof(X) == 4, uint4, uint2>;
-    alignas(16) Four<X> x;
-    if ((reinterpret_cast<uintptr_t>(p) & (sizeof(Vec) - 1)) == 0) {
-        *reinterpret_cast<Vec *>(x.v) = *reinterpret_cast<const Vec *>(p);
+template <typename X, int E> __device__ __forceinline__ Entries<X, E> load_entries(const X *p) {
+    constexpr int kBytes = E * sizeof(X), kVec = kBytes < 16 ? 8 : 16;
+    using Vec = std::conditional_t<kVec == 8, uint2, uint4>;
+    alignas(16) Entries<X, E> x;
+    if ((reinterpret_cast<uintptr_t>(p) & (kVec - 1)) == 0) {
+#pragma unroll
+        for (int i = 0; i < kBytes / kVec; i++) reinterpret_cast<Vec *>(x.v)[i] = reinterpret_cast<const Vec *>(p)[i];
     } else {
 #pragma unroll
-        for (int j = 0; j < 4; j++) x.v[j] = p[j];
+        for (int j = 0; j < E; j++) x.v[j] = p[j];
     }
     return x;
 }
@@ -47,7 +49,8 @@ __device__ __forceinline__ uint64_t product(uint32_t a, uint32_t b) { return (ui
 __device__ __forceinline__ int64_t product(int64_t a, int64_t b) { return a * b; }
 __device__ __forceinline__ float shared_float(uint32_t at) { return *static_cast<const float *>(__cvta_shared_to_generic(at)); }
 
-// LV levels a row.  W lanes take a row, four neighbouring entries at a time each: 16 for rows of up to 64 entries, else 32.
+// LV levels a row.  W lanes take a row, E neighbouring entries each: 16 lanes with four for rows of up to 64 entries, with eight
+// for up to 128, 32 lanes with eight for the others (a row's own cost, addresses and levels, is shared by more entries).
 // The row's levels and the gaps above them lie in shared memory, a word a bank, so lanes that look up different levels
 // do not meet.
 //
@@ -58,10 +61,11 @@ __device__ __forceinline__ float shared_float(uint32_t at) { return *static_cast
 // its bits, denormals whose sums are exact, on the pipe that has room.  The next row is on its way while this one is
 // encoded.
 constexpr int kWriteThreads = 256;
-template <typename X, typename T, int LV, int W, typename I>
+template <typename X, typename T, int LV, int W, int E, typename I>
 __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_constant__ WriteArgs<I> a) {
     constexpr int kRows = kWriteThreads / W;  // of a block at a time
-    __shared__ float books[kRows][32];        // levels, NaN beyond the last (no entry passes it), and gaps from word 16 on
+    __shared__ float books[kRows][48];        // levels, NaN beyond the last (no entry passes it), and gaps from word 16 on; two
+                                              // rows of a warp do not meet in a bank
     const int lane = threadIdx.x % W;
     float *book = books[threadIdx.x / W];
     const uint32_t book_at = (uint32_t)__cvta_generic_to_shared(book);
@@ -71,7 +75,7 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
         I i, h;
         int m;
         float q;
-        Four<X> x;
+        Entries<X, E> x;
     };
     auto row_of_x = [&](I i, I h) { return static_cast<const X *>(a.x) + product(i, a.x_row) + product(h, a.x_head); };
     auto fetch = [&](I row) {
@@ -81,7 +85,7 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
         r.slot = a.slots[r.i];
         r.m = a.m ? a.m[row] : a.s;
         r.q = lane < a.s ? a.Q[product(row, (I)a.s) + lane] : 0.f;
-        if (4 * lane < a.d) r.x = load4(row_of_x(r.i, r.h) + 4 * lane);
+        if (E * lane < a.d) r.x = load_entries<X, E>(row_of_x(r.i, r.h) + E * lane);
         return r;
     };
     int bad = 0;
@@ -111,14 +115,13 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
         }
         __syncwarp(group);
         uint8_t *codes = a.codes + product(page, a.row_page) + product(at, a.row_slot) + product(r.h, a.row_head);
-        Four<X> x = r.x;
-        uint64_t z = a.seed + ((uint64_t)row * (uint32_t)a.d + 4 * lane + 1) * kGamma;
-        for (int e = 4 * lane; e < a.d; e += 4 * W) {
+        if (E * lane < a.d) {
+            const uint64_t z = a.seed + ((uint64_t)row * (uint32_t)a.d + E * lane + 1) * kGamma;
             uint32_t zl = (uint32_t)z, zh = (uint32_t)(z >> 32), word = 0;
             float largest = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float v = to_f32(x.v[j]);
+            for (int j = 0; j < E; j++) {
+                const float v = to_f32(r.x.v[j]);
                 asm("max.NaN.f32 %0, %0, %1;" : "+f"(largest) : "f"(fabsf(v)));
                 float t = __uint_as_float(book_at);  // the address of the largest level passed
 #pragma unroll
@@ -127,13 +130,12 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
                 const float k = __fmul_rn((float)(splitmix64_hi(zl, zh) >> 8), 0x1p-24f);
                 if (__fmul_rn(k, shared_float(__float_as_uint(t) + 64)) < __fsub_rn(v, shared_float(__float_as_uint(t))))
                     t = __fadd_rn(t, __uint_as_float(4));
-                word += __float_as_uint(t) << (4 * j);
+                word += ((__float_as_uint(t) - book_at) >> 2) << (4 * j);
                 add_gamma(zl, zh);
             }
             if (!(largest <= 3.402823466e38f)) bad |= ECASQ_BAD_VALUE;
-            *reinterpret_cast<uint16_t *>(codes + e / 2) = (uint16_t)((word - book_at * 0x1111u) >> 2);
-            if (e + 4 * W < a.d) x = load4(row_of_x(r.i, r.h) + e + 4 * W);
-            z += 4 * W * kGamma;
+            if (E == 8) reinterpret_cast<uint32_t *>(codes)[lane] = word;
+            else reinterpret_cast<uint16_t *>(codes)[lane] = (uint16_t)word;
         }
     }
     if (bad && a.status) atomicOr(a.status, bad);
@@ -141,10 +143,10 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
 
 template <typename X, typename T, typename I>
 static void launch_write(const WriteArgs<I> &a, int32_t levels, cudaStream_t st) {
-    const bool narrow = a.d <= 64;
-    const unsigned blocks = (unsigned)std::min<int64_t>(cdiv((int64_t)a.rows, kWriteThreads / (narrow ? 16 : 32)), 152 * 8);
-    auto *kernel = levels == 8 ? (narrow ? k_cache_write<X, T, 8, 16, I> : k_cache_write<X, T, 8, 32, I>)
-                               : (narrow ? k_cache_write<X, T, 16, 16, I> : k_cache_write<X, T, 16, 32, I>);
+    const int lanes = a.d <= 128 ? 16 : 32;
+    const unsigned blocks = (unsigned)std::min<int64_t>(cdiv((int64_t)a.rows, kWriteThreads / lanes), 152 * 8);
+    auto *kernel = levels == 8 ? (a.d <= 64 ? k_cache_write<X, T, 8, 16, 4, I> : a.d <= 128 ? k_cache_write<X, T, 8, 16, 8, I> : k_cache_write<X, T, 8, 32, 8, I>)
+                               : (a.d <= 64 ? k_cache_write<X, T, 16, 16, 4, I> : a.d <= 128 ? k_cache_write<X, T, 16, 16, 8, I> : k_cache_write<X, T, 16, 32, 8, I>);
     note_launch();
     kernel<<<blocks, kWriteThreads, 0, st>>>(a);
 }

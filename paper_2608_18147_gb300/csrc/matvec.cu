@@ -240,15 +240,15 @@ static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
     const auto over = [](int v, int by) { return (v + by - 1) / by; };
     const int tiles = (int)cdiv(cdiv(cdiv(a.n, 8), row_blocks(a.n)), 2), kb = (int)cdiv(a.k, 128);
     // The warps' split between columns and row tiles, with one to four blocks a warp, that takes the least time: passes over
-    // the rows, rounds in each, and the blocks of a round, which costs about half a block of its own; and more where the
-    // next round's codes have no stage to come into.
+    // the rows, each with about three blocks' time until its first codes are there, rounds, and the blocks of a round, which costs
+    // about half a block of its own; and more where the next round's codes have no stage to come into.
     int64_t best = INT64_MAX;
     int own = 0;
     for (int w = kWarps; w >= 1; w /= 2) {
         const int rounds = over(tiles, kWarps / w), at_once = 16 * (kWarps / w);
         for (int r = 4; r >= 1; r--) {
             const int passes = over(kb, w * r), chunk = 128 * r * w;
-            int64_t cost = (int64_t)passes * rounds * (2 * r + 1);
+            int64_t cost = (int64_t)passes * (rounds * (2 * r + 1) + 6);
             if (cost >= best) continue;
             // A row's room in a stage: its bytes, and what makes it an odd multiple of 64, so that two rows' reads do not meet in
             // a bank; its scales' room: the pieces of 16 bytes that may hold them, and an odd multiple of 16.
