@@ -9,7 +9,7 @@ namespace ecasq {
 // split should be long; and the blocks should fill the card evenly: with `slots` of them at once, n splits a sequence take
 // ceil(b blocks n / slots) rounds of a split's keys and that cost.  With one round a shorter sequence takes shorter splits, so that
 // all blocks still work; with several the splits keep their length, and their number adapts.
-constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kLeastStep = 64;
+constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kLeastStep = 64, kMostTile = 32;
 
 struct Splits {
     int32_t least, count;
@@ -34,13 +34,13 @@ static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots
 // key, so with a start one more tile may be needed.)
 static size_t part_bytes(int64_t b, int64_t heads, int64_t blocks, int32_t d, int64_t max_len) {
     const int64_t all = std::max<int64_t>(1, b * blocks), most = std::max<int64_t>(1, (int64_t)kSms * kMostResident * kMostRounds / all);
-    const int64_t splits = std::min(most, cdiv(max_len + kTile - 1, kLeastStep));
+    const int64_t splits = std::min(most, cdiv(max_len + kMostTile - 1, kLeastStep));
     return splits > 1 ? (size_t)(b * heads * splits * PartAt(d).stride) * 4 : 0;
 }
 
 int split_attend(AttendArgs &a, int64_t b, int resident) {
     const int64_t blocks = (int64_t)(a.heads / a.group) * a.htiles;
-    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? kTile - 1 : 0), kSms * std::min(resident, kMostResident), a.step);
+    const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? a.tile - 1 : 0), kSms * std::min(resident, kMostResident), a.step);
     a.least = s.least;
     a.splits = s.count;
     if (a.splits == 1) return ECASQ_OK;
@@ -222,6 +222,7 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     a.vt_page = v->level_page * 2;
     a.vt_slot = v->level_slot * 2;
     a.vt_head = v->level_head * 2;
+    a.alike = k->row_page == v->row_page && k->row_slot == v->row_slot && k->level_page == v->level_page && k->level_slot == v->level_slot;
     a.q_row = q_row;
     a.q_head = q_head;
     a.out_row = out_row;

@@ -52,7 +52,8 @@ struct AttendArgs {
     uint64_t kt_page, kt_slot, kt_head, vt_page, vt_slot, vt_head;
     int64_t q_row, q_head, out_row, out_head, table_row, pages;
     float scale2;                // scale log2(e)
-    int32_t heads, group, htiles, d, page_size, max_len, splits, step, least;  // group: query heads a key head; least: keys of a split
+    int32_t heads, group, htiles, d, page_size, max_len, splits, tile, step, least;  // group: query heads a key head; least: keys of a split
+    bool alike;                  // the values' strides are the keys'
     uint32_t div_mul, div_shift; // t div page_size = umulhi(t, div_mul) >> div_shift, or t >> div_shift if div_mul is 0
 };
 
@@ -225,13 +226,13 @@ __device__ __forceinline__ Span seq_span(const AttendArgs &a, int64_t seq) {
     if (s.too_long) s.end = a.max_len;
     return s;
 }
-// A sequence's splits are counted from the tile of its first key.  They share its keys evenly, in multiples of a.step,
+// A sequence's splits are counted from the tile of its first key (a.tile keys).  They share its keys evenly, in multiples of a.step,
 // but none but the last has fewer than a.least.
 struct Cut {
     int lead, chunk, count;
 };
 __device__ __forceinline__ Cut cut_of(const AttendArgs &a, const Span &s) {
-    Cut c{s.first & ~(kTile - 1), a.least, 0};
+    Cut c{s.first & -a.tile, a.least, 0};
     if (s.end <= s.first) return c;
     const int keys = s.end - c.lead, even = (keys + a.splits - 1) / a.splits;
     c.chunk = max(a.least, (even + a.step - 1) / a.step * a.step);
@@ -305,7 +306,8 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
     const char *ktb = LV ? a.kt + kh * a.kt_head : nullptr, *vtb = LV ? a.vt + kh * a.vt_head : nullptr;
     const int32_t *table = a.table + seq * a.table_row;
-    const bool whole = a.page_size % kTile == 0;  // sixteen keys lie in one page
+    // What keys of a tile are neighbouring slots of one page: all of it, sixteen, or none for sure.
+    const bool tiles_whole = a.page_size % S::kKeys == 0, whole = a.page_size % kTile == 0;
     const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
     bool bad_page = false;
     struct Found {
@@ -328,36 +330,40 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         bad_page |= f.page != -2 && !ok;
         const uint32_t mask = __ballot_sync(0xffffffffu, ok) & S::kAll;
         if (lane == 0) seen[stage] = mask;
-        char *dv = dst + S::kKeys * S::kRow, *dk = dst;
+        // Sixteen neighbouring slots, the first at kp and vp (chunk c of row r0 of them), to rows 16 half .. of the tile.
+        const int r0 = lane / S::kChunks, c0 = lane % (S::kChunks < 32 ? S::kChunks : 32);
+        auto copy_half = [&](int half, const char *kp, const char *vp) {
+            char *dk = dst + half * kTile * S::kRow, *dv = dk + S::kKeys * S::kRow;
 #pragma unroll
-        for (int half = 0; half < S::kHalves; half++) {
-            if (whole && (mask >> 16 * half & 0xffffu) == 0xffffu) {  // sixteen neighbouring slots
-                const int r0 = lane / S::kChunks, c = lane % (S::kChunks < 32 ? S::kChunks : 32);
-                Found first = f;
-                if (S::kHalves > 1) {
-                    first.page = __shfl_sync(0xffffffffu, f.page, kTile * half);
-                    first.slot = __shfl_sync(0xffffffffu, f.slot, kTile * half) + r0;
-                } else {
-                    first.slot += r0 - (lane & 15);
+            for (int i = 0; i < S::kPieces; i++) {
+                // piece lane + 32 i: chunks come round in a row first
+                constexpr int kSame = S::kChunks > 32 ? S::kChunks / 32 : 1, kRows = S::kChunks > 32 ? 1 : 32 / S::kChunks;
+                const int r = r0 + i / kSame * kRows, c = c0 + i % kSame * 32;
+                if (c < row_chunks) {
+                    copy16(smem_addr(dk + S::k_at(r, c)), kp + i % kSame * 512, true);
+                    copy16(smem_addr(dv + S::v_at(S::v_row(r), c)), vp + i % kSame * 512, true);
                 }
-                const char *kp = kb + first.offset(a.k_page, a.k_slot) + 16 * c;
-                const char *vp = vb + first.offset(a.v_page, a.v_slot) + 16 * c;
+                if (i % kSame == kSame - 1) {
+                    kp += kRows * a.k_slot;
+                    vp += kRows * a.v_slot;
+                }
+            }
+        };
+        if (tiles_whole && mask == S::kAll) {
+            const Found first{f.page, f.slot - (lane & (S::kKeys - 1)) + r0};
+            const uint64_t ko = first.offset(a.k_page, a.k_slot), vo = a.alike ? ko : first.offset(a.v_page, a.v_slot);
 #pragma unroll
-                for (int i = 0; i < S::kPieces; i++) {
-                    // piece lane + 32 i: chunks come round in a row first
-                    constexpr int kSame = S::kChunks > 32 ? S::kChunks / 32 : 1, kRows = S::kChunks > 32 ? 1 : 32 / S::kChunks;
-                    const int r = r0 + i / kSame * kRows, cc = c + i % kSame * 32;
-                    if (cc < row_chunks) {
-                        copy16(smem_addr(dk + S::k_at(r, cc)), kp + i % kSame * 512, true);
-                        copy16(smem_addr(dv + S::v_at(S::v_row(r), cc)), vp + i % kSame * 512, true);
-                    }
-                    if (i % kSame == kSame - 1) {
-                        kp += kRows * a.k_slot;
-                        vp += kRows * a.v_slot;
-                    }
+            for (int half = 0; half < S::kHalves; half++) copy_half(half, kb + ko + 16 * c0 + half * kTile * a.k_slot, vb + vo + 16 * c0 + half * kTile * a.v_slot);
+        } else {
+#pragma unroll
+            for (int half = 0; half < S::kHalves; half++) {
+                if (whole && (mask >> 16 * half & 0xffffu) == 0xffffu) {
+                    Found first{__shfl_sync(0xffffffffu, f.page, kTile * half), __shfl_sync(0xffffffffu, f.slot, kTile * half) + r0};
+                    copy_half(half, kb + first.offset(a.k_page, a.k_slot) + 16 * c0, vb + first.offset(a.v_page, a.v_slot) + 16 * c0);
+                    continue;
                 }
-            } else {
                 const uint64_t krow = ok ? f.offset(a.k_page, a.k_slot) : 0, vrow = ok ? f.offset(a.v_page, a.v_slot) : 0;
+                char *dk = dst + half * kTile * S::kRow, *dv = dk + S::kKeys * S::kRow;
 #pragma unroll
                 for (int i = 0; i < S::kPieces; i++) {
                     const int r = (lane + 32 * i) / S::kChunks, c = (lane + 32 * i) % S::kChunks;
@@ -369,11 +375,10 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                     }
                 }
             }
-            dk += kTile * S::kRow;
-            dv += kTile * S::kRow;
         }
         if (LV) {  // a lane its key's codebooks
-            const char *ks = ok ? ktb + f.offset(a.kt_page, a.kt_slot) : ktb, *vs = ok ? vtb + f.offset(a.vt_page, a.vt_slot) : vtb;
+            const uint64_t ko = ok ? f.offset(a.kt_page, a.kt_slot) : 0, vo = a.alike ? ko : ok ? f.offset(a.vt_page, a.vt_slot) : 0;
+            const char *ks = ktb + ko, *vs = vtb + vo;
             char *to = dst + 2 * S::kKeys * S::kRow;
 #pragma unroll
             for (int i = 0; i < LV / 8; i++) {
@@ -799,6 +804,7 @@ static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
         if (resident < 1) return ECASQ_ECUDA;
         if (device < kDevices) known[device].store(resident, std::memory_order_release);
     }
+    a.tile = S::kKeys;
     a.step = S::kKeys * 4;
     const int rc = split_attend(a, b, resident);
     if (rc) return rc;
