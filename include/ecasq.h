@@ -427,6 +427,7 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
  *           scale_type: `type` or ECASQ_F32
  *   group   a multiple of 32; one >= k means one scale a row
  *   y       device [b rows of y_row elements], of `type`, output
+ *   status  ECASQ_BAD_WAIT
  * ECASQ_EINVAL for n or k < 1, b < 0, m outside [1, 16], a bad type, group or
  * alignment. */
 int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
@@ -483,6 +484,7 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
  * over the keys t in [starts[i], lengths[i]); a sequence without keys gives out = 0 and
  * lse = -inf, and so does one whose weights are all zero.  Scores, weights and sums are fp32;
  * out is rounded once, to q's type.  Nothing outside that range is read, whatever it holds.
+ * Values are finite: an infinity among those seen may give NaN where the sum is infinite.
  *   q        device [b, heads, d] of the cache's type, strides in elements, entries
  *            contiguous; out likewise
  *   k, v     host structs of one type, kind, d, heads, pages and page_size
@@ -492,7 +494,9 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
  *   max_len  host bound of the lengths; sizes the launch and the workspace
  *   lse      device fp32 [b, heads] or NULL
  * Workspace: ecasq_workspace_size_attend with the same sizes (0 bytes may be returned: ws
- * may then be NULL).  Splits and sums do not depend on other sequences' lengths, and equal calls give equal bits.
+ * may then be NULL); it needs no preparation.  How a sequence's sums are cut depends on its own
+ * range and on the call's sizes alone, and equal calls give equal bits.
+ *   status   ECASQ_BAD_PAGE, ECASQ_BAD_LENGTH
  * ECASQ_EINVAL for b outside [0, 65535], max_len outside [0, 2^30], heads not a multiple
  * of k->heads or above 65535, a cache outside the limits of ecasq_cache_t, or caches that
  * differ. */

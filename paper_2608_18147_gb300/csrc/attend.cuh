@@ -163,7 +163,7 @@ template <int LV> struct Book {
         } else {
             // The lower and the upper eight levels by the codes' low three bits, then a choice by the fourth: a byte
             // permute spreads the sign bits of w << 4 and of w, which are the codes' fourth bits.
-            const uint32_t s = (H ? w >> 16 : w) & 0x7777u, m = prmt(w << 4, w, H ? 0xFBEA : 0xD9C8);
+            const uint32_t low3 = w & 0x77777777u, s = H ? low3 >> 16 : low3, m = prmt(w << 4, w, H ? 0xFBEA : 0xD9C8);
             const uint32_t l0 = prmt(lo[0], lo[1], s), l1 = prmt(lo[2 % (LV / 4)], lo[3 % (LV / 4)], s);
             const uint32_t h0 = prmt(hi[0], hi[1], s), h1 = prmt(hi[2 % (LV / 4)], hi[3 % (LV / 4)], s);
             l = (l0 & ~m) | (l1 & m);
@@ -221,7 +221,7 @@ struct Span {
 __device__ __forceinline__ Span seq_span(const AttendArgs &a, int64_t seq) {
     Span s;
     s.end = a.lengths[seq];
-    s.first = a.starts ? max(a.starts[seq], 0) : 0;
+    s.first = a.starts ? min(max(a.starts[seq], 0), a.max_len) : 0;  // (at max_len no key is left, and sums of key numbers fit)
     s.too_long = s.end > a.max_len;
     if (s.too_long) s.end = a.max_len;
     return s;

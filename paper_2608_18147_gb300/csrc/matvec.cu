@@ -41,7 +41,8 @@ __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, i
 // kTableAt + 256 e + 4 l: one byte permute puts the code byte between the lane's constant ones, and that is the address.
 constexpr int kTableAt = 0x20000, kAboveAt = 0x30000, kSmemBytes = 227 * 1024;
 constexpr int kBarBytes = 64, kMostStages = 4;
-constexpr int kBelowRoom = kTableAt - 2048 - kBarBytes, kAboveRoom = kSmemBytes - kAboveAt;  // (the window begins at 1 KB)
+constexpr int kWindowMost = 2048;  // where a block's own shared memory begins at most (it is 1 KB)
+constexpr int kBelowRoom = kTableAt - kWindowMost - kBarBytes, kAboveRoom = kSmemBytes - kAboveAt;
 
 // d = c + A B
 template <typename T> __device__ __forceinline__ void mma_pairs(float (&d)[4], const float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
@@ -223,10 +224,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
     if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
 }
 
+// Whether a block's own shared memory begins where kBelowRoom takes it to: asked once a device.
+static int window_ok() {
+    static std::atomic<int> known[kDevices];
+    int device = 0, reserved = 0;
+    ECASQ_CUDA_TRY(cudaGetDevice(&device));
+    if (device < kDevices && known[device].load(std::memory_order_acquire)) return ECASQ_OK;
+    ECASQ_CUDA_TRY(cudaDeviceGetAttribute(&reserved, cudaDevAttrReservedSharedMemoryPerBlock, device));
+    if (reserved > kWindowMost) return ECASQ_ECUDA;
+    if (device < kDevices) known[device].store(1, std::memory_order_release);
+    return ECASQ_OK;
+}
+
 template <typename T, typename S, bool WIDE, int R>
 static int launch_matvec_blocks(const MatvecArgs &a, cudaStream_t st) {
     static std::atomic<int> allowed[kDevices];
-    const int rc = allow_smem(k_matvec<T, S, WIDE, R>, kSmemBytes, allowed);
+    int rc = window_ok();
+    if (!rc) rc = allow_smem(k_matvec<T, S, WIDE, R>, kSmemBytes, allowed);
     if (rc) return rc;
     note_launch();
     k_matvec<T, S, WIDE, R><<<dim3((unsigned)row_blocks(a.n), (unsigned)cdiv(a.b, 8)), kThreads, kSmemBytes, st>>>(a);

@@ -255,6 +255,45 @@ def test_equal_bits_whatever_else_is_in_the_batch(dtype, levels):
     assert all(torch.equal(x[1:], y[1:]) for x, y in zip(first, other))
 
 
+@pytest.mark.parametrize("dtype,levels", KINDS)
+@pytest.mark.parametrize("page", [16, 32, 9])
+def test_keys_and_values_laid_out_differently(page, dtype, levels):
+    """Keys with the heads inside the slots, values the other way round, in a wider cache."""
+    c = make([70, 333], 3, 2, 64, page, dtype, levels, "nhd", seed=19)
+    v = c["v"]
+
+    def turned(t):
+        wide = torch.full((t.shape[0] + 1, t.shape[2] + 2, t.shape[1], t.shape[3]), 1, dtype=t.dtype, device="cuda")
+        part = wide[1:, 1:-1].transpose(1, 2)
+        part.copy_(t)
+        return part
+
+    v.rows = turned(v.rows)
+    if levels:
+        v.levels = turned(v.levels)
+    check(call(c), reference(c))
+
+
+@pytest.mark.parametrize("dtype,levels", KINDS)
+def test_many_sequences(dtype, levels):
+    """Hundreds of short sequences: a join a warp a head, and sequences of one split beside longer ones."""
+    lengths = [(37 * i) % 300 for i in range(400)]
+    c = make(lengths, 2, 2, 32, 16, dtype, levels, "hnd", seed=20)
+    few = [0, 1, 7, 100, 250, 399]
+    got = call(c)
+    part = dict(c, q=c["q"][few], table=c["table"][few], lengths=c["lengths"][few])
+    check((got[0][few], got[1][few]), reference(part))
+
+
+@pytest.mark.parametrize("dtype,levels", KINDS)
+def test_starts_beyond_every_key(dtype, levels):
+    """A start past the end leaves no key, however far past it is."""
+    c = make([50, 50, 600, 600], 2, 4, 32, 16, dtype, levels, "nhd", seed=21, starts=[2 ** 31 - 1, 49, 2 ** 31 - 40, 3])
+    got = call(c)
+    check(got, reference(c))
+    assert (got[0][[0, 2]] == 0).all() and (got[1][[0, 2]] == -math.inf).all()
+
+
 @pytest.mark.parametrize("dtype,levels", [("bf16", 0), ("f16", 8)])
 def test_offsets_beyond_32_bits(dtype, levels):
     """Pages more than 2^32 entries from the cache's start."""

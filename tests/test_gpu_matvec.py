@@ -143,6 +143,38 @@ def test_strides_and_out(dtype):
     check(one, ref[2], size[2], k, dtype)
 
 
+@pytest.mark.parametrize("dtype,scale_dtype", [("bf16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("before,row", [(1, 0), (3, 1), (5, 3), (8, 8)])
+def test_scales_at_any_address(before, row, group, dtype, scale_dtype):
+    """Scales that begin anywhere, their rows apart by anything; what lies around them is NaN."""
+    import paper_2608_18147_gb300 as E
+    n, k, b = 300, 700, 2
+    x, idx, levels, scales = make(n, k, b, group, dtype, scale_dtype, seed=before)
+    wide = scales.shape[1] + row
+    flat = torch.full((before + n * wide + 9,), float("nan"), dtype=scales.dtype, device="cuda")
+    part = flat[before:before + n * wide].view(n, wide)[:, :scales.shape[1]]
+    part.copy_(scales)
+    y = E.ecasq_matvec(x.cuda(), E.ecasq_pack(idx.cuda()), levels.cuda(), part, group)
+    ref, size = reference(x, idx, levels, scales, group)
+    check(y, ref, size, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,k,b,group", [(90000, 130, 1, 32), (90001, 256, 3, 128), (5000, 4200, 1, 64), (1300, 16500, 2, 128),
+                                         (152 * 40, 6144, 1, 32), (20, 16384, 8, 32), (8, 8192, 1, 8192)])
+def test_many_rows_and_columns(n, k, b, group, dtype):
+    """More rows than one block takes, several passes over the columns, every split of the warps between them."""
+    import paper_2608_18147_gb300 as E
+    x, idx, levels, scales = make(n, k, b, group, dtype, "f32", seed=n)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = E.ecasq_matvec(x.cuda(), E.ecasq_pack(idx.cuda()), levels.cuda(), scales.cuda(), group, status=status)
+    assert status.item() == 0
+    some = torch.cat([torch.arange(0, n, max(1, n // 500)), torch.arange(max(0, n - 40), n)])
+    ref, size = reference(x, idx[some], levels, scales[some], group)
+    check(y[:, some.cuda()], ref, size, k, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_nan_and_inf_stay_in_their_row(dtype):
     import paper_2608_18147_gb300 as E
