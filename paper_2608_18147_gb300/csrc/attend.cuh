@@ -173,14 +173,16 @@ template <int LV> struct Book {
 };
 
 // A tile in shared memory: rows of K, as many of V, then their codebooks.  Sixteen keys, of coded rows 32, whose
-// other costs (maxima, codebooks, addresses) are shared by more keys.  T and LV: the rows' type and
-// levels (0: plain); NV: the row length is at most 64 NV.
+// other costs (maxima, codebooks, addresses) are shared by more keys.  Coded rows of more than 128 entries have many
+// registers' worth of sums and of q, so q lies in shared memory and tiles have sixteen keys, with which twelve warps fit an SM instead of
+// eight (four sequences of 20000 keys of 256 entries, four heads a key head: 33.1 against 34.6 us with eight levels, 50.6
+// against 55.8 with sixteen).  T and LV: the rows' type and levels (0: plain); NV: the row length is at most 64 NV.
 template <typename T, int LV, int NV> struct Shape {
     static constexpr bool kF32 = sizeof(T) == 4;
     static constexpr int kRow = LV ? 32 * NV : 64 * NV * (int)sizeof(T);   // bytes of a row's room
     static constexpr int kChunks = kRow / 16;
     static constexpr int kBook = 2 * LV;                                   // bytes of a codebook
-    static constexpr int kKeys = LV ? 32 : kTile, kHalves = kKeys / kTile;
+    static constexpr int kKeys = LV && NV < 4 ? 32 : kTile, kHalves = kKeys / kTile;
     static constexpr uint32_t kAll = kKeys == 32 ? 0xffffffffu : 0xffffu;
     static constexpr int kBytes = 2 * kKeys * (kRow + kBook);
     static constexpr int kWarps = kBytes > 16384 ? 3 : kBytes > 8192 ? 2 : 4;
@@ -188,7 +190,8 @@ template <typename T, int LV, int NV> struct Shape {
     static constexpr int kRing = kStages * kBytes;                         // of a warp
     static constexpr int kJoin = kHeads * 64 * NV * 4;                     // a warp's sums at the end, in its ring
     static constexpr int kExtra = (kF32 ? kHeads * 64 * NV * 4 + kWarps * kTile * kHeads * 4 : 0) + kWarps * (2 * kHeads * 4) + kWarps * kStages * 4;
-    static constexpr int kSmem = kWarps * kRing + kExtra;
+    static constexpr bool kQShared = LV && NV == 4;                        // q's operands lie in shared memory
+    static constexpr int kSmem = kWarps * kRing + (kExtra + 15) / 16 * 16 + (kQShared ? 512 * 2 * NV : 0);
     static_assert(kJoin <= kRing, "");
     static_assert(kSmem <= 227 * 1024, "");
     static constexpr int kPieces = kTile * kChunks / 32;                   // 16-byte pieces of K (and of V) for a lane and half
@@ -252,7 +255,8 @@ __device__ __forceinline__ void store_out(const AttendArgs &a, int64_t seq, int 
 
 // HT: query heads of a block, 4 or 8.
 template <typename T, int LV, int NV, int HT>
-__global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps, Shape<T, LV, NV>::kQShared ? 3 : 0)
+k_attend(const __grid_constant__ AttendArgs a) {
     using S = Shape<T, LV, NV>;
     constexpr int HL = HT / 4;  // heads of a lane's scores: HT = 8: 2t, 2t + 1; HT = 4: t
     extern __shared__ __align__(16) char smem[];
@@ -289,6 +293,11 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
             qf[i + 3] = v.w;
         }
     }
+    uint4 *q_shared = reinterpret_cast<uint4 *>(smem + S::kWarps * S::kRing + (S::kExtra + 15) / 16 * 16) + lane;
+    if (S::kQShared && wid == 0) {
+#pragma unroll
+        for (int i = 0; i < 2 * kSteps; i += 4) q_shared[8 * i] = make_uint4(qf[i], qf[i + 1], qf[i + 2], qf[i + 3]);
+    }
     const Span span = seq_span(a, seq);
     if (span.too_long && threadIdx.x == 0 && split == 0 && a.status) atomicOr(a.status, ECASQ_BAD_LENGTH);
     const Cut cut = cut_of(a, span);
@@ -306,8 +315,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
     const char *ktb = LV ? a.kt + kh * a.kt_head : nullptr, *vtb = LV ? a.vt + kh * a.vt_head : nullptr;
     const int32_t *table = a.table + seq * a.table_row;
-    // What keys of a tile are neighbouring slots of one page: all of it, sixteen, or none for sure.
-    const bool tiles_whole = a.page_size % S::kKeys == 0, whole = a.page_size % kTile == 0;
+    const bool tiles_whole = a.page_size % S::kKeys == 0;  // a tile's keys are neighbouring slots of one page
     const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
     bool bad_page = false;
     struct Found {
@@ -357,8 +365,9 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         } else {
 #pragma unroll
             for (int half = 0; half < S::kHalves; half++) {
-                if (whole && (mask >> 16 * half & 0xffffu) == 0xffffu) {
-                    Found first{__shfl_sync(0xffffffffu, f.page, kTile * half), __shfl_sync(0xffffffffu, f.slot, kTile * half) + r0};
+                const int slot0 = __shfl_sync(0xffffffffu, f.slot, kTile * half), slot15 = __shfl_sync(0xffffffffu, f.slot, kTile * half + kTile - 1);
+                if (slot15 - slot0 == kTile - 1 && (mask >> 16 * half & 0xffffu) == 0xffffu) {  // sixteen of them are
+                    const Found first{__shfl_sync(0xffffffffu, f.page, kTile * half), slot0 + r0};
                     copy_half(half, kb + first.offset(a.k_page, a.k_slot) + 16 * c0, vb + first.offset(a.v_page, a.v_slot) + 16 * c0);
                     continue;
                 }
@@ -382,8 +391,9 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
             char *to = dst + 2 * S::kKeys * S::kRow;
 #pragma unroll
             for (int i = 0; i < LV / 8; i++) {
-                copy16(smem_addr(to + lane * S::kBook + 16 * i), ks + 16 * i, ok);
-                copy16(smem_addr(to + (S::kKeys + (lane & 16) + S::v_row(lane & 15)) * S::kBook + 16 * i), vs + 16 * i, ok);
+                if (S::kKeys == 32 || lane < 16) copy16(smem_addr(to + lane * S::kBook + 16 * i), ks + 16 * i, ok);
+                if (S::kKeys == 32 || lane >= 16)
+                    copy16(smem_addr(to + (S::kKeys + (lane & (S::kKeys - 16)) + S::v_row(lane & 15)) * S::kBook + 16 * i), vs + 16 * i, ok);
             }
         }
     };
@@ -407,6 +417,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
     Found next_found = found[S::kStages - 1];
     int next = mine + (S::kStages - 1) * step, fill = S::kStages - 1;
 
+    if (S::kQShared) __syncthreads();
     if (S::kF32) {
         for (int i = threadIdx.x; i < kHeads * 64 * NV; i += 32 * S::kWarps) {
             const int h = i / (64 * NV), e = i % (64 * NV);
@@ -443,7 +454,7 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
         const uint32_t mask = seen[use];
         if (LV) {
             Book<LV ? LV : 8>::split(bk + lane * S::kBook);
-            Book<LV ? LV : 8>::split(bv + lane * S::kBook);
+            if (S::kKeys == 32) Book<LV ? LV : 8>::split(bv + lane * S::kBook);  // (else the lanes 16 .. had those of the values)
             __syncwarp();
         }
 
@@ -512,7 +523,11 @@ __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps) k_attend(const 
                         }
 #pragma unroll
                         for (int w = 0; w < kWords; w++) {
-                            const uint32_t *q4 = qf + 4 * (kWords * i + w);
+                            alignas(16) uint32_t q4[4];
+                            if (S::kQShared) *reinterpret_cast<uint4 *>(q4) = q_shared[32 * (kWords * i + w)];
+                            else
+#pragma unroll
+                                for (int j = 0; j < 4; j++) q4[j] = qf[4 * (kWords * i + w) + j];
                             uint32_t xl, xh, yl, yh;
                             b0.template look<0>(x[w], xl, xh);
                             b1.template look<0>(y[w], yl, yh);
