@@ -120,6 +120,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
                 if (lane < 16) reinterpret_cast<float2 *>(table)[16 * (16 * wid + j) + lane] = make_float2(low, high);
             }
         }
+        // Scales of rows g and g + 8, for the lane's words t of a block (WIDE: for the block), read one block ahead.  Rows beyond
+        // the run repeat its last one; their sums are not stored.
+        float next_a, next_b;
+        auto next_scales = [&](int round, int at) {
+            const int row = round * rows_at_once + 16 * wr + g;
+            const uint32_t w = group_of(a, (uint32_t)(k0 / 32) + 4 * at + (WIDE ? 0 : t));
+            next_a = scales[min(row, rows - 1) * a.scale_row + w];
+            next_b = scales[min(row + 8, rows - 1) * a.scale_row + w];
+        };
+        next_scales(0, wk);
         // x, zero beyond k.
         const float *x = static_cast<const float *>(a.x) + i0 * a.x_row + k0;
         for (int i = 0; i < nb; i++)
@@ -130,15 +140,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
             if (!bar_wait(bars + 8 * s, parity >> s & 1)) lost = true;
             parity ^= 1u << s;
             const char *tile = ring + s * stage_bytes + (16 * wr + g) * pitch + 16 * t;
-            // Scales of rows g and g + 8, for the lane's words t of a block (WIDE: for the block).  Rows beyond the run repeat
-            // its last one; their sums are not stored.
-            const int row = round * rows_at_once + 16 * wr + g;
-            const float *qa = scales + min(row, rows - 1) * a.scale_row, *qb = scales + min(row + 8, rows - 1) * a.scale_row;
             Sums acc;
             acc.clear();
             for (int at = wk; at < blocks; at += a.warps_k) {
-                const uint32_t w = group_of(a, (uint32_t)(k0 / 32) + 4 * at + (WIDE ? 0 : t));
-                const float fa = qa[w], fb = qb[w];
+                const float fa = next_a, fb = next_b;
+                if (at + a.warps_k < blocks) next_scales(round, at + a.warps_k);
+                else if (round + 1 < rounds) next_scales(round + 1, wk);
                 const uint4 la = *reinterpret_cast<const uint4 *>(tile + 64 * at), lb = *reinterpret_cast<const uint4 *>(tile + 64 * at + 8 * pitch);
                 const uint32_t wa[4] = {la.x, la.y, la.z, la.w}, wb[4] = {lb.x, lb.y, lb.z, lb.w};
                 Sums part;
