@@ -104,6 +104,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
     // rounds in turn.
     auto sum_at = [&](int i) -> float * { return reinterpret_cast<float *>(table + (i >> 5) * 256 + 128 + (i & 31) * 4); };
 
+    // (Loads are issued before anything waits for another's: the levels here, x before the table is built.)
+    const T level = (lane & 15) < a.m ? static_cast<const T *>(a.levels)[lane & 15] : from_f32<T>(0.f);
     if (tid == 0)
         for (int s = 0; s < a.stages; s++) bar_init(bars + 8 * s);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -143,14 +145,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
 #pragma unroll
         for (int r = 0; r < R; r++) at[r] = (int)(min(group_of(a, (uint32_t)(k0 / 32) + 4 * (wk * R + r) + (WIDE ? 0 : t)), last_group) - first_group) * (int)sizeof(S);
 
-        // The codebook's pairs: warp w the sixteen with the second level w, a lane a copy.
-        if (k0 == 0) {
-            const T mine = (lane & 15) < a.m ? static_cast<const T *>(a.levels)[lane & 15] : from_f32<T>(0.f);
-            const uint32_t bits = reinterpret_cast<const uint16_t &>(mine), high = __shfl_sync(0xffffffffu, bits, wid);
-#pragma unroll
-            for (int j = 0; j < 16; j++)
-                reinterpret_cast<uint32_t *>(table + 256 * (16 * wid + j))[lane] = __shfl_sync(0xffffffffu, bits, j) | high << 16;
-        }
         // x, zero beyond k.
         uint4 xr[R][4];
         {
@@ -193,6 +187,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
                         }
                 }
             }
+        }
+        // The codebook's pairs: warp w the sixteen with the second level w, a lane a copy.
+        if (k0 == 0) {
+            const uint32_t bits = reinterpret_cast<const uint16_t &>(level), high = __shfl_sync(0xffffffffu, bits, wid);
+#pragma unroll
+            for (int j = 0; j < 16; j++)
+                reinterpret_cast<uint32_t *>(table + 256 * (16 * wid + j))[lane] = __shfl_sync(0xffffffffu, bits, j) | high << 16;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
