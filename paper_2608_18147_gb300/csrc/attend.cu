@@ -50,12 +50,12 @@ int split_attend(AttendArgs &a, int64_t b, int resident) {
 }
 
 // The splits' maxima and sums give each split's share, then the entries are added, four a lane.  A head by a warp (WARPS = 1,
-// eight heads a block, nothing to wait for) where there are few splits and many heads, else 64 entries of a head by a
-// block, 16 splits at a time.
+// eight heads a block, nothing to wait for), or 64 entries of a head by a block, 16 splits at a time.  Bound by the latency of
+// its loads: 2 to 3 us after the splits' kernel, whose end its start overlaps.
 // A sequence of one split has its result already.
-constexpr int kJoinThreads = 256, kShares = 1024;
+constexpr int kJoinThreads = 256, kJoinResident = 4, kShares = 1024;  // kJoinResident: blocks an SM holds
 template <typename T, int WARPS>
-__global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, kJoinResident) k_attend_join(const __grid_constant__ AttendArgs a) {
     constexpr int kThreads = 32 * WARPS, kHeadsHere = kJoinThreads / kThreads;
     __shared__ float red[2 * WARPS], share[WARPS == 1 ? 1 : kShares];
     __shared__ __align__(16) float4 sums[WARPS == 1 ? 1 : kJoinThreads];
@@ -159,7 +159,9 @@ static int launch_join(const AttendArgs &a, int64_t b, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    const bool warps = a.splits <= 16 && a.heads * b >= 8 * kSms;  // (few heads: a warp each would leave the card idle)
+    // By warps where blocks would not all run at once.  (32 sequences of 4096 keys, 32 heads of 128: 87.6 us by warps, 94.0 by
+    // blocks; one sequence of 2000: 10.6 by warps, 7.2 by blocks.)
+    const bool warps = a.heads * b * cdiv(a.d, 64) > kJoinResident * kSms;
     cfg.gridDim = dim3((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b, (unsigned)(warps ? 1 : cdiv(a.d, 64)));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;
@@ -222,7 +224,6 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     a.vt_page = v->level_page * 2;
     a.vt_slot = v->level_slot * 2;
     a.vt_head = v->level_head * 2;
-    a.alike = k->row_page == v->row_page && k->row_slot == v->row_slot && k->level_page == v->level_page && k->level_slot == v->level_slot;
     a.q_row = q_row;
     a.q_head = q_head;
     a.out_row = out_row;

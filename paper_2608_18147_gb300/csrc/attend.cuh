@@ -5,10 +5,14 @@
 // moves m to m' = max(m, max s), O and l shrink by 2^(m - m') and gain sum 2^(s - m') V and
 // sum 2^(s - m') (s scaled to base 2).  A key row is read once for up to eight query heads.
 //
-// What bounds it: the cache's bytes.  So each warp works alone on tiles of 16 keys through a ring of its own in
+// What bounds it: the cache's bytes.  So each warp works alone on tiles of 16 or 32 keys through a ring of its own in
 // shared memory that cp.async fills a few tiles ahead, without a barrier in the loop.  The sequence is cut into
 // splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory
-// and k_attend_join joins the splits.
+// and k_attend_join joins the splits.  Measured, both kernels: 32 sequences of up to 8192 bf16 keys of 128, eight heads a key
+// head, 94 us or 5.7 TB/s, 84 % of a copy's rate.  Coded rows are bound by the lookups, byte permutes on the integer
+// pipe, which is 57 to 61 % busy: 16 sequences of 32768 keys of 128 with eight levels 148 us (4.5 TB/s, 67 %), one of
+// 70001 keys of 256 with sixteen 52 us (1.7 TB/s).  Short sequences are bound by latency: lengths, page numbers, rows and
+// the join follow one another; one sequence of 1000 keys takes 6.4 us.
 //
 // 16-bit rows: S^T = K Q^T and O^T = V^T P^T on mma.m16n8k16 with the query heads as n, fp32 sums.  (One
 // token a sequence is a matrix-vector product for each key head; with eight columns there is nothing for the
@@ -20,7 +24,8 @@
 // With up to four heads (HT = 4) a pair of reduction indices is such a pair of entries instead, and a head has two
 // columns, which hold its weights on the even and on the odd index: sum_t V_t[e] P_t and sum_t V_t[e + 1] P_t come
 // out side by side, in as many products as before.  With up to eight (HT = 8) the columns are taken, and two keys'
-// registers are first permuted into pairs of keys.
+// registers are first permuted into pairs of keys.  (Four heads a key head, 16 sequences of 8192 keys: with HT = 4 and 8 50.1
+// and 55.6 us for eight-level rows, 52.3 and 53.6 for sixteen levels and rows of 64, 94.0 and 95.1 for 32 of 4096 bf16 keys.)
 // Weights enter the second product as a high and a low 16-bit part (their sum keeps 16 bits or more): one part alone would
 // add an error as large as the rounding of the result.
 // Coded rows: a lane holds its row's codebook as planes of low and of high bytes; a byte permute with four
@@ -53,7 +58,6 @@ struct AttendArgs {
     int64_t q_row, q_head, out_row, out_head, table_row, pages;
     float scale2;                // scale log2(e)
     int32_t heads, group, htiles, d, page_size, max_len, splits, tile, step, least;  // group: query heads a key head; least: keys of a split
-    bool alike;                  // the values' strides are the keys'
     uint32_t div_mul, div_shift; // t div page_size = umulhi(t, div_mul) >> div_shift, or t >> div_shift if div_mul is 0
 };
 
@@ -338,6 +342,8 @@ k_attend(const __grid_constant__ AttendArgs a) {
         bad_page |= f.page != -2 && !ok;
         const uint32_t mask = __ballot_sync(0xffffffffu, ok) & S::kAll;
         if (lane == 0) seen[stage] = mask;
+        // Rows of one page have one address and a step; others each their own, shuffled from the lane that looked it up (32
+        // sequences of 4096 bf16 keys: 94 and 96 us; 16 of 8192 eight-level keys: 50 and 53).
         // Sixteen neighbouring slots, the first at kp and vp (chunk c of row r0 of them), to rows 16 half .. of the tile.
         const int r0 = lane / S::kChunks, c0 = lane % (S::kChunks < 32 ? S::kChunks : 32);
         auto copy_half = [&](int half, const char *kp, const char *vp) {
@@ -359,7 +365,7 @@ k_attend(const __grid_constant__ AttendArgs a) {
         };
         if (tiles_whole && mask == S::kAll) {
             const Found first{f.page, f.slot - (lane & (S::kKeys - 1)) + r0};
-            const uint64_t ko = first.offset(a.k_page, a.k_slot), vo = a.alike ? ko : first.offset(a.v_page, a.v_slot);
+            const uint64_t ko = first.offset(a.k_page, a.k_slot), vo = first.offset(a.v_page, a.v_slot);
 #pragma unroll
             for (int half = 0; half < S::kHalves; half++) copy_half(half, kb + ko + 16 * c0 + half * kTile * a.k_slot, vb + vo + 16 * c0 + half * kTile * a.v_slot);
         } else {
@@ -386,7 +392,7 @@ k_attend(const __grid_constant__ AttendArgs a) {
             }
         }
         if (LV) {  // a lane its key's codebooks
-            const uint64_t ko = ok ? f.offset(a.kt_page, a.kt_slot) : 0, vo = a.alike ? ko : ok ? f.offset(a.vt_page, a.vt_slot) : 0;
+            const uint64_t ko = ok ? f.offset(a.kt_page, a.kt_slot) : 0, vo = ok ? f.offset(a.vt_page, a.vt_slot) : 0;
             const char *ks = ktb + ko, *vs = vtb + vo;
             char *to = dst + 2 * S::kKeys * S::kRow;
 #pragma unroll

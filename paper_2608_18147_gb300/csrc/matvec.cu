@@ -8,16 +8,30 @@ namespace ecasq {
 // Position of word w of a 128-column block among its sixteen stored words.
 __host__ __device__ constexpr int packed_word(int w) { return 4 * (w & 3) + (w >> 2); }
 
-// One thread a word of eight codes.
+// The low four bits of four bytes, side by side.
+__device__ __forceinline__ uint32_t four_codes(uint32_t w) {
+    w &= 0x0f0f0f0fu;
+    w = (w | w >> 4) & 0x00ff00ffu;
+    return (w | w >> 8) & 0xffffu;
+}
+
+// One thread a word of eight codes of every gridDim.y-th row.  Where the rows allow it a word's indices are one load of eight bytes
+// (28672 x 8192: 90 us, 3.9 TB/s; byte by byte 146).
 __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, int64_t idx_row, int64_t n, int64_t k,
                                               uint8_t *__restrict__ codes, int64_t code_row, int64_t words) {
-    const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n * words; i += stride) {
-        const int64_t r = i / words, w = i % words;
+    const bool vec = ((reinterpret_cast<uintptr_t>(idx) | (uintptr_t)idx_row) & 7) == 0;
+    const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (w >= words) return;
+#pragma unroll 4
+    for (int64_t r = blockIdx.y; r < n; r += gridDim.y) {
+        const uint8_t *from = idx + r * idx_row + 8 * w;
         uint32_t v = 0;
-        for (int j = 0; j < 8; j++) {
-            const int64_t c = 8 * w + j;
-            if (c < k) v |= (uint32_t)(idx[r * idx_row + c] & 15) << (4 * j);
+        if (vec && 8 * w + 8 <= k) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(from);
+            v = four_codes(x.x) | four_codes(x.y) << 16;
+        } else {
+            for (int j = 0; j < 8; j++)
+                if (8 * w + j < k) v |= (uint32_t)(from[j] & 15) << (4 * j);
         }
         const int64_t at = (w & ~(int64_t)15) + packed_word((int)(w & 15));
         *reinterpret_cast<uint32_t *>(codes + r * code_row + 4 * at) = v;
@@ -28,16 +42,18 @@ __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, i
 // whose x it holds in registers, and runs down the rows, a tile of sixteen at a time; with few columns the warps take
 // several tiles at once.  A stage of the ring holds a round's rows, brought in by one bulk copy a row a round or more ahead;
 // a barrier a round joins the warps' sums and frees its stage.  The rows' scales come a round ahead too, by cp.async in the
-// 16-byte pieces that hold them (loads to registers are waited for together with the lookups: 40 against 31 us for 28672 x 8192
-// by eight rows).  More columns than the warps cover take several passes.
+// 16-byte pieces that hold them (loads to registers are waited for together with the lookups: 39.6 against 36.8 us for 28672 x
+// 8192 by eight rows).  More columns than the warps cover take several passes.
 //
 // A pair of weights is an operand register of mma.m16n8k16 as it stands, with the rows of x as its eight columns and
 // fp32 sums; the order of the columns within a product is free.  (With one to eight columns there is no reuse that a
 // larger tensor tile could draw on.)
 //
-// What bounds it: the codes' bytes in the end, and on the way there the issue slots and shared memory.  The table is held
-// once a lane, so that no two lanes meet in a bank; 32 lookups, 8 transactions for the codes themselves and up to 8 for the
-// scales stand, for each KB of codes, against the 44 clocks that memory needs for it.  Entry e of lane l lies at address
+// What bounds it: the codes' bytes in the end, and on the way there the latency of lookups and products at sixteen warps an
+// SM (issue slots 46 %, shared memory 46 %, DRAM 35 % busy with eight rows).  28672 x 8192 by eight rows of bf16 takes 35.5 us,
+// 3.5 TB/s; 8192 x 8192 by one row of fp16, groups of 64, 16.0 us, 2.2 TB/s; a small matrix 4 us: the launch, one memory latency
+// and the table.  The table is held once a lane, so that no two lanes meet in a bank; 32 lookups, 8 transactions for the codes
+// themselves and up to 8 for the scales stand, for each KB of codes, against the 44 clocks that memory needs for it.  Entry e of lane l lies at address
 // kTableAt + 256 e + 4 l: one byte permute puts the code byte between the lane's constant ones, and that is the address.
 constexpr int kTableAt = 0x20000, kAboveAt = 0x30000, kSmemBytes = 227 * 1024;
 constexpr int kBarBytes = 64, kMostStages = 4;
@@ -82,7 +98,8 @@ __device__ __forceinline__ uint4 eight_of(const uint4 &lo, const uint4 &hi, int 
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// WIDE: a scale group holds whole 128-column blocks.
+// WIDE: a scale group holds whole 128-column blocks, so that a block's products are one sum (8192 x 8192 by eight rows, groups of
+// 128: 15.9 us, and 16.9 with a sum for each 32 columns).
 template <typename T, typename S, bool WIDE, int R>
 __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ MatvecArgs a) {
     extern __shared__ __align__(128) char smem[];
@@ -164,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
                         for (int i = 0; i < 4; i++) keep(xr[r][i], have - 128 * r - 32 * i);
             } else {
                 // In the 16-byte pieces that hold them, two blocks' at a time, and without a branch between the loads (value by
-                // value each load would wait for the one before: 12.6 against 11 us for 5003 x 4097 by five rows).
+                // value each load would wait for the one before: 16.0 against 13.3 us for 2046 x 8508 by five rows).
                 const int skip = (int)(reinterpret_cast<uintptr_t>(x) & 15);
                 const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(x) & ~(uintptr_t)15);
 #pragma unroll
@@ -350,8 +367,8 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
         return ECASQ_EINVAL;
     const int64_t words = 16 * cdiv(k, 128);
     note_launch();
-    k_pack<<<(unsigned)std::min<int64_t>(cdiv(n * words, 256), 152 * 8), 256, 0, reinterpret_cast<cudaStream_t>(stream)>>>(
-        idx, idx_row, n, k, codes, code_row, words);
+    const int64_t across = cdiv(words, 256), down = std::min(n, cdiv(152 * 16, across));
+    k_pack<<<dim3((unsigned)across, (unsigned)down), 256, 0, reinterpret_cast<cudaStream_t>(stream)>>>(idx, idx_row, n, k, codes, code_row, words);
     ECASQ_LAUNCH_CHECK();
     return ECASQ_OK;
 }
