@@ -59,12 +59,12 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinResident) k_attend_join(con
     constexpr int kThreads = 32 * WARPS, kHeadsHere = kJoinThreads / kThreads;
     __shared__ float red[2 * WARPS], share[WARPS == 1 ? 1 : kShares];
     __shared__ __align__(16) float4 sums[WARPS == 1 ? 1 : kJoinThreads];
+    wait_before();
     const int64_t seq = blockIdx.y;
     const int h = blockIdx.x * kHeadsHere + threadIdx.x / kThreads, tid = threadIdx.x % kThreads, lane = tid & 31, wid = tid >> 5;
     const int n = cut_of(a, seq_span(a, seq)).count;
     const PartAt at(a.d);
     const float *part = at.at(a.part, seq, a.heads, h, a.splits, 0);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (n <= 1 || h >= a.heads) return;
     float m = -CUDART_INF_F;
     for (int i = tid; i < n; i += kThreads) m = fmaxf(m, part[i * at.stride + a.d]);
@@ -154,23 +154,11 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinResident) k_attend_join(con
 
 template <typename T>
 static int launch_join(const AttendArgs &a, int64_t b, cudaStream_t st) {
-    // May start while the splits' kernel ends: it waits for the results itself.
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
     // By warps where blocks would not all run at once.  (32 sequences of 4096 keys, 32 heads of 128: 87.6 us by warps, 94.0 by
     // blocks; one sequence of 2000: 10.6 by warps, 7.2 by blocks.)
     const bool warps = a.heads * b * cdiv(a.d, 64) > kJoinResident * kSms;
-    cfg.gridDim = dim3((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b, (unsigned)(warps ? 1 : cdiv(a.d, 64)));
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    note_launch();
-    if (warps) ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_attend_join<T, 1>, a));
-    else ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_attend_join<T, kJoinThreads / 32>, a));
-    return ECASQ_OK;
+    const dim3 grid((unsigned)(warps ? cdiv(a.heads, kJoinThreads / 32) : a.heads), (unsigned)b, (unsigned)(warps ? 1 : cdiv(a.d, 64)));
+    return warps ? launch_early(k_attend_join<T, 1>, grid, kJoinThreads, 0, st, a) : launch_early(k_attend_join<T, kJoinThreads / 32>, grid, kJoinThreads, 0, st, a);
 }
 
 static bool sizes_ok(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {

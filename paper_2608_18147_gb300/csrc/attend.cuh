@@ -264,6 +264,7 @@ k_attend(const __grid_constant__ AttendArgs a) {
     using S = Shape<T, LV, NV>;
     constexpr int HL = HT / 4;  // heads of a lane's scores: HT = 8: 2t, 2t + 1; HT = 4: t
     extern __shared__ __align__(16) char smem[];
+    wait_before();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int64_t seq = blockIdx.z;
     const int split = blockIdx.y, kh = blockIdx.x / a.htiles, h0 = kh * a.group + (blockIdx.x % a.htiles) * HT;
@@ -830,10 +831,7 @@ static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
     const int rc = split_attend(a, b, resident);
     if (rc) return rc;
     const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
-    note_launch();
-    k_attend<T, LV, NV, HT><<<grid, 32 * S::kWarps, S::kSmem, st>>>(a);
-    ECASQ_LAUNCH_CHECK();
-    return ECASQ_OK;
+    return launch_early(k_attend<T, LV, NV, HT>, grid, 32 * S::kWarps, S::kSmem, st, a);
 }
 template <typename T, int LV, int HT>
 static int launch_attend_rows(AttendArgs &a, int64_t b, cudaStream_t st) {

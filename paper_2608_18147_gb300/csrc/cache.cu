@@ -90,6 +90,7 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
         if (E * lane < a.d) r.x = load_entries<X, E>(row_of_x(r.i, r.h) + E * lane);
         return r;
     };
+    wait_before();
     int bad = 0;
     const I stride = (I)gridDim.x * kRows;
     I row = (I)blockIdx.x * kRows + threadIdx.x / W;
@@ -144,13 +145,12 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
 }
 
 template <typename X, typename T, typename I>
-static void launch_write(const WriteArgs<I> &a, int32_t levels, cudaStream_t st) {
+static int launch_write(const WriteArgs<I> &a, int32_t levels, cudaStream_t st) {
     const int lanes = a.d <= 128 ? 16 : 32;
     const unsigned blocks = (unsigned)std::min<int64_t>(cdiv((int64_t)a.rows, kWriteThreads / lanes), 152 * 8);
     auto *kernel = levels == 8 ? (a.d <= 64 ? k_cache_write<X, T, 8, 16, 4, I> : a.d <= 128 ? k_cache_write<X, T, 8, 16, 8, I> : k_cache_write<X, T, 8, 32, 8, I>)
                                : (a.d <= 64 ? k_cache_write<X, T, 16, 16, 4, I> : a.d <= 128 ? k_cache_write<X, T, 16, 16, 8, I> : k_cache_write<X, T, 16, 32, 8, I>);
-    note_launch();
-    kernel<<<blocks, kWriteThreads, 0, st>>>(a);
+    return launch_early(kernel, dim3(blocks), kWriteThreads, 0, st, a);
 }
 template <typename I>
 static int write_rows(const void *x, int32_t x_type, int64_t n, int64_t x_row, int64_t x_head, const float *Q, int32_t s, const int32_t *m,
@@ -158,15 +158,8 @@ static int write_rows(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
     const WriteArgs<I> a{x, Q, m, slots, static_cast<uint8_t *>(c.rows), c.levels, c.pages * c.page_size, seed, status, (I)x_row, (I)x_head,
                          (I)c.row_page, (I)c.row_slot, (I)c.row_head, (I)c.level_page, (I)c.level_slot, (I)c.level_head,
                          (I)(n * c.heads), s, c.d, c.heads, c.page_size, FastDiv(c.heads), FastDiv(c.page_size)};
-    if (c.type == ECASQ_F16) {
-        if (x_type == ECASQ_F32) launch_write<float, __half>(a, c.levels_n, st);
-        else launch_write<__half, __half>(a, c.levels_n, st);
-    } else {
-        if (x_type == ECASQ_F32) launch_write<float, __nv_bfloat16>(a, c.levels_n, st);
-        else launch_write<__nv_bfloat16, __nv_bfloat16>(a, c.levels_n, st);
-    }
-    ECASQ_LAUNCH_CHECK();
-    return ECASQ_OK;
+    if (c.type == ECASQ_F16) return x_type == ECASQ_F32 ? launch_write<float, __half>(a, c.levels_n, st) : launch_write<__half, __half>(a, c.levels_n, st);
+    return x_type == ECASQ_F32 ? launch_write<float, __nv_bfloat16>(a, c.levels_n, st) : launch_write<__nv_bfloat16, __nv_bfloat16>(a, c.levels_n, st);
 }
 
 }  // namespace ecasq

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 
 #include <atomic>
+#include <utility>
 
 #include "common.cuh"
 
@@ -49,6 +50,27 @@ template <typename K> static inline int allow_smem(K *kernel, int bytes, std::at
     if (device < kDevices) done[device].store(1, std::memory_order_release);
     return ECASQ_OK;
 }
+
+// Launches a kernel whose first statement is wait_before(): its blocks may be placed while the kernel before it in the stream ends.
+template <typename... P, typename... A>
+static inline int launch_early(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A &&...args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    note_launch();
+    ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...));
+    return ECASQ_OK;
+}
+// Waits until the kernel before this one has ended and what it wrote can be read.  Every block does so before it reads or writes
+// memory, and before it ends, so that the kernel after this one has waited for all that came before.
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // The limits that ecasq_cache_t states; bytes of a row's entries and of its codebook.
 static inline bool cache_ok(const ecasq_cache_t *c) {

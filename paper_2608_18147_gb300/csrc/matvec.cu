@@ -121,6 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
     // rounds in turn.
     auto sum_at = [&](int i) -> float * { return reinterpret_cast<float *>(table + (i >> 5) * 256 + 128 + (i & 31) * 4); };
 
+    wait_before();
     // (Loads are issued before anything waits for another's: the levels here, x before the table is built.)
     const T level = (lane & 15) < a.m ? static_cast<const T *>(a.levels)[lane & 15] : from_f32<T>(0.f);
     if (tid == 0)
@@ -300,10 +301,7 @@ static int launch_matvec_blocks(const MatvecArgs &a, cudaStream_t st) {
     int rc = window_ok();
     if (!rc) rc = allow_smem(k_matvec<T, S, WIDE, R>, kSmemBytes, allowed);
     if (rc) return rc;
-    note_launch();
-    k_matvec<T, S, WIDE, R><<<dim3((unsigned)row_blocks(a.n), (unsigned)cdiv(a.b, 8)), kThreads, kSmemBytes, st>>>(a);
-    ECASQ_LAUNCH_CHECK();
-    return ECASQ_OK;
+    return launch_early(k_matvec<T, S, WIDE, R>, dim3((unsigned)row_blocks(a.n), (unsigned)cdiv(a.b, 8)), kThreads, kSmemBytes, st, a);
 }
 
 template <typename T, typename S>

@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
     const uint8_t *codes = a.codes + r0 * a.code_row;
     const float *scales = static_cast<const float *>(a.scales) + r0 * a.scale_row;
 
+    wait_before();
     if (tid == 0)
         for (int s = 0; s < a.stages; s++) bar_init(bars + 8 * s);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -212,10 +213,7 @@ int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st) {
     auto *kernel = wide ? k_matvec_f32<true> : k_matvec_f32<false>;
     const int rc = allow_smem(kernel, 227 * 1024, allowed[wide]);
     if (rc) return rc;
-    note_launch();
-    kernel<<<dim3((unsigned)blocks, (unsigned)cdiv(a.b, 8)), kThreads, smem, st>>>(a);
-    ECASQ_LAUNCH_CHECK();
-    return ECASQ_OK;
+    return launch_early(kernel, dim3((unsigned)blocks, (unsigned)cdiv(a.b, 8)), kThreads, smem, st, a);
 }
 
 }  // namespace ecasq
