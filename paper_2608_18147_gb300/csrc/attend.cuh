@@ -718,7 +718,6 @@ k_attend(const __grid_constant__ AttendArgs a) {
     }
     copies_wait<0>();
     if (bad_page && a.status) atomicOr(a.status, ECASQ_BAD_PAGE);
-    if (a.splits > 1) asm volatile("griddepcontrol.launch_dependents;");
 
     // ---- the block's warps: maxima and sums, then each warp's O shrunk to the common maximum
 #pragma unroll

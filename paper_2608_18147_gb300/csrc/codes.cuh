@@ -51,7 +51,9 @@ template <typename K> static inline int allow_smem(K *kernel, int bytes, std::at
     return ECASQ_OK;
 }
 
-// Launches a kernel whose first statement is wait_before(): its blocks may be placed while the kernel before it in the stream ends.
+// Launches a kernel whose first statement is wait_before(): its blocks may be placed while the kernel before it in the stream still
+// runs.  (In a row of calls: a product with 1024 x 1024 codes 3.3 us, and 3.9 launched after the kernel before it has ended;
+// attention over 64 sequences of 100 keys 9.8 and 10.2 us; 32 x 8 cache rows 2.3 and 2.7 us.)
 template <typename... P, typename... A>
 static inline int launch_early(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A &&...args) {
     cudaLaunchAttribute attr[1];
@@ -68,9 +70,10 @@ static inline int launch_early(void (*kernel)(P...), dim3 grid, int threads, int
     ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...));
     return ECASQ_OK;
 }
-// Waits until the kernel before this one has ended and what it wrote can be read.  Every block does so before it reads or writes
-// memory, and before it ends, so that the kernel after this one has waited for all that came before.
-__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Waits until the kernel before this one has ended and what it wrote can be read, then lets the blocks of the kernel after this one
+// be placed as soon as all of this one's have been.  Every block does so before it reads or writes memory, and before it ends, so
+// that the kernel after this one has waited for all that came before.
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory"); }
 
 // The limits that ecasq_cache_t states; bytes of a row's entries and of its codebook.
 static inline bool cache_ok(const ecasq_cache_t *c) {
