@@ -43,7 +43,9 @@ __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, i
 // several tiles at once.  A stage of the ring holds a round's rows, brought in by one bulk copy a row a round or more ahead;
 // a barrier a round joins the warps' sums and frees its stage.  The rows' scales come a round ahead too, by cp.async in the
 // 16-byte pieces that hold them (loads to registers are waited for together with the lookups: 39.6 against 36.8 us for 28672 x
-// 8192 by eight rows).  More columns than the warps cover take several passes.
+// 8192 by eight rows).  More columns than the warps cover take several passes, or two or four blocks of a cluster take a slice of
+// the columns each and add their sums over the cluster, which also fills the card where rows are few (393 x 15530 by two rows: 7.1 us
+// by clusters, 14.7 in passes of single blocks; 8192 x 28672 by eight: 41.7 and 51.2).
 //
 // A pair of weights is an operand register of mma.m16n8k16 as it stands, with the rows of x as its eight columns and
 // fp32 sums; the order of the columns within a product is free.  (With one to eight columns there is no reuse that a
@@ -103,15 +105,17 @@ __device__ __forceinline__ uint4 eight_of(const uint4 &lo, const uint4 &hi, int 
 template <typename T, typename S, bool WIDE, int R>
 __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ MatvecArgs a) {
     extern __shared__ __align__(128) char smem[];
-    const uint32_t base = smem_at(smem), bars = base;
+    const uint32_t base = smem_at(smem), bars = base, window = base & 0xff000000u;  // (a cluster's blocks have windows 2^24 apart)
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
-    float *row_sums = reinterpret_cast<float *>(smem + kBarBytes);  // [kRowsMost][8], with several passes
-    char *scale_ring = smem + kBarBytes + (a.chunk < a.k ? kRowSumBytes : 0), *table = smem + (kTableAt - base), *above = smem + (kAboveAt - base);
-    const uint32_t entry0 = kTableAt + 4 * lane;
+    float *row_sums = reinterpret_cast<float *>(smem + kBarBytes);  // [kRowsMost][8], with several passes or slices
+    char *scale_ring = smem + kBarBytes + (a.keep ? kRowSumBytes : 0), *table = smem + (kTableAt + window - base), *above = smem + (kAboveAt + window - base);
+    const uint32_t entry0 = window + kTableAt + 4 * lane;
     const int wk = wid & (a.warps_k - 1), wr = wid / a.warps_k, tiles_at_once = kWarps / a.warps_k;
     const int i0 = 8 * blockIdx.y, nb = min(8, a.b - i0);
-    const int64_t r0 = row_of(a, blockIdx.x);
-    const int rows = (int)(row_of(a, blockIdx.x + 1) - r0), tiles = (rows + 15) / 16, rounds = (tiles + tiles_at_once - 1) / tiles_at_once;
+    const unsigned run = blockIdx.x / a.slices, runs = gridDim.x / a.slices, rank = blockIdx.x % a.slices;
+    const int64_t r0 = row_of(a, run, runs);
+    const uint32_t k_first = rank * a.slice, k_end = min((uint32_t)a.k, k_first + a.slice);
+    const int rows = (int)(row_of(a, run + 1, runs) - r0), tiles = (rows + 15) / 16, rounds = (tiles + tiles_at_once - 1) / tiles_at_once;
     const S *scales = static_cast<const S *>(a.scales) + r0 * a.scale_row;
     // A stage is two pieces, the rows 0 .. 7 and 8 .. 15 of its tiles; as many pieces as fit lie below the table, the others above.
     char *below = scale_ring + 32 * tiles_at_once * a.scale_pitch;  // two rounds' scales
@@ -132,8 +136,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
     uint32_t parity = 0;  // of the stages' next waits, a bit each
     bool lost = false;    // a wait ran out
     int turn = 0;
-    for (int64_t k0 = 0; k0 < a.k; k0 += a.chunk) {
-        const int cols = (int)min((int64_t)a.chunk, a.k - k0), blocks = (cols + 127) / 128;
+    for (uint32_t k0 = k_first; k0 < k_end; k0 += a.chunk) {
+        const int cols = min(a.chunk, (int)(k_end - k0)), blocks = (cols + 127) / 128;
         // A warp brings in one row of each tile.
         const int fetch_row = 16 * lane + wid;
         auto fetch = [&](int round, int s) {
@@ -146,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
         for (int s = 0; s < a.stages && s < rounds; s++) fetch(s, s);
 
         // A round's scales: of each row the pieces that hold its groups first .. last.  A warp takes a row of each tile.
-        const uint32_t first_group = group_of(a, (uint32_t)(k0 / 32)), last_group = group_of(a, (uint32_t)((k0 + cols - 1) / 32));
+        const uint32_t first_group = group_of(a, k0 / 32), last_group = group_of(a, (k0 + cols - 1) / 32);
         const int scale_bytes = (int)(last_group - first_group + 1) * (int)sizeof(S);
         auto fetch_scales = [&](int round) {
             const int first = round * 16 * tiles_at_once;
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
         // Where the lane's scales lie among a row's: of its words t of each block (WIDE: of the block).
         int at[R];
 #pragma unroll
-        for (int r = 0; r < R; r++) at[r] = (int)(min(group_of(a, (uint32_t)(k0 / 32) + 4 * (wk * R + r) + (WIDE ? 0 : t)), last_group) - first_group) * (int)sizeof(S);
+        for (int r = 0; r < R; r++) at[r] = (int)(min(group_of(a, k0 / 32 + 4 * (wk * R + r) + (WIDE ? 0 : t)), last_group) - first_group) * (int)sizeof(S);
 
         // x, zero beyond k.
         uint4 xr[R][4];
@@ -207,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
             }
         }
         // The codebook's pairs: warp w the sixteen with the second level w, a lane a copy.
-        if (k0 == 0) {
+        if (k0 == k_first) {
             const uint32_t bits = reinterpret_cast<const uint16_t &>(level), high = __shfl_sync(0xffffffffu, bits, wid);
 #pragma unroll
             for (int j = 0; j < 16; j++)
@@ -268,17 +272,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
                     float v = 0.f;
 #pragma unroll 8
                     for (int w = 0; w < a.warps_k; w++) v += of[w * 256];  // 128 sums on: four rows of the table
-                    if (a.chunk < a.k) {
-                        if (k0) v += row_sums[row * 8 + col];
-                        row_sums[row * 8 + col] = v;
+                    if (a.keep) {
+                        if (k0 > k_first) v += row_sums[row * 8 + col];
+                        row_sums[row * 8 + col] = lost ? CUDART_NAN_F : v;
                     }
-                    if (k0 + a.chunk >= a.k) static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(lost ? CUDART_NAN_F : v);
+                    if (a.slices == 1 && k0 + a.chunk >= k_end) static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(lost ? CUDART_NAN_F : v);
                 }
             }
             turn ^= 1;  // the next round's sums go to the other half
             s = s + 1 == a.stages ? 0 : s + 1;
         }
-        if (k0 + a.chunk < a.k) __syncthreads();  // the sums of this pass, before the next one's
+        if (k0 + a.chunk < k_end) __syncthreads();  // the sums of this pass, before the next one's
+    }
+    if (a.slices > 1) {  // each block adds its share of the rows over the cluster
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        for (int i = (int)rank * kThreads + tid; i < 8 * rows; i += a.slices * kThreads) {
+            const int row = i / 8, col = i & 7;
+            if (col >= nb) continue;
+            float v = 0.f;
+            for (int s = 0; s < a.slices; s++) {
+                float of;
+                asm volatile("{ .reg .b32 at; mapa.shared::cluster.u32 at, %1, %2; ld.shared::cluster.f32 %0, [at]; }"
+                             : "=f"(of) : "r"(smem_at(row_sums + i)), "r"(s) : "memory");
+                v += of;
+            }
+            static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(v);
+        }
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
     }
     if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
 }
@@ -296,59 +316,102 @@ static int window_ok() {
 }
 
 template <typename T, typename S, bool WIDE, int R>
-static int launch_matvec_blocks(const MatvecArgs &a, cudaStream_t st) {
+static int launch_matvec_blocks(const MatvecArgs &a, int64_t runs, cudaStream_t st) {
     static std::atomic<int> allowed[kDevices];
     int rc = window_ok();
     if (!rc) rc = allow_smem(k_matvec<T, S, WIDE, R>, kSmemBytes, allowed);
     if (rc) return rc;
-    return launch_early(k_matvec<T, S, WIDE, R>, dim3((unsigned)row_blocks(a.n), (unsigned)cdiv(a.b, 8)), kThreads, kSmemBytes, st, a);
+    return launch_clusters(k_matvec<T, S, WIDE, R>, dim3((unsigned)(runs * a.slices), (unsigned)cdiv(a.b, 8)), a.slices, kThreads, kSmemBytes, st, a);
+}
+
+// Clusters of c = 2 or 4 blocks that the card holds at once (76 and 36), asked once a device.  Every k_matvec has the same threads and
+// shared memory.
+static int clusters_held(int c, int *held) {
+    static std::atomic<int> known[2][kDevices], allowed[kDevices];
+    int device = 0;
+    ECASQ_CUDA_TRY(cudaGetDevice(&device));
+    *held = device < kDevices ? known[c / 4][device].load(std::memory_order_acquire) : 0;
+    if (*held > 0) return ECASQ_OK;
+    auto *kernel = k_matvec<__half, __half, false, 1>;
+    const int rc = allow_smem(kernel, kSmemBytes, allowed);
+    if (rc) return rc;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)c;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)c);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ECASQ_CUDA_TRY(cudaOccupancyMaxActiveClusters(held, kernel, &cfg));
+    if (*held < 1) return ECASQ_ECUDA;
+    if (device < kDevices) known[c / 4][device].store(*held, std::memory_order_release);
+    return ECASQ_OK;
 }
 
 template <typename T, typename S>
 static int launch_matvec(MatvecArgs &a, int32_t group, cudaStream_t st) {
     // (32-bit arithmetic: this runs in every call.)
     const auto over = [](int v, int by) { return (v + by - 1) / by; };
-    const int tiles = (int)cdiv(cdiv(cdiv(a.n, 8), row_blocks(a.n)), 2), kb = (int)cdiv(a.k, 128);
-    // The warps' split between columns and row tiles, with one to four blocks a warp, that takes the least time: passes over
-    // the rows, each with about three blocks' time until its first codes are there, rounds, and the blocks of a round, which costs
-    // about half a block of its own; and more where the next round's codes have no stage to come into.
-    int64_t best = INT64_MAX;
+    const int eights = (int)cdiv(a.n, 8), all = (int)cdiv(a.k, 128);
+    // The split of the columns over a cluster, of the warps between columns and row tiles, and the blocks a warp, that take the
+    // least time: passes over the rows, each with about three blocks' time until its first codes are there, rounds, and the
+    // blocks of a round, which costs about half a block of its own; more where the next round's codes have no stage to come
+    // into; and the cluster's barriers.
+    int64_t best = INT64_MAX, runs = 0;
     int own = 0;
-    for (int w = kWarps; w >= 1; w /= 2) {
-        const int rounds = over(tiles, kWarps / w), at_once = 16 * (kWarps / w);
-        for (int r = 4; r >= 1; r--) {
-            const int passes = over(kb, w * r), chunk = 128 * r * w;
-            int64_t cost = (int64_t)passes * (rounds * (2 * r + 1) + 6);
-            if (cost >= best) continue;
-            // A row's room in a stage: its bytes, and what makes it an odd multiple of 64, so that two rows' reads do not meet in
-            // a bank; its scales' room: the pieces of 16 bytes that may hold them, and an odd multiple of 16.
-            const int pitch = chunk / 2 + (r * w % 2 ? 0 : 64), piece = at_once / 2 * pitch;
-            const int groups = std::min(a.groups, chunk / group + 2), scale_pitch = (groups * (int)sizeof(S) + 30) / 32 * 32 + 16;
-            const int left = kBelowRoom - (passes > 1 ? kRowSumBytes : 0) - 2 * at_once * scale_pitch;
-            if (left < 0) continue;
-            const int below = left / piece, stages = std::min({(below + kAboveRoom / piece) / 2, rounds, kMostStages});
-            if (stages < 2 && rounds > 1) cost *= 2;
-            if (stages < 1 || cost >= best) continue;
-            best = cost;
-            own = r;
-            a.warps_k = w;
-            a.chunk = chunk;
-            a.pitch = pitch;
-            a.scale_pitch = scale_pitch;
-            a.stages = stages;
-            a.pieces_below = below;
+    for (int c = 1; c <= 4; c *= 2) {
+        const int kb = over(all, c);
+        int at_once_most = 152;
+        if (c > 1) {
+            if (best <= 12 || a.b > 8 || (c - 1) * kb >= all) break;  // (12: the least cost of a cluster)
+            const int rc = clusters_held(c, &at_once_most);
+            if (rc) return rc;
+        }
+        const int blocks = std::max(std::min(eights, at_once_most), over(eights, kRowsMost / 8)), tiles = over(over(eights, blocks), 2);
+        for (int w = kWarps; w >= 1; w /= 2) {
+            const int rounds = over(tiles, kWarps / w), at_once = 16 * (kWarps / w);
+            for (int r = 4; r >= 1; r--) {
+                const int passes = over(kb, w * r), chunk = 128 * r * w;
+                const bool keep = passes > 1 || c > 1;
+                int64_t cost = (int64_t)over(blocks, at_once_most) * passes * (rounds * (2 * r + 1) + 6) + (c > 1 ? 3 : 0);
+                if (cost >= best) continue;
+                // A row's room in a stage: its bytes, and what makes it an odd multiple of 64, so that two rows' reads do not meet in
+                // a bank; its scales' room: the pieces of 16 bytes that may hold them, and an odd multiple of 16.
+                const int pitch = chunk / 2 + (r * w % 2 ? 0 : 64), piece = at_once / 2 * pitch;
+                const int groups = std::min(a.groups, chunk / group + 2), scale_pitch = (groups * (int)sizeof(S) + 30) / 32 * 32 + 16;
+                const int left = kBelowRoom - (keep ? kRowSumBytes : 0) - 2 * at_once * scale_pitch;
+                if (left < 0) continue;
+                const int below = left / piece, stages = std::min({(below + kAboveRoom / piece) / 2, rounds, kMostStages});
+                if (stages < 2 && rounds > 1) cost *= 2;
+                if (stages < 1 || cost >= best) continue;
+                best = cost;
+                own = r;
+                runs = blocks;
+                a.slices = c;
+                a.slice = c > 1 ? 128 * kb : (int32_t)a.k;
+                a.keep = keep;
+                a.warps_k = w;
+                a.chunk = chunk;
+                a.pitch = pitch;
+                a.scale_pitch = scale_pitch;
+                a.stages = stages;
+                a.pieces_below = below;
+            }
         }
     }
     if (best == INT64_MAX) return ECASQ_EINVAL;  // (no size leads here: one block a warp always fits)
     switch (2 * own + (group % 128 == 0)) {
-        case 2: return launch_matvec_blocks<T, S, false, 1>(a, st);
-        case 3: return launch_matvec_blocks<T, S, true, 1>(a, st);
-        case 4: return launch_matvec_blocks<T, S, false, 2>(a, st);
-        case 5: return launch_matvec_blocks<T, S, true, 2>(a, st);
-        case 6: return launch_matvec_blocks<T, S, false, 3>(a, st);
-        case 7: return launch_matvec_blocks<T, S, true, 3>(a, st);
-        case 8: return launch_matvec_blocks<T, S, false, 4>(a, st);
-        default: return launch_matvec_blocks<T, S, true, 4>(a, st);
+        case 2: return launch_matvec_blocks<T, S, false, 1>(a, runs, st);
+        case 3: return launch_matvec_blocks<T, S, true, 1>(a, runs, st);
+        case 4: return launch_matvec_blocks<T, S, false, 2>(a, runs, st);
+        case 5: return launch_matvec_blocks<T, S, true, 2>(a, runs, st);
+        case 6: return launch_matvec_blocks<T, S, false, 3>(a, runs, st);
+        case 7: return launch_matvec_blocks<T, S, true, 3>(a, runs, st);
+        case 8: return launch_matvec_blocks<T, S, false, 4>(a, runs, st);
+        default: return launch_matvec_blocks<T, S, true, 4>(a, runs, st);
     }
 }
 

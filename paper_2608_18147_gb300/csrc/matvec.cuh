@@ -21,6 +21,8 @@ struct MatvecArgs {
     int32_t b, m, groups;
     int32_t warps_k;              // warps that share a row tile along k, a power of two; the others take other tiles
     int32_t chunk;                // columns that one pass over the rows covers, a multiple of 128
+    int32_t slices, slice;        // 16-bit types: blocks of a cluster that share a run of rows, and their columns each, a multiple of 128
+    bool keep;                    // 16-bit types: sums of rows are kept for another pass or slice
     int32_t stages;               // stages of the codes' ring
     int32_t pitch, scale_pitch;   // 16-bit types: bytes from one row to the next in a stage, and among the scales
     int32_t pieces_below;         // 16-bit types: halves of stages that lie below the table
@@ -60,7 +62,7 @@ __device__ __forceinline__ uint32_t group_of(const MatvecArgs &a, uint32_t w) {
 // Blocks of a launch, one for each SM (152), more where a block would have over kRowsMost rows.  The block's run of rows:
 // whole eights, as even as they can be.
 static inline int64_t row_blocks(int64_t n) { return std::max(std::min<int64_t>(cdiv(n, 8), 152), cdiv(cdiv(n, 8), kRowsMost / 8)); }
-__device__ __forceinline__ int64_t row_of(const MatvecArgs &a, unsigned block) { return min(a.n, (a.n + 7) / 8 * block / gridDim.x * 8); }
+__device__ __forceinline__ int64_t row_of(const MatvecArgs &a, unsigned block, unsigned blocks) { return min(a.n, (a.n + 7) / 8 * block / blocks * 8); }
 
 int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st);
 

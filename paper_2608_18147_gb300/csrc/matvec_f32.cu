@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
     float *xs = reinterpret_cast<float *>(rest);  // x, a.chunk columns a row
     const char *ring = rest + nb * a.chunk * 4;
     const int pitch = a.chunk / 2 + kRowPad, stage_bytes = rows_at_once * pitch;
-    const int64_t r0 = row_of(a, blockIdx.x);
-    const int rows = (int)(row_of(a, blockIdx.x + 1) - r0), rounds = (rows + rows_at_once - 1) / rows_at_once;
+    const int64_t r0 = row_of(a, blockIdx.x, gridDim.x);
+    const int rows = (int)(row_of(a, blockIdx.x + 1, gridDim.x) - r0), rounds = (rows + rows_at_once - 1) / rows_at_once;
     const uint8_t *codes = a.codes + r0 * a.code_row;
     const float *scales = static_cast<const float *>(a.scales) + r0 * a.scale_row;
 

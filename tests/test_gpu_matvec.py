@@ -175,6 +175,22 @@ def test_many_rows_and_columns(n, k, b, group, dtype):
     check(y[:, some.cuda()], ref, size, k, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,k,b,group", [(393, 15530, 2, 128), (64, 16384, 1, 64), (1000, 8192, 8, 128), (700, 20001, 3, 32), (300, 28672, 5, 96),
+                                         (1, 16640, 1, 128), (77, 16385, 7, 256), (2046, 16384, 1, 128), (4100, 28672, 4, 128), (40000, 12800, 1, 128)])
+def test_columns_shared_by_a_cluster(n, k, b, group, dtype):
+    """Few rows and many columns, whose sums several blocks share, at sizes that do not divide evenly; twice for equal bits."""
+    import paper_2608_18147_gb300 as E
+    x, idx, levels, scales = make(n, k, b, group, dtype, "f32", seed=n + k)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = (x.cuda(), E.ecasq_pack(idx.cuda()), levels.cuda(), scales.cuda(), group)
+    y = E.ecasq_matvec(*args, status=status)
+    assert status.item() == 0 and torch.equal(y, E.ecasq_matvec(*args))
+    some = torch.cat([torch.arange(0, n, max(1, n // 300)), torch.arange(max(0, n - 40), n)])
+    ref, size = reference(x, idx[some], levels, scales[some], group)
+    check(y[:, some.cuda()], ref, size, k, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_nan_and_inf_stay_in_their_row(dtype):
     import paper_2608_18147_gb300 as E
