@@ -5,28 +5,44 @@
 
 namespace ecasq {
 
-// Splits.  A block has a fixed cost of its own, about what kCost keys take it (its first loads' latency, the join), so a
-// split should be long; and the blocks should fill the card evenly: with `slots` of them at once, n splits a sequence take
-// ceil(b blocks n / slots) rounds of a split's keys and that cost.  With one round a shorter sequence takes shorter splits, so that
-// all blocks still work; with several the splits keep their length, and their number adapts.
+// Splits.  A block has a fixed cost of its own, about what kCost keys take it (its first loads' latency), and the join's launch
+// about what kJoinCost keys take, so a split should be long; and the blocks should fill the card evenly: with `slots` of them at
+// once, n splits a sequence take ceil(b blocks n / slots) rounds of a split's keys and that cost.  With one round a shorter
+// sequence takes shorter splits, so that all blocks still work; with several the splits keep their length, and their number adapts.
 constexpr int kSms = 152, kMostResident = 8, kMostRounds = 8, kCost = 96, kLeastStep = 64, kMostTile = 32;
+constexpr int kClusterMost = 8, kClusterChunk = 1024, kJoinCost = 64;
+
+// Whether the splits of a sequence are a cluster of blocks that joins them itself, through its shared memory, which saves the join's
+// launch.  Clusters do not fill the SMs evenly, larger ones less so, which costs in proportion to a split's keys; so only where
+// splits are short and blocks few.  (Eight key heads, four heads each, bf16 keys of 128, by clusters and by the join: one sequence of
+// 1000 keys, a head each, 6.0 and 6.5 us, 8 of 600 7.7 and 9.4, 16 of 2000 in three splits 24.9 and 28.0; but 8 of 2000 in
+// seven splits, 448 blocks, 23.4 and 18.5, and 32 of up to 8192, eight heads each, 118 and 94.)
+static bool by_cluster(int64_t count, int64_t chunk, int64_t blocks, int64_t slots) {
+    return count > 1 && count <= kClusterMost && chunk <= kClusterChunk && 2 * blocks <= (count <= kClusterMost / 2 ? 2 * slots : 5 * kSms);
+}
 
 struct Splits {
     int32_t least, count;
+    bool cluster;
 };
 static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots, int64_t step) {
     const int64_t all = std::max<int64_t>(1, b * blocks);
-    Splits best{0, 0};
+    Splits best{0, 0, false};
     int64_t least = INT64_MAX;
-    for (int64_t rounds = 1; rounds <= kMostRounds; rounds++) {  // the most splits that this many rounds hold
-        const int64_t n = std::max<int64_t>(1, slots * rounds / all);
+    const auto consider = [&](int64_t n) {
         const int64_t chunk = std::max<int64_t>(1, cdiv(cdiv(span, n), step)) * step, count = std::max<int64_t>(1, cdiv(span, chunk));
-        const int64_t cost = cdiv(all * count, slots) * (chunk + kCost);
+        const bool cluster = by_cluster(count, chunk, all * count, slots);
+        const int64_t cost = cdiv(all * count, slots) * (chunk + kCost) + (count > 1 && !cluster ? kJoinCost : 0);
         if (cost < least) {
             least = cost;
-            best = {(int32_t)(all * count <= slots ? step : chunk), (int32_t)count};
+            best = {(int32_t)(all * count <= slots ? step : chunk), (int32_t)count, cluster};
         }
-        if (chunk == step) break;
+        return chunk > step;
+    };
+    for (int64_t rounds = 1; rounds <= kMostRounds; rounds++) {  // the most splits that this many rounds hold
+        const int64_t n = std::max<int64_t>(1, slots * rounds / all);
+        if (n > kClusterMost) consider(kClusterMost);
+        if (!consider(n)) break;
     }
     return best;
 }
@@ -43,6 +59,7 @@ int split_attend(AttendArgs &a, int64_t b, int resident) {
     const Splits s = make_splits(b, blocks, a.max_len + (a.starts ? a.tile - 1 : 0), kSms * std::min(resident, kMostResident), a.step);
     a.least = s.least;
     a.splits = s.count;
+    a.cluster = s.cluster;
     if (a.splits == 1) return ECASQ_OK;
     if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, blocks, a.d, a.max_len)) return ECASQ_EWORKSPACE;
     a.part = static_cast<float *>(a.ws);
@@ -237,7 +254,7 @@ int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_
     else if (!k->levels_n) rc = launch_attend_16(a, bf16, b, st);
     else if (k->levels_n == 8) rc = launch_attend_coded8(a, bf16, b, st);
     else rc = launch_attend_coded16(a, bf16, b, st);
-    if (rc || a.splits == 1) return rc;
+    if (rc || a.splits == 1 || a.cluster) return rc;
     if (k->type == ECASQ_F32) return launch_join<float>(a, b, st);
     return bf16 ? launch_join<__nv_bfloat16>(a, b, st) : launch_join<__half>(a, b, st);
 }

@@ -7,12 +7,12 @@
 //
 // What bounds it: the cache's bytes.  So each warp works alone on tiles of 16 or 32 keys through a ring of its own in
 // shared memory that cp.async fills a few tiles ahead, without a barrier in the loop.  The sequence is cut into
-// splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory
-// and k_attend_join joins the splits.  Measured, both kernels: 32 sequences of up to 8192 bf16 keys of 128, eight heads a key
+// splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory,
+// and the splits in that of a cluster of blocks or, by k_attend_join, in memory.  Measured, both kernels: 32 sequences of up to 8192 bf16 keys of 128, eight heads a key
 // head, 94 us or 5.7 TB/s, 84 % of a copy's rate.  Coded rows are bound by the lookups, byte permutes on the integer
 // pipe, which is 57 to 61 % busy: 16 sequences of 32768 keys of 128 with eight levels 148 us (4.5 TB/s, 67 %), one of
 // 70001 keys of 256 with sixteen 52 us (1.7 TB/s).  Short sequences are bound by latency: lengths, page numbers, rows and
-// the join follow one another; one sequence of 1000 keys takes 6.4 us.
+// the join follow one another; one sequence of 1000 keys takes 6.0 us.
 //
 // 16-bit rows: S^T = K Q^T and O^T = V^T P^T on mma.m16n8k16 with the query heads as n, fp32 sums.  (One
 // token a sequence is a matrix-vector product for each key head; with eight columns there is nothing for the
@@ -34,6 +34,7 @@
 // fp32 rows: fp32 products on the FMA pipe in the same frame.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "codes.cuh"
@@ -58,6 +59,7 @@ struct AttendArgs {
     int64_t q_row, q_head, out_row, out_head, table_row, pages;
     float scale2;                // scale log2(e)
     int32_t heads, group, htiles, d, page_size, max_len, splits, tile, step, least;  // group: query heads a key head; least: keys of a split
+    bool cluster;                // the splits are a cluster, which joins them
     uint32_t div_mul, div_shift; // t div page_size = umulhi(t, div_mul) >> div_shift, or t >> div_shift if div_mul is 0
 };
 
@@ -193,7 +195,7 @@ template <typename T, int LV, int NV> struct Shape {
     static constexpr int kStages = kBytes > 5120 ? 2 : 3;
     static constexpr int kRing = kStages * kBytes;                         // of a warp
     static constexpr int kJoin = kHeads * 64 * NV * 4;                     // a warp's sums at the end, in its ring
-    static constexpr int kExtra = (kF32 ? kHeads * 64 * NV * 4 + kWarps * kTile * kHeads * 4 : 0) + kWarps * (2 * kHeads * 4) + kWarps * kStages * 4;
+    static constexpr int kExtra = (kF32 ? kHeads * 64 * NV * 4 + kWarps * kTile * kHeads * 4 : 0) + (kWarps + 1) * (2 * kHeads * 4) + kWarps * kStages * 4;
     static constexpr bool kQShared = LV && NV == 4;                        // q's operands lie in shared memory
     static constexpr int kSmem = kWarps * kRing + (kExtra + 15) / 16 * 16 + (kQShared ? 512 * 2 * NV : 0);
     static_assert(kJoin <= kRing, "");
@@ -257,8 +259,15 @@ __device__ __forceinline__ void store_out(const AttendArgs &a, int64_t seq, int 
     for (int i = 0; i < 4; i++) out[i] = from_f32<T>(sum == 0.f ? 0.f : x[i] / sum);
 }
 
-// HT: query heads of a block, 4 or 8.
-template <typename T, int LV, int NV, int HT>
+__device__ __forceinline__ float shared_of_rank(const float *p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(of_rank(smem_addr(p), rank)) : "memory");
+    return v;
+}
+
+// HT: query heads of a block, 4 or 8.  CLUSTER: the splits are a cluster of blocks, which joins them (apart from the others, whose loop
+// over the tiles comes out slower with this in one kernel: 159 against 149 us for 16 sequences of 32768 eight-level keys).
+template <typename T, int LV, int NV, int HT, bool CLUSTER>
 __global__ void __launch_bounds__(32 * Shape<T, LV, NV>::kWarps, Shape<T, LV, NV>::kQShared ? 3 : 0)
 k_attend(const __grid_constant__ AttendArgs a) {
     using S = Shape<T, LV, NV>;
@@ -307,14 +316,21 @@ k_attend(const __grid_constant__ AttendArgs a) {
     if (span.too_long && threadIdx.x == 0 && split == 0 && a.status) atomicOr(a.status, ECASQ_BAD_LENGTH);
     const Cut cut = cut_of(a, span);
     const int active = cut.count;
-    if (split >= max(active, 1)) return;
+    if (split >= max(active, 1)) {
+        if (CLUSTER && active > 1) {
+            cluster_barrier();
+            cluster_barrier();
+        }
+        return;
+    }
     const int begin = cut.lead + split * cut.chunk, end = min(span.end, begin + cut.chunk);  // keys of this split (from `first` on)
 
     char *ring = smem + wid * S::kRing;
     float *qs = reinterpret_cast<float *>(smem + S::kWarps * S::kRing);  // fp32: q, then each warp's weights
     float *ps = qs + kHeads * 64 * NV + wid * kTile * kHeads;
     float *wmax = qs + (S::kF32 ? kHeads * 64 * NV + S::kWarps * kTile * kHeads : 0), *wsum = wmax + S::kWarps * kHeads;
-    uint32_t *seen = reinterpret_cast<uint32_t *>(wsum + S::kWarps * kHeads) + wid * S::kStages;  // keys of a stage that count
+    float *bmax = wsum + S::kWarps * kHeads, *bsum = bmax + kHeads;                      // of the block, for its cluster
+    uint32_t *seen = reinterpret_cast<uint32_t *>(bsum + kHeads) + wid * S::kStages;  // keys of a stage that count
 
     // ---- copies.  The lane's key of a tile is number lane mod kKeys; find() looks its page up, a tile ahead of fetch().
     const char *kb = a.k + kh * a.k_head, *vb = a.v + kh * a.v_head;
@@ -792,7 +808,13 @@ k_attend(const __grid_constant__ AttendArgs a) {
             v.z += y.z;
             v.w += y.w;
         }
-        if (active > 1) {
+        if (CLUSTER && active > 1) {  // in the place of the first warp's, which only this thread reads
+            *reinterpret_cast<float4 *>(smem + 4 * (h * kWide + e)) = v;
+            if (e == 0) {
+                bmax[h] = x;
+                bsum[h] = sum;
+            }
+        } else if (active > 1) {
             float *part = at.at(a.part, seq, a.heads, h0 + h, a.splits, split);
             *reinterpret_cast<float4 *>(part + e) = v;
             if (e == 0) *reinterpret_cast<float2 *>(part + a.d) = make_float2(x, sum);
@@ -801,15 +823,40 @@ k_attend(const __grid_constant__ AttendArgs a) {
             if (e == 0 && a.lse) a.lse[seq * a.heads + h0 + h] = log_sum(x, sum);
         }
     }
+    if constexpr (CLUSTER) {  // its blocks join each a share of the entries
+        if (active <= 1) return;
+        cluster_barrier();
+        for (int i = threadIdx.x + 32 * S::kWarps * split; i < nh * quads; i += 32 * S::kWarps * active) {
+            const int h = i / quads, e = 4 * (i % quads);
+            float x = -CUDART_INF_F, sum = 0.f;
+            for (int s = 0; s < active; s++) x = fmaxf(x, shared_of_rank(bmax + h, s));
+            const float from = x == -CUDART_INF_F ? 0.f : x;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int s = 0; s < active; s++) {
+                const float share = exp2_fast(shared_of_rank(bmax + h, s) - from);
+                sum = fmaf(shared_of_rank(bsum + h, s), share, sum);
+                float4 y;
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w) : "r"(of_rank(smem_addr(smem + 4 * (h * kWide + e)), s)) : "memory");
+                v.x = fmaf(y.x, share, v.x);
+                v.y = fmaf(y.y, share, v.y);
+                v.z = fmaf(y.z, share, v.z);
+                v.w = fmaf(y.w, share, v.w);
+            }
+            store_out<T>(a, seq, h0 + h, e, v, sum);
+            if (e == 0 && a.lse) a.lse[seq * a.heads + h0 + h] = log_sum(x, sum);
+        }
+        cluster_barrier();  // a block's shared memory stays until all have read it
+    }
 }
 
 // Blocks of a kernel that an SM holds; 0 if the query fails.
-template <typename T, int LV, int NV, int HT>
+template <typename T, int LV, int NV, int HT, bool CLUSTER>
 static int prepare_attend() {
     using S = Shape<T, LV, NV>;
     int n = 0;
-    if (cudaFuncSetAttribute(k_attend<T, LV, NV, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attend<T, LV, NV, HT>, 32 * S::kWarps, S::kSmem) != cudaSuccess) return 0;
+    if (cudaFuncSetAttribute(k_attend<T, LV, NV, HT, CLUSTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_attend<T, LV, NV, HT, CLUSTER>, 32 * S::kWarps, S::kSmem) != cudaSuccess) return 0;
     return n;
 }
 // Splits the sequences (split_attend) and launches.
@@ -821,7 +868,7 @@ static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
     ECASQ_CUDA_TRY(cudaGetDevice(&device));
     int resident = device < kDevices ? known[device].load(std::memory_order_acquire) : 0;
     if (resident < 1) {
-        resident = prepare_attend<T, LV, NV, HT>();
+        resident = std::min(prepare_attend<T, LV, NV, HT, false>(), prepare_attend<T, LV, NV, HT, true>());
         if (resident < 1) return ECASQ_ECUDA;
         if (device < kDevices) known[device].store(resident, std::memory_order_release);
     }
@@ -830,7 +877,8 @@ static int launch_attend(AttendArgs &a, int64_t b, cudaStream_t st) {
     const int rc = split_attend(a, b, resident);
     if (rc) return rc;
     const dim3 grid((unsigned)(a.heads / a.group * a.htiles), (unsigned)a.splits, (unsigned)b);
-    return launch_early(k_attend<T, LV, NV, HT>, grid, 32 * S::kWarps, S::kSmem, st, a);
+    if (a.cluster) return launch_clusters(k_attend<T, LV, NV, HT, true>, grid, dim3(1, (unsigned)a.splits), 32 * S::kWarps, S::kSmem, st, a);
+    return launch_early(k_attend<T, LV, NV, HT, false>, grid, 32 * S::kWarps, S::kSmem, st, a);
 }
 template <typename T, int LV, int HT>
 static int launch_attend_rows(AttendArgs &a, int64_t b, cudaStream_t st) {

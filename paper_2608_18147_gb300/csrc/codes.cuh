@@ -55,32 +55,44 @@ template <typename K> static inline int allow_smem(K *kernel, int bytes, std::at
 // runs.  (In a row of calls: a product with 1024 x 1024 codes 3.3 us, and 3.9 launched after the kernel before it has ended;
 // attention over 64 sequences of 100 keys 9.8 and 10.2 us; 32 x 8 cache rows 2.3 and 2.7 us.)
 template <typename... P, typename... A>
-static inline int launch_clusters(void (*kernel)(P...), dim3 grid, int cluster, int threads, int smem, cudaStream_t st, A &&...args) {
+static inline int launch_clusters(void (*kernel)(P...), dim3 grid, dim3 cluster, int threads, int smem, cudaStream_t st, A &&...args) {
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = cluster.x;
+    attr[1].val.clusterDim.y = cluster.y;
+    attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cfg.numAttrs = cluster.x * cluster.y > 1 ? 2 : 1;
     note_launch();
     ECASQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...));
     return ECASQ_OK;
 }
 template <typename... P, typename... A>
 static inline int launch_early(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A &&...args) {
-    return launch_clusters(kernel, grid, 1, threads, smem, st, std::forward<A>(args)...);
+    return launch_clusters(kernel, grid, dim3(1), threads, smem, st, std::forward<A>(args)...);
 }
 // Waits until the kernel before this one has ended and what it wrote can be read, then lets the blocks of the kernel after this one
 // be placed as soon as all of this one's have been.  Every block does so before it reads or writes memory, and before it ends, so
 // that the kernel after this one has waited for all that came before.
 __device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory"); }
+
+// What a cluster's threads wrote to shared memory before it can be read by all of them after it.  (Threads that have ended do not count.)
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// The address in the cluster of what lies at `at` in the shared memory of block `rank`.
+__device__ __forceinline__ uint32_t of_rank(uint32_t at, uint32_t rank) {
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    return there;
+}
 
 // The limits that ecasq_cache_t states; bytes of a row's entries and of its codebook.
 static inline bool cache_ok(const ecasq_cache_t *c) {

@@ -285,20 +285,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
         if (k0 + a.chunk < k_end) __syncthreads();  // the sums of this pass, before the next one's
     }
     if (a.slices > 1) {  // each block adds its share of the rows over the cluster
-        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        cluster_barrier();
         for (int i = (int)rank * kThreads + tid; i < 8 * rows; i += a.slices * kThreads) {
             const int row = i / 8, col = i & 7;
             if (col >= nb) continue;
             float v = 0.f;
             for (int s = 0; s < a.slices; s++) {
                 float of;
-                asm volatile("{ .reg .b32 at; mapa.shared::cluster.u32 at, %1, %2; ld.shared::cluster.f32 %0, [at]; }"
-                             : "=f"(of) : "r"(smem_at(row_sums + i)), "r"(s) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(of) : "r"(of_rank(smem_at(row_sums + i), s)) : "memory");
                 v += of;
             }
             static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(v);
         }
-        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        cluster_barrier();
     }
     if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
 }
@@ -321,7 +320,7 @@ static int launch_matvec_blocks(const MatvecArgs &a, int64_t runs, cudaStream_t 
     int rc = window_ok();
     if (!rc) rc = allow_smem(k_matvec<T, S, WIDE, R>, kSmemBytes, allowed);
     if (rc) return rc;
-    return launch_clusters(k_matvec<T, S, WIDE, R>, dim3((unsigned)(runs * a.slices), (unsigned)cdiv(a.b, 8)), a.slices, kThreads, kSmemBytes, st, a);
+    return launch_clusters(k_matvec<T, S, WIDE, R>, dim3((unsigned)(runs * a.slices), (unsigned)cdiv(a.b, 8)), dim3((unsigned)a.slices), kThreads, kSmemBytes, st, a);
 }
 
 // Clusters of c = 2 or 4 blocks that the card holds at once (76 and 36), asked once a device.  Every k_matvec has the same threads and

@@ -286,6 +286,18 @@ def test_many_sequences(dtype, levels):
 
 
 @pytest.mark.parametrize("dtype,levels", KINDS)
+@pytest.mark.parametrize("lengths,max_len,starts", [([500, 0, 1, 130, 64], 512, None), ([256, 255], 256, [255, 0]), ([65, 3, 400], 1000, [0, 2, 399]),
+                                                    ([900], 960, [17])])
+def test_few_splits(lengths, max_len, starts, dtype, levels):
+    """Two to eight splits, of which a short sequence fills one or none; twice for equal bits."""
+    c = make(lengths, 2, 3, 96, 16, dtype, levels, "nhd", seed=22, starts=starts, max_len=max_len)
+    got = call(c, max_len=max_len)
+    check(got, reference(c))
+    again = call(c, max_len=max_len)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+@pytest.mark.parametrize("dtype,levels", KINDS)
 def test_starts_beyond_every_key(dtype, levels):
     """A start past the end leaves no key, however far past it is."""
     c = make([50, 50, 600, 600], 2, 4, 32, 16, dtype, levels, "nhd", seed=21, starts=[2 ** 31 - 1, 49, 2 ** 31 - 40, 3])
