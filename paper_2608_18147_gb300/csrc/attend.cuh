@@ -9,8 +9,8 @@
 // shared memory that cp.async fills a few tiles ahead, without a barrier in the loop.  The sequence is cut into
 // splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory,
 // and the splits in that of a cluster of blocks or, by k_attend_join, in memory.  Measured, both kernels: 32 sequences of up to 8192 bf16 keys of 128, eight heads a key
-// head, 94 us or 5.7 TB/s, 84 % of a copy's rate.  Coded rows are bound by the lookups, byte permutes on the integer
-// pipe, which is 57 to 61 % busy: 16 sequences of 32768 keys of 128 with eight levels 148 us (4.5 TB/s, 67 %), one of
+// head, 95 us or 5.6 TB/s, 83 % of a copy's rate.  Coded rows are bound by the lookups, byte permutes on the integer
+// pipe, which is 57 to 61 % busy: 16 sequences of 32768 keys of 128 with eight levels 149 us (4.5 TB/s, 66 %), one of
 // 70001 keys of 256 with sixteen 52 us (1.7 TB/s).  Short sequences are bound by latency: lengths, page numbers, rows and
 // the join follow one another; one sequence of 1000 keys takes 6.0 us.
 //

@@ -55,8 +55,8 @@ __device__ __forceinline__ float shared_float(uint32_t at) { return *static_cast
 // The row's levels and the gaps above them lie in shared memory, a word a bank, so lanes that look up different levels
 // do not meet.
 //
-// What bounds it: instruction issue (70 % of the slots, 62 instructions an entry), as in the flat encode; 8191 x 8 rows of 128
-// take 19.4 us, 1.4 TB/s or 430 entries a nanosecond, a step of 32 x 8 rows 2.6 us.  The rule's draw alone is about 20 instructions an
+// What bounds it: instruction issue (71 % of the slots, 62 instructions an entry), as in the flat encode; 8191 x 8 rows of 128
+// take 18.9 us, 1.5 TB/s or 440 entries a nanosecond, a step of 32 x 8 rows 2.3 us.  The rule's draw alone is about 20 instructions an
 // entry.  So the draw is the 32-bit form of draw.cuh, the search takes log2 LV steps, and the gaps are formed once a row;
 // an entry equal to its level needs no test (its distance 0 is above no product), nor does one at or beyond the last level
 // (the gap there is infinite).  The search's position is a shared-memory address that steps by predicated fp32 additions of

@@ -52,8 +52,8 @@ __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, i
 // larger tensor tile could draw on.)
 //
 // What bounds it: the codes' bytes in the end, and on the way there the latency of lookups and products at sixteen warps an
-// SM (issue slots 46 %, shared memory 46 %, DRAM 35 % busy with eight rows).  28672 x 8192 by eight rows of bf16 takes 35.5 us,
-// 3.5 TB/s; 8192 x 8192 by one row of fp16, groups of 64, 16.0 us, 2.2 TB/s; a small matrix 4 us: the launch, one memory latency
+// SM (issue slots 46 %, shared memory 46 %, DRAM 34 % busy with eight rows).  28672 x 8192 by eight rows of bf16 takes 35.6 us,
+// 3.5 TB/s; 8192 x 8192 by one row of fp16, groups of 64, 15.1 us, 2.4 TB/s; a small matrix 3.3 us: the launch, one memory latency
 // and the table.  The table is held once a lane, so that no two lanes meet in a bank; 32 lookups, 8 transactions for the codes
 // themselves and up to 8 for the scales stand, for each KB of codes, against the 44 clocks that memory needs for it.  Entry e of lane l lies at address
 // kTableAt + 256 e + 4 l: one byte permute puts the code byte between the lane's constant ones, and that is the address.

@@ -7,7 +7,7 @@
 //
 // What bounds it: shared memory and its latency at sixteen warps an SM.  The table of fp32 pairs is held once for each two lanes,
 // so a lookup takes two transactions where the 16-bit types need one, and each eight weights read x once for every row of
-// x.  8192 x 8192 by one row takes 29.8 us (1.2 TB/s), by eight 98 us; 2999 x 2050 by three 9.4 us.
+// x.  8192 x 8192 by one row takes 28.9 us (1.2 TB/s), by eight 98 us; 2999 x 2050 by three 8.8 us.
 #include <algorithm>
 
 #include "matvec.cuh"
