@@ -252,3 +252,40 @@ def test_empty_batch_and_refusals():
     for idx in (idx, idx.cuda().int(), idx.cuda()[0], idx.cuda().t()):
         with pytest.raises(E.EcasqError):
             E.ecasq_pack(idx)
+
+
+def test_waits_for_what_came_before():
+    """Inputs written by a long kernel before the call, in its stream or in another one that its stream waits for, and outputs
+    read behind it; with calls right before and after, whose launches overlap."""
+    import paper_2608_18147_gb300 as E
+    n, k, b = 1024, 1024, 4
+    x, idx, levels, scales = make(n, k, b, 128, "bf16", "f32", seed=31)
+    codes, levels, scales, x = E.ecasq_pack(idx.cuda()), levels.cuda(), scales.cuda(), x.cuda()
+    right = E.ecasq_matvec(x, codes, levels, scales, 128)
+    big = torch.randn(4096, 4096, device="cuda")
+    here, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        late = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(here):
+            torch.mm(big, big)
+            late.copy_(x)
+            first = E.ecasq_matvec(late, codes, levels, scales, 128)
+            second = E.ecasq_matvec(late * 1, codes, levels, scales, 128)
+            kept = second.clone()
+            second.zero_()
+        torch.cuda.synchronize()
+        assert torch.equal(first, right) and torch.equal(kept, right)
+        late = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            torch.mm(big, big)
+            late.copy_(x)
+            done = other.record_event()
+        with torch.cuda.stream(here):
+            E.ecasq_matvec(x, codes, levels, scales, 128)
+            here.wait_event(done)
+            third = E.ecasq_matvec(late, codes, levels, scales, 128)
+        torch.cuda.synchronize()
+        assert torch.equal(third, right)
