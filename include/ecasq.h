@@ -482,8 +482,9 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
  * query head h, which reads key head h div (heads / k->heads):
  *   s_t = scale q . K_t,  out = sum_t softmax(s)_t V_t,  lse = log sum_t exp(s_t)
  * over the keys t in [starts[i], lengths[i]); a sequence without keys gives out = 0 and
- * lse = -inf, and so does one whose weights are all zero.  Scores, weights and sums are fp32;
- * out is rounded once, to q's type.  Nothing outside that range is read, whatever it holds.
+ * lse = -inf, and so does one whose weights are all zero.  Scores, sums and the weights of lse are
+ * fp32; the weights of out are too for F32, and have 16 bits for BF16 and F16 (for F16 in steps of no less
+ * than 2^-40 of the largest weight); out is rounded once, to q's type.  Nothing outside that range is read, whatever it holds.
  * Values are finite: an infinity among those seen may give NaN where the sum is infinite.
  *   q        device [b, heads, d] of the cache's type, strides in elements, entries
  *            contiguous; out likewise

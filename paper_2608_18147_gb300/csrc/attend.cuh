@@ -26,8 +26,11 @@
 // out side by side, in as many products as before.  With up to eight (HT = 8) the columns are taken, and two keys'
 // registers are first permuted into pairs of keys.  (Four heads a key head, 16 sequences of 8192 keys: with HT = 4 and 8 50.1
 // and 55.6 us for eight-level rows, 52.3 and 53.6 for sixteen levels and rows of 64, 94.0 and 95.1 for 32 of 4096 bf16 keys.)
-// Weights enter the second product as a high and a low 16-bit part (their sum keeps 16 bits or more): one part alone would
-// add an error as large as the rounding of the result.
+// Weights enter the second product as a high and a low 16-bit part: one part alone would add an error as large as the rounding of
+// the result.  In bf16 the two keep 16 bits of a weight of any size.  Binary16 has no step below 2^-24, so there the parts are those of
+// 2^15 times the weight, which is at most 1: 16 bits of weights down to 2^-24 of the largest, and steps of 2^-40 of it below
+// (parts of the weight itself lose bits from 2^-9 on, and all of a weight below 2^-25, which is wrong where the heaviest key holds
+// small values).
 // Coded rows: a lane holds its row's codebook as planes of low and of high bytes; a byte permute with four
 // codes as its selector looks four entries up in eight levels at once, so that a pair of entries costs two lookups
 // and two permutes and no shared-memory access.
@@ -71,6 +74,9 @@ struct PartAt {
         return part + ((seq * heads + head) * splits + split) * stride;
     }
 };
+
+// What the weights of the values' product are multiplied by (see above); a power of two, taken off again from the sums.
+template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 0x1p15f : 1.f;
 
 // Sets a.splits, a.least and, where there are several, a.part from the workspace; `resident`: blocks that an SM holds; splits are multiples of a.step keys.
 int split_attend(AttendArgs &a, int64_t b, int resident);
@@ -656,9 +662,10 @@ k_attend(const __grid_constant__ AttendArgs a) {
             uint32_t hi[HT == 4 ? 4 : 2], lo[HT == 4 ? 4 : 2];
 #pragma unroll
             for (int u = 0; u < 2; u++) {
-                const uint32_t h = pack2<T>(c[part][u][0], c[part][u][HL - 1]);
+                const float w0 = c[part][u][0] * kLift<T>, w1 = c[part][u][HL - 1] * kLift<T>;
+                const uint32_t h = pack2<T>(w0, w1);
                 const float2 f = unpack2<T>(h);
-                const uint32_t th = transpose8x8(h), tl = transpose8x8(pack2<T>(c[part][u][0] - f.x, c[part][u][HL - 1] - f.y));
+                const uint32_t th = transpose8x8(h), tl = transpose8x8(pack2<T>(w0 - f.x, w1 - f.y));
                 if constexpr (HT == 4) {
                     hi[2 * u] = prmt(th, 0, sel0);
                     hi[2 * u + 1] = prmt(th, 0, sel1);
@@ -775,7 +782,7 @@ k_attend(const __grid_constant__ AttendArgs a) {
     } else {
         float s[HL];
 #pragma unroll
-        for (int h = 0; h < HL; h++) s[h] = shrink(wid, HL * t + h, top_of(HL * t + h));
+        for (int h = 0; h < HL; h++) s[h] = shrink(wid, HL * t + h, top_of(HL * t + h)) * (1.f / kLift<T>);
 #pragma unroll
         for (int j = 0; j < 2 * NV; j++) {
             // four entries of the lane's heads: plain 8 (g + 8 i) + 4 (j mod 2), i = j div 2; coded 8 NV g + 4 j
