@@ -399,7 +399,7 @@ int ecasq_prepare(const float *x, int64_t d, void *ws, size_t ws_bytes, float *v
 #define ECASQ_BAD_PAGE 1   /* a page number outside [0, pages) (its keys are left out) or a slot beyond the cache (its row is dropped) */
 #define ECASQ_BAD_LENGTH 2 /* a sequence longer than max_len (cut to it) */
 #define ECASQ_BAD_COUNT 4  /* a codebook's m outside [1, s] (clamped) */
-#define ECASQ_BAD_VALUE 8  /* a cache row with NaN or Inf (NaN takes code 0, Inf an end of the codebook) */
+#define ECASQ_BAD_VALUE 8  /* a cache row with NaN or Inf (NaN takes code 0, Inf an end of the codebook), or a level that is NaN or beyond the cache's type */
 #define ECASQ_BAD_WAIT 16  /* a bounded wait for a copy into shared memory ran out (the outputs concerned are NaN) */
 
 /* Indices of ecasq_quantize (one byte each, < 16; only the low four bits are read)
@@ -459,7 +459,8 @@ typedef struct ecasq_cache {
 
 /* Encodes the rows x [n, heads, d] of n new slots into a coded cache, each with its
  * own codebook, by the unbiased rounding of ecasq_quantize (Sec. 2).
- * Row (i, h): its levels are r_j = Q[j] rounded to the cache's type for j < m and
+ * Row (i, h): its levels are r_j = Q[j] rounded to the cache's type for j < m (the
+ * type's largest finite value where Q[j] lies beyond it, which sets ECASQ_BAD_VALUE) and
  * r_j = r_{m-1} beyond.  Entry e with a = max{r_j <= x, j < m} (r_0 if there is none)
  * keeps a's code if it equals a or a is the last; otherwise it takes the next one iff
  * fl32(fl32(k 2^-24) fl32(b - a)) < fl32(x - a), k = top 24 bits of SplitMix64(seed +

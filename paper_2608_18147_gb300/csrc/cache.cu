@@ -47,6 +47,16 @@ template <typename I> __device__ __forceinline__ I quotient(I v, const FastDiv &
 }
 __device__ __forceinline__ uint64_t product(uint32_t a, uint32_t b) { return (uint64_t)a * b; }
 __device__ __forceinline__ int64_t product(int64_t a, int64_t b) { return a * b; }
+// The largest finite value of a 16-bit type, as its bits, and the least fp32 that rounds beyond it.
+template <typename T> struct Range;
+template <> struct Range<__half> {
+    static constexpr uint16_t kMost = 0x7BFF;
+    static constexpr float kBeyond = 65520.f;
+};
+template <> struct Range<__nv_bfloat16> {
+    static constexpr uint16_t kMost = 0x7F7F;
+    static constexpr float kBeyond = 0x1.FFp127f;
+};
 __device__ __forceinline__ float shared_float(uint32_t at) { return *static_cast<const float *>(__cvta_shared_to_generic(at)); }
 
 // LV levels a row.  W lanes take a row, E neighbouring entries each: 16 lanes with four for rows of up to 64 entries, with eight
@@ -56,7 +66,7 @@ __device__ __forceinline__ float shared_float(uint32_t at) { return *static_cast
 // do not meet.
 //
 // What bounds it: instruction issue (71 % of the slots, 62 instructions an entry), as in the flat encode; 8191 x 8 rows of 128
-// take 18.9 us, 1.5 TB/s or 440 entries a nanosecond, a step of 32 x 8 rows 2.3 us.  The rule's draw alone is about 20 instructions an
+// take 19.1 us, 1.4 TB/s or 440 entries a nanosecond, a step of 32 x 8 rows 2.4 us.  The rule's draw alone is about 20 instructions an
 // entry.  So the draw is the 32-bit form of draw.cuh, the search takes log2 LV steps, and the gaps are formed once a row;
 // an entry equal to its level needs no test (its distance 0 is above no product), nor does one at or beyond the last level
 // (the gap there is infinite).  The search's position is a shared-memory address that steps by predicated fp32 additions of
@@ -108,7 +118,12 @@ __global__ void __launch_bounds__(kWriteThreads) k_cache_write(const __grid_cons
         const int m = min(max(r.m, 1), a.s);
         if (m != r.m) bad |= ECASQ_BAD_COUNT;
         __syncwarp(group);  // the row before is done with the book
-        const T rounded = from_f32<T>(r.q);
+        T rounded = from_f32<T>(r.q);  // (a comparison and a choice; a rounding that saturates took 0.2 us more for 8191 x 8 rows of 64)
+        if (lane < m && !(fabsf(r.q) < Range<T>::kBeyond)) {
+            bad |= ECASQ_BAD_VALUE;
+            const uint16_t most = Range<T>::kMost | (uint16_t)(__float_as_uint(r.q) >> 16 & 0x8000u);
+            if (r.q == r.q) rounded = reinterpret_cast<const T &>(most);
+        }
         const float mine = to_f32(rounded), last = __shfl_sync(group, mine, m - 1, W), above = __shfl_down_sync(group, mine, 1, W);
         if (lane < LV) {
             T *levels = static_cast<T *>(a.levels) + product(page, a.level_page) + product(at, a.level_slot) + product(r.h, a.level_head);
