@@ -346,12 +346,12 @@ k_attend(const __grid_constant__ AttendArgs a) {
     const int row_chunks = LV ? a.d / 32 : a.d * (int)sizeof(T) / 16;
     bool bad_page = false;
     struct Found {
-        int page, slot;  // page -2: beyond the split, no error
+        int page, slot;  // slot -1: beyond the split, no error (a table may hold any number)
         __device__ uint64_t offset(uint64_t by_page, uint64_t by_slot) const { return (uint32_t)page * by_page + (uint32_t)slot * by_slot; }
     };
     auto find = [&](int t0) {
         const int key = t0 + (lane & (S::kKeys - 1));
-        Found f{-2, 0};
+        Found f{-1, -1};
         if (key >= span.first && key < end) {
             const int p = page_of(a, key);
             f.slot = key - p * a.page_size;
@@ -362,7 +362,7 @@ k_attend(const __grid_constant__ AttendArgs a) {
     auto fetch = [&](Found f, int stage) {
         char *dst = ring + stage * S::kBytes;
         const bool ok = f.page >= 0 && f.page < a.pages;
-        bad_page |= f.page != -2 && !ok;
+        bad_page |= f.slot >= 0 && !ok;
         const uint32_t mask = __ballot_sync(0xffffffffu, ok) & S::kAll;
         if (lane == 0) seen[stage] = mask;
         // Rows of one page have one address and a step; others each their own, shuffled from the lane that looked it up (32
