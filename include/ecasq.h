@@ -400,7 +400,7 @@ int ecasq_prepare(const float *x, int64_t d, void *ws, size_t ws_bytes, float *v
 #define ECASQ_BAD_LENGTH 2 /* a sequence longer than max_len (cut to it) */
 #define ECASQ_BAD_COUNT 4  /* a codebook's m outside [1, s] (clamped) */
 #define ECASQ_BAD_VALUE 8  /* a cache row with NaN or Inf (NaN takes code 0, Inf an end of the codebook), or a level that is NaN or beyond the cache's type */
-#define ECASQ_BAD_WAIT 16  /* a bounded wait for a copy into shared memory ran out (the outputs concerned are NaN) */
+#define ECASQ_BAD_WAIT 16  /* a bounded wait for a copy into shared memory ran out (all rows of y that its block computes are NaN) */
 
 /* Indices of ecasq_quantize (one byte each, < 16; only the low four bits are read)
  * as the packed rows that ecasq_matvec reads.  Row r of `codes` has
@@ -429,7 +429,10 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
  *   y       device [b rows of y_row elements], of `type`, output
  *   status  ECASQ_BAD_WAIT
  * ECASQ_EINVAL for n or k < 1, b < 0, m outside [1, 16], a bad type, group or
- * alignment. */
+ * alignment.
+ * Test hook: with ECASQ_TEST_LOST_WAIT or-ed into `type` each block goes on as if a wait of its first round
+ * had run out.  Not for production use. */
+#define ECASQ_TEST_LOST_WAIT (1 << 30)
 int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
                  const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
                  int64_t k, int32_t group, void *y, int64_t y_row, int32_t *status, ecasq_stream_t stream);

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, i
 // themselves and up to 8 for the scales stand, for each KB of codes, against the 44 clocks that memory needs for it.  Entry e of lane l lies at address
 // kTableAt + 256 e + 4 l: one byte permute puts the code byte between the lane's constant ones, and that is the address.
 constexpr int kTableAt = 0x20000, kAboveAt = 0x30000, kSmemBytes = 227 * 1024;
-constexpr int kBarBytes = 64, kMostStages = 4;
+constexpr int kBarBytes = 64, kMostStages = 4, kLostAt = 8 * kMostStages;  // barriers, and the word of lost waits
 constexpr int kWindowMost = 2048;  // where a block's own shared memory begins at most (it is 1 KB)
 constexpr int kBelowRoom = kTableAt - kWindowMost - kBarBytes, kAboveRoom = kSmemBytes - kAboveAt;
 
@@ -128,13 +128,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
     wait_before();
     // (Loads are issued before anything waits for another's: the levels here, x before the table is built.)
     const T level = (lane & 15) < a.m ? static_cast<const T *>(a.levels)[lane & 15] : from_f32<T>(0.f);
-    if (tid == 0)
+    const uint32_t lost_at = bars + kLostAt;
+    if (tid == 0) {
         for (int s = 0; s < a.stages; s++) bar_init(bars + 8 * s);
+        set_word(lost_at, a.lost);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
 
     uint32_t parity = 0;  // of the stages' next waits, a bit each
-    bool lost = false;    // a wait ran out
     int turn = 0;
     for (uint32_t k0 = k_first; k0 < k_end; k0 += a.chunk) {
         const int cols = min(a.chunk, (int)(k_end - k0)), blocks = (cols + 127) / 128;
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
             const char *mine = scale_ring + ((round & 1) * 16 * tiles_at_once + row) * a.scale_pitch;
             const uint32_t row0 = (uint32_t)reinterpret_cast<uintptr_t>(scales + first_group), step = (uint32_t)a.scale_row * sizeof(S);
             const char *qa = mine + (row0 + (round * 16 * tiles_at_once + row) * step & 15), *qb = mine + 8 * a.scale_pitch + (row0 + (round * 16 * tiles_at_once + row + 8) * step & 15);
-            if (!bar_wait(bars + 8 * s, parity >> s & 1)) lost = true;
+            if (!bar_wait(bars + 8 * s, parity >> s & 1)) set_word(lost_at, round + 1);
             parity ^= 1u << s;
             const char *up = piece_at(2 * s) + (8 * wr + g) * a.pitch + 64 * R * wk + 16 * t, *low = piece_at(2 * s + 1) + (8 * wr + g) * a.pitch + 64 * R * wk + 16 * t;
             float c[4] = {0.f, 0.f, 0.f, 0.f};  // c[0], c[1]: row g, columns 2t, 2t + 1; c[2], c[3]: row g + 8
@@ -263,7 +265,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncthreads();
-            if (round + a.stages < rounds) fetch(round + a.stages, s);
+            if (round + a.stages < rounds) {
+                if (lost_by(lost_at, round)) {
+                    drain_ahead(bars, parity, s, round, rounds, a.stages);
+                    break;
+                }
+                fetch(round + a.stages, s);
+            }
             // The tiles' sums over their warps, 16 rows of 8 columns each; four warps a tile, others each round.
             for (int i = (tid + 128 * round) & (kThreads - 1); i < 128 * tiles_at_once; i += kThreads) {
                 const int row = round * 16 * tiles_at_once + i / 8, col = i & 7;
@@ -274,15 +282,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
                     for (int w = 0; w < a.warps_k; w++) v += of[w * 256];  // 128 sums on: four rows of the table
                     if (a.keep) {
                         if (k0 > k_first) v += row_sums[row * 8 + col];
-                        row_sums[row * 8 + col] = lost ? CUDART_NAN_F : v;
+                        row_sums[row * 8 + col] = v;
                     }
-                    if (a.slices == 1 && k0 + a.chunk >= k_end) static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(lost ? CUDART_NAN_F : v);
+                    if (a.slices == 1 && k0 + a.chunk >= k_end) static_cast<T *>(a.y)[(i0 + col) * a.y_row + r0 + row] = from_f32<T>(v);
                 }
             }
             turn ^= 1;  // the next round's sums go to the other half
             s = s + 1 == a.stages ? 0 : s + 1;
         }
-        if (k0 + a.chunk < k_end) __syncthreads();  // the sums of this pass, before the next one's
+        if (k0 + a.chunk < k_end && __syncthreads_or(get_word(lost_at))) break;  // (a barrier: the sums of this pass, before the next one's)
+    }
+    if (get_word(lost_at)) {  // all of the block's results are NaN
+        drain_lost(bars, parity, a.stages);
+        __syncthreads();  // behind what it has stored
+        if (tid == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
+        for (int i = tid; i < 8 * rows; i += kThreads) {
+            if (a.slices > 1) row_sums[i] = CUDART_NAN_F;
+            else if ((i & 7) < nb) static_cast<T *>(a.y)[(i0 + (i & 7)) * a.y_row + r0 + i / 8] = from_f32<T>(CUDART_NAN_F);
+        }
     }
     if (a.slices > 1) {  // each block adds its share of the rows over the cluster
         cluster_barrier();
@@ -299,7 +316,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec(const __grid_constant__ 
         }
         cluster_barrier();
     }
-    if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
 }
 
 // Whether a block's own shared memory begins where kBelowRoom takes it to: asked once a device.
@@ -436,6 +452,8 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
 int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
                  const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
                  int64_t k, int32_t group, void *y, int64_t y_row, int32_t *status, ecasq_stream_t stream) {
+    const bool lost_wait = (type & ECASQ_TEST_LOST_WAIT) != 0;
+    type &= ~ECASQ_TEST_LOST_WAIT;
     if (n < 1 || k < 1 || b < 0 || n >= (int64_t)1 << 31 || k >= (int64_t)1 << 31 || b > 8 * 65535 || m < 1 || m > 16 ||
         !type_ok(type) || (scale_type != type && scale_type != ECASQ_F32) || group < 32 || group % 32)
         return ECASQ_EINVAL;
@@ -459,6 +477,7 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
     a.b = (int32_t)b;
     a.m = m;
     a.groups = (int32_t)cdiv(k, group);
+    a.lost = lost_wait;
     const FastDiv div(group / 32);
     a.div_mul = div.mul;
     a.div_shift = div.shift;

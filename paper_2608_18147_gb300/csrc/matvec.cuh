@@ -26,6 +26,7 @@ struct MatvecArgs {
     int32_t stages;               // stages of the codes' ring
     int32_t pitch, scale_pitch;   // 16-bit types: bytes from one row to the next in a stage, and among the scales
     int32_t pieces_below;         // 16-bit types: halves of stages that lie below the table
+    uint32_t lost;                // test hook: 1 where blocks begin as if a wait had run out
     uint32_t div_mul, div_shift;  // words of 32 columns to scale groups: w div (group / 32), as umulhi(w, div_mul) >> div_shift
                                   // or w >> div_shift if div_mul is 0
 };
@@ -51,6 +52,29 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
         if (done) return true;
     }
     return false;
+}
+// Waits that run out.  A word of shared memory holds 0, or 1 more than the round of the pass in which a wait ran out: written
+// before the round's barrier, read behind it.  (A thread that is a round ahead may have written already; `round` tells.)
+__device__ __forceinline__ void set_word(uint32_t at, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ uint32_t get_word(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ bool lost_by(uint32_t at, int round) { return get_word(at) - 1 <= (uint32_t)round; }
+// Before a block whose wait ran out ends, it waits, with the limit again, for the copies that are still on their way, so that none writes
+// to its shared memory when that is another's.  Bit s of `parity` is that of the next wait for stage s.  Those of the rounds
+// after `round`, which has stage s, that were asked for:
+__device__ __forceinline__ void drain_ahead(uint32_t bars, uint32_t &parity, int s, int round, int rounds, int stages) {
+    for (int i = 1; i < stages && round + i < rounds; i++) {
+        s = s + 1 == stages ? 0 : s + 1;
+        bar_wait(bars + 8 * s, parity >> s & 1);
+        parity ^= 1u << s;
+    }
+}
+// and those of every stage that have been waited for.
+__device__ __forceinline__ void drain_lost(uint32_t bars, uint32_t parity, int stages) {
+    for (int s = 0; s < stages; s++) bar_wait(bars + 8 * s, ~parity >> s & 1);
 }
 
 // The scale group of word w (32 columns each).

@@ -14,7 +14,7 @@
 
 namespace ecasq {
 
-constexpr int kMostStages = 4, kTableBytes = 256 * 128, kSumBytes = 2 * kWarps * 16 * 8 * 4, kBarBytes = 64;
+constexpr int kMostStages = 4, kTableBytes = 256 * 128, kSumBytes = 2 * kWarps * 16 * 8 * 4, kBarBytes = 64, kLostAt = 8 * kMostStages;
 constexpr int kRowPad = 64;  // a row's room in a stage is its bytes and this: two rows' reads do not meet in a bank
 
 // Entry `byte J of w` of the table of pairs; l: the address of the lane's copy of entry 0.
@@ -94,15 +94,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
     const float *scales = static_cast<const float *>(a.scales) + r0 * a.scale_row;
 
     wait_before();
-    if (tid == 0)
+    const uint32_t lost_at = bars + kLostAt;
+    if (tid == 0) {
         for (int s = 0; s < a.stages; s++) bar_init(bars + 8 * s);
+        set_word(lost_at, a.lost);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
 
     uint32_t parity = 0;  // of the stages' next waits, a bit each
-    bool lost = false;    // a wait ran out
+    bool lost = false;    // a wait of the block ran out
     int turn = 0;
-    for (int64_t k0 = 0; k0 < a.k; k0 += a.chunk) {
+    for (int64_t k0 = 0; k0 < a.k && !lost; k0 += a.chunk) {
         const int cols = (int)min((int64_t)a.chunk, a.k - k0), blocks = (cols + 127) / 128;
         if (k0) __syncthreads();
         auto fetch = [&](int round, int s) {
@@ -139,7 +142,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
         __syncthreads();
 
         for (int round = 0, s = 0; round < rounds; round++) {
-            if (!bar_wait(bars + 8 * s, parity >> s & 1)) lost = true;
+            if (!bar_wait(bars + 8 * s, parity >> s & 1)) set_word(lost_at, round + 1);
             parity ^= 1u << s;
             const char *tile = ring + s * stage_bytes + (16 * wr + g) * pitch + 16 * t;
             Sums acc;
@@ -165,6 +168,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
             *reinterpret_cast<float2 *>(mine) = make_float2(acc.c[0], acc.c[1]);
             *reinterpret_cast<float2 *>(mine + 64) = make_float2(acc.c[2], acc.c[3]);
             __syncthreads();
+            lost = lost_by(lost_at, round);
+            if (lost) {
+                drain_ahead(bars, parity, s, round, rounds, a.stages);
+                break;
+            }
             if (round + a.stages < rounds) fetch(round + a.stages, s);
             // The tiles' sums over their warps: 16 rows of 8 columns each.
             for (int i = tid; i < 128 * tiles; i += kThreads) {
@@ -177,14 +185,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
                         if (k0) v += row_sums[at * 8 + col];
                         row_sums[at * 8 + col] = v;
                     }
-                    if (k0 + a.chunk >= a.k) static_cast<float *>(a.y)[(i0 + col) * a.y_row + r0 + at] = lost ? CUDART_NAN_F : v;
+                    if (k0 + a.chunk >= a.k) static_cast<float *>(a.y)[(i0 + col) * a.y_row + r0 + at] = v;
                 }
             }
             turn ^= 1;  // the next round's sums go to the other half: one barrier a round
             s = s + 1 == a.stages ? 0 : s + 1;
         }
     }
-    if (lost && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
+    if (lost) {  // all of the block's results are NaN
+        drain_lost(bars, parity, a.stages);
+        __syncthreads();  // behind what it has stored
+        if (tid == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
+        for (int i = tid; i < 8 * rows; i += kThreads)
+            if ((i & 7) < nb) static_cast<float *>(a.y)[(i0 + (i & 7)) * a.y_row + r0 + i / 8] = CUDART_NAN_F;
+    }
 }
 
 int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st) {

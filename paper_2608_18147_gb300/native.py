@@ -24,6 +24,7 @@ ONE_PART_PUBLISH = 128  # accepted, without effect
 UNSEEDED_SEARCH = 256  # fast DP search: no seeded tile skipping (same results)
 TEST_STALL = 1 << 30  # test hook of the bounded waits (include/ecasq.h)
 TEST_SHORT_PARTS = 1 << 28  # test hook: far segments of the fast DP in parts of three tiles (same results)
+TEST_LOST_WAIT = 1 << 30  # test hook of ecasq_matvec, in its `type`: blocks go on as if a wait of their first round had run out
 TEST_SELF_SEED = 1 << 29  # test hook: a fixed-multiplier pass seeded with its own fp32 minima (same results)
 
 _lock = threading.Lock()
