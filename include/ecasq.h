@@ -499,7 +499,8 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
  *   max_len  host bound of the lengths; sizes the launch and the workspace
  *   lse      device fp32 [b, heads] or NULL
  * Workspace: ecasq_workspace_size_attend with the same sizes (0 bytes may be returned: ws
- * may then be NULL); it needs no preparation.  How a sequence's sums are cut depends on its own
+ * may then be NULL); it needs no preparation.  The size never falls as b, heads or max_len grows (kv_heads and d the
+ * same), so one made for the largest serves all smaller calls.  How a sequence's sums are cut depends on its own
  * range and on the call's sizes alone, and equal calls give equal bits.
  *   status   ECASQ_BAD_PAGE, ECASQ_BAD_LENGTH
  * ECASQ_EINVAL for b outside [0, 65535], max_len outside [0, 2^30], heads not a multiple

@@ -46,12 +46,15 @@ static Splits make_splits(int64_t b, int64_t blocks, int64_t span, int64_t slots
     }
     return best;
 }
-// Bytes of the splits' results, for the most splits that make_splits may choose.  (Splits count from the tile of the first
-// key, so with a start one more tile may be needed.)
-static size_t part_bytes(int64_t b, int64_t heads, int64_t blocks, int32_t d, int64_t max_len) {
-    const int64_t all = std::max<int64_t>(1, b * blocks), most = std::max<int64_t>(1, (int64_t)kSms * kMostResident * kMostRounds / all);
-    const int64_t splits = std::min(most, cdiv(max_len + kMostTile - 1, kLeastStep));
-    return splits > 1 ? (size_t)(b * heads * splits * PartAt(d).stride) * 4 : 0;
+// Bytes of the splits' results: room for the most splits that make_splits may choose with as many sequences or with fewer, with
+// keys and heads likewise, so that a workspace made for the largest sizes serves all smaller ones.  Where a sequence
+// has several splits its blocks are b kv_heads ceil(group / kHeads) and all splits together no more than kMostParts blocks, each with a result for
+// min(group, kHeads) heads at most; and a sequence has no more splits than its keys fill.  (Splits count from the tile
+// of the first key, so with a start one more tile may be needed.)
+constexpr int64_t kMostParts = (int64_t)kSms * kMostResident * kMostRounds;
+static size_t part_bytes(int64_t b, int64_t heads, int64_t kv_heads, int32_t d, int64_t max_len) {
+    const int64_t splits = cdiv(max_len + kMostTile - 1, kLeastStep);
+    return splits > 1 ? (size_t)(std::min(b * heads * splits, kMostParts * std::min<int64_t>(heads / kv_heads, kHeads)) * PartAt(d).stride) * 4 : 0;
 }
 
 int split_attend(AttendArgs &a, int64_t b, int resident) {
@@ -61,7 +64,7 @@ int split_attend(AttendArgs &a, int64_t b, int resident) {
     a.splits = s.count;
     a.cluster = s.cluster;
     if (a.splits == 1) return ECASQ_OK;
-    if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, blocks, a.d, a.max_len)) return ECASQ_EWORKSPACE;
+    if (!a.ws || (reinterpret_cast<uintptr_t>(a.ws) & 255) || a.ws_bytes < part_bytes(b, a.heads, a.heads / a.group, a.d, a.max_len)) return ECASQ_EWORKSPACE;
     a.part = static_cast<float *>(a.ws);
     return ECASQ_OK;
 }
@@ -191,7 +194,7 @@ extern "C" {
 
 size_t ecasq_workspace_size_attend(int64_t b, int32_t heads, int32_t kv_heads, int32_t d, int64_t max_len) {
     if (!sizes_ok(b, heads, kv_heads, d, max_len)) return 0;
-    return part_bytes(b, heads, (int64_t)kv_heads * cdiv(heads / kv_heads, kHeads), d, max_len);
+    return part_bytes(b, heads, kv_heads, d, max_len);
 }
 
 int ecasq_attend(const void *q, int64_t q_row, int64_t q_head, int64_t b, int32_t heads, const ecasq_cache_t *k,

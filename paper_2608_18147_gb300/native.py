@@ -724,7 +724,7 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
 
 
 def workspace_attend(b, heads, kv_heads, d, max_len):
-    """A device workspace for ecasq_attend with these sizes (it may be empty)."""
+    """A device workspace for ecasq_attend with these sizes or smaller ones, kv_heads and d the same (it may be empty)."""
     torch = _torch()
     n = int(lib().ecasq_workspace_size_attend(int(b), int(heads), int(kv_heads), int(d), int(max_len)))
     return torch.empty(n, dtype=torch.uint8, device="cuda")
