@@ -3,12 +3,14 @@
 Each translation unit under csrc/ is compiled in parallel, then linked into
 paper_2608_18147_gb300/_build/libecasq.so with the CUDA runtime linked
 statically.  csrc/binding.c becomes a Python extension beside it (the C
-compiler and Python's headers).
+compiler and Python's headers), which the operators on 4-bit codes alone need:
+build_binding() makes it, at their first call if not before.
 """
 from __future__ import annotations
 
 import glob
 import os
+import shlex
 import subprocess
 import sys
 import sysconfig
@@ -45,14 +47,17 @@ def _stale() -> bool:
 
 def build_binding(force: bool = False) -> str:
     """The Python extension of csrc/binding.c; its path."""
-    header = os.path.join(HERE, "..", "include", "ecasq.h")
-    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(map(os.path.getmtime, (BINDING_SRC, header))):
+    deps = [p for p in (BINDING_SRC, os.path.join(HERE, "..", "include", "ecasq.h")) if os.path.exists(p)]
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) >= os.path.getmtime(p) for p in deps):
         return BINDING
     os.makedirs(OUT, exist_ok=True)
     tmp = BINDING + ".%d.tmp" % os.getpid()
-    cmd = [os.environ.get("CC", "gcc"), "-std=c11", "-O2", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], BINDING_SRC,
-           "-o", tmp]
-    done = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    cmd = shlex.split(os.environ.get("CC") or "gcc") + ["-std=c11", "-O2", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"],
+                                                        BINDING_SRC, "-o", tmp]
+    try:
+        done = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    except OSError as e:
+        raise RuntimeError("%s: %s" % (cmd[0], e)) from e
     if done.returncode != 0:
         raise RuntimeError("%s failed:\n%s" % (cmd[0], done.stdout.decode(errors="replace")))
     os.replace(tmp, BINDING)
@@ -60,7 +65,6 @@ def build_binding(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    build_binding(force)
     if not force and not _stale():
         return LIB
     os.makedirs(OUT, exist_ok=True)
@@ -91,3 +95,4 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose=True))
+    print(build_binding(force="--force" in sys.argv))
