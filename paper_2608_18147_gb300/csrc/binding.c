@@ -22,11 +22,11 @@ typedef int (*attend_fn)(const void *, int64_t, int64_t, int64_t, int32_t, const
 static matvec_fn call_matvec;
 static write_fn call_write;
 static attend_fn call_attend;
-static PyObject *tensor_type, *empty, *current_device, *raw_stream, *make_workspace;
+static PyObject *tensor_type, *empty, *current_device, *raw_stream, *make_workspace, *grad_enabled, *forward_ad;
 /* torch's dtypes, in the order of the names below; the first three are ECASQ_F32, ECASQ_F16, ECASQ_BF16 */
 enum { U8 = 3, I32 = 4, I64 = 5, DTYPES = 6 };
 static PyObject *dtypes[DTYPES];
-static PyObject *s_dtype, *s_device, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *empty_kw;
+static PyObject *s_dtype, *s_device, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_requires_grad, *s_level, *s_unpack, *empty_kw;
 
 typedef struct {
     PyObject *o;
@@ -127,6 +127,31 @@ static int status_of(PyObject *o, long device, int32_t **to) {
     return 1;
 }
 
+/* Whether a gradient or a tangent of one of the given tensors (NULL and None allowed) is asked for, which these calls do not give. */
+static int tracked(PyObject *const *o, int n) {
+    PyObject *on = PyObject_CallNoArgs(grad_enabled), *level = PyObject_GetAttr(forward_ad, s_level);
+    int found = !on;
+    const int dual = level && PyLong_AsLong(level) >= 0;
+    PyErr_Clear();
+    for (int i = 0; i < n && !found; i++) {
+        if (!o[i] || o[i] == Py_None) continue;
+        if (on == Py_True) {
+            PyObject *wants = PyObject_GetAttr(o[i], s_requires_grad);
+            found = wants != Py_False;
+            Py_XDECREF(wants);
+        }
+        if (dual && !found) {
+            PyObject *pair = PyObject_CallMethodOneArg(forward_ad, s_unpack, o[i]);
+            found = !pair || !PyTuple_Check(pair) || PyTuple_GET_SIZE(pair) != 2 || PyTuple_GET_ITEM(pair, 1) != Py_None;
+            Py_XDECREF(pair);
+        }
+    }
+    Py_XDECREF(on);
+    Py_XDECREF(level);
+    PyErr_Clear();
+    return found;
+}
+
 #define NO Py_RETURN_NONE
 
 /* matvec(x, codes, levels, scales, group, out, status) */
@@ -148,6 +173,8 @@ static PyObject *py_matvec(PyObject *self, PyObject *const *v, Py_ssize_t n_args
     if ((k > 1 && x.step[x.nd - 1] != 1) || codes.step[1] != 1 || codes.n[1] < (k + 127) / 128 * 64 || levels.n[0] < 1 || levels.n[0] > 16 ||
         !contiguous(&levels) || scales.n[0] != n || scales.n[1] < groups || (scales.n[1] > 1 && scales.step[1] != 1))
         NO;
+    PyObject *const floats[] = {v[0], v[2], v[3], v[5]};
+    if (tracked(floats, 4)) NO;
     if (codes.device != x.device || levels.device != x.device || scales.device != x.device || !status_of(v[6], x.device, &status) ||
         !stream_of(x.device, &stream))
         NO;
@@ -214,6 +241,8 @@ static PyObject *py_write(PyObject *self, PyObject *const *v, Py_ssize_t n_args)
         NO;
     m.at = NULL;
     if (v[2] != Py_None && (!look(v[2], &m) || m.type != I32 || m.count != rows || !contiguous(&m) || m.device != x.device)) NO;
+    PyObject *const floats[] = {v[0], v[1], v[5]};
+    if (tracked(floats, 3)) NO;
     if (!status_of(v[7], x.device, &status) || !stream_of(x.device, &stream)) NO;
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -243,6 +272,8 @@ static PyObject *py_attend(PyObject *self, PyObject *const *v, Py_ssize_t n_args
         PyErr_Clear();
         NO;
     }
+    PyObject *const floats[] = {v[0], v[1], v[2], v[7], v[8], v[10]};
+    if (tracked(floats, 6)) NO;
     if (max_len < 0 || max_len > most || !status_of(v[12], q.device, &status) || !stream_of(q.device, &stream)) NO;
     if (!(made = v[10] == Py_None ? new_tensor(3, q.n, q.type, &q) : Py_NewRef(v[10]))) goto done;
     if (!look(made, &out) || out.type != q.type || out.nd != 3 || out.n[0] != b || out.n[1] != heads || out.n[2] != q.n[2] || out.step[2] != 1 || out.device != q.device) {
@@ -275,11 +306,12 @@ done:
     return both;
 }
 
-/* setup(addresses of matvec, cache_write, attend, torch.Tensor, torch.empty, current device, raw stream, workspace, dtypes) */
+/* setup(addresses of matvec, cache_write, attend, torch.Tensor, torch.empty, current device, raw stream, workspace,
+ * torch.is_grad_enabled, torch.autograd.forward_ad, dtypes) */
 static PyObject *py_setup(PyObject *self, PyObject *args) {
     unsigned long long a[3];
-    PyObject *o[5], *types;
-    if (!PyArg_ParseTuple(args, "KKKOOOOOO!", &a[0], &a[1], &a[2], &o[0], &o[1], &o[2], &o[3], &o[4], &PyTuple_Type, &types)) return NULL;
+    PyObject *o[7], *types;
+    if (!PyArg_ParseTuple(args, "KKKOOOOOOOO!", &a[0], &a[1], &a[2], &o[0], &o[1], &o[2], &o[3], &o[4], &o[5], &o[6], &PyTuple_Type, &types)) return NULL;
     if (PyTuple_GET_SIZE(types) != DTYPES || !PyType_Check(o[0])) {
         PyErr_SetString(PyExc_TypeError, "setup: six dtypes and a tensor type");
         return NULL;
@@ -287,8 +319,8 @@ static PyObject *py_setup(PyObject *self, PyObject *args) {
     call_matvec = (matvec_fn)(uintptr_t)a[0];
     call_write = (write_fn)(uintptr_t)a[1];
     call_attend = (attend_fn)(uintptr_t)a[2];
-    PyObject **to[5] = {&tensor_type, &empty, &current_device, &raw_stream, &make_workspace};
-    for (int i = 0; i < 5; i++) Py_XSETREF(*to[i], Py_NewRef(o[i]));
+    PyObject **to[7] = {&tensor_type, &empty, &current_device, &raw_stream, &make_workspace, &grad_enabled, &forward_ad};
+    for (int i = 0; i < 7; i++) Py_XSETREF(*to[i], Py_NewRef(o[i]));
     for (int i = 0; i < DTYPES; i++) Py_XSETREF(dtypes[i], Py_NewRef(PyTuple_GET_ITEM(types, i)));
     Py_RETURN_NONE;
 }
@@ -301,9 +333,9 @@ static PyMethodDef methods[] = {{"setup", py_setup, METH_VARARGS, NULL},
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_codes", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__codes(void) {
-    PyObject **names[] = {&s_dtype, &s_device, &s_shape, &s_stride, &s_data_ptr, &s_get_device};
-    const char *text[] = {"dtype", "device", "shape", "stride", "data_ptr", "get_device"};
-    for (int i = 0; i < 6; i++)
+    PyObject **names[] = {&s_dtype, &s_device, &s_shape, &s_stride, &s_data_ptr, &s_get_device, &s_requires_grad, &s_level, &s_unpack};
+    const char *text[] = {"dtype", "device", "shape", "stride", "data_ptr", "get_device", "requires_grad", "_current_level", "unpack_dual"};
+    for (int i = 0; i < 9; i++)
         if (!(*names[i] = PyUnicode_InternFromString(text[i]))) return NULL;
     if (!(empty_kw = PyTuple_Pack(2, s_dtype, s_device))) return NULL;
     return PyModule_Create(&module);

@@ -566,6 +566,7 @@ def ecasq_prepare(x, ws=None):
 #
 # These calls are short, so what is in front of them is C too (csrc/binding.c, built beside the library): it looks at the
 # tensors and calls the C entry point.  What it does not take comes back as None, and is looked at here once more to say why.
+# They serve: none has a gradient, and tensors that want one are refused.
 
 _TYPES = {}
 _codes = None
@@ -588,6 +589,7 @@ def _ready():
             address = lambda fn: C.cast(fn, C.c_void_p).value  # noqa: E731
             module.setup(address(L.ecasq_matvec), address(L.ecasq_cache_write), address(L.ecasq_attend), torch.Tensor, torch.empty,
                          torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, workspace_attend,
+                         torch.is_grad_enabled, torch.autograd.forward_ad,
                          (torch.float32, torch.float16, torch.bfloat16, torch.uint8, torch.int32, torch.int64))
             _codes = module
     return _codes
@@ -618,6 +620,15 @@ def _here(where, *tensors):
         _refuse(where, "tensors must be on the current CUDA device")
 
 
+def _no_gradients(where, *tensors):
+    """These operators serve: a tensor (None allowed) whose gradient or tangent is asked for is refused."""
+    torch = _torch()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and ((torch.is_grad_enabled() and t.requires_grad)
+                                            or torch.autograd.forward_ad.unpack_dual(t).tangent is not None):
+            _refuse(where, "no gradients: call it under torch.no_grad() or with detached tensors")
+
+
 def ecasq_pack(idx):
     """Indices [n, k] (uint8, < 16) of a weight matrix as the packed rows that ecasq_matvec reads: uint8
     [n, 64 ceil(k / 128)]."""
@@ -637,6 +648,7 @@ def ecasq_pack(idx):
 def _matvec_refused(torch, x, codes, levels, scales, group, out, status):
     where = "ecasq_matvec"
     _here(where, x, codes, levels, scales, out)
+    _no_gradients(where, x, levels, scales, out)
     k = lambda: x.shape[-1]  # noqa: E731
     _need(where,
           (lambda: x.dtype in _TYPES and x.dim() in (1, 2) and (k() < 2 or x.stride(-1) == 1),
@@ -661,7 +673,8 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
 
     x [b, k] or [k] (float32, float16 or bfloat16), codes [n, 64 ceil(k / 128)] as ecasq_pack gives them,
     levels [m <= 16] of x's type, scales [n, ceil(k / group)] of x's type or float32, group a multiple of 32.
-    status: int32 tensor that BAD_* bits are or-ed into.  Returns y [b, n] or [n] of x's type (`out` if given)."""
+    status: int32 tensor that BAD_* bits are or-ed into.  Returns y [b, n] or [n] of x's type (`out` if given).
+    No gradients: a tensor that requires one is refused while they are recorded."""
     y = (_codes or _ready()).matvec(x, codes, levels, scales, group, out, status)
     if y is None:
         _matvec_refused(_torch(), x, codes, levels, scales, group, out, status)
@@ -693,6 +706,7 @@ _CACHE_IS = ("a cache is [pages, page_size, heads, d] of float32, float16 or bfl
 def _write_refused(torch, x, Q, m, slots, codes, levels, status):
     where = "ecasq_cache_write"
     _here(where, x, Q, m, slots, codes, levels)
+    _no_gradients(where, x, Q, levels)
     rows = lambda: slots.numel() * codes.shape[2]  # noqa: E731
     _need(where,
           (lambda: levels is not None and _cache_type(codes, levels)[0] is not None, _CACHE_IS),
@@ -714,7 +728,8 @@ def ecasq_cache_write(x, Q, m, slots, codes, levels, seed, status=None):
     Q float32 [n * heads, s] or [n, heads, s] and m int32 [n * heads] (or None) as ecasq_solve_batched gives them,
     slots int64 [n] (page * page_size + slot, negative: not written), codes uint8 [pages, page_size, heads, d / 2],
     levels [pages, page_size, heads, 8 or 16] of float16 or bfloat16; x float32 or of levels' type.  status: int32
-    tensor that BAD_* bits are or-ed into.  Returns (codes, levels), written in place."""
+    tensor that BAD_* bits are or-ed into.  Returns (codes, levels), written in place.
+    No gradients: a tensor that requires one is refused while they are recorded."""
     rc = (_codes or _ready()).cache_write(x, Q, m, slots, codes, levels, seed, status)
     if rc is None:
         _write_refused(_torch(), x, Q, m, slots, codes, levels, status)
@@ -733,6 +748,7 @@ def workspace_attend(b, heads, kv_heads, d, max_len):
 def _attend_refused(torch, q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws, status):
     where = "ecasq_attend"
     _here(where, q, k, v, table, lengths, starts, k_levels, v_levels, out, ws)
+    _no_gradients(where, q, k, v, k_levels, v_levels, out)
     row = lambda t: t.dtype == torch.int32 and t.shape == q.shape[:1] and t.is_contiguous()  # noqa: E731
     _need(where,
           (lambda: (k_levels is None) == (v_levels is None), "k and v must both be plain or both be coded"),
@@ -759,7 +775,8 @@ def ecasq_attend(q, k, v, table, lengths, scale=None, starts=None, k_levels=None
     [..., 8 or 16] of q's type; table int32 [b, pages of a sequence]; lengths int32 [b], starts int32 [b] or None: the
     keys [starts, lengths) are seen.  scale: 1 / sqrt(d) if None.  max_len: host bound of the lengths (None: what the table
     holds).  status: int32 tensor that BAD_* bits are or-ed into.  out [b, heads, d] of q's type, lse float32 [b, heads]
-    (natural logarithm; -inf where no key is seen, with out = 0)."""
+    (natural logarithm; -inf where no key is seen, with out = 0).  No gradients: a tensor that requires one is refused while they are
+    recorded."""
     both = (_codes or _ready()).attend(q, k, v, table, lengths, scale, starts, k_levels, v_levels, max_len, out, ws, status)
     if both is None:
         _attend_refused(_torch(), q, k, v, table, lengths, starts, k_levels, v_levels, max_len, out, ws, status)
