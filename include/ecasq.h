@@ -489,7 +489,9 @@ int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, i
  * lse = -inf, and so does one whose weights are all zero.  Scores, sums and the weights of lse are
  * fp32; the weights of out are too for F32, and have 16 bits for BF16 and F16 (for F16 in steps of no less
  * than 2^-40 of the largest weight); out is rounded once, to q's type.  Nothing outside that range is read, whatever it holds.
- * Values are finite: an infinity among those seen may give NaN where the sum is infinite.
+ * Values and levels are finite.  Where one among those seen is not, the entry of out that it enters is not finite either (it may
+ * be NaN where the sum is infinite), and for F16 and BF16 its neighbour in the pair 2i, 2i + 1 may be NaN; other
+ * entries, key heads and sequences do not change.  A key that is NaN makes all of its heads' out and lse NaN.
  *   q        device [b, heads, d] of the cache's type, strides in elements, entries
  *            contiguous; out likewise
  *   k, v     host structs of one type, kind, d, heads, pages and page_size
