@@ -26,7 +26,7 @@ static PyObject *tensor_type, *empty, *current_device, *raw_stream, *make_worksp
 /* torch's dtypes, in the order of the names below; the first three are ECASQ_F32, ECASQ_F16, ECASQ_BF16 */
 enum { U8 = 3, I32 = 4, I64 = 5, DTYPES = 6 };
 static PyObject *dtypes[DTYPES];
-static PyObject *s_dtype, *s_device, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_requires_grad, *s_level, *s_unpack, *empty_kw;
+static PyObject *s_dtype, *s_device, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_numel, *s_requires_grad, *s_level, *s_unpack, *empty_kw;
 
 typedef struct {
     PyObject *o;
@@ -117,14 +117,25 @@ static PyObject *new_tensor(int nd, const int64_t *n, int type, const Tensor *li
     return made;
 }
 
-/* A status word: None, or an int32 tensor on the device. */
+/* A status word: None, or the first element of an int32 tensor of any shape on the device. */
 static int status_of(PyObject *o, long device, int32_t **to) {
-    Tensor t;
+    PyObject *dtype, *count = NULL, *at = NULL, *where = NULL;
+    int ok = 0;
     *to = NULL;
     if (o == Py_None) return 1;
-    if (!look(o, &t) || t.type != I32 || t.count < 1 || t.device != device) return 0;
-    *to = (int32_t *)t.at;
-    return 1;
+    if (!PyObject_TypeCheck(o, (PyTypeObject *)tensor_type)) return 0;
+    if ((dtype = PyObject_GetAttr(o, s_dtype)) == dtypes[I32] && (count = PyObject_CallMethodNoArgs(o, s_numel)) &&
+        (where = PyObject_CallMethodNoArgs(o, s_get_device)) && (at = PyObject_CallMethodNoArgs(o, s_data_ptr))) {
+        ok = PyLong_AsLongLong(count) > 0 && PyLong_AsLong(where) == device;
+        *to = (int32_t *)PyLong_AsVoidPtr(at);
+        ok = ok && !PyErr_Occurred();
+    }
+    if (!ok) PyErr_Clear();
+    Py_XDECREF(dtype);
+    Py_XDECREF(count);
+    Py_XDECREF(where);
+    Py_XDECREF(at);
+    return ok;
 }
 
 /* Whether a gradient or a tangent of one of the given tensors (NULL and None allowed) is asked for, which these calls do not give. */
@@ -333,9 +344,9 @@ static PyMethodDef methods[] = {{"setup", py_setup, METH_VARARGS, NULL},
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_codes", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__codes(void) {
-    PyObject **names[] = {&s_dtype, &s_device, &s_shape, &s_stride, &s_data_ptr, &s_get_device, &s_requires_grad, &s_level, &s_unpack};
-    const char *text[] = {"dtype", "device", "shape", "stride", "data_ptr", "get_device", "requires_grad", "_current_level", "unpack_dual"};
-    for (int i = 0; i < 9; i++)
+    PyObject **names[] = {&s_dtype, &s_device, &s_shape, &s_stride, &s_data_ptr, &s_get_device, &s_numel, &s_requires_grad, &s_level, &s_unpack};
+    const char *text[] = {"dtype", "device", "shape", "stride", "data_ptr", "get_device", "numel", "requires_grad", "_current_level", "unpack_dual"};
+    for (int i = 0; i < 10; i++)
         if (!(*names[i] = PyUnicode_InternFromString(text[i]))) return NULL;
     if (!(empty_kw = PyTuple_Pack(2, s_dtype, s_device))) return NULL;
     return PyModule_Create(&module);
