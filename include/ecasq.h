@@ -388,7 +388,8 @@ int ecasq_prepare(const float *x, int64_t d, void *ws, size_t ws_bytes, float *v
  * What reads and writes codes of at most 16 levels: products with a coded weight
  * matrix, attention over a paged key-value cache whose rows may be coded, and the
  * encode of new cache rows.  These calls neither synchronise nor use host memory
- * after they return, so a graph can capture them; device-side findings go to a
+ * after they return, so a graph can capture them (but not ecasq_solve_batched, which finds the codebooks of
+ * new cache rows and synchronises); device-side findings go to a
  * sticky status word of the caller's (`status`, one int32, may be NULL): bits of
  * ECASQ_BAD_* are or-ed into it and never cleared.
  * Element types: */
@@ -409,7 +410,7 @@ int ecasq_prepare(const float *x, int64_t d, void *ws, size_t ws_bytes, float *v
  * of the block with the lowest column in the lowest four bits; word w is stored as
  * word 4 (w mod 4) + w div 4 of the block.  Columns beyond k are zero.
  *   idx   device [n rows of idx_row bytes], codes device [n rows of code_row bytes]
- * ECASQ_EINVAL for n or k < 1, rows shorter than their contents, code_row not a
+ * ECASQ_EINVAL for n or k outside [1, 2^31), rows shorter than their contents, code_row not a
  * multiple of 16 or codes not 16-byte aligned. */
 int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_t *codes, int64_t code_row,
                ecasq_stream_t stream);
@@ -428,8 +429,8 @@ int ecasq_pack(const uint8_t *idx, int64_t idx_row, int64_t n, int64_t k, uint8_
  *   group   a multiple of 32; one >= k means one scale a row
  *   y       device [b rows of y_row elements], of `type`, output
  *   status  ECASQ_BAD_WAIT
- * ECASQ_EINVAL for n or k < 1, b < 0, m outside [1, 16], a bad type, group or
- * alignment.
+ * ECASQ_EINVAL for n or k outside [1, 2^31), b outside [0, 524280], m outside [1, 16], rows shorter than their contents (rows of x or y
+ * that overlap among them), a bad type, group or alignment.
  * Test hook: with ECASQ_TEST_LOST_WAIT or-ed into `type` each block goes on as if a wait of its first round
  * had run out.  Not for production use. */
 #define ECASQ_TEST_LOST_WAIT (1 << 30)
@@ -477,7 +478,7 @@ typedef struct ecasq_cache {
  *   m      device int32 [n * heads] or NULL (all s)
  *   slots  device int64 [n]: page * page_size + slot; negative: the row is not
  *          written.  Slots of one call are distinct.
- * ECASQ_EINVAL for a plain cache, s outside [1, levels_n], n < 0 or a bad type. */
+ * ECASQ_EINVAL for a plain cache, s outside [1, levels_n], n < 0, more than 2^33 rows or a bad type. */
 int ecasq_cache_write(const void *x, int32_t x_type, int64_t n, int64_t x_row, int64_t x_head, const float *Q,
                       int32_t s, const int32_t *m, const int64_t *slots, const ecasq_cache_t *cache, uint64_t seed,
                       int32_t *status, ecasq_stream_t stream);

@@ -9,10 +9,11 @@
 // shared memory that cp.async fills a few tiles ahead, without a barrier in the loop.  The sequence is cut into
 // splits (one block each, so that few sequences still fill the card); a block's warps join in shared memory,
 // and the splits in that of a cluster of blocks or, by k_attend_join, in memory.  Measured, both kernels: 32 sequences of up to 8192 bf16 keys of 128, eight heads a key
-// head, 95 us or 5.6 TB/s, 83 % of a copy's rate.  Coded rows are bound by the lookups, byte permutes on the integer
-// pipe, which is 57 to 61 % busy: 16 sequences of 32768 keys of 128 with eight levels 149 us (4.5 TB/s, 66 %), one of
-// 70001 keys of 256 with sixteen 52 us (1.7 TB/s).  Short sequences are bound by latency: lengths, page numbers, rows and
-// the join follow one another; one sequence of 1000 keys takes 6.0 us.
+// head, 94 us or 5.7 TB/s, 84 % of a copy's rate.  Over coded rows the integer pipe, whose byte permutes look the levels up, is the
+// fullest unit, but 56 to 60 % busy: twelve warps an SM are too few to fill it (shared memory holds three blocks of four; with sixteen
+// levels and rows of 256 registers hold no more either).  16 sequences of 32768 keys of 128 with eight levels 150 us (4.5 TB/s, 66 %), one of
+// 70001 keys of 256 with sixteen 53 us (1.7 TB/s).  Short sequences are bound by latency: lengths, page numbers, rows and
+// the join follow one another; one sequence of 1000 keys takes 6.1 us.
 //
 // 16-bit rows: S^T = K Q^T and O^T = V^T P^T on mma.m16n8k16 with the query heads as n, fp32 sums.  (One
 // token a sequence is a matrix-vector product for each key head; with eight columns there is nothing for the
@@ -32,8 +33,9 @@
 // (parts of the weight itself lose bits from 2^-9 on, and all of a weight below 2^-25, which is wrong where the heaviest key holds
 // small values).
 // Coded rows: a lane holds its row's codebook as planes of low and of high bytes; a byte permute with four
-// codes as its selector looks four entries up in eight levels at once, so that a pair of entries costs two lookups
-// and two permutes and no shared-memory access.
+// codes as its selector looks one byte of four entries up in eight levels at once, and two more pair the bytes of the four, so that
+// a pair of entries costs two permutes and no shared-memory access.  With sixteen levels the lookups of four entries are nine operations:
+// both halves of the levels, and a choice by the codes' fourth bits.
 // fp32 rows: fp32 products on the FMA pipe in the same frame.
 #pragma once
 

@@ -52,8 +52,8 @@ template <typename K> static inline int allow_smem(K *kernel, int bytes, std::at
 }
 
 // Launches a kernel whose first statement is wait_before(): its blocks may be placed while the kernel before it in the stream still
-// runs.  (In a row of calls: a product with 1024 x 1024 codes 3.3 us, and 3.9 launched after the kernel before it has ended;
-// attention over 64 sequences of 100 keys 9.8 and 10.2 us; 32 x 8 cache rows 2.3 and 2.7 us.)
+// runs.  (In a row of calls: a product with 1024 x 1024 codes 3.5 us, and 3.9 launched after the kernel before it has ended;
+// attention over 64 sequences of 100 keys 9.8 and 10.2 us; 32 x 8 cache rows 2.4 and 2.7 us.)
 template <typename... P, typename... A>
 static inline int launch_clusters(void (*kernel)(P...), dim3 grid, dim3 cluster, int threads, int smem, cudaStream_t st, A &&...args) {
     cudaLaunchAttribute attr[2];

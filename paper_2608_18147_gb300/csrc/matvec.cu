@@ -44,16 +44,16 @@ __global__ void __launch_bounds__(256) k_pack(const uint8_t *__restrict__ idx, i
 // a barrier a round joins the warps' sums and frees its stage.  The rows' scales come a round ahead too, by cp.async in the
 // 16-byte pieces that hold them (loads to registers are waited for together with the lookups: 39.6 against 36.8 us for 28672 x
 // 8192 by eight rows).  More columns than the warps cover take several passes, or two or four blocks of a cluster take a slice of
-// the columns each and add their sums over the cluster, which also fills the card where rows are few (393 x 15530 by two rows: 7.1 us
-// by clusters, 14.7 in passes of single blocks; 8192 x 28672 by eight: 41.7 and 51.2).
+// the columns each and add their sums over the cluster, which also fills the card where rows are few (393 x 15530 by two rows: 7.2 us
+// by clusters, 14.7 in passes of single blocks; 8192 x 28672 by eight: 41.5 and 51.2).
 //
 // A pair of weights is an operand register of mma.m16n8k16 as it stands, with the rows of x as its eight columns and
 // fp32 sums; the order of the columns within a product is free.  (With one to eight columns there is no reuse that a
-// larger tensor tile could draw on.)
+// larger tensor tile could draw on; more rows of x take a pass over the matrix for each eight, where there would be.)
 //
 // What bounds it: the codes' bytes in the end, and on the way there the latency of lookups and products at sixteen warps an
-// SM (issue slots 46 %, shared memory 46 %, DRAM 34 % busy with eight rows).  28672 x 8192 by eight rows of bf16 takes 35.6 us,
-// 3.5 TB/s; 8192 x 8192 by one row of fp16, groups of 64, 15.1 us, 2.4 TB/s; a small matrix 3.3 us: the launch, one memory latency
+// SM (issue slots 45 %, shared memory 46 %, DRAM 35 % busy with eight rows).  28672 x 8192 by eight rows of bf16 takes 35.5 us,
+// 3.5 TB/s; 8192 x 8192 by one row of fp16, groups of 64, 15.2 us, 2.4 TB/s; a small matrix 3.5 us: the launch, one memory latency
 // and the table.  The table is held once a lane, so that no two lanes meet in a bank; 32 lookups, 8 transactions for the codes
 // themselves and up to 8 for the scales stand, for each KB of codes, against the 44 clocks that memory needs for it.  Entry e of lane l lies at address
 // kTableAt + 256 e + 4 l: one byte permute puts the code byte between the lane's constant ones, and that is the address.

@@ -33,7 +33,7 @@ struct MatvecArgs {
 
 constexpr int kWarps = 16, kThreads = 32 * kWarps;  // a block is alone on its SM
 constexpr int kRowsMost = 512, kRowSumBytes = kRowsMost * 8 * 4;  // rows of a block; their sums where several passes add up
-constexpr int kSpins = 1 << 18;                     // of a wait, each of a microsecond or so
+constexpr int kSpins = 1 << 18;                     // of a wait, each of some microseconds: about two seconds
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar) { asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory"); }

@@ -5,9 +5,10 @@
 // holds those tiles' rows, brought in by one bulk copy a row a few stages ahead, and one barrier a stage joins the sums
 // and frees it.  The products are FMAs: a lane holds all eight columns for its share of k.
 //
-// What bounds it: shared memory and its latency at sixteen warps an SM.  The table of fp32 pairs is held once for each two lanes,
+// What bounds it: no unit is full (issue slots 41 %, shared memory 30 %); sixteen warps an SM wait in turn for their lookups, the scales
+// read from memory and the round's barrier.  The table of fp32 pairs is held once for each two lanes,
 // so a lookup takes two transactions where the 16-bit types need one, and each eight weights read x once for every row of
-// x.  8192 x 8192 by one row takes 28.9 us (1.2 TB/s), by eight 98 us; 2999 x 2050 by three 8.8 us.
+// x.  8192 x 8192 by one row takes 29.1 us (1.2 TB/s), by eight 99 us; 2999 x 2050 by three 8.9 us.
 #include <algorithm>
 
 #include "matvec.cuh"
