@@ -3,8 +3,9 @@
  * The other entry points synchronise, and their binding is ctypes.  These are launches of a few microseconds, so what is
  * in front of them has to be short too: here a call's tensors are looked at once (type, shape, strides, device, address), and the
  * C entry point is called.  (A ctypes binding with the same checks took 14, 22 and 9 us for a product, an attention and a cache
- * write; this takes 7 to 13, 11 to 15, with a join 14 to 20, and 5, by process and machine: equal programs differ that much.)  A call returns its result; None where the arguments are not what the entry
- * point takes (the caller says why); or the entry point's status.
+ * write; this takes 7 to 13, 11 to 15, with a join 14 to 20, and 5, by process and machine: equal programs differ that
+ * much.)  A call returns its result; None where the arguments are not what the entry point takes, or where a gradient is asked
+ * for (the caller says why); or the entry point's status.
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
