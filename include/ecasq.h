@@ -438,6 +438,55 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
                  const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
                  int64_t k, int32_t group, void *y, int64_t y_row, int32_t *status, ecasq_stream_t stream);
 
+/* A layer's products around one coded matrix, with what follows them:
+ *   ecasq_project  y[i, r] = act(p[i, r] + bias[r]) + residual[i, r]           for W [n, k]
+ *   ecasq_gated    y[i, r] = act(p[i, r]) p[i, n + r]                          for W [2n, k]: the gate's rows, then the other's
+ * with p = x W^T as in ecasq_matvec.  Sums, bias, activation and residual are fp32; y is rounded once, to x's type.
+ *   act     none; relu; silu v / (1 + e^-v); gelu v Phi(v), Phi the normal distribution's; gelu_tanh
+ *           v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2
+ *   bias    device [n] of `type`, or NULL
+ *   residual  device [b rows of residual_row elements] of `type`, or NULL; y may be the residual itself (same
+ *           address and rows), and overlaps nothing else that is read
+ *   the others as for ecasq_matvec (n < 2^30 for ecasq_gated)
+ * Workspace: ecasq_workspace_size_project with the same sizes, n the matrix's rows (0 bytes may be returned: ws may then be
+ * NULL); it needs no preparation, and one made for the largest b serves all smaller ones.
+ *   status  ECASQ_BAD_WAIT
+ * ECASQ_EINVAL as for ecasq_matvec, and for a bad activation. */
+#define ECASQ_ACT_NONE 0
+#define ECASQ_ACT_RELU 1
+#define ECASQ_ACT_SILU 2
+#define ECASQ_ACT_GELU 3
+#define ECASQ_ACT_GELU_TANH 4
+size_t ecasq_workspace_size_project(int64_t b, int64_t n, int64_t k, int32_t type);
+int ecasq_project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
+                  const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
+                  int64_t k, int32_t group, const void *bias, int32_t activation, const void *residual,
+                  int64_t residual_row, void *y, int64_t y_row, void *ws, size_t ws_bytes, int32_t *status,
+                  ecasq_stream_t stream);
+int ecasq_gated(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
+                const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
+                int64_t k, int32_t group, int32_t activation, void *y, int64_t y_row, void *ws, size_t ws_bytes,
+                int32_t *status, ecasq_stream_t stream);
+
+/* Root-mean-square norm of rows, with the residual's addition before it:
+ *   s = x + residual, rounded to `type` (x itself without a residual);
+ *   y = s / sqrt(mean(s^2) + eps) * weight
+ * in fp32, and then rounded to `type`, or coded to 8 bits: for each `group` columns of a row scale = max |y| / 448 (1 where
+ * that is 0) and e4m3 codes, y / scale rounded to nearest.  A group with a value that is not finite has a scale that is not, and
+ * unspecified codes.
+ *   x, residual (or NULL)  device [b rows of k], of `type`, row strides in elements
+ *   weight  device [k] of weight_type: `type` or ECASQ_F32
+ *   group   0: y is of `type`; else a multiple of 16, or >= k (one scale a row): y is e4m3, one byte an entry
+ *   y       device [b rows of y_row elements]
+ *   sum     device [b rows of sum_row elements] or NULL: where s goes; needs a residual
+ *   scales  device fp32 [b rows of scale_row], ceil(k / group) a row; read for group > 0 only
+ * y of `type` and sum may each be x or the residual itself (same address and rows); nothing else overlaps.
+ * ECASQ_EINVAL for b or k outside [0, 2^31) and [1, 2^31), rows shorter than their contents, eps negative or NaN, a bad type or
+ * group, a sum without a residual. */
+int ecasq_norm(const void *x, int64_t x_row, int32_t type, int64_t b, int64_t k, const void *residual,
+               int64_t residual_row, const void *weight, int32_t weight_type, float eps, int64_t group, void *y,
+               int64_t y_row, void *sum, int64_t sum_row, float *scales, int64_t scale_row, ecasq_stream_t stream);
+
 /* One side (the keys or the values) of a paged cache.  Slot t of a sequence is slot
  * t mod page_size of its page t div page_size; a page has a row of d values for each
  * head in each slot.  Plain rows (levels_n = 0) hold values of `type`.  Coded rows

@@ -20,12 +20,25 @@ typedef int (*attend_fn)(const void *, int64_t, int64_t, int64_t, int32_t, const
                          int64_t, const int32_t *, const int32_t *, int64_t, float, void *, int64_t, int64_t, float *, void *, size_t,
                          int32_t *, ecasq_stream_t);
 
+typedef int (*project_fn)(const void *, int64_t, int32_t, int64_t, const uint8_t *, int64_t, const void *, int32_t, const void *, int64_t, int32_t,
+                          int64_t, int64_t, int32_t, const void *, int32_t, const void *, int64_t, void *, int64_t, void *, size_t, int32_t *,
+                          ecasq_stream_t);
+typedef int (*gated_fn)(const void *, int64_t, int32_t, int64_t, const uint8_t *, int64_t, const void *, int32_t, const void *, int64_t, int32_t,
+                        int64_t, int64_t, int32_t, int32_t, void *, int64_t, void *, size_t, int32_t *, ecasq_stream_t);
+typedef size_t (*room_fn)(int64_t, int64_t, int64_t, int32_t);
+typedef int (*norm_fn)(const void *, int64_t, int32_t, int64_t, int64_t, const void *, int64_t, const void *, int32_t, float, int64_t, void *,
+                       int64_t, void *, int64_t, float *, int64_t, ecasq_stream_t);
+
 static matvec_fn call_matvec;
+static project_fn call_project;
+static gated_fn call_gated;
+static room_fn call_room;
+static norm_fn call_norm;
 static write_fn call_write;
 static attend_fn call_attend;
 static PyObject *tensor_type, *empty, *current_device, *raw_stream, *make_workspace, *grad_enabled, *forward_ad;
 /* torch's dtypes, in the order of the names below; the first three are ECASQ_F32, ECASQ_F16, ECASQ_BF16 */
-enum { U8 = 3, I32 = 4, I64 = 5, DTYPES = 6 };
+enum { U8 = 3, I32 = 4, I64 = 5, E4M3 = 6, DTYPES = 7 };
 static PyObject *dtypes[DTYPES];
 static PyObject *s_dtype, *s_device, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_numel, *s_requires_grad, *s_level, *s_unpack, *empty_kw;
 
@@ -166,49 +179,175 @@ static int tracked(PyObject *const *o, int n) {
 
 #define NO Py_RETURN_NONE
 
-/* matvec(x, codes, levels, scales, group, out, status) */
-static PyObject *py_matvec(PyObject *self, PyObject *const *v, Py_ssize_t n_args) {
-    Tensor x, codes, levels, scales, y;
-    int32_t *status;
-    ecasq_stream_t stream;
-    PyObject *made = NULL;
-    if (n_args != 7 || !look(v[0], &x) || !look(v[1], &codes) || !look(v[2], &levels) || !look(v[3], &scales)) NO;
+/* The operands of a product with a coded matrix: x [b, k] or [k], codes, levels, scales, group; `rows` of the matrix. */
+typedef struct {
+    Tensor x, codes, levels, scales;
+    int64_t k, rows, b;
+    int32_t group;
+} Product;
+
+static int product_of(PyObject *const *v, Product *p) {
+    if (!look(v[0], &p->x) || !look(v[1], &p->codes) || !look(v[2], &p->levels) || !look(v[3], &p->scales)) return 0;
+    const Tensor *x = &p->x, *codes = &p->codes, *levels = &p->levels, *scales = &p->scales;
     const long long group = PyLong_AsLongLong(v[4]);
     if (group == -1 && PyErr_Occurred()) {
         PyErr_Clear();
-        NO;
+        return 0;
     }
-    if (x.type < 0 || x.type > 2 || x.nd > 2 || codes.type != U8 || codes.nd != 2 || levels.type != x.type || levels.nd != 1 ||
-        scales.nd != 2 || (scales.type != x.type && scales.type != ECASQ_F32) || group < 32 || group % 32 || group > INT32_MAX / 2)
-        NO;
-    const int64_t k = x.n[x.nd - 1], n = codes.n[0], b = x.nd == 2 ? x.n[0] : 1, groups = (k + group - 1) / group;
-    if ((k > 1 && x.step[x.nd - 1] != 1) || codes.step[1] != 1 || codes.n[1] < (k + 127) / 128 * 64 || levels.n[0] < 1 || levels.n[0] > 16 ||
-        !contiguous(&levels) || scales.n[0] != n || scales.n[1] < groups || (scales.n[1] > 1 && scales.step[1] != 1))
-        NO;
+    if (x->type < 0 || x->type > 2 || x->nd > 2 || codes->type != U8 || codes->nd != 2 || levels->type != x->type || levels->nd != 1 ||
+        scales->nd != 2 || (scales->type != x->type && scales->type != ECASQ_F32) || group < 32 || group % 32 || group > INT32_MAX / 2)
+        return 0;
+    p->k = x->n[x->nd - 1];
+    p->rows = codes->n[0];
+    p->b = x->nd == 2 ? x->n[0] : 1;
+    p->group = (int32_t)group;
+    if ((p->k > 1 && x->step[x->nd - 1] != 1) || codes->step[1] != 1 || codes->n[1] < (p->k + 127) / 128 * 64 || levels->n[0] < 1 || levels->n[0] > 16 ||
+        !contiguous(levels) || scales->n[0] != p->rows || scales->n[1] < (p->k + group - 1) / group || (scales->n[1] > 1 && scales->step[1] != 1))
+        return 0;
+    return codes->device == x->device && levels->device == x->device && scales->device == x->device;
+}
+static int64_t x_row(const Product *p) { return p->x.nd == 2 ? p->x.step[0] : p->k; }
+static int64_t code_row(const Product *p) { return p->rows > 1 ? p->codes.step[0] : p->codes.n[1]; }
+static int64_t scale_row(const Product *p) { return p->rows > 1 ? p->scales.step[0] : p->scales.n[1]; }
+
+/* A tensor [b, n], or [n] where x has one dimension, of type `type` with contiguous rows, on x's device. */
+static int rows_like(const Tensor *t, const Tensor *x, int64_t b, int64_t n, int type) {
+    return t->type == type && t->nd == x->nd && t->device == x->device && t->n[t->nd - 1] == n && (t->nd == 1 || t->n[0] == b) && (n < 2 || t->step[t->nd - 1] == 1);
+}
+/* `given`, or such a tensor made where that is None; NULL with an exception, or None, where it is not one. */
+static PyObject *output_of(PyObject *given, const Tensor *x, int64_t b, int64_t n, int type, Tensor *y) {
+    PyObject *made;
+    if (given == Py_None) {
+        const int64_t shape[2] = {x->nd == 2 ? b : n, n};
+        if (!(made = new_tensor(x->nd, shape, type, x))) return NULL;
+    } else {
+        made = Py_NewRef(given);
+    }
+    if (look(made, y) && rows_like(y, x, b, n, type)) return made;
+    Py_DECREF(made);
+    NO;
+}
+static int64_t row_step(const Tensor *t, int64_t n) { return t->nd == 2 ? t->step[0] : n; }
+
+/* matvec(x, codes, levels, scales, group, out, status) */
+static PyObject *py_matvec(PyObject *self, PyObject *const *v, Py_ssize_t n_args) {
+    Product p;
+    Tensor y;
+    int32_t *status;
+    ecasq_stream_t stream;
+    PyObject *made;
+    if (n_args != 7 || !product_of(v, &p)) NO;
     PyObject *const floats[] = {v[0], v[2], v[3], v[5]};
     if (tracked(floats, 4)) NO;
-    if (codes.device != x.device || levels.device != x.device || scales.device != x.device || !status_of(v[6], x.device, &status) ||
-        !stream_of(x.device, &stream))
-        NO;
-    if (v[5] == Py_None) {
-        const int64_t shape[2] = {x.nd == 2 ? b : n, n};
-        if (!(made = new_tensor(x.nd, shape, x.type, &x))) return NULL;
-    } else {
-        made = Py_NewRef(v[5]);
-    }
-    if (!look(made, &y) || y.type != x.type || y.nd != x.nd || y.device != x.device || y.n[y.nd - 1] != n || (y.nd == 2 && y.n[0] != b) ||
-        (n > 1 && y.step[y.nd - 1] != 1)) {
-        Py_DECREF(made);
-        NO;
-    }
+    if (!status_of(v[6], p.x.device, &status) || !stream_of(p.x.device, &stream)) NO;
+    if (!(made = output_of(v[5], &p.x, p.b, p.rows, p.x.type, &y)) || made == Py_None) return made;
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = call_matvec(x.at, x.nd == 2 ? x.step[0] : k, x.type, b, codes.at, n > 1 ? codes.step[0] : codes.n[1], levels.at, (int32_t)levels.n[0], scales.at,
-                     n > 1 ? scales.step[0] : scales.n[1], scales.type, n, k, (int32_t)group, y.at, y.nd == 2 ? y.step[0] : n, status, stream);
+    rc = call_matvec(p.x.at, x_row(&p), p.x.type, p.b, p.codes.at, code_row(&p), p.levels.at, (int32_t)p.levels.n[0], p.scales.at, scale_row(&p), p.scales.type,
+                     p.rows, p.k, p.group, y.at, row_step(&y, p.rows), status, stream);
     Py_END_ALLOW_THREADS
     if (!rc) return made;
     Py_DECREF(made);
     return PyLong_FromLong(rc);
+}
+
+/* A product with an epilogue: project(x, codes, levels, scales, group, bias, activation, residual, out, ws, status), and gated(x, codes,
+ * levels, scales, group, activation, out, ws, status) with `gated`. */
+static PyObject *layer_product(PyObject *const *v, int gated) {
+    Product p;
+    Tensor bias, residual, y, ws;
+    int32_t *status;
+    ecasq_stream_t stream;
+    PyObject *made, *space = NULL;
+    PyObject *const *w = v + (gated ? 6 : 8); /* out, ws, status */
+    if (!product_of(v, &p) || (gated && p.rows % 2)) NO;
+    const int64_t n = gated ? p.rows / 2 : p.rows;
+    const long act = PyLong_AsLong(v[gated ? 5 : 6]);
+    if (act == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        NO;
+    }
+    bias.at = residual.at = ws.at = NULL;
+    ws.count = 0;
+    if (!gated && v[5] != Py_None && (!look(v[5], &bias) || bias.type != p.x.type || bias.nd != 1 || bias.n[0] != n || !contiguous(&bias) || bias.device != p.x.device)) NO;
+    if (!gated && v[7] != Py_None && (!look(v[7], &residual) || !rows_like(&residual, &p.x, p.b, n, p.x.type))) NO;
+    PyObject *const floats[] = {v[0], v[2], v[3], w[0], gated ? Py_None : v[5], gated ? Py_None : v[7]};
+    if (tracked(floats, 6)) NO;
+    if (!status_of(w[2], p.x.device, &status) || !stream_of(p.x.device, &stream)) NO;
+    if (w[1] != Py_None && (!look(w[1], &ws) || ws.type != U8 || ws.device != p.x.device || !contiguous(&ws))) NO;
+    if (!(made = output_of(w[0], &p.x, p.b, n, p.x.type, &y)) || made == Py_None) return made;
+    if (w[1] == Py_None) {
+        const int64_t room = (int64_t)call_room(p.b, p.rows, p.k, p.x.type);
+        if (room && (!(space = new_tensor(1, &room, U8, &p.x)) || !look(space, &ws))) {
+            Py_XDECREF(space);
+            Py_DECREF(made);
+            return PyErr_Occurred() ? NULL : Py_NewRef(Py_None);
+        }
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    if (gated)
+        rc = call_gated(p.x.at, x_row(&p), p.x.type, p.b, p.codes.at, code_row(&p), p.levels.at, (int32_t)p.levels.n[0], p.scales.at, scale_row(&p), p.scales.type, n, p.k,
+                        p.group, (int32_t)act, y.at, row_step(&y, n), ws.at, (size_t)ws.count, status, stream);
+    else
+        rc = call_project(p.x.at, x_row(&p), p.x.type, p.b, p.codes.at, code_row(&p), p.levels.at, (int32_t)p.levels.n[0], p.scales.at, scale_row(&p), p.scales.type, n,
+                          p.k, p.group, bias.at, (int32_t)act, residual.at, residual.at ? row_step(&residual, n) : 0, y.at, row_step(&y, n), ws.at, (size_t)ws.count,
+                          status, stream);
+    Py_END_ALLOW_THREADS
+    Py_XDECREF(space);
+    if (!rc) return made;
+    Py_DECREF(made);
+    return PyLong_FromLong(rc);
+}
+static PyObject *py_project(PyObject *self, PyObject *const *v, Py_ssize_t n_args) {
+    if (n_args != 11) NO;
+    return layer_product(v, 0);
+}
+static PyObject *py_gated(PyObject *self, PyObject *const *v, Py_ssize_t n_args) {
+    if (n_args != 9) NO;
+    return layer_product(v, 1);
+}
+
+/* norm(x, weight, eps, residual, group, out, out_sum, out_scales): y; (y, scales); with a residual the sum behind them */
+static PyObject *py_norm(PyObject *self, PyObject *const *v, Py_ssize_t n_args) {
+    Tensor x, weight, residual, y, sum, scales;
+    ecasq_stream_t stream;
+    PyObject *made[3] = {NULL, NULL, NULL}, *all = NULL;
+    if (n_args != 8 || !look(v[0], &x) || !look(v[1], &weight)) NO;
+    const double eps = PyFloat_AsDouble(v[2]);
+    const long long group = v[4] == Py_None ? 0 : PyLong_AsLongLong(v[4]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        NO;
+    }
+    if (x.type < 0 || x.type > 2 || x.nd > 2) NO;
+    const int64_t k = x.n[x.nd - 1], b = x.nd == 2 ? x.n[0] : 1;
+    if ((k > 1 && x.step[x.nd - 1] != 1) || weight.nd != 1 || weight.n[0] != k || !contiguous(&weight) || (weight.type != x.type && weight.type != ECASQ_F32) ||
+        weight.device != x.device || k < 1 || (v[4] != Py_None && group < 1))
+        NO;
+    residual.at = sum.at = scales.at = NULL;
+    if (v[3] != Py_None && (!look(v[3], &residual) || !rows_like(&residual, &x, b, k, x.type))) NO;
+    if ((v[3] == Py_None && v[6] != Py_None) || (!group && v[7] != Py_None)) NO;
+    PyObject *const floats[] = {v[0], v[1], v[3], v[5], v[6], v[7]};
+    if (tracked(floats, 6)) NO;
+    if (!stream_of(x.device, &stream)) NO;
+    const int64_t groups = group ? (k + group - 1) / group : 0;
+    if (!(made[0] = output_of(v[5], &x, b, k, group ? E4M3 : x.type, &y)) || made[0] == Py_None) return made[0];
+    if (group && (!(made[1] = output_of(v[7], &x, b, groups, ECASQ_F32, &scales)) || made[1] == Py_None)) goto done;
+    if (v[3] != Py_None && (!(made[2] = output_of(v[6], &x, b, k, x.type, &sum)) || made[2] == Py_None)) goto done;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = call_norm(x.at, row_step(&x, k), x.type, b, k, residual.at, v[3] != Py_None ? row_step(&residual, k) : 0, weight.at, weight.type, (float)eps, group, y.at,
+                   row_step(&y, k), sum.at, v[3] != Py_None ? row_step(&sum, k) : 0, scales.at, group ? row_step(&scales, groups) : 0, stream);
+    Py_END_ALLOW_THREADS
+    if (rc) all = PyLong_FromLong(rc);
+    else if (made[1] && made[2]) all = PyTuple_Pack(3, made[0], made[1], made[2]);
+    else if (made[1] || made[2]) all = PyTuple_Pack(2, made[0], made[1] ? made[1] : made[2]);
+    else all = Py_NewRef(made[0]);
+done:
+    if (!all && !PyErr_Occurred()) all = Py_NewRef(Py_None);
+    for (int i = 0; i < 3; i++) Py_XDECREF(made[i]);
+    return all;
 }
 
 /* One side of a paged cache: rows and, for coded ones, levels (else None). */
@@ -318,19 +457,25 @@ done:
     return both;
 }
 
-/* setup(addresses of matvec, cache_write, attend, torch.Tensor, torch.empty, current device, raw stream, workspace,
- * torch.is_grad_enabled, torch.autograd.forward_ad, dtypes) */
+/* setup(addresses of matvec, cache_write, attend, project, gated, workspace_size_project, norm, torch.Tensor, torch.empty, current
+ * device, raw stream, workspace, torch.is_grad_enabled, torch.autograd.forward_ad, dtypes) */
 static PyObject *py_setup(PyObject *self, PyObject *args) {
-    unsigned long long a[3];
+    unsigned long long a[7];
     PyObject *o[7], *types;
-    if (!PyArg_ParseTuple(args, "KKKOOOOOOOO!", &a[0], &a[1], &a[2], &o[0], &o[1], &o[2], &o[3], &o[4], &o[5], &o[6], &PyTuple_Type, &types)) return NULL;
+    if (!PyArg_ParseTuple(args, "KKKKKKKOOOOOOOO!", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &o[0], &o[1], &o[2], &o[3], &o[4], &o[5], &o[6], &PyTuple_Type,
+                          &types))
+        return NULL;
     if (PyTuple_GET_SIZE(types) != DTYPES || !PyType_Check(o[0])) {
-        PyErr_SetString(PyExc_TypeError, "setup: six dtypes and a tensor type");
+        PyErr_SetString(PyExc_TypeError, "setup: seven dtypes and a tensor type");
         return NULL;
     }
     call_matvec = (matvec_fn)(uintptr_t)a[0];
     call_write = (write_fn)(uintptr_t)a[1];
     call_attend = (attend_fn)(uintptr_t)a[2];
+    call_project = (project_fn)(uintptr_t)a[3];
+    call_gated = (gated_fn)(uintptr_t)a[4];
+    call_room = (room_fn)(uintptr_t)a[5];
+    call_norm = (norm_fn)(uintptr_t)a[6];
     PyObject **to[7] = {&tensor_type, &empty, &current_device, &raw_stream, &make_workspace, &grad_enabled, &forward_ad};
     for (int i = 0; i < 7; i++) Py_XSETREF(*to[i], Py_NewRef(o[i]));
     for (int i = 0; i < DTYPES; i++) Py_XSETREF(dtypes[i], Py_NewRef(PyTuple_GET_ITEM(types, i)));
@@ -339,6 +484,9 @@ static PyObject *py_setup(PyObject *self, PyObject *args) {
 
 static PyMethodDef methods[] = {{"setup", py_setup, METH_VARARGS, NULL},
                                 {"matvec", (PyCFunction)(void (*)(void))py_matvec, METH_FASTCALL, NULL},
+                                {"project", (PyCFunction)(void (*)(void))py_project, METH_FASTCALL, NULL},
+                                {"gated", (PyCFunction)(void (*)(void))py_gated, METH_FASTCALL, NULL},
+                                {"norm", (PyCFunction)(void (*)(void))py_norm, METH_FASTCALL, NULL},
                                 {"cache_write", (PyCFunction)(void (*)(void))py_write, METH_FASTCALL, NULL},
                                 {"attend", (PyCFunction)(void (*)(void))py_attend, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};

@@ -127,6 +127,12 @@ def lib():
             "ecasq_pack": (C.c_int, [vp, i64, i64, i64, vp, i64, vp]),
             "ecasq_matvec": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, vp, i64, vp,
                                        vp]),
+            "ecasq_workspace_size_project": (sz, [i64, i64, i64, i32]),
+            "ecasq_project": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, vp, i32, vp, i64, vp, i64,
+                                        vp, sz, vp, vp]),
+            "ecasq_gated": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, i32, vp, i64, vp, sz, vp,
+                                      vp]),
+            "ecasq_norm": (C.c_int, [vp, i64, i32, i64, i64, vp, i64, vp, i32, C.c_float, i64, vp, i64, vp, i64, vp, i64, vp]),
             "ecasq_cache_write": (C.c_int, [vp, i32, i64, i64, i64, vp, i32, vp, vp, PC, u64, vp, vp]),
             "ecasq_workspace_size_attend": (sz, [i64, i32, i32, i32, i64]),
             "ecasq_attend": (C.c_int, [vp, i64, i64, i64, i32, PC, PC, vp, i64, vp, vp, i64, C.c_float, vp, i64, i64,
@@ -151,7 +157,8 @@ def exported_symbols():
                  "ecasq_dp_pass",
                  "ecasq_dp_tables", "ecasq_workspace_size_linear", "ecasq_dp_linear", "ecasq_refine", "ecasq_evaluate", "ecasq_quantize", "ecasq_quantize_noalloc",
                  "ecasq_solve_batched",
-                 "ecasq_prepare", "ecasq_pack", "ecasq_matvec", "ecasq_cache_write", "ecasq_workspace_size_attend",
+                 "ecasq_prepare", "ecasq_pack", "ecasq_matvec", "ecasq_workspace_size_project", "ecasq_project", "ecasq_gated",
+                 "ecasq_norm", "ecasq_cache_write", "ecasq_workspace_size_attend",
                  "ecasq_attend", "ecasq_kernel_launches"):
         if hasattr(L, name):
             names.append(name)
@@ -587,10 +594,12 @@ def _ready():
             module = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_codes", path, loader=loader))
             loader.exec_module(module)
             address = lambda fn: C.cast(fn, C.c_void_p).value  # noqa: E731
-            module.setup(address(L.ecasq_matvec), address(L.ecasq_cache_write), address(L.ecasq_attend), torch.Tensor, torch.empty,
+            module.setup(address(L.ecasq_matvec), address(L.ecasq_cache_write), address(L.ecasq_attend), address(L.ecasq_project),
+                         address(L.ecasq_gated), address(L.ecasq_workspace_size_project), address(L.ecasq_norm), torch.Tensor, torch.empty,
                          torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, workspace_attend,
                          torch.is_grad_enabled, torch.autograd.forward_ad,
-                         (torch.float32, torch.float16, torch.bfloat16, torch.uint8, torch.int32, torch.int64))
+                         (torch.float32, torch.float16, torch.bfloat16, torch.uint8, torch.int32, torch.int64,
+                          torch.float8_e4m3fn))
             _codes = module
     return _codes
 
@@ -645,25 +654,32 @@ def ecasq_pack(idx):
     return codes
 
 
+def _product_needs(torch, x, codes, levels, scales, group):
+    """What a product with a coded matrix wants of its operands, for _need()."""
+    k = lambda: x.shape[-1]  # noqa: E731
+    return ((lambda: x.dtype in _TYPES and x.dim() in (1, 2) and (k() < 2 or x.stride(-1) == 1),
+             "x must be [b, k] or [k] of float32, float16 or bfloat16 with contiguous rows"),
+            (lambda: codes.dtype == torch.uint8 and codes.dim() == 2 and codes.stride(1) == 1 and codes.shape[1] >= 64 * -(-k() // 128),
+             "codes must be uint8 [n, 64 ceil(k / 128)] with contiguous rows"),
+            (lambda: levels.dtype == x.dtype and levels.dim() == 1 and levels.is_contiguous() and 1 <= levels.numel() <= 16,
+             "levels must be 1 to 16 values of x's type"),
+            (lambda: group >= 32 and group % 32 == 0, "group must be a multiple of 32"),
+            (lambda: scales.dtype in (x.dtype, torch.float32) and scales.dim() == 2 and scales.shape[0] == codes.shape[0]
+             and scales.shape[1] >= -(-k() // group) and (scales.shape[1] < 2 or scales.stride(1) == 1),
+             "scales must be [n, ceil(k / group)] of x's type or float32 with contiguous rows"))
+
+
+def _rows_like(t, x, n, dtype):
+    """Whether t is [b, n] (or [n], as x is) of dtype with contiguous rows."""
+    return t.dtype == dtype and t.shape == x.shape[:-1] + (n,) and (n < 2 or t.stride(-1) == 1)
+
+
 def _matvec_refused(torch, x, codes, levels, scales, group, out, status):
     where = "ecasq_matvec"
     _here(where, x, codes, levels, scales, out)
     _no_gradients(where, x, levels, scales, out)
-    k = lambda: x.shape[-1]  # noqa: E731
-    _need(where,
-          (lambda: x.dtype in _TYPES and x.dim() in (1, 2) and (k() < 2 or x.stride(-1) == 1),
-           "x must be [b, k] or [k] of float32, float16 or bfloat16 with contiguous rows"),
-          (lambda: codes.dtype == torch.uint8 and codes.dim() == 2 and codes.stride(1) == 1 and codes.shape[1] >= 64 * -(-k() // 128),
-           "codes must be uint8 [n, 64 ceil(k / 128)] with contiguous rows"),
-          (lambda: levels.dtype == x.dtype and levels.dim() == 1 and levels.is_contiguous() and 1 <= levels.numel() <= 16,
-           "levels must be 1 to 16 values of x's type"),
-          (lambda: group >= 32 and group % 32 == 0, "group must be a multiple of 32"),
-          (lambda: scales.dtype in (x.dtype, torch.float32) and scales.dim() == 2 and scales.shape[0] == codes.shape[0]
-           and scales.shape[1] >= -(-k() // group) and (scales.shape[1] < 2 or scales.stride(1) == 1),
-           "scales must be [n, ceil(k / group)] of x's type or float32 with contiguous rows"),
-          (lambda: out is None or (out.dtype == x.dtype and out.shape == x.shape[:-1] + codes.shape[:1]
-                                   and (out.shape[-1] < 2 or out.stride(-1) == 1)),
-           "out must be [b, n] (or [n]) of x's type with contiguous rows"),
+    _need(where, *_product_needs(torch, x, codes, levels, scales, group),
+          (lambda: out is None or _rows_like(out, x, codes.shape[0], x.dtype), "out must be [b, n] (or [n]) of x's type with contiguous rows"),
           (lambda: _is_status(status, x), "status must be an int32 tensor on the device of the others"))
     _refuse(where, "bad arguments")
 
@@ -680,6 +696,112 @@ def ecasq_matvec(x, codes, levels, scales, group, out=None, status=None):
         _matvec_refused(_torch(), x, codes, levels, scales, group, out, status)
     if y.__class__ is int:
         _check(y, "ecasq_matvec")
+    return y
+
+
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}  # ECASQ_ACT_*
+
+
+def _activation(where, name):
+    try:
+        return ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        _refuse(where, "activation must be one of %s" % ", ".join(str(a) for a in ACTIVATIONS))
+
+
+def workspace_project(b, n, k, dtype):
+    """A device workspace for ecasq_project, or ecasq_gated, with a matrix of n rows and k columns and up to b rows of x of `dtype`
+    (it may be empty)."""
+    torch = _torch()
+    _ready()
+    if dtype not in _TYPES:
+        _refuse("workspace_project", "dtype must be float32, float16 or bfloat16")
+    room = int(lib().ecasq_workspace_size_project(int(b), int(n), int(k), _TYPES[dtype]))
+    return torch.empty(room, dtype=torch.uint8, device="cuda")
+
+
+def _layer_product_refused(torch, where, x, codes, levels, scales, group, bias, residual, out, ws, status, halves):
+    _here(where, x, codes, levels, scales, bias, residual, out, ws)
+    _no_gradients(where, x, levels, scales, bias, residual, out)
+    n = lambda: codes.shape[0] // halves  # noqa: E731
+    _need(where, *_product_needs(torch, x, codes, levels, scales, group),
+          (lambda: codes.shape[0] % halves == 0, "codes must have an even number of rows: the gate's, then the other half's"),
+          (lambda: bias is None or (bias.dtype == x.dtype and bias.shape == (n(),) and bias.is_contiguous()),
+           "bias must be contiguous [n] of x's type"),
+          (lambda: residual is None or _rows_like(residual, x, n(), x.dtype),
+           "residual must be [b, n] (or [n]) of x's type with contiguous rows"),
+          (lambda: out is None or _rows_like(out, x, n(), x.dtype), "out must be [b, n] (or [n]) of x's type with contiguous rows"),
+          (lambda: ws is None or (ws.dtype == torch.uint8 and ws.is_contiguous()), "ws must be contiguous uint8"),
+          (lambda: _is_status(status, x), "status must be an int32 tensor on the device of the others"))
+    _refuse(where, "bad arguments")
+
+
+def ecasq_project(x, codes, levels, scales, group, bias=None, activation=None, residual=None, out=None, ws=None, status=None):
+    """y = activation(x W^T + bias) + residual for the 4-bit matrix W of ecasq_matvec, in one call.
+
+    x, codes, levels, scales, group, status as for ecasq_matvec; bias [n] and residual [b, n] (or [n]) of x's type or None;
+    activation None, "relu", "silu", "gelu" or "gelu_tanh".  ws: workspace_project(b, n, k, x.dtype), or None (one is made
+    where one is needed).  Returns y [b, n] or [n] of x's type (`out` if given, which may be the residual itself).
+    No gradients: a tensor that requires one is refused while they are recorded."""
+    act = _activation("ecasq_project", activation)
+    y = (_codes or _ready()).project(x, codes, levels, scales, group, bias, act, residual, out, ws, status)
+    if y is None:
+        _layer_product_refused(_torch(), "ecasq_project", x, codes, levels, scales, group, bias, residual, out, ws, status, 1)
+    if y.__class__ is int:
+        _check(y, "ecasq_project")
+    return y
+
+
+def ecasq_gated(x, codes, levels, scales, group, activation="silu", out=None, ws=None, status=None):
+    """h = activation(x G^T) * (x U^T), the first half of a gated feed-forward block, in one call.
+
+    codes, levels, scales: one coded matrix of 2n rows, those of G and then those of U; x, group and status as for
+    ecasq_matvec; activation and ws (workspace_project(b, 2 * n, k, x.dtype)) as for ecasq_project.  Returns h [b, n] or
+    [n] of x's type (`out` if given).  No gradients: a tensor that requires one is refused while they are recorded."""
+    act = _activation("ecasq_gated", activation)
+    y = (_codes or _ready()).gated(x, codes, levels, scales, group, act, out, ws, status)
+    if y is None:
+        _layer_product_refused(_torch(), "ecasq_gated", x, codes, levels, scales, group, None, None, out, ws, status, 2)
+    if y.__class__ is int:
+        _check(y, "ecasq_gated")
+    return y
+
+
+def _norm_refused(torch, x, weight, eps, residual, group, out, out_sum, out_scales):
+    where = "ecasq_norm"
+    _here(where, x, weight, residual, out, out_sum, out_scales)
+    _no_gradients(where, x, weight, residual, out, out_sum, out_scales)
+    k = lambda: x.shape[-1]  # noqa: E731
+    _need(where,
+          (lambda: x.dtype in _TYPES and x.dim() in (1, 2) and k() > 0 and (k() < 2 or x.stride(-1) == 1),
+           "x must be [b, k] or [k] of float32, float16 or bfloat16 with contiguous rows"),
+          (lambda: weight.dtype in (x.dtype, torch.float32) and weight.shape == (k(),) and weight.is_contiguous(),
+           "weight must be contiguous [k] of x's type or float32"),
+          (lambda: eps >= 0, "eps must not be negative"),
+          (lambda: residual is None or _rows_like(residual, x, k(), x.dtype), "residual must be like x"),
+          (lambda: group is None or group >= k() or (group > 0 and group % 16 == 0), "group must be None, a multiple of 16 or at least k"),
+          (lambda: out is None or _rows_like(out, x, k(), x.dtype if group is None else torch.float8_e4m3fn),
+           "out must be like x, or of float8_e4m3fn with a group"),
+          (lambda: out_sum is None or (residual is not None and _rows_like(out_sum, x, k(), x.dtype)),
+           "out_sum must be like x, and needs a residual"),
+          (lambda: out_scales is None or (group is not None and _rows_like(out_scales, x, -(-k() // group), torch.float32)),
+           "out_scales must be float32 [b, ceil(k / group)] (or [ceil(k / group)]) with contiguous rows, and needs a group"))
+    _refuse(where, "bad arguments")
+
+
+def ecasq_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, out_sum=None, out_scales=None):
+    """Root-mean-square norm of the rows of x [b, k] or [k], after the residual's addition: s = x + residual rounded to x's type
+    (x without one), y = s / sqrt(mean(s^2) + eps) * weight.
+
+    weight [k] of x's type or float32.  With `group` (a multiple of 16, or at least k: one scale a row) y is coded to 8 bits:
+    float8_e4m3fn values y / scale, scale = max |y| / 448 of each group of columns.  Returns y, (y, scales), (y, s) or
+    (y, scales, s); out, out_scales and out_sum are taken for them where given.  out_sum, and out without a group, may be x or
+    the residual itself.  No gradients: a tensor that requires one is refused while they are recorded."""
+    y = (_codes or _ready()).norm(x, weight, eps, residual, group, out, out_sum, out_scales)
+    if y is None:
+        _norm_refused(_torch(), x, weight, eps, residual, group, out, out_sum, out_scales)
+    if y.__class__ is int:
+        _check(y, "ecasq_norm")
     return y
 
 
