@@ -1,18 +1,11 @@
-// project.cu -- products with a matrix of 4-bit codes and what follows them in a served layer (ecasq_project, ecasq_gated).
+// project.cu -- ecasq_project and ecasq_gated: the entry points, and the kernel for few rows of x.
 #include <algorithm>
 
-#include "epilogue.cuh"
+#include "project.cuh"
 
 namespace ecasq {
 
-struct ProjectArgs {
-    const void *x, *levels, *scales;
-    const uint8_t *codes;
-    void *y;
-    int64_t x_row, code_row, scale_row, y_row, n, k, b;
-    int32_t m, group;
-    Epilogue epi;
-};
+constexpr int64_t kFewRows = 8;
 
 // A block takes a tile of 32 outputs of 32 rows of x; 128 columns of both at a time lie in shared memory as fp32.
 template <typename T, typename S, bool GATED>
@@ -62,10 +55,10 @@ __global__ void __launch_bounds__(256) k_project(const __grid_constant__ Project
         }
 }
 
-template <typename T, typename S> static int launch_project(const ProjectArgs &a, bool gated, cudaStream_t st) {
+template <typename T, typename S> static int launch_project(const ProjectArgs &a, cudaStream_t st) {
     const dim3 grid((unsigned)cdiv(a.n, 32), (unsigned)cdiv(a.b, 32));
     note_launch();
-    if (gated) k_project<T, S, true><<<grid, 256, 0, st>>>(a);
+    if (a.gated) k_project<T, S, true><<<grid, 256, 0, st>>>(a);
     else k_project<T, S, false><<<grid, 256, 0, st>>>(a);
     ECASQ_LAUNCH_CHECK();
     return ECASQ_OK;
@@ -75,6 +68,8 @@ template <typename T, typename S> static int launch_project(const ProjectArgs &a
 static int project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row, const void *levels, int32_t m,
                    const void *scales, int64_t scale_row, int32_t scale_type, int64_t n, int64_t k, int32_t group, const Epilogue &epi, void *y,
                    int64_t y_row, void *ws, size_t ws_bytes, int32_t *status, bool gated, cudaStream_t st) {
+    const bool lost_wait = (type & ECASQ_TEST_LOST_WAIT) != 0;
+    type &= ~ECASQ_TEST_LOST_WAIT;
     if (n < 1 || k < 1 || b < 0 || n >= (int64_t)1 << (gated ? 30 : 31) || k >= (int64_t)1 << 31 || b > 8 * 65535 || m < 1 || m > 16 || !type_ok(type) ||
         (scale_type != type && scale_type != ECASQ_F32) || group < 32 || group % 32 || epi.act < ECASQ_ACT_NONE || epi.act > ECASQ_ACT_GELU_TANH)
         return ECASQ_EINVAL;
@@ -82,11 +77,12 @@ static int project(const void *x, int64_t x_row, int32_t type, int64_t b, const 
     if (!x || !codes || !levels || !scales || !y || !aligned16(codes) || code_row % 16 || code_row < 64 * cdiv(k, 128) || scale_row < cdiv(k, group) ||
         (b > 1 && (x_row < k || y_row < n || (epi.residual && epi.residual_row < n))))
         return ECASQ_EINVAL;
-    const ProjectArgs a{x, levels, scales, codes, y, x_row, code_row, scale_row, y_row, n, k, b, m, group, epi};
+    const ProjectArgs a{x, levels, scales, codes, y, status, x_row, code_row, scale_row, y_row, n, k, b, m, group, type, scale_type, gated, lost_wait, epi};
+    if (b > kFewRows) return launch_project_tc(a, ws, ws_bytes, st);
     const bool scales32 = scale_type == ECASQ_F32;
-    if (type == ECASQ_F32) return launch_project<float, float>(a, gated, st);
-    if (type == ECASQ_F16) return scales32 ? launch_project<__half, float>(a, gated, st) : launch_project<__half, __half>(a, gated, st);
-    return scales32 ? launch_project<__nv_bfloat16, float>(a, gated, st) : launch_project<__nv_bfloat16, __nv_bfloat16>(a, gated, st);
+    if (type == ECASQ_F32) return launch_project<float, float>(a, st);
+    if (type == ECASQ_F16) return scales32 ? launch_project<__half, float>(a, st) : launch_project<__half, __half>(a, st);
+    return scales32 ? launch_project<__nv_bfloat16, float>(a, st) : launch_project<__nv_bfloat16, __nv_bfloat16>(a, st);
 }
 
 }  // namespace ecasq
@@ -95,7 +91,10 @@ using namespace ecasq;
 
 extern "C" {
 
-size_t ecasq_workspace_size_project(int64_t b, int64_t n, int64_t k, int32_t type) { return 0; }
+size_t ecasq_workspace_size_project(int64_t b, int64_t n, int64_t k, int32_t type) {
+    if (b <= kFewRows || b > 8 * 65535 || n < 1 || k < 1 || k >= (int64_t)1 << 31 || !type_ok(type)) return 0;
+    return project_tc_room(b, k, type);
+}
 
 int ecasq_project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row, const void *levels,
                   int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n, int64_t k, int32_t group,

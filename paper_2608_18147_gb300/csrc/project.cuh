@@ -1,0 +1,24 @@
+// project.cuh -- what the kernels of ecasq_project and ecasq_gated share.
+#pragma once
+
+#include "epilogue.cuh"
+
+namespace ecasq {
+
+struct ProjectArgs {
+    const void *x, *levels, *scales;
+    const uint8_t *codes;
+    void *y;
+    int32_t *status;
+    int64_t x_row, code_row, scale_row, y_row, n, k, b;  // n: outputs a row of x; a gated matrix has 2n rows
+    int32_t m, group, type, scale_type;
+    bool gated;
+    uint32_t lost;  // test hook: 1 where blocks begin as if a wait had run out
+    Epilogue epi;
+};
+
+// Tensor cores, any number of rows of x; the workspace it may need.
+int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st);
+size_t project_tc_room(int64_t b, int64_t k, int32_t type);
+
+}  // namespace ecasq

@@ -1,0 +1,592 @@
+// project_tc.cu -- ecasq_project and ecasq_gated for more rows of x than a pass of the matrix-vector kernels takes.
+//
+// The matrix is the left operand: its codes become levels, which go to tensor memory as they are (16 bits, exact), 128 rows a
+// block and 256 a pair of blocks; the rows of x are the right operand, in shared memory.  The sums of the columns of one scale group
+// come out of tensor memory, are multiplied by their row's scale, which is one number a thread there, and are added up in registers.  So
+// products and scales are as exact as in ecasq_matvec: nothing is rounded before the end.
+#include <algorithm>
+
+#include "project.cuh"
+#include "tc.cuh"
+
+namespace ecasq {
+
+struct TcArgs {
+    const void *levels, *scales;
+    void *y;
+    int32_t *status;
+    int64_t scale_row, y_row, n, b, k, second;  // second: the first row of a gated matrix's other half
+    int32_t m, group, type, scale_type;
+    int32_t blocks;         // blocks of 128 columns
+    int32_t group_blocks;   // blocks of a scale group, where it holds whole ones
+    int32_t split;          // pairs of a cluster that share the columns
+    int32_t x_tiles, tiles; // tiles of rows of x; of the product
+    uint32_t lost;          // test hook: 1 where blocks begin as if a wait had run out
+    Epilogue epi;
+};
+
+constexpr int kTcSpins = 1 << 18;  // of a wait, each of some microseconds at most: about two seconds
+constexpr int kDBufs = 3;          // sums in tensor memory; behind them 4 stages of 64 columns of levels
+constexpr int kACols = 32, kAStages = 4, kAAt = 512 - kAStages * kACols;
+constexpr int kCodeStage = 128 * 64;
+
+// fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.
+__device__ __constant__ const int8_t kXTerm[6] = {0, 0, 0, 1, 1, 2}, kLevelTerm[6] = {0, 1, 2, 0, 1, 0};
+
+// ND columns (rows of x) a product, NH of them a tile; SPANS scale groups' sums in a block of 128 columns, at least one.
+template <int ND, int NH> struct TcShape {
+    static constexpr int kN = ND * NH;
+    static constexpr int kDecodeWarps = NH == 2 ? 4 : 8, kWarps = 4 + kDecodeWarps + 8, kThreads = 32 * kWarps;
+    static constexpr int kXStage = kN / 2 * 256;
+    static constexpr int kXStages = kN >= 128 ? 5 : kN == 64 ? 10 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 8 : 12;
+    static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
+    static constexpr int kOut = NH == 2 ? 32 : kOwn;              // of them at a time on their way out through shared memory
+    static constexpr int kSums = 8 * kOut * 32 * 4;               // what the eight warps have on their way out
+    static constexpr int kBars = 3 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
+    static constexpr int kTablesAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTablesAt + 128, kBarsAt = kSumsAt + kSums;
+    static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
+};
+
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t s) {
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(s));
+    return d;
+}
+// The levels of a word of eight codes, as four pairs.  t: the low bytes of levels 0-3, 4-7, 8-11, 12-15, then their high bytes.
+// The lower and the upper eight levels are looked up by the codes' low three bits, and a permute that spreads the sign bits of w << 4 and w,
+// which are the codes' fourth bits, chooses.
+__device__ __forceinline__ void decode(uint32_t w, const uint32_t (&t)[8], uint32_t *to) {
+    const uint32_t low3 = w & 0x77777777u, up = w << 4;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const uint32_t s = h ? low3 >> 16 : low3, m = permute(up, w, h ? 0xFBEA : 0xD9C8);
+        const uint32_t l0 = permute(t[0], t[1], s), l1 = permute(t[2], t[3], s), h0 = permute(t[4], t[5], s), h1 = permute(t[6], t[7], s);
+        const uint32_t l = (l0 & ~m) | (l1 & m), hi = (h0 & ~m) | (h1 & m);
+        to[2 * h] = permute(l, hi, 0x5140);
+        to[2 * h + 1] = permute(l, hi, 0x7362);
+    }
+}
+
+// What sums become, of columns c0 to c1 on their way out, which are rows of x from x0 on, and matrix row `row` of this lane (gated: the
+// gate's in the lower half of a warp, the other's in the upper).  sums: entry (c, lane) at 32 c + lane; of split > 1 pairs of the cluster they
+// are added up.
+template <typename T, bool GATED>
+__device__ __forceinline__ void finish(const TcArgs &a, const float *sums, int c0, int c1, int64_t x0, int64_t row, uint32_t rank) {
+    const int lane = threadIdx.x & 31;
+    auto sum = [&](int at) {
+        if (a.split == 1) return sums[at];
+        float v = 0.f;
+        for (int p = 0; p < a.split; p++) {
+            float of;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(of) : "r"(of_rank(shared_at(sums + at), 2 * p + (rank & 1))) : "memory");
+            v += of;
+        }
+        return v;
+    };
+    if (row >= a.n) return;
+    T *y = static_cast<T *>(a.y) + row;
+    if (GATED) {
+        // The lower lanes take the even columns, the upper ones the odd.
+        for (int c = c0 + (lane >> 4); c < c1 && x0 + c < a.b; c += 2)
+            y[(x0 + c) * a.y_row] = from_f32<T>(activate(sum(32 * c + (lane & 15)), a.epi.act) * sum(32 * c + 16 + (lane & 15)));
+    } else {
+        const float bias = a.epi.bias ? to_f32(static_cast<const T *>(a.epi.bias)[row]) : 0.f;
+        const T *residual = static_cast<const T *>(a.epi.residual) + (a.epi.residual ? row : 0);
+        const int end = (int)min((int64_t)c1, a.b - x0);
+        for (int c = c0; c < end; c += 8) {
+            float r[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) r[j] = a.epi.residual && c + j < end ? to_f32(residual[(x0 + c + j) * a.epi.residual_row]) : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (c + j < end) y[(x0 + c + j) * a.y_row] = from_f32<T>(activate(sum(32 * (c + j) + lane) + bias, a.epi.act) + r[j]);
+        }
+    }
+}
+
+// A cluster is `split` pairs of blocks.  Of a block's warps, four bring in tiles, issue products and pass arrivals on; kDecodeWarps turn codes
+// into levels; eight take sums out.  Barriers pass stages between them; those that the products' issuer waits for are in the first block of a
+// pair, which issues for both.
+template <int ND, int NH, bool GATED, int SPANS>
+__global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
+                                                                            const __grid_constant__ TcArgs a) {
+    using Shape = TcShape<ND, NH>;
+    constexpr int kN = Shape::kN, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kOwn = Shape::kOwn;
+    extern __shared__ char smem_raw[];
+    const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
+    char *smem = smem_raw + (base - shared_at(smem_raw));
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const uint32_t rank = cluster_rank(), leader = rank & ~1u, size = 2 * a.split, pair = rank / 2;
+    const uint32_t bars = base + Shape::kBarsAt;
+    const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, x_other = x_empty + 8 * kXStages, c_full = x_other + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
+                   a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
+                   all_done = d_empty + 8 * kDBufs, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
+    uint32_t *tables = reinterpret_cast<uint32_t *>(smem + Shape::kTablesAt);
+    const int terms = a.type == ECASQ_F32 ? 6 : 1;
+    const int kb0 = (int)((int64_t)a.blocks * pair / a.split), kb1 = (int)((int64_t)a.blocks * (pair + 1) / a.split);
+    const int cluster = blockIdx.x / size, clusters = gridDim.x / size;
+
+    auto lose = [&] {
+        for (uint32_t r = 0; r < size; r++) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(of_rank(lost_at, r)), "r"(1) : "memory");
+    };
+    auto lost = [&] {
+        uint32_t v;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(lost_at) : "memory");
+        return v != 0;
+    };
+    // A wait ends when its phase has, or with the loss of the block's work: when the limit has run out here or elsewhere in the cluster.
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (mbar_try(bar, parity)) return true;
+        for (int i = 0; i < kTcSpins; i++) {
+            if (lost()) return false;
+            if (mbar_try(bar, parity)) return true;
+        }
+        lose();
+        return false;
+    };
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
+
+    wait_before();
+    if (tid == 0) {
+        for (int i = 0; i < kXStages; i++) {
+            mbar_init(x_full + 8 * i, 1);
+            mbar_init(x_empty + 8 * i, 1);
+            mbar_init(x_other + 8 * i, 1);
+        }
+        for (int i = 0; i < kCodeStages; i++) {
+            mbar_init(c_full + 8 * i, 1);
+            mbar_init(c_empty + 8 * i, 8);
+        }
+        for (int i = 0; i < kAStages; i++) {
+            mbar_init(a_full + 8 * i, 8);
+            mbar_init(a_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kDBufs; i++) {
+            mbar_init(d_full + 8 * i, 1);
+            mbar_init(d_empty + 8 * i, NH == 2 ? 8 : 16);
+        }
+        mbar_init(all_done, 1);
+        mbar_init(sums_full, 8 * a.split);
+        mbar_init(sums_empty, 8 * a.split);
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(lost_at), "r"(a.lost) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        tile_map_fetch(&xm);
+        tile_map_fetch(&cm);
+    }
+    // The levels' bytes, of fp32 three terms of eight bits each.
+    if (tid < 48) {
+        const int term = tid / 16, j = tid % 16;
+        uint32_t bits = 0;
+        if (j < a.m) {
+            if (a.type == ECASQ_F32) {
+                float v = static_cast<const float *>(a.levels)[j];
+                for (int i = 0; i <= term; i++) {
+                    bits = __float_as_uint(v) >> 16;
+                    v -= __uint_as_float(bits << 16);
+                }
+            } else {
+                bits = static_cast<const uint16_t *>(a.levels)[j];
+            }
+        }
+        reinterpret_cast<uint8_t *>(tables + 8 * term)[j] = (uint8_t)bits;
+        reinterpret_cast<uint8_t *>(tables + 8 * term)[16 + j] = (uint8_t)(bits >> 8);
+    }
+    if (wid == 3) tmem_alloc(tmem_at);
+    __syncthreads();
+    cluster_barrier();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
+
+    // The first row of the matrix that this block has of weight tile t: 128 rows (gated: 64 of each half) from it on.
+    auto rows_at = [&](int t) { return (int64_t)t * (GATED ? 128 : 256) + (int64_t)(rank & 1) * (GATED ? 64 : 128); };
+    const int per_tile = (kb1 - kb0) * terms;  // products' blocks of a tile
+
+    if (wid < 4) {
+        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (lane == 0 && !a.lost) {
+            if (wid == 0) {  // rows of x
+                uint32_t i = 0;
+                bool ok = true;
+                for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                    const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + (int64_t)(rank & 1) * (ND / 2);
+                    for (int v = 0; ok && v < per_tile; v++, i++) {
+                        const uint32_t s = i % kXStages, to = base + s * Shape::kXStage;
+                        if (!(ok = wait(x_empty + 8 * s, (i / kXStages & 1) ^ 1))) break;
+                        mbar_expect(x_full + 8 * s, Shape::kXStage);
+                        const int kb = kb0 + v / terms;
+                        const int64_t from = x0 + (terms > 1 ? kXTerm[v % terms] * a.b : 0);
+#pragma unroll
+                        for (int h = 0; h < NH; h++)
+#pragma unroll
+                            for (int q = 0; q < 2; q++)
+                                tile_load(to + (2 * h + q) * (ND / 2 * 128), &xm, kb * 128 + 64 * q, (int32_t)(from + h * ND), x_full + 8 * s);
+                    }
+                }
+                for (uint32_t j = i > kXStages ? i - kXStages : 0; j < i; j++)  // none is on its way when the block ends
+                    for (int spin = 0; spin < kTcSpins && !mbar_try(x_full + 8 * (j % kXStages), j / kXStages & 1); spin++) {}
+            } else if (wid == 2) {  // codes
+                uint32_t i = 0;
+                bool ok = true;
+                for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                    const int64_t r0 = rows_at(t / a.x_tiles);
+                    for (int v = 0; ok && v < per_tile; v++, i++) {
+                        const uint32_t s = i % kCodeStages, to = base + kXStages * Shape::kXStage + s * kCodeStage;
+                        if (!(ok = wait(c_empty + 8 * s, (i / kCodeStages & 1) ^ 1))) break;
+                        mbar_expect(c_full + 8 * s, kCodeStage);
+                        const int kb = kb0 + v / terms;
+                        tile_load(to, &cm, kb * 64, (int32_t)r0, c_full + 8 * s);
+                        tile_load(to + kCodeStage / 2, &cm, kb * 64, (int32_t)(r0 + (GATED ? a.second : 64)), c_full + 8 * s);
+                    }
+                }
+                for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++)
+                    for (int spin = 0; spin < kTcSpins && !mbar_try(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1); spin++) {}
+            } else if (wid == 3 && rank != leader) {  // tells the first block of the pair that this one's rows of x are there
+                uint32_t i = 0;
+                bool ok = true;
+                const uint32_t there = of_rank(x_other, leader);
+                for (int t = cluster; ok && t < a.tiles; t += clusters)
+                    for (int v = 0; ok && v < per_tile; v++, i++)
+                        if ((ok = wait(x_full + 8 * (i % kXStages), i / kXStages & 1))) mbar_arrive(there + 8 * (i % kXStages));
+            } else if (wid == 1 && rank == leader) {  // products
+                const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
+                const uint16_t both = (uint16_t)(3u << rank);
+                uint32_t i = 0, span = 0;
+                bool ok = true;
+                auto d_of = [&](uint32_t job) { return tmem + job % kDBufs * ND; };
+                auto open = [&](uint32_t job) {
+                    const bool free = wait(d_empty + 8 * (job % kDBufs), (job / kDBufs & 1) ^ 1);
+                    tmem_fence_after();
+                    return free;
+                };
+                for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                    int in_group = kb0 % a.group_blocks;
+                    bool fresh = true;
+                    for (int v = 0; ok && v < per_tile; v++, i++) {
+                        const uint32_t xs = i % kXStages, xp = i / kXStages & 1, x = base + xs * Shape::kXStage;
+                        if (!(ok = wait(x_full + 8 * xs, xp) && wait(x_other + 8 * xs, xp))) break;
+                        // The product of 16 entries number kk of the block with half h of the rows of x.
+                        auto step = [&](uint32_t d, int h, int kk, bool add) {
+                            const uint32_t as = (2 * i + kk / 4) % kAStages;
+                            mma_pair(d, tmem + kAAt + as * kACols + kk % 4 * 8, mma_rows(x + (2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32), kind, add);
+                        };
+                        auto levels = [&](int hb) {
+                            const uint32_t j = 2 * i + hb;
+                            const bool there = wait(a_full + 8 * (j % kAStages), j / kAStages & 1);
+                            tmem_fence_after();
+                            return there;
+                        };
+                        if (SPANS == 1) {
+                            const bool last = v + 1 == per_tile || (v % terms == terms - 1 && in_group + 1 == a.group_blocks);
+                            for (int h = 0; ok && h < NH; h++) {
+                                const uint32_t job = span * NH + h;
+                                if (fresh && !(ok = open(job))) break;
+                                for (int hb = 0; hb < 2; hb++) {
+                                    if (h == 0 && !(ok = levels(hb))) break;
+#pragma unroll
+                                    for (int kk = 0; kk < 4; kk++) step(d_of(job), h, 4 * hb + kk, !fresh || hb || kk);
+                                    if (h == NH - 1) mma_commit(a_empty + 8 * ((2 * i + hb) % kAStages), both);
+                                }
+                                if (ok && last) mma_commit(d_full + 8 * (job % kDBufs), both);
+                            }
+                            fresh = last;
+                            if (last) span++;
+                        } else {
+                            for (int hb = 0; ok && hb < 2; hb++) {
+                                if (!(ok = levels(hb))) break;
+                                for (int sub = 0; ok && sub < SPANS / 2; sub++, span++)
+                                    for (int h = 0; ok && h < NH; h++) {
+                                        const uint32_t job = span * NH + h;
+                                        if (!(ok = open(job))) break;
+#pragma unroll
+                                        for (int kk = 0; kk < 8 / SPANS; kk++) step(d_of(job), h, 4 * hb + sub * (8 / SPANS) + kk, kk > 0);
+                                        mma_commit(d_full + 8 * (job % kDBufs), both);
+                                    }
+                                if (ok) mma_commit(a_empty + 8 * ((2 * i + hb) % kAStages), both);
+                            }
+                        }
+                        if (ok) mma_commit(x_empty + 8 * xs, both);
+                        if (v % terms == terms - 1 && ++in_group == a.group_blocks) in_group = 0;
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (wid < 4 + Shape::kDecodeWarps) {
+        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        // Row of the block's 128: of a gated matrix the lower half of each warp has rows of the gate.
+        const int row = 32 * (wid & 3) + lane, from = GATED ? (lane & 16) * 4 + 16 * (wid & 3) + (lane & 15) : row;
+        const uint32_t there = of_rank(a_full, leader), swizzle = (uint32_t)(from >> 1 & 3);
+        const int first = Shape::kDecodeWarps == 8 ? (wid - 4) / 4 : 0, step = Shape::kDecodeWarps == 8 ? 2 : 1;
+        uint32_t i = 0;
+        bool ok = !a.lost;
+        for (int t = cluster; ok && t < a.tiles; t += clusters)
+            for (int v = 0; ok && v < per_tile; v++, i++) {
+                const uint32_t cs = i % kCodeStages;
+                if (!(ok = wait_warp(c_full + 8 * cs, i / kCodeStages & 1))) break;
+                const char *codes = smem + kXStages * Shape::kXStage + cs * kCodeStage + from * 64;
+                uint32_t table[8];
+                const uint4 *book = reinterpret_cast<const uint4 *>(tables + (terms > 1 ? 8 * kLevelTerm[v % terms] : 0));
+                *reinterpret_cast<uint4 *>(table) = book[0];
+                *reinterpret_cast<uint4 *>(table + 4) = book[1];
+                for (int hb = first; ok && hb < 2; hb += step) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        const uint2 two = *reinterpret_cast<const uint2 *>(codes + ((q ^ swizzle) << 4) + 8 * hb);
+                        w[q] = two.x;
+                        w[q + 4] = two.y;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(c_empty + 8 * cs);
+                    uint32_t pairs[32];
+#pragma unroll
+                    for (int q = 0; q < 8; q++) decode(w[q], table, pairs + 4 * q);
+                    const uint32_t j = 2 * i + hb, as = j % kAStages;
+                    if (!(ok = wait_warp(a_empty + 8 * as, (j / kAStages & 1) ^ 1))) break;
+                    tmem_fence_after();
+                    tmem_store(tmem + ((uint32_t)(wid & 3) << 21) + kAAt + as * kACols, pairs);
+                    tmem_stored();
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(there + 8 * as);
+                }
+            }
+    } else {
+        if (NH == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
+        const uint32_t there = of_rank(d_empty, leader), column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
+        uint32_t span = 0, turn = 0;
+        bool ok = !a.lost;
+        for (int t = cluster; t < a.tiles; t += clusters, turn++) {
+            // This lane's matrix row among the outputs, and in the matrix (one that exists).
+            const int64_t row = rows_at(t / a.x_tiles) + (GATED ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
+            const int64_t at = (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row;
+            auto scale = [&](int col) {
+                const int64_t g = at + col / a.group;
+                if (a.scale_type == ECASQ_F32) return static_cast<const float *>(a.scales)[g];
+                return a.scale_type == ECASQ_F16 ? to_f32(static_cast<const __half *>(a.scales)[g]) : to_f32(static_cast<const __nv_bfloat16 *>(a.scales)[g]);
+            };
+            float acc[kOwn];
+#pragma unroll
+            for (int c = 0; c < kOwn; c++) acc[c] = 0.f;
+            auto add_span = [&](int col) {
+                const uint32_t job = span * NH + (NH == 2 ? part : 0), buf = job % kDBufs;
+                const float s = scale(min(col, (int)a.k - 1));
+                if (!(ok = wait_warp(d_full + 8 * buf, job / kDBufs & 1))) return;
+                tmem_fence_after();
+                constexpr int kChunk = kOwn == 128 ? 32 : kOwn < 16 ? kOwn : 16;
+#pragma unroll
+                for (int c = 0; c < kOwn; c += kChunk) {
+                    uint32_t d[kChunk];
+                    tmem_load<kChunk>(d, column + buf * ND + c);
+                    if (c + kChunk == kOwn) {
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(there + 8 * buf);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kChunk; j++) acc[c + j] = fmaf(s, __uint_as_float(d[j]), acc[c + j]);
+                }
+                span++;
+            };
+            if (SPANS == 1) {
+                // A group's blocks, or what of them is this pair's.
+                for (int kb = kb0; ok && kb < kb1; kb += a.group_blocks - kb % a.group_blocks) add_span(kb * 128);
+            } else {
+                for (int v = 0; ok && v < per_tile; v++)
+#pragma unroll 1
+                    for (int sub = 0; ok && sub < SPANS; sub++) add_span((kb0 + v / terms) * 128 + sub * (128 / SPANS));
+            }
+            constexpr int kOut = Shape::kOut;
+            float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + (part * 4 + quarter) * kOut * 32;
+            int c0 = 0, c1 = kOut;
+            if (NH == 1 && a.split > 1) {  // each pair takes a share of the columns over all pairs
+                ok = ok && wait_warp(sums_empty, (turn & 1) ^ 1);
+                c0 = (int)pair * kOut / a.split;
+                c1 = (int)(pair + 1) * kOut / a.split;
+            }
+#pragma unroll 1
+            for (int q = 0; q < kOwn / kOut; q++) {
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < kOut; c++) {
+                    float v = acc[c];
+#pragma unroll
+                    for (int p = 1; p < kOwn / kOut; p++) v = q == p ? acc[p * kOut + c] : v;
+                    sums[32 * c + lane] = v;
+                }
+                __syncwarp();
+                if (NH == 1 && a.split > 1) {
+                    if (ok && lane < a.split) mbar_arrive(of_rank(sums_full, 2 * lane + (rank & 1)));
+                    ok = ok && wait_warp(sums_full, turn & 1);
+                }
+                if (!ok)  // all of the tile's results are NaN, and those of the tiles after it
+                    for (int c = 0; c < kOut; c++) sums[32 * c + lane] = CUDART_NAN_F;
+                __syncwarp();
+                const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + part * kOwn + q * kOut;
+                if (a.type == ECASQ_F16) finish<__half, GATED>(a, sums, c0, c1, x0, row, rank);
+                else if (a.type == ECASQ_BF16) finish<__nv_bfloat16, GATED>(a, sums, c0, c1, x0, row, rank);
+                else finish<float, GATED>(a, sums, c0, c1, x0, row, rank);
+            }
+            if (NH == 1 && a.split > 1) {
+                __syncwarp();
+                if (ok && lane < a.split) mbar_arrive(of_rank(sums_empty, 2 * lane + (rank & 1)));
+            }
+        }
+        if (!ok && lane == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
+    }
+    // A block ends when the products that read its memory, and the arrivals that they send, are through.
+    __syncthreads();
+    if (wid == 1 && lane == 0) {
+        if (rank == leader) mma_commit(all_done, (uint16_t)(3u << rank));
+        for (int spin = 0; spin < kTcSpins && !mbar_try(all_done, 0); spin++) {}
+    }
+    __syncthreads();
+    cluster_barrier();
+    if (wid == 3) tmem_free(tmem);
+}
+
+// ---------------------------------------------------------------- x in rows that tile_load can read
+// 16-bit rows copied to rows of `to_row` elements, a multiple of 8; fp32 rows as three bf16 terms, of 8 bits each, in three planes of b rows.
+template <bool F32> __global__ void __launch_bounds__(256) k_lay_out(const void *x, int64_t x_row, int64_t b, int64_t k, uint16_t *to, int64_t to_row) {
+    wait_before();
+    for (int64_t i = blockIdx.y; i < b; i += gridDim.y) {
+        const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (c >= k) continue;
+        if (F32) {
+            float v = static_cast<const float *>(x)[i * x_row + c];
+            const bool finite = fabsf(v) <= 3.402823466e38f;
+#pragma unroll
+            for (int p = 0; p < 3; p++) {
+                const uint32_t bits = __float_as_uint(v) >> 16;
+                to[(p * b + i) * to_row + c] = finite ? (uint16_t)bits : p ? 0 : v == v ? (uint16_t)bits : 0x7FFF;
+                v -= __uint_as_float(bits << 16);
+                if (!finite) v = static_cast<const float *>(x)[i * x_row + c];
+            }
+        } else {
+            to[i * to_row + c] = static_cast<const uint16_t *>(x)[i * x_row + c];
+        }
+    }
+}
+
+int make_tile_map(CUtensorMap *map, CUtensorMapDataType type, const void *at, int64_t cols, int64_t rows, int64_t row_bytes, int box_cols, int box_rows,
+                  CUtensorMapSwizzle swizzle) {
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<void *> found;
+    void *fn = found.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult got;
+        ECASQ_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &got));
+        if (got != cudaDriverEntryPointSuccess || !fn) return ECASQ_ECUDA;
+        found.store(fn, std::memory_order_release);
+    }
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    const CUresult rc = reinterpret_cast<Encode>(fn)(map, type, 2, const_cast<void *>(at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? ECASQ_OK : ECASQ_ECUDA;
+}
+
+// The rows of x that lie in the workspace, and how far apart.
+static int64_t laid_row(int64_t k) { return (k + 7) / 8 * 8; }
+size_t project_tc_room(int64_t b, int64_t k, int32_t type) { return align256((size_t)(b * laid_row(k)) * 2 * (type == ECASQ_F32 ? 3 : 1)); }
+
+// Clusters of `size` blocks that the card holds at once, asked once a device.
+template <typename K> static int tc_held(K *kernel, int size, int threads, int smem, std::atomic<int> *known, int *held) {
+    int device = 0;
+    ECASQ_CUDA_TRY(cudaGetDevice(&device));
+    *held = device < kDevices ? known[device].load(std::memory_order_acquire) : 0;
+    if (*held > 0) return ECASQ_OK;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)size);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ECASQ_CUDA_TRY(cudaOccupancyMaxActiveClusters(held, kernel, &cfg));
+    if (*held < 1) return ECASQ_ECUDA;
+    if (device < kDevices) known[device].store(*held, std::memory_order_release);
+    return ECASQ_OK;
+}
+
+template <int ND, int NH, bool GATED, int SPANS> static int launch_tc(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
+    using Shape = TcShape<ND, NH>;
+    static_assert(Shape::kBytes <= 227 * 1024 && Shape::kBytes > 114 * 1024, "one block an SM: tensor memory is the block's alone");
+    static std::atomic<int> allowed[kDevices], known[3][kDevices];
+    auto *kernel = k_project_tc<ND, NH, GATED, SPANS>;
+    int rc = allow_smem(kernel, Shape::kBytes, allowed), held = 0;
+    if (!rc) rc = tc_held(kernel, 2 * a.split, Shape::kThreads, Shape::kBytes, known[a.split / 2], &held);
+    if (rc) return rc;
+    const int clusters = std::min(a.tiles, held);
+    return launch_clusters(kernel, dim3((unsigned)(clusters * 2 * a.split)), dim3((unsigned)(2 * a.split)), Shape::kThreads, Shape::kBytes, st, xm, cm, a);
+}
+template <int ND, int NH, bool GATED> static int launch_tc_spans(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
+    // The tensor core's fp32 sums are cut off, not rounded, at each step: of fp32 operands they are taken out after every 32 columns (an error
+    // of 2.8e-7 of the result for k = 1024; after six products of 128, 2.1e-6).
+    if (a.group % 128 == 0 && a.type != ECASQ_F32) return launch_tc<ND, NH, GATED, 1>(xm, cm, a, st);
+    if (a.group % 64 == 0 && a.type != ECASQ_F32) return launch_tc<ND, NH, GATED, 2>(xm, cm, a, st);
+    return launch_tc<ND, NH, GATED, 4>(xm, cm, a, st);
+}
+
+int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st) {
+    const bool f32 = p.type == ECASQ_F32;
+    const void *x = p.x;
+    int64_t x_row = p.x_row;
+    if (f32 || !aligned16(p.x) || (p.b > 1 && p.x_row % 8)) {
+        if (!ws || ws_bytes < project_tc_room(p.b, p.k, p.type) || !aligned16(ws)) return ECASQ_EWORKSPACE;
+        const dim3 grid((unsigned)cdiv(p.k, 256), (unsigned)std::min<int64_t>(p.b, 4096));
+        const int rc = f32 ? launch_early(k_lay_out<true>, grid, 256, 0, st, p.x, p.x_row, p.b, p.k, static_cast<uint16_t *>(ws), laid_row(p.k))
+                           : launch_early(k_lay_out<false>, grid, 256, 0, st, p.x, p.x_row, p.b, p.k, static_cast<uint16_t *>(ws), laid_row(p.k));
+        if (rc) return rc;
+        x = ws;
+        x_row = laid_row(p.k);
+    }
+    const int64_t rows = p.gated ? 2 * p.n : p.n;
+    TcArgs a{};
+    a.levels = p.levels;
+    a.scales = p.scales;
+    a.y = p.y;
+    a.status = p.status;
+    a.scale_row = p.scale_row;
+    a.y_row = p.y_row;
+    a.n = p.n;
+    a.b = p.b;
+    a.k = p.k;
+    a.second = p.n;
+    a.m = p.m;
+    a.group = p.group;
+    a.type = p.type;
+    a.scale_type = p.scale_type;
+    a.blocks = (int32_t)cdiv(p.k, 128);
+    a.group_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.group / 128, a.blocks));
+    a.lost = p.lost;
+    a.epi = p.epi;
+    const int64_t w_tiles = cdiv(p.n, p.gated ? 128 : 256);
+    const int width = p.b <= 32 ? 32 : p.b <= 64 ? 64 : p.b <= 128 ? 128 : 256;
+    a.x_tiles = (int32_t)cdiv(p.b, width);
+    const int64_t tiles = w_tiles * a.x_tiles;
+    if (tiles > INT32_MAX) return ECASQ_EINVAL;
+    a.tiles = (int32_t)tiles;
+    a.split = 1;
+    if (width < 256)
+        while (a.split < 4 && tiles * 2 * a.split <= 76 && 2 * a.split <= a.blocks) a.split *= 2;
+    CUtensorMap xm, cm;
+    const int nd = width == 256 ? 128 : width;
+    int rc = make_tile_map(&xm, p.type == ECASQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, p.k, f32 ? 3 * p.b : p.b,
+                           (p.b > 1 || f32 ? x_row : laid_row(p.k)) * 2, 64, nd / 2, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (!rc) rc = make_tile_map(&cm, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.codes, 64 * cdiv(p.k, 128), rows, p.code_row, 64, 64, CU_TENSOR_MAP_SWIZZLE_64B);
+    if (rc) return rc;
+    switch (width) {
+        case 32: return p.gated ? launch_tc_spans<32, 1, true>(xm, cm, a, st) : launch_tc_spans<32, 1, false>(xm, cm, a, st);
+        case 64: return p.gated ? launch_tc_spans<64, 1, true>(xm, cm, a, st) : launch_tc_spans<64, 1, false>(xm, cm, a, st);
+        case 128: return p.gated ? launch_tc_spans<128, 1, true>(xm, cm, a, st) : launch_tc_spans<128, 1, false>(xm, cm, a, st);
+        default: return p.gated ? launch_tc_spans<128, 2, true>(xm, cm, a, st) : launch_tc_spans<128, 2, false>(xm, cm, a, st);
+    }
+}
+
+}  // namespace ecasq
