@@ -21,11 +21,12 @@ struct TcArgs {
     int32_t group_blocks;   // blocks of a scale group, where it holds whole ones
     int32_t split;          // pairs of a cluster that share the columns
     int32_t x_tiles, tiles; // tiles of rows of x; of the product
+    uint32_t div_mul, div_shift;  // words of 32 columns to scale groups (FastDiv of group / 32)
+    bool wide;              // y and the residual in 16-byte pieces
     uint32_t lost;          // test hook: 1 where blocks begin as if a wait had run out
     Epilogue epi;
 };
 
-constexpr int kTcSpins = 1 << 18;  // of a wait, each of some microseconds at most: about two seconds
 constexpr int kDBufs = 3;          // sums in tensor memory; behind them 4 stages of 64 columns of levels
 constexpr int kACols = 32, kAStages = 4, kAAt = 512 - kAStages * kACols;
 constexpr int kCodeStage = 128 * 64;
@@ -41,8 +42,8 @@ template <int ND, int NH> struct TcShape {
     static constexpr int kXStages = kN >= 128 ? 5 : kN == 64 ? 10 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 8 : 12;
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
     static constexpr int kOut = NH == 2 ? 32 : kOwn;              // of them at a time on their way out through shared memory
-    static constexpr int kSums = 8 * kOut * 32 * 4;               // what the eight warps have on their way out
-    static constexpr int kBars = 3 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
+    static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
+    static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
     static constexpr int kTablesAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTablesAt + 128, kBarsAt = kSumsAt + kSums;
     static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
 };
@@ -67,39 +68,89 @@ __device__ __forceinline__ void decode(uint32_t w, const uint32_t (&t)[8], uint3
     }
 }
 
-// What sums become, of columns c0 to c1 on their way out, which are rows of x from x0 on, and matrix row `row` of this lane (gated: the
-// gate's in the lower half of a warp, the other's in the upper).  sums: entry (c, lane) at 32 c + lane; of split > 1 pairs of the cluster they
-// are added up.
-template <typename T, bool GATED>
-__device__ __forceinline__ void finish(const TcArgs &a, const float *sums, int c0, int c1, int64_t x0, int64_t row, uint32_t rank) {
-    const int lane = threadIdx.x & 31;
-    auto sum = [&](int at) {
-        if (a.split == 1) return sums[at];
-        float v = 0.f;
-        for (int p = 0; p < a.split; p++) {
-            float of;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(of) : "r"(of_rank(shared_at(sums + at), 2 * p + (rank & 1))) : "memory");
-            v += of;
-        }
-        return v;
-    };
-    if (row >= a.n) return;
-    T *y = static_cast<T *>(a.y) + row;
-    if (GATED) {
-        // The lower lanes take the even columns, the upper ones the odd.
-        for (int c = c0 + (lane >> 4); c < c1 && x0 + c < a.b; c += 2)
-            y[(x0 + c) * a.y_row] = from_f32<T>(activate(sum(32 * c + (lane & 15)), a.epi.act) * sum(32 * c + 16 + (lane & 15)));
-    } else {
-        const float bias = a.epi.bias ? to_f32(static_cast<const T *>(a.epi.bias)[row]) : 0.f;
-        const T *residual = static_cast<const T *>(a.epi.residual) + (a.epi.residual ? row : 0);
-        const int end = (int)min((int64_t)c1, a.b - x0);
-        for (int c = c0; c < end; c += 8) {
-            float r[8];
+// Eight values of T in memory, in 16-byte pieces.
+template <typename T> struct Eight {
+    T v[8];
+};
+template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T *p) {
+    alignas(16) Eight<T> e;
 #pragma unroll
-            for (int j = 0; j < 8; j++) r[j] = a.epi.residual && c + j < end ? to_f32(residual[(x0 + c + j) * a.epi.residual_row]) : 0.f;
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<uint4 *>(e.v)[i] = reinterpret_cast<const uint4 *>(p)[i];
+    return e;
+}
+template <typename T> __device__ __forceinline__ void store_eight(T *p, const Eight<T> &from) {
+    alignas(16) Eight<T> e = from;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e.v)[i];
+}
+
+// What four warps' sums become: columns c0 to c1 of those on their way out, which are rows of x from x0 on, for the block's matrix rows from r0
+// on.  sums: entry (column c, matrix row r of the block) at 128 c + r; over split > 1 pairs of the cluster they are added up.  A thread takes eight neighbouring
+// outputs of a row of x, so that a row's 64 or 128 outputs leave in 16-byte pieces one beside another (each matrix row's outputs on their own, 64 bytes a warp, took
+// 60 us a tile of 256 x 256).  Of a gated matrix a warp had 16 rows of the gate and the same 16 of the other half.
+template <typename T, bool GATED>
+__device__ __forceinline__ void finish(const TcArgs &a, const float *sums, int c0, int c1, int64_t x0, int64_t r0, uint32_t rank) {
+    constexpr int kLanes = GATED ? 8 : 16, kAtOnce = 128 / kLanes;  // threads of a row of x; rows of x at once
+    const int tid = threadIdx.x & 127, part = tid % kLanes, end = (int)min((int64_t)c1, a.b - x0);
+    const int from = GATED ? 32 * (part >> 1) + 8 * (part & 1) : 8 * part;
+    const int64_t row = r0 + 8 * part;
+    const bool whole = a.wide && row + 8 <= a.n;
+    auto eight = [&](int at, float (&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = 0.f;
+        for (int p = 0; p < a.split; p++)
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                float4 f;
+                if (a.split == 1) {
+                    f = *reinterpret_cast<const float4 *>(sums + at + j);
+                } else {
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                                 : "r"(of_rank(shared_at(sums + at + j), 2 * p + (rank & 1))) : "memory");
+                }
+                v[j] += f.x;
+                v[j + 1] += f.y;
+                v[j + 2] += f.z;
+                v[j + 3] += f.w;
+            }
+    };
+    float bias[8];
+    const bool biased = !GATED && a.epi.bias;
+#pragma unroll
+    for (int j = 0; j < 8; j++) bias[j] = biased && row + j < a.n ? to_f32(static_cast<const T *>(a.epi.bias)[row + j]) : 0.f;
+    if (row >= a.n) return;
+#pragma unroll 1
+    for (int c = c0 + tid / kLanes; c < end; c += kAtOnce) {
+        T *y = static_cast<T *>(a.y) + (x0 + c) * a.y_row + row;
+        Eight<T> out;
+        float v[8];
+        eight(128 * c + from, v);
+        if (GATED) {
+            float u[8];
+            eight(128 * c + from + 16, u);
+#pragma unroll
+            for (int j = 0; j < 8; j++) out.v[j] = from_f32<T>(activate(v[j], a.epi.act) * u[j]);
+        } else {
+            Eight<T> residual;
+            const T *r = static_cast<const T *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
+            if (!a.epi.residual) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) residual.v[j] = from_f32<T>(0.f);
+            } else if (whole) {
+                residual = load_eight(r);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; j++) residual.v[j] = row + j < a.n ? r[j] : from_f32<T>(0.f);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j++) out.v[j] = from_f32<T>(activate(v[j] + bias[j], a.epi.act) + to_f32(residual.v[j]));
+        }
+        if (whole) {
+            store_eight(y, out);
+        } else {
 #pragma unroll
             for (int j = 0; j < 8; j++)
-                if (c + j < end) y[(x0 + c + j) * a.y_row] = from_f32<T>(activate(sum(32 * (c + j) + lane) + bias, a.epi.act) + r[j]);
+                if (row + j < a.n) y[j] = out.v[j];
         }
     }
 }
@@ -118,7 +169,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const uint32_t rank = cluster_rank(), leader = rank & ~1u, size = 2 * a.split, pair = rank / 2;
     const uint32_t bars = base + Shape::kBarsAt;
-    const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, x_other = x_empty + 8 * kXStages, c_full = x_other + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
+    const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
                    a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
                    all_done = d_empty + 8 * kDBufs, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
     uint32_t *tables = reinterpret_cast<uint32_t *>(smem + Shape::kTablesAt);
@@ -135,23 +186,25 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
         return v != 0;
     };
     // A wait ends when its phase has, or with the loss of the block's work: when the limit has run out here or elsewhere in the cluster.
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (mbar_try(bar, parity)) return true;
-        for (int i = 0; i < kTcSpins; i++) {
-            if (lost()) return false;
-            if (mbar_try(bar, parity)) return true;
-        }
+    auto wait_for = [&](auto look) {
+        if (look()) return true;
+        for (uint64_t t0 = nanoseconds(); nanoseconds() - t0 < kWaitMost;)
+            for (int i = 0; i < 64; i++) {
+                if (look()) return true;
+                if (lost()) return false;
+            }
         lose();
         return false;
     };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return wait_for([&] { return mbar_try(bar, parity); }); };
     auto wait_warp = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
+    auto wait_cluster = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait_for([&] { return mbar_try<true>(bar, parity); })); };
 
     wait_before();
     if (tid == 0) {
         for (int i = 0; i < kXStages; i++) {
-            mbar_init(x_full + 8 * i, 1);
+            mbar_init(x_full + 8 * i, rank == leader ? 2 : 1);  // this block's copies, and the other's word that its are there
             mbar_init(x_empty + 8 * i, 1);
-            mbar_init(x_other + 8 * i, 1);
         }
         for (int i = 0; i < kCodeStages; i++) {
             mbar_init(c_full + 8 * i, 1);
@@ -202,7 +255,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
     const int per_tile = (kb1 - kb0) * terms;  // products' blocks of a tile
 
     if (wid < 4) {
-        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         if (lane == 0 && !a.lost) {
             if (wid == 0) {  // rows of x
                 uint32_t i = 0;
@@ -222,8 +275,9 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                                 tile_load(to + (2 * h + q) * (ND / 2 * 128), &xm, kb * 128 + 64 * q, (int32_t)(from + h * ND), x_full + 8 * s);
                     }
                 }
+                const uint64_t t0 = nanoseconds();
                 for (uint32_t j = i > kXStages ? i - kXStages : 0; j < i; j++)  // none is on its way when the block ends
-                    for (int spin = 0; spin < kTcSpins && !mbar_try(x_full + 8 * (j % kXStages), j / kXStages & 1); spin++) {}
+                    mbar_drain(x_full + 8 * (j % kXStages), j / kXStages & 1, t0);
             } else if (wid == 2) {  // codes
                 uint32_t i = 0;
                 bool ok = true;
@@ -238,75 +292,99 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                         tile_load(to + kCodeStage / 2, &cm, kb * 64, (int32_t)(r0 + (GATED ? a.second : 64)), c_full + 8 * s);
                     }
                 }
-                for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++)
-                    for (int spin = 0; spin < kTcSpins && !mbar_try(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1); spin++) {}
+                const uint64_t t0 = nanoseconds();
+                for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++) mbar_drain(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1, t0);
             } else if (wid == 3 && rank != leader) {  // tells the first block of the pair that this one's rows of x are there
                 uint32_t i = 0;
                 bool ok = true;
-                const uint32_t there = of_rank(x_other, leader);
+                const uint32_t there = of_rank(x_full, leader);
                 for (int t = cluster; ok && t < a.tiles; t += clusters)
                     for (int v = 0; ok && v < per_tile; v++, i++)
                         if ((ok = wait(x_full + 8 * (i % kXStages), i / kXStages & 1))) mbar_arrive(there + 8 * (i % kXStages));
-            } else if (wid == 1 && rank == leader) {  // products
-                const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
-                const uint16_t both = (uint16_t)(3u << rank);
-                uint32_t i = 0, span = 0;
-                bool ok = true;
-                auto d_of = [&](uint32_t job) { return tmem + job % kDBufs * ND; };
-                auto open = [&](uint32_t job) {
-                    const bool free = wait(d_empty + 8 * (job % kDBufs), (job / kDBufs & 1) ^ 1);
-                    tmem_fence_after();
-                    return free;
-                };
-                for (int t = cluster; ok && t < a.tiles; t += clusters) {
-                    int in_group = kb0 % a.group_blocks;
-                    bool fresh = true;
-                    for (int v = 0; ok && v < per_tile; v++, i++) {
-                        const uint32_t xs = i % kXStages, xp = i / kXStages & 1, x = base + xs * Shape::kXStage;
-                        if (!(ok = wait(x_full + 8 * xs, xp) && wait(x_other + 8 * xs, xp))) break;
-                        // The product of 16 entries number kk of the block with half h of the rows of x.
-                        auto step = [&](uint32_t d, int h, int kk, bool add) {
-                            const uint32_t as = (2 * i + kk / 4) % kAStages;
-                            mma_pair(d, tmem + kAAt + as * kACols + kk % 4 * 8, mma_rows(x + (2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32), kind, add);
-                        };
-                        auto levels = [&](int hb) {
-                            const uint32_t j = 2 * i + hb;
-                            const bool there = wait(a_full + 8 * (j % kAStages), j / kAStages & 1);
-                            tmem_fence_after();
-                            return there;
-                        };
-                        if (SPANS == 1) {
-                            const bool last = v + 1 == per_tile || (v % terms == terms - 1 && in_group + 1 == a.group_blocks);
-                            for (int h = 0; ok && h < NH; h++) {
-                                const uint32_t job = span * NH + h;
-                                if (fresh && !(ok = open(job))) break;
-                                for (int hb = 0; hb < 2; hb++) {
-                                    if (h == 0 && !(ok = levels(hb))) break;
+            }
+        }
+        if (wid == 1 && rank == leader) {  // products: the whole warp, so that addresses stay in uniform registers
+            const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
+            const uint16_t both = (uint16_t)(3u << rank);
+            uint32_t xs = 0, x_parity = 0, as = 0, a_parity = 0, buf = 0, d_parity = 1;
+            bool ok = !a.lost;
+            // The next buffer for sums, once it is free.
+            auto open = [&](uint32_t &d, uint32_t &full) {
+                const bool free = wait_warp(d_empty + 8 * buf, d_parity);
+                tmem_fence_after();
+                d = tmem + buf * ND;
+                full = d_full + 8 * buf;
+                buf = buf + 1 == kDBufs ? 0 : buf + 1;
+                d_parity ^= buf == 0;
+                return free;
+            };
+            auto levels = [&](int hb) {
+                const bool there = wait_warp(a_full + 8 * (as + hb), a_parity);
+                tmem_fence_after();
+                return there;
+            };
+            for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                int in_group = kb0 % a.group_blocks, term = 0;
+                bool fresh = true;
+                uint32_t d[NH], full[NH];
+                for (int v = 0; v < per_tile; v++) {
+                    const uint32_t x = mma_rows(base + xs * Shape::kXStage), levels_at = tmem + kAAt + as * kACols;
+                    if (!(ok = wait_warp(x_full + 8 * xs, x_parity) && levels(0))) break;
+                    // The products of 16 entries number k0 .. k1 of the block with half h of the rows of x.
+                    auto steps = [&](uint32_t to, int h, int k0, int k1, bool add) {
 #pragma unroll
-                                    for (int kk = 0; kk < 4; kk++) step(d_of(job), h, 4 * hb + kk, !fresh || hb || kk);
-                                    if (h == NH - 1) mma_commit(a_empty + 8 * ((2 * i + hb) % kAStages), both);
-                                }
-                                if (ok && last) mma_commit(d_full + 8 * (job % kDBufs), both);
-                            }
-                            fresh = last;
-                            if (last) span++;
-                        } else {
-                            for (int hb = 0; ok && hb < 2; hb++) {
-                                if (!(ok = levels(hb))) break;
-                                for (int sub = 0; ok && sub < SPANS / 2; sub++, span++)
-                                    for (int h = 0; ok && h < NH; h++) {
-                                        const uint32_t job = span * NH + h;
-                                        if (!(ok = open(job))) break;
-#pragma unroll
-                                        for (int kk = 0; kk < 8 / SPANS; kk++) step(d_of(job), h, 4 * hb + sub * (8 / SPANS) + kk, kk > 0);
-                                        mma_commit(d_full + 8 * (job % kDBufs), both);
-                                    }
-                                if (ok) mma_commit(a_empty + 8 * ((2 * i + hb) % kAStages), both);
+                        for (int kk = k0; kk < k1; kk++)
+                            mma_pair(to, levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
+                    };
+                    if (SPANS == 1) {
+                        const bool last = v + 1 == per_tile || (term == terms - 1 && in_group + 1 == a.group_blocks);
+                        if (fresh && !(ok = open(d[0], full[0]))) break;
+                        if (one_lane()) steps(d[0], 0, 0, 4, !fresh);
+                        if (!(ok = levels(1))) break;
+                        if (one_lane()) {
+                            steps(d[0], 0, 4, 8, true);
+                            if (last) mma_commit(full[0], both);
+                        }
+                        if (NH == 2) {
+                            if (fresh && !(ok = open(d[NH - 1], full[NH - 1]))) break;
+                            if (one_lane()) {
+                                steps(d[NH - 1], NH - 1, 0, 4, !fresh);
+                                mma_commit(a_empty + 8 * as, both);
+                                steps(d[NH - 1], NH - 1, 4, 8, true);
+                                if (last) mma_commit(full[NH - 1], both);
                             }
                         }
-                        if (ok) mma_commit(x_empty + 8 * xs, both);
-                        if (v % terms == terms - 1 && ++in_group == a.group_blocks) in_group = 0;
+                        if (one_lane()) {
+                            if (NH == 1) mma_commit(a_empty + 8 * as, both);
+                            mma_commit(a_empty + 8 * as + 8, both);
+                            mma_commit(x_empty + 8 * xs, both);
+                        }
+                        fresh = last;
+                    } else {
+#pragma unroll
+                        for (int sub = 0; sub < SPANS; sub++) {
+                            if (sub == SPANS / 2 && !(ok = ok && levels(1))) break;
+#pragma unroll
+                            for (int h = 0; h < NH; h++) {
+                                if (!(ok = ok && open(d[h], full[h]))) break;
+                                if (one_lane()) {
+                                    steps(d[h], h, sub * (8 / SPANS), (sub + 1) * (8 / SPANS), false);
+                                    mma_commit(full[h], both);
+                                    if (h == NH - 1 && (sub + 1) % (SPANS / 2) == 0) mma_commit(a_empty + 8 * (as + sub / (SPANS / 2)), both);
+                                    if (h == NH - 1 && sub == SPANS - 1) mma_commit(x_empty + 8 * xs, both);
+                                }
+                            }
+                        }
+                        if (!ok) break;
                     }
+                    if (++term == terms) {
+                        term = 0;
+                        if (++in_group == a.group_blocks) in_group = 0;
+                    }
+                    xs = xs + 1 == kXStages ? 0 : xs + 1;
+                    x_parity ^= xs == 0;
+                    as ^= 2;
+                    a_parity ^= as == 0;
                 }
             }
         }
@@ -352,27 +430,30 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                 }
             }
     } else {
-        if (NH == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        if (NH == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
         const uint32_t there = of_rank(d_empty, leader), column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
-        uint32_t span = 0, turn = 0;
+        uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0;
         bool ok = !a.lost;
         for (int t = cluster; t < a.tiles; t += clusters, turn++) {
-            // This lane's matrix row among the outputs, and in the matrix (one that exists).
-            const int64_t row = rows_at(t / a.x_tiles) + (GATED ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
-            const int64_t at = (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row;
-            auto scale = [&](int col) {
-                const int64_t g = at + col / a.group;
+            // This lane's matrix row among the outputs, and its scales in the matrix (of one that exists).
+            const int64_t r0 = rows_at(t / a.x_tiles), row = r0 + (GATED ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
+            const int64_t scales_at = (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row;
+            auto scale = [&](int word) {  // of a word of 32 columns
+                const uint32_t w = min((uint32_t)word, (uint32_t)((a.k - 1) / 32));
+                const int64_t g = scales_at + (a.div_mul ? __umulhi(w, a.div_mul) >> a.div_shift : w >> a.div_shift);
                 if (a.scale_type == ECASQ_F32) return static_cast<const float *>(a.scales)[g];
                 return a.scale_type == ECASQ_F16 ? to_f32(static_cast<const __half *>(a.scales)[g]) : to_f32(static_cast<const __nv_bfloat16 *>(a.scales)[g]);
             };
             float acc[kOwn];
 #pragma unroll
             for (int c = 0; c < kOwn; c++) acc[c] = 0.f;
-            auto add_span = [&](int col) {
-                const uint32_t job = span * NH + (NH == 2 ? part : 0), buf = job % kDBufs;
-                const float s = scale(min(col, (int)a.k - 1));
-                if (!(ok = wait_warp(d_full + 8 * buf, job / kDBufs & 1))) return;
+            // A group's sums, or what of them is this pair's; the next one's scale is on its way meanwhile.
+            float next = scale(4 * kb0);
+            auto add_span = [&](int next_word) {
+                const float s = next;
+                next = scale(next_word);
+                if (!(ok = wait_warp(d_full + 8 * buf, d_parity))) return;
                 tmem_fence_after();
                 constexpr int kChunk = kOwn == 128 ? 32 : kOwn < 16 ? kOwn : 16;
 #pragma unroll
@@ -387,50 +468,62 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
 #pragma unroll
                     for (int j = 0; j < kChunk; j++) acc[c + j] = fmaf(s, __uint_as_float(d[j]), acc[c + j]);
                 }
-                span++;
+                buf += NH;
+                if (buf >= kDBufs) {
+                    buf -= kDBufs;
+                    d_parity ^= 1;
+                }
             };
             if (SPANS == 1) {
-                // A group's blocks, or what of them is this pair's.
-                for (int kb = kb0; ok && kb < kb1; kb += a.group_blocks - kb % a.group_blocks) add_span(kb * 128);
+                for (int kb = kb0; ok && kb < kb1;) {
+                    kb += a.group_blocks - kb % a.group_blocks;
+                    add_span(4 * kb);
+                }
             } else {
-                for (int v = 0; ok && v < per_tile; v++)
+                for (int v = 0, term = 0, kb = kb0; ok && v < per_tile; v++) {
+                    const bool on = ++term == terms;
 #pragma unroll 1
-                    for (int sub = 0; ok && sub < SPANS; sub++) add_span((kb0 + v / terms) * 128 + sub * (128 / SPANS));
+                    for (int sub = 1; ok && sub <= SPANS; sub++) add_span(4 * (sub == SPANS && on ? kb + 1 : kb) + (sub == SPANS ? 0 : sub * (4 / SPANS)));
+                    if (on) {
+                        term = 0;
+                        kb++;
+                    }
+                }
             }
             constexpr int kOut = Shape::kOut;
-            float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + (part * 4 + quarter) * kOut * 32;
+            float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * kOut * 128;
+            auto four_warps = [&] { asm volatile("bar.sync %0, 128;" ::"r"(1 + part) : "memory"); };
             int c0 = 0, c1 = kOut;
             if (NH == 1 && a.split > 1) {  // each pair takes a share of the columns over all pairs
-                ok = ok && wait_warp(sums_empty, (turn & 1) ^ 1);
+                ok = ok && wait_cluster(sums_empty, (turn & 1) ^ 1);
                 c0 = (int)pair * kOut / a.split;
                 c1 = (int)(pair + 1) * kOut / a.split;
             }
 #pragma unroll 1
             for (int q = 0; q < kOwn / kOut; q++) {
-                __syncwarp();
+                four_warps();
 #pragma unroll
                 for (int c = 0; c < kOut; c++) {
                     float v = acc[c];
 #pragma unroll
                     for (int p = 1; p < kOwn / kOut; p++) v = q == p ? acc[p * kOut + c] : v;
-                    sums[32 * c + lane] = v;
+                    sums[128 * c + 32 * quarter + lane] = ok ? v : CUDART_NAN_F;  // (a lost tile's results are NaN, and those of the tiles after it)
                 }
-                __syncwarp();
                 if (NH == 1 && a.split > 1) {
-                    if (ok && lane < a.split) mbar_arrive(of_rank(sums_full, 2 * lane + (rank & 1)));
-                    ok = ok && wait_warp(sums_full, turn & 1);
+                    __syncwarp();
+                    if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_full, 2 * lane + (rank & 1)));
+                    if (!(ok = ok && wait_cluster(sums_full, turn & 1)))
+                        for (int c = 0; c < kOut; c++) sums[128 * c + 32 * quarter + lane] = CUDART_NAN_F;
                 }
-                if (!ok)  // all of the tile's results are NaN, and those of the tiles after it
-                    for (int c = 0; c < kOut; c++) sums[32 * c + lane] = CUDART_NAN_F;
-                __syncwarp();
+                four_warps();
                 const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + part * kOwn + q * kOut;
-                if (a.type == ECASQ_F16) finish<__half, GATED>(a, sums, c0, c1, x0, row, rank);
-                else if (a.type == ECASQ_BF16) finish<__nv_bfloat16, GATED>(a, sums, c0, c1, x0, row, rank);
-                else finish<float, GATED>(a, sums, c0, c1, x0, row, rank);
+                if (a.type == ECASQ_F16) finish<__half, GATED>(a, sums, c0, c1, x0, r0, rank);
+                else if (a.type == ECASQ_BF16) finish<__nv_bfloat16, GATED>(a, sums, c0, c1, x0, r0, rank);
+                else finish<float, GATED>(a, sums, c0, c1, x0, r0, rank);
             }
             if (NH == 1 && a.split > 1) {
                 __syncwarp();
-                if (ok && lane < a.split) mbar_arrive(of_rank(sums_empty, 2 * lane + (rank & 1)));
+                if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_empty, 2 * lane + (rank & 1)));
             }
         }
         if (!ok && lane == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
@@ -439,7 +532,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
     __syncthreads();
     if (wid == 1 && lane == 0) {
         if (rank == leader) mma_commit(all_done, (uint16_t)(3u << rank));
-        for (int spin = 0; spin < kTcSpins && !mbar_try(all_done, 0); spin++) {}
+        mbar_drain(all_done, 0, nanoseconds());
     }
     __syncthreads();
     cluster_barrier();
@@ -566,6 +659,11 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     a.group_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.group / 128, a.blocks));
     a.lost = p.lost;
     a.epi = p.epi;
+    const FastDiv div(p.group / 32);
+    a.div_mul = div.mul;
+    a.div_shift = div.shift;
+    const int64_t pieces = 16 / type_size(p.type);
+    a.wide = aligned16(p.y) && (p.b == 1 || p.y_row % pieces == 0) && (!p.epi.residual || (aligned16(p.epi.residual) && (p.b == 1 || p.epi.residual_row % pieces == 0)));
     const int64_t w_tiles = cdiv(p.n, p.gated ? 128 : 256);
     const int width = p.b <= 32 ? 32 : p.b <= 64 ? 64 : p.b <= 128 ? 128 : 256;
     a.x_tiles = (int32_t)cdiv(p.b, width);

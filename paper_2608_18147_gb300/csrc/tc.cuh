@@ -14,18 +14,46 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 
+// One lane of a warp that is together, the same each time; the compiler keeps what it computes in uniform registers.
+__device__ __forceinline__ bool one_lane() {
+    uint32_t is;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(is));
+    return is;
+}
+
 // ---------------------------------------------------------------- barriers
 __device__ __forceinline__ void mbar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// `bar`: an address in the cluster (of_rank); an own one's address is one too.
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+// An arrival, here or at another block of the cluster (`bar`: an address in the cluster; an own one's address is one too), and the look whether a
+// phase is over.  What they order: tensor memory with its fences, tiles brought in by copies, and the block's own shared memory.  The
+// forms that order all of the cluster's memory (CLUSTER) wait for every store on its way and drop cached lines: with them everywhere a
+// product took five times as long.
+template <bool CLUSTER = false> __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    if (CLUSTER) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+template <bool CLUSTER = false> __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
-                 : "=r"(done) : "r"(bar), "r"(parity), "r"(1000) : "memory");
+    if (CLUSTER)
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done;
+}
+
+// Nanoseconds, for the limits of waits.
+__device__ __forceinline__ uint64_t nanoseconds() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+constexpr uint64_t kWaitMost = 2000000000;  // of a wait: two seconds
+
+// Waits for a phase, until kWaitMost after t0.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, uint64_t t0) {
+    while (!mbar_try(bar, parity) && nanoseconds() - t0 < kWaitMost) {}
 }
 
 // ---------------------------------------------------------------- tensor memory
@@ -72,14 +100,15 @@ __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.s
 __host__ __device__ constexpr uint32_t mma_kind(bool bf16, int m, int n) {
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
-// Operand in shared memory: rows of 128 bytes, eight to a 1024-byte block in the 128-byte swizzle, blocks one after another.
-__device__ __forceinline__ uint64_t mma_rows(uint32_t at) {
-    return (uint64_t)(at >> 4 & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// Operand in shared memory: rows of 128 bytes, eight to a 1024-byte block in the 128-byte swizzle, blocks one after another.  The low word of its
+// descriptor, to which a distance in 16 bytes can be added; the high word is the same for all.
+__device__ __forceinline__ uint32_t mma_rows(uint32_t at) { return at >> 4 | 1u << 16; }
+constexpr uint32_t kMmaRowsHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
 // D (+)= A B^T over 16 entries of the summed index, for a pair of blocks: A in tensor memory, 128 rows in each; B in shared memory, half of
 // the rows in each.
-__device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a, uint64_t b, uint32_t kind, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p; }" ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+__device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t kind, bool add) {
+    asm volatile("{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b),
+                 "r"(kind), "r"((uint32_t)add), "n"(kMmaRowsHigh)
                  : "memory");
 }
 // An arrival at this barrier in the blocks of `mask`, once all products issued before have been done.
