@@ -5,6 +5,7 @@
 // come out of tensor memory, are multiplied by their row's scale, which is one number a thread there, and are added up in registers.  So
 // products and scales are as exact as in ecasq_matvec: nothing is rounded before the end.
 #include <algorithm>
+#include <type_traits>
 
 #include "project.cuh"
 #include "tc.cuh"
@@ -22,7 +23,7 @@ struct TcArgs {
     int32_t split;          // pairs of a cluster that share the columns
     int32_t x_tiles, tiles; // tiles of rows of x; of the product
     uint32_t div_mul, div_shift;  // words of 32 columns to scale groups (FastDiv of group / 32)
-    bool wide;              // y and the residual in 16-byte pieces
+    bool wide;              // y and the residual in pieces of four values
     uint32_t lost;          // test hook: 1 where blocks begin as if a wait had run out
     Epilogue epi;
 };
@@ -34,17 +35,19 @@ constexpr int kCodeStage = 128 * 64;
 // fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.
 __device__ __constant__ const int8_t kXTerm[6] = {0, 0, 0, 1, 1, 2}, kLevelTerm[6] = {0, 1, 2, 0, 1, 0};
 
-// ND columns (rows of x) a product, NH of them a tile; SPANS scale groups' sums in a block of 128 columns, at least one.
-template <int ND, int NH> struct TcShape {
+// ND columns (rows of x) a product, NH of them a tile.  F32: fp32 operands as bf16 terms, whose levels are found by byte permutes; those of 16-bit
+// types by lookups in a table of pairs.
+template <int ND, int NH, bool F32> struct TcShape {
     static constexpr int kN = ND * NH;
     static constexpr int kDecodeWarps = NH == 2 ? 4 : 8, kWarps = 4 + kDecodeWarps + 8, kThreads = 32 * kWarps;
     static constexpr int kXStage = kN / 2 * 256;
-    static constexpr int kXStages = kN >= 128 ? 5 : kN == 64 ? 10 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 8 : 12;
+    static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
+    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 8 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 10 : 12;
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
     static constexpr int kOut = NH == 2 ? 32 : kOwn;              // of them at a time on their way out through shared memory
     static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
     static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
-    static constexpr int kTablesAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTablesAt + 128, kBarsAt = kSumsAt + kSums;
+    static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kBooksAt = kSumsAt + kSums, kBarsAt = kBooksAt + 128;
     static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
 };
 
@@ -68,100 +71,101 @@ __device__ __forceinline__ void decode(uint32_t w, const uint32_t (&t)[8], uint3
     }
 }
 
-// Eight values of T in memory, in 16-byte pieces.
-template <typename T> struct Eight {
-    T v[8];
+// Four values of T in memory, 8 or 16 bytes.
+template <typename T> struct alignas(4 * sizeof(T)) Four {
+    T v[4];
 };
-template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T *p) {
-    alignas(16) Eight<T> e;
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<uint4 *>(e.v)[i] = reinterpret_cast<const uint4 *>(p)[i];
-    return e;
-}
-template <typename T> __device__ __forceinline__ void store_eight(T *p, const Eight<T> &from) {
-    alignas(16) Eight<T> e = from;
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e.v)[i];
-}
 
 // What four warps' sums become: columns c0 to c1 of those on their way out, which are rows of x from x0 on, for the block's matrix rows from r0
-// on.  sums: entry (column c, matrix row r of the block) at 128 c + r; over split > 1 pairs of the cluster they are added up.  A thread takes eight neighbouring
-// outputs of a row of x, so that a row's 64 or 128 outputs leave in 16-byte pieces one beside another (each matrix row's outputs on their own, 64 bytes a warp, took
-// 60 us a tile of 256 x 256).  Of a gated matrix a warp had 16 rows of the gate and the same 16 of the other half.
-template <typename T, bool GATED>
+// on.  sums: entry (column c, matrix row r of the block) at 128 c + r; over split > 1 pairs of the cluster they are added up.  A thread takes four neighbouring
+// outputs of a row of x, so that a row's 64 or 128 outputs leave side by side (each matrix row's outputs on their own, 64 bytes a warp, took
+// 60 us a tile of 256 x 256; eight a thread spill, as a thread's sums of the other columns are held meanwhile).  Of a gated matrix a
+// warp had 16 rows of the gate and the same 16 of the other half.
+template <typename T, bool GATED, bool SPLIT>
 __device__ __forceinline__ void finish(const TcArgs &a, const float *sums, int c0, int c1, int64_t x0, int64_t r0, uint32_t rank) {
-    constexpr int kLanes = GATED ? 8 : 16, kAtOnce = 128 / kLanes;  // threads of a row of x; rows of x at once
+    constexpr int kLanes = GATED ? 16 : 32, kAtOnce = 128 / kLanes;  // threads of a row of x; rows of x at once
     const int tid = threadIdx.x & 127, part = tid % kLanes, end = (int)min((int64_t)c1, a.b - x0);
-    const int from = GATED ? 32 * (part >> 1) + 8 * (part & 1) : 8 * part;
-    const int64_t row = r0 + 8 * part;
-    const bool whole = a.wide && row + 8 <= a.n;
-    auto eight = [&](int at, float (&v)[8]) {
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = 0.f;
-        for (int p = 0; p < a.split; p++)
-#pragma unroll
-            for (int j = 0; j < 8; j += 4) {
-                float4 f;
-                if (a.split == 1) {
-                    f = *reinterpret_cast<const float4 *>(sums + at + j);
-                } else {
-                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                                 : "r"(of_rank(shared_at(sums + at + j), 2 * p + (rank & 1))) : "memory");
-                }
-                v[j] += f.x;
-                v[j + 1] += f.y;
-                v[j + 2] += f.z;
-                v[j + 3] += f.w;
-            }
-    };
-    float bias[8];
-    const bool biased = !GATED && a.epi.bias;
-#pragma unroll
-    for (int j = 0; j < 8; j++) bias[j] = biased && row + j < a.n ? to_f32(static_cast<const T *>(a.epi.bias)[row + j]) : 0.f;
-    if (row >= a.n) return;
-#pragma unroll 1
-    for (int c = c0 + tid / kLanes; c < end; c += kAtOnce) {
-        T *y = static_cast<T *>(a.y) + (x0 + c) * a.y_row + row;
-        Eight<T> out;
-        float v[8];
-        eight(128 * c + from, v);
-        if (GATED) {
-            float u[8];
-            eight(128 * c + from + 16, u);
-#pragma unroll
-            for (int j = 0; j < 8; j++) out.v[j] = from_f32<T>(activate(v[j], a.epi.act) * u[j]);
-        } else {
-            Eight<T> residual;
-            const T *r = static_cast<const T *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
-            if (!a.epi.residual) {
-#pragma unroll
-                for (int j = 0; j < 8; j++) residual.v[j] = from_f32<T>(0.f);
-            } else if (whole) {
-                residual = load_eight(r);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; j++) residual.v[j] = row + j < a.n ? r[j] : from_f32<T>(0.f);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; j++) out.v[j] = from_f32<T>(activate(v[j] + bias[j], a.epi.act) + to_f32(residual.v[j]));
+    const int64_t row = r0 + 4 * part;
+    const bool whole = a.wide && row + 4 <= a.n;
+    auto four = [&](const float *at, float (&v)[4]) {
+        if (!SPLIT || a.split == 1) {
+            const float4 f = *reinterpret_cast<const float4 *>(at);
+            v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+            return;
         }
+        v[0] = v[1] = v[2] = v[3] = 0.f;
+        for (int p = 0; p < a.split; p++) {
+            float4 f;
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                         : "r"(of_rank(shared_at(at), 2 * p + (rank & 1))) : "memory");
+            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        }
+    };
+    if (row >= a.n) return;
+    float bias[4];
+    if (!GATED) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) bias[j] = a.epi.bias && row + j < a.n ? to_f32(static_cast<const T *>(a.epi.bias)[row + j]) : 0.f;
+    }
+    int c = c0 + tid / kLanes;
+    T *y = static_cast<T *>(a.y) + (x0 + c) * a.y_row + row;
+    const T *r = static_cast<const T *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
+    const float *at = sums + 128 * c + (GATED ? 32 * (part >> 2) + 4 * (part & 3) : 4 * part);
+#pragma unroll 1
+    for (; c < end; c += kAtOnce, y += kAtOnce * a.y_row, r += kAtOnce * a.epi.residual_row, at += kAtOnce * 128) {
+        float v[4];
+        four(at, v);
+        if (GATED) {
+            float u[4];
+            four(at + 16, u);
+            activate_all(v, a.epi.act);
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] *= u[j];
+        } else {
+            Four<T> residual;
+            if (a.epi.residual) {
+                if (whole) {
+                    residual = *reinterpret_cast<const Four<T> *>(r);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; j++) residual.v[j] = row + j < a.n ? r[j] : from_f32<T>(0.f);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] += bias[j];
+            activate_all(v, a.epi.act);
+            if (a.epi.residual) {
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] += to_f32(residual.v[j]);
+            }
+        }
+        Four<T> out;
+#pragma unroll
+        for (int j = 0; j < 4; j++) out.v[j] = from_f32<T>(v[j]);
         if (whole) {
-            store_eight(y, out);
+            *reinterpret_cast<Four<T> *>(y) = out;
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; j++)
+            for (int j = 0; j < 4; j++)
                 if (row + j < a.n) y[j] = out.v[j];
         }
     }
 }
 
+// The same by lookups; lane: the address of the lane's copy of the first entry.  (A warp of the permutes takes 21 operations of the integer pipe for
+// eight codes, which left the tensor core waiting for its levels: 558 us for 8192 x 8192 by 4096 rows, and 392 with nothing decoded.)
+__device__ __forceinline__ void look_up(uint32_t w, uint32_t lane, uint32_t *to) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) to[j] = *static_cast<const uint32_t *>(__cvta_shared_to_generic(permute(w, 0, 0x4440 | j) * 128 + lane));
+}
+
 // A cluster is `split` pairs of blocks.  Of a block's warps, four bring in tiles, issue products and pass arrivals on; kDecodeWarps turn codes
 // into levels; eight take sums out.  Barriers pass stages between them; those that the products' issuer waits for are in the first block of a
 // pair, which issues for both.
-template <int ND, int NH, bool GATED, int SPANS>
-__global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
+template <int ND, int NH, bool GATED, int SPANS, bool F32>
+__global__ void __launch_bounds__(TcShape<ND, NH, F32>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
                                                                             const __grid_constant__ TcArgs a) {
-    using Shape = TcShape<ND, NH>;
+    using Shape = TcShape<ND, NH, F32>;
     constexpr int kN = Shape::kN, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kOwn = Shape::kOwn;
     extern __shared__ char smem_raw[];
     const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
@@ -172,8 +176,8 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
     const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
                    a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
                    all_done = d_empty + 8 * kDBufs, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
-    uint32_t *tables = reinterpret_cast<uint32_t *>(smem + Shape::kTablesAt);
-    const int terms = a.type == ECASQ_F32 ? 6 : 1;
+    uint32_t *books = reinterpret_cast<uint32_t *>(smem + Shape::kBooksAt);
+    constexpr int terms = F32 ? 6 : 1;
     const int kb0 = (int)((int64_t)a.blocks * pair / a.split), kb1 = (int)((int64_t)a.blocks * (pair + 1) / a.split);
     const int cluster = blockIdx.x / size, clusters = gridDim.x / size;
 
@@ -203,12 +207,12 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
     wait_before();
     if (tid == 0) {
         for (int i = 0; i < kXStages; i++) {
-            mbar_init(x_full + 8 * i, rank == leader ? 2 : 1);  // this block's copies, and the other's word that its are there
+            mbar_init(x_full + 8 * i, 1);
             mbar_init(x_empty + 8 * i, 1);
         }
         for (int i = 0; i < kCodeStages; i++) {
             mbar_init(c_full + 8 * i, 1);
-            mbar_init(c_empty + 8 * i, 8);
+            mbar_init(c_empty + 8 * i, Shape::kDecodeWarps);
         }
         for (int i = 0; i < kAStages; i++) {
             mbar_init(a_full + 8 * i, 8);
@@ -226,23 +230,27 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
         tile_map_fetch(&xm);
         tile_map_fetch(&cm);
     }
-    // The levels' bytes, of fp32 three terms of eight bits each.
-    if (tid < 48) {
-        const int term = tid / 16, j = tid % 16;
-        uint32_t bits = 0;
-        if (j < a.m) {
-            if (a.type == ECASQ_F32) {
+    if (F32) {  // the levels' bytes: three terms of eight bits each
+        if (tid < 48) {
+            const int term = tid / 16, j = tid % 16;
+            uint32_t bits = 0;
+            if (j < a.m) {
                 float v = static_cast<const float *>(a.levels)[j];
                 for (int i = 0; i <= term; i++) {
                     bits = __float_as_uint(v) >> 16;
                     v -= __uint_as_float(bits << 16);
                 }
-            } else {
-                bits = static_cast<const uint16_t *>(a.levels)[j];
             }
+            reinterpret_cast<uint8_t *>(books + 8 * term)[j] = (uint8_t)bits;
+            reinterpret_cast<uint8_t *>(books + 8 * term)[16 + j] = (uint8_t)(bits >> 8);
         }
-        reinterpret_cast<uint8_t *>(tables + 8 * term)[j] = (uint8_t)bits;
-        reinterpret_cast<uint8_t *>(tables + 8 * term)[16 + j] = (uint8_t)(bits >> 8);
+    } else {  // pairs: a warp those with one second level, a lane a copy
+        const uint16_t *levels = static_cast<const uint16_t *>(a.levels);
+        const uint32_t mine = (lane & 15) < a.m ? levels[lane & 15] : 0;
+        for (int hi = wid; hi < 16; hi += Shape::kWarps)
+#pragma unroll
+            for (int lo = 0; lo < 16; lo++)
+                reinterpret_cast<uint32_t *>(smem + Shape::kTableAt)[(16 * hi + lo) * 32 + lane] = __shfl_sync(0xffffffffu, mine, lo) | __shfl_sync(0xffffffffu, mine, hi) << 16;
     }
     if (wid == 3) tmem_alloc(tmem_at);
     __syncthreads();
@@ -255,7 +263,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
     const int per_tile = (kb1 - kb0) * terms;  // products' blocks of a tile
 
     if (wid < 4) {
-        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (lane == 0 && !a.lost) {
             if (wid == 0) {  // rows of x
                 uint32_t i = 0;
@@ -294,68 +302,67 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                 }
                 const uint64_t t0 = nanoseconds();
                 for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++) mbar_drain(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1, t0);
-            } else if (wid == 3 && rank != leader) {  // tells the first block of the pair that this one's rows of x are there
-                uint32_t i = 0;
-                bool ok = true;
-                const uint32_t there = of_rank(x_full, leader);
-                for (int t = cluster; ok && t < a.tiles; t += clusters)
-                    for (int v = 0; ok && v < per_tile; v++, i++)
-                        if ((ok = wait(x_full + 8 * (i % kXStages), i / kXStages & 1))) mbar_arrive(there + 8 * (i % kXStages));
             }
         }
         if (wid == 1 && rank == leader) {  // products: the whole warp, so that addresses stay in uniform registers
             const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
             const uint16_t both = (uint16_t)(3u << rank);
-            uint32_t xs = 0, x_parity = 0, as = 0, a_parity = 0, buf = 0, d_parity = 1;
+            uint32_t xs = 0, as = 0, a_parity = 0, buf = 0, d_parity = 1;
             bool ok = !a.lost;
-            // The next buffer for sums, once it is free.
-            auto open = [&](uint32_t &d, uint32_t &full) {
-                const bool free = wait_warp(d_empty + 8 * buf, d_parity);
-                tmem_fence_after();
-                d = tmem + buf * ND;
-                full = d_full + 8 * buf;
-                buf = buf + 1 == kDBufs ? 0 : buf + 1;
-                d_parity ^= buf == 0;
-                return free;
-            };
-            auto levels = [&](int hb) {
-                const bool there = wait_warp(a_full + 8 * (as + hb), a_parity);
+            // Waits for the block's levels (with BLOCK; they and the rows of x come together), and, with `fresh`, for the next NH buffers for sums: one wait
+            // for all, as each costs this warp about a hundred clocks, of the thousand that the tensor core takes for a block.
+            uint32_t d[NH], full[NH];
+            auto ready = [&](auto block, bool fresh) {
+                uint32_t empty[NH], parity[NH];
+                if (fresh) {
+#pragma unroll
+                    for (int h = 0; h < NH; h++) {
+                        d[h] = tmem + buf * ND;
+                        full[h] = d_full + 8 * buf;
+                        empty[h] = d_empty + 8 * buf;
+                        parity[h] = d_parity;
+                        buf = buf + 1 == kDBufs ? 0 : buf + 1;
+                        d_parity ^= buf == 0;
+                    }
+                }
+                const bool there = __all_sync(0xffffffffu, wait_for([&] {
+                    bool r = true;
+                    if (block) {
+                        if (NH == 1) r = mbar_try(a_full + 8 * as, a_parity);
+                        r &= mbar_try(a_full + 8 * as + 8, a_parity);  // (with four decoding warps the second half's levels come after the first's)
+                    }
+                    if (fresh) {
+#pragma unroll
+                        for (int h = 0; h < NH; h++) r &= mbar_try(empty[h], parity[h]);
+                    }
+                    return r;
+                }));
                 tmem_fence_after();
                 return there;
             };
             for (int t = cluster; ok && t < a.tiles; t += clusters) {
                 int in_group = kb0 % a.group_blocks, term = 0;
                 bool fresh = true;
-                uint32_t d[NH], full[NH];
                 for (int v = 0; v < per_tile; v++) {
                     const uint32_t x = mma_rows(base + xs * Shape::kXStage), levels_at = tmem + kAAt + as * kACols;
-                    if (!(ok = wait_warp(x_full + 8 * xs, x_parity) && levels(0))) break;
                     // The products of 16 entries number k0 .. k1 of the block with half h of the rows of x.
-                    auto steps = [&](uint32_t to, int h, int k0, int k1, bool add) {
+                    auto steps = [&](int h, int k0, int k1, bool add) {
 #pragma unroll
                         for (int kk = k0; kk < k1; kk++)
-                            mma_pair(to, levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
+                            mma_pair(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
                     };
                     if (SPANS == 1) {
                         const bool last = v + 1 == per_tile || (term == terms - 1 && in_group + 1 == a.group_blocks);
-                        if (fresh && !(ok = open(d[0], full[0]))) break;
-                        if (one_lane()) steps(d[0], 0, 0, 4, !fresh);
-                        if (!(ok = levels(1))) break;
+                        if (!(ok = ready(std::true_type{}, fresh))) break;
                         if (one_lane()) {
-                            steps(d[0], 0, 4, 8, true);
-                            if (last) mma_commit(full[0], both);
-                        }
-                        if (NH == 2) {
-                            if (fresh && !(ok = open(d[NH - 1], full[NH - 1]))) break;
-                            if (one_lane()) {
-                                steps(d[NH - 1], NH - 1, 0, 4, !fresh);
-                                mma_commit(a_empty + 8 * as, both);
-                                steps(d[NH - 1], NH - 1, 4, 8, true);
-                                if (last) mma_commit(full[NH - 1], both);
+                            if (NH == 2) {
+                                steps(0, 0, 8, !fresh);
+                                if (last) mma_commit(full[0], both);
                             }
-                        }
-                        if (one_lane()) {
-                            if (NH == 1) mma_commit(a_empty + 8 * as, both);
+                            steps(NH - 1, 0, 4, !fresh);
+                            mma_commit(a_empty + 8 * as, both);
+                            steps(NH - 1, 4, 8, true);
+                            if (last) mma_commit(full[NH - 1], both);
                             mma_commit(a_empty + 8 * as + 8, both);
                             mma_commit(x_empty + 8 * xs, both);
                         }
@@ -363,16 +370,15 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                     } else {
 #pragma unroll
                         for (int sub = 0; sub < SPANS; sub++) {
-                            if (sub == SPANS / 2 && !(ok = ok && levels(1))) break;
+                            if (!(ok = sub ? ready(std::false_type{}, true) : ready(std::true_type{}, true))) break;
+                            if (one_lane()) {
 #pragma unroll
-                            for (int h = 0; h < NH; h++) {
-                                if (!(ok = ok && open(d[h], full[h]))) break;
-                                if (one_lane()) {
-                                    steps(d[h], h, sub * (8 / SPANS), (sub + 1) * (8 / SPANS), false);
+                                for (int h = 0; h < NH; h++) {
+                                    steps(h, sub * (8 / SPANS), (sub + 1) * (8 / SPANS), false);
                                     mma_commit(full[h], both);
-                                    if (h == NH - 1 && (sub + 1) % (SPANS / 2) == 0) mma_commit(a_empty + 8 * (as + sub / (SPANS / 2)), both);
-                                    if (h == NH - 1 && sub == SPANS - 1) mma_commit(x_empty + 8 * xs, both);
                                 }
+                                if ((sub + 1) % (SPANS / 2) == 0) mma_commit(a_empty + 8 * (as + sub / (SPANS / 2)), both);
+                                if (sub == SPANS - 1) mma_commit(x_empty + 8 * xs, both);
                             }
                         }
                         if (!ok) break;
@@ -382,7 +388,6 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                         if (++in_group == a.group_blocks) in_group = 0;
                     }
                     xs = xs + 1 == kXStages ? 0 : xs + 1;
-                    x_parity ^= xs == 0;
                     as ^= 2;
                     a_parity ^= as == 0;
                 }
@@ -390,47 +395,84 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
         }
         __syncwarp();
     } else if (wid < 4 + Shape::kDecodeWarps) {
-        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        if (NH == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // Row of the block's 128: of a gated matrix the lower half of each warp has rows of the gate.
         const int row = 32 * (wid & 3) + lane, from = GATED ? (lane & 16) * 4 + 16 * (wid & 3) + (lane & 15) : row;
         const uint32_t there = of_rank(a_full, leader), swizzle = (uint32_t)(from >> 1 & 3);
-        const int first = Shape::kDecodeWarps == 8 ? (wid - 4) / 4 : 0, step = Shape::kDecodeWarps == 8 ? 2 : 1;
-        uint32_t i = 0;
-        bool ok = !a.lost;
-        for (int t = cluster; ok && t < a.tiles; t += clusters)
-            for (int v = 0; ok && v < per_tile; v++, i++) {
-                const uint32_t cs = i % kCodeStages;
-                if (!(ok = wait_warp(c_full + 8 * cs, i / kCodeStages & 1))) break;
-                const char *codes = smem + kXStages * Shape::kXStage + cs * kCodeStage + from * 64;
-                uint32_t table[8];
-                const uint4 *book = reinterpret_cast<const uint4 *>(tables + (terms > 1 ? 8 * kLevelTerm[v % terms] : 0));
-                *reinterpret_cast<uint4 *>(table) = book[0];
-                *reinterpret_cast<uint4 *>(table + 4) = book[1];
-                for (int hb = first; ok && hb < 2; hb += step) {
-                    uint32_t w[8];
+        constexpr int kHalves = Shape::kDecodeWarps == 8 ? 1 : 2;  // of a block that a warp decodes
+        const int first = kHalves == 1 ? (wid - 4) / 4 : 0;
+        const int total = a.tiles > cluster ? (a.tiles - cluster + clusters - 1) / clusters * per_tile : 0;  // blocks of all tiles
+        const char *codes = smem + kXStages * Shape::kXStage + from * 64;
+        uint32_t w[8 * kHalves], cs = 0, c_parity = 0, xs = 0, x_parity = 0, as = 0, a_parity = 1, term = 0;
+        // The next block's words, in the order of their columns.
+        auto fetch = [&] {
+            if (!wait_warp(c_full + 8 * cs, c_parity)) return false;
 #pragma unroll
-                    for (int q = 0; q < 4; q++) {
-                        const uint2 two = *reinterpret_cast<const uint2 *>(codes + ((q ^ swizzle) << 4) + 8 * hb);
-                        w[q] = two.x;
-                        w[q + 4] = two.y;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(c_empty + 8 * cs);
-                    uint32_t pairs[32];
-#pragma unroll
-                    for (int q = 0; q < 8; q++) decode(w[q], table, pairs + 4 * q);
-                    const uint32_t j = 2 * i + hb, as = j % kAStages;
-                    if (!(ok = wait_warp(a_empty + 8 * as, (j / kAStages & 1) ^ 1))) break;
-                    tmem_fence_after();
-                    tmem_store(tmem + ((uint32_t)(wid & 3) << 21) + kAAt + as * kACols, pairs);
-                    tmem_stored();
-                    tmem_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(there + 8 * as);
+            for (int q = 0; q < 4; q++) {
+                const char *at = codes + cs * kCodeStage + ((q ^ swizzle) << 4);
+                if (kHalves == 2) {
+                    const uint4 four = *reinterpret_cast<const uint4 *>(at);
+                    w[q] = four.x, w[q + 4] = four.y, w[q + 8 * (kHalves - 1)] = four.z, w[q + 8 * kHalves - 4] = four.w;
+                } else {
+                    const uint2 two = *reinterpret_cast<const uint2 *>(at + 8 * first);
+                    w[q] = two.x, w[q + 4] = two.y;
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(c_empty + 8 * cs);
+            cs = cs + 1 == kCodeStages ? 0 : cs + 1;
+            c_parity ^= cs == 0;
+            return true;
+        };
+        auto decode_half = [&](int half, uint32_t (&pairs)[32]) {
+            if (F32) {
+                uint32_t book[8];
+                const uint4 *from = reinterpret_cast<const uint4 *>(books + 8 * kLevelTerm[term]);
+                *reinterpret_cast<uint4 *>(book) = from[0];
+                *reinterpret_cast<uint4 *>(book + 4) = from[1];
+#pragma unroll
+                for (int q = 0; q < 8; q++) decode(w[8 * half + q], book, pairs + 4 * q);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; q++) look_up(w[8 * half + q], base + Shape::kTableAt + 4 * lane, pairs + 4 * q);
+            }
+        };
+        auto store = [&](int hb, const uint32_t (&pairs)[32]) {
+            const bool free = wait_warp(a_empty + 8 * (as + hb), a_parity);
+            tmem_fence_after();
+            tmem_store(tmem + ((uint32_t)(wid & 3) << 21) + kAAt + (as + hb) * kACols, pairs);
+            return free;
+        };
+        auto stored = [&](int hb) {
+            tmem_stored();
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(there + 8 * (as + hb));
+        };
+        // While a half's levels are on their way to tensor memory, the next half's are looked up.
+        bool ok = !a.lost && (!total || fetch());
+        for (int i = 0; ok && i < total; i++) {
+            uint32_t pairs[32];
+            decode_half(0, pairs);
+            if (!(ok = store(first, pairs))) break;
+            if (kHalves == 2) decode_half(kHalves - 1, pairs);
+            else if (i + 1 < total && !(ok = fetch())) break;
+            // One warp's word stands for the block's rows of x too, so that the issuer has one barrier to wait for.
+            if (wid == 4 && !(ok = wait_warp(x_full + 8 * xs, x_parity))) break;
+            stored(first);
+            if (kHalves == 2) {
+                if (!(ok = store(1, pairs))) break;
+                if (i + 1 < total && !(ok = fetch())) break;
+                stored(1);
+            }
+            xs = xs + 1 == kXStages ? 0 : xs + 1;
+            x_parity ^= xs == 0;
+            as ^= 2;
+            a_parity ^= as == 0;
+            term = term + 1 == terms ? 0 : term + 1;
+        }
     } else {
-        if (NH == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        if (NH == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
         const uint32_t there = of_rank(d_empty, leader), column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
         uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0;
@@ -455,7 +497,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                 next = scale(next_word);
                 if (!(ok = wait_warp(d_full + 8 * buf, d_parity))) return;
                 tmem_fence_after();
-                constexpr int kChunk = kOwn == 128 ? 32 : kOwn < 16 ? kOwn : 16;
+                constexpr int kChunk = kOwn < 16 ? kOwn : 16;
 #pragma unroll
                 for (int c = 0; c < kOwn; c += kChunk) {
                     uint32_t d[kChunk];
@@ -492,7 +534,10 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
             }
             constexpr int kOut = Shape::kOut;
             float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * kOut * 128;
-            auto four_warps = [&] { asm volatile("bar.sync %0, 128;" ::"r"(1 + part) : "memory"); };
+            auto four_warps = [&] {
+                if (part) asm volatile("bar.sync 2, 128;" ::: "memory");
+                else asm volatile("bar.sync 1, 128;" ::: "memory");
+            };
             int c0 = 0, c1 = kOut;
             if (NH == 1 && a.split > 1) {  // each pair takes a share of the columns over all pairs
                 ok = ok && wait_cluster(sums_empty, (turn & 1) ^ 1);
@@ -517,9 +562,9 @@ __global__ void __launch_bounds__(TcShape<ND, NH>::kThreads, 1) k_project_tc(con
                 }
                 four_warps();
                 const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + part * kOwn + q * kOut;
-                if (a.type == ECASQ_F16) finish<__half, GATED>(a, sums, c0, c1, x0, r0, rank);
-                else if (a.type == ECASQ_BF16) finish<__nv_bfloat16, GATED>(a, sums, c0, c1, x0, r0, rank);
-                else finish<float, GATED>(a, sums, c0, c1, x0, r0, rank);
+                if (F32) finish<float, GATED, NH == 1>(a, sums, c0, c1, x0, r0, rank);
+                else if (a.type == ECASQ_F16) finish<__half, GATED, NH == 1>(a, sums, c0, c1, x0, r0, rank);
+                else finish<__nv_bfloat16, GATED, NH == 1>(a, sums, c0, c1, x0, r0, rank);
             }
             if (NH == 1 && a.split > 1) {
                 __syncwarp();
@@ -607,11 +652,11 @@ template <typename K> static int tc_held(K *kernel, int size, int threads, int s
     return ECASQ_OK;
 }
 
-template <int ND, int NH, bool GATED, int SPANS> static int launch_tc(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
-    using Shape = TcShape<ND, NH>;
+template <int ND, int NH, bool GATED, int SPANS, bool F32> static int launch_tc(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
+    using Shape = TcShape<ND, NH, F32>;
     static_assert(Shape::kBytes <= 227 * 1024 && Shape::kBytes > 114 * 1024, "one block an SM: tensor memory is the block's alone");
     static std::atomic<int> allowed[kDevices], known[3][kDevices];
-    auto *kernel = k_project_tc<ND, NH, GATED, SPANS>;
+    auto *kernel = k_project_tc<ND, NH, GATED, SPANS, F32>;
     int rc = allow_smem(kernel, Shape::kBytes, allowed), held = 0;
     if (!rc) rc = tc_held(kernel, 2 * a.split, Shape::kThreads, Shape::kBytes, known[a.split / 2], &held);
     if (rc) return rc;
@@ -621,9 +666,10 @@ template <int ND, int NH, bool GATED, int SPANS> static int launch_tc(const CUte
 template <int ND, int NH, bool GATED> static int launch_tc_spans(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
     // The tensor core's fp32 sums are cut off, not rounded, at each step: of fp32 operands they are taken out after every 32 columns (an error
     // of 2.8e-7 of the result for k = 1024; after six products of 128, 2.1e-6).
-    if (a.group % 128 == 0 && a.type != ECASQ_F32) return launch_tc<ND, NH, GATED, 1>(xm, cm, a, st);
-    if (a.group % 64 == 0 && a.type != ECASQ_F32) return launch_tc<ND, NH, GATED, 2>(xm, cm, a, st);
-    return launch_tc<ND, NH, GATED, 4>(xm, cm, a, st);
+    if (a.type == ECASQ_F32) return launch_tc<ND, NH, GATED, 4, true>(xm, cm, a, st);
+    if (a.group % 128 == 0) return launch_tc<ND, NH, GATED, 1, false>(xm, cm, a, st);
+    if (a.group % 64 == 0) return launch_tc<ND, NH, GATED, 2, false>(xm, cm, a, st);
+    return launch_tc<ND, NH, GATED, 4, false>(xm, cm, a, st);
 }
 
 int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st) {
@@ -662,8 +708,9 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     const FastDiv div(p.group / 32);
     a.div_mul = div.mul;
     a.div_shift = div.shift;
-    const int64_t pieces = 16 / type_size(p.type);
-    a.wide = aligned16(p.y) && (p.b == 1 || p.y_row % pieces == 0) && (!p.epi.residual || (aligned16(p.epi.residual) && (p.b == 1 || p.epi.residual_row % pieces == 0)));
+    const int64_t piece = 4 * type_size(p.type);
+    const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
+    a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
     const int64_t w_tiles = cdiv(p.n, p.gated ? 128 : 256);
     const int width = p.b <= 32 ? 32 : p.b <= 64 ? 64 : p.b <= 128 ? 128 : 256;
     a.x_tiles = (int32_t)cdiv(p.b, width);
