@@ -1,0 +1,722 @@
+// project_tc.cuh -- ecasq_project and ecasq_gated for more rows of x than a pass of the matrix-vector kernels takes.
+//
+// The matrix is the left operand: its codes become levels, which go to tensor memory as they are (16 bits, exact), 128 rows a
+// block and 256 a pair of blocks; the rows of x are the right operand, in shared memory.  The sums of the columns of one scale group
+// come out of tensor memory, are multiplied by their row's scale, which is one number a thread there, and are added up in registers.  So
+// products and scales are as exact as in ecasq_matvec: nothing is rounded before the end.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "project.cuh"
+#include "tc.cuh"
+
+namespace ecasq {
+
+struct TcArgs {
+    const void *levels, *scales;
+    void *y;
+    int32_t *status;
+    int64_t scale_row, y_row, n, b, k, second;  // second: the first row of a gated matrix's other half
+    int32_t m, group, type, scale_type;
+    int32_t blocks;         // blocks of 128 columns
+    int32_t group_blocks;   // blocks of a scale group, where it holds whole ones
+    int32_t split;          // pairs of a cluster that share the columns
+    int32_t x_tiles, tiles; // tiles of rows of x; of the product
+    uint32_t div_mul, div_shift;  // words of 32 columns to scale groups (FastDiv of group / 32)
+    bool wide;              // y and the residual in pieces of four values
+    uint32_t lost;          // test hook: 1 where blocks begin as if a wait had run out
+    Epilogue epi;
+};
+
+constexpr int kDBufs = 3;          // sums in tensor memory; behind them 4 stages of 64 columns of levels
+constexpr int kACols = 32, kAStages = 4, kAAt = 512 - kAStages * kACols;
+constexpr int kCodeStage = 128 * 64;
+
+// fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.
+__device__ __constant__ const int8_t kXTerm[6] = {0, 0, 0, 1, 1, 2}, kLevelTerm[6] = {0, 1, 2, 0, 1, 0};
+
+// ND columns (rows of x) a product, NH of them a tile.  F32: fp32 operands as bf16 terms, whose levels are found by byte permutes; those of 16-bit
+// types by lookups in a table of pairs.
+template <int ND, int NH, bool GATED, bool F32> struct TcShape {
+    static constexpr int kN = ND * NH;
+    static constexpr int kDecodeWarps = NH == 2 ? 4 : 8, kWarps = 4 + kDecodeWarps + 8, kThreads = 32 * kWarps;
+    static constexpr int kXStage = kN / 2 * 256;
+    static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
+    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 8 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 10 : 12;
+    static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
+    static constexpr int kOut = NH == 2 ? (GATED ? 32 : 16) : kOwn;  // of them at a time on their way out through shared memory
+    static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
+    // Registers of a thread of the first four warps, of those that decode and of those that add; together no more than the block was launched with.
+    static constexpr bool kUneven = kOwn >= 64;
+    static constexpr int kRegs = NH == 2 ? 56 : 40, kDecodeRegs = NH == 2 ? 88 : 64, kAddRegs = NH == 2 ? 184 : 152;
+    static_assert(4 * kRegs + kDecodeWarps * kDecodeRegs + 8 * kAddRegs <= kWarps * (65536 / kThreads / 8 * 8), "the split would wait for ever");
+    static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
+    static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kBooksAt = kSumsAt + kSums, kBarsAt = kBooksAt + 128;
+    static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
+};
+
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t s) {
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(s));
+    return d;
+}
+// The levels of a word of eight codes, as four pairs.  t: the low bytes of levels 0-3, 4-7, 8-11, 12-15, then their high bytes.
+// The lower and the upper eight levels are looked up by the codes' low three bits, and a permute that spreads the sign bits of w << 4 and w,
+// which are the codes' fourth bits, chooses.
+__device__ __forceinline__ void decode(uint32_t w, const uint32_t (&t)[8], uint32_t *to) {
+    const uint32_t low3 = w & 0x77777777u, up = w << 4;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const uint32_t s = h ? low3 >> 16 : low3, m = permute(up, w, h ? 0xFBEA : 0xD9C8);
+        const uint32_t l0 = permute(t[0], t[1], s), l1 = permute(t[2], t[3], s), h0 = permute(t[4], t[5], s), h1 = permute(t[6], t[7], s);
+        const uint32_t l = (l0 & ~m) | (l1 & m), hi = (h0 & ~m) | (h1 & m);
+        to[2 * h] = permute(l, hi, 0x5140);
+        to[2 * h + 1] = permute(l, hi, 0x7362);
+    }
+}
+
+// Four neighbouring values of one of the 16-bit types, or of fp32, to fp32 and from it.
+template <bool F32> using FourOf = std::conditional_t<F32, uint4, uint2>;
+__device__ __forceinline__ void widen(const uint4 &p, bool, float (&v)[4]) {
+    v[0] = __uint_as_float(p.x), v[1] = __uint_as_float(p.y), v[2] = __uint_as_float(p.z), v[3] = __uint_as_float(p.w);
+}
+__device__ __forceinline__ void widen(const uint2 &p, bool bf16, float (&v)[4]) {
+    const uint32_t w[2] = {p.x, p.y};
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        if (bf16) {
+            v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 f = __half22float2(reinterpret_cast<const __half2 &>(w[i]));
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        }
+    }
+}
+__device__ __forceinline__ void narrow(const float (&v)[4], bool, uint4 &p) {
+    p = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ void narrow(const float (&v)[4], bool bf16, uint2 &p) {
+    if (bf16) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.x) : "f"(v[1]), "f"(v[0]));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p.y) : "f"(v[3]), "f"(v[2]));
+    } else {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.x) : "f"(v[1]), "f"(v[0]));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p.y) : "f"(v[3]), "f"(v[2]));
+    }
+}
+
+// How four warps' sums leave the block.  They lie in shared memory, entry (column c, matrix row r of the block) at 128 c + r, and
+// a thread takes four neighbouring outputs of a row of x, so that a row's 64 or 128 outputs leave side by side (each matrix row's outputs on their own, 64
+// bytes a warp, took 60 us a tile of 256 x 256; eight a thread spill, as a thread's sums of the other columns are held meanwhile).  Of a gated
+// matrix a warp had 16 rows of the gate and the same 16 of the other half.  Over split > 1 pairs of the cluster sums are added up.
+template <bool GATED, bool SPLIT, bool F32> struct Finish {
+    static constexpr int kLanes = GATED ? 16 : 32, kAtOnce = 128 / kLanes, kTurns = 4;  // threads of a row of x; rows of x at once; turns that are fetched for together
+    using Bits = FourOf<F32>;
+    using One = std::conditional_t<F32, uint32_t, uint16_t>;
+    const TcArgs &a;
+    const float *sums;
+    int64_t row;       // the thread's first output
+    uint32_t rank;
+    bool whole;        // its four lie side by side and aligned
+    Bits residual[GATED ? 1 : kTurns];
+
+    __device__ __forceinline__ Finish(const TcArgs &a, const float *from, int64_t r0, uint32_t rank) : a(a), rank(rank) {
+        const int part = threadIdx.x % kLanes;
+        row = r0 + 4 * part;
+        whole = a.wide && row + 4 <= a.n;
+        sums = from + (GATED ? 32 * (part >> 2) + 4 * (part & 3) : 4 * part);
+    }
+    __device__ __forceinline__ int first() const { return (threadIdx.x & 127) / kLanes; }
+    // The four at p, or those of them that there are.
+    __device__ __forceinline__ Bits load(const One *p) const {
+        if (whole) return *reinterpret_cast<const Bits *>(p);
+        One v[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) v[j] = row + j < a.n ? p[j] : 0;
+        Bits b;
+        memcpy(&b, v, sizeof b);
+        return b;
+    }
+    // Residuals of columns c, c + kAtOnce, ... (rows of x from x0 on), on their way while something else is done.
+    __device__ __forceinline__ void fetch(int64_t x0, int c, int end) {
+        if (GATED || !a.epi.residual || row >= a.n) return;
+        const One *r = static_cast<const One *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
+#pragma unroll
+        for (int i = 0; i < kTurns; i++, r += kAtOnce * a.epi.residual_row)
+            if (c + i * kAtOnce < end) residual[GATED ? 0 : i] = load(r);
+    }
+    // The residuals of columns below `count` come into the L2 cache while the products go on.
+    __device__ __forceinline__ void announce(int64_t x0, int count) const {
+        if (GATED || !a.epi.residual || row >= a.n) return;
+        for (int c = threadIdx.x & 31; c < count && x0 + c < a.b; c += 32) {
+            const One *r = static_cast<const One *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + (row - 4 * (threadIdx.x % kLanes)) + 32 * (threadIdx.x / 32 % 4);
+            if (row - 4 * (threadIdx.x % kLanes) + 32 * (threadIdx.x / 32 % 4) < a.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(r));
+        }
+    }
+    __device__ __forceinline__ void four(const float *at, float (&v)[4]) const {
+        if (!SPLIT || a.split == 1) {
+            const float4 f = *reinterpret_cast<const float4 *>(at);
+            v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+            return;
+        }
+        v[0] = v[1] = v[2] = v[3] = 0.f;
+        for (int p = 0; p < a.split; p++) {
+            float4 f;
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                         : "r"(of_rank(shared_at(at), 2 * p + (rank & 1))) : "memory");
+            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        }
+    }
+    template <int ACT> __device__ __forceinline__ void give_as(int64_t x0, int c, int end) const {
+        const bool bf16 = a.type == ECASQ_BF16;
+        float bias[4] = {0.f, 0.f, 0.f, 0.f};
+        if (!GATED && a.epi.bias) {
+            One v[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] = row + j < a.n ? static_cast<const One *>(a.epi.bias)[row + j] : 0;
+            Bits b;
+            memcpy(&b, v, sizeof b);
+            widen(b, bf16, bias);
+        }
+        One *y = static_cast<One *>(a.y) + (x0 + c) * a.y_row + row;
+        const float *at = sums + 128 * c;
+#pragma unroll
+        for (int i = 0; i < kTurns; i++, c += kAtOnce, y += kAtOnce * a.y_row, at += kAtOnce * 128) {
+            if (c >= end) return;
+            float v[4];
+            four(at, v);
+            if (GATED) {
+                float u[4];
+                four(at + 16, u);
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = activate(v[j], ACT) * u[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = activate(v[j] + bias[j], ACT);
+                if (a.epi.residual) {
+                    float r[4];
+                    widen(residual[GATED ? 0 : i], bf16, r);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) v[j] += r[j];
+                }
+            }
+            Bits out;
+            narrow(v, bf16, out);
+            if (whole) {
+                *reinterpret_cast<Bits *>(y) = out;
+            } else {
+                One o[4];
+                memcpy(o, &out, sizeof out);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (row + j < a.n) y[j] = o[j];
+            }
+        }
+    }
+    // The columns c, c + kAtOnce, ... below end, kTurns of them; what fetch() was asked for is there.
+    __device__ __forceinline__ void give(int64_t x0, int c, int end) const {
+        if (row >= a.n) return;
+        switch (a.epi.act) {
+            case ECASQ_ACT_RELU: return give_as<ECASQ_ACT_RELU>(x0, c, end);
+            case ECASQ_ACT_SILU: return give_as<ECASQ_ACT_SILU>(x0, c, end);
+            case ECASQ_ACT_GELU: return give_as<ECASQ_ACT_GELU>(x0, c, end);
+            case ECASQ_ACT_GELU_TANH: return give_as<ECASQ_ACT_GELU_TANH>(x0, c, end);
+            default: return give_as<ECASQ_ACT_NONE>(x0, c, end);
+        }
+    }
+};
+
+// The same by lookups; lane: the address of the lane's copy of the first entry.  (A warp of the permutes takes 21 operations of the integer pipe for
+// eight codes, which left the tensor core waiting for its levels: 558 us for 8192 x 8192 by 4096 rows, and 392 with nothing decoded.)
+__device__ __forceinline__ void look_up(uint32_t w, uint32_t lane, uint32_t *to) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) to[j] = *static_cast<const uint32_t *>(__cvta_shared_to_generic(permute(w, 0, 0x4440 | j) * 128 + lane));
+}
+
+// A cluster is `split` pairs of blocks.  Of a block's warps, four bring in tiles, issue products and pass arrivals on; kDecodeWarps turn codes
+// into levels; eight take sums out.  Barriers pass stages between them; those that the products' issuer waits for are in the first block of a
+// pair, which issues for both.
+template <int ND, int NH, bool GATED, int SPANS, bool F32>
+__global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
+                                                                            const __grid_constant__ TcArgs a) {
+    using Shape = TcShape<ND, NH, GATED, F32>;
+    constexpr int kN = Shape::kN, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kOwn = Shape::kOwn;
+    extern __shared__ char smem_raw[];
+    const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
+    char *smem = smem_raw + (base - shared_at(smem_raw));
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const uint32_t rank = cluster_rank(), leader = rank & ~1u, size = 2 * a.split, pair = rank / 2;
+    const uint32_t bars = base + Shape::kBarsAt;
+    const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
+                   a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
+                   all_done = d_empty + 8 * kDBufs, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
+    uint32_t *books = reinterpret_cast<uint32_t *>(smem + Shape::kBooksAt);
+    constexpr int terms = F32 ? 6 : 1;
+    const int kb0 = (int)((int64_t)a.blocks * pair / a.split), kb1 = (int)((int64_t)a.blocks * (pair + 1) / a.split);
+    const int cluster = blockIdx.x / size, clusters = gridDim.x / size;
+
+    auto lose = [&] {
+        for (uint32_t r = 0; r < size; r++) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(of_rank(lost_at, r)), "r"(1) : "memory");
+    };
+    auto lost = [&] {
+        uint32_t v;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(lost_at) : "memory");
+        return v != 0;
+    };
+    // A wait ends when its phase has, or with the loss of the block's work: when the limit has run out here or elsewhere in the cluster.
+    auto wait_for = [&](auto look) {
+        if (look()) return true;
+        for (uint64_t t0 = nanoseconds(); nanoseconds() - t0 < kWaitMost;)
+            for (int i = 0; i < 64; i++) {
+                if (look()) return true;
+                if (lost()) return false;
+            }
+        lose();
+        return false;
+    };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return wait_for([&] { return mbar_try(bar, parity); }); };
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait(bar, parity)); };
+    auto wait_cluster = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, wait_for([&] { return mbar_try<true>(bar, parity); })); };
+
+    wait_before();
+    if (tid == 0) {
+        for (int i = 0; i < kXStages; i++) {
+            mbar_init(x_full + 8 * i, 1);
+            mbar_init(x_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kCodeStages; i++) {
+            mbar_init(c_full + 8 * i, 1);
+            mbar_init(c_empty + 8 * i, Shape::kDecodeWarps);
+        }
+        for (int i = 0; i < kAStages; i++) {
+            mbar_init(a_full + 8 * i, 8);
+            mbar_init(a_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kDBufs; i++) {
+            mbar_init(d_full + 8 * i, 1);
+            mbar_init(d_empty + 8 * i, NH == 2 ? 8 : 16);
+        }
+        mbar_init(all_done, 1);
+        mbar_init(sums_full, 8 * a.split);
+        mbar_init(sums_empty, 8 * a.split);
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(lost_at), "r"(a.lost) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        tile_map_fetch(&xm);
+        tile_map_fetch(&cm);
+    }
+    if (F32) {  // the levels' bytes: three terms of eight bits each
+        if (tid < 48) {
+            const int term = tid / 16, j = tid % 16;
+            uint32_t bits = 0;
+            if (j < a.m) {
+                float v = static_cast<const float *>(a.levels)[j];
+                for (int i = 0; i <= term; i++) {
+                    bits = __float_as_uint(v) >> 16;
+                    v -= __uint_as_float(bits << 16);
+                }
+            }
+            reinterpret_cast<uint8_t *>(books + 8 * term)[j] = (uint8_t)bits;
+            reinterpret_cast<uint8_t *>(books + 8 * term)[16 + j] = (uint8_t)(bits >> 8);
+        }
+    } else {  // pairs: a warp those with one second level, a lane a copy
+        const uint16_t *levels = static_cast<const uint16_t *>(a.levels);
+        const uint32_t mine = (lane & 15) < a.m ? levels[lane & 15] : 0;
+        for (int hi = wid; hi < 16; hi += Shape::kWarps)
+#pragma unroll
+            for (int lo = 0; lo < 16; lo++)
+                reinterpret_cast<uint32_t *>(smem + Shape::kTableAt)[(16 * hi + lo) * 32 + lane] = __shfl_sync(0xffffffffu, mine, lo) | __shfl_sync(0xffffffffu, mine, hi) << 16;
+    }
+    if (wid == 3) tmem_alloc(tmem_at);
+    __syncthreads();
+    cluster_barrier();
+    uint32_t tmem;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
+
+    // The first row of the matrix that this block has of weight tile t: 128 rows (gated: 64 of each half) from it on.
+    auto rows_at = [&](int t) { return (int64_t)t * (GATED ? 128 : 256) + (int64_t)(rank & 1) * (GATED ? 64 : 128); };
+    const int per_tile = (kb1 - kb0) * terms;  // products' blocks of a tile
+
+    if (wid < 4) {
+        if (Shape::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kRegs));
+        if (lane == 0 && !a.lost) {
+            if (wid == 0) {  // rows of x
+                uint32_t i = 0;
+                bool ok = true;
+                for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                    const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + (int64_t)(rank & 1) * (ND / 2);
+                    for (int v = 0; ok && v < per_tile; v++, i++) {
+                        const uint32_t s = i % kXStages, to = base + s * Shape::kXStage;
+                        if (!(ok = wait(x_empty + 8 * s, (i / kXStages & 1) ^ 1))) break;
+                        mbar_expect(x_full + 8 * s, Shape::kXStage);
+                        const int kb = kb0 + v / terms;
+                        const int64_t from = x0 + (terms > 1 ? kXTerm[v % terms] * a.b : 0);
+#pragma unroll
+                        for (int h = 0; h < NH; h++)
+#pragma unroll
+                            for (int q = 0; q < 2; q++)
+                                tile_load(to + (2 * h + q) * (ND / 2 * 128), &xm, kb * 128 + 64 * q, (int32_t)(from + h * ND), x_full + 8 * s);
+                    }
+                }
+                const uint64_t t0 = nanoseconds();
+                for (uint32_t j = i > kXStages ? i - kXStages : 0; j < i; j++)  // none is on its way when the block ends
+                    mbar_drain(x_full + 8 * (j % kXStages), j / kXStages & 1, t0);
+            } else if (wid == 2) {  // codes
+                uint32_t i = 0;
+                bool ok = true;
+                for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                    const int64_t r0 = rows_at(t / a.x_tiles);
+                    for (int v = 0; ok && v < per_tile; v++, i++) {
+                        const uint32_t s = i % kCodeStages, to = base + kXStages * Shape::kXStage + s * kCodeStage;
+                        if (!(ok = wait(c_empty + 8 * s, (i / kCodeStages & 1) ^ 1))) break;
+                        mbar_expect(c_full + 8 * s, kCodeStage);
+                        const int kb = kb0 + v / terms;
+                        tile_load(to, &cm, kb * 64, (int32_t)r0, c_full + 8 * s);
+                        tile_load(to + kCodeStage / 2, &cm, kb * 64, (int32_t)(r0 + (GATED ? a.second : 64)), c_full + 8 * s);
+                    }
+                }
+                const uint64_t t0 = nanoseconds();
+                for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++) mbar_drain(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1, t0);
+            }
+        }
+        if (wid == 1 && rank == leader) {  // products: the whole warp, so that addresses stay in uniform registers
+            const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
+            const uint16_t both = (uint16_t)(3u << rank);
+            uint32_t xs = 0, as = 0, a_parity = 0, buf = 0, d_parity = 1;
+            bool ok = !a.lost;
+            // Waits for the block's levels (with BLOCK; they and the rows of x come together), and, with `fresh`, for the next NH buffers for sums: one wait
+            // for all, as each costs this warp about a hundred clocks, of the thousand that the tensor core takes for a block.
+            uint32_t d[NH], full[NH];
+            auto ready = [&](auto block, bool fresh) {
+                uint32_t empty[NH], parity[NH];
+                if (fresh) {
+#pragma unroll
+                    for (int h = 0; h < NH; h++) {
+                        d[h] = tmem + buf * ND;
+                        full[h] = d_full + 8 * buf;
+                        empty[h] = d_empty + 8 * buf;
+                        parity[h] = d_parity;
+                        buf = buf + 1 == kDBufs ? 0 : buf + 1;
+                        d_parity ^= buf == 0;
+                    }
+                }
+                const bool there = __all_sync(0xffffffffu, wait_for([&] {
+                    bool r = true;
+                    if (block) {
+                        if (NH == 1) r = mbar_try(a_full + 8 * as, a_parity);
+                        r &= mbar_try(a_full + 8 * as + 8, a_parity);  // (with four decoding warps the second half's levels come after the first's)
+                    }
+                    if (fresh) {
+#pragma unroll
+                        for (int h = 0; h < NH; h++) r &= mbar_try(empty[h], parity[h]);
+                    }
+                    return r;
+                }));
+                tmem_fence_after();
+                return there;
+            };
+            for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                int in_group = kb0 % a.group_blocks, term = 0;
+                bool fresh = true;
+                for (int v = 0; v < per_tile; v++) {
+                    const uint32_t x = mma_rows(base + xs * Shape::kXStage), levels_at = tmem + kAAt + as * kACols;
+                    // The products of 16 entries number k0 .. k1 of the block with half h of the rows of x.
+                    auto steps = [&](int h, int k0, int k1, bool add) {
+#pragma unroll
+                        for (int kk = k0; kk < k1; kk++)
+                            mma_pair(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
+                    };
+                    if (SPANS == 1) {
+                        const bool last = v + 1 == per_tile || (term == terms - 1 && in_group + 1 == a.group_blocks);
+                        if (!(ok = ready(std::true_type{}, fresh))) break;
+                        if (one_lane()) {
+                            if (NH == 2) {
+                                steps(0, 0, 8, !fresh);
+                                if (last) mma_commit(full[0], both);
+                            }
+                            steps(NH - 1, 0, 4, !fresh);
+                            mma_commit(a_empty + 8 * as, both);
+                            steps(NH - 1, 4, 8, true);
+                            if (last) mma_commit(full[NH - 1], both);
+                            mma_commit(a_empty + 8 * as + 8, both);
+                            mma_commit(x_empty + 8 * xs, both);
+                        }
+                        fresh = last;
+                    } else {
+#pragma unroll
+                        for (int sub = 0; sub < SPANS; sub++) {
+                            if (!(ok = sub ? ready(std::false_type{}, true) : ready(std::true_type{}, true))) break;
+                            if (one_lane()) {
+#pragma unroll
+                                for (int h = 0; h < NH; h++) {
+                                    steps(h, sub * (8 / SPANS), (sub + 1) * (8 / SPANS), false);
+                                    mma_commit(full[h], both);
+                                }
+                                if ((sub + 1) % (SPANS / 2) == 0) mma_commit(a_empty + 8 * (as + sub / (SPANS / 2)), both);
+                                if (sub == SPANS - 1) mma_commit(x_empty + 8 * xs, both);
+                            }
+                        }
+                        if (!ok) break;
+                    }
+                    if (++term == terms) {
+                        term = 0;
+                        if (++in_group == a.group_blocks) in_group = 0;
+                    }
+                    xs = xs + 1 == kXStages ? 0 : xs + 1;
+                    as ^= 2;
+                    a_parity ^= as == 0;
+                }
+            }
+        }
+        __syncwarp();
+    } else if (wid < 4 + Shape::kDecodeWarps) {
+        if (Shape::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kDecodeRegs));
+        // Row of the block's 128: of a gated matrix the lower half of each warp has rows of the gate.
+        const int row = 32 * (wid & 3) + lane, from = GATED ? (lane & 16) * 4 + 16 * (wid & 3) + (lane & 15) : row;
+        const uint32_t there = of_rank(a_full, leader), swizzle = (uint32_t)(from >> 1 & 3);
+        constexpr int kHalves = Shape::kDecodeWarps == 8 ? 1 : 2;  // of a block that a warp decodes
+        const int first = kHalves == 1 ? (wid - 4) / 4 : 0;
+        const int total = a.tiles > cluster ? (a.tiles - cluster + clusters - 1) / clusters * per_tile : 0;  // blocks of all tiles
+        const char *codes = smem + kXStages * Shape::kXStage + from * 64;
+        uint32_t w[8 * kHalves], cs = 0, c_parity = 0, xs = 0, x_parity = 0, as = 0, a_parity = 1, term = 0;
+        // The next block's words, in the order of their columns.
+        auto fetch = [&] {
+            if (!wait_warp(c_full + 8 * cs, c_parity)) return false;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const char *at = codes + cs * kCodeStage + ((q ^ swizzle) << 4);
+                if (kHalves == 2) {
+                    const uint4 four = *reinterpret_cast<const uint4 *>(at);
+                    w[q] = four.x, w[q + 4] = four.y, w[q + 8 * (kHalves - 1)] = four.z, w[q + 8 * kHalves - 4] = four.w;
+                } else {
+                    const uint2 two = *reinterpret_cast<const uint2 *>(at + 8 * first);
+                    w[q] = two.x, w[q + 4] = two.y;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(c_empty + 8 * cs);
+            cs = cs + 1 == kCodeStages ? 0 : cs + 1;
+            c_parity ^= cs == 0;
+            return true;
+        };
+        auto decode_half = [&](int half, uint32_t (&pairs)[32]) {
+            if (F32) {
+                uint32_t book[8];
+                const uint4 *from = reinterpret_cast<const uint4 *>(books + 8 * kLevelTerm[term]);
+                *reinterpret_cast<uint4 *>(book) = from[0];
+                *reinterpret_cast<uint4 *>(book + 4) = from[1];
+#pragma unroll
+                for (int q = 0; q < 8; q++) decode(w[8 * half + q], book, pairs + 4 * q);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; q++) look_up(w[8 * half + q], base + Shape::kTableAt + 4 * lane, pairs + 4 * q);
+            }
+        };
+        auto store = [&](int hb, const uint32_t (&pairs)[32]) {
+            const bool free = wait_warp(a_empty + 8 * (as + hb), a_parity);
+            tmem_fence_after();
+            tmem_store(tmem + ((uint32_t)(wid & 3) << 21) + kAAt + (as + hb) * kACols, pairs);
+            return free;
+        };
+        auto stored = [&](int hb) {
+            tmem_stored();
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(there + 8 * (as + hb));
+        };
+        // While a half's levels are on their way to tensor memory, the next half's are looked up.
+        bool ok = !a.lost && (!total || fetch());
+        for (int i = 0; ok && i < total; i++) {
+            uint32_t pairs[32];
+            decode_half(0, pairs);
+            if (!(ok = store(first, pairs))) break;
+            if (kHalves == 2) decode_half(kHalves - 1, pairs);
+            else if (i + 1 < total && !(ok = fetch())) break;
+            // One warp's word stands for the block's rows of x too, so that the issuer has one barrier to wait for.
+            if (wid == 4 && !(ok = wait_warp(x_full + 8 * xs, x_parity))) break;
+            stored(first);
+            if (kHalves == 2) {
+                if (!(ok = store(1, pairs))) break;
+                if (i + 1 < total && !(ok = fetch())) break;
+                stored(1);
+            }
+            xs = xs + 1 == kXStages ? 0 : xs + 1;
+            x_parity ^= xs == 0;
+            as ^= 2;
+            a_parity ^= as == 0;
+            term = term + 1 == terms ? 0 : term + 1;
+        }
+    } else {
+        if (Shape::kUneven) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kAddRegs));
+        const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
+        const uint32_t there = of_rank(d_empty, leader), column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
+        uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0;
+        bool ok = !a.lost;
+        for (int t = cluster; t < a.tiles; t += clusters, turn++) {
+            // This lane's matrix row among the outputs, and its scales in the matrix (of one that exists).
+            const int64_t r0 = rows_at(t / a.x_tiles), row = r0 + (GATED ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
+            const int64_t scales_at = (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row;
+            auto scale = [&](int word) {  // of a word of 32 columns
+                const uint32_t w = min((uint32_t)word, (uint32_t)((a.k - 1) / 32));
+                const int64_t g = scales_at + (a.div_mul ? __umulhi(w, a.div_mul) >> a.div_shift : w >> a.div_shift);
+                if (a.scale_type == ECASQ_F32) return static_cast<const float *>(a.scales)[g];
+                return a.scale_type == ECASQ_F16 ? to_f32(static_cast<const __half *>(a.scales)[g]) : to_f32(static_cast<const __nv_bfloat16 *>(a.scales)[g]);
+            };
+            float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * Shape::kOut * 128;
+            Finish<GATED, NH == 1, F32>(a, sums, r0, rank).announce((int64_t)(t % a.x_tiles) * kN + part * kOwn, kOwn);
+            float acc[kOwn];
+#pragma unroll
+            for (int c = 0; c < kOwn; c++) acc[c] = 0.f;
+            // A group's sums, or what of them is this pair's; the next one's scale is on its way meanwhile.
+            float next = scale(4 * kb0);
+            auto add_span = [&](int next_word) {
+                const float s = next;
+                next = scale(next_word);
+                if (!(ok = wait_warp(d_full + 8 * buf, d_parity))) return;
+                tmem_fence_after();
+                constexpr int kChunk = kOwn < 16 ? kOwn : 16;
+#pragma unroll
+                for (int c = 0; c < kOwn; c += kChunk) {
+                    uint32_t d[kChunk];
+                    tmem_load<kChunk>(d, column + buf * ND + c);
+                    if (c + kChunk == kOwn) {
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(there + 8 * buf);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kChunk; j++) acc[c + j] = fmaf(s, __uint_as_float(d[j]), acc[c + j]);
+                }
+                buf += NH;
+                if (buf >= kDBufs) {
+                    buf -= kDBufs;
+                    d_parity ^= 1;
+                }
+            };
+            if (SPANS == 1) {
+                for (int kb = kb0; ok && kb < kb1;) {
+                    kb += a.group_blocks - kb % a.group_blocks;
+                    add_span(4 * kb);
+                }
+            } else {
+                for (int v = 0, term = 0, kb = kb0; ok && v < per_tile; v++) {
+                    const bool on = ++term == terms;
+#pragma unroll 1
+                    for (int sub = 1; ok && sub <= SPANS; sub++) add_span(4 * (sub == SPANS && on ? kb + 1 : kb) + (sub == SPANS ? 0 : sub * (4 / SPANS)));
+                    if (on) {
+                        term = 0;
+                        kb++;
+                    }
+                }
+            }
+            constexpr int kOut = Shape::kOut;
+            auto four_warps = [&] {
+                if (part) asm volatile("bar.sync 2, 128;" ::: "memory");
+                else asm volatile("bar.sync 1, 128;" ::: "memory");
+            };
+            int c0 = 0, c1 = kOut;
+            if (NH == 1 && a.split > 1) {  // each pair takes a share of the columns over all pairs
+                ok = ok && wait_cluster(sums_empty, (turn & 1) ^ 1);
+                c0 = (int)pair * kOut / a.split;
+                c1 = (int)(pair + 1) * kOut / a.split;
+            }
+            Finish<GATED, NH == 1, F32> finish(a, sums, r0, rank);
+            constexpr int kTurns = finish.kTurns, kAtOnce = finish.kAtOnce;
+#pragma unroll 1
+            for (int q = 0; q < kOwn / kOut; q++) {
+                const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + part * kOwn + q * kOut;
+                const int end = (int)min((int64_t)c1, a.b - x0);
+                finish.fetch(x0, c0 + finish.first(), end);
+                four_warps();
+#pragma unroll
+                for (int c = 0; c < kOut; c++) {
+                    float v = acc[c];
+#pragma unroll
+                    for (int p = 1; p < kOwn / kOut; p++) v = q == p ? acc[p * kOut + c] : v;
+                    sums[128 * c + 32 * quarter + lane] = ok ? v : CUDART_NAN_F;  // (a lost tile's results are NaN, and those of the tiles after it)
+                }
+                if (NH == 1 && a.split > 1) {
+                    __syncwarp();
+                    if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_full, 2 * lane + (rank & 1)));
+                    if (!(ok = ok && wait_cluster(sums_full, turn & 1)))
+                        for (int c = 0; c < kOut; c++) sums[128 * c + 32 * quarter + lane] = CUDART_NAN_F;
+                }
+                four_warps();
+                for (int c = c0 + finish.first(); c < end; c += kTurns * kAtOnce) {
+                    if (c >= c0 + kTurns * kAtOnce) finish.fetch(x0, c, end);
+                    finish.give(x0, c, end);
+                }
+            }
+            if (NH == 1 && a.split > 1) {
+                __syncwarp();
+                if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_empty, 2 * lane + (rank & 1)));
+            }
+        }
+        if (!ok && lane == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
+    }
+    // A block ends when the products that read its memory, and the arrivals that they send, are through.
+    __syncthreads();
+    if (wid == 1 && lane == 0) {
+        if (rank == leader) mma_commit(all_done, (uint16_t)(3u << rank));
+        mbar_drain(all_done, 0, nanoseconds());
+    }
+    __syncthreads();
+    cluster_barrier();
+    if (wid == 3) tmem_free(tmem);
+}
+
+// Clusters of `size` blocks that the card holds at once, asked once a device.
+template <typename K> static int tc_held(K *kernel, int size, int threads, int smem, std::atomic<int> *known, int *held) {
+    int device = 0;
+    ECASQ_CUDA_TRY(cudaGetDevice(&device));
+    *held = device < kDevices ? known[device].load(std::memory_order_acquire) : 0;
+    if (*held > 0) return ECASQ_OK;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)size);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ECASQ_CUDA_TRY(cudaOccupancyMaxActiveClusters(held, kernel, &cfg));
+    if (*held < 1) return ECASQ_ECUDA;
+    if (device < kDevices) known[device].store(*held, std::memory_order_release);
+    return ECASQ_OK;
+}
+
+template <int ND, int NH, bool GATED, int SPANS, bool F32> static int launch_tc(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
+    using Shape = TcShape<ND, NH, GATED, F32>;
+    static_assert(Shape::kBytes <= 227 * 1024 && Shape::kBytes > 114 * 1024, "one block an SM: tensor memory is the block's alone");
+    static std::atomic<int> allowed[kDevices], known[3][kDevices];
+    auto *kernel = k_project_tc<ND, NH, GATED, SPANS, F32>;
+    int rc = allow_smem(kernel, Shape::kBytes, allowed), held = 0;
+    if (!rc) rc = tc_held(kernel, 2 * a.split, Shape::kThreads, Shape::kBytes, known[a.split / 2], &held);
+    if (rc) return rc;
+    const int clusters = std::min(a.tiles, held);
+    return launch_clusters(kernel, dim3((unsigned)(clusters * 2 * a.split)), dim3((unsigned)(2 * a.split)), Shape::kThreads, Shape::kBytes, st, xm, cm, a);
+}
+template <int ND, int NH, bool GATED> static int launch_tc_spans(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
+    // The tensor core's fp32 sums are cut off, not rounded, at each step: of fp32 operands they are taken out after every 32 columns (an error
+    // of 2.8e-7 of the result for k = 1024; after six products of 128, 2.1e-6).
+    if (a.type == ECASQ_F32) return launch_tc<ND, NH, GATED, 4, true>(xm, cm, a, st);
+    if (a.group % 128 == 0) return launch_tc<ND, NH, GATED, 1, false>(xm, cm, a, st);
+    if (a.group % 64 == 0) return launch_tc<ND, NH, GATED, 2, false>(xm, cm, a, st);
+    return launch_tc<ND, NH, GATED, 4, false>(xm, cm, a, st);
+}
+
+// By the widths of a tile that launch_project_tc chooses among.
+template <bool GATED> static int launch_tc_width(int width, const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
+    switch (width) {
+        case 32: return launch_tc_spans<32, 1, GATED>(xm, cm, a, st);
+        case 64: return launch_tc_spans<64, 1, GATED>(xm, cm, a, st);
+        case 128: return launch_tc_spans<128, 1, GATED>(xm, cm, a, st);
+        default: return launch_tc_spans<128, 2, GATED>(xm, cm, a, st);
+    }
+}
+int launch_tc_gated(int width, const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st);
+
+}  // namespace ecasq
