@@ -30,11 +30,11 @@ struct TcArgs {
     Epilogue epi;
 };
 
-constexpr int kDBufs = 3;          // sums in tensor memory; behind them 4 stages of 64 columns of levels
-constexpr int kACols = 32, kAStages = 4, kAAt = 512 - kAStages * kACols;
+constexpr int kDBufs = 3, kACols = 32;  // buffers for sums in tensor memory; columns of it that 64 columns' levels take
 constexpr int kCodeStage = 128 * 64;
 
-// fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.
+// fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  The tensor core's fp32 sums are
+// cut off, not rounded, at each step, so each term's sums of a block are taken out (k = 1024: an error of 2.8e-7 of the result taken out after every two steps, 2.1e-6 after 48).
 __device__ __constant__ const int8_t kXTerm[6] = {0, 0, 0, 1, 1, 2}, kLevelTerm[6] = {0, 1, 2, 0, 1, 0};
 
 // ND columns (rows of x) a product, NH of them a tile.  F32: fp32 operands as bf16 terms, whose levels are found by byte permutes; those of 16-bit
@@ -43,6 +43,8 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr int kN = ND * NH;
     static constexpr int kDecodeWarps = NH == 2 ? 4 : 8, kWarps = 4 + kDecodeWarps + 8, kThreads = 32 * kWarps;
     static constexpr int kXStage = kN / 2 * 256;
+    static constexpr int kAStages = ND == 128 ? 4 : 8, kAAt = 512 - kAStages * kACols;  // stages of levels, behind the sums
+    static_assert(kAAt >= kDBufs * ND, "the sums' buffers end where the levels begin");
     static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
     static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 8 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 10 : 12;
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
@@ -242,7 +244,7 @@ template <int ND, int NH, bool GATED, int SPANS, bool F32>
 __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
                                                                             const __grid_constant__ TcArgs a) {
     using Shape = TcShape<ND, NH, GATED, F32>;
-    constexpr int kN = Shape::kN, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kOwn = Shape::kOwn;
+    constexpr int kN = Shape::kN, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kAStages = Shape::kAStages, kAAt = Shape::kAAt, kOwn = Shape::kOwn;
     extern __shared__ char smem_raw[];
     const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
     char *smem = smem_raw + (base - shared_at(smem_raw));
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                             mma_pair(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
                     };
                     if (SPANS == 1) {
-                        const bool last = v + 1 == per_tile || (term == terms - 1 && in_group + 1 == a.group_blocks);
+                        const bool last = F32 || v + 1 == per_tile || in_group + 1 == a.group_blocks;  // (fp32: every term's sums)
                         if (!(ok = ready(std::true_type{}, fresh))) break;
                         if (one_lane()) {
                             if (NH == 2) {
@@ -464,7 +466,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                         if (++in_group == a.group_blocks) in_group = 0;
                     }
                     xs = xs + 1 == kXStages ? 0 : xs + 1;
-                    as ^= 2;
+                    as = as + 2 == kAStages ? 0 : as + 2;
                     a_parity ^= as == 0;
                 }
             }
@@ -543,7 +545,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             }
             xs = xs + 1 == kXStages ? 0 : xs + 1;
             x_parity ^= xs == 0;
-            as ^= 2;
+            as = as + 2 == kAStages ? 0 : as + 2;
             a_parity ^= as == 0;
             term = term + 1 == terms ? 0 : term + 1;
         }
@@ -594,7 +596,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                     d_parity ^= 1;
                 }
             };
-            if (SPANS == 1) {
+            if (SPANS == 1 && !F32) {
                 for (int kb = kb0; ok && kb < kb1;) {
                     kb += a.group_blocks - kb % a.group_blocks;
                     add_span(4 * kb);
@@ -700,9 +702,11 @@ template <int ND, int NH, bool GATED, int SPANS, bool F32> static int launch_tc(
     return launch_clusters(kernel, dim3((unsigned)(clusters * 2 * a.split)), dim3((unsigned)(2 * a.split)), Shape::kThreads, Shape::kBytes, st, xm, cm, a);
 }
 template <int ND, int NH, bool GATED> static int launch_tc_spans(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
-    // The tensor core's fp32 sums are cut off, not rounded, at each step: of fp32 operands they are taken out after every 32 columns (an error
-    // of 2.8e-7 of the result for k = 1024; after six products of 128, 2.1e-6).
-    if (a.type == ECASQ_F32) return launch_tc<ND, NH, GATED, 4, true>(xm, cm, a, st);
+    if (a.type == ECASQ_F32) {
+        if (a.group % 128 == 0) return launch_tc<ND, NH, GATED, 1, true>(xm, cm, a, st);
+        if (a.group % 64 == 0) return launch_tc<ND, NH, GATED, 2, true>(xm, cm, a, st);
+        return launch_tc<ND, NH, GATED, 4, true>(xm, cm, a, st);
+    }
     if (a.group % 128 == 0) return launch_tc<ND, NH, GATED, 1, false>(xm, cm, a, st);
     if (a.group % 64 == 0) return launch_tc<ND, NH, GATED, 2, false>(xm, cm, a, st);
     return launch_tc<ND, NH, GATED, 4, false>(xm, cm, a, st);
