@@ -26,12 +26,14 @@ struct TcArgs {
     int32_t x_tiles, tiles; // tiles of rows of x; of the product
     uint32_t div_mul, div_shift;  // words of 32 columns to scale groups (FastDiv of group / 32)
     bool wide;              // y and the residual in pieces of four values
+    uint32_t none;          // 0, which the compiler does not know
     uint32_t lost;          // test hook: 1 where blocks begin as if a wait had run out
     Epilogue epi;
 };
 
 constexpr int kDBufs = 3, kACols = 32;  // buffers for sums in tensor memory; columns of it that 64 columns' levels take
 constexpr int kCodeStage = 128 * 64;
+constexpr int kScales = 8;          // scale groups that a thread has on their way
 
 // fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  The tensor core's fp32 sums are
 // cut off, not rounded, at each step, so each term's sums of a block are taken out (k = 1024: an error of 2.8e-7 of the result taken out after every two steps, 2.1e-6 after 48).
@@ -46,16 +48,16 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr int kAStages = ND == 128 ? 4 : 8, kAAt = 512 - kAStages * kACols;  // stages of levels, behind the sums
     static_assert(kAAt >= kDBufs * ND, "the sums' buffers end where the levels begin");
     static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
-    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 8 : 12, kCodeStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 10 : 12;
+    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 8 : 12, kCodeStages = kN >= 256 ? 3 : kN == 128 ? 5 : kN == 64 ? 10 : 12;
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
-    static constexpr int kOut = NH == 2 ? (GATED ? 32 : 16) : kOwn;  // of them at a time on their way out through shared memory
+    static constexpr int kOut = NH == 2 ? 32 : kOwn;  // of them at a time on their way out through shared memory
     static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
     // Registers of a thread of the first four warps, of those that decode and of those that add; together no more than the block was launched with.
     static constexpr bool kUneven = kOwn >= 64;
-    static constexpr int kRegs = NH == 2 ? 56 : 40, kDecodeRegs = NH == 2 ? 88 : 64, kAddRegs = NH == 2 ? 184 : 152;
+    static constexpr int kRegs = NH == 2 ? 56 : 32, kDecodeRegs = NH == 2 ? 88 : 72, kAddRegs = NH == 2 ? 184 : 152;
     static_assert(4 * kRegs + kDecodeWarps * kDecodeRegs + 8 * kAddRegs <= kWarps * (65536 / kThreads / 8 * 8), "the split would wait for ever");
     static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
-    static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kBooksAt = kSumsAt + kSums, kBarsAt = kBooksAt + 128;
+    static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kScalesAt = kSumsAt + kSums, kBooksAt = kScalesAt + 2 * kScales * 128 * 4, kBarsAt = kBooksAt + 128;
     static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
 };
 
@@ -114,7 +116,7 @@ __device__ __forceinline__ void narrow(const float (&v)[4], bool bf16, uint2 &p)
 // bytes a warp, took 60 us a tile of 256 x 256; eight a thread spill, as a thread's sums of the other columns are held meanwhile).  Of a gated
 // matrix a warp had 16 rows of the gate and the same 16 of the other half.  Over split > 1 pairs of the cluster sums are added up.
 template <bool GATED, bool SPLIT, bool F32> struct Finish {
-    static constexpr int kLanes = GATED ? 16 : 32, kAtOnce = 128 / kLanes, kTurns = 4;  // threads of a row of x; rows of x at once; turns that are fetched for together
+    static constexpr int kLanes = GATED ? 16 : 32, kAtOnce = 128 / kLanes, kTurns = GATED ? 2 : 4;  // threads of a row of x; rows of x at once; turns that are fetched for together
     using Bits = FourOf<F32>;
     using One = std::conditional_t<F32, uint32_t, uint16_t>;
     const TcArgs &a;
@@ -143,7 +145,8 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
     }
     // Residuals of columns c, c + kAtOnce, ... (rows of x from x0 on), on their way while something else is done.
     __device__ __forceinline__ void fetch(int64_t x0, int c, int end) {
-        if (GATED || !a.epi.residual || row >= a.n) return;
+        if constexpr (GATED) return;
+        if (!a.epi.residual || row >= a.n) return;
         const One *r = static_cast<const One *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
 #pragma unroll
         for (int i = 0; i < kTurns; i++, r += kAtOnce * a.epi.residual_row)
@@ -151,7 +154,8 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
     }
     // The residuals of columns below `count` come into the L2 cache while the products go on.
     __device__ __forceinline__ void announce(int64_t x0, int count) const {
-        if (GATED || !a.epi.residual || row >= a.n) return;
+        if constexpr (GATED) return;
+        if (!a.epi.residual || row >= a.n) return;
         for (int c = threadIdx.x & 31; c < count && x0 + c < a.b; c += 32) {
             const One *r = static_cast<const One *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + (row - 4 * (threadIdx.x % kLanes)) + 32 * (threadIdx.x / 32 % 4);
             if (row - 4 * (threadIdx.x % kLanes) + 32 * (threadIdx.x / 32 % 4) < a.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(r));
@@ -290,7 +294,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         }
         for (int i = 0; i < kCodeStages; i++) {
             mbar_init(c_full + 8 * i, 1);
-            mbar_init(c_empty + 8 * i, Shape::kDecodeWarps);
+            mbar_init(c_empty + 8 * i, 4);
         }
         for (int i = 0; i < kAStages; i++) {
             mbar_init(a_full + 8 * i, 8);
@@ -405,10 +409,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 }
                 const bool there = __all_sync(0xffffffffu, wait_for([&] {
                     bool r = true;
-                    if (block) {
-                        if (NH == 1) r = mbar_try(a_full + 8 * as, a_parity);
-                        r &= mbar_try(a_full + 8 * as + 8, a_parity);  // (with four decoding warps the second half's levels come after the first's)
-                    }
+                    if (block) r = mbar_try(a_full + 8 * as + 8, a_parity);  // (the second half's levels come after the first's)
                     if (fresh) {
 #pragma unroll
                         for (int h = 0; h < NH; h++) r &= mbar_try(empty[h], parity[h]);
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                         for (int kk = k0; kk < k1; kk++)
                             mma_pair(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
                     };
-                    if (SPANS == 1) {
+                    if constexpr (SPANS == 1) {
                         const bool last = F32 || v + 1 == per_tile || in_group + 1 == a.group_blocks;  // (fp32: every term's sums)
                         if (!(ok = ready(std::true_type{}, fresh))) break;
                         if (one_lane()) {
@@ -477,29 +478,31 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         // Row of the block's 128: of a gated matrix the lower half of each warp has rows of the gate.
         const int row = 32 * (wid & 3) + lane, from = GATED ? (lane & 16) * 4 + 16 * (wid & 3) + (lane & 15) : row;
         const uint32_t there = of_rank(a_full, leader), swizzle = (uint32_t)(from >> 1 & 3);
-        constexpr int kHalves = Shape::kDecodeWarps == 8 ? 1 : 2;  // of a block that a warp decodes
-        const int first = kHalves == 1 ? (wid - 4) / 4 : 0;
+        constexpr int kTeams = Shape::kDecodeWarps / 4;  // of four warps, which take turns at the blocks
+        const int team = (wid - 4) / 4;
         const int total = a.tiles > cluster ? (a.tiles - cluster + clusters - 1) / clusters * per_tile : 0;  // blocks of all tiles
         const char *codes = smem + kXStages * Shape::kXStage + from * 64;
-        uint32_t w[8 * kHalves], cs = 0, c_parity = 0, xs = 0, x_parity = 0, as = 0, a_parity = 1, term = 0;
+        uint32_t w[16], cs = team, c_parity = 0, xs = team, x_parity = 0, as = 2 * team, a_parity = 1, term = team % terms;
+        auto step = [](uint32_t &at, uint32_t by, uint32_t stages, uint32_t &parity) {
+            at += by;
+            if (at >= stages) {
+                at -= stages;
+                parity ^= 1;
+            }
+        };
         // The next block's words, in the order of their columns.
         auto fetch = [&] {
             if (!wait_warp(c_full + 8 * cs, c_parity)) return false;
 #pragma unroll
             for (int q = 0; q < 4; q++) {
-                const char *at = codes + cs * kCodeStage + ((q ^ swizzle) << 4);
-                if (kHalves == 2) {
-                    const uint4 four = *reinterpret_cast<const uint4 *>(at);
-                    w[q] = four.x, w[q + 4] = four.y, w[q + 8 * (kHalves - 1)] = four.z, w[q + 8 * kHalves - 4] = four.w;
-                } else {
-                    const uint2 two = *reinterpret_cast<const uint2 *>(at + 8 * first);
-                    w[q] = two.x, w[q + 4] = two.y;
-                }
+                const uint4 four = *reinterpret_cast<const uint4 *>(codes + cs * kCodeStage + ((q ^ swizzle) << 4));
+                w[q] = four.x, w[q + 4] = four.y, w[q + 8] = four.z, w[q + 12] = four.w;
             }
+            // The stage is free for other codes once these have arrived in registers: the arrival's address waits for them.  (Loads of shared memory may be
+            // moved behind an arrival that does not; block 3's codes then took the place of block 0's.)
             __syncwarp();
-            if (lane == 0) mbar_arrive(c_empty + 8 * cs);
-            cs = cs + 1 == kCodeStages ? 0 : cs + 1;
-            c_parity ^= cs == 0;
+            if (lane == 0) mbar_arrive(c_empty + 8 * cs + ((w[0] ^ w[1] ^ w[2] ^ w[3]) & a.none));
+            step(cs, kTeams, kCodeStages, c_parity);
             return true;
         };
         auto decode_half = [&](int half, uint32_t (&pairs)[32]) {
@@ -528,26 +531,21 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             if (lane == 0) mbar_arrive(there + 8 * (as + hb));
         };
         // While a half's levels are on their way to tensor memory, the next half's are looked up.
-        bool ok = !a.lost && (!total || fetch());
-        for (int i = 0; ok && i < total; i++) {
+        bool ok = !a.lost && (team >= total || fetch());
+        for (int i = team; ok && i < total; i += kTeams) {
             uint32_t pairs[32];
             decode_half(0, pairs);
-            if (!(ok = store(first, pairs))) break;
-            if (kHalves == 2) decode_half(kHalves - 1, pairs);
-            else if (i + 1 < total && !(ok = fetch())) break;
+            if (!(ok = store(0, pairs))) break;
+            decode_half(1, pairs);
             // One warp's word stands for the block's rows of x too, so that the issuer has one barrier to wait for.
-            if (wid == 4 && !(ok = wait_warp(x_full + 8 * xs, x_parity))) break;
-            stored(first);
-            if (kHalves == 2) {
-                if (!(ok = store(1, pairs))) break;
-                if (i + 1 < total && !(ok = fetch())) break;
-                stored(1);
-            }
-            xs = xs + 1 == kXStages ? 0 : xs + 1;
-            x_parity ^= xs == 0;
-            as = as + 2 == kAStages ? 0 : as + 2;
-            a_parity ^= as == 0;
-            term = term + 1 == terms ? 0 : term + 1;
+            if ((wid & 3) == 0 && !(ok = wait_warp(x_full + 8 * xs, x_parity))) break;
+            stored(0);
+            if (!(ok = store(1, pairs))) break;
+            if (i + kTeams < total && !(ok = fetch())) break;
+            stored(1);
+            step(xs, kTeams, kXStages, x_parity);
+            step(as, 2 * kTeams, kAStages, a_parity);
+            term = (term + kTeams) % terms;
         }
     } else {
         if (Shape::kUneven) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kAddRegs));
@@ -559,36 +557,77 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             // This lane's matrix row among the outputs, and its scales in the matrix (of one that exists).
             const int64_t r0 = rows_at(t / a.x_tiles), row = r0 + (GATED ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
             const int64_t scales_at = (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row;
-            auto scale = [&](int word) {  // of a word of 32 columns
-                const uint32_t w = min((uint32_t)word, (uint32_t)((a.k - 1) / 32));
-                const int64_t g = scales_at + (a.div_mul ? __umulhi(w, a.div_mul) >> a.div_shift : w >> a.div_shift);
-                if (a.scale_type == ECASQ_F32) return static_cast<const float *>(a.scales)[g];
-                return a.scale_type == ECASQ_F16 ? to_f32(static_cast<const __half *>(a.scales)[g]) : to_f32(static_cast<const __nv_bfloat16 *>(a.scales)[g]);
-            };
+            // A group's scale comes into the thread's own place kScales - 1 spans ahead of its use (one span ahead, into a register, memory's latency
+            // held up 28672 x 8192 by 64 rows for a tenth of its time): the four bytes that hold it.
+            const uint32_t scales_to = base + Shape::kScalesAt + (part * kScales * 128 + 32 * quarter + lane) * 4;
+            const int scale_size = a.scale_type == ECASQ_F32 ? 4 : 2, group_words = a.group / 32;
+            const char *const scales = static_cast<const char *>(a.scales) + scales_at * scale_size, *const last_scale = scales + ((a.k - 1) / a.group) * scale_size;
             float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * Shape::kOut * 128;
             Finish<GATED, NH == 1, F32>(a, sums, r0, rank).announce((int64_t)(t % a.x_tiles) * kN + part * kOwn, kOwn);
-            float acc[kOwn];
+            uint64_t acc[kOwn / 2];  // pairs of columns
 #pragma unroll
-            for (int c = 0; c < kOwn; c++) acc[c] = 0.f;
-            // A group's sums, or what of them is this pair's; the next one's scale is on its way meanwhile.
-            float next = scale(4 * kb0);
-            auto add_span = [&](int next_word) {
-                const float s = next;
-                next = scale(next_word);
+            for (int c = 0; c < kOwn / 2; c++) acc[c] = 0;
+            // Spans: a group's blocks, or what of them is this pair's; or 64 or 32 columns; of fp32 for each term.
+            struct Span {
+                const char *scale;
+                int word, left, term;  // its first word of 32 columns; words that its group still has; fp32: the term
+            };
+            auto advance = [&](Span &s) {
+                constexpr int kWords = 4 / SPANS;
+                int by = SPANS == 1 && !F32 ? s.left : kWords;
+                if (F32 && (s.word + by) % 4 == 0) {
+                    if (++s.term < terms) by -= 4;  // the block again
+                    else s.term = 0;
+                }
+                s.word += by;
+                s.left -= by;
+                while (F32 && s.left > group_words) {
+                    s.left -= group_words;
+                    s.scale -= scale_size;
+                }
+                if (s.left <= 0) {
+                    s.left += group_words;
+                    s.scale += scale_size;
+                }
+            };
+            Span now{scales + 4 * kb0 / group_words * scale_size, 4 * kb0, group_words - 4 * kb0 % group_words, 0}, ahead = now;
+            auto ask_scale = [&](uint32_t slot) {
+                const char *from = ahead.scale < last_scale ? ahead.scale : last_scale;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n\tcp.async.commit_group;" ::"r"(scales_to + slot * 512), "l"((uintptr_t)from & ~(uintptr_t)3) : "memory");
+                advance(ahead);
+            };
+            uint32_t slot = 0;
+            asm volatile("cp.async.wait_all;" ::: "memory");  // those of the tile before that were not needed
+            for (int j = 0; j < kScales - 1; j++) ask_scale(j);
+            auto add_span = [&] {
+                ask_scale((slot + kScales - 1) % kScales);
+                uint32_t bits;
+                asm volatile("cp.async.wait_group %1;\n\tld.shared.u32 %0, [%2];" : "=r"(bits) : "n"(kScales - 1), "r"(scales_to + slot * 512) : "memory");
+                slot = (slot + 1) % kScales;
+                if (a.scale_type != ECASQ_F32) {
+                    const uint16_t half = (uint16_t)((uintptr_t)(now.scale < last_scale ? now.scale : last_scale) & 2 ? bits >> 16 : bits);
+                    bits = __float_as_uint(a.scale_type == ECASQ_F16 ? to_f32(reinterpret_cast<const __half &>(half)) : to_f32(reinterpret_cast<const __nv_bfloat16 &>(half)));
+                }
+                const uint64_t s = bits | (uint64_t)bits << 32;
+                advance(now);
                 if (!(ok = wait_warp(d_full + 8 * buf, d_parity))) return;
                 tmem_fence_after();
+                // A chunk is on its way while the one before is added.
                 constexpr int kChunk = kOwn < 16 ? kOwn : 16;
+                uint32_t d[2][kChunk];
+                tmem_load<kChunk>(d[0], column + buf * ND);
 #pragma unroll
                 for (int c = 0; c < kOwn; c += kChunk) {
-                    uint32_t d[kChunk];
-                    tmem_load<kChunk>(d, column + buf * ND + c);
-                    if (c + kChunk == kOwn) {
+                    tmem_loaded(d[c / kChunk & 1]);
+                    if (c + kChunk < kOwn) {
+                        tmem_load<kChunk>(d[c / kChunk + 1 & 1], column + buf * ND + c + kChunk);
+                    } else {
                         tmem_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(there + 8 * buf);
                     }
 #pragma unroll
-                    for (int j = 0; j < kChunk; j++) acc[c + j] = fmaf(s, __uint_as_float(d[j]), acc[c + j]);
+                    for (int j = 0; j < kChunk / 2; j++) acc[c / 2 + j] = fma_pair(s, d[c / kChunk & 1][2 * j] | (uint64_t)d[c / kChunk & 1][2 * j + 1] << 32, acc[c / 2 + j]);
                 }
                 buf += NH;
                 if (buf >= kDBufs) {
@@ -596,22 +635,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                     d_parity ^= 1;
                 }
             };
-            if (SPANS == 1 && !F32) {
-                for (int kb = kb0; ok && kb < kb1;) {
-                    kb += a.group_blocks - kb % a.group_blocks;
-                    add_span(4 * kb);
-                }
-            } else {
-                for (int v = 0, term = 0, kb = kb0; ok && v < per_tile; v++) {
-                    const bool on = ++term == terms;
-#pragma unroll 1
-                    for (int sub = 1; ok && sub <= SPANS; sub++) add_span(4 * (sub == SPANS && on ? kb + 1 : kb) + (sub == SPANS ? 0 : sub * (4 / SPANS)));
-                    if (on) {
-                        term = 0;
-                        kb++;
-                    }
-                }
-            }
+            while (ok && now.word < 4 * kb1) add_span();
             constexpr int kOut = Shape::kOut;
             auto four_warps = [&] {
                 if (part) asm volatile("bar.sync 2, 128;" ::: "memory");
@@ -632,11 +656,13 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 finish.fetch(x0, c0 + finish.first(), end);
                 four_warps();
 #pragma unroll
-                for (int c = 0; c < kOut; c++) {
-                    float v = acc[c];
+                for (int c = 0; c < kOut; c += 2) {
+                    uint64_t v = acc[c / 2];
 #pragma unroll
-                    for (int p = 1; p < kOwn / kOut; p++) v = q == p ? acc[p * kOut + c] : v;
-                    sums[128 * c + 32 * quarter + lane] = ok ? v : CUDART_NAN_F;  // (a lost tile's results are NaN, and those of the tiles after it)
+                    for (int p = 1; p < kOwn / kOut; p++) v = q == p ? acc[(p * kOut + c) / 2] : v;
+                    // (A lost tile's results are NaN, and those of the tiles after it.)
+                    sums[128 * c + 32 * quarter + lane] = ok ? __uint_as_float((uint32_t)v) : CUDART_NAN_F;
+                    sums[128 * c + 128 + 32 * quarter + lane] = ok ? __uint_as_float((uint32_t)(v >> 32)) : CUDART_NAN_F;
                 }
                 if (NH == 1 && a.split > 1) {
                     __syncwarp();
