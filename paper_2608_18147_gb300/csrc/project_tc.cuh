@@ -33,7 +33,7 @@ struct TcArgs {
 
 constexpr int kDBufs = 3, kACols = 32;  // buffers for sums in tensor memory; columns of it that 64 columns' levels take
 constexpr int kCodeStage = 128 * 64;
-constexpr int kScales = 8;          // scale groups that a thread has on their way
+constexpr int kScales = 8, kScaleLag = 6;  // scale groups in shared memory; of them on their way
 
 // fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  The tensor core's fp32 sums are
 // cut off, not rounded, at each step, so each term's sums of a block are taken out (k = 1024: an error of 2.8e-7 of the result taken out after every two steps, 2.1e-6 after 48).
@@ -54,10 +54,10 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
     // Registers of a thread of the first four warps, of those that decode and of those that add; together no more than the block was launched with.
     static constexpr bool kUneven = kOwn >= 64;
-    static constexpr int kRegs = NH == 2 ? 56 : 32, kDecodeRegs = NH == 2 ? 88 : 72, kAddRegs = NH == 2 ? 184 : 152;
+    static constexpr int kRegs = 48, kDecodeRegs = 80, kAddRegs = NH == 2 ? 192 : 136;
     static_assert(4 * kRegs + kDecodeWarps * kDecodeRegs + 8 * kAddRegs <= kWarps * (65536 / kThreads / 8 * 8), "the split would wait for ever");
-    static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 3;
-    static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kScalesAt = kSumsAt + kSums, kBooksAt = kScalesAt + 2 * kScales * 128 * 4, kBarsAt = kBooksAt + 128;
+    static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 2 * kScales + 3;
+    static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kScalesAt = kSumsAt + kSums, kBooksAt = kScalesAt + kScales * 128 * 4, kBarsAt = kBooksAt + 128;
     static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
 };
 
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
     const uint32_t bars = base + Shape::kBarsAt;
     const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
                    a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
-                   all_done = d_empty + 8 * kDBufs, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
+                   s_full = d_empty + 8 * kDBufs, s_empty = s_full + 8 * kScales, all_done = s_empty + 8 * kScales, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
     uint32_t *books = reinterpret_cast<uint32_t *>(smem + Shape::kBooksAt);
     constexpr int terms = F32 ? 6 : 1;
     const int kb0 = (int)((int64_t)a.blocks * pair / a.split), kb1 = (int)((int64_t)a.blocks * (pair + 1) / a.split);
@@ -303,6 +303,10 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         for (int i = 0; i < kDBufs; i++) {
             mbar_init(d_full + 8 * i, 1);
             mbar_init(d_empty + 8 * i, NH == 2 ? 8 : 16);
+        }
+        for (int i = 0; i < kScales; i++) {
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(s_empty + 8 * i, 8);
         }
         mbar_init(all_done, 1);
         mbar_init(sums_full, 8 * a.split);
@@ -385,6 +389,74 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 const uint64_t t0 = nanoseconds();
                 for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++) mbar_drain(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1, t0);
             }
+        }
+        if (wid == 3) {
+            // Scales: of each span its groups' scales of the block's 128 rows, four a lane, as fp32.  They come kScaleLag spans ahead, the four bytes
+            // that hold each.  Spans are a group's blocks, or what of them is this pair's; or 64 or 32 columns; of fp32 for each term.
+            struct Span {
+                int group, word, left, term;  // its first word of 32 columns; words that its group still has; fp32: the term
+            };
+            const int scale_size = a.scale_type == ECASQ_F32 ? 4 : 2, group_words = a.group / 32, last_group = (int)((a.k - 1) / a.group);
+            auto advance = [&](Span &s) {
+                constexpr int kWords = 4 / SPANS;
+                int by = SPANS == 1 && !F32 ? s.left : kWords;
+                if (F32 && (s.word + by) % 4 == 0) {
+                    if (++s.term < terms) by -= 4;  // the block again
+                    else s.term = 0;
+                }
+                s.word += by;
+                s.left -= by;
+                while (F32 && s.left > group_words) {
+                    s.left -= group_words;
+                    s.group--;
+                }
+                if (s.left <= 0) {
+                    s.left += group_words;
+                    s.group++;
+                }
+            };
+            uint32_t asked = 0, given = 0;
+            bool ok = !a.lost;
+            const uint32_t to = base + Shape::kScalesAt + 4 * lane;
+            for (int t = cluster; ok && t < a.tiles; t += clusters) {
+                const char *from[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int64_t row = rows_at(t / a.x_tiles) + (GATED ? 16 * i + (lane & 15) : 32 * i + lane);
+                    from[i] = static_cast<const char *>(a.scales) + (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row * scale_size;
+                }
+                Span ask{4 * kb0 / group_words, 4 * kb0, group_words - 4 * kb0 % group_words, 0}, give = ask;
+                for (int turn = 0; ok && give.word < 4 * kb1; turn++) {
+                    if (ask.word < 4 * kb1) {
+                        const uint32_t slot = asked % kScales;
+                        if (!(ok = wait_warp(s_empty + 8 * slot, (asked / kScales & 1) ^ 1))) break;
+                        const int64_t at = (int64_t)min(ask.group, last_group) * scale_size;
+#pragma unroll
+                        for (int i = 0; i < 4; i++)
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + slot * 512 + 128 * i), "l"((uintptr_t)(from[i] + at) & ~(uintptr_t)3) : "memory");
+                        advance(ask);
+                        asked++;
+                    }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (turn < kScaleLag) continue;
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kScaleLag) : "memory");
+                    const uint32_t slot = given % kScales;
+                    if (scale_size == 2) {
+                        uint32_t *v = reinterpret_cast<uint32_t *>(smem + Shape::kScalesAt) + slot * 128 + lane;
+                        const int64_t at = (int64_t)min(give.group, last_group) * 2;
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            const uint16_t half = (uint16_t)((uintptr_t)(from[i] + at) & 2 ? v[32 * i] >> 16 : v[32 * i]);
+                            v[32 * i] = __float_as_uint(a.scale_type == ECASQ_F16 ? to_f32(reinterpret_cast<const __half &>(half)) : to_f32(reinterpret_cast<const __nv_bfloat16 &>(half)));
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_full + 8 * slot);
+                    advance(give);
+                    given++;
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
         }
         if (wid == 1 && rank == leader) {  // products: the whole warp, so that addresses stay in uniform registers
             const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
@@ -551,91 +623,61 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         if (Shape::kUneven) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kAddRegs));
         const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
         const uint32_t there = of_rank(d_empty, leader), column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
-        uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0;
+        // Spans of a tile.
+        const int spans = SPANS == 1 && !F32 ? (kb1 - 1) / a.group_blocks - kb0 / a.group_blocks + 1 : per_tile * SPANS;
+        uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0, span = 0;
         bool ok = !a.lost;
         for (int t = cluster; t < a.tiles; t += clusters, turn++) {
-            // This lane's matrix row among the outputs, and its scales in the matrix (of one that exists).
-            const int64_t r0 = rows_at(t / a.x_tiles), row = r0 + (GATED ? 16 * quarter + (lane & 15) : 32 * quarter + lane);
-            const int64_t scales_at = (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row;
-            // A group's scale comes into the thread's own place kScales - 1 spans ahead of its use (one span ahead, into a register, memory's latency
-            // held up 28672 x 8192 by 64 rows for a tenth of its time): the four bytes that hold it.
-            const uint32_t scales_to = base + Shape::kScalesAt + (part * kScales * 128 + 32 * quarter + lane) * 4;
-            const int scale_size = a.scale_type == ECASQ_F32 ? 4 : 2, group_words = a.group / 32;
-            const char *const scales = static_cast<const char *>(a.scales) + scales_at * scale_size, *const last_scale = scales + ((a.k - 1) / a.group) * scale_size;
+            const int64_t r0 = rows_at(t / a.x_tiles);
             float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * Shape::kOut * 128;
             Finish<GATED, NH == 1, F32>(a, sums, r0, rank).announce((int64_t)(t % a.x_tiles) * kN + part * kOwn, kOwn);
             uint64_t acc[kOwn / 2];  // pairs of columns
 #pragma unroll
             for (int c = 0; c < kOwn / 2; c++) acc[c] = 0;
-            // Spans: a group's blocks, or what of them is this pair's; or 64 or 32 columns; of fp32 for each term.
-            struct Span {
-                const char *scale;
-                int word, left, term;  // its first word of 32 columns; words that its group still has; fp32: the term
-            };
-            auto advance = [&](Span &s) {
-                constexpr int kWords = 4 / SPANS;
-                int by = SPANS == 1 && !F32 ? s.left : kWords;
-                if (F32 && (s.word + by) % 4 == 0) {
-                    if (++s.term < terms) by -= 4;  // the block again
-                    else s.term = 0;
-                }
-                s.word += by;
-                s.left -= by;
-                while (F32 && s.left > group_words) {
-                    s.left -= group_words;
-                    s.scale -= scale_size;
-                }
-                if (s.left <= 0) {
-                    s.left += group_words;
-                    s.scale += scale_size;
-                }
-            };
-            Span now{scales + 4 * kb0 / group_words * scale_size, 4 * kb0, group_words - 4 * kb0 % group_words, 0}, ahead = now;
-            auto ask_scale = [&](uint32_t slot) {
-                const char *from = ahead.scale < last_scale ? ahead.scale : last_scale;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n\tcp.async.commit_group;" ::"r"(scales_to + slot * 512), "l"((uintptr_t)from & ~(uintptr_t)3) : "memory");
-                advance(ahead);
-            };
-            uint32_t slot = 0;
-            asm volatile("cp.async.wait_all;" ::: "memory");  // those of the tile before that were not needed
-            for (int j = 0; j < kScales - 1; j++) ask_scale(j);
             auto add_span = [&] {
-                ask_scale((slot + kScales - 1) % kScales);
-                uint32_t bits;
-                asm volatile("cp.async.wait_group %1;\n\tld.shared.u32 %0, [%2];" : "=r"(bits) : "n"(kScales - 1), "r"(scales_to + slot * 512) : "memory");
-                slot = (slot + 1) % kScales;
-                if (a.scale_type != ECASQ_F32) {
-                    const uint16_t half = (uint16_t)((uintptr_t)(now.scale < last_scale ? now.scale : last_scale) & 2 ? bits >> 16 : bits);
-                    bits = __float_as_uint(a.scale_type == ECASQ_F16 ? to_f32(reinterpret_cast<const __half &>(half)) : to_f32(reinterpret_cast<const __nv_bfloat16 &>(half)));
-                }
+                const uint32_t slot = 8 * (span % kScales), parity = span / kScales & 1;
+                ok = __all_sync(0xffffffffu, wait_for([&] {
+                    const bool there = mbar_try(s_full + slot, parity);
+                    return (bool)(mbar_try(d_full + 8 * buf, d_parity) & there);
+                }));
+                if (!ok) return;
+                const uint32_t bits = reinterpret_cast<const uint32_t *>(smem + Shape::kScalesAt)[16 * slot + 32 * quarter + lane];
                 const uint64_t s = bits | (uint64_t)bits << 32;
-                advance(now);
-                if (!(ok = wait_warp(d_full + 8 * buf, d_parity))) return;
                 tmem_fence_after();
-                // A chunk is on its way while the one before is added.
-                constexpr int kChunk = kOwn < 16 ? kOwn : 16;
+                // Sixteen columns are on their way while the sixteen before them are added: a load takes about ninety clocks until its values are there,
+                // whatever its width.
+                constexpr int kChunk = kOwn < 32 ? kOwn / 2 : 16;
                 uint32_t d[2][kChunk];
                 tmem_load<kChunk>(d[0], column + buf * ND);
+                tmem_load<kChunk>(d[1], column + buf * ND + kChunk);
 #pragma unroll
-                for (int c = 0; c < kOwn; c += kChunk) {
-                    tmem_loaded(d[c / kChunk & 1]);
-                    if (c + kChunk < kOwn) {
-                        tmem_load<kChunk>(d[c / kChunk + 1 & 1], column + buf * ND + c + kChunk);
-                    } else {
+                for (int c = 0; c < kOwn; c += 2 * kChunk) {
+                    tmem_loaded(d[0], d[1]);
+                    if (c + 2 * kChunk == kOwn) {
                         tmem_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(there + 8 * buf);
                     }
 #pragma unroll
-                    for (int j = 0; j < kChunk / 2; j++) acc[c / 2 + j] = fma_pair(s, d[c / kChunk & 1][2 * j] | (uint64_t)d[c / kChunk & 1][2 * j + 1] << 32, acc[c / 2 + j]);
+                    for (int half = 0; half < 2; half++) {
+#pragma unroll
+                        for (int j = 0; j < kChunk / 2; j++) {
+                            uint64_t &to = acc[(c + half * kChunk) / 2 + j];
+                            to = fma_pair(s, d[half][2 * j] | (uint64_t)d[half][2 * j + 1] << 32, to);
+                        }
+                        if (c + 2 * kChunk < kOwn) tmem_load<kChunk>(d[half], column + buf * ND + c + (2 + half) * kChunk);
+                    }
                 }
+                span++;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_empty + slot + (bits & a.none));
                 buf += NH;
                 if (buf >= kDBufs) {
                     buf -= kDBufs;
                     d_parity ^= 1;
                 }
             };
-            while (ok && now.word < 4 * kb1) add_span();
+            for (int j = 0; ok && j < spans; j++) add_span();
             constexpr int kOut = Shape::kOut;
             auto four_warps = [&] {
                 if (part) asm volatile("bar.sync 2, 128;" ::: "memory");
