@@ -8,7 +8,7 @@
 
 #include <algorithm>
 
-#include "codes.cuh"
+#include "epilogue.cuh"
 
 namespace ecasq {
 
@@ -27,6 +27,8 @@ struct MatvecArgs {
     int32_t pitch, scale_pitch;   // 16-bit types: bytes from one row to the next in a stage, and among the scales
     int32_t pieces_below;         // 16-bit types: halves of stages that lie below the table
     uint32_t lost;                // test hook: 1 where blocks begin as if a wait had run out
+    int64_t second;               // gated: rows of the matrix before its other half
+    Epilogue epi;                 // what follows the product
     uint32_t div_mul, div_shift;  // words of 32 columns to scale groups: w div (group / 32), as umulhi(w, div_mul) >> div_shift
                                   // or w >> div_shift if div_mul is 0
 };
@@ -83,11 +85,29 @@ __device__ __forceinline__ uint32_t group_of(const MatvecArgs &a, uint32_t w) {
     return min(w, (uint32_t)a.groups - 1);
 }
 
-// Blocks of a launch, one for each SM (152), more where a block would have over kRowsMost rows.  The block's run of rows:
+// Blocks of a launch, one for each SM (152), more where a block would have over `most` rows.  The block's run of rows:
 // whole eights, as even as they can be.
-static inline int64_t row_blocks(int64_t n) { return std::max(std::min<int64_t>(cdiv(n, 8), 152), cdiv(cdiv(n, 8), kRowsMost / 8)); }
+static inline int64_t row_blocks(int64_t n, int most) { return std::max(std::min<int64_t>(cdiv(n, 8), 152), cdiv(cdiv(n, 8), most / 8)); }
 __device__ __forceinline__ int64_t row_of(const MatvecArgs &a, unsigned block, unsigned blocks) { return min(a.n, (a.n + 7) / 8 * block / blocks * 8); }
 
-int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st);
+// What follows a product's sum v: nothing, ecasq_project's epilogue, or with u, that of the same row of the other half, ecasq_gated's.
+enum After { kPlain, kProject, kGated };
+template <typename T, After AFTER> __device__ __forceinline__ T result(const MatvecArgs &a, float v, float u, float bias, float residual) {
+    if (AFTER == kProject) v = activate(v + bias, a.epi.act) + residual;
+    if (AFTER == kGated) v = activate(v, a.epi.act) * u;
+    return from_f32<T>(v);
+}
+// What ecasq_project adds to output r of row i of x.
+template <typename T, After AFTER> __device__ __forceinline__ float bias_of(const MatvecArgs &a, int64_t r) {
+    return AFTER == kProject && a.epi.bias ? to_f32(static_cast<const T *>(a.epi.bias)[r]) : 0.f;
+}
+template <typename T, After AFTER> __device__ __forceinline__ float residual_of(const MatvecArgs &a, int64_t i, int64_t r) {
+    return AFTER == kProject && a.epi.residual ? to_f32(static_cast<const T *>(a.epi.residual)[i * a.epi.residual_row + r]) : 0.f;
+}
+
+// The kernels' launches, a unit each: fp32 and 16-bit types; a.n is the number of outputs.
+int launch_matvec_f32(MatvecArgs &a, After after, int32_t group, cudaStream_t st);
+int launch_matvec_project(MatvecArgs &a, int32_t type, bool scales32, int32_t group, cudaStream_t st);
+int launch_matvec_gated(MatvecArgs &a, int32_t type, bool scales32, int32_t group, cudaStream_t st);
 
 }  // namespace ecasq

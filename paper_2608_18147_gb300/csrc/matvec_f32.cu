@@ -73,8 +73,11 @@ struct Sums {
 };
 
 // WIDE: a scale group holds whole 128-column blocks (8192 x 8192 by one row, groups of 128: 29.9 us, and 33.0 without).
-template <bool WIDE>
+// Of a gated matrix a tile is eight rows of the gate and the same eight of the other half.
+template <bool WIDE, After AFTER>
 __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constant__ MatvecArgs a) {
+    constexpr bool kTwo = AFTER == kGated;
+    constexpr int kTile = kTwo ? 8 : 16;  // outputs of a tile
     extern __shared__ __align__(128) char smem[];
     char *table = smem;
     float *sums = reinterpret_cast<float *>(smem + kTableBytes);
@@ -84,13 +87,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
     if (a.chunk < a.k) rest += kRowSumBytes;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t entry0 = smem_at(table) + 8 * (lane & 15);
-    const int wk = wid & (a.warps_k - 1), wr = wid / a.warps_k, tiles = kWarps / a.warps_k, rows_at_once = 16 * tiles;
+    const int wk = wid & (a.warps_k - 1), wr = wid / a.warps_k, tiles = kWarps / a.warps_k, rows_at_once = 16 * tiles, outputs = kTile * tiles;
     const int i0 = 8 * blockIdx.y, nb = min(8, a.b - i0);
     float *xs = reinterpret_cast<float *>(rest);  // x, a.chunk columns a row
     const char *ring = rest + nb * a.chunk * 4;
     const int pitch = a.chunk / 2 + kRowPad, stage_bytes = rows_at_once * pitch;
     const int64_t r0 = row_of(a, blockIdx.x, gridDim.x);
-    const int rows = (int)(row_of(a, blockIdx.x + 1, gridDim.x) - r0), rounds = (rows + rows_at_once - 1) / rows_at_once;
+    const int rows = (int)(row_of(a, blockIdx.x + 1, gridDim.x) - r0), rounds = (rows + outputs - 1) / outputs;
     const uint8_t *codes = a.codes + r0 * a.code_row;
     const float *scales = static_cast<const float *>(a.scales) + r0 * a.scale_row;
 
@@ -110,9 +113,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
         const int cols = (int)min((int64_t)a.chunk, a.k - k0), blocks = (cols + 127) / 128;
         if (k0) __syncthreads();
         auto fetch = [&](int round, int s) {
-            const int first = round * rows_at_once, count = min(rows_at_once, rows - first);
-            if (tid == 0) bar_expect(bars + 8 * s, count * blocks * 64);
-            if (tid < count) bulk_copy(smem_at(ring + s * stage_bytes + tid * pitch), codes + (first + tid) * a.code_row + k0 / 2, blocks * 64, bars + 8 * s);
+            const int first = round * outputs, count = min(outputs, rows - first), output = kTwo ? tid / 16 * 8 + (tid & 7) : tid;
+            if (tid == 0) bar_expect(bars + 8 * s, count * (16 / kTile) * blocks * 64);
+            if (tid < rows_at_once && output < count)
+                bulk_copy(smem_at(ring + s * stage_bytes + tid * pitch), codes + (first + output + (kTwo ? (tid >> 3 & 1) * a.second : 0)) * a.code_row + k0 / 2, blocks * 64, bars + 8 * s);
         };
         for (int s = 0; s < a.stages && s < rounds; s++) fetch(s, s);
 
@@ -130,10 +134,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
         // the run repeat its last one; their sums are not stored.
         float next_a, next_b;
         auto next_scales = [&](int round, int at) {
-            const int row = round * rows_at_once + 16 * wr + g;
+            const int row = round * outputs + kTile * wr + g;
             const uint32_t w = group_of(a, (uint32_t)(k0 / 32) + 4 * at + (WIDE ? 0 : t));
             next_a = scales[min(row, rows - 1) * a.scale_row + w];
-            next_b = scales[min(row + 8, rows - 1) * a.scale_row + w];
+            next_b = scales[(kTwo ? min(row, rows - 1) + a.second : min(row + 8, rows - 1)) * a.scale_row + w];
         };
         next_scales(0, wk);
         // x, zero beyond k.
@@ -176,17 +180,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
             }
             if (round + a.stages < rounds) fetch(round + a.stages, s);
             // The tiles' sums over their warps: 16 rows of 8 columns each.
-            for (int i = tid; i < 128 * tiles; i += kThreads) {
-                float v = 0.f;
-                const float *from = buf + (i >> 7) * a.warps_k * 128 + (i & 127);
-                for (int w = 0; w < a.warps_k; w++) v += from[w * 128];
-                const int at = round * rows_at_once + i / 8, col = i & 7;
-                if (at < rows && col < nb) {
+            for (int i = tid; i < 8 * outputs; i += kThreads) {
+                float v = 0.f, u = 0.f;
+                const int at = round * outputs + i / 8, col = i & 7;
+                const bool there = at < rows && col < nb, last = there && k0 + a.chunk >= a.k;
+                const float bias = last ? bias_of<float, AFTER>(a, r0 + at) : 0.f, residual = last ? residual_of<float, AFTER>(a, i0 + col, r0 + at) : 0.f;
+                const float *from = buf + i / (8 * kTile) * a.warps_k * 128 + i % (8 * kTile);
+                for (int w = 0; w < a.warps_k; w++) {
+                    v += from[w * 128];
+                    if (kTwo) u += from[w * 128 + 64];
+                }
+                if (there) {
                     if (a.chunk < a.k) {
                         if (k0) v += row_sums[at * 8 + col];
                         row_sums[at * 8 + col] = v;
+                        if (kTwo) {
+                            if (k0) u += row_sums[kRowsMost / 2 * 8 + at * 8 + col];
+                            row_sums[kRowsMost / 2 * 8 + at * 8 + col] = u;
+                        }
                     }
-                    if (k0 + a.chunk >= a.k) static_cast<float *>(a.y)[(i0 + col) * a.y_row + r0 + at] = v;
+                    if (last) static_cast<float *>(a.y)[(i0 + col) * a.y_row + r0 + at] = result<float, AFTER>(a, v, u, bias, residual);
                 }
             }
             turn ^= 1;  // the next round's sums go to the other half: one barrier a round
@@ -202,8 +215,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_matvec_f32(const __grid_constan
     }
 }
 
-int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st) {
-    const int64_t blocks = row_blocks(a.n), tiles = cdiv(cdiv(cdiv(a.n, 8), blocks), 2), kb = cdiv(a.k, 128), nb = std::min(a.b, 8);
+template <After AFTER> static int launch_f32(MatvecArgs &a, int32_t group, cudaStream_t st) {
+    const int64_t blocks = row_blocks(a.n, AFTER == kGated ? kRowsMost / 2 : kRowsMost), tiles = cdiv(cdiv(cdiv(a.n, 8), blocks), AFTER == kGated ? 1 : 2), kb = cdiv(a.k, 128), nb = std::min(a.b, 8);
     const int64_t room = 227 * 1024 - kTableBytes - kSumBytes - kBarBytes - kRowSumBytes;
     // The warps' split between columns and row tiles that leaves the fullest warp the least; of equal ones that with the
     // fewest warps a tile, whose sums have to be joined.
@@ -225,10 +238,15 @@ int launch_matvec_f32(MatvecArgs &a, int32_t group, cudaStream_t st) {
     const int smem = (int)(227 * 1024 - room - (a.chunk < a.k ? 0 : kRowSumBytes) + x_bytes + a.stages * stage(chunk));
     static std::atomic<int> allowed[2][kDevices];
     const bool wide = group % 128 == 0;
-    auto *kernel = wide ? k_matvec_f32<true> : k_matvec_f32<false>;
+    auto *kernel = wide ? k_matvec_f32<true, AFTER> : k_matvec_f32<false, AFTER>;
     const int rc = allow_smem(kernel, 227 * 1024, allowed[wide]);
     if (rc) return rc;
     return launch_early(kernel, dim3((unsigned)blocks, (unsigned)cdiv(a.b, 8)), kThreads, smem, st, a);
+}
+
+int launch_matvec_f32(MatvecArgs &a, After after, int32_t group, cudaStream_t st) {
+    if (after == kGated) return launch_f32<kGated>(a, group, st);
+    return after == kProject ? launch_f32<kProject>(a, group, st) : launch_f32<kPlain>(a, group, st);
 }
 
 }  // namespace ecasq
