@@ -88,19 +88,20 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     const int64_t piece = 4 * type_size(p.type);
     const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
     a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
-    const int64_t w_tiles = cdiv(p.n, p.gated ? 128 : 256);
     const int width = p.b <= 32 ? 32 : p.b <= 64 ? 64 : p.b <= 128 ? 128 : 256;
+    const bool pair = width > 64;
+    const int64_t w_tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1));
     a.x_tiles = (int32_t)cdiv(p.b, width);
     const int64_t tiles = w_tiles * a.x_tiles;
     if (tiles > INT32_MAX) return ECASQ_EINVAL;
     a.tiles = (int32_t)tiles;
     a.split = 1;
     if (width < 256)
-        while (a.split < 4 && tiles * 2 * a.split <= 76 && 2 * a.split <= a.blocks) a.split *= 2;
+        while (a.split < 4 && tiles * 2 * a.split <= (pair ? 76 : 152) && 2 * a.split <= a.blocks) a.split *= 2;
     CUtensorMap xm, cm;
-    const int nd = width == 256 ? 128 : width;
+    const int x_rows = std::min(width, 128) / (pair ? 2 : 1);
     int rc = make_tile_map(&xm, p.type == ECASQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, p.k, f32 ? 3 * p.b : p.b,
-                           (p.b > 1 || f32 ? x_row : laid_row(p.k)) * 2, 64, nd / 2, CU_TENSOR_MAP_SWIZZLE_128B);
+                           (p.b > 1 || f32 ? x_row : laid_row(p.k)) * 2, 64, x_rows, CU_TENSOR_MAP_SWIZZLE_128B);
     if (!rc) rc = make_tile_map(&cm, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.codes, 64 * cdiv(p.k, 128), rows, p.code_row, 64, 64, CU_TENSOR_MAP_SWIZZLE_64B);
     if (rc) return rc;
     return p.gated ? launch_tc_gated(width, xm, cm, a, st) : launch_tc_width<false>(width, xm, cm, a, st);

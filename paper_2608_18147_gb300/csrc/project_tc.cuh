@@ -31,7 +31,7 @@ struct TcArgs {
     Epilogue epi;
 };
 
-constexpr int kDBufs = 3, kACols = 32;  // buffers for sums in tensor memory; columns of it that 64 columns' levels take
+constexpr int kACols = 32;  // columns of tensor memory that 64 columns' levels take
 constexpr int kCodeStage = 128 * 64;
 constexpr int kScales = 8, kScaleLag = 6;  // scale groups in shared memory; of them on their way
 
@@ -44,11 +44,17 @@ __device__ __constant__ const int8_t kXTerm[6] = {0, 0, 0, 1, 1, 2}, kLevelTerm[
 template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr int kN = ND * NH;
     static constexpr int kDecodeWarps = NH == 2 ? 4 : 8, kWarps = 4 + kDecodeWarps + 8, kThreads = 32 * kWarps;
-    static constexpr int kXStage = kN / 2 * 256;
+    // Two blocks of a cluster take 256 rows of the matrix together, and each brings half of the rows of x, where these are many; where they are few, and what
+    // takes time are the ways between the warps, not the bytes, a block works alone: none of its barriers is another's.
+    static constexpr bool kPair = kN > 64;
+    static constexpr int kBlocks = kPair ? 2 : 1, kXRows = ND / kBlocks;  // rows of x that a block brings for one product
+    static constexpr int kRows = (GATED ? 64 : 128) * kBlocks;            // outputs of a row of x in a tile
+    static constexpr int kXStage = NH * kXRows * 256;
+    static constexpr int kDBufs = ND == 128 ? 3 : ND == 64 ? 4 : 8;       // buffers for sums in tensor memory
     static constexpr int kAStages = ND == 128 ? 4 : 8, kAAt = 512 - kAStages * kACols;  // stages of levels, behind the sums
     static_assert(kAAt >= kDBufs * ND, "the sums' buffers end where the levels begin");
     static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
-    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 8 : 12, kCodeStages = kN >= 256 ? 3 : kN == 128 ? 5 : kN == 64 ? 10 : 12;
+    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 5 : 8, kCodeStages = kN >= 256 ? 3 : kN == 128 ? 5 : kN == 64 ? 9 : 12;
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
     static constexpr int kOut = NH == 2 ? 32 : kOwn;  // of them at a time on their way out through shared memory
     static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
@@ -122,17 +128,17 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
     const TcArgs &a;
     const float *sums;
     int64_t row;       // the thread's first output
-    uint32_t rank;
+    uint32_t first, stride;  // ranks of the blocks whose sums are added up: first, first + stride, ...
     bool whole;        // its four lie side by side and aligned
     Bits residual[GATED ? 1 : kTurns];
 
-    __device__ __forceinline__ Finish(const TcArgs &a, const float *from, int64_t r0, uint32_t rank) : a(a), rank(rank) {
+    __device__ __forceinline__ Finish(const TcArgs &a, const float *from, int64_t r0, uint32_t first, uint32_t stride) : a(a), first(first), stride(stride) {
         const int part = threadIdx.x % kLanes;
         row = r0 + 4 * part;
         whole = a.wide && row + 4 <= a.n;
         sums = from + (GATED ? 32 * (part >> 2) + 4 * (part & 3) : 4 * part);
     }
-    __device__ __forceinline__ int first() const { return (threadIdx.x & 127) / kLanes; }
+    __device__ __forceinline__ int turn() const { return (threadIdx.x & 127) / kLanes; }
     // The four at p, or those of them that there are.
     __device__ __forceinline__ Bits load(const One *p) const {
         if (whole) return *reinterpret_cast<const Bits *>(p);
@@ -171,7 +177,7 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
         for (int p = 0; p < a.split; p++) {
             float4 f;
             asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                         : "r"(of_rank(shared_at(at), 2 * p + (rank & 1))) : "memory");
+                         : "r"(of_rank(shared_at(at), first + p * stride)) : "memory");
             v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
         }
     }
@@ -248,12 +254,13 @@ template <int ND, int NH, bool GATED, int SPANS, bool F32>
 __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
                                                                             const __grid_constant__ TcArgs a) {
     using Shape = TcShape<ND, NH, GATED, F32>;
-    constexpr int kN = Shape::kN, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kAStages = Shape::kAStages, kAAt = Shape::kAAt, kOwn = Shape::kOwn;
+    constexpr bool kPair = Shape::kPair;
+    constexpr int kN = Shape::kN, kDBufs = Shape::kDBufs, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kAStages = Shape::kAStages, kAAt = Shape::kAAt, kOwn = Shape::kOwn;
     extern __shared__ char smem_raw[];
     const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
     char *smem = smem_raw + (base - shared_at(smem_raw));
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const uint32_t rank = cluster_rank(), leader = rank & ~1u, size = 2 * a.split, pair = rank / 2;
+    const uint32_t rank = cluster_rank(), half = kPair ? rank & 1 : 0, leader = rank - half, size = Shape::kBlocks * a.split, pair = rank / Shape::kBlocks;
     const uint32_t bars = base + Shape::kBarsAt;
     const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
                    a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
@@ -297,12 +304,12 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             mbar_init(c_empty + 8 * i, 4);
         }
         for (int i = 0; i < kAStages; i++) {
-            mbar_init(a_full + 8 * i, 8);
+            mbar_init(a_full + 8 * i, 4 * Shape::kBlocks);
             mbar_init(a_empty + 8 * i, 1);
         }
         for (int i = 0; i < kDBufs; i++) {
             mbar_init(d_full + 8 * i, 1);
-            mbar_init(d_empty + 8 * i, NH == 2 ? 8 : 16);
+            mbar_init(d_empty + 8 * i, (NH == 2 ? 4 : 8) * Shape::kBlocks);
         }
         for (int i = 0; i < kScales; i++) {
             mbar_init(s_full + 8 * i, 1);
@@ -338,14 +345,14 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             for (int lo = 0; lo < 16; lo++)
                 reinterpret_cast<uint32_t *>(smem + Shape::kTableAt)[(16 * hi + lo) * 32 + lane] = __shfl_sync(0xffffffffu, mine, lo) | __shfl_sync(0xffffffffu, mine, hi) << 16;
     }
-    if (wid == 3) tmem_alloc(tmem_at);
+    if (wid == 3) tmem_alloc<kPair>(tmem_at);
     __syncthreads();
     cluster_barrier();
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
 
     // The first row of the matrix that this block has of weight tile t: 128 rows (gated: 64 of each half) from it on.
-    auto rows_at = [&](int t) { return (int64_t)t * (GATED ? 128 : 256) + (int64_t)(rank & 1) * (GATED ? 64 : 128); };
+    auto rows_at = [&](int t) { return (int64_t)t * Shape::kRows + half * (GATED ? 64 : 128); };
     const int per_tile = (kb1 - kb0) * terms;  // products' blocks of a tile
 
     if (wid < 4) {
@@ -355,7 +362,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 uint32_t i = 0;
                 bool ok = true;
                 for (int t = cluster; ok && t < a.tiles; t += clusters) {
-                    const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + (int64_t)(rank & 1) * (ND / 2);
+                    const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + half * Shape::kXRows;
                     for (int v = 0; ok && v < per_tile; v++, i++) {
                         const uint32_t s = i % kXStages, to = base + s * Shape::kXStage;
                         if (!(ok = wait(x_empty + 8 * s, (i / kXStages & 1) ^ 1))) break;
@@ -366,7 +373,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                         for (int h = 0; h < NH; h++)
 #pragma unroll
                             for (int q = 0; q < 2; q++)
-                                tile_load(to + (2 * h + q) * (ND / 2 * 128), &xm, kb * 128 + 64 * q, (int32_t)(from + h * ND), x_full + 8 * s);
+                                tile_load(to + (2 * h + q) * (Shape::kXRows * 128), &xm, kb * 128 + 64 * q, (int32_t)(from + h * ND), x_full + 8 * s);
                     }
                 }
                 const uint64_t t0 = nanoseconds();
@@ -451,7 +458,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                         }
                     }
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(s_full + 8 * slot);
+                    if (lane == 0) mbar_arrive_own(s_full + 8 * slot);
                     advance(give);
                     given++;
                 }
@@ -459,8 +466,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             asm volatile("cp.async.wait_all;" ::: "memory");
         }
         if (wid == 1 && rank == leader) {  // products: the whole warp, so that addresses stay in uniform registers
-            const uint32_t kind = mma_kind(a.type != ECASQ_F16, 256, ND);
-            const uint16_t both = (uint16_t)(3u << rank);
+            const uint32_t kind = mma_kind(a.type != ECASQ_F16, 128 * Shape::kBlocks, ND);
             uint32_t xs = 0, as = 0, a_parity = 0, buf = 0, d_parity = 1;
             bool ok = !a.lost;
             // Waits for the block's levels (with BLOCK; they and the rows of x come together), and, with `fresh`, for the next NH buffers for sums: one wait
@@ -500,7 +506,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                     auto steps = [&](int h, int k0, int k1, bool add) {
 #pragma unroll
                         for (int kk = k0; kk < k1; kk++)
-                            mma_pair(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (ND / 2 * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
+                            mma<kPair>(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (Shape::kXRows * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
                     };
                     if constexpr (SPANS == 1) {
                         const bool last = F32 || v + 1 == per_tile || in_group + 1 == a.group_blocks;  // (fp32: every term's sums)
@@ -508,14 +514,14 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                         if (one_lane()) {
                             if (NH == 2) {
                                 steps(0, 0, 8, !fresh);
-                                if (last) mma_commit(full[0], both);
+                                if (last) mma_commit<kPair>(full[0], rank);
                             }
                             steps(NH - 1, 0, 4, !fresh);
-                            mma_commit(a_empty + 8 * as, both);
+                            mma_commit<kPair>(a_empty + 8 * as, rank);
                             steps(NH - 1, 4, 8, true);
-                            if (last) mma_commit(full[NH - 1], both);
-                            mma_commit(a_empty + 8 * as + 8, both);
-                            mma_commit(x_empty + 8 * xs, both);
+                            if (last) mma_commit<kPair>(full[NH - 1], rank);
+                            mma_commit<kPair>(a_empty + 8 * as + 8, rank);
+                            mma_commit<kPair>(x_empty + 8 * xs, rank);
                         }
                         fresh = last;
                     } else {
@@ -526,10 +532,10 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
 #pragma unroll
                                 for (int h = 0; h < NH; h++) {
                                     steps(h, sub * (8 / SPANS), (sub + 1) * (8 / SPANS), false);
-                                    mma_commit(full[h], both);
+                                    mma_commit<kPair>(full[h], rank);
                                 }
-                                if ((sub + 1) % (SPANS / 2) == 0) mma_commit(a_empty + 8 * (as + sub / (SPANS / 2)), both);
-                                if (sub == SPANS - 1) mma_commit(x_empty + 8 * xs, both);
+                                if ((sub + 1) % (SPANS / 2) == 0) mma_commit<kPair>(a_empty + 8 * (as + sub / (SPANS / 2)), rank);
+                                if (sub == SPANS - 1) mma_commit<kPair>(x_empty + 8 * xs, rank);
                             }
                         }
                         if (!ok) break;
@@ -549,7 +555,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         if (Shape::kUneven) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kDecodeRegs));
         // Row of the block's 128: of a gated matrix the lower half of each warp has rows of the gate.
         const int row = 32 * (wid & 3) + lane, from = GATED ? (lane & 16) * 4 + 16 * (wid & 3) + (lane & 15) : row;
-        const uint32_t there = of_rank(a_full, leader), swizzle = (uint32_t)(from >> 1 & 3);
+        const uint32_t there = kPair ? of_rank(a_full, leader) : a_full, swizzle = (uint32_t)(from >> 1 & 3);
         constexpr int kTeams = Shape::kDecodeWarps / 4;  // of four warps, which take turns at the blocks
         const int team = (wid - 4) / 4;
         const int total = a.tiles > cluster ? (a.tiles - cluster + clusters - 1) / clusters * per_tile : 0;  // blocks of all tiles
@@ -573,7 +579,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             // The stage is free for other codes once these have arrived in registers: the arrival's address waits for them.  (Loads of shared memory may be
             // moved behind an arrival that does not; block 3's codes then took the place of block 0's.)
             __syncwarp();
-            if (lane == 0) mbar_arrive(c_empty + 8 * cs + ((w[0] ^ w[1] ^ w[2] ^ w[3]) & a.none));
+            if (lane == 0) mbar_arrive_own(c_empty + 8 * cs + ((w[0] ^ w[1] ^ w[2] ^ w[3]) & a.none));
             step(cs, kTeams, kCodeStages, c_parity);
             return true;
         };
@@ -600,7 +606,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             tmem_stored();
             tmem_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(there + 8 * (as + hb));
+            if (lane == 0) mbar_arrive_at<kPair>(there + 8 * (as + hb));
         };
         // While a half's levels are on their way to tensor memory, the next half's are looked up.
         bool ok = !a.lost && (team >= total || fetch());
@@ -622,7 +628,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
     } else {
         if (Shape::kUneven) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kAddRegs));
         const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
-        const uint32_t there = of_rank(d_empty, leader), column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
+        const uint32_t there = kPair ? of_rank(d_empty, leader) : d_empty, column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
         // Spans of a tile.
         const int spans = SPANS == 1 && !F32 ? (kb1 - 1) / a.group_blocks - kb0 / a.group_blocks + 1 : per_tile * SPANS;
         uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0, span = 0;
@@ -630,7 +636,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         for (int t = cluster; t < a.tiles; t += clusters, turn++) {
             const int64_t r0 = rows_at(t / a.x_tiles);
             float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * Shape::kOut * 128;
-            Finish<GATED, NH == 1, F32>(a, sums, r0, rank).announce((int64_t)(t % a.x_tiles) * kN + part * kOwn, kOwn);
+            Finish<GATED, NH == 1, F32>(a, sums, r0, half, Shape::kBlocks).announce((int64_t)(t % a.x_tiles) * kN + part * kOwn, kOwn);
             uint64_t acc[kOwn / 2];  // pairs of columns
 #pragma unroll
             for (int c = 0; c < kOwn / 2; c++) acc[c] = 0;
@@ -656,7 +662,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                     if (c + 2 * kChunk == kOwn) {
                         tmem_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(there + 8 * buf);
+                        if (lane == 0) mbar_arrive_at<kPair>(there + 8 * buf);
                     }
 #pragma unroll
                     for (int half = 0; half < 2; half++) {
@@ -670,7 +676,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 }
                 span++;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(s_empty + slot + (bits & a.none));
+                if (lane == 0) mbar_arrive_own(s_empty + slot + (bits & a.none));
                 buf += NH;
                 if (buf >= kDBufs) {
                     buf -= kDBufs;
@@ -689,13 +695,13 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 c0 = (int)pair * kOut / a.split;
                 c1 = (int)(pair + 1) * kOut / a.split;
             }
-            Finish<GATED, NH == 1, F32> finish(a, sums, r0, rank);
+            Finish<GATED, NH == 1, F32> finish(a, sums, r0, half, Shape::kBlocks);
             constexpr int kTurns = finish.kTurns, kAtOnce = finish.kAtOnce;
 #pragma unroll 1
             for (int q = 0; q < kOwn / kOut; q++) {
                 const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + part * kOwn + q * kOut;
                 const int end = (int)min((int64_t)c1, a.b - x0);
-                finish.fetch(x0, c0 + finish.first(), end);
+                finish.fetch(x0, c0 + finish.turn(), end);
                 four_warps();
 #pragma unroll
                 for (int c = 0; c < kOut; c += 2) {
@@ -708,19 +714,19 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 }
                 if (NH == 1 && a.split > 1) {
                     __syncwarp();
-                    if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_full, 2 * lane + (rank & 1)));
+                    if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_full, Shape::kBlocks * lane + half));
                     if (!(ok = ok && wait_cluster(sums_full, turn & 1)))
                         for (int c = 0; c < kOut; c++) sums[128 * c + 32 * quarter + lane] = CUDART_NAN_F;
                 }
                 four_warps();
-                for (int c = c0 + finish.first(); c < end; c += kTurns * kAtOnce) {
+                for (int c = c0 + finish.turn(); c < end; c += kTurns * kAtOnce) {
                     if (c >= c0 + kTurns * kAtOnce) finish.fetch(x0, c, end);
                     finish.give(x0, c, end);
                 }
             }
             if (NH == 1 && a.split > 1) {
                 __syncwarp();
-                if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_empty, 2 * lane + (rank & 1)));
+                if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_empty, Shape::kBlocks * lane + half));
             }
         }
         if (!ok && lane == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
@@ -728,12 +734,12 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
     // A block ends when the products that read its memory, and the arrivals that they send, are through.
     __syncthreads();
     if (wid == 1 && lane == 0) {
-        if (rank == leader) mma_commit(all_done, (uint16_t)(3u << rank));
+        if (rank == leader) mma_commit<kPair>(all_done, rank);
         mbar_drain(all_done, 0, nanoseconds());
     }
     __syncthreads();
     cluster_barrier();
-    if (wid == 3) tmem_free(tmem);
+    if (wid == 3) tmem_free<kPair>(tmem);
 }
 
 // Clusters of `size` blocks that the card holds at once, asked once a device.
@@ -763,11 +769,11 @@ template <int ND, int NH, bool GATED, int SPANS, bool F32> static int launch_tc(
     static_assert(Shape::kBytes <= 227 * 1024 && Shape::kBytes > 114 * 1024, "one block an SM: tensor memory is the block's alone");
     static std::atomic<int> allowed[kDevices], known[3][kDevices];
     auto *kernel = k_project_tc<ND, NH, GATED, SPANS, F32>;
+    const int size = Shape::kBlocks * a.split;
     int rc = allow_smem(kernel, Shape::kBytes, allowed), held = 0;
-    if (!rc) rc = tc_held(kernel, 2 * a.split, Shape::kThreads, Shape::kBytes, known[a.split / 2], &held);
+    if (!rc) rc = tc_held(kernel, size, Shape::kThreads, Shape::kBytes, known[a.split / 2], &held);
     if (rc) return rc;
-    const int clusters = std::min(a.tiles, held);
-    return launch_clusters(kernel, dim3((unsigned)(clusters * 2 * a.split)), dim3((unsigned)(2 * a.split)), Shape::kThreads, Shape::kBytes, st, xm, cm, a);
+    return launch_clusters(kernel, dim3((unsigned)(std::min(a.tiles, held) * size)), dim3((unsigned)size), Shape::kThreads, Shape::kBytes, st, xm, cm, a);
 }
 template <int ND, int NH, bool GATED> static int launch_tc_spans(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
     if (a.type == ECASQ_F32) {

@@ -26,13 +26,17 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, int count) { asm volatil
 __device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// An arrival, here or at another block of the cluster (`bar`: an address in the cluster; an own one's address is one too), and the look whether a
-// phase is over.  What they order: tensor memory with its fences, tiles brought in by copies, and the block's own shared memory.  The
-// forms that order all of the cluster's memory (CLUSTER) wait for every store on its way and drop cached lines: with them everywhere a
-// product took five times as long.
+// An arrival at a barrier of the block; one at any of the cluster (`bar`: an address in it); and the look whether a phase is over.  What they order: tensor
+// memory with its fences, tiles brought in by copies, and the block's own shared memory.  The forms that order all of the cluster's
+// memory (CLUSTER) wait for every store on its way and drop cached lines: with them everywhere a product took five times as long.
+__device__ __forceinline__ void mbar_arrive_own(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 template <bool CLUSTER = false> __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     if (CLUSTER) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
     else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+template <bool ELSEWHERE> __device__ __forceinline__ void mbar_arrive_at(uint32_t bar) {
+    if (ELSEWHERE) mbar_arrive(bar);
+    else mbar_arrive_own(bar);
 }
 template <bool CLUSTER = false> __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
@@ -57,10 +61,14 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, uint64
 }
 
 // ---------------------------------------------------------------- tensor memory
-// All 512 columns, for both blocks of a pair; a whole warp of each calls these.
-__device__ __forceinline__ void tmem_alloc(uint32_t to) { asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(to) : "memory"); }
-__device__ __forceinline__ void tmem_free(uint32_t at) {
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n\ttcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
+// All 512 columns, of a block or of both blocks of a pair (PAIR); a whole warp of each calls these.
+template <bool PAIR> __device__ __forceinline__ void tmem_alloc(uint32_t to) {
+    if (PAIR) asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n\ttcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::"r"(to) : "memory");
+    else asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n\ttcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::"r"(to) : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void tmem_free(uint32_t at) {
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -111,16 +119,24 @@ __host__ __device__ constexpr uint32_t mma_kind(bool bf16, int m, int n) {
 // descriptor, to which a distance in 16 bytes can be added; the high word is the same for all.
 __device__ __forceinline__ uint32_t mma_rows(uint32_t at) { return at >> 4 | 1u << 16; }
 constexpr uint32_t kMmaRowsHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
-// D (+)= A B^T over 16 entries of the summed index, for a pair of blocks: A in tensor memory, 128 rows in each; B in shared memory, half of
-// the rows in each.
-__device__ __forceinline__ void mma_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t kind, bool add) {
-    asm volatile("{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b),
-                 "r"(kind), "r"((uint32_t)add), "n"(kMmaRowsHigh)
-                 : "memory");
+// D (+)= A B^T over 16 entries of the summed index: A in tensor memory, 128 rows; B in shared memory.  For a pair of blocks (PAIR) each has its own rows of A and
+// of D, and half of the rows of B.
+template <bool PAIR> __device__ __forceinline__ void mma(uint32_t d, uint32_t a, uint32_t b, uint32_t kind, bool add) {
+    if (PAIR)
+        asm volatile("{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b),
+                     "r"(kind), "r"((uint32_t)add), "n"(kMmaRowsHigh)
+                     : "memory");
+    else
+        asm volatile("{ .reg .pred p; .reg .b64 b; mov.b64 b, {%2, %5}; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p; }" ::"r"(d), "r"(a), "r"(b),
+                     "r"(kind), "r"((uint32_t)add), "n"(kMmaRowsHigh)
+                     : "memory");
 }
-// An arrival at this barrier in the blocks of `mask`, once all products issued before have been done.
-__device__ __forceinline__ void mma_commit(uint32_t bar, uint16_t mask) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
+// An arrival at this barrier, of a pair in both blocks, once all products issued before have been done; rank: the first block's.
+template <bool PAIR> __device__ __forceinline__ void mma_commit(uint32_t bar, uint32_t rank) {
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)(3u << rank)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 // ---------------------------------------------------------------- tiles
