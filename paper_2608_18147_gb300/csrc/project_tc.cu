@@ -89,15 +89,22 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
     a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
     const int width = p.b <= 32 ? 32 : p.b <= 64 ? 64 : p.b <= 128 ? 128 : 256;
-    const bool pair = width > 64;
+    const bool pair = width > 128;
     const int64_t w_tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1));
     a.x_tiles = (int32_t)cdiv(p.b, width);
     const int64_t tiles = w_tiles * a.x_tiles;
     if (tiles > INT32_MAX) return ECASQ_EINVAL;
     a.tiles = (int32_t)tiles;
+    // The blocks of a cluster that share a tile's columns: what takes the fewest blocks of columns one after another, each tile with six blocks' time for its
+    // start and its results, and two more for their joining.  (Clusters of more than two leave some SMs out.)
     a.split = 1;
-    if (width < 256)
-        while (a.split < 4 && tiles * 2 * a.split <= (pair ? 76 : 152) && 2 * a.split <= a.blocks) a.split *= 2;
+    int64_t best = INT64_MAX;
+    for (int s = 1; s <= (pair ? 1 : kSplitMost) && s <= a.blocks; s++) {
+        const int64_t held = s <= 2 ? 152 / s / (pair ? 2 : 1) : 144 / s, cost = cdiv(tiles, held) * (cdiv(a.blocks, s) + (s > 1 ? 8 : 6));
+        if (cost >= best) continue;
+        best = cost;
+        a.split = s;
+    }
     CUtensorMap xm, cm;
     const int x_rows = std::min(width, 128) / (pair ? 2 : 1);
     int rc = make_tile_map(&xm, p.type == ECASQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, p.k, f32 ? 3 * p.b : p.b,

@@ -32,7 +32,7 @@ struct TcArgs {
 };
 
 constexpr int kACols = 32;  // columns of tensor memory that 64 columns' levels take
-constexpr int kCodeStage = 128 * 64;
+constexpr int kCodeStage = 128 * 64, kSplitMost = 8;
 constexpr int kScales = 8, kScaleLag = 6;  // scale groups in shared memory; of them on their way
 
 // fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  The tensor core's fp32 sums are
@@ -46,7 +46,7 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr int kDecodeWarps = NH == 2 ? 4 : 8, kWarps = 4 + kDecodeWarps + 8, kThreads = 32 * kWarps;
     // Two blocks of a cluster take 256 rows of the matrix together, and each brings half of the rows of x, where these are many; where they are few, and what
     // takes time are the ways between the warps, not the bytes, a block works alone: none of its barriers is another's.
-    static constexpr bool kPair = kN > 64;
+    static constexpr bool kPair = kN > 128;
     static constexpr int kBlocks = kPair ? 2 : 1, kXRows = ND / kBlocks;  // rows of x that a block brings for one product
     static constexpr int kRows = (GATED ? 64 : 128) * kBlocks;            // outputs of a row of x in a tile
     static constexpr int kXStage = NH * kXRows * 256;
@@ -54,7 +54,7 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr int kAStages = ND == 128 ? 4 : 8, kAAt = 512 - kAStages * kACols;  // stages of levels, behind the sums
     static_assert(kAAt >= kDBufs * ND, "the sums' buffers end where the levels begin");
     static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
-    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 5 : kN == 64 ? 5 : 8, kCodeStages = kN >= 256 ? 3 : kN == 128 ? 5 : kN == 64 ? 9 : 12;
+    static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 3 : kN == 64 ? 5 : 8, kCodeStages = kN >= 128 ? 3 : kN == 64 ? 9 : 12;
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
     static constexpr int kOut = NH == 2 ? 32 : kOwn;  // of them at a time on their way out through shared memory
     static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
@@ -767,11 +767,11 @@ template <typename K> static int tc_held(K *kernel, int size, int threads, int s
 template <int ND, int NH, bool GATED, int SPANS, bool F32> static int launch_tc(const CUtensorMap &xm, const CUtensorMap &cm, const TcArgs &a, cudaStream_t st) {
     using Shape = TcShape<ND, NH, GATED, F32>;
     static_assert(Shape::kBytes <= 227 * 1024 && Shape::kBytes > 114 * 1024, "one block an SM: tensor memory is the block's alone");
-    static std::atomic<int> allowed[kDevices], known[3][kDevices];
+    static std::atomic<int> allowed[kDevices], known[kSplitMost + 1][kDevices];
     auto *kernel = k_project_tc<ND, NH, GATED, SPANS, F32>;
     const int size = Shape::kBlocks * a.split;
     int rc = allow_smem(kernel, Shape::kBytes, allowed), held = 0;
-    if (!rc) rc = tc_held(kernel, size, Shape::kThreads, Shape::kBytes, known[a.split / 2], &held);
+    if (!rc) rc = tc_held(kernel, size, Shape::kThreads, Shape::kBytes, known[a.split], &held);
     if (rc) return rc;
     return launch_clusters(kernel, dim3((unsigned)(std::min(a.tiles, held) * size)), dim3((unsigned)size), Shape::kThreads, Shape::kBytes, st, xm, cm, a);
 }
