@@ -88,23 +88,35 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     const int64_t piece = 4 * type_size(p.type);
     const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
     a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
-    const int width = p.b <= 32 ? 32 : p.b <= 64 ? 64 : p.b <= 128 ? 128 : 256;
-    const bool pair = width > 128;
-    const int64_t w_tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1));
+    // The width of a tile and the blocks of a cluster that share its columns that take the least time: rounds of tiles over the card, each of its blocks of
+    // columns one after another, whose time goes by the width and by the scale groups in one (measured: 0.55 + 0.28 us a group for 128 rows of x), and of
+    // the tile's start and results.  Only tiles of 256 rows take pairs of blocks; clusters of more than two leave some SMs out.
+    struct Choice {
+        int width, block, group, tile;  // rows of x; hundredths of a microsecond
+    };
+    static constexpr Choice kChoices[] = {{32, 35, 16, 200}, {64, 45, 23, 250}, {128, 55, 28, 300}, {256, 50, 40, 400}};
+    const int terms = f32 ? 6 : 1, share = f32 ? std::min(p.group, 128) : (int)std::min<int64_t>(p.group, 1 << 20);
+    int64_t best = INT64_MAX;
+    int width = 0;
+    for (const Choice &c : kChoices) {
+        if (c.width < 256 && p.b > 4 * c.width) continue;  // (more than four tiles side by side decode the matrix too often)
+        const bool pair = c.width == 256;
+        const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * cdiv(p.b, c.width);
+        for (int s = 1; s <= (pair ? 1 : kSplitMost) && s <= a.blocks; s++) {
+            const int64_t held = pair ? 76 : s <= 2 ? 152 / s : 144 / s;
+            const int64_t cost = cdiv(tiles, held) * (cdiv(a.blocks, s) * terms * (c.block + c.group * 128 / share) + c.tile + (s > 1 ? 60 : 0));
+            if (cost >= best) continue;
+            best = cost;
+            width = c.width;
+            a.split = s;
+        }
+        if (c.width >= p.b) break;
+    }
+    const bool pair = width == 256;
     a.x_tiles = (int32_t)cdiv(p.b, width);
-    const int64_t tiles = w_tiles * a.x_tiles;
+    const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * a.x_tiles;
     if (tiles > INT32_MAX) return ECASQ_EINVAL;
     a.tiles = (int32_t)tiles;
-    // The blocks of a cluster that share a tile's columns: what takes the fewest blocks of columns one after another, each tile with six blocks' time for its
-    // start and its results, and two more for their joining.  (Clusters of more than two leave some SMs out.)
-    a.split = 1;
-    int64_t best = INT64_MAX;
-    for (int s = 1; s <= (pair ? 1 : kSplitMost) && s <= a.blocks; s++) {
-        const int64_t held = s <= 2 ? 152 / s / (pair ? 2 : 1) : 144 / s, cost = cdiv(tiles, held) * (cdiv(a.blocks, s) + (s > 1 ? 8 : 6));
-        if (cost >= best) continue;
-        best = cost;
-        a.split = s;
-    }
     CUtensorMap xm, cm;
     const int x_rows = std::min(width, 128) / (pair ? 2 : 1);
     int rc = make_tile_map(&xm, p.type == ECASQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, p.k, f32 ? 3 * p.b : p.b,
