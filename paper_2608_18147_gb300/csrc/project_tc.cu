@@ -89,22 +89,24 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
     a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
     // The width of a tile and the blocks of a cluster that share its columns that take the least time: rounds of tiles over the card, each of its blocks of
-    // columns one after another, whose time goes by the width and by the scale groups in one (measured: 0.55 + 0.28 us a group for 128 rows of x), and of
-    // the tile's start and results.  Only tiles of 256 rows take pairs of blocks; clusters of more than two leave some SMs out.
+    // columns one after another, whose time goes by the width and by the scale groups in one (measured: 0.27 + 0.35 us a group for 128 rows of x), and of
+    // the tile's start and results.  Only tiles of 256 rows take pairs of blocks; clusters of more than two leave some SMs out (kHeld: what the card holds
+    // of each size).
     struct Choice {
         int width, block, group, tile;  // rows of x; hundredths of a microsecond
     };
-    static constexpr Choice kChoices[] = {{32, 35, 16, 200}, {64, 45, 23, 250}, {128, 55, 28, 300}, {256, 50, 40, 400}};
+    static constexpr Choice kChoices[] = {{32, 24, 21, 110}, {64, 23, 28, 190}, {128, 27, 35, 350}, {256, 38, 40, 690}};
+    static constexpr int kHeld[] = {152, 76, 46, 36, 28, 23};
+    static_assert(sizeof kHeld / sizeof *kHeld == kSplitMost, "");
     const int terms = f32 ? 6 : 1, share = f32 ? std::min(p.group, 128) : (int)std::min<int64_t>(p.group, 1 << 20);
     int64_t best = INT64_MAX;
     int width = 0;
     for (const Choice &c : kChoices) {
-        if (c.width < 256 && p.b > 4 * c.width) continue;  // (more than four tiles side by side decode the matrix too often)
         const bool pair = c.width == 256;
         const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * cdiv(p.b, c.width);
         for (int s = 1; s <= (pair ? 1 : kSplitMost) && s <= a.blocks; s++) {
-            const int64_t held = pair ? 76 : s <= 2 ? 152 / s : 144 / s;
-            const int64_t cost = cdiv(tiles, held) * (cdiv(a.blocks, s) * terms * (c.block + c.group * 128 / share) + c.tile + (s > 1 ? 60 : 0));
+            const int64_t held = pair ? 76 : kHeld[s - 1];
+            const int64_t cost = cdiv(tiles, held) * (cdiv(a.blocks, s) * terms * (c.block + c.group * 128 / share) + c.tile + (s > 1 ? 20 + 30 * s : 0));
             if (cost >= best) continue;
             best = cost;
             width = c.width;

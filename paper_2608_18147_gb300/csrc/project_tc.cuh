@@ -32,7 +32,7 @@ struct TcArgs {
 };
 
 constexpr int kACols = 32;  // columns of tensor memory that 64 columns' levels take
-constexpr int kCodeStage = 128 * 64, kSplitMost = 8;
+constexpr int kCodeStage = 128 * 64, kSplitMost = 6;
 constexpr int kScales = 8, kScaleLag = 6;  // scale groups in shared memory; of them on their way
 
 // fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  The tensor core's fp32 sums are
