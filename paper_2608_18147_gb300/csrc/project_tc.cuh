@@ -131,6 +131,8 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
     uint32_t first, stride;  // ranks of the blocks whose sums are added up: first, first + stride, ...
     bool whole;        // its four lie side by side and aligned
     Bits residual[GATED ? 1 : kTurns];
+    const One *ahead = nullptr;  // the next residual; columns from it on
+    int left = 0;
 
     __device__ __forceinline__ Finish(const TcArgs &a, const float *from, int64_t r0, uint32_t first, uint32_t stride) : a(a), first(first), stride(stride) {
         const int part = threadIdx.x % kLanes;
@@ -149,14 +151,20 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
         memcpy(&b, v, sizeof b);
         return b;
     }
-    // Residuals of columns c, c + kAtOnce, ... (rows of x from x0 on), on their way while something else is done.
-    __device__ __forceinline__ void fetch(int64_t x0, int c, int end) {
+    // The residuals of a thread's columns, kTurns of them on their way: begin() asks for the first, of rows of x from x0 on, and each turn for the one that takes
+    // its place, below column `end`.
+    __device__ __forceinline__ void begin(int64_t x0, int c, int end) {
         if constexpr (GATED) return;
         if (!a.epi.residual || row >= a.n) return;
-        const One *r = static_cast<const One *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
+        ahead = static_cast<const One *>(a.epi.residual) + (x0 + c) * a.epi.residual_row + row;
+        left = end - c;
 #pragma unroll
-        for (int i = 0; i < kTurns; i++, r += kAtOnce * a.epi.residual_row)
-            if (c + i * kAtOnce < end) residual[GATED ? 0 : i] = load(r);
+        for (int i = 0; i < kTurns; i++) next(i);
+    }
+    __device__ __forceinline__ void next(int i) {
+        if (left > 0) residual[GATED ? 0 : i] = load(ahead);
+        ahead += kAtOnce * a.epi.residual_row;
+        left -= kAtOnce;
     }
     // The residuals of columns below `count` come into the L2 cache while the products go on.
     __device__ __forceinline__ void announce(int64_t x0, int count) const {
@@ -181,7 +189,7 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
             v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
         }
     }
-    template <int ACT> __device__ __forceinline__ void give_as(int64_t x0, int c, int end) const {
+    template <int ACT> __device__ __forceinline__ void give_as(int64_t x0, int c, int end) {
         const bool bf16 = a.type == ECASQ_BF16;
         float bias[4] = {0.f, 0.f, 0.f, 0.f};
         if (!GATED && a.epi.bias) {
@@ -210,6 +218,7 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
                 if (a.epi.residual) {
                     float r[4];
                     widen(residual[GATED ? 0 : i], bf16, r);
+                    next(i);
 #pragma unroll
                     for (int j = 0; j < 4; j++) v[j] += r[j];
                 }
@@ -227,8 +236,8 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
             }
         }
     }
-    // The columns c, c + kAtOnce, ... below end, kTurns of them; what fetch() was asked for is there.
-    __device__ __forceinline__ void give(int64_t x0, int c, int end) const {
+    // The columns c, c + kAtOnce, ... below end, kTurns of them.
+    __device__ __forceinline__ void give(int64_t x0, int c, int end) {
         if (row >= a.n) return;
         switch (a.epi.act) {
             case ECASQ_ACT_RELU: return give_as<ECASQ_ACT_RELU>(x0, c, end);
@@ -697,11 +706,12 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             }
             Finish<GATED, NH == 1, F32> finish(a, sums, r0, half, Shape::kBlocks);
             constexpr int kTurns = finish.kTurns, kAtOnce = finish.kAtOnce;
+            const int64_t first_x = (int64_t)(t % a.x_tiles) * kN + part * kOwn;
+            finish.begin(first_x, c0 + finish.turn(), (int)min((int64_t)(NH == 2 ? kOwn : c1), a.b - first_x));
 #pragma unroll 1
             for (int q = 0; q < kOwn / kOut; q++) {
-                const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + part * kOwn + q * kOut;
+                const int64_t x0 = first_x + q * kOut;
                 const int end = (int)min((int64_t)c1, a.b - x0);
-                finish.fetch(x0, c0 + finish.turn(), end);
                 four_warps();
 #pragma unroll
                 for (int c = 0; c < kOut; c += 2) {
@@ -719,10 +729,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                         for (int c = 0; c < kOut; c++) sums[128 * c + 32 * quarter + lane] = CUDART_NAN_F;
                 }
                 four_warps();
-                for (int c = c0 + finish.turn(); c < end; c += kTurns * kAtOnce) {
-                    if (c >= c0 + kTurns * kAtOnce) finish.fetch(x0, c, end);
-                    finish.give(x0, c, end);
-                }
+                for (int c = c0 + finish.turn(); c < end; c += kTurns * kAtOnce) finish.give(x0, c, end);
             }
             if (NH == 1 && a.split > 1) {
                 __syncwarp();
