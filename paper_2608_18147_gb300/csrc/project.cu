@@ -8,8 +8,7 @@ namespace ecasq {
 // tensor cores 62 (8192 x 8192: 16, 32 and 21).
 constexpr int64_t kFewRows = 8;
 
-// Few rows of x: the kernels of ecasq_matvec with what follows.
-static int launch_few(const ProjectArgs &p, cudaStream_t st) {
+int launch_project_few(const ProjectArgs &p, cudaStream_t st) {
     MatvecArgs a{};
     a.x = p.x;
     a.levels = p.levels;
@@ -50,7 +49,7 @@ static int project(const void *x, int64_t x_row, int32_t type, int64_t b, const 
         (b > 1 && (x_row < k || y_row < n || (epi.residual && epi.residual_row < n))))
         return ECASQ_EINVAL;
     const ProjectArgs a{x, levels, scales, codes, y, status, x_row, code_row, scale_row, y_row, n, k, b, m, group, type, scale_type, gated, lost_wait, epi};
-    return b > kFewRows ? launch_project_tc(a, ws, ws_bytes, st) : launch_few(a, st);
+    return b > kFewRows ? launch_project_tc(a, ws, ws_bytes, st) : launch_project_few(a, st);
 }
 
 }  // namespace ecasq

@@ -17,7 +17,9 @@ struct ProjectArgs {
     Epilogue epi;
 };
 
-// Tensor cores, any number of rows of x; the workspace it may need.
+// The matrix-vector kernels, which read the matrix again for each eight rows of x.
+int launch_project_few(const ProjectArgs &p, cudaStream_t st);
+// Tensor cores, or those where they are faster; the workspace it may need.
 int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st);
 size_t project_tc_room(int64_t b, int64_t k, int32_t type);
 

@@ -49,19 +49,10 @@ int make_tile_map(CUtensorMap *map, CUtensorMapDataType type, const void *at, in
 static int64_t laid_row(int64_t k) { return (k + 7) / 8 * 8; }
 size_t project_tc_room(int64_t b, int64_t k, int32_t type) { return align256((size_t)(b * laid_row(k)) * 2 * (type == ECASQ_F32 ? 3 : 1)); }
 
+constexpr int64_t kPanelBytes = 24 << 20;
+
 int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st) {
     const bool f32 = p.type == ECASQ_F32;
-    const void *x = p.x;
-    int64_t x_row = p.x_row;
-    if (f32 || !aligned16(p.x) || (p.b > 1 && p.x_row % 8)) {
-        if (!ws || ws_bytes < project_tc_room(p.b, p.k, p.type) || !aligned16(ws)) return ECASQ_EWORKSPACE;
-        const dim3 grid((unsigned)cdiv(p.k, 256), (unsigned)std::min<int64_t>(p.b, 4096));
-        const int rc = f32 ? launch_early(k_lay_out<true>, grid, 256, 0, st, p.x, p.x_row, p.b, p.k, static_cast<uint16_t *>(ws), laid_row(p.k))
-                           : launch_early(k_lay_out<false>, grid, 256, 0, st, p.x, p.x_row, p.b, p.k, static_cast<uint16_t *>(ws), laid_row(p.k));
-        if (rc) return rc;
-        x = ws;
-        x_row = laid_row(p.k);
-    }
     const int64_t rows = p.gated ? 2 * p.n : p.n;
     TcArgs a{};
     a.levels = p.levels;
@@ -114,11 +105,30 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
         }
         if (c.width >= p.b) break;
     }
+    // The matrix-vector kernels, a pass for each eight rows, are the faster ones for small matrices (300 x 8192 by 16 rows: 6.3 us, and 11.8 here; 1024 x 1024
+    // 6.8 and 8.3; 4096 x 4096 13.3 and 11.5).  Their blocks take 3.2 us each and their codes at 16 bytes a nanosecond (fp32 6.2 us, 2.4 bytes), a round
+    // of 152 after another; these stand at 5 us for a launch, 2 for rows of x that are laid out first, and what is counted above.
+    const int64_t few_blocks = std::min<int64_t>(cdiv(p.n, 8), 152), few = cdiv(few_blocks * cdiv(p.b, 8), 152) * ((f32 ? 620 : 320) + rows * p.k / 2 / few_blocks / (f32 ? 24 : 158));
+    if (few < best + (f32 ? 700 : 500)) return launch_project_few(p, st);
     const bool pair = width == 256;
     a.x_tiles = (int32_t)cdiv(p.b, width);
     const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * a.x_tiles;
     if (tiles > INT32_MAX) return ECASQ_EINVAL;
     a.tiles = (int32_t)tiles;
+    a.w_tiles = (int32_t)(tiles / a.x_tiles);
+    a.panel = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.x_tiles, kPanelBytes / (width * p.k * 2 * (f32 ? 3 : 1))));
+    a.panel = (int32_t)cdiv(a.x_tiles, cdiv(a.x_tiles, a.panel));  // (panels alike)
+    const void *x = p.x;
+    int64_t x_row = p.x_row;
+    if (f32 || !aligned16(p.x) || (p.b > 1 && p.x_row % 8)) {
+        if (!ws || ws_bytes < project_tc_room(p.b, p.k, p.type) || !aligned16(ws)) return ECASQ_EWORKSPACE;
+        const dim3 grid((unsigned)cdiv(p.k, 256), (unsigned)std::min<int64_t>(p.b, 4096));
+        const int rc = f32 ? launch_early(k_lay_out<true>, grid, 256, 0, st, p.x, p.x_row, p.b, p.k, static_cast<uint16_t *>(ws), laid_row(p.k))
+                           : launch_early(k_lay_out<false>, grid, 256, 0, st, p.x, p.x_row, p.b, p.k, static_cast<uint16_t *>(ws), laid_row(p.k));
+        if (rc) return rc;
+        x = ws;
+        x_row = laid_row(p.k);
+    }
     CUtensorMap xm, cm;
     const int x_rows = std::min(width, 128) / (pair ? 2 : 1);
     int rc = make_tile_map(&xm, p.type == ECASQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, p.k, f32 ? 3 * p.b : p.b,

@@ -23,7 +23,8 @@ struct TcArgs {
     int32_t blocks;         // blocks of 128 columns
     int32_t group_blocks;   // blocks of a scale group, where it holds whole ones
     int32_t split;          // pairs of a cluster that share the columns
-    int32_t x_tiles, tiles; // tiles of rows of x; of the product
+    int32_t x_tiles, w_tiles, tiles;  // tiles of rows of x; of the matrix's rows; of the product
+    int32_t panel;          // tiles of rows of x that the tiles of the matrix's rows go by before the next ones
     uint32_t div_mul, div_shift;  // words of 32 columns to scale groups (FastDiv of group / 32)
     bool wide;              // y and the residual in pieces of four values
     uint32_t none;          // 0, which the compiler does not know
@@ -360,6 +361,11 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
     uint32_t tmem;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at) : "memory");
 
+    // Tile t: the rows of x and of the matrix, by panels of rows of x that stay in the L2 cache while all of the matrix goes by.
+    auto tile_of = [&](int t) {
+        const int whole = a.panel * a.w_tiles, first = t / whole * a.panel, wide = min(a.panel, a.x_tiles - first), rest = t % whole;
+        return make_int2(first + rest % wide, rest / wide);
+    };
     // The first row of the matrix that this block has of weight tile t: 128 rows (gated: 64 of each half) from it on.
     auto rows_at = [&](int t) { return (int64_t)t * Shape::kRows + half * (GATED ? 64 : 128); };
     const int per_tile = (kb1 - kb0) * terms;  // products' blocks of a tile
@@ -371,7 +377,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 uint32_t i = 0;
                 bool ok = true;
                 for (int t = cluster; ok && t < a.tiles; t += clusters) {
-                    const int64_t x0 = (int64_t)(t % a.x_tiles) * kN + half * Shape::kXRows;
+                    const int64_t x0 = (int64_t)tile_of(t).x * kN + half * Shape::kXRows;
                     for (int v = 0; ok && v < per_tile; v++, i++) {
                         const uint32_t s = i % kXStages, to = base + s * Shape::kXStage;
                         if (!(ok = wait(x_empty + 8 * s, (i / kXStages & 1) ^ 1))) break;
@@ -392,7 +398,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 uint32_t i = 0;
                 bool ok = true;
                 for (int t = cluster; ok && t < a.tiles; t += clusters) {
-                    const int64_t r0 = rows_at(t / a.x_tiles);
+                    const int64_t r0 = rows_at(tile_of(t).y);
                     for (int v = 0; ok && v < per_tile; v++, i++) {
                         const uint32_t s = i % kCodeStages, to = base + kXStages * Shape::kXStage + s * kCodeStage;
                         if (!(ok = wait(c_empty + 8 * s, (i / kCodeStages & 1) ^ 1))) break;
@@ -438,7 +444,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 const char *from[4];
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    const int64_t row = rows_at(t / a.x_tiles) + (GATED ? 16 * i + (lane & 15) : 32 * i + lane);
+                    const int64_t row = rows_at(tile_of(t).y) + (GATED ? 16 * i + (lane & 15) : 32 * i + lane);
                     from[i] = static_cast<const char *>(a.scales) + (min(row, a.n - 1) + (GATED && (lane & 16) ? a.second : 0)) * a.scale_row * scale_size;
                 }
                 Span ask{4 * kb0 / group_words, 4 * kb0, group_words - 4 * kb0 % group_words, 0}, give = ask;
@@ -643,9 +649,9 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0, span = 0;
         bool ok = !a.lost;
         for (int t = cluster; t < a.tiles; t += clusters, turn++) {
-            const int64_t r0 = rows_at(t / a.x_tiles);
+            const int64_t r0 = rows_at(tile_of(t).y);
             float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * Shape::kOut * 128;
-            Finish<GATED, NH == 1, F32>(a, sums, r0, half, Shape::kBlocks).announce((int64_t)(t % a.x_tiles) * kN + part * kOwn, kOwn);
+            Finish<GATED, NH == 1, F32>(a, sums, r0, half, Shape::kBlocks).announce((int64_t)tile_of(t).x * kN + part * kOwn, kOwn);
             uint64_t acc[kOwn / 2];  // pairs of columns
 #pragma unroll
             for (int c = 0; c < kOwn / 2; c++) acc[c] = 0;
@@ -706,7 +712,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             }
             Finish<GATED, NH == 1, F32> finish(a, sums, r0, half, Shape::kBlocks);
             constexpr int kTurns = finish.kTurns, kAtOnce = finish.kAtOnce;
-            const int64_t first_x = (int64_t)(t % a.x_tiles) * kN + part * kOwn;
+            const int64_t first_x = (int64_t)tile_of(t).x * kN + part * kOwn;
             finish.begin(first_x, c0 + finish.turn(), (int)min((int64_t)(NH == 2 ? kOwn : c1), a.b - first_x));
 #pragma unroll 1
             for (int q = 0; q < kOwn / kOut; q++) {
