@@ -441,17 +441,22 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
 /* A layer's products around one coded matrix, with what follows them:
  *   ecasq_project  y[i, r] = act(p[i, r] + bias[r]) + residual[i, r]           for W [n, k]
  *   ecasq_gated    y[i, r] = act(p[i, r]) p[i, n + r]                          for W [2n, k]: the gate's rows, then the other's
- * with p = x W^T as in ecasq_matvec.  Sums, bias, activation and residual are fp32; y is rounded once, to x's type.
- *   act     none; relu; silu v / (1 + e^-v); gelu v Phi(v), Phi the normal distribution's; gelu_tanh
+ * with p = x W^T as in ecasq_matvec.  Products with scales, sums, bias, activation and residual are fp32; y is rounded once, to x's
+ * type.  (More than eight rows of F32 are multiplied as three bf16 terms of 8 bits each: products are within 2^-21 of themselves, for values from about
+ * 2^-100 on, and a row with an infinity may be NaN.)
+ *   act     none; relu; silu v / (1 + e^-v); gelu v Phi(v), Phi the normal distribution's, to 2^-23; gelu_tanh
  *           v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2
  *   bias    device [n] of `type`, or NULL
  *   residual  device [b rows of residual_row elements] of `type`, or NULL; y may be the residual itself (same
  *           address and rows), and overlaps nothing else that is read
  *   the others as for ecasq_matvec (n < 2^30 for ecasq_gated)
  * Workspace: ecasq_workspace_size_project with the same sizes, n the matrix's rows (0 bytes may be returned: ws may then be
- * NULL); it needs no preparation, and one made for the largest b serves all smaller ones.
- *   status  ECASQ_BAD_WAIT
- * ECASQ_EINVAL as for ecasq_matvec, and for a bad activation. */
+ * NULL); it needs no preparation, is 16-byte aligned, and one made for the largest b serves all smaller ones.  It holds rows of x: a 16-bit x whose rows
+ * all begin at multiples of 16 bytes needs none.
+ *   status  ECASQ_BAD_WAIT: here what a block had not stored when the wait ran out is NaN
+ * Which kernel takes a call goes by its sizes and types alone: equal calls give equal bits.
+ * ECASQ_EINVAL as for ecasq_matvec, and for a bad activation; ECASQ_EWORKSPACE where a workspace is needed and is too small.
+ * ECASQ_TEST_LOST_WAIT as for ecasq_matvec. */
 #define ECASQ_ACT_NONE 0
 #define ECASQ_ACT_RELU 1
 #define ECASQ_ACT_SILU 2

@@ -214,17 +214,33 @@ static int64_t scale_row(const Product *p) { return p->rows > 1 ? p->scales.step
 static int rows_like(const Tensor *t, const Tensor *x, int64_t b, int64_t n, int type) {
     return t->type == type && t->nd == x->nd && t->device == x->device && t->n[t->nd - 1] == n && (t->nd == 1 || t->n[0] == b) && (n < 2 || t->step[t->nd - 1] == 1);
 }
+/* What new_tensor made: all but its address is known. */
+static int look_at_made(PyObject *o, int nd, const int64_t *n, int type, const Tensor *like, Tensor *t) {
+    PyObject *at = PyObject_CallMethodNoArgs(o, s_data_ptr);
+    if (!at) return 0;
+    t->o = o;
+    t->type = type;
+    t->nd = nd;
+    t->device = like->device;
+    t->at = PyLong_AsVoidPtr(at);
+    t->count = 1;
+    for (int i = nd - 1; i >= 0; i--) {
+        t->n[i] = n[i];
+        t->step[i] = t->count;
+        t->count *= n[i];
+    }
+    Py_DECREF(at);
+    return !PyErr_Occurred();
+}
 /* `given`, or such a tensor made where that is None; NULL with an exception, or None, where it is not one. */
 static PyObject *output_of(PyObject *given, const Tensor *x, int64_t b, int64_t n, int type, Tensor *y) {
-    PyObject *made;
     if (given == Py_None) {
         const int64_t shape[2] = {x->nd == 2 ? b : n, n};
-        if (!(made = new_tensor(x->nd, shape, type, x))) return NULL;
-    } else {
-        made = Py_NewRef(given);
+        PyObject *made = new_tensor(x->nd, shape, type, x);
+        if (made && !look_at_made(made, x->nd, shape, type, x, y)) Py_CLEAR(made);
+        return made;
     }
-    if (look(made, y) && rows_like(y, x, b, n, type)) return made;
-    Py_DECREF(made);
+    if (look(given, y) && rows_like(y, x, b, n, type)) return Py_NewRef(given);
     NO;
 }
 static int64_t row_step(const Tensor *t, int64_t n) { return t->nd == 2 ? t->step[0] : n; }
@@ -277,7 +293,9 @@ static PyObject *layer_product(PyObject *const *v, int gated) {
     if (w[1] != Py_None && (!look(w[1], &ws) || ws.type != U8 || ws.device != p.x.device || !contiguous(&ws))) NO;
     if (!(made = output_of(w[0], &p.x, p.b, n, p.x.type, &y)) || made == Py_None) return made;
     if (w[1] == Py_None) {
-        const int64_t room = (int64_t)call_room(p.b, p.rows, p.k, p.x.type);
+        /* (16-bit rows of x on 16-byte boundaries need none) */
+        const int plain = p.x.type != ECASQ_F32 && ((uintptr_t)p.x.at & 15) == 0 && (p.b == 1 || x_row(&p) % 8 == 0);
+        const int64_t room = plain ? 0 : (int64_t)call_room(p.b, p.rows, p.k, p.x.type);
         if (room && (!(space = new_tensor(1, &room, U8, &p.x)) || !look(space, &ws))) {
             Py_XDECREF(space);
             Py_DECREF(made);

@@ -741,7 +741,7 @@ def ecasq_project(x, codes, levels, scales, group, bias=None, activation=None, r
 
     x, codes, levels, scales, group, status as for ecasq_matvec; bias [n] and residual [b, n] (or [n]) of x's type or None;
     activation None, "relu", "silu", "gelu" or "gelu_tanh".  ws: workspace_project(b, n, k, x.dtype), or None (one is made
-    where one is needed).  Returns y [b, n] or [n] of x's type (`out` if given, which may be the residual itself).
+    where one is needed: for float32, and for rows of x off 16-byte boundaries).  Returns y [b, n] or [n] of x's type (`out` if given, which may be the residual itself).
     No gradients: a tensor that requires one is refused while they are recorded."""
     act = _activation("ecasq_project", activation)
     y = (_codes or _ready()).project(x, codes, levels, scales, group, bias, act, residual, out, ws, status)
