@@ -73,3 +73,91 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for x, m, out, ws, want in jobs:
         assert torch.equal(out, want)
+
+
+def test_captured_before_any_other_call():
+    """A process whose first calls are captured into a graph: what the library asks the card once is asked then."""
+    import os
+    import subprocess
+    import sys
+    src = """
+import torch
+import paper_2608_18147_gb300 as E
+gen = torch.Generator(device="cuda").manual_seed(1)
+idx = torch.randint(0, 16, (512, 640), generator=gen, device="cuda", dtype=torch.uint8)
+codes, levels, scales = E.ecasq_pack(idx), torch.linspace(-1, 1, 16, device="cuda").half(), torch.rand(512, 5, generator=gen, device="cuda")
+few, many, most = (torch.randn(b, 640, generator=gen, device="cuda").half() for b in (3, 100, 700))
+w = torch.rand(640, device="cuda")
+side = torch.cuda.Stream()
+side.wait_stream(torch.cuda.current_stream())
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+    got = [f(x, codes, levels, scales, 128) for x in (few, many, most) for f in (E.ecasq_project, E.ecasq_gated)] + [E.ecasq_norm(many, w)]
+graph.replay()
+torch.cuda.synchronize()
+want = [f(x, codes, levels, scales, 128) for x in (few, many, most) for f in (E.ecasq_project, E.ecasq_gated)] + [E.ecasq_norm(many, w)]
+assert all(torch.equal(a, b) and a.float().abs().sum() > 0 for a, b in zip(got, want))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", src], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+
+
+@pytest.mark.parametrize("b", [1, 9, 40, 130, 600])
+def test_levels_scales_and_rows_of_a_larger_tensor(b):
+    """Levels that begin off 4-byte boundaries, 16-bit scales in a wider tensor at odd places, codes with longer rows."""
+    import paper_2608_18147_gb300 as E
+    gen = torch.Generator(device="cuda").manual_seed(b)
+    n, k, group = 270, 900, 32
+    idx = torch.randint(0, 16, (n, k), generator=gen, device="cuda", dtype=torch.uint8)
+    packed = E.ecasq_pack(idx)
+    codes = torch.full((n, packed.shape[1] + 48), 255, dtype=torch.uint8, device="cuda")
+    codes[:, :packed.shape[1]] = packed
+    levels = torch.cat([torch.zeros(1, device="cuda"), torch.linspace(-1, 1, 16, device="cuda")]).bfloat16()[1:]
+    for lead in (1, 2, 3):
+        scales = torch.full((n, 29 + lead + 2), float("nan"), dtype=torch.bfloat16, device="cuda")[:, lead:lead + 29]
+        scales.copy_(torch.rand(n, 29, generator=gen, device="cuda") / 30)
+        x = torch.randn(b, k, generator=gen, device="cuda").bfloat16()
+        want = E.ecasq_project(x, packed, levels.clone(), scales.contiguous(), group)
+        assert torch.equal(E.ecasq_project(x, codes[:, :packed.shape[1]], levels, scales, group), want) and want.isfinite().all()
+        half = E.ecasq_gated(x, packed, levels.clone(), scales.contiguous(), group)
+        assert torch.equal(E.ecasq_gated(x, codes[:, :packed.shape[1]], levels, scales, group), half)
+
+
+@pytest.mark.parametrize("b", [2, 400])
+@pytest.mark.parametrize("dtype,weight,k", [(torch.bfloat16, torch.float32, k) for k in (12176, 12192, 12200, 12224, 12248, 12256, 12264)] +
+                         [(torch.float32, torch.float32, k) for k in (12192, 12208, 12240, 12268, 12272, 12276)] +
+                         [(torch.float16, torch.float16, k) for k in (24448, 24512, 24544, 24552)])
+def test_norm_where_weights_nearly_fill_the_ordinary_shared_memory(b, dtype, weight, k):
+    """Weights of 48 KB less a few words: what the kernel has beside them is counted too.  Roundings: fp32 sums of k squares in any order k 2^-24
+    at most (their root half of that), four more of a product, the output's half step."""
+    import paper_2608_18147_gb300 as E
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    x = torch.randn(b, k, generator=gen, device="cuda").to(dtype)
+    w = torch.rand(k, generator=gen, device="cuda").to(weight)
+    got = E.ecasq_norm(x, w, 1e-6)
+    want = x.double() / (x.double().square().mean(1, keepdim=True) + 1e-6).sqrt() * w.double()
+    assert ((got.double() - want).abs() <= want.abs() * (torch.finfo(dtype).eps / 2 + (k / 2 + 4) * 2.0**-24) + 1e-7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_workspaces_that_do_not_do(dtype):
+    """Too small, or not on a 16-byte boundary: refused where one is needed; one of the right size gives what a call without one does."""
+    import paper_2608_18147_gb300 as E
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    b, n, k = 600, 2048, 1001  # rows of 1001 values do not begin on 16-byte boundaries
+    codes = E.ecasq_pack(torch.randint(0, 16, (n, k), generator=gen, device="cuda", dtype=torch.uint8))
+    levels, scales = torch.linspace(-1, 1, 16, device="cuda").to(dtype), torch.rand(n, 8, generator=gen, device="cuda")
+    x = torch.randn(b, k, generator=gen, device="cuda").to(dtype)
+    room = E.workspace_project(b, n, k, dtype)
+    room = room.numel() * room.element_size()
+    want = E.ecasq_project(x, codes, levels, scales, 128)
+    whole = torch.empty(room + 16, dtype=torch.uint8, device="cuda")
+    for ws in (whole[:room - 256], whole[:0], whole[1:room + 1], whole[8:room + 8], whole[:room].cpu()):
+        with pytest.raises((ValueError, RuntimeError, TypeError)):
+            E.ecasq_project(x, codes, levels, scales, 128, ws=ws)
+        with pytest.raises((ValueError, RuntimeError, TypeError)):
+            E.ecasq_gated(x, codes, levels, scales, 128, ws=ws)
+    whole.fill_(255)
+    assert torch.equal(E.ecasq_project(x, codes, levels, scales, 128, ws=whole[:room]), want)
+    assert torch.equal(E.ecasq_project(x, codes, levels, scales, 128, ws=whole[16:]), want)
