@@ -31,27 +31,4 @@ __device__ __forceinline__ float activate(float v, int act) {
     }
 }
 
-// N values at once, with one choice of the activation for all of them.
-template <int N> __device__ __forceinline__ void activate_all(float (&v)[N], int act) {
-    switch (act) {
-        case ECASQ_ACT_RELU:
-#pragma unroll
-            for (int j = 0; j < N; j++) v[j] = activate(v[j], ECASQ_ACT_RELU);
-            break;
-        case ECASQ_ACT_SILU:
-#pragma unroll
-            for (int j = 0; j < N; j++) v[j] = activate(v[j], ECASQ_ACT_SILU);
-            break;
-        case ECASQ_ACT_GELU:
-#pragma unroll
-            for (int j = 0; j < N; j++) v[j] = activate(v[j], ECASQ_ACT_GELU);
-            break;
-        case ECASQ_ACT_GELU_TANH:
-#pragma unroll
-            for (int j = 0; j < N; j++) v[j] = activate(v[j], ECASQ_ACT_GELU_TANH);
-            break;
-        default: break;
-    }
-}
-
 }  // namespace ecasq

@@ -73,9 +73,6 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     a.group_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.group / 128, a.blocks));
     a.lost = p.lost;
     a.epi = p.epi;
-    const FastDiv div(p.group / 32);
-    a.div_mul = div.mul;
-    a.div_shift = div.shift;
     const int64_t piece = 4 * type_size(p.type);
     const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
     a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
@@ -113,7 +110,7 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     const bool pair = width == 256;
     a.x_tiles = (int32_t)cdiv(p.b, width);
     const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * a.x_tiles;
-    if (tiles > INT32_MAX) return ECASQ_EINVAL;
+    if (tiles > INT32_MAX - 1024) return ECASQ_EINVAL;  // (a block's last step goes beyond them by at most a card's clusters)
     a.tiles = (int32_t)tiles;
     a.w_tiles = (int32_t)(tiles / a.x_tiles);
     a.panel = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.x_tiles, kPanelBytes / (width * p.k * 2 * (f32 ? 3 : 1))));

@@ -3,7 +3,16 @@
 // The matrix is the left operand: its codes become levels, which go to tensor memory as they are (16 bits, exact), 128 rows a
 // block and 256 a pair of blocks; the rows of x are the right operand, in shared memory.  The sums of the columns of one scale group
 // come out of tensor memory, are multiplied by their row's scale, which is one number a thread there, and are added up in registers.  So
-// products and scales are as exact as in ecasq_matvec: nothing is rounded before the end.
+// products and scales are as exact as in ecasq_matvec: nothing is rounded before the end.  (Levels times scales, rounded to 16 bits before the
+// product, would need no sums in between, but are off by as much as the output's own rounding.)
+//
+// What bounds it (8192 x 8192 of bf16, groups of 128, by 4096 rows: 385 to 395 us, 1.4 PFLOP/s, three quarters of a library's 16-bit product on the same
+// card): the tensor core is busy 59 % of the time.  At its rate a block of 128 columns of a pair's 256 x 256 tile is 1024 clocks; an adding warp took 740 for
+// its share of a block's sums (eight loads of 16 columns from tensor memory, 92 clocks each, before two of them were under way at once), so smaller groups,
+// with more sums, cost more: 551 us in groups of 64, 930 in groups of 32, 365 in groups of 256.  With the results left unwritten it took 368 us: about
+// 3 us for each of a pair's seven tiles.  A residual adds about 8 us a tile (440 us).  With few rows of x it is the ways between the warps: where each block
+// has a tile of its own, 128 columns take 0.38 us by 32 rows and 0.60 by 128 rows, on top of 6 us for the shortest product.  9700 x 8192 by 64 rows takes 25 us
+// in single blocks and took 42 in pairs; where a pair has as many tiles as a block there is little to gain (8192 x 8192 by 16 rows 21 us both ways, by 128 rows 28 and 29).
 #pragma once
 
 #include <algorithm>
@@ -22,10 +31,9 @@ struct TcArgs {
     int32_t m, group, type, scale_type;
     int32_t blocks;         // blocks of 128 columns
     int32_t group_blocks;   // blocks of a scale group, where it holds whole ones
-    int32_t split;          // pairs of a cluster that share the columns
+    int32_t split;          // blocks, or pairs of them, of a cluster that share the columns
     int32_t x_tiles, w_tiles, tiles;  // tiles of rows of x; of the matrix's rows; of the product
     int32_t panel;          // tiles of rows of x that the tiles of the matrix's rows go by before the next ones
-    uint32_t div_mul, div_shift;  // words of 32 columns to scale groups (FastDiv of group / 32)
     bool wide;              // y and the residual in pieces of four values
     uint32_t none;          // 0, which the compiler does not know
     uint32_t lost;          // test hook: 1 where blocks begin as if a wait had run out
@@ -257,9 +265,11 @@ __device__ __forceinline__ void look_up(uint32_t w, uint32_t lane, uint32_t *to)
     for (int j = 0; j < 4; j++) to[j] = *static_cast<const uint32_t *>(__cvta_shared_to_generic(permute(w, 0, 0x4440 | j) * 128 + lane));
 }
 
-// A cluster is `split` pairs of blocks.  Of a block's warps, four bring in tiles, issue products and pass arrivals on; kDecodeWarps turn codes
-// into levels; eight take sums out.  Barriers pass stages between them; those that the products' issuer waits for are in the first block of a
-// pair, which issues for both.
+// A cluster is `split` blocks, or pairs of them.  Of a block's warps, the first brings in rows of x, the second issues products, the third brings in codes, the
+// fourth scales; kDecodeWarps turn codes into levels; eight take sums out, each its share of the columns.  Barriers pass stages between them; those that
+// the products' issuer waits for are in the first block of a pair, which issues for both.  The issuer's warp runs together, so that addresses stay in
+// uniform registers: with them in one lane's registers, 8192 x 8192 by 4096 rows took 1404 us where it then took 560 (with that, results also began to leave in
+// 16-byte pieces).
 template <int ND, int NH, bool GATED, int SPANS, bool F32>
 __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_project_tc(const __grid_constant__ CUtensorMap xm, const __grid_constant__ CUtensorMap cm,
                                                                             const __grid_constant__ TcArgs a) {
@@ -573,7 +583,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         const uint32_t there = kPair ? of_rank(a_full, leader) : a_full, swizzle = (uint32_t)(from >> 1 & 3);
         constexpr int kTeams = Shape::kDecodeWarps / 4;  // of four warps, which take turns at the blocks
         const int team = (wid - 4) / 4;
-        const int total = a.tiles > cluster ? (a.tiles - cluster + clusters - 1) / clusters * per_tile : 0;  // blocks of all tiles
+        const int64_t total = a.tiles > cluster ? (int64_t)((a.tiles - cluster + clusters - 1) / clusters) * per_tile : 0;  // blocks of all tiles
         const char *codes = smem + kXStages * Shape::kXStage + from * 64;
         uint32_t w[16], cs = team, c_parity = 0, xs = team, x_parity = 0, as = 2 * team, a_parity = 1, term = team % terms;
         auto step = [](uint32_t &at, uint32_t by, uint32_t stages, uint32_t &parity) {
@@ -625,7 +635,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         };
         // While a half's levels are on their way to tensor memory, the next half's are looked up.
         bool ok = !a.lost && (team >= total || fetch());
-        for (int i = team; ok && i < total; i += kTeams) {
+        for (int64_t i = team; ok && i < total; i += kTeams) {
             uint32_t pairs[32];
             decode_half(0, pairs);
             if (!(ok = store(0, pairs))) break;
