@@ -132,9 +132,9 @@ template <typename W, int N, bool ALIGNED> __device__ __forceinline__ void weigh
 // changes neither the mean nor a maximum, and what is stored of such a piece goes value by value.
 // Groups whose columns threads that lie together share: one maximum by shuffles; the whole row: one more reduction; others: words of shared memory,
 // of the bits of values that are not negative, raised by atomics (whose order does not matter).
-// What bounds it: memory where rows are aligned (8192 x 8192 of bf16 with a residual 91 us, 5.9 TB/s; to 8 bits by groups of 128 95 us, 4.9 TB/s, where a third
-// of the issue slots go to maxima and conversions); the shifting of weights where they are not (3001 x 5003 of fp32 27 us, 4.5 TB/s); one
-// row of 4096 takes 2.5 us, two memory latencies and a launch.  With weights in registers instead of shared memory, and pieces that every
+// What bounds it: memory where rows are aligned (8192 x 8192 of bf16 with a residual 91 us, 5.9 TB/s; to 8 bits by groups of 128 95 us, 4.9 TB/s, where the
+// normed values are found, their maxima exchanged and the codes made between a row's loads and its stores, with issue slots half used: latency); the shifting of weights where they are not (3001 x 5003 of fp32 27 us, 4.5 TB/s); one
+// row of 4096 takes 2.3 us, two memory latencies and a launch.  With weights in registers instead of shared memory, and pieces that every
 // thread looked at value by value, the aligned cases took 141 and 185 us: two blocks an SM instead of three, and code that did not fit its cache.
 template <typename T, typename W, int P, int NT, bool ALIGNED>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 3 : NT == 512 && P <= 3 ? 2 : 1) k_norm(const __grid_constant__ NormArgs a) {

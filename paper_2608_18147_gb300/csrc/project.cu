@@ -4,8 +4,8 @@
 
 namespace ecasq {
 
-// Rows of x up to which the matrix-vector kernels take a call, one pass of theirs: 28672 x 8192 by eight rows takes them 36 us, by sixteen, in two passes, 71, and the
-// tensor cores 62 (8192 x 8192: 16, 32 and 21).
+// Rows of x up to which the matrix-vector kernels take a call, one pass of theirs: 28672 x 8192 by eight rows takes them 36 us, by sixteen, in two passes, twice that,
+// and the tensor cores 53 (8192 x 8192: 16, twice that and 21).
 constexpr int64_t kFewRows = 8;
 
 int launch_project_few(const ProjectArgs &p, cudaStream_t st) {
