@@ -485,9 +485,9 @@ int ecasq_gated(const void *x, int64_t x_row, int32_t type, int64_t b, const uin
  *   y       device [b rows of y_row elements]
  *   sum     device [b rows of sum_row elements] or NULL: where s goes; needs a residual
  *   scales  device fp32 [b rows of scale_row], ceil(k / group) a row; read for group > 0 only
- * y of `type` and sum may each be x or the residual itself (same address and rows); nothing else overlaps.
+ * y of `type` and sum may each be x or the residual itself (same address and rows), but not both the same; nothing else overlaps.
  * ECASQ_EINVAL for b or k outside [0, 2^31) and [1, 2^31), rows shorter than their contents, eps negative or NaN, a bad type or
- * group, a sum without a residual. */
+ * group, a sum without a residual or at the address of a y of `type`. */
 int ecasq_norm(const void *x, int64_t x_row, int32_t type, int64_t b, int64_t k, const void *residual,
                int64_t residual_row, const void *weight, int32_t weight_type, float eps, int64_t group, void *y,
                int64_t y_row, void *sum, int64_t sum_row, float *scales, int64_t scale_row, ecasq_stream_t stream);

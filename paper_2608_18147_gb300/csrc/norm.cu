@@ -457,7 +457,7 @@ extern "C" int ecasq_norm(const void *x, int64_t x_row, int32_t type, int64_t b,
         return ECASQ_EINVAL;
     if (b == 0) return ECASQ_OK;
     const int64_t groups = group ? cdiv(k, group) : 0;
-    if (!x || !weight || !y || (sum && !residual) || (group && (!scales || (b > 1 && scale_row < groups))) ||
+    if (!x || !weight || !y || (sum && (!residual || (!group && sum == y))) || (group && (!scales || (b > 1 && scale_row < groups))) ||
         (b > 1 && (x_row < k || y_row < k || (residual && residual_row < k) || (sum && sum_row < k))))
         return ECASQ_EINVAL;
     NormArgs a{x, residual, weight, y, sum, scales, x_row, residual_row, y_row, sum_row, scale_row, b, k, group, groups, eps, 0};

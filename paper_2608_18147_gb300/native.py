@@ -796,7 +796,7 @@ def ecasq_norm(x, weight, eps=1e-6, residual=None, group=None, out=None, out_sum
     weight [k] of x's type or float32.  With `group` (a multiple of 16, or at least k: one scale a row) y is coded to 8 bits:
     float8_e4m3fn values y / scale, scale = max |y| / 448 of each group of columns.  Returns y, (y, scales), (y, s) or
     (y, scales, s); out, out_scales and out_sum are taken for them where given.  out_sum, and out without a group, may be x or
-    the residual itself.  No gradients: a tensor that requires one is refused while they are recorded."""
+    the residual itself, but not both the same.  No gradients: a tensor that requires one is refused while they are recorded."""
     y = (_codes or _ready()).norm(x, weight, eps, residual, group, out, out_sum, out_scales)
     if y is None:
         _norm_refused(_torch(), x, weight, eps, residual, group, out, out_sum, out_scales)

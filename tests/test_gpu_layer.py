@@ -161,3 +161,97 @@ def test_workspaces_that_do_not_do(dtype):
     whole.fill_(255)
     assert torch.equal(E.ecasq_project(x, codes, levels, scales, 128, ws=whole[:room]), want)
     assert torch.equal(E.ecasq_project(x, codes, levels, scales, 128, ws=whole[16:]), want)
+
+
+def right_or_refused(call, want):
+    """The same bits as `want`, or an error of the framework's own."""
+    import paper_2608_18147_gb300 as E
+    try:
+        got = call()
+    except E.EcasqError:
+        return False
+    assert torch.equal(got, want)
+    return True
+
+
+@pytest.mark.parametrize("b", [3, 40, 600])
+def test_strided_and_expanded_arguments(b):
+    """Every second entry of a vector, columns for rows, one row for all: never read as if they lay side by side."""
+    import paper_2608_18147_gb300 as E
+    gen = torch.Generator(device="cuda").manual_seed(b)
+    n, k = 256, 384
+    codes = E.ecasq_pack(torch.randint(0, 16, (n, k), generator=gen, device="cuda", dtype=torch.uint8))
+    levels, scales = torch.linspace(-1, 1, 16, device="cuda").half(), torch.rand(n, 3, generator=gen, device="cuda")
+    x, bias, residual = (torch.randn(*s, generator=gen, device="cuda").half() for s in ((b, k), (n,), (b, n)))
+    second = lambda v: v.repeat_interleave(2)[::2]  # noqa: E731
+    project = lambda *a, **o: E.ecasq_project(*a, 128, **o)  # noqa: E731
+    want = project(x, codes, levels, scales, bias=bias, residual=residual)
+    right_or_refused(lambda: project(x, codes, levels, scales, bias=second(bias), residual=residual), want)
+    right_or_refused(lambda: project(x, codes, second(levels), scales, bias=bias, residual=residual), want)
+    right_or_refused(lambda: project(x, codes, levels, scales.T.contiguous().T, bias=bias, residual=residual), want)
+    right_or_refused(lambda: project(x.T.contiguous().T, codes, levels, scales, bias=bias, residual=residual), want)
+    right_or_refused(lambda: project(x, codes, levels, scales, bias=bias, residual=residual.T.contiguous().T), want)
+    same = x[:1].expand(b, k)
+    right_or_refused(lambda: project(same, codes, levels, scales), project(same.contiguous(), codes, levels, scales))
+    right_or_refused(lambda: project(x, codes, levels, scales, residual=residual[:1].expand(b, n)),
+                     project(x, codes, levels, scales, residual=residual[:1].expand(b, n).contiguous()))
+    right_or_refused(lambda: project(x, codes, levels, scales[:1].expand(n, 3)), project(x, codes, levels, scales[:1].expand(n, 3).contiguous()))
+    right_or_refused(lambda: project(x, codes, levels, scales, bias=bias[:1].expand(n)), project(x, codes, levels, scales, bias=bias[:1].expand(n).contiguous()))
+    with pytest.raises(E.EcasqError):
+        project(x, codes, levels, scales, out=torch.empty(1, n, dtype=x.dtype, device="cuda").expand(b, n))
+    w = torch.rand(k, generator=gen, device="cuda").half()
+    want = E.ecasq_norm(x, w)
+    right_or_refused(lambda: E.ecasq_norm(x, second(w)), want)
+    right_or_refused(lambda: E.ecasq_norm(x.T.contiguous().T, w), want)
+    right_or_refused(lambda: E.ecasq_norm(same, w), E.ecasq_norm(same.contiguous(), w))
+    right_or_refused(lambda: E.ecasq_norm(x, w, residual=same)[0], E.ecasq_norm(x, w, residual=same.contiguous())[0])
+    right_or_refused(lambda: E.ecasq_norm(x, w[:1].expand(k)), E.ecasq_norm(x, w[:1].expand(k).contiguous()))
+    with pytest.raises(E.EcasqError):
+        E.ecasq_norm(x, w, out=torch.empty(1, k, dtype=x.dtype, device="cuda").expand(b, k))
+    with pytest.raises(E.EcasqError):
+        E.ecasq_norm(x, w, group=128, out_scales=torch.empty(1, 3, device="cuda").expand(b, 3))
+
+
+def test_threads_that_call_at_once():
+    """Four threads with streams of their own, each with calls of every kernel: the results of calls in a row."""
+    import threading
+    import paper_2608_18147_gb300 as E
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    n, k = 512, 640
+    codes = E.ecasq_pack(torch.randint(0, 16, (n, k), generator=gen, device="cuda", dtype=torch.uint8))
+    levels, scales = torch.linspace(-1, 1, 16, device="cuda").bfloat16(), torch.rand(n, 5, generator=gen, device="cuda")
+    w = torch.rand(k, device="cuda")
+    xs = [torch.randn(b, k, generator=gen, device="cuda").bfloat16() for b in (2, 50, 300, 700)]
+    run = lambda x: (E.ecasq_project(x, codes, levels, scales, 128, activation="gelu"), E.ecasq_gated(x, codes, levels, scales, 128), E.ecasq_norm(x, w))  # noqa: E731
+    want = [run(x) for x in xs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for turn in range(20):
+                    j = (i + turn) % len(xs)
+                    got = run(xs[j])
+                    stream.synchronize()
+                    if not all(torch.equal(a, c) for a, c in zip(got, want[j])):
+                        wrong.append((i, turn))
+        except Exception as e:  # noqa: BLE001
+            wrong.append(repr(e))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_norm_refuses_one_tensor_for_both_outputs():
+    import paper_2608_18147_gb300 as E
+    x, r, w = torch.ones(3, 64, device="cuda"), torch.ones(3, 64, device="cuda"), torch.ones(64, device="cuda")
+    for t in (x, r, torch.empty_like(x)):
+        with pytest.raises(E.EcasqError):
+            E.ecasq_norm(x, w, residual=r, out=t, out_sum=t)
+    y, s = E.ecasq_norm(x, w, 0.0, residual=r, out=x, out_sum=r)
+    assert (y == 1).all() and (s == 2).all()

@@ -71,3 +71,14 @@ def test_binding_refuses_tensors_of_the_host():
         assert err.value.code == native.EINVAL
     with pytest.raises(native.EcasqError, match="activation"):
         native.ecasq_gated(f, z, f[0, :16], f, 32, activation="tanh")
+
+
+def test_norm_refuses_one_place_for_both_outputs():
+    from paper_2608_18147_gb300 import native
+    L = native.lib()
+    x, y, residual = V, V + 4096, V + 8192  # addresses that nothing reads: the call is refused
+    good = dict(x=x, x_row=100, type=native.BF16, b=3, k=100, residual=residual, residual_row=100, weight=V, weight_type=native.F32, eps=1e-6, group=0, y=y, y_row=100,
+                sum=None, sum_row=100, scales=None, scale_row=0, stream=None)
+    assert L.ecasq_norm(*dict(good, b=0).values()) == native.OK
+    for at in (x, y, residual):
+        assert L.ecasq_norm(*dict(good, y=at, sum=at).values()) == native.EINVAL
