@@ -349,7 +349,7 @@ static PyObject *py_norm(PyObject *self, PyObject *const *v, Py_ssize_t n_args) 
     PyObject *const floats[] = {v[0], v[1], v[3], v[5], v[6], v[7]};
     if (tracked(floats, 6)) NO;
     if (!stream_of(x.device, &stream)) NO;
-    const int64_t groups = group ? (k + group - 1) / group : 0;
+    const int64_t groups = !group ? 0 : group >= k ? 1 : (k + group - 1) / group;
     if (!(made[0] = output_of(v[5], &x, b, k, group ? E4M3 : x.type, &y)) || made[0] == Py_None) return made[0];
     if (group && (!(made[1] = output_of(v[7], &x, b, groups, ECASQ_F32, &scales)) || made[1] == Py_None)) goto done;
     if (v[3] != Py_None && (!(made[2] = output_of(v[6], &x, b, k, x.type, &sum)) || made[2] == Py_None)) goto done;

@@ -456,7 +456,7 @@ extern "C" int ecasq_norm(const void *x, int64_t x_row, int32_t type, int64_t b,
         k >= (int64_t)1 << 31 || (group < k && group % 16))
         return ECASQ_EINVAL;
     if (b == 0) return ECASQ_OK;
-    const int64_t groups = group ? cdiv(k, group) : 0;
+    const int64_t groups = !group ? 0 : group >= k ? 1 : cdiv(k, group);  // (any group from k on is one: cdiv would go beyond 64 bits for the largest)
     if (!x || !weight || !y || (sum && (!residual || (!group && sum == y))) || (group && (!scales || (b > 1 && scale_row < groups))) ||
         (b > 1 && (x_row < k || y_row < k || (residual && residual_row < k) || (sum && sum_row < k))))
         return ECASQ_EINVAL;
