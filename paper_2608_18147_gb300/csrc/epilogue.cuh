@@ -11,15 +11,25 @@ struct Epilogue {
     int32_t act;  // ECASQ_ACT_*
 };
 
-// The normal distribution's Phi(v), off by 0.8e-7 at most: erfc(x) = (a1 t + ... + a5 t^5) e^(-x^2), t = 1 / (1 + p x), of Abramowitz and Stegun
-// 7.1.26 at x = |v| / sqrt(2).  (CUDA's normcdff is exact to its last bits and took 80 us more for a gated block of 2 x 16384 x 4096 by 2048 rows.)
+// The normal distribution's Phi(v), off by 2^-23 at most, and for v >= -12 by (2^-21 + v^2 2^-23) of itself at most.  Near zero 1/2 + v P(v^2); elsewhere the tail,
+// e^(-v^2 / 2) Q(1 / (1 + 0.32 |v|)).  P and Q are minimax polynomials found by Remez' exchange: P on |v| <= 1.25 (4e-9 of Phi), Q on 1.25 <= |v| <= 14
+// (1.4e-7 of the tail); of roundings there are no more than a sum of positive terms has, as their values change little.  (CUDA's normcdff took 80 us more for a gated
+// block of 2 x 16384 x 4096 by 2048 rows.  A polynomial with error bounded against 1 alone, such as Abramowitz and Stegun's 7.1.26, is off by a quarter of Phi at v = -5.)
 __device__ __forceinline__ float normal_below(float v) {
-    const float x = fabsf(v) * 0.70710678f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float q = 0.5f * p * __expf(-x * x);
-    return v > 0.f ? 1.f - q : q;
+    const float x = fabsf(v), y = v * v, t = __fdividef(1.f, fmaf(0.32f, x, 1.f));
+    float p = fmaf(y, -6.83135290e-6f, 1.11127045e-4f), q = fmaf(t, -0.0797425291f, 0.173089872f);
+    p = fmaf(y, p, -1.18395555e-3f);
+    p = fmaf(y, p, 9.97234950e-3f);
+    p = fmaf(y, p, -0.0664902212f);
+    p = fmaf(y, p, 0.398942277f);
+    q = fmaf(t, q, 0.0160783282f);
+    q = fmaf(t, q, 0.139521287f);
+    q = fmaf(t, q, 0.122674665f);
+    q = fmaf(t, q, 0.128200076f);
+    q = fmaf(t, q, -2.42528593e-5f) * exp2f(-0.72134752f * y);
+    return x < 1.25f ? fmaf(v, p, 0.5f) : v > 0.f ? 1.f - q : q;
 }
-// Activations in fp32.  The exponentials are the hardware's (2^-22 or so); one that overflows gives the limit, 0.
+// Activations in fp32.  The exponentials are the hardware's, off by 2^-21 + |u| 2^-23 of themselves for e^u or so; one that overflows gives the limit, 0.
 __device__ __forceinline__ float activate(float v, int act) {
     switch (act) {
         case ECASQ_ACT_RELU: return v <= 0.f ? 0.f : v;  // (NaN stays NaN)
