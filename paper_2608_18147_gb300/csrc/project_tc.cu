@@ -70,7 +70,7 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     a.type = p.type;
     a.scale_type = p.scale_type;
     a.blocks = (int32_t)cdiv(p.k, 128);
-    a.group_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.group / 128, a.blocks));
+    a.span_blocks = p.group / 128 >= a.blocks || p.group / 128 % kSpanMost == 0 ? std::min(kSpanMost, a.blocks) : 1;
     a.lost = p.lost;
     a.epi = p.epi;
     const int64_t piece = 4 * type_size(p.type);
@@ -86,7 +86,7 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     static constexpr Choice kChoices[] = {{32, 24, 21, 110}, {64, 23, 28, 190}, {128, 27, 35, 350}, {256, 38, 40, 690}};
     static constexpr int kHeld[] = {152, 76, 46, 36, 28, 23};
     static_assert(sizeof kHeld / sizeof *kHeld == kSplitMost, "");
-    const int terms = f32 ? 6 : 1, share = f32 ? std::min(p.group, 128) : (int)std::min<int64_t>(p.group, 1 << 20);
+    const int terms = f32 ? 6 : 1, share = f32 ? std::min(p.group, 128) : p.group % 128 ? std::min(p.group, 1 << 20) : 128 * a.span_blocks;
     int64_t best = INT64_MAX;
     int width = 0;
     for (const Choice &c : kChoices) {

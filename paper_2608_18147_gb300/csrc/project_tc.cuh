@@ -1,9 +1,9 @@
 // project_tc.cuh -- ecasq_project and ecasq_gated for more rows of x than a pass of the matrix-vector kernels takes.
 //
 // The matrix is the left operand: its codes become levels, which go to tensor memory as they are (16 bits, exact), 128 rows a
-// block and 256 a pair of blocks; the rows of x are the right operand, in shared memory.  The sums of the columns of one scale group
+// block and 256 a pair of blocks; the rows of x are the right operand, in shared memory.  The sums of the columns of one scale group, 256 of them at most,
 // come out of tensor memory, are multiplied by their row's scale, which is one number a thread there, and are added up in registers.  So
-// products and scales are as exact as in ecasq_matvec: nothing is rounded before the end.  (Levels times scales, rounded to 16 bits before the
+// products and scales are exact to fp32, as in ecasq_matvec.  (Levels times scales, rounded to 16 bits before the
 // product, would need no sums in between, but are off by as much as the output's own rounding.)
 //
 // What bounds it (8192 x 8192 of bf16, groups of 128, by 4096 rows: 385 to 395 us, 1.4 PFLOP/s, three quarters of a library's 16-bit product on the same
@@ -30,7 +30,7 @@ struct TcArgs {
     int64_t scale_row, y_row, n, b, k, second;  // second: the first row of a gated matrix's other half
     int32_t m, group, type, scale_type;
     int32_t blocks;         // blocks of 128 columns
-    int32_t group_blocks;   // blocks of a scale group, where it holds whole ones
+    int32_t span_blocks;    // blocks whose sums are taken out together, where a scale group holds whole ones: spans begin at multiples of it, and groups too
     int32_t split;          // blocks, or pairs of them, of a cluster that share the columns
     int32_t x_tiles, w_tiles, tiles;  // tiles of rows of x; of the matrix's rows; of the product
     int32_t panel;          // tiles of rows of x that the tiles of the matrix's rows go by before the next ones
@@ -44,8 +44,11 @@ constexpr int kACols = 32;  // columns of tensor memory that 64 columns' levels 
 constexpr int kCodeStage = 128 * 64, kSplitMost = 6;
 constexpr int kScales = 8, kScaleLag = 6;  // scale groups in shared memory; of them on their way
 
-// fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  The tensor core's fp32 sums are
-// cut off, not rounded, at each step, so each term's sums of a block are taken out (k = 1024: an error of 2.8e-7 of the result taken out after every two steps, 2.1e-6 after 48).
+// The tensor core's fp32 sums are cut off, not rounded, at each step of 16 columns, which makes them smaller by up to a unit in the last place a step.  So no sum stays there for more than
+// kSpanMost blocks: in a group of 16384 columns of values of one sign sums were 5.3e-5 too small when they stayed for the whole group; they are 1.2e-6 too small taken out after two blocks, 0.55e-6 after one.
+constexpr int kSpanMost = 2;
+
+// fp32 operands are three bf16 terms, most significant first (8 bits each); of their nine products the six that reach 2^-16.  Each term's sums are taken out after every block.
 __device__ __constant__ const int8_t kXTerm[6] = {0, 0, 0, 1, 1, 2}, kLevelTerm[6] = {0, 1, 2, 0, 1, 0};
 
 // ND columns (rows of x) a product, NH of them a tile.  F32: fp32 operands as bf16 terms, whose levels are found by byte permutes; those of 16-bit
@@ -424,14 +427,14 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         }
         if (wid == 3) {
             // Scales: of each span its groups' scales of the block's 128 rows, four a lane, as fp32.  They come kScaleLag spans ahead, the four bytes
-            // that hold each.  Spans are a group's blocks, or what of them is this pair's; or 64 or 32 columns; of fp32 for each term.
+            // that hold each.  Spans are span_blocks, or what of them is this block's; or 64 or 32 columns; of fp32 for each term.
             struct Span {
                 int group, word, left, term;  // its first word of 32 columns; words that its group still has; fp32: the term
             };
             const int scale_size = a.scale_type == ECASQ_F32 ? 4 : 2, group_words = a.group / 32, last_group = (int)((a.k - 1) / a.group);
             auto advance = [&](Span &s) {
                 constexpr int kWords = 4 / SPANS;
-                int by = SPANS == 1 && !F32 ? s.left : kWords;
+                int by = SPANS == 1 && !F32 ? 4 * a.span_blocks - (s.word & (4 * a.span_blocks - 1)) : kWords;  // (span_blocks: a power of two)
                 if (F32 && (s.word + by) % 4 == 0) {
                     if (++s.term < terms) by -= 4;  // the block again
                     else s.term = 0;
@@ -523,7 +526,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 return there;
             };
             for (int t = cluster; ok && t < a.tiles; t += clusters) {
-                int in_group = kb0 % a.group_blocks, term = 0;
+                int in_span = kb0 % a.span_blocks, term = 0;
                 bool fresh = true;
                 for (int v = 0; v < per_tile; v++) {
                     const uint32_t x = mma_rows(base + xs * Shape::kXStage), levels_at = tmem + kAAt + as * kACols;
@@ -534,7 +537,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                             mma<kPair>(d[h], levels_at + kk * 8, x + ((2 * h + kk / 4) * (Shape::kXRows * 128) + kk % 4 * 32) / 16, kind, add || kk > k0);
                     };
                     if constexpr (SPANS == 1) {
-                        const bool last = F32 || v + 1 == per_tile || in_group + 1 == a.group_blocks;  // (fp32: every term's sums)
+                        const bool last = F32 || v + 1 == per_tile || in_span + 1 == a.span_blocks;  // (fp32: every term's sums)
                         if (!(ok = ready(std::true_type{}, fresh))) break;
                         if (one_lane()) {
                             if (NH == 2) {
@@ -567,7 +570,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                     }
                     if (++term == terms) {
                         term = 0;
-                        if (++in_group == a.group_blocks) in_group = 0;
+                        if (++in_span == a.span_blocks) in_span = 0;
                     }
                     xs = xs + 1 == kXStages ? 0 : xs + 1;
                     as = as + 2 == kAStages ? 0 : as + 2;
@@ -655,7 +658,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         const int part = (wid - 4 - Shape::kDecodeWarps) / 4, quarter = wid & 3;
         const uint32_t there = kPair ? of_rank(d_empty, leader) : d_empty, column = tmem + ((uint32_t)quarter << 21) + (NH == 2 ? 0 : part * kOwn);
         // Spans of a tile.
-        const int spans = SPANS == 1 && !F32 ? (kb1 - 1) / a.group_blocks - kb0 / a.group_blocks + 1 : per_tile * SPANS;
+        const int spans = SPANS == 1 && !F32 ? (kb1 - 1) / a.span_blocks - kb0 / a.span_blocks + 1 : per_tile * SPANS;
         uint32_t buf = NH == 2 ? part : 0, d_parity = 0, turn = 0, span = 0;
         bool ok = !a.lost;
         for (int t = cluster; t < a.tiles; t += clusters, turn++) {
