@@ -443,7 +443,7 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
  *   ecasq_gated    y[i, r] = act(p[i, r]) p[i, n + r]                          for W [2n, k]: the gate's rows, then the other's
  * with p = x W^T as in ecasq_matvec.  Products with scales, sums, bias, activation and residual are fp32; y is rounded once, to x's
  * type.  (More than eight rows of F32 are multiplied as three bf16 terms of 8 bits each: products are within 2^-21 of themselves, for values from about
- * 2^-100 on, and a row with an infinity may be NaN.)
+ * 2^-100 on and finite levels.)
  *   act     none; relu; silu v / (1 + e^-v); gelu v Phi(v), Phi the normal distribution's, to 2^-23 and, for
  *           v >= -12, to 2^-21 + v^2 2^-23 of itself; gelu_tanh v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2
  *   bias    device [n] of `type`, or NULL

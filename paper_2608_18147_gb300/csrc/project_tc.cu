@@ -4,7 +4,8 @@
 namespace ecasq {
 
 // ---------------------------------------------------------------- x in rows that tile_load can read
-// 16-bit rows copied to rows of `to_row` elements, a multiple of 8; fp32 rows as three bf16 terms, of 8 bits each, in three planes of b rows.
+// 16-bit rows copied to rows of `to_row` elements, a multiple of 8; fp32 rows as three bf16 terms, of 8 bits each, in three planes of b rows.  A value that is not finite is its last term
+// alone, which is multiplied by the levels' first terms and by no other: theirs are zero only where the level is (an infinity times a lower term that is zero would be NaN).
 template <bool F32> __global__ void __launch_bounds__(256) k_lay_out(const void *x, int64_t x_row, int64_t b, int64_t k, uint16_t *to, int64_t to_row) {
     wait_before();
     for (int64_t i = blockIdx.y; i < b; i += gridDim.y) {
@@ -16,9 +17,8 @@ template <bool F32> __global__ void __launch_bounds__(256) k_lay_out(const void 
 #pragma unroll
             for (int p = 0; p < 3; p++) {
                 const uint32_t bits = __float_as_uint(v) >> 16;
-                to[(p * b + i) * to_row + c] = finite ? (uint16_t)bits : p ? 0 : v == v ? (uint16_t)bits : 0x7FFF;
-                v -= __uint_as_float(bits << 16);
-                if (!finite) v = static_cast<const float *>(x)[i * x_row + c];
+                to[(p * b + i) * to_row + c] = finite ? (uint16_t)bits : p < 2 ? 0 : v == v ? (uint16_t)bits : 0x7FFF;
+                if (finite) v -= __uint_as_float(bits << 16);
             }
         } else {
             to[i * to_row + c] = static_cast<const uint16_t *>(x)[i * x_row + c];
