@@ -463,6 +463,11 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
 #define ECASQ_ACT_GELU 3
 #define ECASQ_ACT_GELU_TANH 4
 size_t ecasq_workspace_size_project(int64_t b, int64_t n, int64_t k, int32_t type);
+/* Which kernels such a call takes, n outputs a row (test hook; the host's part alone): plan[0] rows of x of a tile on the tensor cores, or 0, with all others 0, for
+ * the matrix-vector kernels; [1] blocks of a cluster that share a tile's columns; [2] clusters (tiles of 256 rows: pairs of blocks) that the
+ * card is taken to hold at once; [3], [4] tiles of rows of x and of the matrix; [5] of the former, those that all of the matrix goes by before the next ones.
+ * ECASQ_EINVAL for sizes that the calls refuse. */
+int ecasq_project_plan(int64_t b, int64_t n, int64_t k, int32_t type, int32_t group, int32_t gated, int64_t *plan);
 int ecasq_project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
                   const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
                   int64_t k, int32_t group, const void *bias, int32_t activation, const void *residual,

@@ -4,7 +4,7 @@
 
 namespace ecasq {
 
-// Rows of x up to which the matrix-vector kernels take a call, one pass of theirs: 28672 x 8192 by eight rows takes them 36 us, by sixteen, in two passes, twice that,
+// Rows of x up to which the matrix-vector kernels take every call, one pass of theirs; plan_project_tc sends them calls with more rows where it counts them the faster ones.  28672 x 8192 by eight rows takes them 36 us, by sixteen, in two passes, twice that,
 // and the tensor cores 53 (8192 x 8192: 16, twice that and 21).
 constexpr int64_t kFewRows = 8;
 
@@ -61,6 +61,18 @@ extern "C" {
 size_t ecasq_workspace_size_project(int64_t b, int64_t n, int64_t k, int32_t type) {
     if (b <= kFewRows || b > 8 * 65535 || n < 1 || k < 1 || k >= (int64_t)1 << 31 || !type_ok(type)) return 0;
     return project_tc_room(b, k, type);
+}
+
+int ecasq_project_plan(int64_t b, int64_t n, int64_t k, int32_t type, int32_t group, int32_t gated, int64_t *plan) {
+    if (b < 0 || b > 8 * 65535 || n < 1 || n >= (int64_t)1 << (gated ? 30 : 31) || k < 1 || k >= (int64_t)1 << 31 || !type_ok(type) || group < 32 || group % 32 || !plan) return ECASQ_EINVAL;
+    const ProjectPlan p = b > kFewRows ? plan_project_tc(b, n, k, type, group, gated != 0) : ProjectPlan{};
+    plan[0] = p.width;
+    plan[1] = p.split;
+    plan[2] = p.held;
+    plan[3] = p.x_tiles;
+    plan[4] = p.w_tiles;
+    plan[5] = p.panel;
+    return ECASQ_OK;
 }
 
 int ecasq_project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row, const void *levels,

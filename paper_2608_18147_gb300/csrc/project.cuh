@@ -17,6 +17,13 @@ struct ProjectArgs {
     Epilogue epi;
 };
 
+// How a call with more than eight rows of x is shared out; width 0: it goes to the matrix-vector kernels.
+struct ProjectPlan {
+    int32_t width, split, held;       // rows of x of a tile; blocks of a cluster that share its columns; clusters, or for tiles of 256 rows pairs of blocks, that the card holds
+    int64_t x_tiles, w_tiles, panel;  // tiles of rows of x, and of the matrix; tiles of rows of x that all tiles of the matrix go by before the next ones
+};
+ProjectPlan plan_project_tc(int64_t b, int64_t n, int64_t k, int32_t type, int32_t group, bool gated);
+
 // The matrix-vector kernels, which read the matrix again for each eight rows of x.
 int launch_project_few(const ProjectArgs &p, cudaStream_t st);
 // Tensor cores, or those where they are faster; the workspace it may need.

@@ -51,9 +51,57 @@ size_t project_tc_room(int64_t b, int64_t k, int32_t type) { return align256((si
 
 constexpr int64_t kPanelBytes = 24 << 20;
 
+// Blocks whose sums are taken out together, for groups of whole blocks: kSpanMost where groups hold that many evenly, or there is one group.
+static int32_t span_blocks(int64_t group, int64_t blocks) { return group / 128 >= blocks || group / 128 % kSpanMost == 0 ? (int32_t)std::min<int64_t>(kSpanMost, blocks) : 1; }
+
+ProjectPlan plan_project_tc(int64_t b, int64_t n, int64_t k, int32_t type, int32_t group, bool gated) {
+    const bool f32 = type == ECASQ_F32;
+    const int64_t blocks = cdiv(k, 128), rows = gated ? 2 * n : n;
+    ProjectPlan plan{};
+    // The width of a tile and the blocks of a cluster that share its columns that take the least time: rounds of tiles over the card, each of its blocks of
+    // columns one after another, whose time goes by the width and by the scale groups in one (measured: 0.27 + 0.35 us a group for 128 rows of x), and of
+    // the tile's start and results.  Only tiles of 256 rows take pairs of blocks; clusters of more than two leave some SMs out (kHeld: what the card holds
+    // of each size).
+    struct Choice {
+        int width, block, group, tile;  // rows of x; hundredths of a microsecond
+    };
+    static constexpr Choice kChoices[] = {{32, 24, 21, 110}, {64, 23, 28, 190}, {128, 27, 35, 350}, {256, 38, 40, 690}};
+    static constexpr int kHeld[] = {152, 76, 46, 36, 28, 23};
+    static_assert(sizeof kHeld / sizeof *kHeld == kSplitMost, "");
+    const int terms = f32 ? 6 : 1, share = f32 ? std::min(group, 128) : group % 128 ? std::min(group, 1 << 20) : 128 * span_blocks(group, blocks);
+    int64_t best = INT64_MAX;
+    for (const Choice &c : kChoices) {
+        const bool pair = c.width == 256;
+        const int64_t tiles = cdiv(n, (gated ? 64 : 128) * (pair ? 2 : 1)) * cdiv(b, c.width);
+        for (int s = 1; s <= (pair ? 1 : kSplitMost) && s <= blocks; s++) {
+            const int held = pair ? 76 : kHeld[s - 1];
+            const int64_t cost = cdiv(tiles, held) * (cdiv(blocks, s) * terms * (c.block + c.group * 128 / share) + c.tile + (s > 1 ? 20 + 30 * s : 0));
+            if (cost >= best) continue;
+            best = cost;
+            plan.width = c.width;
+            plan.split = s;
+            plan.held = held;
+        }
+        if (c.width >= b) break;
+    }
+    // The matrix-vector kernels, a pass for each eight rows, are the faster ones for small matrices (300 x 8192 by 16 rows: 6.3 us, and 11.8 here; 1024 x 1024
+    // 6.8 and 8.3; 4096 x 4096 13.3 and 11.5).  Their blocks take 3.2 us each and their codes at 16 bytes a nanosecond (fp32 6.2 us, 2.4 bytes), a round
+    // of 152 after another; these stand at 5 us for a launch, 2 for rows of x that are laid out first, and what is counted above.
+    const int64_t few_blocks = std::min<int64_t>(cdiv(n, 8), 152), few = cdiv(few_blocks * cdiv(b, 8), 152) * ((f32 ? 620 : 320) + rows * k / 2 / few_blocks / (f32 ? 24 : 158));
+    if (few < best + (f32 ? 700 : 500)) return ProjectPlan{};
+    plan.x_tiles = cdiv(b, plan.width);
+    plan.w_tiles = cdiv(n, (gated ? 64 : 128) * (plan.width == 256 ? 2 : 1));
+    plan.panel = std::max<int64_t>(1, std::min<int64_t>(plan.x_tiles, kPanelBytes / (plan.width * k * 2 * (f32 ? 3 : 1))));
+    plan.panel = cdiv(plan.x_tiles, cdiv(plan.x_tiles, plan.panel));  // (panels alike)
+    return plan;
+}
+
 int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st) {
-    const bool f32 = p.type == ECASQ_F32;
-    const int64_t rows = p.gated ? 2 * p.n : p.n;
+    const ProjectPlan plan = plan_project_tc(p.b, p.n, p.k, p.type, p.group, p.gated);
+    if (!plan.width) return launch_project_few(p, st);
+    const bool f32 = p.type == ECASQ_F32, pair = plan.width == 256;
+    const int64_t rows = p.gated ? 2 * p.n : p.n, tiles = plan.w_tiles * plan.x_tiles;
+    if (tiles > INT32_MAX - 1024) return ECASQ_EINVAL;  // (a block's last step goes beyond them by at most a card's clusters)
     TcArgs a{};
     a.levels = p.levels;
     a.scales = p.scales;
@@ -70,51 +118,17 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
     a.type = p.type;
     a.scale_type = p.scale_type;
     a.blocks = (int32_t)cdiv(p.k, 128);
-    a.span_blocks = p.group / 128 >= a.blocks || p.group / 128 % kSpanMost == 0 ? std::min(kSpanMost, a.blocks) : 1;
+    a.span_blocks = span_blocks(p.group, a.blocks);
+    a.split = plan.split;
+    a.x_tiles = (int32_t)plan.x_tiles;
+    a.w_tiles = (int32_t)plan.w_tiles;
+    a.tiles = (int32_t)tiles;
+    a.panel = (int32_t)plan.panel;
     a.lost = p.lost;
     a.epi = p.epi;
     const int64_t piece = 4 * type_size(p.type);
     const auto in_pieces = [&](const void *at, int64_t row) { return reinterpret_cast<uintptr_t>(at) % piece == 0 && (p.b == 1 || row % 4 == 0); };
     a.wide = in_pieces(p.y, p.y_row) && in_pieces(p.epi.residual, p.epi.residual_row);
-    // The width of a tile and the blocks of a cluster that share its columns that take the least time: rounds of tiles over the card, each of its blocks of
-    // columns one after another, whose time goes by the width and by the scale groups in one (measured: 0.27 + 0.35 us a group for 128 rows of x), and of
-    // the tile's start and results.  Only tiles of 256 rows take pairs of blocks; clusters of more than two leave some SMs out (kHeld: what the card holds
-    // of each size).
-    struct Choice {
-        int width, block, group, tile;  // rows of x; hundredths of a microsecond
-    };
-    static constexpr Choice kChoices[] = {{32, 24, 21, 110}, {64, 23, 28, 190}, {128, 27, 35, 350}, {256, 38, 40, 690}};
-    static constexpr int kHeld[] = {152, 76, 46, 36, 28, 23};
-    static_assert(sizeof kHeld / sizeof *kHeld == kSplitMost, "");
-    const int terms = f32 ? 6 : 1, share = f32 ? std::min(p.group, 128) : p.group % 128 ? std::min(p.group, 1 << 20) : 128 * a.span_blocks;
-    int64_t best = INT64_MAX;
-    int width = 0;
-    for (const Choice &c : kChoices) {
-        const bool pair = c.width == 256;
-        const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * cdiv(p.b, c.width);
-        for (int s = 1; s <= (pair ? 1 : kSplitMost) && s <= a.blocks; s++) {
-            const int64_t held = pair ? 76 : kHeld[s - 1];
-            const int64_t cost = cdiv(tiles, held) * (cdiv(a.blocks, s) * terms * (c.block + c.group * 128 / share) + c.tile + (s > 1 ? 20 + 30 * s : 0));
-            if (cost >= best) continue;
-            best = cost;
-            width = c.width;
-            a.split = s;
-        }
-        if (c.width >= p.b) break;
-    }
-    // The matrix-vector kernels, a pass for each eight rows, are the faster ones for small matrices (300 x 8192 by 16 rows: 6.3 us, and 11.8 here; 1024 x 1024
-    // 6.8 and 8.3; 4096 x 4096 13.3 and 11.5).  Their blocks take 3.2 us each and their codes at 16 bytes a nanosecond (fp32 6.2 us, 2.4 bytes), a round
-    // of 152 after another; these stand at 5 us for a launch, 2 for rows of x that are laid out first, and what is counted above.
-    const int64_t few_blocks = std::min<int64_t>(cdiv(p.n, 8), 152), few = cdiv(few_blocks * cdiv(p.b, 8), 152) * ((f32 ? 620 : 320) + rows * p.k / 2 / few_blocks / (f32 ? 24 : 158));
-    if (few < best + (f32 ? 700 : 500)) return launch_project_few(p, st);
-    const bool pair = width == 256;
-    a.x_tiles = (int32_t)cdiv(p.b, width);
-    const int64_t tiles = cdiv(p.n, (p.gated ? 64 : 128) * (pair ? 2 : 1)) * a.x_tiles;
-    if (tiles > INT32_MAX - 1024) return ECASQ_EINVAL;  // (a block's last step goes beyond them by at most a card's clusters)
-    a.tiles = (int32_t)tiles;
-    a.w_tiles = (int32_t)(tiles / a.x_tiles);
-    a.panel = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.x_tiles, kPanelBytes / (width * p.k * 2 * (f32 ? 3 : 1))));
-    a.panel = (int32_t)cdiv(a.x_tiles, cdiv(a.x_tiles, a.panel));  // (panels alike)
     const void *x = p.x;
     int64_t x_row = p.x_row;
     if (f32 || !aligned16(p.x) || (p.b > 1 && p.x_row % 8)) {
@@ -127,12 +141,12 @@ int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStrea
         x_row = laid_row(p.k);
     }
     CUtensorMap xm, cm;
-    const int x_rows = std::min(width, 128) / (pair ? 2 : 1);
+    const int x_rows = std::min(plan.width, 128) / (pair ? 2 : 1);
     int rc = make_tile_map(&xm, p.type == ECASQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, p.k, f32 ? 3 * p.b : p.b,
                            (p.b > 1 || f32 ? x_row : laid_row(p.k)) * 2, 64, x_rows, CU_TENSOR_MAP_SWIZZLE_128B);
     if (!rc) rc = make_tile_map(&cm, CU_TENSOR_MAP_DATA_TYPE_UINT8, p.codes, 64 * cdiv(p.k, 128), rows, p.code_row, 64, 64, CU_TENSOR_MAP_SWIZZLE_64B);
     if (rc) return rc;
-    return p.gated ? launch_tc_gated(width, xm, cm, a, st) : launch_tc_width<false>(width, xm, cm, a, st);
+    return p.gated ? launch_tc_gated(plan.width, xm, cm, a, st) : launch_tc_width<false>(plan.width, xm, cm, a, st);
 }
 
 }  // namespace ecasq
