@@ -31,7 +31,7 @@ struct TcArgs {
     int32_t m, group, type, scale_type;
     int32_t blocks;         // blocks of 128 columns
     int32_t span_blocks;    // blocks whose sums are taken out together, where a scale group holds whole ones: spans begin at multiples of it, and groups too
-    int32_t split;          // blocks, or pairs of them, of a cluster that share the columns
+    int32_t split;          // blocks of a cluster that share the columns; 1 for pairs
     int32_t x_tiles, w_tiles, tiles;  // tiles of rows of x; of the matrix's rows; of the product
     int32_t panel;          // tiles of rows of x that the tiles of the matrix's rows go by before the next ones
     bool wide;              // y and the residual in pieces of four values
@@ -132,7 +132,7 @@ __device__ __forceinline__ void narrow(const float (&v)[4], bool bf16, uint2 &p)
 // How four warps' sums leave the block.  They lie in shared memory, entry (column c, matrix row r of the block) at 128 c + r, and
 // a thread takes four neighbouring outputs of a row of x, so that a row's 64 or 128 outputs leave side by side (each matrix row's outputs on their own, 64
 // bytes a warp, took 60 us a tile of 256 x 256; eight a thread spill, as a thread's sums of the other columns are held meanwhile).  Of a gated
-// matrix a warp had 16 rows of the gate and the same 16 of the other half.  Over split > 1 pairs of the cluster sums are added up.
+// matrix a warp had 16 rows of the gate and the same 16 of the other half.  Where split > 1 blocks share the columns, their sums are added up.
 template <bool GATED, bool SPLIT, bool F32> struct Finish {
     static constexpr int kLanes = GATED ? 16 : 32, kAtOnce = 128 / kLanes, kTurns = GATED ? 2 : 4;  // threads of a row of x; rows of x at once; turns that are fetched for together
     using Bits = FourOf<F32>;
@@ -140,13 +140,12 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
     const TcArgs &a;
     const float *sums;
     int64_t row;       // the thread's first output
-    uint32_t first, stride;  // ranks of the blocks whose sums are added up: first, first + stride, ...
     bool whole;        // its four lie side by side and aligned
     Bits residual[GATED ? 1 : kTurns];
     const One *ahead = nullptr;  // the next residual; columns from it on
     int left = 0;
 
-    __device__ __forceinline__ Finish(const TcArgs &a, const float *from, int64_t r0, uint32_t first, uint32_t stride) : a(a), first(first), stride(stride) {
+    __device__ __forceinline__ Finish(const TcArgs &a, const float *from, int64_t r0) : a(a) {
         const int part = threadIdx.x % kLanes;
         row = r0 + 4 * part;
         whole = a.wide && row + 4 <= a.n;
@@ -197,7 +196,7 @@ template <bool GATED, bool SPLIT, bool F32> struct Finish {
         for (int p = 0; p < a.split; p++) {
             float4 f;
             asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                         : "r"(of_rank(shared_at(at), first + p * stride)) : "memory");
+                         : "r"(of_rank(shared_at(at), p)) : "memory");
             v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
         }
     }
@@ -268,7 +267,7 @@ __device__ __forceinline__ void look_up(uint32_t w, uint32_t lane, uint32_t *to)
     for (int j = 0; j < 4; j++) to[j] = *static_cast<const uint32_t *>(__cvta_shared_to_generic(permute(w, 0, 0x4440 | j) * 128 + lane));
 }
 
-// A cluster is `split` blocks, or pairs of them.  Of a block's warps, the first brings in rows of x, the second issues products, the third brings in codes, the
+// A cluster is `split` blocks, or a pair.  Of a block's warps, the first brings in rows of x, the second issues products, the third brings in codes, the
 // fourth scales; kDecodeWarps turn codes into levels; eight take sums out, each its share of the columns.  Barriers pass stages between them; those that
 // the products' issuer waits for are in the first block of a pair, which issues for both.  The issuer's warp runs together, so that addresses stay in
 // uniform registers: with them in one lane's registers, 8192 x 8192 by 4096 rows took 1404 us where it then took 560 (with that, results also began to leave in
@@ -283,14 +282,14 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
     const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
     char *smem = smem_raw + (base - shared_at(smem_raw));
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const uint32_t rank = cluster_rank(), half = kPair ? rank & 1 : 0, leader = rank - half, size = Shape::kBlocks * a.split, pair = rank / Shape::kBlocks;
+    const uint32_t rank = cluster_rank(), half = kPair ? rank & 1 : 0, leader = rank - half, size = Shape::kBlocks * a.split, share = rank / Shape::kBlocks;  // (share is 0 for pairs; where the compiler knew that, 8192 x 8192 by 4096 rows took 472 us and not 390)
     const uint32_t bars = base + Shape::kBarsAt;
     const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
                    a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
                    s_full = d_empty + 8 * kDBufs, s_empty = s_full + 8 * kScales, all_done = s_empty + 8 * kScales, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
     uint32_t *books = reinterpret_cast<uint32_t *>(smem + Shape::kBooksAt);
     constexpr int terms = F32 ? 6 : 1;
-    const int kb0 = (int)((int64_t)a.blocks * pair / a.split), kb1 = (int)((int64_t)a.blocks * (pair + 1) / a.split);
+    const int kb0 = (int)((int64_t)a.blocks * share / a.split), kb1 = (int)((int64_t)a.blocks * (share + 1) / a.split);
     const int cluster = blockIdx.x / size, clusters = gridDim.x / size;
 
     auto lose = [&] {
@@ -664,7 +663,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         for (int t = cluster; t < a.tiles; t += clusters, turn++) {
             const int64_t r0 = rows_at(tile_of(t).y);
             float *sums = reinterpret_cast<float *>(smem + Shape::kSumsAt) + part * Shape::kOut * 128;
-            Finish<GATED, NH == 1, F32>(a, sums, r0, half, Shape::kBlocks).announce((int64_t)tile_of(t).x * kN + part * kOwn, kOwn);
+            Finish<GATED, NH == 1, F32>(a, sums, r0).announce((int64_t)tile_of(t).x * kN + part * kOwn, kOwn);
             uint64_t acc[kOwn / 2];  // pairs of columns
 #pragma unroll
             for (int c = 0; c < kOwn / 2; c++) acc[c] = 0;
@@ -718,12 +717,12 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 else asm volatile("bar.sync 1, 128;" ::: "memory");
             };
             int c0 = 0, c1 = kOut;
-            if (NH == 1 && a.split > 1) {  // each pair takes a share of the columns over all pairs
+            if (NH == 1 && a.split > 1) {  // each block finishes a share of the columns, of which it adds up all blocks' sums
                 ok = ok && wait_cluster(sums_empty, (turn & 1) ^ 1);
-                c0 = (int)pair * kOut / a.split;
-                c1 = (int)(pair + 1) * kOut / a.split;
+                c0 = (int)share * kOut / a.split;
+                c1 = (int)(share + 1) * kOut / a.split;
             }
-            Finish<GATED, NH == 1, F32> finish(a, sums, r0, half, Shape::kBlocks);
+            Finish<GATED, NH == 1, F32> finish(a, sums, r0);
             constexpr int kTurns = finish.kTurns, kAtOnce = finish.kAtOnce;
             const int64_t first_x = (int64_t)tile_of(t).x * kN + part * kOwn;
             finish.begin(first_x, c0 + finish.turn(), (int)min((int64_t)(NH == 2 ? kOwn : c1), a.b - first_x));
@@ -743,7 +742,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 }
                 if (NH == 1 && a.split > 1) {
                     __syncwarp();
-                    if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_full, Shape::kBlocks * lane + half));
+                    if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_full, lane));
                     if (!(ok = ok && wait_cluster(sums_full, turn & 1)))
                         for (int c = 0; c < kOut; c++) sums[128 * c + 32 * quarter + lane] = CUDART_NAN_F;
                 }
@@ -752,7 +751,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             }
             if (NH == 1 && a.split > 1) {
                 __syncwarp();
-                if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_empty, Shape::kBlocks * lane + half));
+                if (ok && lane < a.split) mbar_arrive<true>(of_rank(sums_empty, lane));
             }
         }
         if (!ok && lane == 0 && a.status) atomicOr(a.status, ECASQ_BAD_WAIT);
