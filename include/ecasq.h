@@ -455,7 +455,7 @@ int ecasq_matvec(const void *x, int64_t x_row, int32_t type, int64_t b, const ui
  * all begin at multiples of 16 bytes needs none.
  *   status  ECASQ_BAD_WAIT: here what a block had not stored when the wait ran out is NaN
  * Which kernel takes a call goes by its sizes and types alone: equal calls give equal bits.
- * ECASQ_EINVAL as for ecasq_matvec, and for a bad activation; ECASQ_EWORKSPACE where a workspace is needed and is too small.
+ * ECASQ_EINVAL as for ecasq_matvec, for a bad activation, and for y at x's address; ECASQ_EWORKSPACE where a workspace is needed and is too small.
  * ECASQ_TEST_LOST_WAIT as for ecasq_matvec. */
 #define ECASQ_ACT_NONE 0
 #define ECASQ_ACT_RELU 1

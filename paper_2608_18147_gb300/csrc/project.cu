@@ -45,7 +45,7 @@ static int project(const void *x, int64_t x_row, int32_t type, int64_t b, const 
         (scale_type != type && scale_type != ECASQ_F32) || group < 32 || group % 32 || epi.act < ECASQ_ACT_NONE || epi.act > ECASQ_ACT_GELU_TANH)
         return ECASQ_EINVAL;
     if (b == 0) return ECASQ_OK;
-    if (!x || !codes || !levels || !scales || !y || !aligned16(codes) || code_row % 16 || code_row < 64 * cdiv(k, 128) || scale_row < cdiv(k, group) ||
+    if (!x || !codes || !levels || !scales || !y || y == x || !aligned16(codes) || code_row % 16 || code_row < 64 * cdiv(k, 128) || scale_row < cdiv(k, group) ||
         (b > 1 && (x_row < k || y_row < n || (epi.residual && epi.residual_row < n))))
         return ECASQ_EINVAL;
     const ProjectArgs a{x, levels, scales, codes, y, status, x_row, code_row, scale_row, y_row, n, k, b, m, group, type, scale_type, gated, lost_wait, epi};

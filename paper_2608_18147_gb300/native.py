@@ -742,8 +742,8 @@ def ecasq_project(x, codes, levels, scales, group, bias=None, activation=None, r
 
     x, codes, levels, scales, group, status as for ecasq_matvec; bias [n] and residual [b, n] (or [n]) of x's type or None;
     activation None, "relu", "silu", "gelu" or "gelu_tanh".  ws: workspace_project(b, n, k, x.dtype), or None (one is made
-    where one is needed: for float32, and for rows of x off 16-byte boundaries).  Returns y [b, n] or [n] of x's type (`out` if given, which may be the residual itself).
-    No gradients: a tensor that requires one is refused while they are recorded."""
+    where one is needed: for float32, and for rows of x off 16-byte boundaries).  Returns y [b, n] or [n] of x's type (`out` if given, which may be the
+    residual itself, not x).  No gradients: a tensor that requires one is refused while they are recorded."""
     act = _activation("ecasq_project", activation)
     y = (_codes or _ready()).project(x, codes, levels, scales, group, bias, act, residual, out, ws, status)
     if y is None:
@@ -758,7 +758,7 @@ def ecasq_gated(x, codes, levels, scales, group, activation="silu", out=None, ws
 
     codes, levels, scales: one coded matrix of 2n rows, those of G and then those of U; x, group and status as for
     ecasq_matvec; activation and ws (workspace_project(b, 2 * n, k, x.dtype)) as for ecasq_project.  Returns h [b, n] or
-    [n] of x's type (`out` if given).  No gradients: a tensor that requires one is refused while they are recorded."""
+    [n] of x's type (`out` if given, not x).  No gradients: a tensor that requires one is refused while they are recorded."""
     act = _activation("ecasq_gated", activation)
     y = (_codes or _ready()).gated(x, codes, levels, scales, group, act, out, ws, status)
     if y is None:
