@@ -44,7 +44,7 @@ template <bool MAX, int NT> __device__ __forceinline__ float over_row(float v, f
     return v;
 }
 
-// A group's scale from its largest value: the quotient by 448, e4m3's largest, rounded once (a product with the reciprocal and its correction).
+// A group's scale from its largest value: the quotient by 448, e4m3's largest, rounded once: a product with the reciprocal, and its remainder's (Markstein 1990).
 __device__ __forceinline__ float scale_of(float most) {
     const float q = __fmul_rn(most, 1.f / 448.f), scale = __fmaf_rn(__fmaf_rn(-448.f, q, most), 1.f / 448.f, q);
     return scale == 0.f ? 1.f : scale;
@@ -136,6 +136,8 @@ template <typename W, int N, bool ALIGNED> __device__ __forceinline__ void weigh
 // normed values are found, their maxima exchanged and the codes made between a row's loads and its stores, with issue slots half used: latency); the shifting of weights where they are not (3001 x 5003 of fp32 27 us, 4.5 TB/s); one
 // row of 4096 takes 2.3 us, two memory latencies and a launch.  With weights in registers instead of shared memory, and pieces that every
 // thread looked at value by value, the aligned cases took 141 and 185 us: two blocks an SM instead of three, and code that did not fit its cache.
+// Chosen at run time, the forms (none, one scale a row, groups by shuffles, groups by atomics) share their registers: 38 of this file's 135 kernels spill, that of the 8192 x 8192 of bf16 to
+// 8 bits 24 bytes, fp16 ones read up to 664 back.
 template <typename T, typename W, int P, int NT, bool ALIGNED>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT, NT <= 256 ? 3 : NT == 512 && P <= 3 ? 2 : 1) k_norm(const __grid_constant__ NormArgs a) {
     constexpr int kThreads = NT < 256 ? 256 : NT, kAtOnce = kThreads / NT, N = Piece<T>::kValues;  // rows of a block; values of a piece

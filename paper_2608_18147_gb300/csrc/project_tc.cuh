@@ -9,9 +9,9 @@
 // What bounds it (8192 x 8192 of bf16, groups of 128, by 4096 rows: 385 to 395 us, 1.4 PFLOP/s, three quarters of a library's 16-bit product on the same
 // card): the tensor core is busy 59 % of the time.  At its rate a block of 128 columns of a pair's 256 x 256 tile is 1024 clocks; an adding warp took 740 for
 // its share of a block's sums (eight loads of 16 columns from tensor memory, 92 clocks each, before two of them were under way at once), so smaller groups,
-// with more sums, cost more: 551 us in groups of 64, 930 in groups of 32, 365 in groups of 256.  With the results left unwritten it took 368 us: about
-// 3 us for each of a pair's seven tiles.  A residual adds about 8 us a tile (440 us).  With few rows of x it is the ways between the warps: where each block
-// has a tile of its own, 128 columns take 0.38 us by 32 rows and 0.60 by 128 rows, on top of 6 us for the shortest product.  9700 x 8192 by 64 rows takes 25 us
+// with more sums, cost more: 551 us in groups of 64, 930 in groups of 32, 370 in groups of 256, and 380 in longer
+// ones, whose sums are taken out as often.  With the results left unwritten it took 368 us: about 3 us for each of a pair's seven tiles.  A residual adds about 8 us a tile (447 us).  Registers
+// spill in 21 of the 48 kernels, 12 bytes stored and 40 read in this case's.  With few rows of x it is the ways between the warps: where each block has a tile of its own, 128 columns take 0.38 us by 32 rows and 0.60 by 128 rows, on top of 6 us for the shortest product.  9700 x 8192 by 64 rows takes 25 us
 // in single blocks and took 42 in pairs; where a pair has as many tiles as a block there is little to gain (8192 x 8192 by 16 rows 21 us both ways, by 128 rows 28 and 29).
 #pragma once
 
