@@ -468,6 +468,9 @@ size_t ecasq_workspace_size_project(int64_t b, int64_t n, int64_t k, int32_t typ
  * card is taken to hold at once; [3], [4] tiles of rows of x and of the matrix; [5] of the former, those that all of the matrix goes by before the next ones.
  * ECASQ_EINVAL for sizes that the calls refuse. */
 int ecasq_project_plan(int64_t b, int64_t n, int64_t k, int32_t type, int32_t group, int32_t gated, int64_t *plan);
+/* The rings of the kernel with tiles of `width` rows of x (test hook; the host's part alone): rings[0] teams of warps that take turns at blocks of columns; [1], [2] stages of codes, and
+ * barriers that say that they are there; [3] stages of x; [4] blocks whose levels there is room for; [5] parts of a tile's rows of x; [6] buffers of sums. */
+int ecasq_project_rings(int32_t width, int32_t type, int32_t gated, int32_t *rings);
 int ecasq_project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row,
                   const void *levels, int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n,
                   int64_t k, int32_t group, const void *bias, int32_t activation, const void *residual,

@@ -75,6 +75,12 @@ int ecasq_project_plan(int64_t b, int64_t n, int64_t k, int32_t type, int32_t gr
     return ECASQ_OK;
 }
 
+int ecasq_project_rings(int32_t width, int32_t type, int32_t gated, int32_t *rings) {
+    if ((width != 32 && width != 64 && width != 128 && width != 256) || !type_ok(type) || !rings) return ECASQ_EINVAL;
+    project_tc_rings(width, type == ECASQ_F32, gated != 0, rings);
+    return ECASQ_OK;
+}
+
 int ecasq_project(const void *x, int64_t x_row, int32_t type, int64_t b, const uint8_t *codes, int64_t code_row, const void *levels,
                   int32_t m, const void *scales, int64_t scale_row, int32_t scale_type, int64_t n, int64_t k, int32_t group,
                   const void *bias, int32_t activation, const void *residual, int64_t residual_row, void *y, int64_t y_row, void *ws,

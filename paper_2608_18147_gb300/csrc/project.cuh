@@ -24,6 +24,8 @@ struct ProjectPlan {
 };
 ProjectPlan plan_project_tc(int64_t b, int64_t n, int64_t k, int32_t type, int32_t group, bool gated);
 
+void project_tc_rings(int width, bool f32, bool gated, int32_t *rings);
+
 // The matrix-vector kernels, which read the matrix again for each eight rows of x.
 int launch_project_few(const ProjectArgs &p, cudaStream_t st);
 // Tensor cores, or those where they are faster; the workspace it may need.

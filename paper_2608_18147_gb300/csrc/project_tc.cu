@@ -1,4 +1,6 @@
 // project_tc.cu -- ecasq_project and ecasq_gated on the tensor cores: the host's part, and the kernels of ecasq_project.
+#include <iterator>
+
 #include "project_tc.cuh"
 
 namespace ecasq {
@@ -94,6 +96,22 @@ ProjectPlan plan_project_tc(int64_t b, int64_t n, int64_t k, int32_t type, int32
     plan.panel = std::max<int64_t>(1, std::min<int64_t>(plan.x_tiles, kPanelBytes / (plan.width * k * 2 * (f32 ? 3 : 1))));
     plan.panel = cdiv(plan.x_tiles, cdiv(plan.x_tiles, plan.panel));  // (panels alike)
     return plan;
+}
+
+template <int ND, int NH, bool GATED, bool F32> static void rings_of(int32_t *to) {
+    using Shape = TcShape<ND, NH, GATED, F32>;
+    const int32_t rings[] = {Shape::kTeams, Shape::kCodeStages, Shape::kCodeBars, Shape::kXStages, Shape::kAStages / 2, NH, Shape::kDBufs};
+    std::copy(std::begin(rings), std::end(rings), to);
+}
+template <bool GATED, bool F32> static void rings_of_width(int width, int32_t *to) {
+    if (width == 32) rings_of<32, 1, GATED, F32>(to);
+    else if (width == 64) rings_of<64, 1, GATED, F32>(to);
+    else if (width == 128) rings_of<128, 1, GATED, F32>(to);
+    else rings_of<128, 2, GATED, F32>(to);
+}
+void project_tc_rings(int width, bool f32, bool gated, int32_t *rings) {
+    if (gated) f32 ? rings_of_width<true, true>(width, rings) : rings_of_width<true, false>(width, rings);
+    else f32 ? rings_of_width<false, true>(width, rings) : rings_of_width<false, false>(width, rings);
 }
 
 int launch_project_tc(const ProjectArgs &p, void *ws, size_t ws_bytes, cudaStream_t st) {

@@ -67,6 +67,13 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static_assert(kAAt >= kDBufs * ND, "the sums' buffers end where the levels begin");
     static constexpr int kTable = F32 ? 0 : 256 * 128;            // a pair of levels for each byte of codes, a copy a lane
     static constexpr int kXStages = kN >= 256 ? 4 : kN == 128 ? 3 : kN == 64 ? 5 : 8, kCodeStages = kN >= 128 ? 3 : kN == 64 ? 9 : 12;
+    // A wait for a barrier's phase ends at once where the phase before it has not ended either, so a warp may wait for a phase only if it knows of the one before.  The warps that decode are teams, which take
+    // turns at the blocks: where they would also take turns at a stage of codes, each has barriers of its own for it, whose phases it has all waited for.  (With one barrier a stage a team went on with
+    // the codes of three blocks before, and freed the stage for others, when the copy for the other team came later than both copies after it.)  Of a stage of x a team has waited for
+    // its levels' stage before, which was free once the products of the block kAStages / 2 before, and all before them, had been done.
+    static constexpr int kTeams = kDecodeWarps / 4, kCodeBars = kCodeStages % kTeams ? kCodeStages * kTeams : kCodeStages;
+    static_assert(kXStages % kTeams == 0 || kXStages >= kAStages / 2, "a team might wait for a phase of a stage of x and not know of the one before");
+    static_assert(kAStages / 2 % kTeams == 0, "stages of levels are a team's own");
     static constexpr int kOwn = NH == 2 ? ND : ND / 2;            // columns of an adding thread
     static constexpr int kOut = NH == 2 ? 32 : kOwn;  // of them at a time on their way out through shared memory
     static constexpr int kSums = 2 * kOut * 128 * 4;              // what the adding warps have on their way out
@@ -74,7 +81,7 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     static constexpr bool kUneven = kOwn >= 64;
     static constexpr int kRegs = 48, kDecodeRegs = 80, kAddRegs = NH == 2 ? 192 : 136;
     static_assert(4 * kRegs + kDecodeWarps * kDecodeRegs + 8 * kAddRegs <= kWarps * (65536 / kThreads / 8 * 8), "the split would wait for ever");
-    static constexpr int kBars = 2 * kXStages + 2 * kCodeStages + 2 * kAStages + 2 * kDBufs + 2 * kScales + 3;
+    static constexpr int kBars = 2 * kXStages + kCodeBars + kCodeStages + 2 * kAStages + 2 * kDBufs + 2 * kScales + 3;
     static constexpr int kTableAt = kXStages * kXStage + kCodeStages * kCodeStage, kSumsAt = kTableAt + kTable, kScalesAt = kSumsAt + kSums, kBooksAt = kScalesAt + kScales * 128 * 4, kBarsAt = kBooksAt + 128;
     static constexpr int kBytes = 1024 + kBarsAt + 8 * kBars + 16;  // 1024: to begin at a multiple of it
 };
@@ -277,14 +284,14 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                                                                             const __grid_constant__ TcArgs a) {
     using Shape = TcShape<ND, NH, GATED, F32>;
     constexpr bool kPair = Shape::kPair;
-    constexpr int kN = Shape::kN, kDBufs = Shape::kDBufs, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kAStages = Shape::kAStages, kAAt = Shape::kAAt, kOwn = Shape::kOwn;
+    constexpr int kN = Shape::kN, kDBufs = Shape::kDBufs, kXStages = Shape::kXStages, kCodeStages = Shape::kCodeStages, kCodeBars = Shape::kCodeBars, kAStages = Shape::kAStages, kAAt = Shape::kAAt, kOwn = Shape::kOwn;
     extern __shared__ char smem_raw[];
     const uint32_t base = shared_at(smem_raw) + 1023 & ~1023u;
     char *smem = smem_raw + (base - shared_at(smem_raw));
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const uint32_t rank = cluster_rank(), half = kPair ? rank & 1 : 0, leader = rank - half, size = Shape::kBlocks * a.split, share = rank / Shape::kBlocks;  // (share is 0 for pairs; where the compiler knew that, 8192 x 8192 by 4096 rows took 472 us and not 390)
     const uint32_t bars = base + Shape::kBarsAt;
-    const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeStages,
+    const uint32_t x_full = bars, x_empty = x_full + 8 * kXStages, c_full = x_empty + 8 * kXStages, c_empty = c_full + 8 * kCodeBars,
                    a_full = c_empty + 8 * kCodeStages, a_empty = a_full + 8 * kAStages, d_full = a_empty + 8 * kAStages, d_empty = d_full + 8 * kDBufs,
                    s_full = d_empty + 8 * kDBufs, s_empty = s_full + 8 * kScales, all_done = s_empty + 8 * kScales, sums_full = all_done + 8, sums_empty = sums_full + 8, lost_at = sums_empty + 8, tmem_at = lost_at + 4;
     uint32_t *books = reinterpret_cast<uint32_t *>(smem + Shape::kBooksAt);
@@ -321,10 +328,8 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             mbar_init(x_full + 8 * i, 1);
             mbar_init(x_empty + 8 * i, 1);
         }
-        for (int i = 0; i < kCodeStages; i++) {
-            mbar_init(c_full + 8 * i, 1);
-            mbar_init(c_empty + 8 * i, 4);
-        }
+        for (int i = 0; i < kCodeBars; i++) mbar_init(c_full + 8 * i, 1);
+        for (int i = 0; i < kCodeStages; i++) mbar_init(c_empty + 8 * i, 4);
         for (int i = 0; i < kAStages; i++) {
             mbar_init(a_full + 8 * i, 4 * Shape::kBlocks);
             mbar_init(a_empty + 8 * i, 1);
@@ -412,16 +417,16 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
                 for (int t = cluster; ok && t < a.tiles; t += clusters) {
                     const int64_t r0 = rows_at(tile_of(t).y);
                     for (int v = 0; ok && v < per_tile; v++, i++) {
-                        const uint32_t s = i % kCodeStages, to = base + kXStages * Shape::kXStage + s * kCodeStage;
+                        const uint32_t s = i % kCodeStages, to = base + kXStages * Shape::kXStage + s * kCodeStage, full = c_full + 8 * (i % kCodeBars);
                         if (!(ok = wait(c_empty + 8 * s, (i / kCodeStages & 1) ^ 1))) break;
-                        mbar_expect(c_full + 8 * s, kCodeStage);
+                        mbar_expect(full, kCodeStage);
                         const int kb = kb0 + v / terms;
-                        tile_load(to, &cm, kb * 64, (int32_t)r0, c_full + 8 * s);
-                        tile_load(to + kCodeStage / 2, &cm, kb * 64, (int32_t)(r0 + (GATED ? a.second : 64)), c_full + 8 * s);
+                        tile_load(to, &cm, kb * 64, (int32_t)r0, full);
+                        tile_load(to + kCodeStage / 2, &cm, kb * 64, (int32_t)(r0 + (GATED ? a.second : 64)), full);
                     }
                 }
                 const uint64_t t0 = nanoseconds();
-                for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++) mbar_drain(c_full + 8 * (j % kCodeStages), j / kCodeStages & 1, t0);
+                for (uint32_t j = i > kCodeStages ? i - kCodeStages : 0; j < i; j++) mbar_drain(c_full + 8 * (j % kCodeBars), j / kCodeBars & 1, t0);
             }
         }
         if (wid == 3) {
@@ -583,11 +588,11 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         // Row of the block's 128: of a gated matrix the lower half of each warp has rows of the gate.
         const int row = 32 * (wid & 3) + lane, from = GATED ? (lane & 16) * 4 + 16 * (wid & 3) + (lane & 15) : row;
         const uint32_t there = kPair ? of_rank(a_full, leader) : a_full, swizzle = (uint32_t)(from >> 1 & 3);
-        constexpr int kTeams = Shape::kDecodeWarps / 4;  // of four warps, which take turns at the blocks
+        constexpr int kTeams = Shape::kTeams;  // of four warps, which take turns at the blocks
         const int team = (wid - 4) / 4;
         const int64_t total = a.tiles > cluster ? (int64_t)((a.tiles - cluster + clusters - 1) / clusters) * per_tile : 0;  // blocks of all tiles
         const char *codes = smem + kXStages * Shape::kXStage + from * 64;
-        uint32_t w[16], cs = team, c_parity = 0, xs = team, x_parity = 0, as = 2 * team, a_parity = 1, term = team % terms;
+        uint32_t w[16], cs = team, cb = team, c_parity = 0, xs = team, x_parity = 0, as = 2 * team, a_parity = 1, term = team % terms;
         auto step = [](uint32_t &at, uint32_t by, uint32_t stages, uint32_t &parity) {
             at += by;
             if (at >= stages) {
@@ -597,7 +602,7 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
         };
         // The next block's words, in the order of their columns.
         auto fetch = [&] {
-            if (!wait_warp(c_full + 8 * cs, c_parity)) return false;
+            if (!wait_warp(c_full + 8 * cb, c_parity)) return false;
 #pragma unroll
             for (int q = 0; q < 4; q++) {
                 const uint4 four = *reinterpret_cast<const uint4 *>(codes + cs * kCodeStage + ((q ^ swizzle) << 4));
@@ -607,7 +612,8 @@ __global__ void __launch_bounds__(TcShape<ND, NH, GATED, F32>::kThreads, 1) k_pr
             // moved behind an arrival that does not; block 3's codes then took the place of block 0's.)
             __syncwarp();
             if (lane == 0) mbar_arrive_own(c_empty + 8 * cs + ((w[0] ^ w[1] ^ w[2] ^ w[3]) & a.none));
-            step(cs, kTeams, kCodeStages, c_parity);
+            cs = cs + kTeams >= kCodeStages ? cs + kTeams - kCodeStages : cs + kTeams;
+            step(cb, kTeams, kCodeBars, c_parity);
             return true;
         };
         auto decode_half = [&](int half, uint32_t (&pairs)[32]) {

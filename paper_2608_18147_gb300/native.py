@@ -129,6 +129,7 @@ def lib():
                                        vp]),
             "ecasq_workspace_size_project": (sz, [i64, i64, i64, i32]),
             "ecasq_project_plan": (C.c_int, [i64, i64, i64, i32, i32, i32, pi64]),
+            "ecasq_project_rings": (C.c_int, [i32, i32, i32, pi32]),
             "ecasq_project": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, vp, i32, vp, i64, vp, i64,
                                         vp, sz, vp, vp]),
             "ecasq_gated": (C.c_int, [vp, i64, i32, i64, vp, i64, vp, i32, vp, i64, i32, i64, i64, i32, i32, vp, i64, vp, sz, vp,
