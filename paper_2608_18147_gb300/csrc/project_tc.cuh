@@ -70,7 +70,9 @@ template <int ND, int NH, bool GATED, bool F32> struct TcShape {
     // A wait for a barrier's phase ends at once where the phase before it has not ended either, so a warp may wait for a phase only if it knows of the one before.  The warps that decode are teams, which take
     // turns at the blocks: where they would also take turns at a stage of codes, each has barriers of its own for it, whose phases it has all waited for.  (With one barrier a stage a team went on with
     // the codes of three blocks before, and freed the stage for others, when the copy for the other team came later than both copies after it.)  Of a stage of x a team has waited for
-    // its levels' stage before, which was free once the products of the block kAStages / 2 before, and all before them, had been done.
+    // its levels' stage before, which was free once the products of the block kAStages / 2 before, and all before them, had been done.  Of the three buffers of sums of a pair the two parts of a tile's rows of x
+    // take turns too: sums are ready in the order of their products, so a part that has added up those two before knows of those three before.  (Barriers of their own for the parts took
+    // 405 us where 8192 x 8192 by 4096 rows takes 385.)
     static constexpr int kTeams = kDecodeWarps / 4, kCodeBars = kCodeStages % kTeams ? kCodeStages * kTeams : kCodeStages;
     static_assert(kXStages % kTeams == 0 || kXStages >= kAStages / 2, "a team might wait for a phase of a stage of x and not know of the one before");
     static_assert(kAStages / 2 % kTeams == 0, "stages of levels are a team's own");
